@@ -1,0 +1,416 @@
+"""The parts of a training step around the graph layers, as measured cases.
+
+A case names a kind of pass, its sizes and a type:
+
+* ``lookup``  rows of a table of node features by id, scaled (what a server or an evaluation does);
+* ``embed``   the lookup and the gradient of the table (what a training step does);
+* ``norm``    group norm with an activation over rows of channels, forward only;
+* ``norm_train``  the same with the gradients of the rows, weights and biases;
+* ``ortho``   an update (or a stack of them) orthogonalised by five Newton-Schulz steps;
+* ``muon``    one optimiser step of a model's weight matrices: momentum, orthogonalisation, update.
+
+Rows of a norm come in graphs of a batch (``graphs``: ragged, by offsets) or in equal stacks (``maps``).
+Ids outside the table (here -1, padding) stand for no row: zeros, and no gradient.
+"""
+import math
+
+import torch
+
+own = False
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+STEPS = 5
+EPS = 1e-5
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def listed():
+    return [
+        # one node's features for one request: the latency of a call
+        dict(name="lookup_one", kind="lookup", n=1, V=100_000, D=64, dtype="fp32", ids="int64", skew=1.0, pad=0.0),
+        # a large batch of wide rows in 16 bits: the rate of the memory
+        dict(name="lookup_32k_768_bf16", kind="lookup", n=32_768, V=50_000, D=768, dtype="bf16", ids="int64", skew=2.0,
+             pad=0.0),
+        # a small batch of an odd width, as class scores have it; a tenth of it is padding
+        dict(name="embed_777_75", kind="embed", n=777, V=1500, D=75, dtype="fp32", ids="int32", skew=1.0, pad=0.1),
+        # sampled nodes of a power-law graph of 2^20 nodes at the layers' width
+        dict(name="embed_300k_64", kind="embed", n=300_000, V=1 << 20, D=64, dtype="fp32", ids="int32", skew=3.0,
+             pad=0.0),
+        # ids with heavy repeats, wide rows in 16 bits, a width that is no power of two
+        dict(name="embed_16k_1000_fp16", kind="embed", n=16_384, V=50_000, D=1000, dtype="fp16", ids="int64", skew=3.0,
+             pad=0.05),
+        # one small graph: the latency of a call
+        dict(name="norm_one_graph", kind="norm", form="graphs", graphs=1, rows=24, groups=8, C=64, dtype="fp32",
+             act="silu"),
+        # feature maps, channels last, 16 bits
+        dict(name="norm_maps_bf16", kind="norm", form="maps", graphs=16, rows=4096, groups=32, C=320, dtype="bf16",
+             act="silu"),
+        # a training batch of many small graphs (molecules), graphs without a node among them
+        dict(name="norm_molecules_train", kind="norm_train", form="graphs", graphs=20_000, rows=24, groups=8, C=64,
+             dtype="fp32", act="relu"),
+        # one large graph (the road network of the benchmark) between two layers
+        dict(name="norm_road_train", kind="norm_train", form="graphs", graphs=1, rows=2_000_000, groups=4, C=64,
+             dtype="fp32", act="relu"),
+        # the optimiser step of the 5-layer model that the framework trains: ten matrices of 16 x 64 to 64 x 64
+        dict(name="muon_gin_h64", kind="muon", features=16, hidden=64, layers=5, dtype="fp32"),
+        # a stack of updates of an odd size, 32 bits
+        dict(name="ortho_4x1000x333", kind="ortho", batch=4, m=1000, n=333, dtype="fp32"),
+        # the largest: one square update in 16 bits, bound by its products
+        dict(name="ortho_4096_bf16", kind="ortho", batch=1, m=4096, n=4096, dtype="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return math.exp(rng.uniform(math.log(lo), math.log(hi)))
+
+
+def draw(rng):
+    kind = rng.choice(["lookup", "embed", "embed", "norm", "norm_train", "norm_train", "ortho", "ortho", "muon"])
+    if kind in ("lookup", "embed"):
+        D = int(_log(rng, 4, 2048))
+        V = int(_log(rng, 64, min(1 << 20, (1 << 27) / D)))
+        n = int(_log(rng, 1 if kind == "lookup" else 16, min(500_000, (1 << 27) / D)))
+        return dict(kind=kind, n=n, V=V, D=D, dtype=rng.choice(list(TYPES)), ids=rng.choice(["int32", "int64"]),
+                    skew=round(rng.uniform(1.0, 3.0), 2), pad=rng.choice([0.0, 0.1]))
+    if kind in ("norm", "norm_train"):
+        groups = rng.choice([1, 2, 4, 8, 16, 32])
+        C = groups * max(1, int(_log(rng, 1, 64)))
+        form = rng.choice(["graphs", "maps"])
+        n = int(_log(rng, 16, min(2_000_000, (1 << 27) / C)))
+        graphs = max(1, int(_log(rng, 1, min(20_000, n / 8)))) if form == "graphs" else rng.randint(1, min(16, n // 8))
+        return dict(kind=kind, form=form, graphs=graphs, rows=max(1, n // graphs), groups=groups, C=C,
+                    dtype=rng.choice(list(TYPES)), act=rng.choice(["none", "relu", "silu", "gelu"]))
+    if kind == "muon":
+        return dict(kind=kind, features=rng.randint(4, 64), hidden=rng.randint(8, 128), layers=rng.randint(2, 6),
+                    dtype="fp32")
+    m, n = int(_log(rng, 8, 4096)), int(_log(rng, 8, 4096))
+    batch = max(1, min(16, int(_log(rng, 1, 2e10 / (m * n * min(m, n)) + 1.0))))
+    return dict(kind=kind, batch=batch, m=m, n=n, dtype=rng.choice(list(TYPES)))
+
+
+# ------------------------------------------------------------------------------ inputs
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(int(seed))
+
+
+def _normal(g, *shape, dtype=torch.float32):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def _gin_shapes(case):
+    dims = [case["features"]] + [case["hidden"]] * (case["layers"] - 1) + [case["features"]]
+    return [s for a, b in zip(dims, dims[1:]) for s in ((b, a), (b, b))]
+
+
+def _inputs(case, seed):
+    g, kind, dtype = _gen(seed), case["kind"], TYPES[case["dtype"]]
+    if kind in ("lookup", "embed"):
+        n, V, D = case["n"], case["V"], case["D"]
+        # the share of ids below x V is x^(1/skew); which ids are the frequent ones is left to chance
+        u = torch.rand(n, generator=g, device="cuda", dtype=torch.float64)
+        order = torch.randperm(V, generator=g, device="cuda")
+        ids = order[(u ** case["skew"] * V).long().clamp_(max=V - 1)]
+        ids = torch.where(torch.rand(n, generator=g, device="cuda") < case["pad"], torch.full_like(ids, -1), ids)
+        s = dict(ids=ids.to(torch.int32 if case["ids"] == "int32" else torch.int64), table=_normal(g, V, D, dtype=dtype),
+                 scale=math.sqrt(D))
+        if kind == "embed":
+            s["dout"] = _normal(g, n, D, dtype=dtype)
+        return s
+    if kind in ("norm", "norm_train"):
+        B, rows, C = case["graphs"], case["rows"], case["C"]
+        if case["form"] == "maps":
+            n, offsets = B * rows, None
+        elif B == 1:
+            n, offsets = rows, None
+        else:
+            cut = torch.sort(torch.rand(B - 1, generator=g, device="cuda", dtype=torch.float64) * 0.5
+                             + torch.arange(1, B, device="cuda", dtype=torch.float64) - 0.25).values
+            n = B * rows
+            offsets = torch.cat([torch.zeros(1, device="cuda", dtype=torch.int64), (cut * rows).long(),
+                                 torch.full((1,), n, device="cuda", dtype=torch.int64)])
+            if B > 8:  # one graph in eight has lost its nodes to the one before it
+                k = torch.arange(1, B, 8, device="cuda")
+                offsets[k] = offsets[k + 1]
+        X = _normal(g, n, C) * (0.5 + torch.rand(C, generator=g, device="cuda")) + _normal(g, C)
+        X = X.to(dtype)
+        s = dict(X=X.view(B, rows, C) if case["form"] == "maps" else X, offsets=offsets, groups=case["groups"],
+                 act=case["act"], weight=1.0 + 0.2 * _normal(g, C), bias=0.2 * _normal(g, C))
+        if kind == "norm_train":
+            s["dout"] = _normal(g, *s["X"].shape, dtype=dtype)
+        return s
+    if kind == "muon":
+        shapes = _gin_shapes(case)
+        return dict(weights=[_normal(g, *s, dtype=dtype) / math.sqrt(s[1]) for s in shapes],
+                    grads=[_spectrum(g, 1, *s)[0].to(dtype) for s in shapes],
+                    momenta=[_spectrum(g, 1, *s)[0] for s in shapes], lr=0.02, momentum=0.95, weight_decay=0.01)
+    return dict(G=_spectrum(g, case["batch"], case["m"], case["n"]).to(dtype))
+
+
+def _spectrum(g, batch, m, n):
+    """Matrices like gradients: a few strong directions over a wide rest"""
+    k = max(1, min(m, n) // 16)
+    strong = torch.bmm(_normal(g, batch, m, k), _normal(g, batch, k, n)) * (2.0 / math.sqrt(k))
+    return (strong + _normal(g, batch, m, n)) * 1e-3
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s["kind"] = case["kind"]
+    for name in ("table", "X", "weight", "bias"):  # what a training step wants gradients of
+        if name in s and case["kind"] in ("embed", "norm_train"):
+            s[name].requires_grad_()
+    if own and case["kind"] == "muon":  # a program keeps its optimiser
+        from paper_2605_15695_amd.muon import Muon
+
+        s["weights"] = [torch.nn.Parameter(w) for w in s["weights"]]
+        s["optimizer"] = Muon(s["weights"], lr=s["lr"], momentum=s["momentum"], weight_decay=s["weight_decay"])
+        for w, grad, buf in zip(s["weights"], s["grads"], s["momenta"]):
+            w.grad = grad
+            s["optimizer"].state[w]["momentum"] = buf
+    return s
+
+
+# ------------------------------------------------------------------------------ one pass
+def run(s):
+    return (_run_own if own else _run_plain)(s)
+
+
+def _run_own(s):
+    kind = s["kind"]
+    if kind == "lookup":
+        from paper_2605_15695_amd.embedding import embedding
+
+        return embedding(s["ids"], s["table"], s["scale"])
+    if kind == "embed":
+        from paper_2605_15695_amd.embedding import embedding
+
+        out = embedding(s["ids"], s["table"], s["scale"])
+        return [out, *torch.autograd.grad(out, [s["table"]], s["dout"])]
+    if kind in ("norm", "norm_train"):
+        from paper_2605_15695_amd.norm import group_norm
+
+        out = group_norm(s["X"], s["groups"], s["weight"], s["bias"], offsets=s["offsets"], eps=EPS, activation=s["act"])
+        if kind == "norm":
+            return out
+        return [out, *torch.autograd.grad(out, [s["X"], s["weight"], s["bias"]], s["dout"])]
+    if kind == "muon":
+        s["optimizer"].step()
+        return [s["weights"], s["momenta"]]
+    from paper_2605_15695_amd.muon import orthogonalize
+
+    return orthogonalize(s["G"], steps=STEPS, coefficients=COEFFICIENTS)
+
+
+@torch.no_grad()
+def _run_plain(s):
+    kind = s["kind"]
+    if kind == "lookup":
+        return _lookup(s)[0]
+    if kind == "embed":
+        out, ids, ok = _lookup(s)
+        rows = s["dout"].float() * s["scale"]
+        grad = torch.zeros(s["table"].shape, device="cuda").index_add_(0, ids, torch.where(ok[:, None], rows, 0.0))
+        return [out, grad.to(s["table"].dtype)]
+    if kind in ("norm", "norm_train"):
+        return _norm(s)
+    if kind == "muon":
+        return _muon(s)
+    return _newton_schulz(s["G"].float()).to(s["G"].dtype)
+
+
+def _lookup(s):
+    ids = s["ids"].long()
+    ok = (ids >= 0) & (ids < s["table"].shape[0])
+    ids = torch.where(ok, ids, 0)
+    rows = torch.where(ok[:, None], s["table"][ids].float() * s["scale"], 0.0)
+    return rows.to(s["table"].dtype), ids, ok
+
+
+def _norm(s):
+    X, G, act = s["X"], s["groups"], s["act"]
+    C = X.shape[-1]
+    w, b = s["weight"].view(G, C // G), s["bias"].view(G, C // G)
+    offsets = s["offsets"]
+    if offsets is None:  # equal stacks: (B, rows, G, C/G)
+        x = X.float().view(1 if X.dim() == 2 else X.shape[0], -1, G, C // G)
+        count = x.shape[1] * x.shape[3]
+
+        def total(v):
+            return v.sum((1, 3), keepdim=True)
+    else:  # ragged: (n, G, C/G), sums by the rows' graph
+        x = X.float().view(-1, G, C // G)
+        graph = torch.searchsorted(offsets[1:], torch.arange(x.shape[0], device="cuda"), right=True)
+        count = ((offsets[1:] - offsets[:-1])[graph] * (C // G)).view(-1, 1, 1).float()
+
+        def total(v):
+            sums = torch.zeros(offsets.shape[0] - 1, G, device="cuda").index_add_(0, graph, v.sum(2))
+            return sums[graph].unsqueeze(2)
+    x = x - total(x) / count
+    rstd = 1.0 / torch.sqrt(total(x * x) / count + EPS)
+    xhat = x * rstd
+    z = xhat * w + b
+    y, slope = _activation(z, act)
+    y = y.to(X.dtype).view(X.shape)
+    if "dout" not in s:
+        return y
+    dz = s["dout"].float().view(z.shape) * slope
+    rows = dz.dim() - 2
+    dw, db = (dz * xhat).sum(tuple(range(rows))), dz.sum(tuple(range(rows)))
+    dxhat = dz * w
+    dx = rstd * (dxhat - (total(dxhat) + xhat * total(dxhat * xhat)) / count)
+    return [y, dx.to(X.dtype).view(X.shape), dw.view(C), db.view(C)]
+
+
+def _activation(z, act):
+    if act == "relu":
+        return torch.relu(z), (z > 0).float()
+    if act == "silu":
+        p = torch.sigmoid(z)
+        return z * p, p * (1.0 + z * (1.0 - p))
+    if act == "gelu":
+        p = 0.5 * (1.0 + torch.erf(z * math.sqrt(0.5)))
+        return z * p, p + z * torch.exp(-0.5 * z * z) * (1.0 / math.sqrt(2.0 * math.pi))
+    return z, torch.ones_like(z)
+
+
+def _newton_schulz(X):
+    """(batch, m, n) in 32 bits"""
+    a, b, c = COEFFICIENTS
+    flip = X.shape[1] > X.shape[2]
+    if flip:
+        X = X.transpose(1, 2).contiguous()
+    norm = torch.sqrt((X * X).sum((1, 2), keepdim=True))
+    X = X / torch.where(norm > 0, norm, 1.0)
+    for _ in range(STEPS):
+        A = torch.bmm(X, X.transpose(1, 2).contiguous())
+        X = a * X + torch.bmm(b * A + c * torch.bmm(A, A), X)
+    return X.transpose(1, 2).contiguous() if flip else X
+
+
+def _muon(s):
+    """The matrices of one model side by side: rows and columns of zeros change nothing"""
+    lr, mu = s["lr"], s["momentum"]
+    top = max(max(w.shape) for w in s["weights"])
+    stack = [[torch.nn.functional.pad(t.float(), (0, top - t.shape[1], 0, top - t.shape[0])) for t in s[k]]
+             for k in ("weights", "grads", "momenta")]
+    W, grad, buf = (torch.stack(t) for t in stack)
+    buf = mu * buf + grad
+    update = _newton_schulz(grad + mu * buf)
+    size = torch.tensor([math.sqrt(max(1.0, w.shape[0] / w.shape[1])) for w in s["weights"]], device="cuda")
+    W = (1.0 - lr * s["weight_decay"]) * W - lr * size.view(-1, 1, 1) * update
+    return [[w.copy_(v[:w.shape[0], :w.shape[1]]) for w, v in zip(s["weights"], W)],
+            [m.copy_(v[:m.shape[0], :m.shape[1]]) for m, v in zip(s["momenta"], buf)]]
+
+
+# ------------------------------------------------------------------------------ what a pass cannot do without
+def _size(case):
+    return 4 if case["dtype"] == "fp32" else 2
+
+
+def _products(m, n):
+    """Multiply-adds of a step, twice: X X^T and A A are symmetric"""
+    m, n = min(m, n), max(m, n)
+    return 3.0 * m * m * n + 1.0 * m ** 3
+
+
+def work(case):
+    kind, e = case["kind"], _size(case)
+    if kind in ("lookup", "embed"):
+        n, V, D, i = case["n"], case["V"], case["D"], 4 if case["ids"] == "int32" else 8
+        b = n * i + min(n, V) * D * e + n * D * e
+        f = 1.0 * n * D
+        if kind == "embed":
+            b, f = b + n * D * e + V * D * e, f + 2.0 * n * D
+        return {"bytes": b, "flops": f}
+    if kind in ("norm", "norm_train"):
+        x = case["graphs"] * case["rows"] * case["C"]
+        return {"bytes": x * e * (2 if kind == "norm" else 5), "flops": x * (8.0 if kind == "norm" else 24.0)}
+    if kind == "muon":
+        sizes = _gin_shapes(case)
+        return {"bytes": sum(a * b for a, b in sizes) * (e + 2 * e + 8), "flops": STEPS * sum(_products(*s) for s in sizes)}
+    m, n, k = case["m"], case["n"], case["batch"]
+    return {"bytes": 2.0 * k * m * n * e, "flops": STEPS * k * _products(m, n)}
+
+
+# ------------------------------------------------------------------------------ the definitions in 64 bits
+@torch.no_grad()
+def exact(case, seed):
+    s = _inputs(case, seed)
+    kind = case["kind"]
+    if kind in ("lookup", "embed"):
+        V = case["V"]
+        table = torch.cat([s["table"].double() * s["scale"], torch.zeros(1, case["D"], device="cuda", dtype=torch.float64)])
+        ids = torch.where((s["ids"] < 0) | (s["ids"] >= V), V, s["ids"]).long()
+        out = table.index_select(0, ids)
+        if kind == "lookup":
+            return out
+        grad = torch.zeros_like(table).index_put_((ids,), s["dout"].double(), accumulate=True)
+        return [out, grad[:V] * s["scale"]]
+    if kind in ("norm", "norm_train"):
+        return _exact_norm(case, s)
+    if kind == "muon":
+        outs, bufs = [], []
+        for w, g, b in zip(s["weights"], s["grads"], s["momenta"]):
+            b = s["momentum"] * b.double() + g.double()
+            o = _exact_polynomial(g.double() + s["momentum"] * b)
+            gain = max(1.0, w.shape[0] / w.shape[1]) ** 0.5
+            outs.append(w.double() * (1.0 - s["lr"] * s["weight_decay"]) - s["lr"] * gain * o)
+            bufs.append(b)
+        return [outs, bufs]
+    return torch.stack([_exact_polynomial(g) for g in s["G"].double()])
+
+
+def _exact_polynomial(G):
+    """X (a + b X^T X + c (X^T X)^2) five times over, from G over its Frobenius norm, on the smaller side"""
+    X = G / G.norm().clamp_min(1e-300)
+    a, b, c = COEFFICIENTS
+    eye = torch.eye(min(X.shape), device="cuda", dtype=torch.float64)
+    for _ in range(STEPS):
+        if X.shape[0] >= X.shape[1]:
+            S = X.t().contiguous() @ X
+            X = X @ (a * eye + b * S + c * (S @ S))
+        else:
+            S = X @ X.t().contiguous()
+            X = (a * eye + b * S + c * (S @ S)) @ X
+    return X
+
+
+def _exact_norm(case, s):
+    X = s["X"]
+    C, G = case["C"], case["groups"]
+    x = X.double().view(-1, C)
+    B, rows = case["graphs"], case["rows"]
+    if s["offsets"] is None:
+        length = torch.full((B,), x.shape[0] // B, device="cuda", dtype=torch.int64)
+    else:
+        length = s["offsets"].diff()
+    starts = torch.cat([length.new_zeros(1), length.cumsum(0)])
+
+    def over_graphs(v):
+        """(B, G): sums of (n, C) over the rows of a graph and the channels of a group"""
+        v = v.view(-1, G, C // G).sum(2)
+        if s["offsets"] is None:
+            return v.view(B, -1, G).sum(1)
+        c = torch.cat([v.new_zeros(1, G), v.cumsum(0)])
+        return c[starts[1:]] - c[starts[:-1]]
+
+    def spread(v):
+        return v.repeat_interleave(length, 0, output_size=x.shape[0]).repeat_interleave(C // G, 1)
+
+    m = (length.double() * (C // G)).view(-1, 1).clamp_min(1.0)
+    mean = spread(over_graphs(x) / m)
+    rstd = spread((over_graphs((x - mean).square()) / m + EPS).rsqrt())
+    xhat = (x - mean) * rstd
+    w, b = s["weight"].double(), s["bias"].double()
+    z = xhat * w + b
+    with torch.enable_grad():
+        t = z.detach().requires_grad_()
+        y = {"none": lambda v: v * 1.0, "relu": torch.relu, "silu": lambda v: v / (1.0 + torch.exp(-v)),
+             "gelu": lambda v: 0.5 * v * torch.erfc(-v / 2.0 ** 0.5)}[case["act"]](t)
+        slope, = torch.autograd.grad(y.sum(), t)
+    y = y.detach().view(X.shape)
+    if "dout" not in s:
+        return y
+    dz = s["dout"].double().view(-1, C) * slope
+    dx = rstd * (dz * w - spread(over_graphs(dz * w) / m) - xhat * spread(over_graphs(dz * w * xhat) / m))
+    return [y, dx.view(X.shape), (dz * xhat).sum(0), dz.sum(0)]
