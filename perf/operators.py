@@ -41,16 +41,16 @@ def listed():
              pad=0.05),
         # one small graph: the latency of a call
         dict(name="norm_one_graph", kind="norm", form="graphs", graphs=1, rows=24, groups=8, C=64, dtype="fp32",
-             act="silu"),
+             act="relu"),
         # feature maps, channels last, 16 bits
         dict(name="norm_maps_bf16", kind="norm", form="maps", graphs=16, rows=4096, groups=32, C=320, dtype="bf16",
              act="silu"),
         # a training batch of many small graphs (molecules), graphs without a node among them
         dict(name="norm_molecules_train", kind="norm_train", form="graphs", graphs=20_000, rows=24, groups=8, C=64,
-             dtype="fp32", act="relu"),
+             dtype="fp32", act="silu"),
         # one large graph (the road network of the benchmark) between two layers
         dict(name="norm_road_train", kind="norm_train", form="graphs", graphs=1, rows=2_000_000, groups=4, C=64,
-             dtype="fp32", act="relu"),
+             dtype="fp32", act="gelu"),
         # the optimiser step of the 5-layer model that the framework trains: ten matrices of 16 x 64 to 64 x 64
         dict(name="muon_gin_h64", kind="muon", features=16, hidden=64, layers=5, dtype="fp32"),
         # a stack of updates of an odd size, 32 bits
@@ -78,8 +78,10 @@ def draw(rng):
         form = rng.choice(["graphs", "maps"])
         n = int(_log(rng, 16, min(2_000_000, (1 << 27) / C)))
         graphs = max(1, int(_log(rng, 1, min(20_000, n / 8)))) if form == "graphs" else rng.randint(1, min(16, n // 8))
+        # two right sums of one value near 0 can have two signs: gradients are compared where they are continuous
+        act = rng.choice(["none", "silu", "gelu"] + ["relu"] * (kind == "norm"))
         return dict(kind=kind, form=form, graphs=graphs, rows=max(1, n // graphs), groups=groups, C=C,
-                    dtype=rng.choice(list(TYPES)), act=rng.choice(["none", "relu", "silu", "gelu"]))
+                    dtype=rng.choice(list(TYPES)), act=act)
     if kind == "muon":
         return dict(kind=kind, features=rng.randint(4, 64), hidden=rng.randint(8, 128), layers=rng.randint(2, 6),
                     dtype="fp32")
