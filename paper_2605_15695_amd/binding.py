@@ -43,6 +43,15 @@ class pcsr_epilogue_t(ctypes.Structure):
     _fields_ += [("relu", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class pcsr_norm_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("channels", ctypes.c_int64), ("groups", ctypes.c_int64),
+                ("graphs", ctypes.c_int64), ("offsets", ctypes.c_void_p)]
+    _fields_ += [(n, ctypes.c_int32) for n in ("wide", "type", "param_type", "act")]
+    _fields_ += [("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("weight", ctypes.c_void_p),
+                 ("bias", ctypes.c_void_p), ("eps", ctypes.c_float), ("mean", ctypes.c_void_p),
+                 ("rstd", ctypes.c_void_p)]
+
+
 class PcsrError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -103,13 +112,24 @@ def _lib():
         lib.pcsr_gnn_linear_backward.argtypes = [i64, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
         lib.pcsr_gnn_wgrad.argtypes = [i64, i32, i32, vp, vp, vp, vp, vp, vp]
         lib.pcsr_gnn_colsum.argtypes = [i64, i32, vp, vp, vp, vp]
+        f32 = ctypes.c_float
+        lib.pcsr_embed.argtypes = [i64, i64, i64, i32, vp, i32, vp, i64, f32, vp, vp]
+        lib.pcsr_embed_workspace.argtypes = [i64, i64, i64]
+        lib.pcsr_embed_workspace.restype = i64
+        lib.pcsr_embed_backward.argtypes = [i64, i64, i64, i32, vp, i32, vp, i64, f32, vp, vp, vp]
+        pn = ctypes.POINTER(pcsr_norm_t)
+        lib.pcsr_norm_workspace.argtypes = [pn, i32]
+        lib.pcsr_norm_workspace.restype = i64
+        lib.pcsr_norm.argtypes = [pn, vp, vp, vp]
+        lib.pcsr_norm_backward.argtypes = [pn, vp, i64, vp, vp, vp, vp, vp]
         for name in ("pcsr_build", "pcsr_spmm", "pcsr_free", "pcsr_set_kernel_params",
                      "pcsr_query_launch", "pcsr_query_kernel", "pcsr_export", "pcsr_features", "pcsr_select",
                      "pcsr_window_stats", "pcsr_features_device", "pcsr_reorder", "pcsr_permute_csr",
                      "pcsr_transpose_csr", "pcsr_workspace_bytes", "pcsr_reserve_workspace", "pcsr_spmm_static",
                      "pcsr_export_schedule", "pcsr_reorder_by_degree", "pcsr_spmm_epilogue", "pcsr_gnn_linear",
                      "pcsr_gnn_mlp", "pcsr_gnn_mlp_backward", "pcsr_gnn_linear_backward", "pcsr_gnn_wgrad",
-                     "pcsr_gnn_colsum", "pcsr_operator_build", "pcsr_release_cached"):
+                     "pcsr_gnn_colsum", "pcsr_operator_build", "pcsr_release_cached", "pcsr_embed",
+                     "pcsr_embed_backward", "pcsr_norm", "pcsr_norm_backward"):
             getattr(lib, name).restype = ctypes.c_int
         _LIB = lib
     return _LIB
