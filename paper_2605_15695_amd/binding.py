@@ -52,6 +52,18 @@ class pcsr_norm_t(ctypes.Structure):
                  ("rstd", ctypes.c_void_p)]
 
 
+class pcsr_matrix_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("grad", "buf", "out")]
+    _fields_ += [(n, ctypes.c_int64) for n in ("rows", "cols", "grad_ld", "buf_ld", "out_ld")]
+    _fields_ += [("rate", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class pcsr_ortho_t(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("steps", ctypes.c_int32), ("coefficients", ctypes.c_void_p),
+                ("update", ctypes.c_int32), ("nesterov", ctypes.c_int32), ("momentum", ctypes.c_float),
+                ("keep", ctypes.c_float)]
+
+
 class PcsrError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -122,6 +134,10 @@ def _lib():
         lib.pcsr_norm_workspace.restype = i64
         lib.pcsr_norm.argtypes = [pn, vp, vp, vp]
         lib.pcsr_norm_backward.argtypes = [pn, vp, i64, vp, vp, vp, vp, vp]
+        pm, po = ctypes.POINTER(pcsr_matrix_t), ctypes.POINTER(pcsr_ortho_t)
+        lib.pcsr_ortho_workspace.argtypes = [pm, i64, po]
+        lib.pcsr_ortho_workspace.restype = i64
+        lib.pcsr_orthogonalize.argtypes = [pm, i64, po, vp, vp]
         for name in ("pcsr_build", "pcsr_spmm", "pcsr_free", "pcsr_set_kernel_params",
                      "pcsr_query_launch", "pcsr_query_kernel", "pcsr_export", "pcsr_features", "pcsr_select",
                      "pcsr_window_stats", "pcsr_features_device", "pcsr_reorder", "pcsr_permute_csr",
@@ -129,7 +145,7 @@ def _lib():
                      "pcsr_export_schedule", "pcsr_reorder_by_degree", "pcsr_spmm_epilogue", "pcsr_gnn_linear",
                      "pcsr_gnn_mlp", "pcsr_gnn_mlp_backward", "pcsr_gnn_linear_backward", "pcsr_gnn_wgrad",
                      "pcsr_gnn_colsum", "pcsr_operator_build", "pcsr_release_cached", "pcsr_embed",
-                     "pcsr_embed_backward", "pcsr_norm", "pcsr_norm_backward"):
+                     "pcsr_embed_backward", "pcsr_norm", "pcsr_norm_backward", "pcsr_orthogonalize"):
             getattr(lib, name).restype = ctypes.c_int
         _LIB = lib
     return _LIB

@@ -20,7 +20,7 @@ DEVICE = ["--offload-arch=gfx950", "-munsafe-fp-atomics",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 SOURCES = ["pcsr_kernels.hip", "pcsr_build_gpu.hip", "pcsr_gnn.hip", "pcsr_api.cpp", "pcsr_host.cpp", "pcsr_reorder.cpp",
            "pcsr_pool.cpp", "pcsr_window_gpu.hip", "pcsr_relabel_gpu.hip", "pcsr_cluster_gpu.hip",
-           "pcsr_transpose_gpu.hip", "pcsr_embed.hip", "pcsr_norm.hip"]
+           "pcsr_transpose_gpu.hip", "pcsr_embed.hip", "pcsr_norm.hip", "pcsr_ortho.hip"]
 
 
 def _compile(src: str) -> pathlib.Path:

@@ -571,11 +571,6 @@ template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, con
 
 template <typename I> __global__ void __launch_bounds__(kT) fill_kernel(Fill f) { fill(f, blockIdx.x, gridDim.x); }
 
-int launched()
-{
-    return hipGetLastError() == hipSuccess ? PCSR_OK : PCSR_E_HIP;
-}
-
 } // namespace
 } // namespace pcsr
 

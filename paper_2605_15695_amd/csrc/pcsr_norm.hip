@@ -656,11 +656,6 @@ int64_t part_bytes(const pcsr_norm_t &a, const NormPlan &q, bool backward)
     return ((int64_t)q.chunks * kSlots * a.groups * 2 * (backward ? 4 : 8) + 15) / 16 * 16;
 }
 
-int norm_launched()
-{
-    return hipGetLastError() == hipSuccess ? PCSR_OK : PCSR_E_HIP;
-}
-
 } // namespace
 } // namespace pcsr
 
@@ -690,13 +685,10 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
         const size_t stat = sizeof(float) * 2 * (q.cs / p.cpg), lds = sizeof(double) * 2 * q.rpp * (q.one ? q.tpr : q.cs) + stat;
         return for_act(a->act, [&](auto v) {
             constexpr int ACT = decltype(v)::value;
-            if (lds > 64 * 1024 &&
-                hipFuncSetAttribute(reinterpret_cast<const void *>(&norm_kernel<T, ACT>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) !=
-                    hipSuccess)
-                return (int)PCSR_E_HIP;
+            if (!allow_lds(&norm_kernel<T, ACT>, lds)) return (int)PCSR_E_HIP;
             hipLaunchKernelGGL((norm_kernel<T, ACT>), dim3(q.shorts + q.chunks, q.slices), dim3(q.threads), lds, s, p);
             if (q.chunks) hipLaunchKernelGGL((norm_apply_kernel<T, ACT>), dim3(q.chunks, q.slices), dim3(q.threads), stat, s, p);
-            return norm_launched();
+            return launched();
         });
     });
 }
@@ -714,7 +706,7 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
     const unsigned columns = (unsigned)((2 * a->channels + 31) / 32);
     if (a->rows == 0) {
         if (sums) hipLaunchKernelGGL(norm_params_kernel, dim3(columns), dim3(1024), 0, s, nullptr, 0, a->channels, dweight, dbias, a->param_type);
-        return norm_launched();
+        return launched();
     }
     return for_type(a->type, [&](auto t) {
         typedef decltype(t) T;
@@ -728,16 +720,13 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
         const size_t lds = sums && col > first ? col : first;
         return for_act(a->act, [&](auto v) {
             constexpr int ACT = decltype(v)::value;
-            if (lds > 64 * 1024 &&
-                hipFuncSetAttribute(reinterpret_cast<const void *>(&norm_backward_kernel<T, ACT>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                    160 * 1024) != hipSuccess)
-                return (int)PCSR_E_HIP;
+            if (!allow_lds(&norm_backward_kernel<T, ACT>, lds)) return (int)PCSR_E_HIP;
             hipLaunchKernelGGL((norm_backward_kernel<T, ACT>), dim3(q.shorts + q.chunks, q.slices), dim3(q.threads), lds, s, p);
             if (q.chunks && dx) hipLaunchKernelGGL((norm_dx_kernel<T, ACT>), dim3(q.chunks, q.slices), dim3(q.threads), stat, s, p);
             if (sums)
                 hipLaunchKernelGGL(norm_params_kernel, dim3(columns), dim3(1024), 0, s, p.sums, (int64_t)q.shorts + q.chunks, a->channels, dweight, dbias,
                                    a->param_type);
-            return norm_launched();
+            return launched();
         });
     });
 }

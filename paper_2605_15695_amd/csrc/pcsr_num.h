@@ -61,6 +61,16 @@ template <typename T, int N> __device__ __forceinline__ void store_upto(T *p, in
         store_some<T, N>(p, m, x);
 }
 
+// Lets a kernel have so much LDS beside what it declares; more than 64 KB have to be asked for.
+template <typename K> bool allow_lds(K *kernel, size_t bytes)
+{
+    if (bytes <= 64 * 1024) return true;
+    const bool ok = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+    if (!ok) (void)hipGetLastError(); // the caller reports it: not the next call's
+    return ok;
+}
+inline int launched() { return hipGetLastError() == hipSuccess ? PCSR_OK : PCSR_E_HIP; }
+
 // f(a number of the type that `type` names), for kernels that are made for each
 template <typename F> int for_type(int type, F f)
 {

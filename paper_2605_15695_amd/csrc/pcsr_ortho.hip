@@ -1,0 +1,687 @@
+// Updates of weight matrices orthogonalised by Newton-Schulz products (see pcsr_train.h).
+//
+// X <- a X + (b A + c A A) X with A = X X^T, X the update over its Frobenius norm, turned so that it is m x n with m <= n.  Every singular
+// value s of X becomes a s + b s^3 + c s^5; singular vectors stay.
+//
+// Products run on the fp16 matrix instructions, 16 times the rate of the fp32 ones, summed in fp32.  Operands of fp32 and fp16 matrices
+// and of small matrices are two fp16 numbers each, h + l = x to 2^-23 of it, and a product is h h + h l + l h (the last, l l, is below 2^-22):
+// three instructions, 5 times the fp32 rate.  Operands of bf16 matrices with sides from kOnePiece are one fp16 number: 2^-12 of rounding, an eighth of what the result is
+// rounded by in the end.  X itself is held in fp32 from step to step (a X and the sum are fp32), so that what is rounded are the
+// operands of the products alone: directions of small singular values, which a step makes 3.4 times as large, keep their bits.
+// fp16 ends at 65504 and loses bits below 2^-14: the planes hold numbers times a power of two that the host finds from how
+// large singular values can be in that step: (X0 has norm 1, then the polynomial's maximum over the range).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <type_traits>
+
+#include "pcsr_num.h"
+
+namespace pcsr {
+namespace {
+
+typedef half_t h8 __attribute__((ext_vector_type(8)));
+typedef half_t h4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kItems = 24;  // matrices of a launch
+constexpr int kSteps = PCSR_ORTHO_STEPS;
+constexpr int kSmall = 128; // widest side of a matrix that one workgroup takes whole
+constexpr int kT = 256;
+
+struct Item {
+    const void *grad;
+    float *buf;
+    void *out;
+    int rows, cols;
+    int64_t grad_ld, buf_ld, out_ld;
+    float rate;
+    int flip; // X is the transpose
+};
+struct Items {
+    Item item[kItems];
+    int update, nesterov;
+    float momentum, keep;
+};
+
+// the update's number at (r, c) of the matrix; buf is written
+template <typename T> __device__ __forceinline__ float take(const Items &q, const Item &it, int r, int c, bool write)
+{
+    const float g = (float)static_cast<const T *>(it.grad)[r * it.grad_ld + c];
+    if (!it.buf) return g;
+    float *at = it.buf + r * it.buf_ld + c;
+    float b = *at;
+    if (write) {
+        b = q.momentum * b + g;
+        *at = b;
+    }
+    return q.nesterov ? g + q.momentum * b : b;
+}
+template <typename T> __device__ __forceinline__ void give(const Items &q, const Item &it, int r, int c, float v)
+{
+    T *at = static_cast<T *>(it.out) + r * it.out_ld + c;
+    *at = (T)(q.update ? q.keep * (float)*at - it.rate * v : v);
+}
+
+// what one step multiplies with, and the powers of two in the planes it reads and writes
+struct Step {
+    float a, b, c;
+    float x, over_xx, A, over_AA, B, over_Bx, next; // of X, 1 / (of X X), of A, 1 / (A A), of B, 1 / (B X), of the X that comes out
+};
+
+// ---------------------------------------------------------------------------------- small matrices
+// One workgroup of 16 wavefronts to a matrix, everything in LDS (two pieces whatever the type, which costs little here): bound by the latency of fifteen dependent products, so no wavefront has more
+// than Q x Q tiles of 16 x 16.  X's planes make room for A's and B's, X transposed stays beside them, X in fp32 is in registers.
+struct SmallArgs {
+    Items q;
+    Step step[kSteps];
+    int steps;
+};
+
+// 16x16x32: lane l holds A[i = l % 16][k = 8 (l / 16) ..] and B[k][j = l % 16] likewise; D[i = 4 (l / 16) + r][j = l % 16]
+template <int Q> struct Tiles {
+    f4 v[Q][Q];
+    __device__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+#pragma unroll
+            for (int j = 0; j < Q; ++j) v[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+};
+constexpr int kP = 2; // pieces
+template <int S> struct SmallPlanes {
+    static constexpr int LD = S + 8; // rows 16 bytes apart in the banks
+    half_t p[kP][S][LD];
+};
+
+// sums over k of p[i][k] q[j][k]
+template <int Q, int S>
+__device__ __forceinline__ void small_product(const SmallPlanes<S> &p, const SmallPlanes<S> &q, int K, int wr, int wc, int lane,
+                                              int rows, int cols, Tiles<Q> &out)
+{
+    Tiles<Q> low;
+    out.zero();
+    low.zero();
+    if (wr * Q * 16 >= rows || wc * Q * 16 >= cols) return;
+    const int i = lane & 15, k0 = (lane >> 4) * 8;
+    for (int k = 0; k < K; k += 32) {
+        h8 a[Q][kP], b[Q][kP];
+#pragma unroll
+        for (int t = 0; t < Q; ++t)
+#pragma unroll
+            for (int o = 0; o < kP; ++o) {
+                a[t][o] = *reinterpret_cast<const h8 *>(&p.p[o][(wr * Q + t) * 16 + i][k + k0]);
+                b[t][o] = *reinterpret_cast<const h8 *>(&q.p[o][(wc * Q + t) * 16 + i][k + k0]);
+            }
+#pragma unroll
+        for (int r = 0; r < Q; ++r)
+#pragma unroll
+            for (int c = 0; c < Q; ++c) {
+                low.v[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[r][1], b[c][0], low.v[r][c], 0, 0, 0);
+                low.v[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[r][0], b[c][1], low.v[r][c], 0, 0, 0);
+                out.v[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[r][0], b[c][0], out.v[r][c], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < Q; ++r)
+#pragma unroll
+        for (int c = 0; c < Q; ++c) out.v[r][c] += low.v[r][c];
+}
+
+// a number times the plane's power of two, in P pieces
+template <int P> __device__ __forceinline__ void pieces(float x, half_t (&h)[P])
+{
+    h[0] = (half_t)x;
+    if (P == 2) h[1 % P] = (half_t)(x - (float)h[0]);
+}
+
+// tiles into planes, as they are and transposed (where TURN)
+template <int Q, int S, bool ROWS, bool TURN>
+__device__ __forceinline__ void small_put(const Tiles<Q> &v, float scale, int wr, int wc, int lane, SmallPlanes<S> *rows, SmallPlanes<S> *turned)
+{
+#pragma unroll
+    for (int r = 0; r < Q; ++r)
+#pragma unroll
+        for (int c = 0; c < Q; ++c) {
+            const int i = (wr * Q + r) * 16 + (lane >> 4) * 4, j = (wc * Q + c) * 16 + (lane & 15);
+            half_t h[4][kP];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pieces<kP>(v.v[r][c][e] * scale, h[e]);
+#pragma unroll
+            for (int o = 0; o < kP; ++o) {
+                if (ROWS)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rows->p[o][i + e][j] = h[e][o];
+                if (TURN) *reinterpret_cast<h4 *>(&turned->p[o][j][i]) = h4{h[0][o], h[1][o], h[2][o], h[3][o]};
+            }
+        }
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+template <typename T, int Q> __global__ void __launch_bounds__(1024) small_kernel(SmallArgs a)
+{
+    constexpr int S = 64 * Q;
+    extern __shared__ char memory[];
+    __shared__ double part[16];
+    typedef SmallPlanes<S> Planes;
+    Planes &first = *reinterpret_cast<Planes *>(memory), &turned = *reinterpret_cast<Planes *>(memory + sizeof(Planes));
+    const Item &it = a.q.item[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave >> 2, wc = wave & 3;
+    const int m = it.flip ? it.cols : it.rows, n = it.flip ? it.rows : it.cols;
+    Tiles<Q> X, A;
+    double sum = 0.0;
+#pragma unroll
+    for (int r = 0; r < Q; ++r)
+#pragma unroll
+        for (int c = 0; c < Q; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = (wr * Q + r) * 16 + (lane >> 4) * 4 + e, j = (wc * Q + c) * 16 + (lane & 15);
+                float v = 0.0f;
+                if (i < m && j < n) v = it.flip ? take<T>(a.q, it, j, i, true) : take<T>(a.q, it, i, j, true);
+                X.v[r][c][e] = v;
+                sum += (double)v * (double)v;
+            }
+    sum = wave_sum(sum);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += part[w];
+    const double over = sum == 0.0 ? 0.0 : 1.0 / sqrt(sum); // in 64 bits: squares of fp32 neither overflow nor vanish
+#pragma unroll
+    for (int r = 0; r < Q; ++r)
+#pragma unroll
+        for (int c = 0; c < Q; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) X.v[r][c][e] = (float)((double)X.v[r][c][e] * over);
+    for (int s = 0; s < a.steps; ++s) {
+        const Step &st = a.step[s];
+        small_put<Q, S, true, true>(X, st.x, wr, wc, lane, &first, &turned);
+        __syncthreads();
+        small_product<Q, S>(first, first, n, wr, wc, lane, m, m, A);
+#pragma unroll
+        for (int r = 0; r < Q; ++r)
+#pragma unroll
+            for (int c = 0; c < Q; ++c) A.v[r][c] *= st.over_xx;
+        __syncthreads();
+        small_put<Q, S, false, true>(A, st.A, wr, wc, lane, nullptr, &first); // symmetric
+        __syncthreads();
+        Tiles<Q> B;
+        small_product<Q, S>(first, first, m, wr, wc, lane, m, m, B);
+#pragma unroll
+        for (int r = 0; r < Q; ++r)
+#pragma unroll
+            for (int c = 0; c < Q; ++c) B.v[r][c] = st.b * A.v[r][c] + st.c * st.over_AA * B.v[r][c];
+        __syncthreads();
+        small_put<Q, S, false, true>(B, st.B, wr, wc, lane, nullptr, &first);
+        __syncthreads();
+        small_product<Q, S>(first, turned, m, wr, wc, lane, m, n, A);
+#pragma unroll
+        for (int r = 0; r < Q; ++r)
+#pragma unroll
+            for (int c = 0; c < Q; ++c) X.v[r][c] = st.a * X.v[r][c] + st.over_Bx * A.v[r][c];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < Q; ++r)
+#pragma unroll
+        for (int c = 0; c < Q; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = (wr * Q + r) * 16 + (lane >> 4) * 4 + e, j = (wc * Q + c) * 16 + (lane & 15);
+                if (i < m && j < n) {
+                    if (it.flip) give<T>(a.q, it, j, i, X.v[r][c][e]);
+                    else give<T>(a.q, it, i, j, X.v[r][c][e]);
+                }
+            }
+}
+
+// ---------------------------------------------------------------------------------- large matrices
+// Sides padded with zeros to whole tiles.  Planes of a matrix, one after the other (P of each): X [Mp][Np], its transpose twice (one is
+// read while the other is written), A, B; then X and A in fp32.
+struct Space {
+    int64_t Mp, Np, x, t[2], A, B, xf, Af, bytes; // bytes of a matrix
+    Space(int64_t m, int64_t n, int tile, int P)
+    {
+        Mp = (m + tile - 1) / tile * tile, Np = (n + tile - 1) / tile * tile;
+        int64_t at = 0;
+        auto room = [&](int64_t b) { const int64_t o = at; at += b; return o; };
+        x = room(2 * P * Mp * Np), t[0] = room(2 * P * Mp * Np), t[1] = room(2 * P * Mp * Np), A = room(2 * P * Mp * Mp), B = room(2 * P * Mp * Mp);
+        xf = room(4 * Mp * Np), Af = room(4 * Mp * Mp);
+        bytes = at;
+    }
+};
+constexpr int kNormBlocks = 256; // partial sums of a matrix's squares
+
+template <typename T> __global__ void __launch_bounds__(kT) measure_kernel(Items q, double *sums)
+{
+    __shared__ double part[kT / 64];
+    const Item &it = q.item[blockIdx.y];
+    const int64_t all = (int64_t)it.rows * it.cols;
+    double sum = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * kT + threadIdx.x; i < all; i += (int64_t)gridDim.x * kT) {
+        const int r = (int)(i / it.cols), c = (int)(i - (int64_t)r * it.cols);
+        const double v = take<T>(q, it, r, c, true);
+        sum += v * v;
+    }
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) sums[blockIdx.y * kNormBlocks + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+}
+
+// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup
+template <typename T, int P> __global__ void __launch_bounds__(kT) pack_kernel(Items q, const double *sums, int blocks, char *ws, Space sp, float scale)
+{
+    __shared__ float tile[32][33];
+    const Item &it = q.item[blockIdx.z];
+    char *base = ws + blockIdx.z * sp.bytes;
+    double sum = 0.0;
+    for (int k = threadIdx.x & 63; k < blocks; k += 64) sum += sums[blockIdx.z * kNormBlocks + k];
+    sum = wave_sum(sum);
+    const double over = sum == 0.0 ? 0.0 : 1.0 / sqrt(sum);
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t i0 = (int64_t)blockIdx.y * 32, j0 = (int64_t)blockIdx.x * 32; // of X
+    for (int k = ty; k < 32; k += 8) { // rows of the matrix, as they lie
+        const int64_t r = (it.flip ? j0 : i0) + k, c = (it.flip ? i0 : j0) + tx;
+        float v = 0.0f;
+        if (r < it.rows && c < it.cols) v = (float)((double)take<T>(q, it, (int)r, (int)c, false) * over);
+        tile[k][tx] = v;
+    }
+    __syncthreads();
+    half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[0]);
+    float *xf = reinterpret_cast<float *>(base + sp.xf);
+    const int64_t plane = sp.Mp * sp.Np;
+    for (int k = ty; k < 32; k += 8) {
+        const float v = it.flip ? tile[tx][k] : tile[k][tx], w = it.flip ? tile[k][tx] : tile[tx][k]; // X[i0 + k][j0 + tx], X[i0 + tx][j0 + k]
+        half_t hv[P], hw[P];
+        pieces<P>(v * scale, hv);
+        pieces<P>(w * scale, hw);
+        xf[(i0 + k) * sp.Np + j0 + tx] = v;
+#pragma unroll
+        for (int o = 0; o < P; ++o) {
+            x[o * plane + (i0 + k) * sp.Np + j0 + tx] = hv[o];
+            t[o * plane + (j0 + k) * sp.Mp + i0 + tx] = hw[o];
+        }
+    }
+}
+
+// Products D[i][j] = sum over k of p[i][k] q[j][k], rows of both contiguous in k.
+enum { MAKE_A, MAKE_B, MAKE_X, LAST_X }; // A = X X^T; B = b A + c A A; X <- a X + B X; the last one
+struct ProductArgs {
+    char *ws;
+    Space sp;
+    Step st;
+    int64_t K;
+    int tiles_i; // of D; symmetric: the tiles with i >= j
+    int turn;    // which of the transposes is read
+};
+
+// 256 threads, 2 x 2 wavefronts of F x F tiles of 32 x 32.  Numbers go from memory to registers while the stage before is multiplied, then to LDS: two
+// stages of 128 bytes of every row (both pieces).  16-byte chunks of a row are exchanged by its number, so that the 16 rows
+// that a quarter of a wavefront reads lie in different banks.
+// 32x32x16: lane l holds A[i = l % 32][k = 8 (l / 32) ..], B[k][j = l % 32] likewise; D[i = 8 (r / 4) + 4 (l / 32) + r % 4][j = l % 32].
+template <typename T, int F, int P, int MODE> __global__ void __launch_bounds__(kT, 2) product_kernel(ProductArgs a, Items items)
+{
+    constexpr int TILE = 64 * F, BK = 64 / P, CH = BK / 8, ROT = 16 / CH, LOADS = TILE * CH / kT * P; // per operand and thread
+    static_assert(TILE * CH % kT == 0, "whole loads");
+    __shared__ h8 lds[2][2][P][TILE * CH];
+    const Space &sp = a.sp;
+    char *base = a.ws + blockIdx.y * sp.bytes;
+    int ti, tj;
+    {
+        const int all = gridDim.x, per = all / 8, bid = blockIdx.x;
+        // workgroups are dealt to the 8 dies one by one: neighbouring tiles to one of them
+        const int t = bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
+        if (MODE == MAKE_A || MODE == MAKE_B) {
+            ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+            while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
+            while (ti * (ti + 1) / 2 > t) --ti;
+            tj = t - ti * (ti + 1) / 2;
+        } else {
+            ti = t % a.tiles_i, tj = t / a.tiles_i;
+        }
+    }
+    const int64_t Kp = a.K; // also the distance of rows of both operands
+    const half_t *p, *q;
+    int64_t p_plane, q_plane;
+    if (MODE == MAKE_A) p = q = reinterpret_cast<const half_t *>(base + sp.x), p_plane = q_plane = sp.Mp * sp.Np;
+    else if (MODE == MAKE_B) p = q = reinterpret_cast<const half_t *>(base + sp.A), p_plane = q_plane = sp.Mp * sp.Mp;
+    else p = reinterpret_cast<const half_t *>(base + sp.B), q = reinterpret_cast<const half_t *>(base + sp.t[a.turn]), p_plane = sp.Mp * sp.Mp, q_plane = sp.Mp * sp.Np;
+    p += (int64_t)ti * TILE * Kp;
+    q += (int64_t)tj * TILE * Kp;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave >> 1, wc = wave & 1;
+    f16v acc[F][F], low[F][F];
+#pragma unroll
+    for (int r = 0; r < F; ++r)
+#pragma unroll
+        for (int c = 0; c < F; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[r][c][e] = low[r][c][e] = 0.0f;
+    h8 pv[LOADS], qv[LOADS];
+    constexpr int ROUNDS = LOADS / P;
+    auto fetch = [&](int64_t k) {
+#pragma unroll
+        for (int o = 0; o < P; ++o)
+#pragma unroll
+            for (int u = 0; u < ROUNDS; ++u) {
+                const int id = tid + u * kT, row = id / CH, c = id % CH;
+                pv[o * ROUNDS + u] = *reinterpret_cast<const h8 *>(p + o * p_plane + row * Kp + k + c * 8);
+                qv[o * ROUNDS + u] = *reinterpret_cast<const h8 *>(q + o * q_plane + row * Kp + k + c * 8);
+            }
+    };
+    auto stage = [&](int s) {
+#pragma unroll
+        for (int o = 0; o < P; ++o)
+#pragma unroll
+            for (int u = 0; u < ROUNDS; ++u) {
+                const int id = tid + u * kT, row = id / CH, c = id % CH, at = row * CH + (c ^ (row / ROT % CH));
+                lds[s][0][o][at] = pv[o * ROUNDS + u];
+                lds[s][1][o][at] = qv[o * ROUNDS + u];
+            }
+    };
+    const int i = lane & 31, half = lane >> 5;
+    auto multiply = [&](int s) {
+#pragma unroll
+        for (int kk = 0; kk < BK / 16; ++kk) {
+            h8 x[F][P], y[F][P];
+#pragma unroll
+            for (int f = 0; f < F; ++f)
+#pragma unroll
+                for (int o = 0; o < P; ++o) {
+                    const int c = kk * 2 + half, r0 = (wr * F + f) * 32 + i, r1 = (wc * F + f) * 32 + i;
+                    x[f][o] = lds[s][0][o][r0 * CH + (c ^ (r0 / ROT % CH))];
+                    y[f][o] = lds[s][1][o][r1 * CH + (c ^ (r1 / ROT % CH))];
+                }
+#pragma unroll
+            for (int r = 0; r < F; ++r)
+#pragma unroll
+                for (int c = 0; c < F; ++c) {
+                    if (P == 2) {
+                        low[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][1 % P], y[c][0], low[r][c], 0, 0, 0);
+                        low[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][1 % P], low[r][c], 0, 0, 0);
+                    }
+                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][0], acc[r][c], 0, 0, 0);
+                }
+        }
+    };
+    fetch(0);
+    stage(0);
+    __syncthreads();
+    const int steps = (int)(Kp / BK);
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) fetch((int64_t)(s + 1) * BK);
+        multiply(s & 1);
+        if (s + 1 < steps) stage((s + 1) & 1); // read last before the barrier behind it
+        __syncthreads();
+    }
+    if (P == 2) {
+#pragma unroll
+        for (int r = 0; r < F; ++r)
+#pragma unroll
+            for (int c = 0; c < F; ++c) acc[r][c] += low[r][c];
+    }
+    const Step &st = a.st;
+    const int64_t i0 = (int64_t)ti * TILE + wr * F * 32 + half * 4, j0 = (int64_t)tj * TILE + wc * F * 32 + i;
+#pragma unroll
+    for (int r = 0; r < F; ++r)
+#pragma unroll
+        for (int c = 0; c < F; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { // four rows in a row
+                const int64_t ii = i0 + r * 32 + e * 8, jj = j0 + c * 32;
+                f4 v = {acc[r][c][e * 4], acc[r][c][e * 4 + 1], acc[r][c][e * 4 + 2], acc[r][c][e * 4 + 3]};
+                if (MODE == MAKE_A || MODE == MAKE_B) {
+                    float *Af = reinterpret_cast<float *>(base + sp.Af);
+                    half_t *out = reinterpret_cast<half_t *>(base + (MODE == MAKE_A ? sp.A : sp.B));
+                    const int64_t plane = sp.Mp * sp.Mp;
+                    if (MODE == MAKE_A) {
+                        v *= st.over_xx;
+                        *reinterpret_cast<f4 *>(Af + jj * sp.Mp + ii) = v; // only its lower half by rows is read: A[j][i], i >= j
+                    } else {
+                        v = st.b * *reinterpret_cast<const f4 *>(Af + jj * sp.Mp + ii) + st.c * st.over_AA * v;
+                    }
+                    h4 h[P];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        half_t t[P];
+                        pieces<P>(v[k] * (MODE == MAKE_A ? st.A : st.B), t);
+#pragma unroll
+                        for (int o = 0; o < P; ++o) h[o][k] = t[o];
+                    }
+#pragma unroll
+                    for (int o = 0; o < P; ++o) {
+                        *reinterpret_cast<h4 *>(out + o * plane + jj * sp.Mp + ii) = h[o];
+                        if (ti != tj)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) out[o * plane + (ii + k) * sp.Mp + jj] = h[o][k];
+                    }
+                } else {
+                    float *xf = reinterpret_cast<float *>(base + sp.xf);
+                    const int64_t plane = sp.Mp * sp.Np;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = st.a * xf[(ii + k) * sp.Np + jj] + st.over_Bx * v[k];
+                    if (MODE == LAST_X) {
+                        const Item &it = items.item[blockIdx.y];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int row = (int)(it.flip ? jj : ii + k), col = (int)(it.flip ? ii + k : jj);
+                            if (row < it.rows && col < it.cols) give<T>(items, it, row, col, v[k]);
+                        }
+                    } else {
+                        half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[1 - a.turn]);
+                        h4 h[P];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            xf[(ii + k) * sp.Np + jj] = v[k];
+                            half_t s[P];
+                            pieces<P>(v[k] * st.next, s);
+#pragma unroll
+                            for (int o = 0; o < P; ++o) {
+                                x[o * plane + (ii + k) * sp.Np + jj] = s[o];
+                                h[o][k] = s[o];
+                            }
+                        }
+#pragma unroll
+                        for (int o = 0; o < P; ++o) *reinterpret_cast<h4 *>(t + o * plane + jj * sp.Mp + ii) = h[o];
+                    }
+                }
+            }
+}
+
+// ---------------------------------------------------------------------------------- host
+float power_below(double bound) // the power of two that takes numbers up to `bound` to 32768 at most, 2^14 at most
+{
+    int e = 14;
+    if (bound > 0.0) {
+        const int up = 15 - (int)std::ceil(std::log2(bound));
+        e = up < e ? up : e;
+    }
+    return (float)std::ldexp(1.0, e);
+}
+
+// Powers of two of every step, from the largest singular value that can occur: X0's is 1 at most.  false: they leave fp32's range.
+bool plan_steps(const pcsr_ortho_t &how, Step *out)
+{
+    double s = 1.0;
+    constexpr int N = 4096;
+    float x = power_below(s * 1.01);
+    for (int k = 0; k < how.steps; ++k) {
+        const double a = how.coefficients[3 * k], b = how.coefficients[3 * k + 1], c = how.coefficients[3 * k + 2];
+        double most_B = 0.0, most_x = 0.0;
+        for (int i = 0; i <= N; ++i) {
+            const double v = s * i / N, w = v * v;
+            most_B = std::fmax(most_B, std::fabs(b * w + c * w * w));
+            most_x = std::fmax(most_x, std::fabs(v * (a + b * w + c * w * w)));
+        }
+        if (!(std::isfinite(a) && std::isfinite(b) && std::isfinite(c)) || !(most_x < 0x1p24) || !(most_B < 0x1p100)) return false;
+        Step &st = out[k];
+        st.a = (float)a, st.b = (float)b, st.c = (float)c;
+        st.x = x;
+        st.A = power_below(s * s * 1.01), st.B = power_below(most_B * 1.01);
+        s = most_x * 1.001;
+        st.next = x = power_below(s * 1.01);
+        st.over_xx = 1.0f / st.x / st.x, st.over_AA = 1.0f / st.A / st.A, st.over_Bx = 1.0f / st.B / st.x;
+    }
+    return true;
+}
+
+bool is_small(const pcsr_matrix_t &m) { return m.rows <= kSmall && m.cols <= kSmall; }
+// One piece only where roundings of many directions average out: a single direction of a bf16 matrix was off by 1.1 times its result's own
+// rounding (129 x 5).
+constexpr int kOnePiece = 256;
+int pieces_of(int type, int64_t m) { return type == PCSR_BF16 && m >= kOnePiece ? 1 : 2; }
+
+// tiles of 128 where there are enough of them for the compute units, of 64 otherwise
+int tile_of(int64_t m, int64_t n, int64_t count)
+{
+    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128) * count;
+    return tiles >= 192 ? 128 : 64;
+}
+
+// the matrices from `first` on that go with it in one launch
+int64_t group_of(const pcsr_matrix_t *m, int64_t count, int64_t first, const char *done, int64_t *members)
+{
+    int64_t n = 0;
+    const bool small = is_small(m[first]);
+    const auto wide = [](const pcsr_matrix_t &x) { return x.rows > 64 || x.cols > 64; };
+    for (int64_t k = first; k < count && n < kItems; ++k) {
+        if (done && done[k]) continue;
+        if (small ? is_small(m[k]) && wide(m[k]) == wide(m[first]) : m[k].rows == m[first].rows && m[k].cols == m[first].cols) members[n++] = k;
+    }
+    return n;
+}
+
+int64_t group_bytes(const pcsr_matrix_t &x, int64_t n, int type)
+{
+    if (is_small(x)) return 0;
+    const int64_t m = x.rows < x.cols ? x.rows : x.cols, w = x.rows < x.cols ? x.cols : x.rows;
+    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, tile_of(m, w, n), pieces_of(type, m)).bytes;
+}
+
+int ortho_check(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t *how)
+{
+    if (count < 0 || (count && !m) || !how || !how->coefficients || how->steps < 1 || how->steps > kSteps) return PCSR_E_INVALID_ARG;
+    if (how->type < PCSR_F32 || how->type > PCSR_F16) return PCSR_E_UNSUPPORTED;
+    for (int64_t k = 0; k < count; ++k) {
+        const pcsr_matrix_t &x = m[k];
+        if (x.rows < 0 || x.cols < 0) return PCSR_E_INVALID_ARG;
+        if (x.rows == 0 || x.cols == 0) continue;
+        if (!x.grad || !x.out || x.grad_ld < x.cols || x.out_ld < x.cols || (x.buf && x.buf_ld < x.cols)) return PCSR_E_INVALID_ARG;
+        if (x.rows > (1 << 17) || x.cols > (1 << 17) || x.rows * x.cols > int64_t(1) << 32) return PCSR_E_TOO_LARGE;
+    }
+    return PCSR_OK;
+}
+
+template <typename T, int Q> int run_small(const SmallArgs &a, int n, hipStream_t s)
+{
+    const size_t lds = 2 * sizeof(SmallPlanes<64 * Q>);
+    if (!allow_lds(&small_kernel<T, Q>, lds)) return PCSR_E_HIP;
+    hipLaunchKernelGGL((small_kernel<T, Q>), dim3(n), dim3(1024), lds, s, a);
+    return PCSR_OK;
+}
+
+template <typename T, int F, int P> void run_large(const Items &q, int n, const Step *step, int steps, char *ws, hipStream_t s)
+{
+    constexpr int TILE = 64 * F;
+    const Item &it = q.item[0];
+    const int64_t m = it.flip ? it.cols : it.rows, w = it.flip ? it.rows : it.cols;
+    const Space sp(m, w, TILE, P);
+    double *sums = reinterpret_cast<double *>(ws);
+    ws += kItems * kNormBlocks * sizeof(double);
+    const int64_t want = (m * w + kT * 4 - 1) / (kT * 4);
+    const int blocks = (int)(want < kNormBlocks ? want : kNormBlocks);
+    hipLaunchKernelGGL((measure_kernel<T>), dim3(blocks, n), dim3(kT), 0, s, q, sums);
+    hipLaunchKernelGGL((pack_kernel<T, P>), dim3((unsigned)(sp.Np / 32), (unsigned)(sp.Mp / 32), n), dim3(kT), 0, s, q, sums, blocks, ws, sp, step[0].x);
+    const unsigned ti = (unsigned)(sp.Mp / TILE), tj = (unsigned)(sp.Np / TILE), sym = ti * (ti + 1) / 2;
+    for (int k = 0; k < steps; ++k) {
+        ProductArgs a = {ws, sp, step[k], sp.Np, (int)ti, k & 1};
+        hipLaunchKernelGGL((product_kernel<T, F, P, MAKE_A>), dim3(sym, n), dim3(kT), 0, s, a, q);
+        a.K = sp.Mp;
+        hipLaunchKernelGGL((product_kernel<T, F, P, MAKE_B>), dim3(sym, n), dim3(kT), 0, s, a, q);
+        if (k + 1 < steps)
+            hipLaunchKernelGGL((product_kernel<T, F, P, MAKE_X>), dim3(ti * tj, n), dim3(kT), 0, s, a, q);
+        else
+            hipLaunchKernelGGL((product_kernel<T, F, P, LAST_X>), dim3(ti * tj, n), dim3(kT), 0, s, a, q);
+    }
+}
+
+} // namespace
+} // namespace pcsr
+
+using namespace pcsr;
+
+extern "C" {
+
+int64_t pcsr_ortho_workspace(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t *how)
+{
+    if (ortho_check(m, count, how) != PCSR_OK) return 0;
+    int64_t most = 0, members[kItems];
+    for (int64_t k = 0; k < count; ++k) { // a group that starts at any of them is no larger than all that are like it
+        const int64_t n = group_of(m, count, k, nullptr, members);
+        for (int64_t c = 1; c <= n; ++c) { // fewer matrices can mean smaller tiles, but never more memory than counted here
+            const int64_t b = group_bytes(m[k], c, how->type);
+            most = b > most ? b : most;
+        }
+    }
+    return most;
+}
+
+int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t *how, void *ws, void *stream)
+{
+    const int rc = ortho_check(m, count, how);
+    if (rc != PCSR_OK) return rc;
+    SmallArgs a;
+    a.steps = how->steps;
+    if (!plan_steps(*how, a.step)) return PCSR_E_UNSUPPORTED;
+    if (!ws && pcsr_ortho_workspace(m, count, how)) return PCSR_E_INVALID_ARG;
+    a.q.update = how->update, a.q.nesterov = how->nesterov, a.q.momentum = how->momentum, a.q.keep = how->keep;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int64_t members[kItems];
+    // matrices are taken in the order they come, each with those behind it that are like it; `from` marks what is done
+    constexpr int64_t kMost = 4096;
+    if (count > kMost) return PCSR_E_TOO_LARGE;
+    char done[kMost] = {};
+    for (int64_t k = 0; k < count; ++k) {
+        if (done[k]) continue;
+        if (m[k].rows == 0 || m[k].cols == 0) continue;
+        const int64_t n = group_of(m, count, k, done, members);
+        int used = 0;
+        for (int64_t i = 0; i < n; ++i) {
+            const pcsr_matrix_t &x = m[members[i]];
+            done[members[i]] = 1;
+            if (x.rows == 0 || x.cols == 0) continue;
+            a.q.item[used++] = {x.grad, x.buf, x.out, (int)x.rows, (int)x.cols, x.grad_ld, x.buf_ld, x.out_ld, x.rate, x.rows > x.cols};
+        }
+        const int r = for_type(how->type, [&](auto t) {
+            typedef decltype(t) T;
+            if (is_small(m[k])) return m[k].rows > 64 || m[k].cols > 64 ? run_small<T, 2>(a, used, s) : run_small<T, 1>(a, used, s);
+            const int64_t lo = m[k].rows < m[k].cols ? m[k].rows : m[k].cols, hi = m[k].rows < m[k].cols ? m[k].cols : m[k].rows;
+            char *at = static_cast<char *>(ws);
+            const bool wide = tile_of(lo, hi, used) == 128;
+            if constexpr (std::is_same<T, bfloat_t>::value) {
+                if (pieces_of(how->type, lo) == 1) {
+                    if (wide) run_large<T, 2, 1>(a.q, used, a.step, a.steps, at, s);
+                    else run_large<T, 1, 1>(a.q, used, a.step, a.steps, at, s);
+                    return (int)PCSR_OK;
+                }
+            }
+            if (wide) run_large<T, 2, 2>(a.q, used, a.step, a.steps, at, s);
+            else run_large<T, 1, 2>(a.q, used, a.step, a.steps, at, s);
+            return (int)PCSR_OK;
+        });
+        if (r != PCSR_OK) return r;
+    }
+    return launched();
+}
+
+} // extern "C"

@@ -54,4 +54,30 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream);
 // From dy (rows dy_stride numbers apart): dx [rows x channels], dweight and dbias [channels]; each may be null.
 int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, void *dx, void *dweight, void *dbias, void *ws,
                        void *stream);
+
+// ---------------------------------------------------------------------------------- orthogonalised updates (pcsr_ortho.hip)
+// One matrix.  Update U = grad, or with momentum: buf = momentum * buf + grad, U = grad + momentum * buf (nesterov) or buf.
+// O = `steps` times X <- a X + (b A + c A A) X, A = X X^T, from X = U / ||U|| (Frobenius; zeros stay zeros).
+// out = O, or with `update`: out = keep * out - rate * O.  grad and out have `type`, buf is fp32.
+typedef struct {
+    const void *grad;
+    float *buf;         // null: no momentum
+    void *out;
+    int64_t rows, cols;
+    int64_t grad_ld, buf_ld, out_ld; // distance of rows
+    float rate;
+    int32_t reserved;
+} pcsr_matrix_t;
+typedef struct {
+    int32_t type, steps; // steps 0 to PCSR_ORTHO_STEPS
+    const double *coefficients; // host, [steps][3]
+    int32_t update, nesterov;
+    float momentum, keep;
+} pcsr_ortho_t;
+#define PCSR_ORTHO_STEPS 16
+// matrices: host, [count], which may overlap with no other's buf or out.  Products of fp16 numbers added up in fp32: operands are two fp16
+// numbers each (22 bits), of bf16 matrices with 256 rows and columns or more one (11 bits).
+// ws: 16-byte aligned, pcsr_ortho_workspace bytes.  UNSUPPORTED where the coefficients let the numbers grow out of fp32's range.
+int64_t pcsr_ortho_workspace(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how);
+int pcsr_orthogonalize(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how, void *ws, void *stream);
 }
