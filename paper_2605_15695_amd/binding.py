@@ -13,6 +13,7 @@ import numpy as np
 _PKG = pathlib.Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libpcsr.so"
 PY_PATH = _PKG / "_pcsr_py.so"
+TRAIN_PATH = _PKG / "_pcsr_train.so"
 
 PCSR_OK = 0
 PCSR_E_INVALID_ARG, PCSR_E_BAD_CSR, PCSR_E_UNSUPPORTED = -1, -2, -3
@@ -272,24 +273,45 @@ def load_call_module() -> None:
     global _spmm
     if _spmm is not _first_spmm:
         return
+    lib = _lib()
+    mod = _load_module("_pcsr_py", PY_PATH, (lib.pcsr_spmm, lib.pcsr_release_cached_if_low), "pcsr_spmm's calls")
+    _spmm = _spmm_checked if mod is None else mod.spmm
+
+
+def _load_module(name, path, functions, what):
+    """A module of calls on tensors' C++ objects, given the library's functions; None (and a warning) where it is missing
+    or made for another torch."""
     import importlib.util
     import warnings
 
     import torch  # its libraries have to be there
 
-    lib = _lib()
     try:
-        spec = importlib.util.spec_from_file_location("_pcsr_py", PY_PATH)
+        spec = importlib.util.spec_from_file_location(name, path)
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
         if mod.torch_version != str(torch.__version__):
             raise ImportError(f"built for torch {mod.torch_version}")
-        mod.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.pcsr_spmm, lib.pcsr_release_cached_if_low)))
-        _spmm = mod.spmm
+        mod.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in functions))
+        return mod
     except (ImportError, OSError) as e:
-        warnings.warn(f"{PY_PATH.name} does not load ({e}); pcsr_spmm's calls go through ctypes and cost a few "
+        warnings.warn(f"{path.name} does not load ({e}); {what} go through ctypes and cost a few "
                       "microseconds more: build it with `python -m paper_2605_15695_amd.build`", RuntimeWarning)
-        _spmm = _spmm_checked
+        return None
+
+
+_train = False  # not asked for yet
+
+
+def train_module():
+    """The module that makes the calls of embedding.py, norm.py and muon.py without ctypes, or None."""
+    global _train
+    if _train is False:
+        lib = _lib()
+        _train = _load_module("_pcsr_train", TRAIN_PATH, [getattr(lib, "pcsr_" + n) for n in (
+            "embed", "embed_workspace", "embed_backward", "norm", "norm_workspace", "norm_backward", "orthogonalize",
+            "ortho_workspace", "strerror")], "calls of the training step")
+    return _train
 
 
 def _first_spmm(h, B, C, K, stream):

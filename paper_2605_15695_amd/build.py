@@ -12,6 +12,7 @@ OBJ = PKG / "_build"
 LIB = PKG / "libpcsr.so"
 BASELINE_LIB = PKG / "libpcsr_baseline.so"
 PY_LIB = PKG / "_pcsr_py.so"
+TRAIN_LIB = PKG / "_pcsr_train.so"
 
 HIPCC = "/opt/rocm/bin/hipcc"
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-command-line-argument"]
@@ -35,8 +36,8 @@ def _compile(src: str) -> pathlib.Path:
     return obj
 
 
-def _build_py() -> pathlib.Path:
-    """The binding's per-call module: host code against torch's headers, found beside this file."""
+def _build_py(src: str = "pcsr_py.cpp", lib: pathlib.Path = PY_LIB) -> pathlib.Path:
+    """A per-call module of the binding: host code against torch's headers, found beside this file."""
     import sysconfig
 
     import torch
@@ -45,20 +46,21 @@ def _build_py() -> pathlib.Path:
     libdir = pathlib.Path(torch.__file__).parent / "lib"
     inc = [p for p in cpp_extension.include_paths()] + [sysconfig.get_paths()["include"], "/opt/rocm/include"]
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           "-D__HIP_PLATFORM_AMD__=1", f'-DPCSR_TORCH_VERSION="{torch.__version__}"', *[f"-isystem{p}" for p in inc], str(CSRC / "pcsr_py.cpp"), "-o", str(PY_LIB),
-           f"-L{libdir}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", f"-Wl,-rpath,{libdir}"]
+           "-D__HIP_PLATFORM_AMD__=1", f'-DPCSR_TORCH_VERSION="{torch.__version__}"', *[f"-isystem{p}" for p in inc], str(CSRC / src), "-o", str(lib),
+           f"-L{libdir}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_hip", f"-Wl,-rpath,{libdir}"]
     r = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"g++ failed on pcsr_py.cpp:\n{r.stderr}")
-    return PY_LIB
+        raise RuntimeError(f"g++ failed on {src}:\n{r.stderr}")
+    return lib
 
 
 def build(verbose: bool = False) -> pathlib.Path:
     OBJ.mkdir(exist_ok=True)
     with concurrent.futures.ThreadPoolExecutor(max_workers=4) as ex:
-        py = ex.submit(_build_py)
+        py = [ex.submit(_build_py), ex.submit(_build_py, "pcsr_train_py.cpp", TRAIN_LIB)]
         objs = list(ex.map(_compile, SOURCES))
-        py.result()
+        for p in py:
+            p.result()
     cmd = [HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", *map(str, objs), "-o", str(LIB),
            "-lpthread"]
     subprocess.run(cmd, check=True)

@@ -22,6 +22,11 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0) -> tor
     for no row (padding): zeros, and no gradient.  table: (rows, d); rows may lie apart, numbers of a
     row may not (such a table is copied).  The gradient is dense, of the table's type; its sums are
     taken in 32 bits, in an order that the sizes alone decide: the same bits on every run."""
+    fast = pc.train_module()
+    if fast is not None:
+        out = fast.embed(ids, table, scale)
+        if out is not NotImplemented:
+            return out
     if not isinstance(ids, torch.Tensor) or ids.dtype not in (torch.int32, torch.int64):
         raise ValueError("ids must be an int32 or int64 tensor")
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.dtype not in _TYPES or table.shape[1] < 1:

@@ -10,6 +10,7 @@ launch for up to 24 of them, larger ones three per Newton-Schulz step for all of
 from __future__ import annotations
 
 import ctypes
+import math
 
 import torch
 
@@ -61,6 +62,14 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS) ->
     G: (rows, columns) or (matrices, rows, columns) of float32, bfloat16 or float16 on a GPU; any strides.
     coefficients: (a, b, c), or one for each step.  The result has G's type; products are taken of 22 bits of their
     operands (of 11 for bfloat16 matrices with 256 rows and columns or more) and summed in 32; X itself is held in 32."""
+    fast = pc.train_module()
+    if fast is not None and isinstance(steps, int):
+        co = _coefficients(coefficients, steps)
+        out = fast.orthogonalize(G, steps, ctypes.addressof(co))
+        if isinstance(out, int):
+            raise pc.PcsrError(out, "pcsr_orthogonalize")
+        if out is not NotImplemented:
+            return out
     if not isinstance(G, torch.Tensor) or G.dim() not in (2, 3) or G.dtype not in _TYPES or not G.is_cuda:
         raise ValueError("G must be a float32, bfloat16 or float16 CUDA tensor of two or three dimensions")
     co = _coefficients(coefficients, steps)
@@ -115,30 +124,45 @@ class Muon(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for group in self.param_groups:
-            by_type, back = {}, []
-            for p in group["params"]:
-                if p.grad is None or p.numel() == 0:
+            steps, co = group["steps"], _coefficients(group["coefficients"], group["steps"])
+            lr, momentum, keep = float(group["lr"]), float(group["momentum"]), 1.0 - float(group["lr"] * group["weight_decay"])
+            params = [p for p in group["params"] if p.grad is not None and p.numel()]
+            if not params:
+                continue
+            bufs = [self._momentum(p) for p in params]
+            rates = [lr * math.sqrt(max(1.0, p.shape[0] / p.shape[1])) for p in params]
+            fast = pc.train_module()
+            if fast is not None:
+                rc = fast.update(params, bufs, rates, steps, ctypes.addressof(co), group["nesterov"], momentum, keep)
+                if rc is not NotImplemented:
+                    if rc != pc.PCSR_OK:
+                        raise pc.PcsrError(rc, "pcsr_orthogonalize")
                     continue
-                if not p.is_cuda or p.grad.is_sparse or p.grad.dtype != p.dtype:
+            by_type, back = {}, []
+            for p, buf, rate in zip(params, bufs, rates):
+                if not p.is_cuda or p.grad.layout != torch.strided or p.grad.dtype != p.dtype:
                     raise ValueError("Muon steps dense matrices on a GPU, with gradients of their type")
-                state = self.state[p]
-                if "momentum" not in state:
-                    state["momentum"] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
-                buf, grad, out = state["momentum"], p.grad, p.detach()
+                grad, out = p.grad, p.detach()
                 if _ld(grad) is None:
                     grad = grad.contiguous()
                 if _ld(out) is None:
                     out = out.contiguous()
                     back.append((p, out))
-                if buf.shape != p.shape or buf.dtype != torch.float32 or buf.device != p.device or _ld(buf) is None:
-                    state["momentum"] = buf = buf.to(p.device, torch.float32).reshape(p.shape).contiguous()
-                rate = group["lr"] * max(1.0, p.shape[0] / p.shape[1]) ** 0.5
                 by_type.setdefault((p.dtype, p.device), []).append((grad, pc.pcsr_matrix_t(
                     grad.data_ptr(), buf.data_ptr(), out.data_ptr(), *p.shape, _ld(grad), _ld(buf), _ld(out), rate, 0)))
-            co = _coefficients(group["coefficients"], group["steps"])
             for (dtype, device), mats in by_type.items():
-                _run([m for _, m in mats], dtype, device, group["steps"], co, True, group["nesterov"], group["momentum"],
-                     1.0 - group["lr"] * group["weight_decay"])
+                _run([m for _, m in mats], dtype, device, steps, co, True, group["nesterov"], momentum, keep)
             for p, out in back:
                 p.copy_(out)
+            torch.autograd.graph.increment_version(params)
         return loss
+
+    def _momentum(self, p):
+        state = self.state[p]
+        buf = state.get("momentum")
+        if buf is None:
+            buf = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+        elif buf.shape != p.shape or buf.dtype != torch.float32 or buf.device != p.device or _ld(buf) is None:
+            buf = buf.to(p.device, torch.float32).reshape(p.shape).contiguous()
+        state["momentum"] = buf
+        return buf

@@ -30,6 +30,11 @@ def group_norm(X: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     ascend give wrong numbers, never an access outside the arrays.
     weight, bias: (channels,) of one type, float32 or X's.  activation: none, relu, silu or gelu (the exact one).
     Statistics are float32 at least, sums in an order that the sizes alone decide."""
+    fast = pc.train_module()
+    if fast is not None and activation in ACTIVATIONS:
+        out = fast.group_norm(X, groups, weight, bias, offsets, eps, ACTIVATIONS[activation])
+        if out is not NotImplemented:
+            return out
     if not isinstance(X, torch.Tensor) or X.dim() < 2 or X.dtype not in _TYPES or not X.is_cuda:
         raise ValueError("X must be a float32, bfloat16 or float16 CUDA tensor of two dimensions or more")
     C = X.shape[-1]

@@ -63,8 +63,8 @@ def _check(ids, table, dout, scale, kind):
                                    (8200, "one"), (16385, "skewed"), (16384, "outside")])
 def test_against_64_bits(kind, rows, d, n, how):
     g = _gen(n * 31 + rows + d)
-    if n * d > 2 << 20:
-        n = (2 << 20) // d
+    if n * d > 1 << 18:
+        n = (1 << 18) // d
     ids = _ids(g, n, rows, how)
     table = torch.randn(rows, d, generator=g, device="cuda").to(TYPES[kind][0])
     dout = torch.randn(n, d, generator=g, device="cuda").to(TYPES[kind][0])
@@ -202,3 +202,34 @@ def test_module_learns_its_rows():
         assert not bool(emb.weight.grad[1::2].any())
         opt.step()
     assert float(loss) < 1e-3 * first and np.isfinite(first)
+
+
+# the module of calls on C++ objects, and the Python code that stands in for it
+def test_without_the_call_module(monkeypatch):
+    from paper_2605_15695_amd import binding
+    from paper_2605_15695_amd.embedding import embedding
+
+    g = _gen(12)
+    table = torch.randn(300, 40, generator=g, device="cuda").requires_grad_()
+    ids = torch.randint(-3, 303, (4, 90), generator=g, device="cuda")
+    dout = torch.randn(4, 90, 40, generator=g, device="cuda")
+    assert binding.train_module() is not None
+    want = embedding(ids, table, 3.0)
+    grad, = torch.autograd.grad(want, table, dout)
+    monkeypatch.setattr(binding, "_train", None)
+    out = embedding(ids, table, 3.0)
+    assert torch.equal(out, want) and torch.equal(torch.autograd.grad(out, table, dout)[0], grad)
+    monkeypatch.setattr(binding, "_train", False)
+    monkeypatch.setattr(binding, "TRAIN_PATH", binding.TRAIN_PATH.with_name("_no_such_module.so"))
+    with pytest.warns(RuntimeWarning, match="_no_such_module"):
+        assert torch.equal(embedding(ids, table, 3.0), want)
+
+
+def test_gradients_of_gradients_are_refused():
+    from paper_2605_15695_amd.embedding import embedding
+
+    table = torch.randn(10, 4, device="cuda").requires_grad_()
+    out = embedding(torch.tensor([1, 2], device="cuda"), table)
+    grad, = torch.autograd.grad(out.square().sum(), table, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()

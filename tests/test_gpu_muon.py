@@ -265,3 +265,30 @@ def test_a_model_learns():
             o.step()
         losses.append(float(loss.detach()))
     assert losses[-1] < 0.3 * losses[0]
+
+
+# the module of calls on C++ objects, and the Python code that stands in for it
+def test_without_the_call_module(monkeypatch):
+    from paper_2605_15695_amd import binding
+    from paper_2605_15695_amd.muon import Muon, orthogonalize
+
+    assert binding.train_module() is not None
+    g = _gen(13)
+    G = torch.randn(3, 50, 70, generator=g, device="cuda")
+    start = [torch.randn(s, generator=g, device="cuda") for s in ((20, 30), (200, 140))]
+    grads = [torch.randn(p.shape, generator=g, device="cuda") for p in start]
+
+    def run():
+        params = [torch.nn.Parameter(p.clone()) for p in start]
+        opt = Muon(params, lr=0.1)
+        for p, x in zip(params, grads):
+            p.grad = x
+        versions = [p._version for p in params]
+        opt.step()
+        opt.step()
+        assert all(p._version > v for p, v in zip(params, versions))
+        return [p.detach() for p in params] + [orthogonalize(G), orthogonalize(G[1])]
+
+    want = run()
+    monkeypatch.setattr(binding, "_train", None)
+    assert all(torch.equal(a, b) for a, b in zip(run(), want))

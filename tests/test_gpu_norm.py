@@ -319,3 +319,34 @@ def test_module_between_layers():
     assert torch.equal(norm(X, off), group_norm(X, 4, norm.weight, norm.bias, off, activation="relu"))
     norm(X).square().sum().backward()
     assert norm.weight.grad.shape == (32,) and norm.bias.grad.shape == (32,)
+
+
+# the module of calls on C++ objects, and the Python code that stands in for it
+def test_without_the_call_module(monkeypatch):
+    from paper_2605_15695_amd import binding
+    from paper_2605_15695_amd.norm import group_norm
+
+    assert binding.train_module() is not None
+    for lengths, shape in (([40, 0, 60], None), ([50, 50], (2, 50, 24))):
+        X, w, b = _inputs(14, 100, 24, "bf16")
+        X = X if shape is None else X.view(shape)
+        off = _offsets(lengths) if shape is None else None
+        leaves = [t.requires_grad_() for t in (X, w, b)]
+
+        def step():
+            y = group_norm(X, 3, w, b, off, activation="gelu")
+            return [y, *torch.autograd.grad(y, leaves, torch.ones_like(y))]
+
+        want = step()
+        with monkeypatch.context() as m:
+            m.setattr(binding, "_train", None)
+            assert all(torch.equal(a, c) for a, c in zip(step(), want))
+
+
+def test_gradients_of_gradients_are_refused():
+    from paper_2605_15695_amd.norm import group_norm
+
+    X = torch.randn(10, 4, device="cuda").requires_grad_()
+    grad, = torch.autograd.grad(group_norm(X, 2).square().sum(), X, create_graph=True)
+    with pytest.raises(RuntimeError):
+        grad.sum().backward()
