@@ -17,10 +17,11 @@ namespace {
 constexpr int kT = 256;          // threads of a workgroup
 constexpr int kAhead = 4;        // rows of the table a group of lanes has on their way
 constexpr int kRankMost = 16384; // ids that are sorted by counting the smaller ones
+constexpr int kRankT = 1024;     // threads of that
 constexpr int kRankKeys = 8192;  // of their keys in LDS at a time
 constexpr int kTile = 2048;      // ids a workgroup of a sorting pass holds in registers
 constexpr int kTiles = 512;      // workgroups of a sorting pass at most
-constexpr int kDigit = 10;       // bits of a sorting pass at most
+constexpr int kDigit = 11;       // bits of a sorting pass at most
 constexpr int kRounds = kTile / kT;
 constexpr int kGradAhead = 8;    // rows of the gradient a group of lanes has on their way
 
@@ -88,7 +89,7 @@ struct Fill { // zeros, by the workgroups behind those that sort
 __device__ __forceinline__ void fill(const Fill &f, int64_t block, int64_t blocks)
 {
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    const int64_t at = (block * kT + threadIdx.x) * 16, step = blocks * kT * 16;
+    const int64_t at = (block * blockDim.x + threadIdx.x) * 16, step = blocks * blockDim.x * 16;
     const int64_t head = (16 - (reinterpret_cast<uintptr_t>(f.p) & 15)) & 15; // up to 16-byte alignment
     const int64_t whole = f.bytes > head ? (f.bytes - head) / 16 * 16 : 0;
     for (int64_t i = at; i < whole; i += step) *reinterpret_cast<u4 *>(f.p + head + i) = u4{0, 0, 0, 0};
@@ -99,41 +100,45 @@ __device__ __forceinline__ void fill(const Fill &f, int64_t block, int64_t block
 }
 
 // The place of an id among n sorted ones is the number of smaller ones and of equal ones before it.  64 ids to a
-// workgroup, a quarter of the keys to each of its wavefronts, read from LDS four at a time.  One launch: 16,384 ids are 2.7e8
-// comparisons, where the passes below would be six launches.
+// workgroup, a sixteenth of the keys to each of its wavefronts, read from LDS four at a time.  Bound by the comparisons, 2.7e8 for 16,384 ids
+// in one launch, where the passes below would be six.
 template <typename I>
-__global__ void __launch_bounds__(kT) rank_kernel(int64_t n_ids, int64_t rows, const void *ids, uint32_t *key, uint32_t *pos,
-                                                  int sorters, Fill f)
+__global__ void __launch_bounds__(kRankT) rank_kernel(int64_t n_ids, int64_t rows, const void *ids, uint32_t *key, uint32_t *pos,
+                                                      int sorters, Fill f)
 {
+    constexpr int W = kRankT / 64;
     __shared__ uint4 keys4[kRankKeys / 4];
-    __shared__ int part[kT / 64][64];
+    __shared__ int part[W][64];
     if ((int)blockIdx.x >= sorters) {
         fill(f, blockIdx.x - sorters, gridDim.x - sorters);
         return;
     }
     uint32_t *keys = reinterpret_cast<uint32_t *>(keys4);
-    const int n = (int)n_ids, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = (int)n_ids, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int first = blockIdx.x * 64, i = first + lane; // first: a multiple of 4
     const uint32_t own = key_of<I>(ids, i < n ? i : n - 1, rows);
     int count = 0;
     for (int base = 0; base < n; base += kRankKeys) {
         const int here = n - base < kRankKeys ? n - base : kRankKeys, n4 = (here + 3) / 4;
         __syncthreads(); // the keys before are read
-        for (int j = tid; j < n4 * 4; j += kT) keys[j] = j < here ? key_of<I>(ids, base + j, rows) : 0xffffffffu;
+        for (int j = tid; j < n4 * 4; j += kRankT) keys[j] = j < here ? key_of<I>(ids, base + j, rows) : 0xffffffffu;
         __syncthreads();
-        const int per = (n4 + kT / 64 - 1) / (kT / 64);
+        const int per = (n4 + W - 1) / W;
         const int hi = (wave + 1) * per < n4 ? (wave + 1) * per : n4, at = (first - base) / 4;
         int j = wave * per;
-        for (const int end = hi < at ? hi : at; j < end; ++j) {
+        const int end0 = hi < at ? hi : at, end1 = hi < at + 16 ? hi : at + 16;
+#pragma unroll 8
+        for (; j < end0; ++j) {
             const uint4 k = keys4[j];
             count += (k.x <= own) + (k.y <= own) + (k.z <= own) + (k.w <= own);
         }
-        for (const int end = hi < at + 16 ? hi : at + 16; j < end; ++j) {
+        for (; j < end1; ++j) {
             const uint4 k = keys4[j];
             const int o = base + j * 4;
             count += (k.x < own || (k.x == own && o < i)) + (k.y < own || (k.y == own && o + 1 < i)) +
                      (k.z < own || (k.z == own && o + 2 < i)) + (k.w < own || (k.w == own && o + 3 < i));
         }
+#pragma unroll 8
         for (; j < hi; ++j) {
             const uint4 k = keys4[j];
             count += (k.x < own) + (k.y < own) + (k.z < own) + (k.w < own);
@@ -142,7 +147,9 @@ __global__ void __launch_bounds__(kT) rank_kernel(int64_t n_ids, int64_t rows, c
     part[wave][lane] = count;
     __syncthreads();
     if (wave == 0 && i < n) {
-        const int to = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+        int to = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) to += part[w][lane];
         key[to] = own;
         pos[to] = i;
     }
@@ -434,6 +441,141 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(G
     }
 }
 
+// ------------------------------------------------------------------ few ids
+// With up to kOwnMost ids no order is made of them: a workgroup owns a stretch of rows, looks through all ids for those of its
+// rows (each wavefront through a quarter, in order, into a list in LDS), and a group of lanes adds up a row or writes its zeros.  One launch, bound
+// by its round trips and the zeros.  The whole workgroup takes a row, a stretch of its ids to each group, where the table has few, and
+// where it has more than kOwnAlone ids; the parts of a sum are added in order.
+constexpr int kOwnMost = 4096, kOwnAlone = 48;
+struct OwnArgs {
+    int64_t n, rows, d, stride;
+    int own, whole; // rows of a workgroup; whether all of it takes each of them, not a group of lanes
+    const void *ids, *dout;
+    void *grad;
+    float scale;
+};
+template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) own_kernel(OwnArgs p)
+{
+    constexpr int N = kPer16<T>, G = kT / L, W = kT / 64;
+    extern __shared__ uint32_t list[]; // [W][per]: position and row of ids in the stretch: position << 8 | row
+    __shared__ int length[W];
+    __shared__ float shared[G][L * N];
+    __shared__ int heavy[256];
+    const int tid = threadIdx.x, lane64 = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = tid % L, group = tid / L, n = (int)p.n, per = (n + W - 1) / W;
+    const int64_t r0 = (int64_t)blockIdx.x * p.own, c = ((int64_t)blockIdx.y * L + lane) * N;
+    const int rows = p.rows - r0 < p.own ? (int)(p.rows - r0) : p.own;
+    const bool in = c < p.d;
+    const int m = !in ? 0 : p.d - c < N ? (int)(p.d - c) : N;
+    const T *dout = static_cast<const T *>(p.dout);
+    T *grad = static_cast<T *>(p.grad) + r0 * p.d + c;
+    uint32_t *mine = list + wave * per;
+    int have = 0;
+    const int end = (wave + 1) * per < n ? (wave + 1) * per : n;
+    constexpr int U = 8; // ids of a lane on their way
+    for (int i = wave * per; i < end; i += U * 64) {
+        int64_t row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) row[u] = i + u * 64 + lane64 < end ? id_at<I>(p.ids, i + u * 64 + lane64) - r0 : -1;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool hit = row[u] >= 0 && row[u] < rows;
+            const unsigned long long all = __ballot(hit);
+            if (hit) mine[have + __popcll(all & ((1ull << lane64) - 1))] = (uint32_t)(i + u * 64 + lane64) << 8 | (uint32_t)row[u];
+            have += __popcll(all);
+        }
+    }
+    if (lane64 == 0) length[wave] = have;
+    if (tid < 256) heavy[tid] = 0;
+    __syncthreads();
+    // f(position) for the ids of a row in order, `share` of `shares` of them: every lane sees the same
+    auto each = [&](int row, int share, int shares, auto f) {
+        int seen = 0, total = 0;
+        if (shares > 1) {
+            for (int w = 0; w < W; ++w)
+                for (int i = 0; i < length[w]; i += L) {
+                    const bool hit = i + lane < length[w] && (list[w * per + i + lane] & 255) == (uint32_t)row;
+                    total += __popcll(__ballot(hit) >> (lane64 - lane) & (L == 64 ? ~0ull : (1ull << L) - 1));
+                }
+        }
+        const int each_of = (total + shares - 1) / shares, lo = share * each_of, hi = shares > 1 ? lo + each_of : INT32_MAX;
+        for (int w = 0; w < W; ++w)
+            for (int i = 0; i < length[w]; i += L) {
+                const bool hit = i + lane < length[w] && (list[w * per + i + lane] & 255) == (uint32_t)row;
+                unsigned long long all = __ballot(hit) >> (lane64 - lane) & (L == 64 ? ~0ull : (1ull << L) - 1);
+                while (all) {
+                    const int k = __ffsll(all) - 1;
+                    all &= all - 1;
+                    if (seen >= lo && seen < hi) f((int)(list[w * per + i + k] >> 8));
+                    ++seen;
+                }
+            }
+        return seen;
+    };
+    auto sum_row = [&](int row, int share, int shares, float (&sum)[N]) {
+        int at[kGradAhead], held = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.0f;
+        auto flush = [&] {
+            float x[kGradAhead][N];
+#pragma unroll
+            for (int k = 0; k < kGradAhead; ++k)
+                if (k < held && in) load_upto<T, N>(dout + (int64_t)at[k] * p.stride + c, m, x[k]);
+#pragma unroll
+            for (int k = 0; k < kGradAhead; ++k)
+                if (k < held && in)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) sum[i] += x[k][i];
+            held = 0;
+        };
+        each(row, share, shares, [&](int position) {
+#pragma unroll
+            for (int k = 0; k < kGradAhead; ++k)
+                if (k == held) at[k] = position;
+            if (++held == kGradAhead) flush();
+        });
+        flush();
+    };
+    auto finish = [&](int row, float (&sum)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] *= p.scale;
+        if (in) store_upto<T, N>(grad + (int64_t)row * p.d, m, sum);
+    };
+    if (!p.whole) {
+        for (int row = group; row < rows; row += G) {
+            int count = 0;
+            for (int w = 0; w < W; ++w)
+                for (int i = 0; i < length[w]; i += L) {
+                    const bool hit = i + lane < length[w] && (list[w * per + i + lane] & 255) == (uint32_t)row;
+                    count += __popcll(__ballot(hit) >> (lane64 - lane) & (L == 64 ? ~0ull : (1ull << L) - 1));
+                }
+            if (count > kOwnAlone) {
+                if (lane == 0) heavy[row] = 1;
+                continue;
+            }
+            float sum[N];
+            sum_row(row, 0, 1, sum);
+            finish(row, sum);
+        }
+        __syncthreads();
+    }
+    for (int row = 0; row < rows; ++row) { // the whole workgroup; the same branch for all of it
+        if (!p.whole && !heavy[row]) continue;
+        float sum[N];
+        sum_row(row, group, G, sum);
+#pragma unroll
+        for (int i = 0; i < N; ++i) shared[group][lane * N + i] = sum[i];
+        __syncthreads();
+        if (group == 0) {
+            for (int o = 1; o < G; ++o)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += shared[o][lane * N + i];
+            finish(row, sum);
+        }
+        __syncthreads();
+    }
+}
+
 // lanes to a row of `vectors` of 16 bytes: as many as leave the fewest idle, the most of those
 int lanes_for(int64_t vectors)
 {
@@ -477,7 +619,7 @@ template <typename V> GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, V p
     q.slices = (vectors + q.lanes - 1) / q.lanes;
     // enough groups to keep the memory busy, long enough tiles that few runs cross them
     q.tile = 64;
-    while (q.tile > 8 && n / q.tile * q.slices * q.lanes < 4096 * 16) q.tile /= 2;
+    while (q.tile > 8 && n / q.tile * q.slices * q.lanes < 16384 * 16) q.tile /= 2;
     q.groups = (n + q.tile - 1) / q.tile;
     const int64_t subs = (n + kTile - 1) / kTile, per = (subs + kTiles - 1) / kTiles;
     q.chunk = (per < 1 ? 1 : per) * kTile;
@@ -532,6 +674,20 @@ template <typename T> struct Runs {
     };
 };
 
+template <typename T, typename I> struct Own {
+    template <int L> struct Of {
+        static void run(OwnArgs p, int64_t slices, hipStream_t s)
+        {
+            constexpr int G = kT / L;
+            p.whole = p.rows < 512;
+            const int64_t per = p.rows / 1024;
+            p.own = p.whole ? 1 : (int)(per < G ? G : per > 256 ? 256 : per);
+            const dim3 grid((unsigned)((p.rows + p.own - 1) / p.own), (unsigned)slices);
+            hipLaunchKernelGGL((own_kernel<T, I, L>), grid, dim3(kT), (size_t)((p.n + kT / 64 - 1) / (kT / 64) * (kT / 64) * 4), s, p);
+        }
+    };
+};
+
 template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, const GradPlan &q, const GradSpace &w, char *ws, Fill f,
                                    hipStream_t s)
 {
@@ -540,7 +696,7 @@ template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, con
     uint32_t *key = reinterpret_cast<uint32_t *>(ws + w.key), *pos = reinterpret_cast<uint32_t *>(ws + w.pos);
     if (n <= kRankMost) {
         const int sorters = (int)((n + 63) / 64);
-        hipLaunchKernelGGL((rank_kernel<I>), dim3(sorters + fillers), dim3(kT), 0, s, n, rows, ids, key, pos,
+        hipLaunchKernelGGL((rank_kernel<I>), dim3(sorters + (fillers + 3) / 4), dim3(kRankT), 0, s, n, rows, ids, key, pos,
                            sorters, f);
         return PCSR_OK;
     }
@@ -600,7 +756,7 @@ int pcsr_embed(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids
 
 int64_t pcsr_embed_workspace(int64_t n, int64_t rows, int64_t d)
 {
-    if (!sizes_ok(n, rows, d) || !sizes_fit(n, rows, d) || n == 0) return 0;
+    if (!sizes_ok(n, rows, d) || !sizes_fit(n, rows, d) || n <= kOwnMost) return 0;
     int64_t most = 0;
     for (int per16 : {4, 8}) {
         const GradPlan q = grad_plan(n, rows, d, per16);
@@ -613,7 +769,7 @@ int64_t pcsr_embed_workspace(int64_t n, int64_t rows, int64_t d)
 int pcsr_embed_backward(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids, int32_t wide, const void *dout,
                         int64_t stride, float scale, void *grad, void *ws, void *stream)
 {
-    if (!sizes_ok(n, rows, d) || stride < d || (n && (!ids || !dout || !ws)) || (rows && !grad)) return PCSR_E_INVALID_ARG;
+    if (!sizes_ok(n, rows, d) || stride < d || (n && (!ids || !dout)) || (n > kOwnMost && !ws) || (rows && !grad)) return PCSR_E_INVALID_ARG;
     if (!sizes_fit(n, rows, d) || stride > (int64_t(1) << 31)) return PCSR_E_TOO_LARGE;
     if (type < PCSR_F32 || type > PCSR_F16) return PCSR_E_UNSUPPORTED;
     if (rows == 0) return PCSR_OK;
@@ -626,6 +782,14 @@ int pcsr_embed_backward(int64_t n, int64_t rows, int64_t d, int32_t type, const 
             return launched();
         }
         const GradPlan q = grad_plan(n, rows, d, kPer16<T>);
+        if (n <= kOwnMost) {
+            const OwnArgs o = {n, rows, d, stride, 0, 0, ids, dout, grad, scale};
+            if (wide)
+                for_lanes<Own<T, int64_t>::template Of>(q.lanes, o, q.slices, s);
+            else
+                for_lanes<Own<T, int32_t>::template Of>(q.lanes, o, q.slices, s);
+            return launched();
+        }
         const GradSpace w(n, q, d);
         char *at = static_cast<char *>(ws);
         int rc = wide ? sort_ids<int64_t>(n, rows, ids, q, w, at, f, s) : sort_ids<int32_t>(n, rows, ids, q, w, at, f, s);

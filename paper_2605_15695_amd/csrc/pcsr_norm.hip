@@ -4,13 +4,15 @@
 // act(z).  Backward, with dz = dy act'(z): db = sum dz, dw = sum dz xhat, and in each group
 // dx = rstd (w dz - (S1 + xhat S2) / m), S1 = sum w dz, S2 = sum w dz xhat.
 //
-// Bound by memory.  A thread owns 16 bytes of channels of every few rows.  A short graph belongs to one workgroup, which keeps it in
-// registers between its sums and its results: read once.  Long graphs are cut into chunks of rows whose sums go to a
-// workspace, and a second kernel adds those of its graph and reads the rows again: twice, the second time from the
-// memory-side cache where they fit.  Which graph is short is found out on the GPU: the host does not know the offsets.  A graph is long
-// if it has more rows than a chunk, so that a chunk meets two long graphs at most, and there are two places for its sums.
+// Bound by memory.  A thread owns 16 bytes of channels of every few rows.  A short graph belongs to a team (a wavefront where graphs are
+// a few kilobytes, a workgroup otherwise), which keeps it in registers between its sums and its results: read once.  Long graphs are
+// cut into chunks of rows whose sums go to a workspace; a second kernel adds those of a graph, a third reads the rows again,
+// the last chunks first, since those are in the memory-side cache.  Which graph is long is found out on the GPU: the host does not know the
+// offsets.  A long graph has more rows than a chunk, so that a chunk meets two of them at most, and there are two places for its sums.
 // Sums of x and x^2 are held in 64 bits: the variance is a difference, and of numbers far from 0 32 bits would leave little.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "pcsr_num.h"
 
@@ -18,16 +20,22 @@ namespace pcsr {
 namespace {
 
 constexpr int kMost = 512;     // threads of a workgroup at most
-constexpr int kKept = 16;      // 16-byte pieces a thread keeps of a short graph
-constexpr int kKeptBack = 8;   // of its rows and of their gradients, each
+constexpr int kKept = 8;       // 16-byte pieces a thread keeps of a short graph (of its rows and of their gradients, each)
 constexpr int kAhead = 4;      // pieces a thread has on their way
 constexpr int kSlots = 2;      // long graphs that meet a chunk
+constexpr int kGroupsOf = 8;   // groups that a workgroup adds up over the chunks
 
+// how a kernel's threads lie over rows and channels
+struct Shape {
+    int threads, team, slices; // of a workgroup; that work together; of the channels
+    int cs, tpr, rpp;          // channels of a slice (whole groups), threads to a row, rows to a pass
+    int lanes;                 // that add up one group
+};
 struct NormArgs {
     int64_t rows, C, graphs, length; // length: of a graph, where there are no offsets
     int groups, cpg;                 // channels of a group
     const void *offsets;
-    int wide, ptype;
+    int wide, ptype, act;
     const void *x;
     int64_t xs;
     const void *w, *b;
@@ -38,14 +46,14 @@ struct NormArgs {
     const void *dy;
     int64_t dys;
     void *dx;
-    float *sums; // [workgroup][2][C]: of dz and dz xhat
+    float *sums;  // [workgroup][2][C]: of dz and dz xhat; first those of short graphs
+    float *means; // [graphs][groups][2]: S1 / m and S2 / m of long graphs
+    void *dw, *db;
     // shape of the launch
-    int64_t chunk; // rows of a chunk
-    int shorts, chunks; // workgroups for short graphs, for chunks
-    int cs, tpr, rpp;   // channels of a slice (whole groups), threads to a row, rows to a pass
-    int one;            // a thread's channels are of one group
-    int lanes;          // that add up one group
-    void *part;         // [chunk][kSlots][groups] pairs of doubles (forward) or floats (backward)
+    Shape sh;
+    int64_t longer, chunk; // a graph of more rows is long; rows of a chunk, no more than that
+    int shorts, chunks;    // workgroups for short graphs, for chunks
+    void *part;            // [chunk][kSlots][groups] pairs of doubles (forward) or floats (backward)
 };
 
 __device__ __forceinline__ int64_t begin_of(const NormArgs &a, int64_t s)
@@ -56,15 +64,18 @@ __device__ __forceinline__ int64_t begin_of(const NormArgs &a, int64_t s)
     const int64_t o = a.wide ? static_cast<const int64_t *>(a.offsets)[s] : (int64_t) static_cast<const int32_t *>(a.offsets)[s];
     return o < 0 ? 0 : (o < a.rows ? o : a.rows);
 }
-// the last graph that begins at or before a row
+// the last graph that begins at or before a row, found by a wavefront: 64 probes at a time, since such a search is bound by its
+// round trips (20,000 graphs: three of them).  All lanes ask for the same row.
 __device__ __forceinline__ int64_t graph_of(const NormArgs &a, int64_t row)
 {
     if (!a.offsets) return a.length > 0 ? row / a.length : 0;
-    int64_t lo = 0, hi = a.graphs;
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = a.graphs; // lo begins there or before
     while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (begin_of(a, mid) <= row) lo = mid;
-        else hi = mid;
+        const int64_t step = (hi - lo + 63) / 64, probe = lo + lane * step;
+        const int below = __popcll(__ballot(probe < hi && begin_of(a, probe) <= row)); // 1 at least: lane 0's
+        lo += (int64_t)(below > 0 ? below - 1 : 0) * step;
+        hi = hi < lo + step ? hi : lo + step;
     }
     return lo;
 }
@@ -93,83 +104,121 @@ template <typename T> __device__ __forceinline__ Raw<T> raw(const T *p, int m)
     return v;
 }
 
-template <int ACT> __device__ __forceinline__ float act(float z)
+// The share of the normal distribution below z, by formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions (error
+// 7.5e-8); bell: exp(-z^2 / 2), which the slope of gelu needs as well.
+__device__ __forceinline__ float below_normal(float z, float bell)
 {
-    if (ACT == PCSR_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
-    if (ACT == PCSR_ACT_SILU) return z / (1.0f + __expf(-z));
-    if (ACT == PCSR_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    return z;
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678f * fabsf(z));
+    const float q = 0.5f * bell * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    return z < 0.0f ? q : 1.0f - q;
 }
-template <int ACT> __device__ __forceinline__ float slope(float z)
+template <int N> __device__ __forceinline__ void activate(float (&z)[N], int act)
 {
-    if (ACT == PCSR_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (ACT == PCSR_ACT_SILU) {
-        const float p = 1.0f / (1.0f + __expf(-z));
-        return p * (1.0f + z * (1.0f - p));
+    switch (act) { // the same for the whole launch
+    case PCSR_ACT_RELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i]; // a NaN stays one
+        break;
+    case PCSR_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-z[i]));
+        break;
+    case PCSR_ACT_GELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] * below_normal(z[i], __expf(-0.5f * z[i] * z[i]));
+        break;
     }
-    if (ACT == PCSR_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
-    return 1.0f;
+}
+// z becomes the activation's slope there
+template <int N> __device__ __forceinline__ void slopes(float (&z)[N], int act)
+{
+    switch (act) {
+    case PCSR_ACT_RELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] > 0.0f ? 1.0f : z[i] <= 0.0f ? 0.0f : z[i];
+        break;
+    case PCSR_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-z[i]));
+            z[i] = p * (1.0f + z[i] * (1.0f - p));
+        }
+        break;
+    case PCSR_ACT_GELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float bell = __expf(-0.5f * z[i] * z[i]);
+            z[i] = below_normal(z[i], bell) + z[i] * 0.39894228f * bell;
+        }
+        break;
+    default:
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = 1.0f;
+    }
 }
 
 // a thread's place in a slice
-struct Place {
+template <bool WAVE> struct Place {
+    int t;           // thread of the team
     int r, unit, m;  // row of a pass, 16-byte piece of the row, channels of it (0: the thread has none)
     int64_t c;       // first channel
     int c0, c1, g0, ng; // the slice's channels and groups
     __device__ Place(const NormArgs &a, int per16)
     {
-        c0 = blockIdx.y * a.cs, c1 = c0 + a.cs < a.C ? c0 + a.cs : (int)a.C;
+        t = WAVE ? threadIdx.x & 63 : threadIdx.x;
+        c0 = blockIdx.y * a.sh.cs, c1 = c0 + a.sh.cs < a.C ? c0 + a.sh.cs : (int)a.C;
         g0 = c0 / a.cpg, ng = (c1 - c0) / a.cpg;
-        r = threadIdx.x / a.tpr, unit = threadIdx.x - r * a.tpr;
+        r = t / a.sh.tpr, unit = t - r * a.sh.tpr;
         c = c0 + unit * per16;
-        m = r < a.rpp && c < c1 ? (c1 - (int)c < per16 ? c1 - (int)c : per16) : 0;
+        m = r < a.sh.rpp && c < c1 ? (c1 - (int)c < per16 ? c1 - (int)c : per16) : 0;
     }
 };
-
-// Sums of a pair over the threads of each group: v (N pairs of a thread, one for each of its channels) go through LDS; `lanes`
-// lanes then add up a group and the first of them calls done(group, pair).
-template <int N, typename V, typename F>
-__device__ __forceinline__ void group_sums(const NormArgs &a, const Place &at, V *shared, const V (&s)[N], const V (&q)[N], F done)
+// what was written to LDS can be read by the team
+template <bool WAVE> __device__ __forceinline__ void team_sync()
 {
-    const int units = a.one ? a.tpr : a.cs; // of a row
-    if (a.one) {
-        V s1 = 0, q1 = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < at.m) s1 += s[i], q1 += q[i];
-        if (at.m) {
-            shared[(at.r * units + at.unit) * 2] = s1;
-            shared[(at.r * units + at.unit) * 2 + 1] = q1;
-        }
+    if (WAVE) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < at.m) {
-                shared[(at.r * units + (int)at.c - at.c0 + i) * 2] = s[i];
-                shared[(at.r * units + (int)at.c - at.c0 + i) * 2 + 1] = q[i];
-            }
+        __syncthreads();
     }
-    __syncthreads();
-    const int per = a.one ? a.cpg / N : a.cpg, lane = threadIdx.x & (a.lanes - 1), step = blockDim.x / a.lanes;
-    for (int g = threadIdx.x / a.lanes; g - (int)(threadIdx.x / a.lanes) < at.ng; g += step) { // all lanes of a wavefront stay
+}
+
+// Sums of a pair over the threads of each group: a thread's pairs (one for each of its channels; ONE: its channels are of one group, and
+// there is one pair) go through LDS; `lanes` lanes then add up a group and the first of them calls done(group, pair).
+template <bool WAVE, bool ONE, int A, typename V, typename F>
+__device__ __forceinline__ void group_sums(const NormArgs &a, const Place<WAVE> &at, V *shared, const V (&s)[A], const V (&q)[A], int per16, F done)
+{
+    const Shape &sh = a.sh;
+    const int units = ONE ? sh.tpr : sh.cs; // of a row
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+        if (i < at.m) {
+            V *to = shared + (at.r * units + (ONE ? at.unit : (int)at.c - at.c0 + i)) * 2;
+            to[0] = s[i], to[1] = q[i];
+        }
+    team_sync<WAVE>();
+    const int per = ONE ? a.cpg / per16 : a.cpg, all = per * sh.rpp;
+    const int lane = at.t & (sh.lanes - 1), mine = at.t / sh.lanes, step = sh.team / sh.lanes;
+    for (int g = mine; g - mine < at.ng; g += step) { // all lanes of a wavefront stay
         V s1 = 0, q1 = 0;
         if (g < at.ng) {
-            for (int r = 0; r < a.rpp; ++r)
-                for (int k = lane; k < per; k += a.lanes) {
-                    s1 += shared[(r * units + g * per + k) * 2];
-                    q1 += shared[(r * units + g * per + k) * 2 + 1];
-                }
+            for (int e = lane; e < all; e += sh.lanes) {
+                const int r = e / per, k = e - r * per;
+                const V *from = shared + (r * units + g * per + k) * 2;
+                s1 += from[0], q1 += from[1];
+            }
         }
-        for (int m = 1; m < a.lanes; m <<= 1) s1 += __shfl_xor(s1, m), q1 += __shfl_xor(q1, m);
+        for (int m = 1; m < sh.lanes; m <<= 1) s1 += __shfl_xor(s1, m), q1 += __shfl_xor(q1, m);
         if (g < at.ng && lane == 0) done(g, s1, q1);
     }
-    __syncthreads();
+    team_sync<WAVE>();
 }
 
 // what a thread's channels need: mean, rstd, weight, bias
 template <int N> struct Channel {
     float mean[N], rstd[N], w[N], b[N];
-    __device__ __forceinline__ void params(const NormArgs &a, const Place &at)
+    template <bool WAVE> __device__ __forceinline__ void params(const NormArgs &a, const Place<WAVE> &at)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -178,7 +227,7 @@ template <int N> struct Channel {
         }
     }
     // stat: pairs of the slice's groups
-    __device__ __forceinline__ void stats(const NormArgs &a, const Place &at, const float *stat)
+    template <bool WAVE> __device__ __forceinline__ void stats(const NormArgs &a, const Place<WAVE> &at, const float *stat)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -186,65 +235,81 @@ template <int N> struct Channel {
             mean[i] = stat[g * 2], rstd[i] = stat[g * 2 + 1];
         }
     }
+    // as a kernel before left them
+    template <bool WAVE> __device__ __forceinline__ void stats_of(const NormArgs &a, const Place<WAVE> &at, int64_t graph)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t g = graph * a.groups + at.g0 + (i < at.m ? ((int)at.c - at.c0 + i) / a.cpg : 0);
+            mean[i] = a.mean[g], rstd[i] = a.rstd[g];
+        }
+    }
 };
 
-// variance from sums in 64 bits; never below 0
-__device__ __forceinline__ void mean_rstd(double s, double q, double m, float eps, float *mean, float *rstd)
+// mean and 1 / sqrt(variance + eps) from sums in 64 bits; the variance is never below 0, and a NaN stays one
+__device__ __forceinline__ void mean_rstd(double s, double q, double over, float eps, float *mean, float *rstd)
 {
-    const double mu = s / m, var = q / m - mu * mu;
+    const double mu = s * over, var = q * over - mu * mu, v = (var < 0.0 ? 0.0 : var) + (double)eps;
+    double r = __builtin_amdgcn_rsq(v); // to half its bits, then twice as many
+    r = r * (1.5 - 0.5 * v * r * r);
+    r = r * (1.5 - 0.5 * v * r * r);
     *mean = (float)mu;
-    *rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps)); // a NaN stays one
+    *rstd = (float)r;
 }
 
-template <typename T, int ACT> __device__ __forceinline__ void apply(const Raw<T> &v, const Channel<kPer16<T>> &ch, T *y, int m)
+template <typename T> __device__ __forceinline__ void apply(const NormArgs &a, const Raw<T> &v, const Channel<kPer16<T>> &ch, T *y, int m)
 {
     constexpr int N = kPer16<T>;
     float z[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = act<ACT>(((float)v[i] - ch.mean[i]) * ch.rstd[i] * ch.w[i] + ch.b[i]);
+    for (int i = 0; i < N; ++i) z[i] = ((float)v[i] - ch.mean[i]) * ch.rstd[i] * ch.w[i] + ch.b[i];
+    activate(z, a.act);
     store_upto<T, N>(y, m, z);
 }
 
-// f(row, piece of x [, piece of dy]) for the thread's rows of [lo, hi), kAhead of them on their way
-template <typename T, typename F> __device__ __forceinline__ void each_row(const NormArgs &a, const Place &at, int64_t lo, int64_t hi, F f)
+// f(row, piece of x [, piece of dy]) for the thread's rows of [lo, hi), kAhead pieces on their way
+template <typename T, bool WAVE, typename F>
+__device__ __forceinline__ void each_row(const NormArgs &a, const Place<WAVE> &at, int64_t lo, int64_t hi, F f)
 {
     const T *x = static_cast<const T *>(a.x);
-    for (int64_t row = lo + at.r; row < hi; row += (int64_t)kAhead * a.rpp) {
+    const int rpp = a.sh.rpp;
+    for (int64_t row = lo + at.r; row < hi; row += (int64_t)kAhead * rpp) {
         Raw<T> v[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (row + k * a.rpp < hi) v[k] = raw(x + (row + k * a.rpp) * a.xs + at.c, at.m);
+            if (row + k * rpp < hi) v[k] = raw(x + (row + k * rpp) * a.xs + at.c, at.m);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (row + k * a.rpp < hi) f(row + k * a.rpp, v[k]);
+            if (row + k * rpp < hi) f(row + k * rpp, v[k]);
     }
 }
-template <typename T, typename F>
-__device__ __forceinline__ void each_pair(const NormArgs &a, const Place &at, int64_t lo, int64_t hi, F f)
+template <typename T, bool WAVE, typename F>
+__device__ __forceinline__ void each_pair(const NormArgs &a, const Place<WAVE> &at, int64_t lo, int64_t hi, F f)
 {
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
     constexpr int U = kAhead / 2;
-    for (int64_t row = lo + at.r; row < hi; row += (int64_t)U * a.rpp) {
+    const int rpp = a.sh.rpp;
+    for (int64_t row = lo + at.r; row < hi; row += (int64_t)U * rpp) {
         Raw<T> v[U], g[U];
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            if (row + k * a.rpp < hi) {
-                v[k] = raw(x + (row + k * a.rpp) * a.xs + at.c, at.m);
-                g[k] = raw(dy + (row + k * a.rpp) * a.dys + at.c, at.m);
+            if (row + k * rpp < hi) {
+                v[k] = raw(x + (row + k * rpp) * a.xs + at.c, at.m);
+                g[k] = raw(dy + (row + k * rpp) * a.dys + at.c, at.m);
             }
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            if (row + k * a.rpp < hi) f(row + k * a.rpp, v[k], g[k]);
+            if (row + k * rpp < hi) f(row + k * rpp, v[k], g[k]);
     }
 }
 
-template <typename T, int N> __device__ __forceinline__ void add_squares(const Raw<T> &v, double (&s)[N], double (&q)[N])
+template <typename T, bool ONE, int A> __device__ __forceinline__ void add_squares(const Raw<T> &v, double (&s)[A], double (&q)[A])
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < kPer16<T>; ++i) {
         const double x = (double)(float)v[i];
-        s[i] += x;
-        q[i] = fma(x, x, q[i]);
+        s[ONE ? 0 : i] += x;
+        q[ONE ? 0 : i] = fma(x, x, q[ONE ? 0 : i]);
     }
 }
 
@@ -257,355 +322,382 @@ struct ChunkPart {
         lo = j * a.chunk, hi = lo + a.chunk < a.rows ? lo + a.chunk : a.rows;
         graph = graph_of(a, slot ? hi - 1 : lo);
         first = begin_of(a, graph), end = begin_of(a, graph + 1);
-        any = end - first > a.chunk && (slot == 0 || first > lo);
+        any = end - first > a.longer && (slot == 0 || first > lo);
         lo = lo > first ? lo : first, hi = hi < end ? hi : end;
     }
 };
 
-template <typename T, int ACT> __global__ void __launch_bounds__(kMost) norm_kernel(NormArgs a)
+// short graphs, one to a team
+template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMost) norm_kernel(NormArgs a)
 {
-    constexpr int N = kPer16<T>;
-    extern __shared__ double shared[];
-    float *stat = reinterpret_cast<float *>(shared + (size_t)2 * a.rpp * (a.one ? a.tpr : a.cs));
-    const Place at(a, N);
-    Channel<N> ch;
-    double s[N], q[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = q[i] = 0.0;
-    if ((int64_t)blockIdx.x >= a.shorts) { // sums of a chunk
-        const int64_t j = blockIdx.x - a.shorts;
-        for (int slot = 0; slot < kSlots; ++slot) {
-            const ChunkPart p(a, j, slot);
-            if (!p.any) continue;
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[i] = q[i] = 0.0;
-            if (at.m) each_row<T>(a, at, p.lo, p.hi, [&](int64_t, const Raw<T> &v) { add_squares<T, N>(v, s, q); });
-            double *out = static_cast<double *>(a.part) + ((j * kSlots + slot) * a.groups + at.g0) * 2;
-            group_sums<N>(a, at, shared, s, q, [&](int g, double s1, double q1) { out[g * 2] = s1, out[g * 2 + 1] = q1; });
-        }
-        return;
-    }
-    const int64_t graph = blockIdx.x, lo = begin_of(a, graph), hi = begin_of(a, graph + 1);
-    if (hi <= lo || hi - lo > a.chunk) return;
-    const double count = (double)(hi - lo) * a.cpg;
+    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
+    extern __shared__ double memory[];
+    const int each = a.sh.rpp * (ONE ? a.sh.tpr : a.sh.cs) * 2, team = WAVE ? threadIdx.x >> 6 : 0;
+    const Place<WAVE> at(a, N);
+    double *shared = memory + (size_t)team * (each + at.ng);
+    float *stat = reinterpret_cast<float *>(shared + each);
+    const int64_t graph = WAVE ? (int64_t)blockIdx.x * (blockDim.x >> 6) + team : blockIdx.x;
+    const int64_t lo = begin_of(a, graph), hi = begin_of(a, graph + 1);
+    if (hi <= lo || hi - lo > a.longer) return;
+    const double over = 1.0 / ((double)(hi - lo) * a.cpg);
     auto found = [&](int g, double s1, double q1) {
         float mu, rs;
-        mean_rstd(s1, q1, count, a.eps, &mu, &rs);
+        mean_rstd(s1, q1, over, a.eps, &mu, &rs);
         stat[g * 2] = mu, stat[g * 2 + 1] = rs;
         a.mean[graph * a.groups + at.g0 + g] = mu, a.rstd[graph * a.groups + at.g0 + g] = rs;
     };
     T *y = static_cast<T *>(a.y);
-    ch.params(a, at);
-    if (hi - lo <= (int64_t)kKept * a.rpp) {
+    const int rpp = a.sh.rpp;
+    double s[A], q[A];
+#pragma unroll
+    for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0;
+    Channel<N> ch;
+    if (hi - lo <= (int64_t)kKept * rpp) {
         const T *x = static_cast<const T *>(a.x);
+        const int mine = at.m && lo + at.r < hi ? ((int)(hi - lo) - at.r + rpp - 1) / rpp : 0; // rows of the thread
         Raw<T> v[kKept];
 #pragma unroll
         for (int k = 0; k < kKept; ++k)
-            if (lo + k * a.rpp < hi && at.m && lo + k * a.rpp + at.r < hi) v[k] = raw(x + (lo + k * a.rpp + at.r) * a.xs + at.c, at.m);
+            if (k < mine) v[k] = raw(x + (lo + k * rpp + at.r) * a.xs + at.c, at.m);
+        ch.params(a, at);
 #pragma unroll
         for (int k = 0; k < kKept; ++k)
-            if (lo + k * a.rpp < hi && at.m && lo + k * a.rpp + at.r < hi) add_squares<T, N>(v[k], s, q);
-        group_sums<N>(a, at, shared, s, q, found);
-        if (!at.m) return;
+            if (k < mine) add_squares<T, ONE>(v[k], s, q);
+        group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
         ch.stats(a, at, stat);
 #pragma unroll
         for (int k = 0; k < kKept; ++k)
-            if (lo + k * a.rpp < hi && lo + k * a.rpp + at.r < hi)
-                apply<T, ACT>(v[k], ch, y + (lo + k * a.rpp + at.r) * a.C + at.c, at.m);
+            if (k < mine) apply<T>(a, v[k], ch, y + (lo + k * rpp + at.r) * a.C + at.c, at.m);
         return;
     }
-    if (at.m) each_row<T>(a, at, lo, hi, [&](int64_t, const Raw<T> &v) { add_squares<T, N>(v, s, q); });
-    group_sums<N>(a, at, shared, s, q, found);
+    ch.params(a, at);
+    if (at.m) each_row<T>(a, at, lo, hi, [&](int64_t, const Raw<T> &v) { add_squares<T, ONE>(v, s, q); });
+    group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
     if (!at.m) return;
     ch.stats(a, at, stat);
-    each_row<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v) { apply<T, ACT>(v, ch, y + row * a.C + at.c, at.m); });
+    each_row<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v) { apply<T>(a, v, ch, y + row * a.C + at.c, at.m); });
 }
 
-// done(group, pair): sums of the chunks of the part's graph
-template <typename V, typename F>
-__device__ __forceinline__ void graph_sums(const NormArgs &a, const Place &at, const ChunkPart &p, F done)
+// sums of a chunk
+template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_chunk_kernel(NormArgs a)
 {
-    const int64_t j0 = p.first / a.chunk, j1 = (p.end - 1) / a.chunk;
-    const int slot0 = p.first > j0 * a.chunk; // of the first chunk; 0 in the others
-    const int lane = threadIdx.x & (a.lanes - 1), step = blockDim.x / a.lanes;
-    const V *part = static_cast<const V *>(a.part);
-    for (int g = threadIdx.x / a.lanes; g - (int)(threadIdx.x / a.lanes) < at.ng; g += step) {
-        V s = 0, q = 0;
-        if (g < at.ng) {
-#pragma unroll 8
-            for (int64_t j = j0 + lane; j <= j1; j += a.lanes) {
-                const V *in = part + ((j * kSlots + (j == j0 ? slot0 : 0)) * a.groups + at.g0 + g) * 2;
-                s += in[0], q += in[1];
-            }
-        }
-        for (int m = 1; m < a.lanes; m <<= 1) s += __shfl_xor(s, m), q += __shfl_xor(q, m);
-        if (g < at.ng && lane == 0) done(g, s, q);
-    }
-    __syncthreads();
-}
-
-template <typename T, int ACT> __global__ void __launch_bounds__(kMost) norm_apply_kernel(NormArgs a)
-{
-    constexpr int N = kPer16<T>;
-    extern __shared__ double shared[];
-    float *stat = reinterpret_cast<float *>(shared);
-    const Place at(a, N);
-    Channel<N> ch;
-    ch.params(a, at);
+    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
+    extern __shared__ double memory[];
+    const Place<false> at(a, N);
     const int64_t j = blockIdx.x;
-    T *y = static_cast<T *>(a.y);
     for (int slot = 0; slot < kSlots; ++slot) {
         const ChunkPart p(a, j, slot);
         if (!p.any) continue;
-        const double count = (double)(p.end - p.first) * a.cpg;
-        graph_sums<double>(a, at, p, [&](int g, double s, double q) {
-            float mu, rs;
-            mean_rstd(s, q, count, a.eps, &mu, &rs);
-            stat[g * 2] = mu, stat[g * 2 + 1] = rs;
-            if (p.lo == p.first) a.mean[p.graph * a.groups + at.g0 + g] = mu, a.rstd[p.graph * a.groups + at.g0 + g] = rs;
-        });
-        if (at.m) {
-            ch.stats(a, at, stat);
-            each_row<T>(a, at, p.lo, p.hi, [&](int64_t row, const Raw<T> &v) { apply<T, ACT>(v, ch, y + row * a.C + at.c, at.m); });
+        double s[A], q[A];
+#pragma unroll
+        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0;
+        if (at.m) each_row<T>(a, at, p.lo, p.hi, [&](int64_t, const Raw<T> &v) { add_squares<T, ONE>(v, s, q); });
+        double *out = static_cast<double *>(a.part) + ((j * kSlots + slot) * a.groups + at.g0) * 2;
+        group_sums<false, ONE>(a, at, memory, s, q, N, [&](int g, double s1, double q1) { out[g * 2] = s1, out[g * 2 + 1] = q1; });
+    }
+}
+
+// For the long graphs that begin in chunk j: done(graph, its rows, group, pair), the pair added up over their chunks by 32 lanes.
+template <typename V, typename F> __device__ __forceinline__ void add_chunks(const NormArgs &a, int64_t j, int64_t group, F done)
+{
+    const V *part = static_cast<const V *>(a.part);
+    const int lane = threadIdx.x & 31;
+    for (int slot = 0; slot < kSlots; ++slot) {
+        const ChunkPart p(a, j, slot);
+        if (!p.any || p.lo != p.first) continue;
+        const int64_t j1 = (p.end - 1) / a.chunk;
+        V s = 0, q = 0;
+        if (group < a.groups) {
+#pragma unroll 8
+            for (int64_t k = j + lane; k <= j1; k += 32) {
+                const V *in = part + ((k * kSlots + (k == j ? slot : 0)) * a.groups + group) * 2;
+                s += in[0], q += in[1];
+            }
         }
-        __syncthreads(); // stat is read
+        for (int m = 1; m < 32; m <<= 1) s += __shfl_xor(s, m), q += __shfl_xor(q, m);
+        if (lane == 0 && group < a.groups) done(p.graph, p.end - p.first, group, s, q);
+    }
+}
+__global__ void __launch_bounds__(32 * kGroupsOf) norm_combine_kernel(NormArgs a)
+{
+    add_chunks<double>(a, blockIdx.x, (int64_t)blockIdx.y * kGroupsOf + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, double s, double q) {
+        mean_rstd(s, q, 1.0 / ((double)rows * a.cpg), a.eps, a.mean + graph * a.groups + g, a.rstd + graph * a.groups + g);
+    });
+}
+
+template <typename T> __global__ void __launch_bounds__(kMost) norm_apply_kernel(NormArgs a)
+{
+    constexpr int N = kPer16<T>;
+    const Place<false> at(a, N);
+    Channel<N> ch;
+    ch.params(a, at);
+    const int64_t j = gridDim.x - 1 - blockIdx.x;
+    T *y = static_cast<T *>(a.y);
+    for (int slot = 0; slot < kSlots; ++slot) {
+        const ChunkPart p(a, j, slot);
+        if (!p.any || !at.m) continue;
+        ch.stats_of(a, at, p.graph);
+        each_row<T>(a, at, p.lo, p.hi, [&](int64_t row, const Raw<T> &v) { apply<T>(a, v, ch, y + row * a.C + at.c, at.m); });
     }
 }
 
 // ---------------------------------------------------------------------------------- backward
-template <typename T, int ACT, int N>
-__device__ __forceinline__ void add_pair(const Raw<T> &v, const Raw<T> &g, const Channel<N> &ch, float (&s)[N], float (&q)[N])
+// of a piece: its sums for the thread's channels, and for its groups
+template <typename T, bool ONE, int N, int A>
+__device__ __forceinline__ void add_pair(const NormArgs &a, const Raw<T> &v, const Raw<T> &g, const Channel<N> &ch, float (&cs)[N], float (&cq)[N],
+                                         float (&s)[A], float (&q)[A])
 {
+    float xhat[N], dz[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float xhat = ((float)v[i] - ch.mean[i]) * ch.rstd[i];
-        const float dz = (float)g[i] * slope<ACT>(xhat * ch.w[i] + ch.b[i]);
-        s[i] += dz;
-        q[i] += dz * xhat;
+        xhat[i] = ((float)v[i] - ch.mean[i]) * ch.rstd[i];
+        dz[i] = xhat[i] * ch.w[i] + ch.b[i];
+    }
+    slopes(dz, a.act);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        dz[i] *= (float)g[i];
+        cs[i] += dz[i];
+        cq[i] += dz[i] * xhat[i];
+        const float d = dz[i] * ch.w[i];
+        s[ONE ? 0 : i] += d;
+        q[ONE ? 0 : i] += d * xhat[i];
     }
 }
 // s1, s2: the group's sums over its count, for each channel.  Products are rounded by themselves: in a group of one number the
 // difference is 0.
-template <typename T, int ACT, int N>
-__device__ __forceinline__ void put_dx(const Raw<T> &v, const Raw<T> &g, const Channel<N> &ch, const float (&s1)[N], const float (&s2)[N], T *dx,
-                                       int m)
+template <typename T, int N>
+__device__ __forceinline__ void put_dx(const NormArgs &a, const Raw<T> &v, const Raw<T> &g, const Channel<N> &ch, const float (&s1)[N],
+                                       const float (&s2)[N], T *dx, int m)
 {
 #pragma clang fp contract(off)
-    float o[N];
+    float o[N], xhat[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float xhat = ((float)v[i] - ch.mean[i]) * ch.rstd[i];
-        const float dz = (float)g[i] * slope<ACT>(xhat * ch.w[i] + ch.b[i]);
-        o[i] = ch.rstd[i] * ((dz * ch.w[i] - s1[i]) - xhat * s2[i]);
+        xhat[i] = ((float)v[i] - ch.mean[i]) * ch.rstd[i];
+        o[i] = __builtin_fmaf(xhat[i], ch.w[i], ch.b[i]);
+    }
+    slopes(o, a.act);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float d = (o[i] * (float)g[i]) * ch.w[i];
+        o[i] = ch.rstd[i] * ((d - s1[i]) - xhat[i] * s2[i]);
     }
     store_upto<T, N>(dx, m, o);
 }
-template <int N> __device__ __forceinline__ void group_means(const NormArgs &a, const Place &at, const float *stat, float (&s1)[N], float (&s2)[N])
+template <bool WAVE, int N>
+__device__ __forceinline__ void group_means(const NormArgs &a, const Place<WAVE> &at, const float *pairs, float (&s1)[N], float (&s2)[N])
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int g = i < at.m ? ((int)at.c - at.c0 + i) / a.cpg : 0;
-        s1[i] = stat[g * 2], s2[i] = stat[g * 2 + 1];
+        s1[i] = pairs[g * 2], s2[i] = pairs[g * 2 + 1];
     }
 }
-// mean and rstd as the forward call left them
-template <int N> __device__ __forceinline__ void saved_stats(const NormArgs &a, const Place &at, int64_t graph, Channel<N> &ch)
+// a workgroup's sums of each channel, [2][all rows of its teams][cs] of LDS, to row `to` of a.sums
+template <bool WAVE, int N>
+__device__ __forceinline__ void put_sums(const NormArgs &a, const Place<WAVE> &at, float *col, const float (&cs)[N], const float (&cq)[N], int64_t to)
 {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int64_t g = graph * a.groups + at.g0 + (i < at.m ? ((int)at.c - at.c0 + i) / a.cpg : 0);
-        ch.mean[i] = a.mean[g], ch.rstd[i] = a.rstd[g];
-    }
-}
-
-template <typename T, int ACT> __global__ void __launch_bounds__(kMost) norm_backward_kernel(NormArgs a)
-{
-    constexpr int N = kPer16<T>;
-    extern __shared__ double shared_[];
-    float *shared = reinterpret_cast<float *>(shared_);
-    const int units = a.one ? a.tpr : a.cs;
-    float *stat = shared + (size_t)2 * a.rpp * units;
-    const Place at(a, N);
-    Channel<N> ch;
-    ch.params(a, at);
-    float all_s[N], all_q[N]; // of the thread's channels over all its rows
-#pragma unroll
-    for (int i = 0; i < N; ++i) all_s[i] = all_q[i] = 0.0f;
-    T *dx = static_cast<T *>(a.dx);
-    auto group_part = [&](float (&s)[N], float (&q)[N], auto done) {
-        float ws[N], wq[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            all_s[i] += s[i], all_q[i] += q[i];
-            ws[i] = s[i] * ch.w[i], wq[i] = q[i] * ch.w[i];
-        }
-        if (a.dx) group_sums<N>(a, at, shared, ws, wq, done);
-    };
-    if ((int64_t)blockIdx.x >= a.shorts) {
-        const int64_t j = blockIdx.x - a.shorts;
-        for (int slot = 0; slot < kSlots; ++slot) {
-            const ChunkPart p(a, j, slot);
-            if (!p.any) continue;
-            float s[N], q[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[i] = q[i] = 0.0f;
-            if (at.m) {
-                saved_stats(a, at, p.graph, ch);
-                each_pair<T>(a, at, p.lo, p.hi, [&](int64_t, const Raw<T> &v, const Raw<T> &g) { add_pair<T, ACT, N>(v, g, ch, s, q); });
-            }
-            float *out = static_cast<float *>(a.part) + ((j * kSlots + slot) * a.groups + at.g0) * 2;
-            group_part(s, q, [&](int g, float s1, float q1) { out[g * 2] = s1, out[g * 2 + 1] = q1; });
-        }
-    } else {
-        for (int64_t graph = blockIdx.x; graph < a.graphs; graph += a.shorts) {
-            const int64_t lo = begin_of(a, graph), hi = begin_of(a, graph + 1);
-            if (hi <= lo || hi - lo > a.chunk) continue;
-            const float over = 1.0f / ((float)(hi - lo) * (float)a.cpg);
-            auto found = [&](int g, float s1, float q1) { stat[g * 2] = s1 * over, stat[g * 2 + 1] = q1 * over; };
-            float s[N], q[N], s1[N], s2[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[i] = q[i] = 0.0f;
-            if (at.m) saved_stats(a, at, graph, ch);
-            if (hi - lo <= (int64_t)kKeptBack * a.rpp) {
-                const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-                Raw<T> v[kKeptBack], d[kKeptBack];
-#pragma unroll
-                for (int k = 0; k < kKeptBack; ++k)
-                    if (lo + k * a.rpp < hi && at.m && lo + k * a.rpp + at.r < hi) {
-                        v[k] = raw(x + (lo + k * a.rpp + at.r) * a.xs + at.c, at.m);
-                        d[k] = raw(dy + (lo + k * a.rpp + at.r) * a.dys + at.c, at.m);
-                    }
-#pragma unroll
-                for (int k = 0; k < kKeptBack; ++k)
-                    if (lo + k * a.rpp < hi && at.m && lo + k * a.rpp + at.r < hi) add_pair<T, ACT, N>(v[k], d[k], ch, s, q);
-                group_part(s, q, found);
-                if (a.dx && at.m) {
-                    group_means(a, at, stat, s1, s2);
-#pragma unroll
-                    for (int k = 0; k < kKeptBack; ++k)
-                        if (lo + k * a.rpp < hi && lo + k * a.rpp + at.r < hi)
-                            put_dx<T, ACT, N>(v[k], d[k], ch, s1, s2, dx + (lo + k * a.rpp + at.r) * a.C + at.c, at.m);
-                }
-            } else {
-                if (at.m)
-                    each_pair<T>(a, at, lo, hi, [&](int64_t, const Raw<T> &v, const Raw<T> &g) { add_pair<T, ACT, N>(v, g, ch, s, q); });
-                group_part(s, q, found);
-                if (a.dx && at.m) {
-                    group_means(a, at, stat, s1, s2);
-                    each_pair<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v, const Raw<T> &g) {
-                        put_dx<T, ACT, N>(v, g, ch, s1, s2, dx + row * a.C + at.c, at.m);
-                    });
-                }
-            }
-            __syncthreads(); // stat is read
-        }
-    }
-    if (!a.sums) return;
-    // the workgroup's sums of each channel
+    const int teams = WAVE ? blockDim.x >> 6 : 1, R = a.sh.rpp * teams, r = at.r + (WAVE ? threadIdx.x >> 6 : 0) * a.sh.rpp;
     __syncthreads();
-    float *col = shared; // [2][rpp][cs]
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < at.m) {
-            col[at.r * a.cs + (int)at.c - at.c0 + i] = all_s[i];
-            col[(a.rpp + at.r) * a.cs + (int)at.c - at.c0 + i] = all_q[i];
+            col[r * a.sh.cs + (int)at.c - at.c0 + i] = cs[i];
+            col[(R + r) * a.sh.cs + (int)at.c - at.c0 + i] = cq[i];
         }
     __syncthreads();
-    for (int k = threadIdx.x; k < 2 * (at.c1 - at.c0); k += blockDim.x) {
-        const int which = k >= at.c1 - at.c0, c = k - which * (at.c1 - at.c0);
+    const int n = at.c1 - at.c0;
+    for (int k = threadIdx.x; k < 2 * n; k += blockDim.x) {
+        const int which = k >= n, c = k - which * n;
         float v = 0.0f;
-        for (int r = 0; r < a.rpp; ++r) v += col[(which * a.rpp + r) * a.cs + c];
-        a.sums[((int64_t)blockIdx.x * 2 + which) * a.C + at.c0 + c] = v;
+        for (int o = 0; o < R; ++o) v += col[(which * R + o) * a.sh.cs + c];
+        a.sums[(to * 2 + which) * a.C + at.c0 + c] = v;
     }
 }
 
-// dx of the chunks
-template <typename T, int ACT> __global__ void __launch_bounds__(kMost) norm_dx_kernel(NormArgs a)
+template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMost) norm_backward_kernel(NormArgs a)
 {
-    constexpr int N = kPer16<T>;
-    extern __shared__ double shared[];
-    float *stat = reinterpret_cast<float *>(shared);
-    const Place at(a, N);
+    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
+    extern __shared__ float room[];
+    const int each = a.sh.rpp * (ONE ? a.sh.tpr : a.sh.cs) * 2, teams = WAVE ? blockDim.x >> 6 : 1, team = WAVE ? threadIdx.x >> 6 : 0;
+    const Place<WAVE> at(a, N);
+    float *shared = room + (size_t)team * (each + 2 * at.ng), *stat = shared + each;
     Channel<N> ch;
     ch.params(a, at);
-    const int64_t j = blockIdx.x;
+    float cs[N], cq[N]; // of the thread's channels over all its rows
+#pragma unroll
+    for (int i = 0; i < N; ++i) cs[i] = cq[i] = 0.0f;
+    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
     T *dx = static_cast<T *>(a.dx);
+    const int rpp = a.sh.rpp;
+    for (int64_t graph = (int64_t)blockIdx.x * teams + team; graph < a.graphs; graph += (int64_t)a.shorts * teams) {
+        const int64_t lo = begin_of(a, graph), hi = begin_of(a, graph + 1);
+        if (hi <= lo || hi - lo > a.longer) continue;
+        const float over = 1.0f / ((float)(hi - lo) * (float)a.cpg);
+        auto found = [&](int g, float s1, float q1) { stat[g * 2] = s1 * over, stat[g * 2 + 1] = q1 * over; };
+        float s[A], q[A], s1[N], s2[N];
+#pragma unroll
+        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0f;
+        if (hi - lo <= (int64_t)kKept * rpp) {
+            const int mine = at.m && lo + at.r < hi ? ((int)(hi - lo) - at.r + rpp - 1) / rpp : 0;
+            Raw<T> v[kKept], d[kKept];
+#pragma unroll
+            for (int k = 0; k < kKept; ++k)
+                if (k < mine) {
+                    v[k] = raw(x + (lo + k * rpp + at.r) * a.xs + at.c, at.m);
+                    d[k] = raw(dy + (lo + k * rpp + at.r) * a.dys + at.c, at.m);
+                }
+            ch.stats_of(a, at, graph);
+#pragma unroll
+            for (int k = 0; k < kKept; ++k)
+                if (k < mine) add_pair<T, ONE>(a, v[k], d[k], ch, cs, cq, s, q);
+            if (!dx) continue; // the same for the whole launch
+            group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
+            group_means(a, at, stat, s1, s2);
+#pragma unroll
+            for (int k = 0; k < kKept; ++k)
+                if (k < mine) put_dx<T, N>(a, v[k], d[k], ch, s1, s2, dx + (lo + k * rpp + at.r) * a.C + at.c, at.m);
+        } else {
+            ch.stats_of(a, at, graph);
+            if (at.m) each_pair<T>(a, at, lo, hi, [&](int64_t, const Raw<T> &v, const Raw<T> &g) { add_pair<T, ONE>(a, v, g, ch, cs, cq, s, q); });
+            if (!dx) continue;
+            group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
+            group_means(a, at, stat, s1, s2);
+            if (at.m)
+                each_pair<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v, const Raw<T> &g) {
+                    put_dx<T, N>(a, v, g, ch, s1, s2, dx + row * a.C + at.c, at.m);
+                });
+        }
+        team_sync<WAVE>(); // stat is read
+    }
+    if (a.sums) put_sums(a, at, room, cs, cq, blockIdx.x);
+}
+
+template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_backward_chunk_kernel(NormArgs a)
+{
+    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
+    extern __shared__ float room[];
+    const Place<false> at(a, N);
+    Channel<N> ch;
+    ch.params(a, at);
+    float cs[N], cq[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) cs[i] = cq[i] = 0.0f;
+    const int64_t j = blockIdx.x;
     for (int slot = 0; slot < kSlots; ++slot) {
         const ChunkPart p(a, j, slot);
         if (!p.any) continue;
-        const float over = 1.0f / ((float)(p.end - p.first) * (float)a.cpg);
-        graph_sums<float>(a, at, p, [&](int g, float s, float q) { stat[g * 2] = s * over, stat[g * 2 + 1] = q * over; });
-        if (at.m) {
-            float s1[N], s2[N];
-            saved_stats(a, at, p.graph, ch);
-            group_means(a, at, stat, s1, s2);
-            each_pair<T>(a, at, p.lo, p.hi, [&](int64_t row, const Raw<T> &v, const Raw<T> &g) {
-                put_dx<T, ACT, N>(v, g, ch, s1, s2, dx + row * a.C + at.c, at.m);
-            });
-        }
-        __syncthreads();
+        float s[A], q[A];
+#pragma unroll
+        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0f;
+        ch.stats_of(a, at, p.graph);
+        if (at.m) each_pair<T>(a, at, p.lo, p.hi, [&](int64_t, const Raw<T> &v, const Raw<T> &g) { add_pair<T, ONE>(a, v, g, ch, cs, cq, s, q); });
+        float *out = static_cast<float *>(a.part) + ((j * kSlots + slot) * a.groups + at.g0) * 2;
+        if (a.dx) group_sums<false, ONE>(a, at, room, s, q, N, [&](int g, float s1, float q1) { out[g * 2] = s1, out[g * 2 + 1] = q1; });
+    }
+    if (a.sums) put_sums(a, at, room, cs, cq, a.shorts + j);
+}
+
+// dx of the chunks
+template <typename T> __global__ void __launch_bounds__(kMost) norm_dx_kernel(NormArgs a)
+{
+    constexpr int N = kPer16<T>;
+    const Place<false> at(a, N);
+    Channel<N> ch;
+    ch.params(a, at);
+    const int64_t j = gridDim.x - 1 - blockIdx.x;
+    T *dx = static_cast<T *>(a.dx);
+    for (int slot = 0; slot < kSlots; ++slot) {
+        const ChunkPart p(a, j, slot);
+        if (!p.any || !at.m) continue;
+        float s1[N], s2[N];
+        ch.stats_of(a, at, p.graph);
+        group_means(a, at, a.means + (p.graph * a.groups + at.g0) * 2, s1, s2);
+        each_pair<T>(a, at, p.lo, p.hi, [&](int64_t row, const Raw<T> &v, const Raw<T> &g) {
+            put_dx<T, N>(a, v, g, ch, s1, s2, dx + row * a.C + at.c, at.m);
+        });
     }
 }
 
-// dweight and dbias: column sums of [groups of workgroups][2][C], 32 columns to a workgroup
+// dweight and dbias: column sums of [workgroups][2][C], 32 columns to a workgroup; behind those the sums of long graphs' groups
 constexpr int kSumRows = 32;
-__global__ void __launch_bounds__(1024) norm_params_kernel(const float *sums, int64_t n, int64_t C, void *dw, void *db, int ptype)
+__global__ void __launch_bounds__(1024) norm_finish_kernel(NormArgs a, int columns)
 {
     __shared__ float part[kSumRows][33];
+    if ((int)blockIdx.x >= columns) {
+        if (threadIdx.x >= 32 * kGroupsOf) return;
+        const int parts = (a.groups + kGroupsOf - 1) / kGroupsOf, k = blockIdx.x - columns;
+        add_chunks<float>(a, k / parts, (int64_t)(k % parts) * kGroupsOf + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, float s, float q) {
+            const float over = 1.0f / ((float)rows * (float)a.cpg);
+            a.means[(graph * a.groups + g) * 2] = s * over, a.means[(graph * a.groups + g) * 2 + 1] = q * over;
+        });
+        return;
+    }
     const int lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-    const int64_t k = (int64_t)blockIdx.x * 32 + lane; // column of 2 C
+    const int64_t k = (int64_t)blockIdx.x * 32 + lane, n = (int64_t)a.shorts + a.chunks; // column of 2 C
     float v = 0.0f;
-    if (k < 2 * C) {
+    if (k < 2 * a.C) {
 #pragma unroll 8
-        for (int64_t i = r; i < n; i += kSumRows) v += sums[i * 2 * C + k];
+        for (int64_t i = r; i < n; i += kSumRows) v += a.sums[i * 2 * a.C + k];
     }
     part[r][lane] = v;
     __syncthreads();
-    if (r == 0 && k < 2 * C) {
+    if (r == 0 && k < 2 * a.C) {
         for (int o = 1; o < kSumRows; ++o) v += part[o][lane];
-        void *to = k < C ? db : dw;
-        if (to) put_param(to, ptype, k < C ? k : k - C, v);
+        void *to = k < a.C ? a.db : a.dw;
+        if (to) put_param(to, a.ptype, k < a.C ? k : k - a.C, v);
     }
 }
 
 // ---------------------------------------------------------------------------------- launch shapes
+// n: numbers of 16 bytes.  A slice is as many whole groups as `team` threads have 16-byte pieces of a row for, or fewer: halved while
+// `count` workgroups a slice are too few and a row's piece stays a line.
+Shape shape_of(const pcsr_norm_t &a, int n, int threads, int team, int64_t count, int want)
+{
+    const int cpg = (int)(a.channels / a.groups), size = 16 / n;
+    int64_t gs = a.groups;
+    while (gs > 1 && (gs * cpg + n - 1) / n > team) gs = (gs + 1) / 2;
+    while (gs > 1 && count * ((a.groups + gs - 1) / gs) < want && (gs + 1) / 2 * cpg * size >= 128) gs = (gs + 1) / 2;
+    Shape s;
+    s.threads = threads, s.team = team;
+    s.cs = (int)(gs * cpg), s.slices = (int)((a.groups + gs - 1) / gs);
+    s.tpr = (s.cs + n - 1) / n, s.rpp = team / s.tpr;
+    s.lanes = 1;
+    while (s.lanes < 64 && s.lanes * 2 * gs <= team) s.lanes *= 2;
+    return s;
+}
 struct NormPlan {
-    int threads, slices;
-    int shorts, chunks, cs, tpr, rpp, one, lanes;
-    int64_t chunk;
+    Shape few, many; // for short graphs, for chunks
+    int64_t longer, chunk;
+    int shorts, chunks;
+    bool one, wave;
 };
-
-
-// n: numbers of 16 bytes.  Few rows are cut into slices of whole groups, so that more workgroups have them.
 NormPlan norm_plan(const pcsr_norm_t &a, int n, bool backward)
 {
     NormPlan q;
-    const int cpg = (int)(a.channels / a.groups);
-    const int64_t mean = a.rows / (a.graphs > 0 ? a.graphs : 1);
-    const int size = 16 / n, kept = backward ? kKeptBack : kKept;
-    const int64_t bytes = mean * a.channels * size;
-    q.threads = bytes <= 64 * 16 * 8 ? 64 : bytes <= 256 * 16 * 8 ? 256 : kMost;
-    // a slice: whole groups, a thread to each 16 bytes of a row
-    int64_t gs = a.groups;
-    auto too_wide = [&](int64_t g) { return (g * cpg + n - 1) / n > q.threads; };
-    while (gs > 1 && too_wide(gs)) gs = (gs + 1) / 2;
-    while (q.threads < kMost && too_wide(gs)) q.threads *= 2;
-    const int64_t count = a.graphs > 256 ? a.graphs : a.rows * a.channels * size / (64 << 10) + a.graphs;
-    while (gs > 1 && count * ((a.groups + gs - 1) / gs) < 512 && (gs + 1) / 2 * cpg * size >= 128) gs = (gs + 1) / 2;
-    q.cs = (int)(gs * cpg);
-    q.slices = (int)((a.groups + gs - 1) / gs);
-    q.tpr = (q.cs + n - 1) / n;
-    q.rpp = q.threads / q.tpr;
+    const int cpg = (int)(a.channels / a.groups), size = 16 / n;
+    const int64_t mean = a.rows / (a.graphs > 0 ? a.graphs : 1), bytes = mean * a.channels * size, pieces = (cpg + n - 1) / n;
     q.one = cpg % n == 0;
-    q.lanes = 1;
-    while (q.lanes < 64 && q.lanes * 2 * gs <= q.threads) q.lanes *= 2;
-    const int64_t target = q.threads == 64 ? 4096 : q.threads == 256 ? 1024 : 512, keeps = (int64_t)kept * q.rpp;
-    q.chunk = (a.rows + target - 1) / target;
-    if (q.chunk < keeps) q.chunk = keeps;
+    const int64_t most = kMost;
+    q.wave = a.graphs >= 512 && pieces <= 64 && bytes <= 64 * 16 * kKept;
+    if (q.wave) {
+        q.few = shape_of(a, n, 256, 64, a.graphs, 0);
+    } else {
+        const int t = bytes <= 256 * 16 * kKept && pieces <= 256 ? 256 : (int)most;
+        q.few = shape_of(a, n, t, t, a.graphs, 512);
+    }
+    const int t = pieces <= 256 ? 256 : (int)most;
+    q.many = shape_of(a, n, t, t, 1024, 0);
+    const int64_t keeps = (int64_t)kKept * q.few.rpp, least = (int64_t)kAhead * q.many.rpp;
+    q.chunk = (a.rows + 1023) / 1024;
+    if (q.chunk < least) q.chunk = least;
+    q.longer = keeps > q.chunk ? keeps : q.chunk;
     const bool known = !a.offsets || a.graphs == 1; // every graph has `mean` rows
-    const bool any_short = !known || mean <= q.chunk, any_long = known ? mean > q.chunk : a.rows > q.chunk;
-    const int64_t most = backward ? 4096 * 64 / q.threads : a.graphs;
-    q.shorts = any_short ? (int)(a.graphs < most ? a.graphs : most) : 0;
+    const bool any_short = !known || mean <= q.longer, any_long = known ? mean > q.longer : a.rows > q.longer;
+    const int teams = q.few.threads / q.few.team;
+    const int64_t groups = (a.graphs + teams - 1) / teams, cap = backward ? 4096 : groups;
+    q.shorts = any_short ? (int)(groups < cap ? groups : cap) : 0;
     q.chunks = any_long ? (int)((a.rows + q.chunk - 1) / q.chunk) : 0;
     return q;
 }
@@ -634,26 +726,30 @@ NormArgs norm_args(const pcsr_norm_t &a, const NormPlan &q, void *ws)
     NormArgs p = {};
     p.rows = a.rows, p.C = a.channels, p.graphs = a.graphs, p.length = a.graphs ? a.rows / a.graphs : 0;
     p.groups = (int)a.groups, p.cpg = (int)(a.channels / a.groups);
-    p.offsets = a.graphs == 1 ? nullptr : a.offsets, p.wide = a.wide, p.ptype = a.param_type;
+    p.offsets = a.graphs == 1 ? nullptr : a.offsets, p.wide = a.wide, p.ptype = a.param_type, p.act = a.act;
     p.x = a.x, p.xs = a.x_stride, p.w = a.weight, p.b = a.bias, p.eps = a.eps, p.mean = a.mean, p.rstd = a.rstd;
-    p.chunk = q.chunk, p.shorts = q.shorts, p.chunks = q.chunks, p.cs = q.cs, p.tpr = q.tpr, p.rpp = q.rpp, p.one = q.one, p.lanes = q.lanes;
+    p.longer = q.longer, p.chunk = q.chunk, p.shorts = q.shorts, p.chunks = q.chunks;
     p.part = ws;
     return p;
 }
 
-template <typename F> int for_act(int act, F f)
-{
-    switch (act) {
-    case PCSR_ACT_RELU: return f(std::integral_constant<int, PCSR_ACT_RELU>{});
-    case PCSR_ACT_SILU: return f(std::integral_constant<int, PCSR_ACT_SILU>{});
-    case PCSR_ACT_GELU: return f(std::integral_constant<int, PCSR_ACT_GELU>{});
+struct NormSpace { // of the workspace
+    int64_t part, means, sums, bytes;
+    NormSpace(const pcsr_norm_t &a, const NormPlan &q, bool backward)
+    {
+        auto up = [](int64_t b) { return (b + 15) / 16 * 16; };
+        part = 0;
+        means = up((int64_t)q.chunks * kSlots * a.groups * 2 * (backward ? 4 : 8));
+        sums = means + (backward && q.chunks ? up(a.graphs * a.groups * 8) : 0);
+        bytes = sums + (backward ? ((int64_t)q.shorts + q.chunks) * 2 * a.channels * 4 : 0);
     }
-    return f(std::integral_constant<int, PCSR_ACT_NONE>{});
-}
+};
 
-int64_t part_bytes(const pcsr_norm_t &a, const NormPlan &q, bool backward)
+// f<ONE, WAVE>
+template <typename F> int for_plan(const NormPlan &q, F f)
 {
-    return ((int64_t)q.chunks * kSlots * a.groups * 2 * (backward ? 4 : 8) + 15) / 16 * 16;
+    if (q.one) return q.wave ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+    return q.wave ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
 
 } // namespace
@@ -666,8 +762,7 @@ extern "C" {
 int64_t pcsr_norm_workspace(const pcsr_norm_t *a, int32_t backward)
 {
     if (!norm_sizes_ok(a) || a->rows == 0 || a->channels / a->groups > widest(a->type)) return 0;
-    const NormPlan q = norm_plan(*a, a->type == PCSR_F32 ? 4 : 8, backward);
-    return part_bytes(*a, q, backward) + (backward ? ((int64_t)q.shorts + q.chunks) * 2 * a->channels * 4 : 0);
+    return NormSpace(*a, norm_plan(*a, a->type == PCSR_F32 ? 4 : 8, backward), backward).bytes;
 }
 
 int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
@@ -682,12 +777,23 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
         if (!y || (q.chunks && !ws)) return (int)PCSR_E_INVALID_ARG;
         NormArgs p = norm_args(*a, q, ws);
         p.y = y;
-        const size_t stat = sizeof(float) * 2 * (q.cs / p.cpg), lds = sizeof(double) * 2 * q.rpp * (q.one ? q.tpr : q.cs) + stat;
-        return for_act(a->act, [&](auto v) {
-            constexpr int ACT = decltype(v)::value;
-            if (!allow_lds(&norm_kernel<T, ACT>, lds)) return (int)PCSR_E_HIP;
-            hipLaunchKernelGGL((norm_kernel<T, ACT>), dim3(q.shorts + q.chunks, q.slices), dim3(q.threads), lds, s, p);
-            if (q.chunks) hipLaunchKernelGGL((norm_apply_kernel<T, ACT>), dim3(q.chunks, q.slices), dim3(q.threads), stat, s, p);
+        return for_plan(q, [&](auto one, auto wave) {
+            constexpr bool ONE = decltype(one)::value, WAVE = decltype(wave)::value;
+            auto lds = [&](const Shape &sh, bool stat) {
+                return sizeof(double) * (sh.threads / sh.team) * ((size_t)2 * sh.rpp * (ONE ? sh.tpr : sh.cs) + (stat ? sh.cs / p.cpg : 0));
+            };
+            if (q.shorts) {
+                p.sh = q.few;
+                if (!allow_lds(&norm_kernel<T, ONE, WAVE>, lds(p.sh, true))) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_kernel<T, ONE, WAVE>), dim3(q.shorts, p.sh.slices), dim3(p.sh.threads), lds(p.sh, true), s, p);
+            }
+            if (q.chunks) {
+                p.sh = q.many;
+                if (!allow_lds(&norm_chunk_kernel<T, ONE>, lds(p.sh, false))) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_chunk_kernel<T, ONE>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), lds(p.sh, false), s, p);
+                hipLaunchKernelGGL(norm_combine_kernel, dim3(q.chunks, (p.groups + kGroupsOf - 1) / kGroupsOf), dim3(32 * kGroupsOf), 0, s, p);
+                hipLaunchKernelGGL((norm_apply_kernel<T>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), 0, s, p);
+            }
             return launched();
         });
     });
@@ -703,29 +809,38 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
     if (a->rows && (!dy || dy_stride < a->channels)) return PCSR_E_INVALID_ARG;
     if (dy_stride > (int64_t(1) << 31)) return PCSR_E_TOO_LARGE;
     if (!dx && !sums) return PCSR_OK;
-    const unsigned columns = (unsigned)((2 * a->channels + 31) / 32);
-    if (a->rows == 0) {
-        if (sums) hipLaunchKernelGGL(norm_params_kernel, dim3(columns), dim3(1024), 0, s, nullptr, 0, a->channels, dweight, dbias, a->param_type);
-        return launched();
-    }
+    const int columns = sums ? (int)((2 * a->channels + 31) / 32) : 0;
     return for_type(a->type, [&](auto t) {
         typedef decltype(t) T;
-        const NormPlan q = norm_plan(*a, kPer16<T>, true);
-        if (!ws && (q.chunks || sums)) return (int)PCSR_E_INVALID_ARG;
+        NormPlan q = {};
+        if (a->rows) q = norm_plan(*a, kPer16<T>, true);
+        const NormSpace w(*a, q, true);
+        if (!ws && a->rows && (q.chunks || sums)) return (int)PCSR_E_INVALID_ARG;
         NormArgs p = norm_args(*a, q, ws);
-        p.dy = dy, p.dys = dy_stride, p.dx = dx;
-        p.sums = sums ? reinterpret_cast<float *>(static_cast<char *>(ws) + part_bytes(*a, q, true)) : nullptr;
-        const size_t stat = sizeof(float) * 2 * (q.cs / p.cpg);
-        const size_t first = sizeof(float) * 2 * q.rpp * (q.one ? q.tpr : q.cs) + stat, col = sizeof(float) * 2 * q.rpp * q.cs;
-        const size_t lds = sums && col > first ? col : first;
-        return for_act(a->act, [&](auto v) {
-            constexpr int ACT = decltype(v)::value;
-            if (!allow_lds(&norm_backward_kernel<T, ACT>, lds)) return (int)PCSR_E_HIP;
-            hipLaunchKernelGGL((norm_backward_kernel<T, ACT>), dim3(q.shorts + q.chunks, q.slices), dim3(q.threads), lds, s, p);
-            if (q.chunks && dx) hipLaunchKernelGGL((norm_dx_kernel<T, ACT>), dim3(q.chunks, q.slices), dim3(q.threads), stat, s, p);
-            if (sums)
-                hipLaunchKernelGGL(norm_params_kernel, dim3(columns), dim3(1024), 0, s, p.sums, (int64_t)q.shorts + q.chunks, a->channels, dweight, dbias,
-                                   a->param_type);
+        char *at = static_cast<char *>(ws);
+        p.dy = dy, p.dys = dy_stride, p.dx = dx, p.dw = dweight, p.db = dbias;
+        p.sums = sums ? reinterpret_cast<float *>(at + w.sums) : nullptr;
+        p.means = reinterpret_cast<float *>(at + w.means);
+        return for_plan(q, [&](auto one, auto wave) {
+            constexpr bool ONE = decltype(one)::value, WAVE = decltype(wave)::value;
+            auto lds = [&](const Shape &sh, bool stat) {
+                const size_t teams = sh.threads / sh.team, pairs = teams * ((size_t)2 * sh.rpp * (ONE ? sh.tpr : sh.cs) + (stat ? 2 * (sh.cs / p.cpg) : 0));
+                const size_t col = sums ? teams * 2 * sh.rpp * sh.cs : 0;
+                return sizeof(float) * (pairs > col ? pairs : col);
+            };
+            if (q.shorts) {
+                p.sh = q.few;
+                if (!allow_lds(&norm_backward_kernel<T, ONE, WAVE>, lds(p.sh, true))) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_backward_kernel<T, ONE, WAVE>), dim3(q.shorts, p.sh.slices), dim3(p.sh.threads), lds(p.sh, true), s, p);
+            }
+            if (q.chunks) {
+                p.sh = q.many;
+                if (!allow_lds(&norm_backward_chunk_kernel<T, ONE>, lds(p.sh, false))) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_backward_chunk_kernel<T, ONE>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), lds(p.sh, false), s, p);
+            }
+            const int more = dx ? q.chunks * ((p.groups + kGroupsOf - 1) / kGroupsOf) : 0;
+            if (columns + more) hipLaunchKernelGGL(norm_finish_kernel, dim3(columns + more), dim3(1024), 0, s, p, columns);
+            if (dx && q.chunks) hipLaunchKernelGGL((norm_dx_kernel<T>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), 0, s, p);
             return launched();
         });
     });

@@ -21,7 +21,7 @@ int pcsr_embed(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids
                int64_t stride, float scale, void *out, void *stream);
 // grad[rows x d] = scale * the sum of dout[i] over the i with ids[i] = row, in 32 bits in an order that n, rows and d
 // alone decide, rounded once; zeros for rows without an id.  Rows of dout are `stride` numbers apart.
-// ws: pcsr_embed_workspace bytes, 16-byte aligned.
+// ws: pcsr_embed_workspace bytes (0 for few ids), 16-byte aligned.
 int64_t pcsr_embed_workspace(int64_t n, int64_t rows, int64_t d);
 int pcsr_embed_backward(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids, int32_t wide,
                         const void *dout, int64_t stride, float scale, void *grad, void *ws, void *stream);
