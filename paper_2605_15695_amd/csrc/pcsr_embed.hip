@@ -19,7 +19,7 @@ constexpr int kAhead = 4;        // rows of the table a group of lanes has on th
 constexpr int kRankMost = 16384; // ids that are sorted by counting the smaller ones
 constexpr int kRankT = 1024;     // threads of that
 constexpr int kRankKeys = 8192;  // of their keys in LDS at a time
-constexpr int kTile = 2048;      // ids a workgroup of a sorting pass holds in registers
+constexpr int kTile = 1024;      // ids a workgroup of a sorting pass holds in registers
 constexpr int kTiles = 512;      // workgroups of a sorting pass at most
 constexpr int kDigit = 11;       // bits of a sorting pass at most
 constexpr int kRounds = kTile / kT;
@@ -82,7 +82,9 @@ template <typename I> __device__ __forceinline__ uint32_t key_of(const void *ids
     return (uint32_t)(id >= 0 && id < rows ? id : rows);
 }
 
-struct Fill { // zeros, by the workgroups behind those that sort
+// Zeros, by the workgroups behind those that sort: sorting waits for its round trips and leaves the memory idle, so every launch of it has
+// a share.
+struct Fill {
     char *p;
     int64_t bytes;
 };
@@ -196,8 +198,12 @@ __device__ __forceinline__ int32_t wave_upto(int32_t v, int lane)
 }
 
 // counts of a digit, summed over the tiles before (in place); its total
-__global__ void __launch_bounds__(kT) tiles_kernel(int bins, int tiles, int32_t *counts, int32_t *totals)
+__global__ void __launch_bounds__(kT) tiles_kernel(int bins, int tiles, int32_t *counts, int32_t *totals, int sorters, Fill f)
 {
+    if ((int)blockIdx.x >= sorters) {
+        fill(f, blockIdx.x - sorters, gridDim.x - sorters);
+        return;
+    }
     const int lane = threadIdx.x & 63, d = blockIdx.x * (kT / 64) + (threadIdx.x >> 6);
     if (d >= bins) return;
     int32_t *row = counts + (int64_t)d * tiles;
@@ -213,8 +219,12 @@ __global__ void __launch_bounds__(kT) tiles_kernel(int bins, int tiles, int32_t 
 
 // A wavefront ranks 64 ids at a time by ballots over the digit's bits, in the order they come, and keeps its own
 // running counts; the wavefronts' counts are then added up in order.
-template <typename I, bool FIRST> __global__ void __launch_bounds__(kT) scatter_kernel(SortArgs p)
+template <typename I, bool FIRST> __global__ void __launch_bounds__(kT) scatter_kernel(SortArgs p, Fill f)
 {
+    if ((int)blockIdx.x >= p.tiles) {
+        fill(f, blockIdx.x - p.tiles, gridDim.x - p.tiles);
+        return;
+    }
     constexpr int W = kT / 64, N = (1 << kDigit) / kT;
     __shared__ int32_t cnt[W][1 << kDigit];
     __shared__ int32_t next[1 << kDigit]; // where the next id of a digit goes
@@ -691,12 +701,14 @@ template <typename T, typename I> struct Own {
 template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, const GradPlan &q, const GradSpace &w, char *ws, Fill f,
                                    hipStream_t s)
 {
-    const int64_t want = (f.bytes / 16 + kT * 4 - 1) / (kT * 4);
-    const unsigned fillers = (unsigned)(want < 1 ? 1 : want > 2048 ? 2048 : want);
+    const auto fillers = [](int64_t bytes, int threads) {
+        const int64_t want = (bytes / 16 + threads * 4 - 1) / (threads * 4), most = 2048 * kT / threads;
+        return (unsigned)(want < most ? want : most);
+    };
     uint32_t *key = reinterpret_cast<uint32_t *>(ws + w.key), *pos = reinterpret_cast<uint32_t *>(ws + w.pos);
     if (n <= kRankMost) {
         const int sorters = (int)((n + 63) / 64);
-        hipLaunchKernelGGL((rank_kernel<I>), dim3(sorters + (fillers + 3) / 4), dim3(kRankT), 0, s, n, rows, ids, key, pos,
+        hipLaunchKernelGGL((rank_kernel<I>), dim3(sorters + fillers(f.bytes, kRankT)), dim3(kRankT), 0, s, n, rows, ids, key, pos,
                            sorters, f);
         return PCSR_OK;
     }
@@ -704,23 +716,40 @@ template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, con
     p.n = n, p.chunk = q.chunk, p.rows = rows, p.bits = q.bits, p.tiles = q.tiles, p.ids = ids;
     p.counts = reinterpret_cast<int32_t *>(ws + w.counts), p.totals = reinterpret_cast<int32_t *>(ws + w.totals);
     uint32_t *key2 = reinterpret_cast<uint32_t *>(ws + w.key2), *pos2 = reinterpret_cast<uint32_t *>(ws + w.pos2);
+    // shares of the zeros, as long as the launches take without (300,000 ids: 6, 4 and 12 us)
+    constexpr int kShares[3] = {3, 2, 5};
+    int64_t filled = 0;
+    int parts = 0;
+    const auto share = [&](int which) {
+        parts += kShares[which];
+        int64_t to = f.bytes * parts / (10 * q.passes) / 4096 * 4096;
+        if (parts == 10 * q.passes) to = f.bytes;
+        const Fill part = {f.p + filled, to - filled};
+        filled = to;
+        return part;
+    };
     for (int i = 0; i < q.passes; ++i) {
         p.shift = i * q.bits;
         p.kin = p.kout, p.vin = p.vout;
         const bool here = (q.passes - 1 - i) % 2 == 0; // the last pass ends in key and pos
         p.kout = here ? key : key2, p.vout = here ? pos : pos2;
+        Fill part = share(0);
+        dim3 grid(p.tiles + fillers(part.bytes, kT));
         if (i == 0) {
             p.kin = p.vin = nullptr;
-            hipLaunchKernelGGL((count_kernel<I, true>), dim3(p.tiles + fillers), dim3(kT), 0, s, p, f);
+            hipLaunchKernelGGL((count_kernel<I, true>), grid, dim3(kT), 0, s, p, part);
         } else {
-            hipLaunchKernelGGL((count_kernel<I, false>), dim3(p.tiles), dim3(kT), 0, s, p, f);
+            hipLaunchKernelGGL((count_kernel<I, false>), grid, dim3(kT), 0, s, p, part);
         }
-        const int bins = 1 << p.bits;
-        hipLaunchKernelGGL(tiles_kernel, dim3((bins + kT / 64 - 1) / (kT / 64)), dim3(kT), 0, s, bins, p.tiles, p.counts, p.totals);
+        const int bins = 1 << p.bits, sorters = (bins + kT / 64 - 1) / (kT / 64);
+        part = share(1);
+        hipLaunchKernelGGL(tiles_kernel, dim3(sorters + fillers(part.bytes, kT)), dim3(kT), 0, s, bins, p.tiles, p.counts, p.totals, sorters, part);
+        part = share(2);
+        grid = dim3(p.tiles + fillers(part.bytes, kT));
         if (i == 0)
-            hipLaunchKernelGGL((scatter_kernel<I, true>), dim3(p.tiles), dim3(kT), 0, s, p);
+            hipLaunchKernelGGL((scatter_kernel<I, true>), grid, dim3(kT), 0, s, p, part);
         else
-            hipLaunchKernelGGL((scatter_kernel<I, false>), dim3(p.tiles), dim3(kT), 0, s, p);
+            hipLaunchKernelGGL((scatter_kernel<I, false>), grid, dim3(kT), 0, s, p, part);
     }
     return PCSR_OK;
 }

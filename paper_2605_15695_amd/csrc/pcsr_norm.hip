@@ -50,7 +50,7 @@ struct NormArgs {
     float *means; // [graphs][groups][2]: S1 / m and S2 / m of long graphs
     void *dw, *db;
     // shape of the launch
-    Shape sh;
+    Shape few, many; // for short graphs, for chunks
     int64_t longer, chunk; // a graph of more rows is long; rows of a chunk, no more than that
     int shorts, chunks;    // workgroups for short graphs, for chunks
     void *part;            // [chunk][kSlots][groups] pairs of doubles (forward) or floats (backward)
@@ -163,14 +163,15 @@ template <bool WAVE> struct Place {
     int r, unit, m;  // row of a pass, 16-byte piece of the row, channels of it (0: the thread has none)
     int64_t c;       // first channel
     int c0, c1, g0, ng; // the slice's channels and groups
-    __device__ Place(const NormArgs &a, int per16)
+    const Shape &sh;
+    __device__ Place(const NormArgs &a, const Shape &of, int per16) : sh(of)
     {
         t = WAVE ? threadIdx.x & 63 : threadIdx.x;
-        c0 = blockIdx.y * a.sh.cs, c1 = c0 + a.sh.cs < a.C ? c0 + a.sh.cs : (int)a.C;
+        c0 = blockIdx.y * sh.cs, c1 = c0 + sh.cs < a.C ? c0 + sh.cs : (int)a.C;
         g0 = c0 / a.cpg, ng = (c1 - c0) / a.cpg;
-        r = t / a.sh.tpr, unit = t - r * a.sh.tpr;
+        r = t / sh.tpr, unit = t - r * sh.tpr;
         c = c0 + unit * per16;
-        m = r < a.sh.rpp && c < c1 ? (c1 - (int)c < per16 ? c1 - (int)c : per16) : 0;
+        m = r < sh.rpp && c < c1 ? (c1 - (int)c < per16 ? c1 - (int)c : per16) : 0;
     }
 };
 // what was written to LDS can be read by the team
@@ -189,7 +190,7 @@ template <bool WAVE> __device__ __forceinline__ void team_sync()
 template <bool WAVE, bool ONE, int A, typename V, typename F>
 __device__ __forceinline__ void group_sums(const NormArgs &a, const Place<WAVE> &at, V *shared, const V (&s)[A], const V (&q)[A], int per16, F done)
 {
-    const Shape &sh = a.sh;
+    const Shape &sh = at.sh;
     const int units = ONE ? sh.tpr : sh.cs; // of a row
 #pragma unroll
     for (int i = 0; i < A; ++i)
@@ -272,7 +273,7 @@ template <typename T, bool WAVE, typename F>
 __device__ __forceinline__ void each_row(const NormArgs &a, const Place<WAVE> &at, int64_t lo, int64_t hi, F f)
 {
     const T *x = static_cast<const T *>(a.x);
-    const int rpp = a.sh.rpp;
+    const int rpp = at.sh.rpp;
     for (int64_t row = lo + at.r; row < hi; row += (int64_t)kAhead * rpp) {
         Raw<T> v[kAhead];
 #pragma unroll
@@ -288,7 +289,7 @@ __device__ __forceinline__ void each_pair(const NormArgs &a, const Place<WAVE> &
 {
     const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
     constexpr int U = kAhead / 2;
-    const int rpp = a.sh.rpp;
+    const int rpp = at.sh.rpp;
     for (int64_t row = lo + at.r; row < hi; row += (int64_t)U * rpp) {
         Raw<T> v[U], g[U];
 #pragma unroll
@@ -327,13 +328,43 @@ struct ChunkPart {
     }
 };
 
-// short graphs, one to a team
+// sums of a chunk
+template <typename T, bool ONE> __device__ __forceinline__ void chunk_sums(const NormArgs &a, int64_t j, double *memory)
+{
+    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
+    if ((int)blockIdx.y >= a.many.slices) return;
+    const Place<false> at(a, a.many, N);
+    for (int slot = 0; slot < kSlots; ++slot) {
+        const ChunkPart p(a, j, slot);
+        if (!p.any) continue;
+        double s[A], q[A];
+#pragma unroll
+        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0;
+        if (at.m) each_row<T>(a, at, p.lo, p.hi, [&](int64_t, const Raw<T> &v) { add_squares<T, ONE>(v, s, q); });
+        double *out = static_cast<double *>(a.part) + ((j * kSlots + slot) * a.groups + at.g0) * 2;
+        group_sums<false, ONE>(a, at, memory, s, q, N, [&](int g, double s1, double q1) { out[g * 2] = s1, out[g * 2 + 1] = q1; });
+    }
+}
+
+// chunks alone, with the registers that those need: 16 us for 34 of 16 x 4096 x 320 in bf16
+template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_chunk_kernel(NormArgs a)
+{
+    extern __shared__ double memory[];
+    chunk_sums<T, ONE>(a, blockIdx.x, memory);
+}
+
+// short graphs, one to a team; behind them the chunks of long ones
 template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMost) norm_kernel(NormArgs a)
 {
     constexpr int N = kPer16<T>, A = ONE ? 1 : N;
     extern __shared__ double memory[];
-    const int each = a.sh.rpp * (ONE ? a.sh.tpr : a.sh.cs) * 2, team = WAVE ? threadIdx.x >> 6 : 0;
-    const Place<WAVE> at(a, N);
+    if ((int)blockIdx.x >= a.shorts) {
+        chunk_sums<T, ONE>(a, blockIdx.x - a.shorts, memory);
+        return;
+    }
+    if ((int)blockIdx.y >= a.few.slices) return;
+    const int each = a.few.rpp * (ONE ? a.few.tpr : a.few.cs) * 2, team = WAVE ? threadIdx.x >> 6 : 0;
+    const Place<WAVE> at(a, a.few, N);
     double *shared = memory + (size_t)team * (each + at.ng);
     float *stat = reinterpret_cast<float *>(shared + each);
     const int64_t graph = WAVE ? (int64_t)blockIdx.x * (blockDim.x >> 6) + team : blockIdx.x;
@@ -347,7 +378,7 @@ template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMo
         a.mean[graph * a.groups + at.g0 + g] = mu, a.rstd[graph * a.groups + at.g0 + g] = rs;
     };
     T *y = static_cast<T *>(a.y);
-    const int rpp = a.sh.rpp;
+    const int rpp = a.few.rpp;
     double s[A], q[A];
 #pragma unroll
     for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0;
@@ -378,44 +409,33 @@ template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMo
     each_row<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v) { apply<T>(a, v, ch, y + row * a.C + at.c, at.m); });
 }
 
-// sums of a chunk
-template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_chunk_kernel(NormArgs a)
-{
-    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
-    extern __shared__ double memory[];
-    const Place<false> at(a, N);
-    const int64_t j = blockIdx.x;
-    for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
-        if (!p.any) continue;
-        double s[A], q[A];
-#pragma unroll
-        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0;
-        if (at.m) each_row<T>(a, at, p.lo, p.hi, [&](int64_t, const Raw<T> &v) { add_squares<T, ONE>(v, s, q); });
-        double *out = static_cast<double *>(a.part) + ((j * kSlots + slot) * a.groups + at.g0) * 2;
-        group_sums<false, ONE>(a, at, memory, s, q, N, [&](int g, double s1, double q1) { out[g * 2] = s1, out[g * 2 + 1] = q1; });
-    }
-}
-
-// For the long graphs that begin in chunk j: done(graph, its rows, group, pair), the pair added up over their chunks by 32 lanes.
+// done(graph, its rows, group, pair), the pair added up over the chunks by 32 lanes, for the long graphs that begin in chunk j; without
+// offsets for graph j.
 template <typename V, typename F> __device__ __forceinline__ void add_chunks(const NormArgs &a, int64_t j, int64_t group, F done)
 {
     const V *part = static_cast<const V *>(a.part);
     const int lane = threadIdx.x & 31;
-    for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
-        if (!p.any || p.lo != p.first) continue;
-        const int64_t j1 = (p.end - 1) / a.chunk;
+    const auto add = [&](int64_t graph, int64_t first, int64_t end) {
+        const int64_t j0 = first / a.chunk, j1 = (end - 1) / a.chunk;
+        const int slot = first > j0 * a.chunk; // in its first chunk; 0 in the others
         V s = 0, q = 0;
         if (group < a.groups) {
 #pragma unroll 8
-            for (int64_t k = j + lane; k <= j1; k += 32) {
-                const V *in = part + ((k * kSlots + (k == j ? slot : 0)) * a.groups + group) * 2;
+            for (int64_t k = j0 + lane; k <= j1; k += 32) {
+                const V *in = part + ((k * kSlots + (k == j0 ? slot : 0)) * a.groups + group) * 2;
                 s += in[0], q += in[1];
             }
         }
         for (int m = 1; m < 32; m <<= 1) s += __shfl_xor(s, m), q += __shfl_xor(q, m);
-        if (lane == 0 && group < a.groups) done(p.graph, p.end - p.first, group, s, q);
+        if (lane == 0 && group < a.groups) done(graph, end - first, group, s, q);
+    };
+    if (!a.offsets) {
+        add(j, j * a.length, (j + 1) * a.length);
+        return;
+    }
+    for (int slot = 0; slot < kSlots; ++slot) {
+        const ChunkPart p(a, j, slot);
+        if (p.any && p.lo == p.first) add(p.graph, p.first, p.end);
     }
 }
 __global__ void __launch_bounds__(32 * kGroupsOf) norm_combine_kernel(NormArgs a)
@@ -428,7 +448,7 @@ __global__ void __launch_bounds__(32 * kGroupsOf) norm_combine_kernel(NormArgs a
 template <typename T> __global__ void __launch_bounds__(kMost) norm_apply_kernel(NormArgs a)
 {
     constexpr int N = kPer16<T>;
-    const Place<false> at(a, N);
+    const Place<false> at(a, a.many, N);
     Channel<N> ch;
     ch.params(a, at);
     const int64_t j = gridDim.x - 1 - blockIdx.x;
@@ -498,93 +518,35 @@ __device__ __forceinline__ void group_means(const NormArgs &a, const Place<WAVE>
 template <bool WAVE, int N>
 __device__ __forceinline__ void put_sums(const NormArgs &a, const Place<WAVE> &at, float *col, const float (&cs)[N], const float (&cq)[N], int64_t to)
 {
-    const int teams = WAVE ? blockDim.x >> 6 : 1, R = a.sh.rpp * teams, r = at.r + (WAVE ? threadIdx.x >> 6 : 0) * a.sh.rpp;
+    const Shape &sh = at.sh;
+    const int teams = WAVE ? blockDim.x >> 6 : 1, R = sh.rpp * teams, r = at.r + (WAVE ? threadIdx.x >> 6 : 0) * sh.rpp;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < at.m) {
-            col[r * a.sh.cs + (int)at.c - at.c0 + i] = cs[i];
-            col[(R + r) * a.sh.cs + (int)at.c - at.c0 + i] = cq[i];
+            col[r * sh.cs + (int)at.c - at.c0 + i] = cs[i];
+            col[(R + r) * sh.cs + (int)at.c - at.c0 + i] = cq[i];
         }
     __syncthreads();
     const int n = at.c1 - at.c0;
     for (int k = threadIdx.x; k < 2 * n; k += blockDim.x) {
         const int which = k >= n, c = k - which * n;
         float v = 0.0f;
-        for (int o = 0; o < R; ++o) v += col[(which * R + o) * a.sh.cs + c];
+        for (int o = 0; o < R; ++o) v += col[(which * R + o) * sh.cs + c];
         a.sums[(to * 2 + which) * a.C + at.c0 + c] = v;
     }
 }
 
-template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMost) norm_backward_kernel(NormArgs a)
+template <typename T, bool ONE> __device__ __forceinline__ void chunk_gradients(const NormArgs &a, int64_t j, float *room)
 {
     constexpr int N = kPer16<T>, A = ONE ? 1 : N;
-    extern __shared__ float room[];
-    const int each = a.sh.rpp * (ONE ? a.sh.tpr : a.sh.cs) * 2, teams = WAVE ? blockDim.x >> 6 : 1, team = WAVE ? threadIdx.x >> 6 : 0;
-    const Place<WAVE> at(a, N);
-    float *shared = room + (size_t)team * (each + 2 * at.ng), *stat = shared + each;
-    Channel<N> ch;
-    ch.params(a, at);
-    float cs[N], cq[N]; // of the thread's channels over all its rows
-#pragma unroll
-    for (int i = 0; i < N; ++i) cs[i] = cq[i] = 0.0f;
-    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-    T *dx = static_cast<T *>(a.dx);
-    const int rpp = a.sh.rpp;
-    for (int64_t graph = (int64_t)blockIdx.x * teams + team; graph < a.graphs; graph += (int64_t)a.shorts * teams) {
-        const int64_t lo = begin_of(a, graph), hi = begin_of(a, graph + 1);
-        if (hi <= lo || hi - lo > a.longer) continue;
-        const float over = 1.0f / ((float)(hi - lo) * (float)a.cpg);
-        auto found = [&](int g, float s1, float q1) { stat[g * 2] = s1 * over, stat[g * 2 + 1] = q1 * over; };
-        float s[A], q[A], s1[N], s2[N];
-#pragma unroll
-        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0f;
-        if (hi - lo <= (int64_t)kKept * rpp) {
-            const int mine = at.m && lo + at.r < hi ? ((int)(hi - lo) - at.r + rpp - 1) / rpp : 0;
-            Raw<T> v[kKept], d[kKept];
-#pragma unroll
-            for (int k = 0; k < kKept; ++k)
-                if (k < mine) {
-                    v[k] = raw(x + (lo + k * rpp + at.r) * a.xs + at.c, at.m);
-                    d[k] = raw(dy + (lo + k * rpp + at.r) * a.dys + at.c, at.m);
-                }
-            ch.stats_of(a, at, graph);
-#pragma unroll
-            for (int k = 0; k < kKept; ++k)
-                if (k < mine) add_pair<T, ONE>(a, v[k], d[k], ch, cs, cq, s, q);
-            if (!dx) continue; // the same for the whole launch
-            group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
-            group_means(a, at, stat, s1, s2);
-#pragma unroll
-            for (int k = 0; k < kKept; ++k)
-                if (k < mine) put_dx<T, N>(a, v[k], d[k], ch, s1, s2, dx + (lo + k * rpp + at.r) * a.C + at.c, at.m);
-        } else {
-            ch.stats_of(a, at, graph);
-            if (at.m) each_pair<T>(a, at, lo, hi, [&](int64_t, const Raw<T> &v, const Raw<T> &g) { add_pair<T, ONE>(a, v, g, ch, cs, cq, s, q); });
-            if (!dx) continue;
-            group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
-            group_means(a, at, stat, s1, s2);
-            if (at.m)
-                each_pair<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v, const Raw<T> &g) {
-                    put_dx<T, N>(a, v, g, ch, s1, s2, dx + row * a.C + at.c, at.m);
-                });
-        }
-        team_sync<WAVE>(); // stat is read
-    }
-    if (a.sums) put_sums(a, at, room, cs, cq, blockIdx.x);
-}
-
-template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_backward_chunk_kernel(NormArgs a)
-{
-    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
-    extern __shared__ float room[];
-    const Place<false> at(a, N);
+    if ((int)blockIdx.y >= a.many.slices) return;
+    const Place<false> at(a, a.many, N);
     Channel<N> ch;
     ch.params(a, at);
     float cs[N], cq[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) cs[i] = cq[i] = 0.0f;
-    const int64_t j = blockIdx.x;
     for (int slot = 0; slot < kSlots; ++slot) {
         const ChunkPart p(a, j, slot);
         if (!p.any) continue;
@@ -599,11 +561,59 @@ template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_ba
     if (a.sums) put_sums(a, at, room, cs, cq, a.shorts + j);
 }
 
+template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_backward_chunk_kernel(NormArgs a)
+{
+    extern __shared__ float room[];
+    chunk_gradients<T, ONE>(a, blockIdx.x, room);
+}
+
+// As the forward kernel; rows are read twice, the second time from L2: keeping them took 181 registers, two wavefronts a SIMD, and
+// 176 us for 119 (20,000 graphs of 24 rows of 64).
+template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMost) norm_backward_kernel(NormArgs a)
+{
+    constexpr int N = kPer16<T>, A = ONE ? 1 : N;
+    extern __shared__ float room[];
+    if ((int)blockIdx.x >= a.shorts) {
+        chunk_gradients<T, ONE>(a, blockIdx.x - a.shorts, room);
+        return;
+    }
+    if ((int)blockIdx.y >= a.few.slices) return;
+    const int each = a.few.rpp * (ONE ? a.few.tpr : a.few.cs) * 2, teams = WAVE ? blockDim.x >> 6 : 1, team = WAVE ? threadIdx.x >> 6 : 0;
+    const Place<WAVE> at(a, a.few, N);
+    float *shared = room + (size_t)team * (each + 2 * at.ng), *stat = shared + each;
+    Channel<N> ch;
+    ch.params(a, at);
+    float cs[N], cq[N]; // of the thread's channels over all its rows
+#pragma unroll
+    for (int i = 0; i < N; ++i) cs[i] = cq[i] = 0.0f;
+    T *dx = static_cast<T *>(a.dx);
+    for (int64_t graph = (int64_t)blockIdx.x * teams + team; graph < a.graphs; graph += (int64_t)a.shorts * teams) {
+        const int64_t lo = begin_of(a, graph), hi = begin_of(a, graph + 1);
+        if (hi <= lo || hi - lo > a.longer) continue;
+        const float over = 1.0f / ((float)(hi - lo) * (float)a.cpg);
+        auto found = [&](int g, float s1, float q1) { stat[g * 2] = s1 * over, stat[g * 2 + 1] = q1 * over; };
+        float s[A], q[A], s1[N], s2[N];
+#pragma unroll
+        for (int i = 0; i < A; ++i) s[i] = q[i] = 0.0f;
+        ch.stats_of(a, at, graph);
+        if (at.m) each_pair<T>(a, at, lo, hi, [&](int64_t, const Raw<T> &v, const Raw<T> &g) { add_pair<T, ONE>(a, v, g, ch, cs, cq, s, q); });
+        if (!dx) continue; // the same for the whole launch
+        group_sums<WAVE, ONE>(a, at, shared, s, q, N, found);
+        group_means(a, at, stat, s1, s2);
+        if (at.m)
+            each_pair<T>(a, at, lo, hi, [&](int64_t row, const Raw<T> &v, const Raw<T> &g) {
+                put_dx<T, N>(a, v, g, ch, s1, s2, dx + row * a.C + at.c, at.m);
+            });
+        team_sync<WAVE>(); // stat is read
+    }
+    if (a.sums) put_sums(a, at, room, cs, cq, blockIdx.x);
+}
+
 // dx of the chunks
 template <typename T> __global__ void __launch_bounds__(kMost) norm_dx_kernel(NormArgs a)
 {
     constexpr int N = kPer16<T>;
-    const Place<false> at(a, N);
+    const Place<false> at(a, a.many, N);
     Channel<N> ch;
     ch.params(a, at);
     const int64_t j = gridDim.x - 1 - blockIdx.x;
@@ -679,16 +689,14 @@ NormPlan norm_plan(const pcsr_norm_t &a, int n, bool backward)
     const int cpg = (int)(a.channels / a.groups), size = 16 / n;
     const int64_t mean = a.rows / (a.graphs > 0 ? a.graphs : 1), bytes = mean * a.channels * size, pieces = (cpg + n - 1) / n;
     q.one = cpg % n == 0;
-    const int64_t most = kMost;
     q.wave = a.graphs >= 512 && pieces <= 64 && bytes <= 64 * 16 * kKept;
     if (q.wave) {
         q.few = shape_of(a, n, 256, 64, a.graphs, 0);
     } else {
-        const int t = bytes <= 256 * 16 * kKept && pieces <= 256 ? 256 : (int)most;
+        const int t = pieces <= 256 ? 256 : kMost;
         q.few = shape_of(a, n, t, t, a.graphs, 512);
     }
-    const int t = pieces <= 256 ? 256 : (int)most;
-    q.many = shape_of(a, n, t, t, 1024, 0);
+    q.many = shape_of(a, n, q.few.threads, q.few.threads, 1024, 0);
     const int64_t keeps = (int64_t)kKept * q.few.rpp, least = (int64_t)kAhead * q.many.rpp;
     q.chunk = (a.rows + 1023) / 1024;
     if (q.chunk < least) q.chunk = least;
@@ -729,7 +737,7 @@ NormArgs norm_args(const pcsr_norm_t &a, const NormPlan &q, void *ws)
     p.offsets = a.graphs == 1 ? nullptr : a.offsets, p.wide = a.wide, p.ptype = a.param_type, p.act = a.act;
     p.x = a.x, p.xs = a.x_stride, p.w = a.weight, p.b = a.bias, p.eps = a.eps, p.mean = a.mean, p.rstd = a.rstd;
     p.longer = q.longer, p.chunk = q.chunk, p.shorts = q.shorts, p.chunks = q.chunks;
-    p.part = ws;
+    p.few = q.few, p.many = q.many, p.part = ws;
     return p;
 }
 
@@ -744,6 +752,12 @@ struct NormSpace { // of the workspace
         bytes = sums + (backward ? ((int64_t)q.shorts + q.chunks) * 2 * a.channels * 4 : 0);
     }
 };
+
+unsigned slices(const NormPlan &q)
+{
+    const int few = q.shorts ? q.few.slices : 0, many = q.chunks ? q.many.slices : 0;
+    return (unsigned)(few > many ? few : many);
+}
 
 // f<ONE, WAVE>
 template <typename F> int for_plan(const NormPlan &q, F f)
@@ -779,20 +793,23 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
         p.y = y;
         return for_plan(q, [&](auto one, auto wave) {
             constexpr bool ONE = decltype(one)::value, WAVE = decltype(wave)::value;
-            auto lds = [&](const Shape &sh, bool stat) {
-                return sizeof(double) * (sh.threads / sh.team) * ((size_t)2 * sh.rpp * (ONE ? sh.tpr : sh.cs) + (stat ? sh.cs / p.cpg : 0));
+            const auto lds_of = [&](const Shape &sh, int teams, bool stat) {
+                return sizeof(double) * teams * ((size_t)2 * sh.rpp * (ONE ? sh.tpr : sh.cs) + (stat ? sh.cs / p.cpg : 0));
             };
+            const size_t lds0 = q.shorts ? lds_of(q.few, q.few.threads / q.few.team, true) : 0, lds1 = q.chunks ? lds_of(q.many, 1, false) : 0;
+            const size_t lds = lds0 > lds1 ? lds0 : lds1;
+            const dim3 grid(q.shorts + q.chunks, slices(q)), block(q.few.threads);
             if (q.shorts) {
-                p.sh = q.few;
-                if (!allow_lds(&norm_kernel<T, ONE, WAVE>, lds(p.sh, true))) return (int)PCSR_E_HIP;
-                hipLaunchKernelGGL((norm_kernel<T, ONE, WAVE>), dim3(q.shorts, p.sh.slices), dim3(p.sh.threads), lds(p.sh, true), s, p);
+                if (!allow_lds(&norm_kernel<T, ONE, WAVE>, lds)) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_kernel<T, ONE, WAVE>), grid, block, lds, s, p);
+            } else {
+                if (!allow_lds(&norm_chunk_kernel<T, ONE>, lds)) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_chunk_kernel<T, ONE>), grid, block, lds, s, p);
             }
             if (q.chunks) {
-                p.sh = q.many;
-                if (!allow_lds(&norm_chunk_kernel<T, ONE>, lds(p.sh, false))) return (int)PCSR_E_HIP;
-                hipLaunchKernelGGL((norm_chunk_kernel<T, ONE>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), lds(p.sh, false), s, p);
-                hipLaunchKernelGGL(norm_combine_kernel, dim3(q.chunks, (p.groups + kGroupsOf - 1) / kGroupsOf), dim3(32 * kGroupsOf), 0, s, p);
-                hipLaunchKernelGGL((norm_apply_kernel<T>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), 0, s, p);
+                hipLaunchKernelGGL(norm_combine_kernel, dim3(p.offsets ? q.chunks : (unsigned)p.graphs, (p.groups + kGroupsOf - 1) / kGroupsOf),
+                                   dim3(32 * kGroupsOf), 0, s, p);
+                hipLaunchKernelGGL((norm_apply_kernel<T>), dim3(q.chunks, q.many.slices), dim3(q.many.threads), 0, s, p);
             }
             return launched();
         });
@@ -823,24 +840,24 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
         p.means = reinterpret_cast<float *>(at + w.means);
         return for_plan(q, [&](auto one, auto wave) {
             constexpr bool ONE = decltype(one)::value, WAVE = decltype(wave)::value;
-            auto lds = [&](const Shape &sh, bool stat) {
-                const size_t teams = sh.threads / sh.team, pairs = teams * ((size_t)2 * sh.rpp * (ONE ? sh.tpr : sh.cs) + (stat ? 2 * (sh.cs / p.cpg) : 0));
+            const auto lds_of = [&](const Shape &sh, size_t teams, bool stat) {
+                const size_t pairs = teams * ((size_t)2 * sh.rpp * (ONE ? sh.tpr : sh.cs) + (stat ? 2 * (sh.cs / p.cpg) : 0));
                 const size_t col = sums ? teams * 2 * sh.rpp * sh.cs : 0;
                 return sizeof(float) * (pairs > col ? pairs : col);
             };
+            const size_t lds0 = q.shorts ? lds_of(q.few, q.few.threads / q.few.team, true) : 0, lds1 = q.chunks ? lds_of(q.many, 1, false) : 0;
+            const size_t lds = lds0 > lds1 ? lds0 : lds1;
+            const dim3 grid(q.shorts + q.chunks, slices(q)), block(q.few.threads);
             if (q.shorts) {
-                p.sh = q.few;
-                if (!allow_lds(&norm_backward_kernel<T, ONE, WAVE>, lds(p.sh, true))) return (int)PCSR_E_HIP;
-                hipLaunchKernelGGL((norm_backward_kernel<T, ONE, WAVE>), dim3(q.shorts, p.sh.slices), dim3(p.sh.threads), lds(p.sh, true), s, p);
+                if (!allow_lds(&norm_backward_kernel<T, ONE, WAVE>, lds)) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_backward_kernel<T, ONE, WAVE>), grid, block, lds, s, p);
+            } else if (q.chunks) {
+                if (!allow_lds(&norm_backward_chunk_kernel<T, ONE>, lds)) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL((norm_backward_chunk_kernel<T, ONE>), grid, block, lds, s, p);
             }
-            if (q.chunks) {
-                p.sh = q.many;
-                if (!allow_lds(&norm_backward_chunk_kernel<T, ONE>, lds(p.sh, false))) return (int)PCSR_E_HIP;
-                hipLaunchKernelGGL((norm_backward_chunk_kernel<T, ONE>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), lds(p.sh, false), s, p);
-            }
-            const int more = dx ? q.chunks * ((p.groups + kGroupsOf - 1) / kGroupsOf) : 0;
+            const int more = dx && q.chunks ? (p.offsets ? q.chunks : (int)p.graphs) * ((p.groups + kGroupsOf - 1) / kGroupsOf) : 0;
             if (columns + more) hipLaunchKernelGGL(norm_finish_kernel, dim3(columns + more), dim3(1024), 0, s, p, columns);
-            if (dx && q.chunks) hipLaunchKernelGGL((norm_dx_kernel<T>), dim3(q.chunks, p.sh.slices), dim3(p.sh.threads), 0, s, p);
+            if (dx && q.chunks) hipLaunchKernelGGL((norm_dx_kernel<T>), dim3(q.chunks, q.many.slices), dim3(q.many.threads), 0, s, p);
             return launched();
         });
     });

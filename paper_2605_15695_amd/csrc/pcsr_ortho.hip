@@ -326,15 +326,117 @@ struct ProductArgs {
     int turn;    // which of the transposes is read
 };
 
-// 256 threads, 2 x 2 wavefronts of F x F tiles of 32 x 32.  Numbers go from memory to registers while the stage before is multiplied, then to LDS: two
-// stages of 128 bytes of every row (both pieces).  16-byte chunks of a row are exchanged by its number, so that the 16 rows
-// that a quarter of a wavefront reads lie in different banks.
+// WI x WJ wavefronts of FI x FJ tiles of 32 x 32.  Stages of 32 numbers of k go from memory straight to a ring of S places in LDS, S - 1 of
+// them on their way while one is multiplied: a round trip to memory is some 2,000 cycles, a stage's products 500 to 1,000.  64 bytes of a row
+// and piece lie together; 16-byte chunks of a row are exchanged by bits 2 and 3 of its number, so that the 16 rows that a
+// quarter of a wavefront reads lie in different banks.
 // 32x32x16: lane l holds A[i = l % 32][k = 8 (l / 32) ..], B[k][j = l % 32] likewise; D[i = 8 (r / 4) + 4 (l / 32) + r % 4][j = l % 32].
-template <typename T, int F, int P, int MODE> __global__ void __launch_bounds__(kT, 2) product_kernel(ProductArgs a, Items items)
+// Two pieces: a stage's products have a sum of their own, which is then added to the rest: the matrix instructions cut off what
+// does not reach a sum's last bit, always downwards, and over 1,000 numbers that was 1.5 times the error of fp32 products.
+template <int TI_, int TJ_, int WI_, int WJ_, int P_, int S_> struct Tiling {
+    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, P = P_, S = S_;
+    static constexpr int threads = 64 * WI * WJ, FI = TI / 32 / WI, FJ = TJ / 32 / WJ, blocks = (TI + TJ) / 16 * P; // 16 rows, 1 KB
+    static constexpr int loads = blocks / (WI * WJ), stage = blocks * 1024, lds = S * stage;
+    static_assert(blocks % (WI * WJ) == 0 && lds <= 160 * 1024, "whole loads, in LDS");
+};
+typedef Tiling<64, 64, 2, 2, 1, 6> Small1;
+typedef Tiling<64, 64, 2, 2, 2, 4> Small2;
+typedef Tiling<256, 256, 2, 4, 1, 4> Large1;
+typedef Tiling<128, 128, 2, 2, 2, 4> Large2;
+
+template <int N> __device__ __forceinline__ void wait_loads() // until N of the wavefront's loads are on their way, for all wavefronts
 {
-    constexpr int TILE = 64 * F, BK = 64 / P, CH = BK / 8, ROT = 16 / CH, LOADS = TILE * CH / kT * P; // per operand and thread
-    static_assert(TILE * CH % kT == 0, "whole loads");
-    __shared__ h8 lds[2][2][P][TILE * CH];
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <typename C> struct Sums {
+    f16v v[C::FI][C::FJ];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int r = 0; r < C::FI; ++r)
+#pragma unroll
+            for (int c = 0; c < C::FJ; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[r][c][e] = 0.0f;
+    }
+};
+
+template <typename C>
+__device__ __forceinline__ void product(const half_t *p, int64_t p_plane, const half_t *q, int64_t q_plane, int64_t Kp, char *lds, int lane, int wave,
+                                        Sums<C> &sum)
+{
+    constexpr int P = C::P;
+    typedef __attribute__((address_space(3))) void *Lds;
+    typedef __attribute__((address_space(1))) const void *Global;
+    const int64_t place = (int64_t)(lane >> 2) * Kp + (((lane & 3) ^ (lane >> 4)) << 3); // of a lane's chunk in 16 rows
+    const half_t *from[C::loads];
+#pragma unroll
+    for (int u = 0; u < C::loads; ++u) {
+        const int block = wave + u * C::WI * C::WJ;
+        constexpr int PI = C::TI / 16, PJ = C::TJ / 16;
+        const bool second = block >= P * PI;
+        const int rest = second ? block - P * PI : block, per = second ? PJ : PI, plane = rest / per, row = (rest - plane * per) * 16;
+        from[u] = (second ? q + plane * q_plane : p + plane * p_plane) + row * Kp + place;
+    }
+    const auto fetch = [&](int s) {
+        char *to = lds + s % C::S * C::stage + wave * 1024;
+#pragma unroll
+        for (int u = 0; u < C::loads; ++u)
+            __builtin_amdgcn_global_load_lds((Global)(from[u] + (int64_t)s * 32), (Lds)(to + u * C::WI * C::WJ * 1024), 16, 0, 0);
+    };
+    const int i = lane & 31, half = lane >> 5, wr = wave / C::WJ, wc = wave % C::WJ;
+    const int row = (i >> 4) * 1024 + (i & 15) * 64, turn = (i >> 2) & 3;
+    const int at0 = wr * C::FI * 2048 + row, at1 = P * C::TI * 64 + wc * C::FJ * 2048 + row;
+    const int steps = (int)(Kp / 32);
+    sum.zero();
+#pragma unroll
+    for (int s = 0; s < C::S - 1; ++s)
+        if (s < steps) fetch(s);
+    for (int s = 0; s < steps; ++s) {
+        if (s + C::S - 2 < steps) wait_loads<C::loads * (C::S - 2)>();
+        else wait_loads<0>();
+        if (s + C::S - 1 < steps) fetch(s + C::S - 1); // where the stage before the last barrier was
+        const char *here = lds + s % C::S * C::stage;
+        Sums<C> part;
+        if (P == 2) part.zero();
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            h8 x[C::FI][P], y[C::FJ][P];
+            const int chunk = ((kk * 2 + half) ^ turn) * 16;
+#pragma unroll
+            for (int o = 0; o < P; ++o) {
+#pragma unroll
+                for (int f = 0; f < C::FI; ++f) x[f][o] = *reinterpret_cast<const h8 *>(here + at0 + o * C::TI * 64 + f * 2048 + chunk);
+#pragma unroll
+                for (int f = 0; f < C::FJ; ++f) y[f][o] = *reinterpret_cast<const h8 *>(here + at1 + o * C::TJ * 64 + f * 2048 + chunk);
+            }
+#pragma unroll
+            for (int r = 0; r < C::FI; ++r)
+#pragma unroll
+                for (int c = 0; c < C::FJ; ++c) {
+                    if (P == 2) {
+                        part.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][1 % P], y[c][0], part.v[r][c], 0, 0, 0);
+                        part.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][1 % P], part.v[r][c], 0, 0, 0);
+                        part.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][0], part.v[r][c], 0, 0, 0);
+                    } else {
+                        sum.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][0], sum.v[r][c], 0, 0, 0);
+                    }
+                }
+        }
+        if (P == 2) {
+#pragma unroll
+            for (int r = 0; r < C::FI; ++r)
+#pragma unroll
+                for (int c = 0; c < C::FJ; ++c) sum.v[r][c] += part.v[r][c];
+        }
+    }
+}
+
+template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C::threads) product_kernel(ProductArgs a, Items items)
+{
+    constexpr int P = C::P;
+    extern __shared__ char memory[];
     const Space &sp = a.sp;
     char *base = a.ws + blockIdx.y * sp.bytes;
     int ti, tj;
@@ -357,96 +459,28 @@ template <typename T, int F, int P, int MODE> __global__ void __launch_bounds__(
     if (MODE == MAKE_A) p = q = reinterpret_cast<const half_t *>(base + sp.x), p_plane = q_plane = sp.Mp * sp.Np;
     else if (MODE == MAKE_B) p = q = reinterpret_cast<const half_t *>(base + sp.A), p_plane = q_plane = sp.Mp * sp.Mp;
     else p = reinterpret_cast<const half_t *>(base + sp.B), q = reinterpret_cast<const half_t *>(base + sp.t[a.turn]), p_plane = sp.Mp * sp.Mp, q_plane = sp.Mp * sp.Np;
-    p += (int64_t)ti * TILE * Kp;
-    q += (int64_t)tj * TILE * Kp;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave >> 1, wc = wave & 1;
-    f16v acc[F][F], low[F][F];
-#pragma unroll
-    for (int r = 0; r < F; ++r)
-#pragma unroll
-        for (int c = 0; c < F; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[r][c][e] = low[r][c][e] = 0.0f;
-    h8 pv[LOADS], qv[LOADS];
-    constexpr int ROUNDS = LOADS / P;
-    auto fetch = [&](int64_t k) {
-#pragma unroll
-        for (int o = 0; o < P; ++o)
-#pragma unroll
-            for (int u = 0; u < ROUNDS; ++u) {
-                const int id = tid + u * kT, row = id / CH, c = id % CH;
-                pv[o * ROUNDS + u] = *reinterpret_cast<const h8 *>(p + o * p_plane + row * Kp + k + c * 8);
-                qv[o * ROUNDS + u] = *reinterpret_cast<const h8 *>(q + o * q_plane + row * Kp + k + c * 8);
-            }
-    };
-    auto stage = [&](int s) {
-#pragma unroll
-        for (int o = 0; o < P; ++o)
-#pragma unroll
-            for (int u = 0; u < ROUNDS; ++u) {
-                const int id = tid + u * kT, row = id / CH, c = id % CH, at = row * CH + (c ^ (row / ROT % CH));
-                lds[s][0][o][at] = pv[o * ROUNDS + u];
-                lds[s][1][o][at] = qv[o * ROUNDS + u];
-            }
-    };
-    const int i = lane & 31, half = lane >> 5;
-    auto multiply = [&](int s) {
-#pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) {
-            h8 x[F][P], y[F][P];
-#pragma unroll
-            for (int f = 0; f < F; ++f)
-#pragma unroll
-                for (int o = 0; o < P; ++o) {
-                    const int c = kk * 2 + half, r0 = (wr * F + f) * 32 + i, r1 = (wc * F + f) * 32 + i;
-                    x[f][o] = lds[s][0][o][r0 * CH + (c ^ (r0 / ROT % CH))];
-                    y[f][o] = lds[s][1][o][r1 * CH + (c ^ (r1 / ROT % CH))];
-                }
-#pragma unroll
-            for (int r = 0; r < F; ++r)
-#pragma unroll
-                for (int c = 0; c < F; ++c) {
-                    if (P == 2) {
-                        low[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][1 % P], y[c][0], low[r][c], 0, 0, 0);
-                        low[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][1 % P], low[r][c], 0, 0, 0);
-                    }
-                    acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][0], acc[r][c], 0, 0, 0);
-                }
-        }
-    };
-    fetch(0);
-    stage(0);
-    __syncthreads();
-    const int steps = (int)(Kp / BK);
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch((int64_t)(s + 1) * BK);
-        multiply(s & 1);
-        if (s + 1 < steps) stage((s + 1) & 1); // read last before the barrier behind it
-        __syncthreads();
-    }
-    if (P == 2) {
-#pragma unroll
-        for (int r = 0; r < F; ++r)
-#pragma unroll
-            for (int c = 0; c < F; ++c) acc[r][c] += low[r][c];
-    }
+    p += (int64_t)ti * C::TI * Kp;
+    q += (int64_t)tj * C::TJ * Kp;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Sums<C> acc;
+    product<C>(p, p_plane, q, q_plane, Kp, memory, lane, wave, acc);
     const Step &st = a.st;
-    const int64_t i0 = (int64_t)ti * TILE + wr * F * 32 + half * 4, j0 = (int64_t)tj * TILE + wc * F * 32 + i;
+    const int64_t i0 = (int64_t)ti * C::TI + wave / C::WJ * C::FI * 32 + (lane >> 5) * 4, j0 = (int64_t)tj * C::TJ + wave % C::WJ * C::FJ * 32 + (lane & 31);
 #pragma unroll
-    for (int r = 0; r < F; ++r)
+    for (int r = 0; r < C::FI; ++r)
 #pragma unroll
-        for (int c = 0; c < F; ++c)
+        for (int c = 0; c < C::FJ; ++c)
 #pragma unroll
             for (int e = 0; e < 4; ++e) { // four rows in a row
                 const int64_t ii = i0 + r * 32 + e * 8, jj = j0 + c * 32;
-                f4 v = {acc[r][c][e * 4], acc[r][c][e * 4 + 1], acc[r][c][e * 4 + 2], acc[r][c][e * 4 + 3]};
+                f4 v = {acc.v[r][c][e * 4], acc.v[r][c][e * 4 + 1], acc.v[r][c][e * 4 + 2], acc.v[r][c][e * 4 + 3]};
                 if (MODE == MAKE_A || MODE == MAKE_B) {
                     float *Af = reinterpret_cast<float *>(base + sp.Af);
                     half_t *out = reinterpret_cast<half_t *>(base + (MODE == MAKE_A ? sp.A : sp.B));
                     const int64_t plane = sp.Mp * sp.Mp;
                     if (MODE == MAKE_A) {
                         v *= st.over_xx;
-                        *reinterpret_cast<f4 *>(Af + jj * sp.Mp + ii) = v; // only its lower half by rows is read: A[j][i], i >= j
+                        *reinterpret_cast<f4 *>(Af + jj * sp.Mp + ii) = v; // A[j][i], i >= j by tiles: that half alone is read
                     } else {
                         v = st.b * *reinterpret_cast<const f4 *>(Af + jj * sp.Mp + ii) + st.c * st.over_AA * v;
                     }
@@ -541,12 +575,13 @@ bool is_small(const pcsr_matrix_t &m) { return m.rows <= kSmall && m.cols <= kSm
 constexpr int kOnePiece = 256;
 int pieces_of(int type, int64_t m) { return type == PCSR_BF16 && m >= kOnePiece ? 1 : 2; }
 
-// tiles of 128 where there are enough of them for the compute units, of 64 otherwise
-int tile_of(int64_t m, int64_t n, int64_t count)
+// large tiles (of 256 with one piece, of 128 with two) where there are enough of them for the compute units, of 64 otherwise
+bool large_tiles(int64_t m, int64_t n, int64_t count, int pieces)
 {
-    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128) * count;
-    return tiles >= 192 ? 128 : 64;
+    const int64_t t = pieces == 1 ? 256 : 128, tiles = ((m + t - 1) / t) * ((n + t - 1) / t) * count;
+    return tiles >= 128;
 }
+int tile_of(int64_t m, int64_t n, int64_t count, int pieces) { return large_tiles(m, n, count, pieces) ? (pieces == 1 ? 256 : 128) : 64; }
 
 // the matrices from `first` on that go with it in one launch
 int64_t group_of(const pcsr_matrix_t *m, int64_t count, int64_t first, const char *done, int64_t *members)
@@ -565,7 +600,7 @@ int64_t group_bytes(const pcsr_matrix_t &x, int64_t n, int type)
 {
     if (is_small(x)) return 0;
     const int64_t m = x.rows < x.cols ? x.rows : x.cols, w = x.rows < x.cols ? x.cols : x.rows;
-    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, tile_of(m, w, n), pieces_of(type, m)).bytes;
+    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, tile_of(m, w, n, pieces_of(type, m)), pieces_of(type, m)).bytes;
 }
 
 int ortho_check(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t *how)
@@ -590,29 +625,34 @@ template <typename T, int Q> int run_small(const SmallArgs &a, int n, hipStream_
     return PCSR_OK;
 }
 
-template <typename T, int F, int P> void run_large(const Items &q, int n, const Step *step, int steps, char *ws, hipStream_t s)
+template <typename T, typename C, int MODE> bool run_product(const ProductArgs &a, const Items &q, unsigned tiles, int n, hipStream_t s)
 {
-    constexpr int TILE = 64 * F;
+    if (!allow_lds(&product_kernel<T, C, MODE>, C::lds)) return false;
+    hipLaunchKernelGGL((product_kernel<T, C, MODE>), dim3(tiles, n), dim3(C::threads), C::lds, s, a, q);
+    return true;
+}
+template <typename T, typename C> int run_large(const Items &q, int n, const Step *step, int steps, char *ws, hipStream_t s)
+{
+    static_assert(C::TI == C::TJ, "square tiles");
     const Item &it = q.item[0];
     const int64_t m = it.flip ? it.cols : it.rows, w = it.flip ? it.rows : it.cols;
-    const Space sp(m, w, TILE, P);
+    const Space sp(m, w, C::TI, C::P);
     double *sums = reinterpret_cast<double *>(ws);
     ws += kItems * kNormBlocks * sizeof(double);
     const int64_t want = (m * w + kT * 4 - 1) / (kT * 4);
     const int blocks = (int)(want < kNormBlocks ? want : kNormBlocks);
     hipLaunchKernelGGL((measure_kernel<T>), dim3(blocks, n), dim3(kT), 0, s, q, sums);
-    hipLaunchKernelGGL((pack_kernel<T, P>), dim3((unsigned)(sp.Np / 32), (unsigned)(sp.Mp / 32), n), dim3(kT), 0, s, q, sums, blocks, ws, sp, step[0].x);
-    const unsigned ti = (unsigned)(sp.Mp / TILE), tj = (unsigned)(sp.Np / TILE), sym = ti * (ti + 1) / 2;
-    for (int k = 0; k < steps; ++k) {
+    hipLaunchKernelGGL((pack_kernel<T, C::P>), dim3((unsigned)(sp.Np / 32), (unsigned)(sp.Mp / 32), n), dim3(kT), 0, s, q, sums, blocks, ws, sp, step[0].x);
+    const unsigned ti = (unsigned)(sp.Mp / C::TI), tj = (unsigned)(sp.Np / C::TJ), sym = ti * (ti + 1) / 2;
+    bool ok = true;
+    for (int k = 0; k < steps && ok; ++k) {
         ProductArgs a = {ws, sp, step[k], sp.Np, (int)ti, k & 1};
-        hipLaunchKernelGGL((product_kernel<T, F, P, MAKE_A>), dim3(sym, n), dim3(kT), 0, s, a, q);
+        ok = run_product<float, C, MAKE_A>(a, q, sym, n, s); // (the type matters to the last alone)
         a.K = sp.Mp;
-        hipLaunchKernelGGL((product_kernel<T, F, P, MAKE_B>), dim3(sym, n), dim3(kT), 0, s, a, q);
-        if (k + 1 < steps)
-            hipLaunchKernelGGL((product_kernel<T, F, P, MAKE_X>), dim3(ti * tj, n), dim3(kT), 0, s, a, q);
-        else
-            hipLaunchKernelGGL((product_kernel<T, F, P, LAST_X>), dim3(ti * tj, n), dim3(kT), 0, s, a, q);
+        ok = ok && run_product<float, C, MAKE_B>(a, q, sym, n, s);
+        ok = ok && (k + 1 < steps ? run_product<float, C, MAKE_X>(a, q, ti * tj, n, s) : run_product<T, C, LAST_X>(a, q, ti * tj, n, s));
     }
+    return ok ? PCSR_OK : PCSR_E_HIP;
 }
 
 } // namespace
@@ -667,17 +707,12 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
             if (is_small(m[k])) return m[k].rows > 64 || m[k].cols > 64 ? run_small<T, 2>(a, used, s) : run_small<T, 1>(a, used, s);
             const int64_t lo = m[k].rows < m[k].cols ? m[k].rows : m[k].cols, hi = m[k].rows < m[k].cols ? m[k].cols : m[k].rows;
             char *at = static_cast<char *>(ws);
-            const bool wide = tile_of(lo, hi, used) == 128;
+            const int pieces = pieces_of(how->type, lo);
+            const bool large = large_tiles(lo, hi, used, pieces);
             if constexpr (std::is_same<T, bfloat_t>::value) {
-                if (pieces_of(how->type, lo) == 1) {
-                    if (wide) run_large<T, 2, 1>(a.q, used, a.step, a.steps, at, s);
-                    else run_large<T, 1, 1>(a.q, used, a.step, a.steps, at, s);
-                    return (int)PCSR_OK;
-                }
+                if (pieces == 1) return large ? run_large<T, Large1>(a.q, used, a.step, a.steps, at, s) : run_large<T, Small1>(a.q, used, a.step, a.steps, at, s);
             }
-            if (wide) run_large<T, 2, 2>(a.q, used, a.step, a.steps, at, s);
-            else run_large<T, 1, 2>(a.q, used, a.step, a.steps, at, s);
-            return (int)PCSR_OK;
+            return large ? run_large<T, Large2>(a.q, used, a.step, a.steps, at, s) : run_large<T, Small2>(a.q, used, a.step, a.steps, at, s);
         });
         if (r != PCSR_OK) return r;
     }
