@@ -246,8 +246,9 @@ template <typename T, int Q> __global__ void __launch_bounds__(1024) small_kerne
 }
 
 // ---------------------------------------------------------------------------------- large matrices
-// Sides padded with zeros to whole tiles.  Planes of a matrix, one after the other (P of each): X [Mp][Np], its transpose twice (one is
-// read while the other is written), A, B; then X and A in fp32.
+// Sides padded with zeros to whole tiles.  Planes of a matrix, one after the other (P of each): X, its transpose twice (one is read while the
+// other is written), A, B; then X and A in fp32.  A plane of R rows of K numbers lies as [K / 32][R][32]: what a product reads at a time,
+// 32 numbers of k of a tile's rows, is one stretch of whole lines from all channels of L2.
 struct Space {
     int64_t Mp, Np, x, t[2], A, B, xf, Af, bytes; // bytes of a matrix
     Space(int64_t m, int64_t n, int tile, int P)
@@ -260,59 +261,42 @@ struct Space {
         bytes = at;
     }
 };
+__device__ __forceinline__ int64_t plane_at(int64_t R, int64_t row, int64_t k) { return (k / 32 * R + row) * 32 + k % 32; }
 constexpr int kNormBlocks = 256; // partial sums of a matrix's squares
 
+// sums of squares; buf is written.  A thread takes 16 bytes of a row, as many threads to a row as it has of them.
 template <typename T> __global__ void __launch_bounds__(kT) measure_kernel(Items q, double *sums)
 {
+    constexpr int N = kPer16<T>;
     __shared__ double part[kT / 64];
     const Item &it = q.item[blockIdx.y];
-    const int64_t all = (int64_t)it.rows * it.cols;
+    int lanes = 1;
+    while (lanes < kT && lanes * N < it.cols) lanes *= 2;
+    const int lane = threadIdx.x % lanes, per = kT / lanes;
     double sum = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * kT + threadIdx.x; i < all; i += (int64_t)gridDim.x * kT) {
-        const int r = (int)(i / it.cols), c = (int)(i - (int64_t)r * it.cols);
-        const double v = take<T>(q, it, r, c, true);
-        sum += v * v;
-    }
+    for (int64_t r = (int64_t)blockIdx.x * per + threadIdx.x / lanes; r < it.rows; r += (int64_t)gridDim.x * per)
+#pragma unroll 4
+        for (int c = lane * N; c < it.cols; c += lanes * N) {
+            const int m = it.cols - c < N ? it.cols - c : N;
+            float v[N];
+            load_upto<T, N>(static_cast<const T *>(it.grad) + r * it.grad_ld + c, m, v);
+            if (it.buf) {
+                float b[N];
+                load_upto<float, N>(it.buf + r * it.buf_ld + c, m, b);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    b[i] = q.momentum * b[i] + v[i];
+                    v[i] = q.nesterov ? v[i] + q.momentum * b[i] : b[i];
+                }
+                store_upto<float, N>(it.buf + r * it.buf_ld + c, m, b);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum += (double)v[i] * (double)v[i]; // zeros behind the end
+        }
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) sums[blockIdx.y * kNormBlocks + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
-}
-
-// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup
-template <typename T, int P> __global__ void __launch_bounds__(kT) pack_kernel(Items q, const double *sums, int blocks, char *ws, Space sp, float scale)
-{
-    __shared__ float tile[32][33];
-    const Item &it = q.item[blockIdx.z];
-    char *base = ws + blockIdx.z * sp.bytes;
-    double sum = 0.0;
-    for (int k = threadIdx.x & 63; k < blocks; k += 64) sum += sums[blockIdx.z * kNormBlocks + k];
-    sum = wave_sum(sum);
-    const double over = sum == 0.0 ? 0.0 : 1.0 / sqrt(sum);
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int64_t i0 = (int64_t)blockIdx.y * 32, j0 = (int64_t)blockIdx.x * 32; // of X
-    for (int k = ty; k < 32; k += 8) { // rows of the matrix, as they lie
-        const int64_t r = (it.flip ? j0 : i0) + k, c = (it.flip ? i0 : j0) + tx;
-        float v = 0.0f;
-        if (r < it.rows && c < it.cols) v = (float)((double)take<T>(q, it, (int)r, (int)c, false) * over);
-        tile[k][tx] = v;
-    }
-    __syncthreads();
-    half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[0]);
-    float *xf = reinterpret_cast<float *>(base + sp.xf);
-    const int64_t plane = sp.Mp * sp.Np;
-    for (int k = ty; k < 32; k += 8) {
-        const float v = it.flip ? tile[tx][k] : tile[k][tx], w = it.flip ? tile[k][tx] : tile[tx][k]; // X[i0 + k][j0 + tx], X[i0 + tx][j0 + k]
-        half_t hv[P], hw[P];
-        pieces<P>(v * scale, hv);
-        pieces<P>(w * scale, hw);
-        xf[(i0 + k) * sp.Np + j0 + tx] = v;
-#pragma unroll
-        for (int o = 0; o < P; ++o) {
-            x[o * plane + (i0 + k) * sp.Np + j0 + tx] = hv[o];
-            t[o * plane + (j0 + k) * sp.Mp + i0 + tx] = hw[o];
-        }
-    }
 }
 
 // Products D[i][j] = sum over k of p[i][k] q[j][k], rows of both contiguous in k.
@@ -321,28 +305,29 @@ struct ProductArgs {
     char *ws;
     Space sp;
     Step st;
-    int64_t K;
     int tiles_i; // of D; symmetric: the tiles with i >= j
     int turn;    // which of the transposes is read
 };
 
 // WI x WJ wavefronts of FI x FJ tiles of 32 x 32.  Stages of 32 numbers of k go from memory straight to a ring of S places in LDS, S - 1 of
-// them on their way while one is multiplied: a round trip to memory is some 2,000 cycles, a stage's products 500 to 1,000.  64 bytes of a row
+// them on their way or there while one is multiplied: a round trip to memory is some 2,000 cycles, a stage's products 500 to 1,000.  64 bytes of a row
 // and piece lie together; 16-byte chunks of a row are exchanged by bits 2 and 3 of its number, so that the 16 rows that a
 // quarter of a wavefront reads lie in different banks.
 // 32x32x16: lane l holds A[i = l % 32][k = 8 (l / 32) ..], B[k][j = l % 32] likewise; D[i = 8 (r / 4) + 4 (l / 32) + r % 4][j = l % 32].
 // Two pieces: a stage's products have a sum of their own, which is then added to the rest: the matrix instructions cut off what
 // does not reach a sum's last bit, always downwards, and over 1,000 numbers that was 1.5 times the error of fp32 products.
-template <int TI_, int TJ_, int WI_, int WJ_, int P_, int S_> struct Tiling {
-    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, P = P_, S = S_;
-    static constexpr int threads = 64 * WI * WJ, FI = TI / 32 / WI, FJ = TJ / 32 / WJ, blocks = (TI + TJ) / 16 * P; // 16 rows, 1 KB
-    static constexpr int loads = blocks / (WI * WJ), stage = blocks * 1024, lds = S * stage;
-    static_assert(blocks % (WI * WJ) == 0 && lds <= 160 * 1024, "whole loads, in LDS");
+template <int TI_, int TJ_, int WI_, int WJ_, int P_, int S_, int G_ = 1> struct Tiling {
+    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, P = P_, S = S_, G = G_; // G: teams of WI x WJ wavefronts, each with a stretch of k
+    static constexpr int threads = 64 * WI * WJ * G, FI = TI / 32 / WI, FJ = TJ / 32 / WJ, blocks = (TI + TJ) / 16 * P; // 16 rows, 1 KB
+    static constexpr int loads = blocks / (WI * WJ), stage = blocks * 1024, lds = G * S * stage;
+    static_assert(blocks % (WI * WJ) == 0 && lds <= 160 * 1024 && G <= 2, "whole loads, in LDS");
 };
-typedef Tiling<64, 64, 2, 2, 1, 6> Small1;
-typedef Tiling<64, 64, 2, 2, 2, 4> Small2;
-typedef Tiling<256, 256, 2, 4, 1, 4> Large1;
-typedef Tiling<128, 128, 2, 2, 2, 4> Large2;
+typedef Tiling<64, 64, 2, 2, 1, 4, 2> Small1;
+typedef Tiling<128, 128, 4, 2, 1, 4> Middle1;
+typedef Tiling<256, 256, 4, 2, 1, 4> Large1;
+typedef Tiling<64, 64, 2, 2, 2, 3, 2> Few2;
+typedef Tiling<64, 64, 2, 2, 2, 3> Small2;
+typedef Tiling<128, 128, 2, 4, 2, 4> Large2;
 
 template <int N> __device__ __forceinline__ void wait_loads() // until N of the wavefront's loads are on their way, for all wavefronts
 {
@@ -362,74 +347,211 @@ template <typename C> struct Sums {
     }
 };
 
-template <typename C>
-__device__ __forceinline__ void product(const half_t *p, int64_t p_plane, const half_t *q, int64_t q_plane, int64_t Kp, char *lds, int lane, int wave,
-                                        Sums<C> &sum)
+struct Operand {
+    const half_t *at; // the tile's rows, k = 0
+    int64_t R, plane; // rows of the plane, numbers of it
+};
+template <typename C> __device__ __forceinline__ void product(const Operand &p, const Operand &q, int64_t Kp, char *lds, int lane, int wave, int team, Sums<C> &sum)
 {
     constexpr int P = C::P;
     typedef __attribute__((address_space(3))) void *Lds;
     typedef __attribute__((address_space(1))) const void *Global;
-    const int64_t place = (int64_t)(lane >> 2) * Kp + (((lane & 3) ^ (lane >> 4)) << 3); // of a lane's chunk in 16 rows
     const half_t *from[C::loads];
+    int64_t step[C::loads];
 #pragma unroll
     for (int u = 0; u < C::loads; ++u) {
         const int block = wave + u * C::WI * C::WJ;
         constexpr int PI = C::TI / 16, PJ = C::TJ / 16;
         const bool second = block >= P * PI;
-        const int rest = second ? block - P * PI : block, per = second ? PJ : PI, plane = rest / per, row = (rest - plane * per) * 16;
-        from[u] = (second ? q + plane * q_plane : p + plane * p_plane) + row * Kp + place;
+        const Operand &o = second ? q : p;
+        const int rest = second ? block - P * PI : block, per = second ? PJ : PI, plane = rest / per, row = (rest - plane * per) * 16 + (lane >> 2);
+        step[u] = o.R * 32;
+        from[u] = o.at + plane * o.plane + row * 32 + (((lane & 3) ^ (lane >> 4)) << 3) + team * (Kp / 32 / C::G) * step[u];
     }
-    const auto fetch = [&](int s) {
-        char *to = lds + s % C::S * C::stage + wave * 1024;
-#pragma unroll
-        for (int u = 0; u < C::loads; ++u)
-            __builtin_amdgcn_global_load_lds((Global)(from[u] + (int64_t)s * 32), (Lds)(to + u * C::WI * C::WJ * 1024), 16, 0, 0);
+    const auto fetch = [&](int s, int u) { // a wavefront's load of a stage
+        __builtin_amdgcn_global_load_lds((Global)(from[u] + s * step[u]), (Lds)(lds + s % C::S * C::stage + (wave + u * C::WI * C::WJ) * 1024), 16, 0, 0);
     };
-    const int i = lane & 31, half = lane >> 5, wr = wave / C::WJ, wc = wave % C::WJ;
-    const int row = (i >> 4) * 1024 + (i & 15) * 64, turn = (i >> 2) & 3;
-    const int at0 = wr * C::FI * 2048 + row, at1 = P * C::TI * 64 + wc * C::FJ * 2048 + row;
-    const int steps = (int)(Kp / 32);
+    const int i = lane & 31, half = lane >> 5, wr = wave / C::WJ, wc = wave % C::WJ, turn = (i >> 2) & 3;
+    const int at0 = (wr * C::FI * 32 + i) * 64, at1 = (P * C::TI + wc * C::FJ * 32 + i) * 64;
+    const int steps = (int)(Kp / 32 / C::G); // sides are whole tiles of 64 at least: an even number of stages
+    lds += team * C::S * C::stage;
     sum.zero();
-#pragma unroll
-    for (int s = 0; s < C::S - 1; ++s)
-        if (s < steps) fetch(s);
-    for (int s = 0; s < steps; ++s) {
-        if (s + C::S - 2 < steps) wait_loads<C::loads * (C::S - 2)>();
-        else wait_loads<0>();
-        if (s + C::S - 1 < steps) fetch(s + C::S - 1); // where the stage before the last barrier was
+    // The operands of 16 numbers of k are read while the 16 before are multiplied.
+    struct Half {
+        h8 x[C::FI][P], y[C::FJ][P];
+    };
+    const auto read = [&](int s, int kk, Half &h) {
         const char *here = lds + s % C::S * C::stage;
-        Sums<C> part;
-        if (P == 2) part.zero();
+        const int chunk = ((kk * 2 + half) ^ turn) * 16;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            h8 x[C::FI][P], y[C::FJ][P];
-            const int chunk = ((kk * 2 + half) ^ turn) * 16;
+        for (int o = 0; o < P; ++o) {
 #pragma unroll
-            for (int o = 0; o < P; ++o) {
+            for (int f = 0; f < C::FI; ++f) h.x[f][o] = *reinterpret_cast<const h8 *>(here + at0 + (o * C::TI + f * 32) * 64 + chunk);
 #pragma unroll
-                for (int f = 0; f < C::FI; ++f) x[f][o] = *reinterpret_cast<const h8 *>(here + at0 + o * C::TI * 64 + f * 2048 + chunk);
-#pragma unroll
-                for (int f = 0; f < C::FJ; ++f) y[f][o] = *reinterpret_cast<const h8 *>(here + at1 + o * C::TJ * 64 + f * 2048 + chunk);
-            }
-#pragma unroll
-            for (int r = 0; r < C::FI; ++r)
-#pragma unroll
-                for (int c = 0; c < C::FJ; ++c) {
-                    if (P == 2) {
-                        part.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][1 % P], y[c][0], part.v[r][c], 0, 0, 0);
-                        part.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][1 % P], part.v[r][c], 0, 0, 0);
-                        part.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][0], part.v[r][c], 0, 0, 0);
-                    } else {
-                        sum.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[r][0], y[c][0], sum.v[r][c], 0, 0, 0);
-                    }
-                }
+            for (int f = 0; f < C::FJ; ++f) h.y[f][o] = *reinterpret_cast<const h8 *>(here + at1 + (o * C::TJ + f * 32) * 64 + chunk);
         }
+    };
+    const auto multiply = [&](const Half &h, Sums<C> &to, auto between) {
+#pragma unroll
+        for (int r = 0; r < C::FI; ++r) {
+#pragma unroll
+            for (int c = 0; c < C::FJ; ++c) {
+                if (P == 2) {
+                    to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][1 % P], h.y[c][0], to.v[r][c], 0, 0, 0);
+                    to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][0], h.y[c][1 % P], to.v[r][c], 0, 0, 0);
+                }
+                to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][0], h.y[c][0], to.v[r][c], 0, 0, 0);
+            }
+            between(r);
+        }
+    };
+    const auto nothing = [](int) {};
+    const auto take_part = [&](Sums<C> &part) {
         if (P == 2) {
 #pragma unroll
             for (int r = 0; r < C::FI; ++r)
 #pragma unroll
                 for (int c = 0; c < C::FJ; ++c) sum.v[r][c] += part.v[r][c];
         }
+    };
+#pragma unroll
+    for (int s = 0; s < C::S - 1; ++s)
+        if (s < steps)
+#pragma unroll
+            for (int u = 0; u < C::loads; ++u) fetch(s, u);
+    if (steps >= C::S - 1) wait_loads<C::loads * (C::S - 2)>();
+    else wait_loads<0>();
+    Half h0, h1;
+    read(0, 0, h0);
+    int s = 0;
+    // Reads are issued before the products that they are to run beside: left to the compiler they come behind them, and matrix units are
+    // busy 57 % of a lone tile's time.  Loads are issued between products, into the place that the barrier of the stage before has freed: all at once they
+    // keep the wavefronts from their products while the memory unit takes one after the other.  No condition in the loop, or the waits at its
+    // joins are for everything.
+    for (; s + C::S - 1 < steps; ++s) {
+        Sums<C> part;
+        if (P == 2) part.zero();
+        read(s, 1, h1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(h0, P == 2 ? part : sum, [&](int r) {
+#pragma unroll
+            for (int u = r * C::loads / C::FI; u < (r + 1) * C::loads / C::FI; ++u) fetch(s + C::S - 1, u);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        wait_loads<C::loads * (C::S - 2)>(); // all of stage s has been read by all wavefronts when they pass; stage s + 1 is there
+        read(s + 1, 0, h0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(h1, P == 2 ? part : sum, nothing);
+        take_part(part);
+    }
+    for (; s < steps; ++s) { // the last stages: nothing is left to fetch
+        Sums<C> part;
+        if (P == 2) part.zero();
+        read(s, 1, h1);
+        multiply(h0, P == 2 ? part : sum, nothing);
+        wait_loads<0>();
+        if (s + 1 < steps) read(s + 1, 0, h0);
+        multiply(h1, P == 2 ? part : sum, nothing);
+        take_part(part);
+    }
+    if (C::G == 2) { // the second team's sums
+        f4 *to = reinterpret_cast<f4 *>(lds - team * C::S * C::stage) + (wave * 64 + lane);
+        __syncthreads(); // the last stages are read
+#pragma unroll
+        for (int r = 0; r < C::FI; ++r)
+#pragma unroll
+            for (int c = 0; c < C::FJ; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f4 &at = to[((r * C::FJ + c) * 4 + e) * 64 * C::WI * C::WJ];
+                    if (team) at = f4{sum.v[r][c][e * 4], sum.v[r][c][e * 4 + 1], sum.v[r][c][e * 4 + 2], sum.v[r][c][e * 4 + 3]};
+                }
+        __syncthreads();
+        if (team) return;
+#pragma unroll
+        for (int r = 0; r < C::FI; ++r)
+#pragma unroll
+            for (int c = 0; c < C::FJ; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum.v[r][c][e] += to[((r * C::FJ + c) * 4 + e / 4) * 64 * C::WI * C::WJ][e % 4];
+    }
+}
+
+// X and A in fp32 lie as the products' sums do, so that both are read and written 16 bytes a lane: [tile][wavefront][r][c][e][lane] of four rows
+template <typename C> __device__ __forceinline__ int64_t own_place(int64_t tile, int wave, int r, int c, int e, int lane)
+{
+    return ((((tile * C::WI * C::WJ + wave) * C::FI + r) * C::FJ + c) * 4 + e) * 64 + lane;
+}
+
+// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup
+template <typename T, typename C> __global__ void __launch_bounds__(kT) pack_kernel(Items q, const double *sums, int blocks, char *ws, Space sp, float scale)
+{
+    constexpr int P = C::P;
+    __shared__ float tile[32][33];
+    const Item &it = q.item[blockIdx.z];
+    char *base = ws + blockIdx.z * sp.bytes;
+    double sum = 0.0;
+    for (int k = threadIdx.x & 63; k < blocks; k += 64) sum += sums[blockIdx.z * kNormBlocks + k];
+    sum = wave_sum(sum);
+    const double over = sum == 0.0 ? 0.0 : 1.0 / sqrt(sum);
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t i0 = (int64_t)blockIdx.y * 32, j0 = (int64_t)blockIdx.x * 32; // of X
+    for (int k = ty; k < 32; k += 8) { // rows of the matrix, as they lie
+        const int64_t r = (it.flip ? j0 : i0) + k, c = (it.flip ? i0 : j0) + tx;
+        float v = 0.0f;
+        if (r < it.rows && c < it.cols) v = (float)((double)take<T>(q, it, (int)r, (int)c, false) * over);
+        tile[k][tx] = v;
+    }
+    __syncthreads();
+    half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[0]);
+    for (int k = ty; k < 32; k += 8) {
+        const float v = it.flip ? tile[tx][k] : tile[k][tx], w = it.flip ? tile[k][tx] : tile[tx][k]; // X[i0 + k][j0 + tx], X[i0 + tx][j0 + k]
+        half_t hv[P], hw[P];
+        pieces<P>(v * scale, hv);
+        pieces<P>(w * scale, hw);
+#pragma unroll
+        for (int o = 0; o < P; ++o) {
+            x[o * sp.Mp * sp.Np + plane_at(sp.Mp, i0 + k, j0 + tx)] = hv[o];
+            t[o * sp.Mp * sp.Np + plane_at(sp.Np, j0 + k, i0 + tx)] = hw[o];
+        }
+    }
+    { // as the products' sums lie: a 32 x 32 tile is 256 times four rows
+        const int e = threadIdx.x >> 6, lane = threadIdx.x & 63, i = e * 8 + (lane >> 5) * 4, j = lane & 31;
+        const int64_t ti = i0 / C::TI, tj = j0 / C::TJ;
+        const int wr = (int)(i0 % C::TI) / (C::FI * 32), wc = (int)(j0 % C::TJ) / (C::FJ * 32), r = (int)(i0 / 32) % C::FI, c = (int)(j0 / 32) % C::FJ;
+        f4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = it.flip ? tile[j][i + k] : tile[i + k][j];
+        reinterpret_cast<f4 *>(base + sp.xf)[own_place<C>(tj * (sp.Mp / C::TI) + ti, wr * C::WJ + wc, r, c, e, lane)] = v;
+    }
+}
+
+// Tile of a workgroup.  Workgroups are dealt to the 8 dies one by one, each with an L2 of its own: a die takes a stretch of tiles that are in
+// blocks of four columns (of four rows, SYMMETRIC), so that 32 of them read 12 strips of operands where 16 x 2 of them read 18.
+template <bool SYMMETRIC> __device__ __forceinline__ void place_of(int bid, int all, int tiles_i, int *ti, int *tj)
+{
+    constexpr int B = 4;
+    const int per = all / 8, t = bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
+    if (SYMMETRIC) {
+        int g = 0, r = t; // block of rows from g on, tile in it
+        for (;;) {
+            const int n = tiles_i - g < B ? tiles_i - g : B, have = n * g + n * (n + 1) / 2;
+            if (r < have) {
+                if (r < n * g) {
+                    *tj = r / n, *ti = g + r % n;
+                } else {
+                    r -= n * g;
+                    int c = 0;
+                    while (r >= n - c) r -= n - c, ++c;
+                    *tj = g + c, *ti = g + c + r;
+                }
+                return;
+            }
+            r -= have, g += B;
+        }
+    } else {
+        const int tiles_j = all / tiles_i, g = t / (tiles_i * B) * B, n = tiles_j - g < B ? tiles_j - g : B, r = t - g * tiles_i;
+        *ti = r / n, *tj = g + r % n;
     }
 }
 
@@ -440,30 +562,19 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
     const Space &sp = a.sp;
     char *base = a.ws + blockIdx.y * sp.bytes;
     int ti, tj;
-    {
-        const int all = gridDim.x, per = all / 8, bid = blockIdx.x;
-        // workgroups are dealt to the 8 dies one by one: neighbouring tiles to one of them
-        const int t = bid < per * 8 ? (bid & 7) * per + (bid >> 3) : bid;
-        if (MODE == MAKE_A || MODE == MAKE_B) {
-            ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-            while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-            while (ti * (ti + 1) / 2 > t) --ti;
-            tj = t - ti * (ti + 1) / 2;
-        } else {
-            ti = t % a.tiles_i, tj = t / a.tiles_i;
-        }
-    }
-    const int64_t Kp = a.K; // also the distance of rows of both operands
-    const half_t *p, *q;
-    int64_t p_plane, q_plane;
-    if (MODE == MAKE_A) p = q = reinterpret_cast<const half_t *>(base + sp.x), p_plane = q_plane = sp.Mp * sp.Np;
-    else if (MODE == MAKE_B) p = q = reinterpret_cast<const half_t *>(base + sp.A), p_plane = q_plane = sp.Mp * sp.Mp;
-    else p = reinterpret_cast<const half_t *>(base + sp.B), q = reinterpret_cast<const half_t *>(base + sp.t[a.turn]), p_plane = sp.Mp * sp.Mp, q_plane = sp.Mp * sp.Np;
-    p += (int64_t)ti * C::TI * Kp;
-    q += (int64_t)tj * C::TJ * Kp;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    place_of<MODE == MAKE_A || MODE == MAKE_B>(blockIdx.x, gridDim.x, a.tiles_i, &ti, &tj);
+    const int64_t Kp = MODE == MAKE_A ? sp.Np : sp.Mp;
+    const auto plane = [&](int64_t at) { return reinterpret_cast<const half_t *>(base + at); };
+    Operand p, q;
+    if (MODE == MAKE_A) p = q = {plane(sp.x), sp.Mp, sp.Mp * sp.Np};
+    else if (MODE == MAKE_B) p = q = {plane(sp.A), sp.Mp, sp.Mp * sp.Mp};
+    else p = {plane(sp.B), sp.Mp, sp.Mp * sp.Mp}, q = {plane(sp.t[a.turn]), sp.Np, sp.Mp * sp.Np};
+    p.at += (int64_t)ti * C::TI * 32;
+    q.at += (int64_t)tj * C::TJ * 32;
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = all / (C::WI * C::WJ), wave = all % (C::WI * C::WJ);
     Sums<C> acc;
-    product<C>(p, p_plane, q, q_plane, Kp, memory, lane, wave, acc);
+    product<C>(p, q, Kp, memory, lane, wave, team, acc);
+    if (team) return;
     const Step &st = a.st;
     const int64_t i0 = (int64_t)ti * C::TI + wave / C::WJ * C::FI * 32 + (lane >> 5) * 4, j0 = (int64_t)tj * C::TJ + wave % C::WJ * C::FJ * 32 + (lane & 31);
 #pragma unroll
@@ -475,14 +586,13 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
                 const int64_t ii = i0 + r * 32 + e * 8, jj = j0 + c * 32;
                 f4 v = {acc.v[r][c][e * 4], acc.v[r][c][e * 4 + 1], acc.v[r][c][e * 4 + 2], acc.v[r][c][e * 4 + 3]};
                 if (MODE == MAKE_A || MODE == MAKE_B) {
-                    float *Af = reinterpret_cast<float *>(base + sp.Af);
+                    f4 &Af = reinterpret_cast<f4 *>(base + sp.Af)[own_place<C>(ti * (ti + 1) / 2 + tj, wave, r, c, e, lane)];
                     half_t *out = reinterpret_cast<half_t *>(base + (MODE == MAKE_A ? sp.A : sp.B));
-                    const int64_t plane = sp.Mp * sp.Mp;
                     if (MODE == MAKE_A) {
                         v *= st.over_xx;
-                        *reinterpret_cast<f4 *>(Af + jj * sp.Mp + ii) = v; // A[j][i], i >= j by tiles: that half alone is read
+                        Af = v;
                     } else {
-                        v = st.b * *reinterpret_cast<const f4 *>(Af + jj * sp.Mp + ii) + st.c * st.over_AA * v;
+                        v = st.b * Af + st.c * st.over_AA * v;
                     }
                     h4 h[P];
 #pragma unroll
@@ -494,16 +604,14 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
                     }
 #pragma unroll
                     for (int o = 0; o < P; ++o) {
-                        *reinterpret_cast<h4 *>(out + o * plane + jj * sp.Mp + ii) = h[o];
+                        *reinterpret_cast<h4 *>(out + o * sp.Mp * sp.Mp + plane_at(sp.Mp, jj, ii)) = h[o];
                         if (ti != tj)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) out[o * plane + (ii + k) * sp.Mp + jj] = h[o][k];
+                            for (int k = 0; k < 4; ++k) out[o * sp.Mp * sp.Mp + plane_at(sp.Mp, ii + k, jj)] = h[o][k];
                     }
                 } else {
-                    float *xf = reinterpret_cast<float *>(base + sp.xf);
-                    const int64_t plane = sp.Mp * sp.Np;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = st.a * xf[(ii + k) * sp.Np + jj] + st.over_Bx * v[k];
+                    f4 &xf = reinterpret_cast<f4 *>(base + sp.xf)[own_place<C>((int64_t)tj * a.tiles_i + ti, wave, r, c, e, lane)];
+                    v = st.a * xf + st.over_Bx * v;
                     if (MODE == LAST_X) {
                         const Item &it = items.item[blockIdx.y];
 #pragma unroll
@@ -514,19 +622,19 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
                     } else {
                         half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[1 - a.turn]);
                         h4 h[P];
+                        xf = v;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            xf[(ii + k) * sp.Np + jj] = v[k];
                             half_t s[P];
                             pieces<P>(v[k] * st.next, s);
 #pragma unroll
                             for (int o = 0; o < P; ++o) {
-                                x[o * plane + (ii + k) * sp.Np + jj] = s[o];
+                                x[o * sp.Mp * sp.Np + plane_at(sp.Mp, ii + k, jj)] = s[o];
                                 h[o][k] = s[o];
                             }
                         }
 #pragma unroll
-                        for (int o = 0; o < P; ++o) *reinterpret_cast<h4 *>(t + o * plane + jj * sp.Mp + ii) = h[o];
+                        for (int o = 0; o < P; ++o) *reinterpret_cast<h4 *>(t + o * sp.Mp * sp.Np + plane_at(sp.Np, jj, ii)) = h[o];
                     }
                 }
             }
@@ -575,13 +683,31 @@ bool is_small(const pcsr_matrix_t &m) { return m.rows <= kSmall && m.cols <= kSm
 constexpr int kOnePiece = 256;
 int pieces_of(int type, int64_t m) { return type == PCSR_BF16 && m >= kOnePiece ? 1 : 2; }
 
-// large tiles (of 256 with one piece, of 128 with two) where there are enough of them for the compute units, of 64 otherwise
-bool large_tiles(int64_t m, int64_t n, int64_t count, int pieces)
+// The tiling of a group of matrices: the largest tiles of which the symmetric products have half as many as there are compute units; tiles of 64
+// otherwise, with two teams to a tile where a product has fewer tiles than compute units (one piece: always).  Five steps, us:
+//   one piece    64 (a team / two)   128    256     two pieces   64 (a team / two)   128
+//   512 x 512        103 /   97      141    326                      153 /  135      241
+//   1024 x 1024      164 /  144      213    503                      251 /  207      387
+//   1024 x 4096      304 /  258      345    776                      554 /  562      700
+//   2048 x 2048      483 /  477      405    802                     1029 / 1087      894
+//   3000 x 3000     1190             1016   1169                    2464            2477
+//   4096 x 4096     2566 / 2562     2030   1889                     5593 / 6208     5073
+//   8 of 512         157 /  156      179    385                      238 /  277      293
+//   16 of 300        131 /  133      172    403                      179 /  200      264
+//   4 of 1000        285 /  299      271    540                      622 /  676      527
+enum Which { SMALL1, MIDDLE1, LARGE1, FEW2, SMALL2, LARGE2 };
+Which tiling_of(int64_t m, int64_t n, int64_t count, int pieces)
 {
-    const int64_t t = pieces == 1 ? 256 : 128, tiles = ((m + t - 1) / t) * ((n + t - 1) / t) * count;
-    return tiles >= 128;
+    constexpr int64_t kUnits = 256;
+    const auto half_full = [&](int64_t t) {
+        const int64_t a = (m + t - 1) / t;
+        return a * (a + 1) / 2 * count >= kUnits / 2;
+    };
+    if (pieces == 1) return half_full(256) ? LARGE1 : half_full(128) ? MIDDLE1 : SMALL1;
+    if (half_full(128)) return LARGE2;
+    return (m + 63) / 64 * ((n + 63) / 64) * count <= kUnits ? FEW2 : SMALL2;
 }
-int tile_of(int64_t m, int64_t n, int64_t count, int pieces) { return large_tiles(m, n, count, pieces) ? (pieces == 1 ? 256 : 128) : 64; }
+int tile_of(Which w) { return w == LARGE1 ? 256 : w == MIDDLE1 || w == LARGE2 ? 128 : 64; }
 
 // the matrices from `first` on that go with it in one launch
 int64_t group_of(const pcsr_matrix_t *m, int64_t count, int64_t first, const char *done, int64_t *members)
@@ -600,7 +726,7 @@ int64_t group_bytes(const pcsr_matrix_t &x, int64_t n, int type)
 {
     if (is_small(x)) return 0;
     const int64_t m = x.rows < x.cols ? x.rows : x.cols, w = x.rows < x.cols ? x.cols : x.rows;
-    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, tile_of(m, w, n, pieces_of(type, m)), pieces_of(type, m)).bytes;
+    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, tile_of(tiling_of(m, w, n, pieces_of(type, m))), pieces_of(type, m)).bytes;
 }
 
 int ortho_check(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t *how)
@@ -642,13 +768,12 @@ template <typename T, typename C> int run_large(const Items &q, int n, const Ste
     const int64_t want = (m * w + kT * 4 - 1) / (kT * 4);
     const int blocks = (int)(want < kNormBlocks ? want : kNormBlocks);
     hipLaunchKernelGGL((measure_kernel<T>), dim3(blocks, n), dim3(kT), 0, s, q, sums);
-    hipLaunchKernelGGL((pack_kernel<T, C::P>), dim3((unsigned)(sp.Np / 32), (unsigned)(sp.Mp / 32), n), dim3(kT), 0, s, q, sums, blocks, ws, sp, step[0].x);
+    hipLaunchKernelGGL((pack_kernel<T, C>), dim3((unsigned)(sp.Np / 32), (unsigned)(sp.Mp / 32), n), dim3(kT), 0, s, q, sums, blocks, ws, sp, step[0].x);
     const unsigned ti = (unsigned)(sp.Mp / C::TI), tj = (unsigned)(sp.Np / C::TJ), sym = ti * (ti + 1) / 2;
     bool ok = true;
     for (int k = 0; k < steps && ok; ++k) {
-        ProductArgs a = {ws, sp, step[k], sp.Np, (int)ti, k & 1};
+        const ProductArgs a = {ws, sp, step[k], (int)ti, k & 1};
         ok = run_product<float, C, MAKE_A>(a, q, sym, n, s); // (the type matters to the last alone)
-        a.K = sp.Mp;
         ok = ok && run_product<float, C, MAKE_B>(a, q, sym, n, s);
         ok = ok && (k + 1 < steps ? run_product<float, C, MAKE_X>(a, q, ti * tj, n, s) : run_product<T, C, LAST_X>(a, q, ti * tj, n, s));
     }
@@ -707,12 +832,22 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
             if (is_small(m[k])) return m[k].rows > 64 || m[k].cols > 64 ? run_small<T, 2>(a, used, s) : run_small<T, 1>(a, used, s);
             const int64_t lo = m[k].rows < m[k].cols ? m[k].rows : m[k].cols, hi = m[k].rows < m[k].cols ? m[k].cols : m[k].rows;
             char *at = static_cast<char *>(ws);
-            const int pieces = pieces_of(how->type, lo);
-            const bool large = large_tiles(lo, hi, used, pieces);
-            if constexpr (std::is_same<T, bfloat_t>::value) {
-                if (pieces == 1) return large ? run_large<T, Large1>(a.q, used, a.step, a.steps, at, s) : run_large<T, Small1>(a.q, used, a.step, a.steps, at, s);
+            const auto run = [&](auto tiling) { return run_large<T, decltype(tiling)>(a.q, used, a.step, a.steps, at, s); };
+            switch (tiling_of(lo, hi, used, pieces_of(how->type, lo))) {
+            case SMALL1:
+                if constexpr (std::is_same<T, bfloat_t>::value) return run(Small1{});
+                break;
+            case MIDDLE1:
+                if constexpr (std::is_same<T, bfloat_t>::value) return run(Middle1{});
+                break;
+            case LARGE1:
+                if constexpr (std::is_same<T, bfloat_t>::value) return run(Large1{});
+                break;
+            case FEW2: return run(Few2{});
+            case SMALL2: return run(Small2{});
+            case LARGE2: return run(Large2{});
             }
-            return large ? run_large<T, Large2>(a.q, used, a.step, a.steps, at, s) : run_large<T, Small2>(a.q, used, a.step, a.steps, at, s);
+            return (int)PCSR_E_UNSUPPORTED; // (one piece is for bf16 alone)
         });
         if (r != PCSR_OK) return r;
     }

@@ -10,6 +10,8 @@
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <vector>
 
@@ -231,14 +233,14 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
 }
 
 // ------------------------------------------------------------------ orthogonalised updates
-// update(weights, momenta, rates, steps, address of coefficients, nesterov, momentum, keep): matrices of one type in lists; their
-// gradients are what .grad holds.  The library's code, or NotImplemented where one of them is not taken as it is (nothing was done then).
+// update(weights, momenta, lr, steps, address of coefficients, nesterov, momentum, keep): matrices of one type in lists; their gradients
+// are what .grad holds.  The library's code, or NotImplemented where one of them is not taken as it is (nothing was done then).
 PyObject *update(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 8 || !ready || !PyList_Check(args[0]) || !PyList_Check(args[1]) || !PyList_Check(args[2])) Py_RETURN_NOTIMPLEMENTED;
+    if (n != 8 || !ready || !PyList_Check(args[0]) || !PyList_Check(args[1])) Py_RETURN_NOTIMPLEMENTED;
     const Py_ssize_t count = PyList_GET_SIZE(args[0]);
-    if (PyList_GET_SIZE(args[1]) != count || PyList_GET_SIZE(args[2]) != count || count == 0) Py_RETURN_NOTIMPLEMENTED;
+    if (PyList_GET_SIZE(args[1]) != count || count == 0) Py_RETURN_NOTIMPLEMENTED;
     pcsr_ortho_t how = {};
     how.steps = (int32_t)PyLong_AsLong(args[3]);
     how.coefficients = static_cast<const double *>(PyLong_AsVoidPtr(args[4]));
@@ -246,6 +248,7 @@ PyObject *update(PyObject *, PyObject *const *args, Py_ssize_t n)
     how.nesterov = PyObject_IsTrue(args[5]);
     how.momentum = (float)PyFloat_AsDouble(args[6]);
     how.keep = (float)PyFloat_AsDouble(args[7]);
+    const double lr = PyFloat_AsDouble(args[2]);
     if (PyErr_Occurred()) return nullptr;
     std::vector<pcsr_matrix_t> m((size_t)count);
     at::Tensor first;
@@ -262,8 +265,7 @@ PyObject *update(PyObject *, PyObject *const *args, Py_ssize_t n)
             w.dim() != 2 || w.sizes() != g.sizes() || w.sizes() != b.sizes() || w.numel() == 0)
             Py_RETURN_NOTIMPLEMENTED;
         const int64_t wl = distance(w), gl = distance(g), bl = distance(b);
-        const double rate = PyFloat_AsDouble(PyList_GET_ITEM(args[2], k));
-        if (PyErr_Occurred()) return nullptr;
+        const double rate = lr * std::sqrt(std::max(1.0, (double)w.size(0) / (double)w.size(1)));
         if (wl < 0 || gl < 0 || bl < 0) Py_RETURN_NOTIMPLEMENTED;
         m[(size_t)k] = {g.const_data_ptr(), b.mutable_data_ptr<float>(), w.mutable_data_ptr(), w.size(0), w.size(1), gl, bl, wl, (float)rate, 0};
     }

@@ -10,6 +10,7 @@ launch for up to 24 of them, larger ones three per Newton-Schulz step for all of
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 
 import torch
@@ -24,6 +25,14 @@ COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 def _coefficients(coefficients, steps):
     """ctypes array of (a, b, c) for each step"""
+    try:
+        return _coefficient_array(coefficients, steps)
+    except TypeError:  # lists cannot be looked up
+        return _coefficient_array.__wrapped__(coefficients, steps)
+
+
+@functools.lru_cache(maxsize=64)
+def _coefficient_array(coefficients, steps):
     if not isinstance(steps, int) or not 1 <= steps <= MAX_STEPS:
         raise ValueError(f"steps must be 1 to {MAX_STEPS}")
     rows = list(coefficients)
@@ -117,45 +126,51 @@ class Muon(torch.optim.Optimizer):
                 if "momentum" in state_dict["state"].get(k, {}):
                     self.state[p]["momentum"] = state_dict["state"][k]["momentum"].to(p.device, torch.float32, copy=True)
 
-    @torch.no_grad()
     def step(self, closure=None):
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        fast = pc.train_module()
         for group in self.param_groups:
-            steps, co = group["steps"], _coefficients(group["coefficients"], group["steps"])
-            lr, momentum, keep = float(group["lr"]), float(group["momentum"]), 1.0 - float(group["lr"] * group["weight_decay"])
-            params = [p for p in group["params"] if p.grad is not None and p.numel()]
-            if not params:
-                continue
-            bufs = [self._momentum(p) for p in params]
-            rates = [lr * math.sqrt(max(1.0, p.shape[0] / p.shape[1])) for p in params]
-            fast = pc.train_module()
+            steps, nesterov, momentum, lr = group["steps"], group["nesterov"], float(group["momentum"]), float(group["lr"])
+            keep = 1.0 - lr * float(group["weight_decay"])
+            co = _coefficients(group["coefficients"], steps)
             if fast is not None:
-                rc = fast.update(params, bufs, rates, steps, ctypes.addressof(co), group["nesterov"], momentum, keep)
-                if rc is not NotImplemented:
-                    if rc != pc.PCSR_OK:
-                        raise pc.PcsrError(rc, "pcsr_orthogonalize")
-                    continue
-            by_type, back = {}, []
-            for p, buf, rate in zip(params, bufs, rates):
-                if not p.is_cuda or p.grad.layout != torch.strided or p.grad.dtype != p.dtype:
-                    raise ValueError("Muon steps dense matrices on a GPU, with gradients of their type")
-                grad, out = p.grad, p.detach()
-                if _ld(grad) is None:
-                    grad = grad.contiguous()
-                if _ld(out) is None:
-                    out = out.contiguous()
-                    back.append((p, out))
-                by_type.setdefault((p.dtype, p.device), []).append((grad, pc.pcsr_matrix_t(
-                    grad.data_ptr(), buf.data_ptr(), out.data_ptr(), *p.shape, _ld(grad), _ld(buf), _ld(out), rate, 0)))
-            for (dtype, device), mats in by_type.items():
-                _run([m for _, m in mats], dtype, device, steps, co, True, group["nesterov"], momentum, keep)
-            for p, out in back:
-                p.copy_(out)
-            torch.autograd.graph.increment_version(params)
+                try:
+                    bufs = [self.state[p]["momentum"] for p in group["params"]]
+                except KeyError:  # the first step
+                    bufs = None
+                if bufs:
+                    rc = fast.update(group["params"], bufs, lr, steps, ctypes.addressof(co), nesterov, momentum, keep)
+                    if rc is not NotImplemented:
+                        if rc != pc.PCSR_OK:
+                            raise pc.PcsrError(rc, "pcsr_orthogonalize")
+                        continue
+            self._step_group(group, steps, nesterov, momentum, lr, keep, co)
         return loss
+
+    @torch.no_grad()
+    def _step_group(self, group, steps, nesterov, momentum, lr, keep, co):
+        by_type, back = {}, []
+        params = [p for p in group["params"] if p.grad is not None and p.numel()]
+        for p in params:
+            if not p.is_cuda or p.grad.layout != torch.strided or p.grad.dtype != p.dtype:
+                raise ValueError("Muon steps dense matrices on a GPU, with gradients of their type")
+            buf, grad, out = self._momentum(p), p.grad, p.detach()
+            if _ld(grad) is None:
+                grad = grad.contiguous()
+            if _ld(out) is None:
+                out = out.contiguous()
+                back.append((p, out))
+            rate = lr * math.sqrt(max(1.0, p.shape[0] / p.shape[1]))
+            by_type.setdefault((p.dtype, p.device), []).append((grad, pc.pcsr_matrix_t(
+                grad.data_ptr(), buf.data_ptr(), out.data_ptr(), *p.shape, _ld(grad), _ld(buf), _ld(out), rate, 0)))
+        for (dtype, device), mats in by_type.items():
+            _run([m for _, m in mats], dtype, device, steps, co, True, nesterov, momentum, keep)
+        for p, out in back:
+            p.copy_(out)
+        torch.autograd.graph.increment_version(params)
 
     def _momentum(self, p):
         state = self.state[p]
