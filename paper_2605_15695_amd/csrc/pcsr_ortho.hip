@@ -651,20 +651,32 @@ float power_below(double bound) // the power of two that takes numbers up to `bo
     return (float)std::ldexp(1.0, e);
 }
 
+// Largest magnitudes of b w + c w^2 and of v (a + b w + c w^2), w = v^2, for v in [0, s]: at the end or where the slope is 0.
+void largest(double a, double b, double c, double s, double *of_B, double *of_x)
+{
+    const double end = s * s;
+    const auto B = [&](double w) { return std::fabs(w * (b + c * w)); };
+    const auto x = [&](double w) { return std::fabs(std::sqrt(w) * (a + w * (b + c * w))); };
+    *of_B = B(end), *of_x = x(end);
+    const auto look = [&](double w) { // (a NaN is nowhere)
+        if (w > 0.0 && w < end) *of_B = std::fmax(*of_B, B(w)), *of_x = std::fmax(*of_x, x(w));
+    };
+    look(-b / (2.0 * c));
+    const double d = 9.0 * b * b - 20.0 * a * c, r = std::sqrt(d); // a + 3 b w + 5 c w^2 = 0
+    look((-3.0 * b + r) / (10.0 * c));
+    look((-3.0 * b - r) / (10.0 * c));
+    look(-a / (3.0 * b)); // c = 0
+}
+
 // Powers of two of every step, from the largest singular value that can occur: X0's is 1 at most.  false: they leave fp32's range.
 bool plan_steps(const pcsr_ortho_t &how, Step *out)
 {
     double s = 1.0;
-    constexpr int N = 4096;
     float x = power_below(s * 1.01);
     for (int k = 0; k < how.steps; ++k) {
         const double a = how.coefficients[3 * k], b = how.coefficients[3 * k + 1], c = how.coefficients[3 * k + 2];
         double most_B = 0.0, most_x = 0.0;
-        for (int i = 0; i <= N; ++i) {
-            const double v = s * i / N, w = v * v;
-            most_B = std::fmax(most_B, std::fabs(b * w + c * w * w));
-            most_x = std::fmax(most_x, std::fabs(v * (a + b * w + c * w * w)));
-        }
+        largest(a, b, c, s, &most_B, &most_x);
         if (!(std::isfinite(a) && std::isfinite(b) && std::isfinite(c)) || !(most_x < 0x1p24) || !(most_B < 0x1p100)) return false;
         Step &st = out[k];
         st.a = (float)a, st.b = (float)b, st.c = (float)c;
@@ -695,17 +707,16 @@ int pieces_of(int type, int64_t m) { return type == PCSR_BF16 && m >= kOnePiece 
 //   8 of 512         157 /  156      179    385                      238 /  277      293
 //   16 of 300        131 /  133      172    403                      179 /  200      264
 //   4 of 1000        285 /  299      271    540                      622 /  676      527
-enum Which { SMALL1, MIDDLE1, LARGE1, FEW2, SMALL2, LARGE2 };
+constexpr int64_t kUnits = 256; // compute units
+enum Which { SMALL1, MIDDLE1, LARGE1, SMALL2, LARGE2 };
 Which tiling_of(int64_t m, int64_t n, int64_t count, int pieces)
 {
-    constexpr int64_t kUnits = 256;
     const auto half_full = [&](int64_t t) {
         const int64_t a = (m + t - 1) / t;
         return a * (a + 1) / 2 * count >= kUnits / 2;
     };
     if (pieces == 1) return half_full(256) ? LARGE1 : half_full(128) ? MIDDLE1 : SMALL1;
-    if (half_full(128)) return LARGE2;
-    return (m + 63) / 64 * ((n + 63) / 64) * count <= kUnits ? FEW2 : SMALL2;
+    return half_full(128) ? LARGE2 : SMALL2;
 }
 int tile_of(Which w) { return w == LARGE1 ? 256 : w == MIDDLE1 || w == LARGE2 ? 128 : 64; }
 
@@ -773,9 +784,16 @@ template <typename T, typename C> int run_large(const Items &q, int n, const Ste
     bool ok = true;
     for (int k = 0; k < steps && ok; ++k) {
         const ProductArgs a = {ws, sp, step[k], (int)ti, k & 1};
-        ok = run_product<float, C, MAKE_A>(a, q, sym, n, s); // (the type matters to the last alone)
-        ok = ok && run_product<float, C, MAKE_B>(a, q, sym, n, s);
-        ok = ok && (k + 1 < steps ? run_product<float, C, MAKE_X>(a, q, ti * tj, n, s) : run_product<T, C, LAST_X>(a, q, ti * tj, n, s));
+        const auto run = [&](auto type, auto mode, unsigned tiles) {
+            typedef decltype(type) U;
+            constexpr int MODE = decltype(mode)::value;
+            if constexpr (std::is_same<C, Small2>::value) // the same tiles and places
+                if ((int64_t)tiles * n <= kUnits) return run_product<U, Few2, MODE>(a, q, tiles, n, s);
+            return run_product<U, C, MODE>(a, q, tiles, n, s);
+        };
+        ok = run(float{}, std::integral_constant<int, MAKE_A>{}, sym); // (the type matters to the last alone)
+        ok = ok && run(float{}, std::integral_constant<int, MAKE_B>{}, sym);
+        ok = ok && (k + 1 < steps ? run(float{}, std::integral_constant<int, MAKE_X>{}, ti * tj) : run(T{}, std::integral_constant<int, LAST_X>{}, ti * tj));
     }
     return ok ? PCSR_OK : PCSR_E_HIP;
 }
@@ -843,7 +861,6 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
             case LARGE1:
                 if constexpr (std::is_same<T, bfloat_t>::value) return run(Large1{});
                 break;
-            case FEW2: return run(Few2{});
             case SMALL2: return run(Small2{});
             case LARGE2: return run(Large2{});
             }
