@@ -32,6 +32,15 @@ struct EmbedArgs {
     float scale;
 };
 
+// A row's 16-byte piece number `piece`: its first number and how many it has.  The last piece of a row whose width is no multiple of one
+// begins early, so that it is whole: two lanes then work out the same numbers.  (Rows of less than a piece have one short one.)
+template <int N> __device__ __forceinline__ int64_t piece_at(int64_t piece, int64_t d, int *m)
+{
+    *m = d < N ? (int)d : N;
+    const int64_t c = piece * N;
+    return d < N ? 0 : (c <= d - N ? c : d - N);
+}
+
 template <typename I> __device__ __forceinline__ int64_t id_at(const void *ids, int64_t i)
 {
     return (int64_t) reinterpret_cast<const I *>(ids)[i];
@@ -51,8 +60,10 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) l
         row[k] = first + k < p.n ? id_at<I>(p.ids, first + k) : -1;
         if (row[k] >= p.rows) row[k] = -1;
     }
-    for (int64_t c = (int64_t)lane * N; c < p.d; c += L * N) {
-        const int m = p.d - c < N ? (int)(p.d - c) : N;
+    const int64_t pieces = (p.d + N - 1) / N;
+    for (int64_t piece = lane; piece < pieces; piece += L) {
+        int m;
+        const int64_t c = piece_at<N>(piece, p.d, &m);
         float x[kAhead][N];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -163,7 +174,7 @@ struct SortArgs { // one pass over a digit of the keys
     const void *ids;        // in the first pass
     const uint32_t *kin, *vin;
     uint32_t *kout, *vout;
-    int32_t *counts, *totals; // [digit][tile], [digit]
+    int32_t *counts, *totals; // [tile][digit], [digit]
 };
 template <typename I, bool FIRST> __device__ __forceinline__ uint32_t sort_key(const SortArgs &p, int64_t t)
 {
@@ -184,7 +195,7 @@ template <typename I, bool FIRST> __global__ void __launch_bounds__(kT) count_ke
     for (int64_t t = t0 + threadIdx.x; t < t1; t += kT)
         atomicAdd(&cnt[(sort_key<I, FIRST>(p, t) >> p.shift) & (bins - 1)], 1);
     __syncthreads();
-    for (int d = threadIdx.x; d < bins; d += kT) p.counts[(int64_t)d * p.tiles + blockIdx.x] = cnt[d];
+    for (int d = threadIdx.x; d < bins; d += kT) p.counts[(int64_t)blockIdx.x * bins + d] = cnt[d];
 }
 
 __device__ __forceinline__ int32_t wave_upto(int32_t v, int lane)
@@ -197,24 +208,32 @@ __device__ __forceinline__ int32_t wave_upto(int32_t v, int lane)
     return v;
 }
 
-// counts of a digit, summed over the tiles before (in place); its total
-__global__ void __launch_bounds__(kT) tiles_kernel(int bins, int tiles, int32_t *counts, int32_t *totals, int sorters, Fill f)
+// Counts of a digit, summed over the tiles before (in place); its total.  64 digits to a workgroup, a stretch of the tiles to each of its wavefronts.
+constexpr int kTilesT = 1024;
+__global__ void __launch_bounds__(kTilesT) tiles_kernel(int bins, int tiles, int32_t *counts, int32_t *totals, int sorters, Fill f)
 {
     if ((int)blockIdx.x >= sorters) {
         fill(f, blockIdx.x - sorters, gridDim.x - sorters);
         return;
     }
-    const int lane = threadIdx.x & 63, d = blockIdx.x * (kT / 64) + (threadIdx.x >> 6);
-    if (d >= bins) return;
-    int32_t *row = counts + (int64_t)d * tiles;
+    constexpr int W = kTilesT / 64, N = kTiles / W;
+    __shared__ int32_t sums[W][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane, per = (tiles + W - 1) / W, t0 = wave * per;
+    int32_t v[N], all = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = k < per && t0 + k < tiles && d < bins ? counts[(int64_t)(t0 + k) * bins + d] : 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) all += v[k];
+    sums[wave][lane] = all;
+    __syncthreads();
     int32_t before = 0;
-    for (int k = 0; k < tiles; k += 64) {
-        const int32_t v = k + lane < tiles ? row[k + lane] : 0;
-        const int32_t upto = wave_upto(v, lane);
-        if (k + lane < tiles) row[k + lane] = before + upto - v;
-        before += __shfl(upto, 63);
+    for (int w = 0; w < wave; ++w) before += sums[w][lane];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if (k < per && t0 + k < tiles && d < bins) counts[(int64_t)(t0 + k) * bins + d] = before;
+        before += v[k];
     }
-    if (lane == 0) totals[d] = before;
+    if (wave == W - 1 && d < bins) totals[d] = before;
 }
 
 // A wavefront ranks 64 ids at a time by ballots over the digit's bits, in the order they come, and keeps its own
@@ -243,7 +262,7 @@ template <typename I, bool FIRST> __global__ void __launch_bounds__(kT) scatter_
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int d = tid * N + k;
-            if (d < bins) next[d] = ex + p.counts[(int64_t)d * p.tiles + blockIdx.x];
+            if (d < bins) next[d] = ex + p.counts[(int64_t)blockIdx.x * bins + d];
             ex += v[k];
         }
     }
@@ -328,10 +347,11 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) runs_kernel(G
 {
     constexpr int N = kPer16<T>, G = kT / L;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int64_t g = (int64_t)blockIdx.x * G + group, c = ((int64_t)blockIdx.y * L + lane) * N;
+    const int64_t g = (int64_t)blockIdx.x * G + group, piece = (int64_t)blockIdx.y * L + lane;
     const int64_t t0 = g * p.tile, t1 = t0 + p.tile < p.n ? t0 + p.tile : p.n;
-    if (t0 >= p.n || c >= p.d) return;
-    const int m = p.d - c < N ? (int)(p.d - c) : N;
+    if (t0 >= p.n || piece * N >= p.d) return;
+    int m;
+    const int64_t c = piece_at<N>(piece, p.d, &m);
     const T *dout = static_cast<const T *>(p.dout);
     uint32_t cur = p.key[t0];
     bool before = t0 > 0 && p.key[t0 - 1] == cur; // the run of cur began before the tile
@@ -385,9 +405,10 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(G
     __shared__ float shared[G][L * N];
     __shared__ int64_t last_of[G];
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int64_t g0 = (int64_t)blockIdx.x * G, g = g0 + group, c = ((int64_t)blockIdx.y * L + lane) * N;
-    const bool in = c < p.d;
-    const int m = !in ? 0 : p.d - c < N ? (int)(p.d - c) : N;
+    const int64_t g0 = (int64_t)blockIdx.x * G, g = g0 + group, piece = (int64_t)blockIdx.y * L + lane;
+    const bool in = piece * N < p.d;
+    int m;
+    const int64_t c = piece_at<N>(piece, p.d, &m);
     const int64_t t0 = g * p.tile, t1 = t0 + p.tile;
     int64_t last = 0; // the last tile of the run, 0 = none begins here
     uint32_t row = 0;
@@ -473,10 +494,11 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
     __shared__ int heavy[256];
     const int tid = threadIdx.x, lane64 = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid % L, group = tid / L, n = (int)p.n, per = (n + W - 1) / W;
-    const int64_t r0 = (int64_t)blockIdx.x * p.own, c = ((int64_t)blockIdx.y * L + lane) * N;
+    const int64_t r0 = (int64_t)blockIdx.x * p.own, piece = (int64_t)blockIdx.y * L + lane;
     const int rows = p.rows - r0 < p.own ? (int)(p.rows - r0) : p.own;
-    const bool in = c < p.d;
-    const int m = !in ? 0 : p.d - c < N ? (int)(p.d - c) : N;
+    const bool in = piece * N < p.d;
+    int m;
+    const int64_t c = piece_at<N>(piece, p.d, &m);
     const T *dout = static_cast<const T *>(p.dout);
     T *grad = static_cast<T *>(p.grad) + r0 * p.d + c;
     uint32_t *mine = list + wave * per;
@@ -586,10 +608,15 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
     }
 }
 
-// lanes to a row of `vectors` of 16 bytes: as many as leave the fewest idle, the most of those
-int lanes_for(int64_t vectors)
+// lanes to a row of `vectors` of 16 bytes: as many as leave the fewest idle, the most of those; where rows are so few that lanes are
+// idle anyhow, enough to have all of a row on its way at once
+int lanes_for(int64_t vectors, int64_t rows)
 {
     int best = 64;
+    if (rows * vectors < (1 << 17)) {
+        while (best > 4 && best / 2 >= vectors) best /= 2;
+        return best;
+    }
     int64_t cost = INT64_MAX;
     for (int l = 64; l >= 4; l /= 2) {
         const int64_t c = (vectors + l - 1) / l * l;
@@ -625,7 +652,7 @@ template <typename V> GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, V p
 {
     GradPlan q;
     const int64_t vectors = (d + per16 - 1) / per16;
-    q.lanes = lanes_for(vectors);
+    q.lanes = lanes_for(vectors, n > kOwnMost ? n : rows);
     q.slices = (vectors + q.lanes - 1) / q.lanes;
     // enough groups to keep the memory busy, long enough tiles that few runs cross them
     q.tile = 64;
@@ -741,9 +768,9 @@ template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, con
         } else {
             hipLaunchKernelGGL((count_kernel<I, false>), grid, dim3(kT), 0, s, p, part);
         }
-        const int bins = 1 << p.bits, sorters = (bins + kT / 64 - 1) / (kT / 64);
+        const int bins = 1 << p.bits, sorters = (bins + 63) / 64;
         part = share(1);
-        hipLaunchKernelGGL(tiles_kernel, dim3(sorters + fillers(part.bytes, kT)), dim3(kT), 0, s, bins, p.tiles, p.counts, p.totals, sorters, part);
+        hipLaunchKernelGGL(tiles_kernel, dim3(sorters + fillers(part.bytes, kTilesT)), dim3(kTilesT), 0, s, bins, p.tiles, p.counts, p.totals, sorters, part);
         part = share(2);
         grid = dim3(p.tiles + fillers(part.bytes, kT));
         if (i == 0)
@@ -774,7 +801,7 @@ int pcsr_embed(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids
     EmbedArgs p = {n, rows, d, stride, ids, table, out, scale};
     return for_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const int lanes = lanes_for((d + kPer16<T> - 1) / kPer16<T>);
+        const int lanes = lanes_for((d + kPer16<T> - 1) / kPer16<T>, n);
         if (wide)
             for_lanes<Lookup<T, int64_t>::template Of>(lanes, p, s);
         else

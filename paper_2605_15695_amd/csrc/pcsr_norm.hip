@@ -54,6 +54,7 @@ struct NormArgs {
     int64_t longer, chunk; // a graph of more rows is long; rows of a chunk, no more than that
     int shorts, chunks;    // workgroups for short graphs, for chunks
     void *part;            // [chunk][kSlots][groups] pairs of doubles (forward) or floats (backward)
+    int32_t *met;          // [chunk]: whether it meets a long graph, for the kernels behind the first
 };
 
 __device__ __forceinline__ int64_t begin_of(const NormArgs &a, int64_t s)
@@ -64,20 +65,33 @@ __device__ __forceinline__ int64_t begin_of(const NormArgs &a, int64_t s)
     const int64_t o = a.wide ? static_cast<const int64_t *>(a.offsets)[s] : (int64_t) static_cast<const int32_t *>(a.offsets)[s];
     return o < 0 ? 0 : (o < a.rows ? o : a.rows);
 }
-// the last graph that begins at or before a row, found by a wavefront: 64 probes at a time, since such a search is bound by its
-// round trips (20,000 graphs: three of them).  All lanes ask for the same row.
-__device__ __forceinline__ int64_t graph_of(const NormArgs &a, int64_t row)
+// The last graphs that begin at or before two rows, found by a wavefront: 64 probes at a time and for both, since such a search is bound by
+// its round trips (20,000 graphs: three of them).  All lanes ask for the same rows.
+__device__ __forceinline__ void graphs_of(const NormArgs &a, const int64_t (&row)[2], int64_t (&graph)[2])
 {
-    if (!a.offsets) return a.length > 0 ? row / a.length : 0;
-    const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = a.graphs; // lo begins there or before
-    while (hi - lo > 1) {
-        const int64_t step = (hi - lo + 63) / 64, probe = lo + lane * step;
-        const int below = __popcll(__ballot(probe < hi && begin_of(a, probe) <= row)); // 1 at least: lane 0's
-        lo += (int64_t)(below > 0 ? below - 1 : 0) * step;
-        hi = hi < lo + step ? hi : lo + step;
+    if (!a.offsets) {
+        for (int k = 0; k < 2; ++k) graph[k] = a.length > 0 ? row[k] / a.length : 0;
+        return;
     }
-    return lo;
+    const int lane = threadIdx.x & 63;
+    int64_t lo[2] = {0, 0}, hi[2] = {a.graphs, a.graphs}; // lo begins there or before
+    while (hi[0] - lo[0] > 1 || hi[1] - lo[1] > 1) {
+        int64_t step[2], at[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            step[k] = (hi[k] - lo[k] + 63) / 64;
+            const int64_t probe = lo[k] + lane * step[k];
+            at[k] = begin_of(a, probe < hi[k] ? probe : a.graphs); // (behind the end: all rows, more than any)
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int below = __popcll(__ballot(at[k] <= row[k])); // 1 at least: lane 0's
+            lo[k] += (int64_t)(below > 0 ? below - 1 : 0) * step[k];
+            hi[k] = hi[k] < lo[k] + step[k] ? hi[k] : lo[k] + step[k];
+            if (lo[k] >= hi[k]) lo[k] = hi[k] - 1; // offsets that do not ascend
+        }
+    }
+    graph[0] = lo[0], graph[1] = lo[1];
 }
 
 __device__ __forceinline__ float param(const void *p, int type, int64_t c)
@@ -314,17 +328,28 @@ template <typename T, bool ONE, int A> __device__ __forceinline__ void add_squar
     }
 }
 
-// the part of the graph that has a chunk's first (slot 0) or last row (slot 1) that lies in the chunk, if the graph is long
+// The parts of the graphs that have a chunk's first (slot 0) and last row (slot 1) that lie in the chunk, if those graphs are long; the second only
+// if it is another one.
 struct ChunkPart {
     int64_t lo, hi, graph, first, end; // rows of the part, its graph and the graph's rows
     bool any;
-    __device__ ChunkPart(const NormArgs &a, int64_t j, int slot)
+};
+struct ChunkParts {
+    ChunkPart part[kSlots];
+    __device__ __forceinline__ ChunkPart at(int slot) const { return slot ? part[1] : part[0]; } // (in registers)
+    __device__ ChunkParts(const NormArgs &a, int64_t j)
     {
-        lo = j * a.chunk, hi = lo + a.chunk < a.rows ? lo + a.chunk : a.rows;
-        graph = graph_of(a, slot ? hi - 1 : lo);
-        first = begin_of(a, graph), end = begin_of(a, graph + 1);
-        any = end - first > a.longer && (slot == 0 || first > lo);
-        lo = lo > first ? lo : first, hi = hi < end ? hi : end;
+        const int64_t lo = j * a.chunk, hi = lo + a.chunk < a.rows ? lo + a.chunk : a.rows;
+        const int64_t row[2] = {lo, hi - 1};
+        int64_t graph[2];
+        graphs_of(a, row, graph);
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k) {
+            ChunkPart &p = part[k];
+            p.graph = graph[k], p.first = begin_of(a, graph[k]), p.end = begin_of(a, graph[k] + 1);
+            p.any = p.end - p.first > a.longer && (k == 0 || p.first > lo);
+            p.lo = lo > p.first ? lo : p.first, p.hi = hi < p.end ? hi : p.end;
+        }
     }
 };
 
@@ -334,8 +359,10 @@ template <typename T, bool ONE> __device__ __forceinline__ void chunk_sums(const
     constexpr int N = kPer16<T>, A = ONE ? 1 : N;
     if ((int)blockIdx.y >= a.many.slices) return;
     const Place<false> at(a, a.many, N);
+    const ChunkParts parts(a, j);
+    if (threadIdx.x == 0 && blockIdx.y == 0) a.met[j] = parts.part[0].any || parts.part[1].any;
     for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
+        const ChunkPart p = parts.at(slot);
         if (!p.any) continue;
         double s[A], q[A];
 #pragma unroll
@@ -433,8 +460,10 @@ template <typename V, typename F> __device__ __forceinline__ void add_chunks(con
         add(j, j * a.length, (j + 1) * a.length);
         return;
     }
+    if (!a.met[j]) return;
+    const ChunkParts parts(a, j);
     for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
+        const ChunkPart p = parts.at(slot);
         if (p.any && p.lo == p.first) add(p.graph, p.first, p.end);
     }
 }
@@ -448,13 +477,15 @@ __global__ void __launch_bounds__(32 * kGroupsOf) norm_combine_kernel(NormArgs a
 template <typename T> __global__ void __launch_bounds__(kMost) norm_apply_kernel(NormArgs a)
 {
     constexpr int N = kPer16<T>;
+    const int64_t j = gridDim.x - 1 - blockIdx.x;
+    if (!a.met[j]) return;
     const Place<false> at(a, a.many, N);
     Channel<N> ch;
     ch.params(a, at);
-    const int64_t j = gridDim.x - 1 - blockIdx.x;
     T *y = static_cast<T *>(a.y);
+    const ChunkParts parts(a, j);
     for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
+        const ChunkPart p = parts.at(slot);
         if (!p.any || !at.m) continue;
         ch.stats_of(a, at, p.graph);
         each_row<T>(a, at, p.lo, p.hi, [&](int64_t row, const Raw<T> &v) { apply<T>(a, v, ch, y + row * a.C + at.c, at.m); });
@@ -542,13 +573,17 @@ template <typename T, bool ONE> __device__ __forceinline__ void chunk_gradients(
     constexpr int N = kPer16<T>, A = ONE ? 1 : N;
     if ((int)blockIdx.y >= a.many.slices) return;
     const Place<false> at(a, a.many, N);
+    const ChunkParts parts(a, j);
+    const bool met = parts.part[0].any || parts.part[1].any;
+    if (threadIdx.x == 0 && blockIdx.y == 0) a.met[j] = met;
+    if (!met) return;
     Channel<N> ch;
     ch.params(a, at);
     float cs[N], cq[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) cs[i] = cq[i] = 0.0f;
     for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
+        const ChunkPart p = parts.at(slot);
         if (!p.any) continue;
         float s[A], q[A];
 #pragma unroll
@@ -569,7 +604,7 @@ template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_ba
 
 // As the forward kernel; rows are read twice, the second time from L2: keeping them took 181 registers, two wavefronts a SIMD, and
 // 176 us for 119 (20,000 graphs of 24 rows of 64).
-template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMost) norm_backward_kernel(NormArgs a)
+template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(WAVE ? 256 : kMost) norm_backward_kernel(NormArgs a)
 {
     constexpr int N = kPer16<T>, A = ONE ? 1 : N;
     extern __shared__ float room[];
@@ -613,13 +648,15 @@ template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(kMo
 template <typename T> __global__ void __launch_bounds__(kMost) norm_dx_kernel(NormArgs a)
 {
     constexpr int N = kPer16<T>;
+    const int64_t j = gridDim.x - 1 - blockIdx.x;
+    if (!a.met[j]) return;
     const Place<false> at(a, a.many, N);
     Channel<N> ch;
     ch.params(a, at);
-    const int64_t j = gridDim.x - 1 - blockIdx.x;
     T *dx = static_cast<T *>(a.dx);
+    const ChunkParts parts(a, j);
     for (int slot = 0; slot < kSlots; ++slot) {
-        const ChunkPart p(a, j, slot);
+        const ChunkPart p = parts.at(slot);
         if (!p.any || !at.m) continue;
         float s1[N], s2[N];
         ch.stats_of(a, at, p.graph);
@@ -630,13 +667,13 @@ template <typename T> __global__ void __launch_bounds__(kMost) norm_dx_kernel(No
     }
 }
 
-// dweight and dbias: column sums of [workgroups][2][C], 32 columns to a workgroup; behind those the sums of long graphs' groups
-constexpr int kSumRows = 32;
-__global__ void __launch_bounds__(1024) norm_finish_kernel(NormArgs a, int columns)
+static_assert(2 * 128 == 32 * kGroupsOf, "one workgroup for both");
+// dweight and dbias: column sums of [workgroups][2][C], kSumCols columns to a workgroup; behind those the sums of long graphs' groups
+constexpr int kSumCols = 2, kSumRows = 128;
+__global__ void __launch_bounds__(kSumCols * kSumRows) norm_finish_kernel(NormArgs a, int columns)
 {
-    __shared__ float part[kSumRows][33];
+    __shared__ float part[kSumRows][kSumCols + 1];
     if ((int)blockIdx.x >= columns) {
-        if (threadIdx.x >= 32 * kGroupsOf) return;
         const int parts = (a.groups + kGroupsOf - 1) / kGroupsOf, k = blockIdx.x - columns;
         add_chunks<float>(a, k / parts, (int64_t)(k % parts) * kGroupsOf + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, float s, float q) {
             const float over = 1.0f / ((float)rows * (float)a.cpg);
@@ -644,17 +681,22 @@ __global__ void __launch_bounds__(1024) norm_finish_kernel(NormArgs a, int colum
         });
         return;
     }
-    const int lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-    const int64_t k = (int64_t)blockIdx.x * 32 + lane, n = (int64_t)a.shorts + a.chunks; // column of 2 C
+    const int lane = threadIdx.x % kSumCols, r = threadIdx.x / kSumCols;
+    const int64_t k = (int64_t)blockIdx.x * kSumCols + lane; // column of 2 C
     float v = 0.0f;
     if (k < 2 * a.C) {
 #pragma unroll 8
-        for (int64_t i = r; i < n; i += kSumRows) v += a.sums[i * 2 * a.C + k];
+        for (int64_t i = r; i < a.shorts; i += kSumRows) v += a.sums[i * 2 * a.C + k];
+#pragma unroll 8
+        for (int64_t i = r; i < a.chunks; i += kSumRows) v += a.met[i] ? a.sums[(a.shorts + i) * 2 * a.C + k] : 0.0f;
     }
     part[r][lane] = v;
     __syncthreads();
+    for (int half = kSumRows / 2; half; half /= 2) {
+        if (r < half) part[r][lane] = v = v + part[r + half][lane];
+        __syncthreads();
+    }
     if (r == 0 && k < 2 * a.C) {
-        for (int o = 1; o < kSumRows; ++o) v += part[o][lane];
         void *to = k < a.C ? a.db : a.dw;
         if (to) put_param(to, a.ptype, k < a.C ? k : k - a.C, v);
     }
@@ -704,7 +746,7 @@ NormPlan norm_plan(const pcsr_norm_t &a, int n, bool backward)
     const bool known = !a.offsets || a.graphs == 1; // every graph has `mean` rows
     const bool any_short = !known || mean <= q.longer, any_long = known ? mean > q.longer : a.rows > q.longer;
     const int teams = q.few.threads / q.few.team;
-    const int64_t groups = (a.graphs + teams - 1) / teams, cap = backward ? 4096 : groups;
+    const int64_t groups = (a.graphs + teams - 1) / teams, cap = backward ? 1024 : groups; // backward: as many as run at once
     q.shorts = any_short ? (int)(groups < cap ? groups : cap) : 0;
     q.chunks = any_long ? (int)((a.rows + q.chunk - 1) / q.chunk) : 0;
     return q;
@@ -742,14 +784,15 @@ NormArgs norm_args(const pcsr_norm_t &a, const NormPlan &q, void *ws)
 }
 
 struct NormSpace { // of the workspace
-    int64_t part, means, sums, bytes;
+    int64_t part, means, sums, met, bytes;
     NormSpace(const pcsr_norm_t &a, const NormPlan &q, bool backward)
     {
         auto up = [](int64_t b) { return (b + 15) / 16 * 16; };
         part = 0;
         means = up((int64_t)q.chunks * kSlots * a.groups * 2 * (backward ? 4 : 8));
         sums = means + (backward && q.chunks ? up(a.graphs * a.groups * 8) : 0);
-        bytes = sums + (backward ? ((int64_t)q.shorts + q.chunks) * 2 * a.channels * 4 : 0);
+        met = sums + (backward ? ((int64_t)q.shorts + q.chunks) * 2 * a.channels * 4 : 0);
+        bytes = met + (int64_t)q.chunks * 4;
     }
 };
 
@@ -791,6 +834,7 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
         if (!y || (q.chunks && !ws)) return (int)PCSR_E_INVALID_ARG;
         NormArgs p = norm_args(*a, q, ws);
         p.y = y;
+        p.met = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + NormSpace(*a, q, false).met);
         return for_plan(q, [&](auto one, auto wave) {
             constexpr bool ONE = decltype(one)::value, WAVE = decltype(wave)::value;
             const auto lds_of = [&](const Shape &sh, int teams, bool stat) {
@@ -826,7 +870,7 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
     if (a->rows && (!dy || dy_stride < a->channels)) return PCSR_E_INVALID_ARG;
     if (dy_stride > (int64_t(1) << 31)) return PCSR_E_TOO_LARGE;
     if (!dx && !sums) return PCSR_OK;
-    const int columns = sums ? (int)((2 * a->channels + 31) / 32) : 0;
+    const int columns = sums ? (int)((2 * a->channels + kSumCols - 1) / kSumCols) : 0;
     return for_type(a->type, [&](auto t) {
         typedef decltype(t) T;
         NormPlan q = {};
@@ -838,6 +882,7 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
         p.dy = dy, p.dys = dy_stride, p.dx = dx, p.dw = dweight, p.db = dbias;
         p.sums = sums ? reinterpret_cast<float *>(at + w.sums) : nullptr;
         p.means = reinterpret_cast<float *>(at + w.means);
+        p.met = reinterpret_cast<int32_t *>(at + w.met);
         return for_plan(q, [&](auto one, auto wave) {
             constexpr bool ONE = decltype(one)::value, WAVE = decltype(wave)::value;
             const auto lds_of = [&](const Shape &sh, size_t teams, bool stat) {
@@ -856,7 +901,7 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
                 hipLaunchKernelGGL((norm_backward_chunk_kernel<T, ONE>), grid, block, lds, s, p);
             }
             const int more = dx && q.chunks ? (p.offsets ? q.chunks : (int)p.graphs) * ((p.groups + kGroupsOf - 1) / kGroupsOf) : 0;
-            if (columns + more) hipLaunchKernelGGL(norm_finish_kernel, dim3(columns + more), dim3(1024), 0, s, p, columns);
+            if (columns + more) hipLaunchKernelGGL(norm_finish_kernel, dim3(columns + more), dim3(kSumCols * kSumRows), 0, s, p, columns);
             if (dx && q.chunks) hipLaunchKernelGGL((norm_dx_kernel<T>), dim3(q.chunks, q.many.slices), dim3(q.many.threads), 0, s, p);
             return launched();
         });
