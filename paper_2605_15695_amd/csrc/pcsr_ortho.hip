@@ -97,14 +97,14 @@ template <int S> struct SmallPlanes {
 };
 
 // sums over k of p[i][k] q[j][k]
-template <int Q, int S>
+template <int Q, int S, bool SYMMETRIC>
 __device__ __forceinline__ void small_product(const SmallPlanes<S> &p, const SmallPlanes<S> &q, int K, int wr, int wc, int lane,
                                               int rows, int cols, Tiles<Q> &out)
 {
     Tiles<Q> low;
     out.zero();
     low.zero();
-    if (wr * Q * 16 >= rows || wc * Q * 16 >= cols) return;
+    if (wr * Q * 16 >= rows || wc * Q * 16 >= cols || (SYMMETRIC && wc > wr)) return;
     const int i = lane & 15, k0 = (lane >> 4) * 8;
     for (int k = 0; k < K; k += 32) {
         h8 a[Q][kP], b[Q][kP];
@@ -137,6 +137,24 @@ template <int P> __device__ __forceinline__ void pieces(float x, half_t (&h)[P])
     if (P == 2) h[1 % P] = (half_t)(x - (float)h[0]);
 }
 
+// A lane holds four rows of its column; four lanes side by side exchange them, and each ends up with four columns of a row of its own (its
+// number in the four): 8 bytes of a row in one store.
+__device__ __forceinline__ h4 quad_turn(const h4 &v, int lane)
+{
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    const u2 d = __builtin_bit_cast(u2, v);
+    const bool odd = lane & 1, high = lane & 2;
+    const unsigned keep = high ? d[1] : d[0], send = high ? d[0] : d[1];
+    const unsigned got = __builtin_amdgcn_mov_dpp((int)send, 0x4e, 0xf, 0xf, true); // from the lane two further
+    const unsigned even_rows = (keep & 0xffffu) | got << 16, odd_rows = keep >> 16 | (got & 0xffff0000u); // columns j and j ^ 2
+    const unsigned own = odd ? odd_rows : even_rows, other = odd ? even_rows : odd_rows;
+    const unsigned next = __builtin_amdgcn_mov_dpp((int)other, 0xb1, 0xf, 0xf, true); // columns j ^ 1 and j ^ 3, from the lane beside
+    const unsigned x = odd ? next : own, y = odd ? own : next; // columns 0 and 1 of their pairs
+    const unsigned lo = (x & 0xffffu) | y << 16, hi = x >> 16 | (y & 0xffff0000u);
+    const u2 out = {high ? hi : lo, high ? lo : hi};
+    return __builtin_bit_cast(h4, out);
+}
+
 // tiles into planes, as they are and transposed (where TURN)
 template <int Q, int S, bool ROWS, bool TURN>
 __device__ __forceinline__ void small_put(const Tiles<Q> &v, float scale, int wr, int wc, int lane, SmallPlanes<S> *rows, SmallPlanes<S> *turned)
@@ -146,15 +164,18 @@ __device__ __forceinline__ void small_put(const Tiles<Q> &v, float scale, int wr
 #pragma unroll
         for (int c = 0; c < Q; ++c) {
             const int i = (wr * Q + r) * 16 + (lane >> 4) * 4, j = (wc * Q + c) * 16 + (lane & 15);
-            half_t h[4][kP];
+            h4 h[kP];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pieces<kP>(v.v[r][c][e] * scale, h[e]);
+            for (int e = 0; e < 4; ++e) {
+                half_t t[kP];
+                pieces<kP>(v.v[r][c][e] * scale, t);
+#pragma unroll
+                for (int o = 0; o < kP; ++o) h[o][e] = t[o];
+            }
 #pragma unroll
             for (int o = 0; o < kP; ++o) {
-                if (ROWS)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) rows->p[o][i + e][j] = h[e][o];
-                if (TURN) *reinterpret_cast<h4 *>(&turned->p[o][j][i]) = h4{h[0][o], h[1][o], h[2][o], h[3][o]};
+                if (ROWS) *reinterpret_cast<h4 *>(&rows->p[o][i + (lane & 3)][j & ~3]) = quad_turn(h[o], lane);
+                if (TURN) *reinterpret_cast<h4 *>(&turned->p[o][j][i]) = h[o];
             }
         }
 }
@@ -203,28 +224,33 @@ template <typename T, int Q> __global__ void __launch_bounds__(1024) small_kerne
         for (int c = 0; c < Q; ++c)
 #pragma unroll
             for (int e = 0; e < 4; ++e) X.v[r][c][e] = (float)((double)X.v[r][c][e] * over);
+    // of a symmetric product wavefronts on and below the diagonal have their tiles, and put them at both places
+    const auto put_symmetric = [&](const Tiles<Q> &v, float scale) {
+        if (wr == wc) small_put<Q, S, false, true>(v, scale, wr, wc, lane, nullptr, &first);
+        if (wr > wc) small_put<Q, S, true, true>(v, scale, wr, wc, lane, &first, &first);
+    };
     for (int s = 0; s < a.steps; ++s) {
         const Step &st = a.step[s];
         small_put<Q, S, true, true>(X, st.x, wr, wc, lane, &first, &turned);
         __syncthreads();
-        small_product<Q, S>(first, first, n, wr, wc, lane, m, m, A);
+        small_product<Q, S, true>(first, first, n, wr, wc, lane, m, m, A);
 #pragma unroll
         for (int r = 0; r < Q; ++r)
 #pragma unroll
             for (int c = 0; c < Q; ++c) A.v[r][c] *= st.over_xx;
         __syncthreads();
-        small_put<Q, S, false, true>(A, st.A, wr, wc, lane, nullptr, &first); // symmetric
+        put_symmetric(A, st.A);
         __syncthreads();
         Tiles<Q> B;
-        small_product<Q, S>(first, first, m, wr, wc, lane, m, m, B);
+        small_product<Q, S, true>(first, first, m, wr, wc, lane, m, m, B);
 #pragma unroll
         for (int r = 0; r < Q; ++r)
 #pragma unroll
             for (int c = 0; c < Q; ++c) B.v[r][c] = st.b * A.v[r][c] + st.c * st.over_AA * B.v[r][c];
         __syncthreads();
-        small_put<Q, S, false, true>(B, st.B, wr, wc, lane, nullptr, &first);
+        put_symmetric(B, st.B);
         __syncthreads();
-        small_product<Q, S>(first, turned, m, wr, wc, lane, m, n, A);
+        small_product<Q, S, false>(first, turned, m, wr, wc, lane, m, n, A);
 #pragma unroll
         for (int r = 0; r < Q; ++r)
 #pragma unroll
@@ -605,9 +631,7 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
 #pragma unroll
                     for (int o = 0; o < P; ++o) {
                         *reinterpret_cast<h4 *>(out + o * sp.Mp * sp.Mp + plane_at(sp.Mp, jj, ii)) = h[o];
-                        if (ti != tj)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) out[o * sp.Mp * sp.Mp + plane_at(sp.Mp, ii + k, jj)] = h[o][k];
+                        if (ti != tj) *reinterpret_cast<h4 *>(out + o * sp.Mp * sp.Mp + plane_at(sp.Mp, ii + (lane & 3), jj & ~3)) = quad_turn(h[o], lane);
                     }
                 } else {
                     f4 &xf = reinterpret_cast<f4 *>(base + sp.xf)[own_place<C>((int64_t)tj * a.tiles_i + ti, wave, r, c, e, lane)];
@@ -628,13 +652,13 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
                             half_t s[P];
                             pieces<P>(v[k] * st.next, s);
 #pragma unroll
-                            for (int o = 0; o < P; ++o) {
-                                x[o * sp.Mp * sp.Np + plane_at(sp.Mp, ii + k, jj)] = s[o];
-                                h[o][k] = s[o];
-                            }
+                            for (int o = 0; o < P; ++o) h[o][k] = s[o];
                         }
 #pragma unroll
-                        for (int o = 0; o < P; ++o) *reinterpret_cast<h4 *>(t + o * sp.Mp * sp.Np + plane_at(sp.Np, jj, ii)) = h[o];
+                        for (int o = 0; o < P; ++o) {
+                            *reinterpret_cast<h4 *>(x + o * sp.Mp * sp.Np + plane_at(sp.Mp, ii + (lane & 3), jj & ~3)) = quad_turn(h[o], lane);
+                            *reinterpret_cast<h4 *>(t + o * sp.Mp * sp.Np + plane_at(sp.Np, jj, ii)) = h[o];
+                        }
                     }
                 }
             }
@@ -724,11 +748,10 @@ int tile_of(Which w) { return w == LARGE1 ? 256 : w == MIDDLE1 || w == LARGE2 ? 
 int64_t group_of(const pcsr_matrix_t *m, int64_t count, int64_t first, const char *done, int64_t *members)
 {
     int64_t n = 0;
-    const bool small = is_small(m[first]);
-    const auto wide = [](const pcsr_matrix_t &x) { return x.rows > 64 || x.cols > 64; };
+    const bool small = is_small(m[first]); // all small ones together: a compute unit each, side by side
     for (int64_t k = first; k < count && n < kItems; ++k) {
         if (done && done[k]) continue;
-        if (small ? is_small(m[k]) && wide(m[k]) == wide(m[first]) : m[k].rows == m[first].rows && m[k].cols == m[first].cols) members[n++] = k;
+        if (small ? is_small(m[k]) : m[k].rows == m[first].rows && m[k].cols == m[first].cols) members[n++] = k;
     }
     return n;
 }
@@ -809,7 +832,9 @@ int64_t pcsr_ortho_workspace(const pcsr_matrix_t *m, int64_t count, const pcsr_o
 {
     if (ortho_check(m, count, how) != PCSR_OK) return 0;
     int64_t most = 0, members[kItems];
-    for (int64_t k = 0; k < count; ++k) { // a group that starts at any of them is no larger than all that are like it
+    for (int64_t k = 0; k < count; ++k) {
+        if (m[k].rows == 0 || m[k].cols == 0) continue;
+        // a group that starts at any of them is no larger than all that are like it
         const int64_t n = group_of(m, count, k, nullptr, members);
         for (int64_t c = 1; c <= n; ++c) { // fewer matrices can mean smaller tiles, but never more memory than counted here
             const int64_t b = group_bytes(m[k], c, how->type);
@@ -830,6 +855,7 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
     a.q.update = how->update, a.q.nesterov = how->nesterov, a.q.momentum = how->momentum, a.q.keep = how->keep;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int64_t members[kItems];
+    bool any = false;
     // matrices are taken in the order they come, each with those behind it that are like it; `from` marks what is done
     constexpr int64_t kMost = 4096;
     if (count > kMost) return PCSR_E_TOO_LARGE;
@@ -839,15 +865,17 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
         if (m[k].rows == 0 || m[k].cols == 0) continue;
         const int64_t n = group_of(m, count, k, done, members);
         int used = 0;
+        bool wide = false;
         for (int64_t i = 0; i < n; ++i) {
             const pcsr_matrix_t &x = m[members[i]];
             done[members[i]] = 1;
             if (x.rows == 0 || x.cols == 0) continue;
+            wide = wide || x.rows > 64 || x.cols > 64;
             a.q.item[used++] = {x.grad, x.buf, x.out, (int)x.rows, (int)x.cols, x.grad_ld, x.buf_ld, x.out_ld, x.rate, x.rows > x.cols};
         }
         const int r = for_type(how->type, [&](auto t) {
             typedef decltype(t) T;
-            if (is_small(m[k])) return m[k].rows > 64 || m[k].cols > 64 ? run_small<T, 2>(a, used, s) : run_small<T, 1>(a, used, s);
+            if (is_small(m[k])) return wide ? run_small<T, 2>(a, used, s) : run_small<T, 1>(a, used, s);
             const int64_t lo = m[k].rows < m[k].cols ? m[k].rows : m[k].cols, hi = m[k].rows < m[k].cols ? m[k].cols : m[k].rows;
             char *at = static_cast<char *>(ws);
             const auto run = [&](auto tiling) { return run_large<T, decltype(tiling)>(a.q, used, a.step, a.steps, at, s); };
@@ -867,8 +895,9 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
             return (int)PCSR_E_UNSUPPORTED; // (one piece is for bf16 alone)
         });
         if (r != PCSR_OK) return r;
+        any = true;
     }
-    return launched();
+    return any ? launched() : PCSR_OK;
 }
 
 } // extern "C"
