@@ -4,7 +4,8 @@ dB = A^T * dC, both through pcsr_spmm, plus minimal GCN / GIN layers built on it
 
 torch supplies tensors, streams, the loss and the optimiser; every sparse product runs in the
 library's kernels, and so do the dense products of layers up to MAX_WIDTH features wide with
-what surrounds them (bias, ReLU, its backward, the gradient sums): see FusedLayers.
+what surrounds them (bias, ReLU, its backward, the gradient sums): see FusedLayers.  embedding.py, norm.py
+and muon.py have what a training step needs around the layers.
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ import torch
 from torch.nn.modules import module as _all_modules
 
 from . import binding as pc
+from .norm import GroupNorm
 
 
 class PcsrOperator:
@@ -453,10 +455,17 @@ class GINLayer(torch.nn.Module):
 
 class LayerChain(torch.nn.Sequential):
     """Graph layers with ReLU between them, run as one chain where FusedLayers applies and module
-    by module otherwise (other operators, data types or devices, hooks, wide layers)."""
+    by module otherwise (other operators, data types or devices, hooks, wide layers, norms between
+    the layers).  offsets: of the graphs in a batch, for the norms."""
 
-    def forward(self, X):
+    def forward(self, X, offsets=None):
         mods = list(self)
+        if any(isinstance(m, GroupNorm) for m in mods):
+            for m in mods:
+                X = m(X, offsets) if isinstance(m, GroupNorm) else m(X)
+            return X
+        if offsets is not None:
+            raise ValueError("offsets are for norms, and there are none between these layers")
         chain = []
         for i, m in enumerate(mods):
             if type(m) is torch.nn.ReLU and chain and not chain[-1][1] and i + 1 < len(mods):
@@ -470,14 +479,16 @@ class LayerChain(torch.nn.Sequential):
         return out if out is not None else super().forward(X)
 
 
-def make_model(kind: str, op: PcsrOperator, d_in: int, hidden: int, d_out: int, n_layers: int = 5):
+def make_model(kind: str, op: PcsrOperator, d_in: int, hidden: int, d_out: int, n_layers: int = 5,
+               norm_groups: int = 0):
     """n_layers graph layers with ReLU between them (the paper trains 5-layer GCN / GIN
-    models with hidden sizes 32, 64, 128 and 16 input / output features)."""
+    models with hidden sizes 32, 64, 128 and 16 input / output features).  norm_groups: a group norm of
+    so many groups in front of each ReLU, over the nodes of a graph."""
     dims = [d_in] + [hidden] * (n_layers - 1) + [d_out]
     layer = {"gcn": GCNLayer, "gin": GINLayer}[kind]
     mods = []
     for i in range(n_layers):
         mods.append(layer(op, dims[i], dims[i + 1]))
         if i + 1 < n_layers:
-            mods.append(torch.nn.ReLU())
+            mods.append(GroupNorm(norm_groups, hidden, activation="relu") if norm_groups else torch.nn.ReLU())
     return LayerChain(*mods)

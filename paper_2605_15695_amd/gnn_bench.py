@@ -5,6 +5,12 @@ size 32 / 64 / 128.  Synthetic graphs and random features stand in for the OGB g
 
     python -m paper_2605_15695_amd.gnn_bench --workload road --model gcn --hidden 64
 
+--embed, --norm and --optimizer muon put the parts around the layers into the step: a learned table of node
+features looked up by id (every node once, in random order), a group norm in front of each ReLU, the
+orthogonalised update of the layers' weight matrices (Adam keeps the rest); without torch.sparse beside it.
+
+    python -m paper_2605_15695_amd.gnn_bench --workload road --model gin --embed --norm 8 --optimizer muon
+
 --dense times the layers' dense kernels on their own, the calls of a backward or a GIN layer both
 in one pass and one after the other, beside the torch operations they stand for.
 
@@ -93,13 +99,18 @@ def main(argv=None) -> int:
     ap.add_argument("--steps", type=int, default=20)
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--no-torch-sparse", action="store_true")
+    ap.add_argument("--embed", action="store_true")
+    ap.add_argument("--norm", type=int, default=0, metavar="GROUPS")
+    ap.add_argument("--optimizer", default="adam", choices=["adam", "muon"])
     ap.add_argument("--dense", type=int, default=0, metavar="ROWS")
     args = ap.parse_args(argv)
 
     import torch
 
     import synth
+    from .embedding import NodeEmbedding
     from .gnn import PcsrOperator, make_model
+    from .muon import Muon
 
     if not torch.cuda.is_available():
         print("gnn_bench: no GPU visible", file=sys.stderr)
@@ -115,14 +126,20 @@ def main(argv=None) -> int:
 
     def run(op, label):
         torch.manual_seed(0)
-        model = make_model(args.model, op, 16, args.hidden, 16, args.layers).cuda()
-        opt = torch.optim.Adam(model.parameters(), lr=1e-3)
+        model = make_model(args.model, op, 16, args.hidden, 16, args.layers, args.norm).cuda()
+        table = NodeEmbedding(g.n_cols, 16, scale=4.0, device="cuda") if args.embed else None
+        ids = torch.randperm(g.n_cols, device="cuda") if args.embed else None
+        matrices = [p for p in model.parameters() if p.dim() == 2] if args.optimizer == "muon" else []
+        rest = [p for p in model.parameters() if not any(p is m for m in matrices)] + list(table.parameters() if args.embed else [])
+        opts = [torch.optim.Adam(rest, lr=1e-3)] + ([Muon(matrices)] if matrices else [])
 
         def step():
-            opt.zero_grad(set_to_none=True)
-            loss = torch.nn.functional.mse_loss(model(X), Y)
+            for opt in opts:
+                opt.zero_grad(set_to_none=True)
+            loss = torch.nn.functional.mse_loss(model(X if table is None else table(ids)), Y)
             loss.backward()
-            opt.step()
+            for opt in opts:
+                opt.step()
             return loss
 
         for _ in range(args.warmup):
@@ -135,13 +152,13 @@ def main(argv=None) -> int:
             torch.cuda.synchronize()
             ts.append((time.perf_counter() - t0) * 1e3)
         return {"impl": label, "ms_per_step_median": statistics.median(ts), "ms_per_step_min": min(ts),
-                "final_loss": float(loss)}
+                "final_loss": float(loss.detach())}
 
     t0 = time.time()
     op = PcsrOperator(g.n_rows, g.n_cols, g.rowptr, g.colidx, g.vals, symmetric=symmetric, K_hint=args.hidden)
     build_s = time.time() - t0
     res = [run(op, "pcsr")]
-    if not args.no_torch_sparse:
+    if not (args.no_torch_sparse or args.embed or args.norm or args.optimizer != "adam"):
         A = torch.sparse_csr_tensor(torch.from_numpy(g.rowptr).cuda(), torch.from_numpy(g.colidx).cuda(),
                                     torch.from_numpy(g.vals).cuda(), size=(g.n_rows, g.n_cols))
 
@@ -154,7 +171,8 @@ def main(argv=None) -> int:
         except Exception as e:  # noqa: BLE001
             res.append({"impl": "torch.sparse", "error": repr(e)[:200]})
     out = {"workload": f"{args.workload}-{args.size}", "n": g.n_rows, "nnz": g.nnz, "model": args.model,
-           "layers": args.layers, "hidden": args.hidden, "operator_build_s": build_s, "results": res}
+           "layers": args.layers, "hidden": args.hidden, "embed": args.embed, "norm_groups": args.norm,
+           "optimizer": args.optimizer, "operator_build_s": build_s, "results": res}
     if len(res) == 2 and "ms_per_step_median" in res[1]:
         out["speedup_vs_torch_sparse"] = res[1]["ms_per_step_median"] / res[0]["ms_per_step_median"]
     print(json.dumps(out))
