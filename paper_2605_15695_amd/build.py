@@ -76,7 +76,7 @@ def build(verbose: bool = False) -> pathlib.Path:
     return LIB
 
 
-def resources(sources=("pcsr_kernels.hip", "pcsr_gnn.hip")) -> str:
+def resources(sources=("pcsr_kernels.hip", "pcsr_gnn.hip", "pcsr_embed.hip", "pcsr_norm.hip", "pcsr_ortho.hip")) -> str:
     """Registers, scratch, LDS and occupancy of every kernel in `sources` as the compiler
     reports them (-Rpass-analysis=kernel-resource-usage), as a markdown table."""
     import re

@@ -46,7 +46,8 @@ template <typename I> __device__ __forceinline__ int64_t id_at(const void *ids, 
     return (int64_t) reinterpret_cast<const I *>(ids)[i];
 }
 
-// L lanes to a row, 16 bytes each; kAhead rows at a time
+// L lanes to a row, 16 bytes each; kAhead rows at a time (8: 19.7 us for 17.0).  32,768 rows of 768 in bf16: 17 us, 5.9 TB/s.  300,000 rows
+// of 64 in fp32: 40 us, 3.9 TB/s, bound by rows of 256 bytes at random places of 268 MB (16 us out of a table of 1000 rows).
 template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) lookup_kernel(EmbedArgs p)
 {
     constexpr int N = kPer16<T>, G = kT / L;
@@ -114,7 +115,7 @@ __device__ __forceinline__ void fill(const Fill &f, int64_t block, int64_t block
 
 // The place of an id among n sorted ones is the number of smaller ones and of equal ones before it.  64 ids to a
 // workgroup, a sixteenth of the keys to each of its wavefronts, read from LDS four at a time.  Bound by the comparisons, 2.7e8 for 16,384 ids
-// in one launch, where the passes below would be six.
+// in one launch, where the passes below would be six: 33 us with 100 MB of zeros beside it, which alone take 16.
 template <typename I>
 __global__ void __launch_bounds__(kRankT) rank_kernel(int64_t n_ids, int64_t rows, const void *ids, uint32_t *key, uint32_t *pos,
                                                       int sorters, Fill f)
@@ -181,6 +182,8 @@ template <typename I, bool FIRST> __device__ __forceinline__ uint32_t sort_key(c
     return FIRST ? key_of<I>(p.ids, t, p.rows) : p.kin[t];
 }
 
+// Sorting passes of kDigit bits: counts of a digit by tile, sums of them over the tiles, places.  300,000 ids below 2^20: two passes, 75 us
+// with 268 MB of zeros beside them, which alone take 39: what the launches wait for (counts, then their sums) is not hidden.
 template <typename I, bool FIRST> __global__ void __launch_bounds__(kT) count_kernel(SortArgs p, Fill f)
 {
     __shared__ int32_t cnt[1 << kDigit];
@@ -343,6 +346,8 @@ template <typename T, int N> __device__ __forceinline__ void put(const GradArgs 
     store_upto<T, N>(static_cast<T *>(p.grad) + (int64_t)row * p.d + c, m, sum);
 }
 
+// A group of lanes to a tile.  300,000 gradients of 64 in fp32: 42 us (77 MB read at random, 3 MB of sums at most to the workspace);
+// 16,384 of 1000 in fp16: 14 us, 2.8 TB/s.
 template <typename T, int L> __global__ void __launch_bounds__(kT) runs_kernel(GradArgs p)
 {
     constexpr int N = kPer16<T>, G = kT / L;
@@ -397,7 +402,8 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) runs_kernel(G
 }
 
 // The run that goes on behind a tile and did not begin before it: its pieces, in order.  Runs of more than kJoinAlone
-// tiles are left to the whole workgroup, whose groups take a stretch of them each.
+// tiles are left to the whole workgroup, whose groups take a stretch of them each.  11 us after the 42 above, 8 after the 14: a chain of
+// round trips (key, its run's end, pieces).
 constexpr int kJoinAlone = 32;
 template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(GradArgs p)
 {
@@ -476,7 +482,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(G
 // With up to kOwnMost ids no order is made of them: a workgroup owns a stretch of rows, looks through all ids for those of its
 // rows (each wavefront through a quarter, in order, into a list in LDS), and a group of lanes adds up a row or writes its zeros.  One launch, bound
 // by its round trips and the zeros.  The whole workgroup takes a row, a stretch of its ids to each group, where the table has few, and
-// where it has more than kOwnAlone ids; the parts of a sum are added in order.
+// where it has more than kOwnAlone ids; the parts of a sum are added in order.  777 ids of 75 numbers in a table of 1500: 6.5 us.
 constexpr int kOwnMost = 4096, kOwnAlone = 48;
 struct OwnArgs {
     int64_t n, rows, d, stride;
