@@ -596,8 +596,8 @@ template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_ba
     chunk_gradients<T, ONE>(a, blockIdx.x, room);
 }
 
-// As the forward kernel; rows are read twice, the second time from L2: keeping them took 163 registers, three wavefronts a SIMD for four,
-// and 137 us for 113.  20,000 graphs of 24 rows of 64 in fp32, with silu: 103 us, 3.6 TB/s; vector units are at work half of the time.
+// As the forward kernel; rows are read twice, mostly from the memory-side cache: keeping them took 163 registers, three wavefronts a SIMD for
+// four, and 137 us for 113.  20,000 graphs of 24 rows of 64 in fp32, with silu: 103 us, 573 MB (367 read and written once) at 5.6 TB/s.
 // The bound of three wavefronts is for 8 channels of several groups in a thread, which would take two with a few registers more.
 template <typename T, bool ONE, bool WAVE> __global__ void __launch_bounds__(WAVE ? 256 : kMost, 3) norm_backward_kernel(NormArgs a)
 {
