@@ -828,6 +828,7 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
         typedef decltype(t) T;
         const NormPlan q = norm_plan(*a, kPer16<T>, false);
         if (!y || (q.chunks && !ws)) return (int)PCSR_E_INVALID_ARG;
+        if (((int64_t)q.shorts + q.chunks) * q.few.threads >= int64_t(1) << 32) return (int)PCSR_E_TOO_LARGE; // threads of a launch
         NormArgs p = norm_args(*a, q, ws);
         p.y = y;
         p.met = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + NormSpace(*a, q, false).met);

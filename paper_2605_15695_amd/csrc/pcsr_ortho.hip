@@ -841,7 +841,7 @@ int64_t pcsr_ortho_workspace(const pcsr_matrix_t *m, int64_t count, const pcsr_o
     if (ortho_check(m, count, how) != PCSR_OK) return 0;
     int64_t most = 0, members[kItems];
     for (int64_t k = 0; k < count; ++k) {
-        if (m[k].rows == 0 || m[k].cols == 0) continue;
+        if (m[k].rows == 0 || m[k].cols == 0 || is_small(m[k])) continue; // they need none
         // a group that starts at any of them is no larger than all that are like it
         const int64_t n = group_of(m, count, k, nullptr, members);
         for (int64_t c = 1; c <= n; ++c) { // fewer matrices can mean smaller tiles, but never more memory than counted here

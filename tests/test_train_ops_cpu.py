@@ -60,6 +60,8 @@ def test_norm_entry_points():
             assert call(**bad) == UNSUPPORTED, bad
         assert call(x_stride=(1 << 31) + 1) == TOO_LARGE
     assert fwd(y=None) == INVALID and fwd(rows=0, y=None) == OK
+    many = dict(rows=1 << 25, graphs=1 << 25, channels=512, groups=1, x_stride=512, type=0)  # a workgroup each: more threads than a launch has
+    assert fwd(**many) == TOO_LARGE
     assert bwd(dy=None) == INVALID and bwd(stride=11) == INVALID and bwd(dx=None, dw=None, db=None) == OK
     big = _norm(rows=100_000, channels=64, groups=4, x_stride=64)
     assert lib.pcsr_norm_workspace(ctypes.byref(big), 0) > 0
