@@ -497,7 +497,7 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
     extern __shared__ uint32_t list[]; // [W][per]: position and row of ids in the stretch: position << 8 | row
     __shared__ int length[W];
     __shared__ float shared[G][L * N];
-    __shared__ int heavy[256];
+    __shared__ int heavy[256], met[256]; // rows: of many ids, of any
     const int tid = threadIdx.x, lane64 = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid % L, group = tid / L, n = (int)p.n, per = (n + W - 1) / W;
     const int64_t r0 = (int64_t)blockIdx.x * p.own, piece = (int64_t)blockIdx.y * L + lane;
@@ -524,7 +524,9 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
         }
     }
     if (lane64 == 0) length[wave] = have;
-    if (tid < 256) heavy[tid] = 0;
+    heavy[tid] = met[tid] = 0; // (256 of each, and threads)
+    __syncthreads();
+    for (int i = lane64; i < have; i += 64) met[mine[i] & 255] = 1;
     __syncthreads();
     // f(position) for the ids of a row in order, `share` of `shares` of them: every lane sees the same
     auto each = [&](int row, int share, int shares, auto f) {
@@ -580,7 +582,13 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
         if (in) store_upto<T, N>(grad + (int64_t)row * p.d, m, sum);
     };
     if (!p.whole) {
+        bool any = false; // rows left to the whole workgroup
         for (int row = group; row < rows; row += G) {
+            if (!met[row]) { // most rows of a large table: nothing but the store (48 ids in 92,826 rows of 204 in bf16: XX us for YY)
+                float zero[N] = {};
+                finish(row, zero);
+                continue;
+            }
             int count = 0;
             for (int w = 0; w < W; ++w)
                 for (int i = 0; i < length[w]; i += L) {
@@ -589,13 +597,14 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
                 }
             if (count > kOwnAlone) {
                 if (lane == 0) heavy[row] = 1;
+                any = true;
                 continue;
             }
             float sum[N];
             sum_row(row, 0, 1, sum);
             finish(row, sum);
         }
-        __syncthreads();
+        if (!__syncthreads_or(any)) return; // (looking at 256 rows one by one took longer than all the rest)
     }
     for (int row = 0; row < rows; ++row) { // the whole workgroup; the same branch for all of it
         if (!p.whole && !heavy[row]) continue;
