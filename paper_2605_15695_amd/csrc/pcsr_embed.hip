@@ -482,7 +482,8 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(G
 // With up to kOwnMost ids no order is made of them: a workgroup owns a stretch of rows, looks through all ids for those of its
 // rows (each wavefront through a quarter, in order, into a list in LDS), and a group of lanes adds up a row or writes its zeros.  One launch, bound
 // by its round trips and the zeros.  The whole workgroup takes a row, a stretch of its ids to each group, where the table has few, and
-// where it has more than kOwnAlone ids; the parts of a sum are added in order.  777 ids of 75 numbers in a table of 1500: 6.5 us.
+// where it has more than kOwnAlone ids; the parts of a sum are added in order.  777 ids of 75 numbers in a table of 1500: 6.2 us; 48 ids
+// in 92,826 rows of 204 in bf16: 11 us, 38 MB (21 in slices of 4 lanes, which left fewer of them idle).
 constexpr int kOwnMost = 4096, kOwnAlone = 48;
 struct OwnArgs {
     int64_t n, rows, d, stride;
@@ -584,7 +585,7 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
     if (!p.whole) {
         bool any = false; // rows left to the whole workgroup
         for (int row = group; row < rows; row += G) {
-            if (!met[row]) { // most rows of a large table: nothing but the store (48 ids in 92,826 rows of 204 in bf16: XX us for YY)
+            if (!met[row]) { // most rows of a large table: nothing but the store
                 float zero[N] = {};
                 finish(row, zero);
                 continue;
@@ -667,7 +668,7 @@ template <typename V> GradPlan grad_plan(int64_t n, int64_t rows, int64_t d, V p
 {
     GradPlan q;
     const int64_t vectors = (d + per16 - 1) / per16;
-    q.lanes = lanes_for(vectors, n > kOwnMost ? n : rows);
+    q.lanes = lanes_for(vectors, n > kOwnMost ? n : 0); // few ids: whole rows, since a slice of them looks through all ids again
     q.slices = (vectors + q.lanes - 1) / q.lanes;
     // enough groups to keep the memory busy, long enough tiles that few runs cross them
     q.tile = 64;
