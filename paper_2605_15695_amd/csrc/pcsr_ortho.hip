@@ -3,10 +3,11 @@
 // X <- a X + (b A + c A A) X with A = X X^T, X the update over its Frobenius norm, turned so that it is m x n with m <= n.  Every singular
 // value s of X becomes a s + b s^3 + c s^5; singular vectors stay.
 //
-// Products run on the fp16 matrix instructions, 16 times the rate of the fp32 ones, summed in fp32.  Operands of fp32 and fp16 matrices
-// and of small matrices are two fp16 numbers each, h + l = x to 2^-23 of it, and a product is h h + h l + l h (the last, l l, is below 2^-22):
-// three instructions, 5 times the fp32 rate.  Operands of bf16 matrices with sides from kOnePiece are one fp16 number: 2^-12 of rounding, an
-// eighth of what the result is rounded by in the end.  X itself is held in fp32 from step to step (a X and the sum are fp32), so that what is rounded are the
+// Products run on the fp16 matrix instructions, 16 times the rate of the fp32 ones, summed in fp32.  Operands are two fp16 numbers each,
+// h + l = x to 2^-23 of it, and a product is h h + h l + l h (the last, l l, is below 2^-22): three instructions, 5 times the fp32 rate.  So it is for
+// bf16 matrices as well: one fp16 number, 2^-12 of rounding, is an eighth of what their result is rounded by, but where a matrix has few directions the
+// roundings do not average out, and the polynomial's terms, which cancel, make them 20 times as large in a step (a matrix of equal numbers was off by
+// 0.010, the result's own rounding being 0.002).  X itself is held in fp32 from step to step (a X and the sum are fp32), so that what is rounded are the
 // operands of the products alone: directions of small singular values, which a step makes 3.4 times as large, keep their bits.
 // fp16 ends at 65504 and loses bits below 2^-14: the planes hold numbers times a power of two that the host finds from how
 // large singular values can be in that step (X0 has norm 1, then the polynomial's maximum over the range).
@@ -29,6 +30,7 @@ constexpr int kItems = 24;  // matrices of a launch
 constexpr int kSteps = PCSR_ORTHO_STEPS;
 constexpr int kSmall = 128; // widest side of a matrix that one workgroup takes whole
 constexpr int kT = 256;
+constexpr int kP = 2;       // pieces of an operand
 
 struct Item {
     const void *grad;
@@ -71,7 +73,7 @@ struct Step {
 };
 
 // ---------------------------------------------------------------------------------- small matrices
-// One workgroup of 16 wavefronts to a matrix, everything in LDS (two pieces whatever the type, which costs little here): bound by the latency
+// One workgroup of 16 wavefronts to a matrix, everything in LDS: bound by the latency
 // of fifteen dependent products, so no wavefront has more than Q x Q tiles of 16 x 16.  X's planes make room for A's and B's, X transposed stays beside them, X in fp32 is in registers.
 struct SmallArgs {
     Items q;
@@ -90,7 +92,6 @@ template <int Q> struct Tiles {
             for (int j = 0; j < Q; ++j) v[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 };
-constexpr int kP = 2; // pieces
 template <int S> struct SmallPlanes {
     static constexpr int LD = S + 8; // rows 16 bytes apart in the banks
     half_t p[kP][S][LD];
@@ -130,11 +131,11 @@ __device__ __forceinline__ void small_product(const SmallPlanes<S> &p, const Sma
         for (int c = 0; c < Q; ++c) out.v[r][c] += low.v[r][c];
 }
 
-// a number times the plane's power of two, in P pieces
-template <int P> __device__ __forceinline__ void pieces(float x, half_t (&h)[P])
+// a number times the plane's power of two, in pieces
+__device__ __forceinline__ void pieces(float x, half_t (&h)[kP])
 {
     h[0] = (half_t)x;
-    if (P == 2) h[1 % P] = (half_t)(x - (float)h[0]);
+    h[1] = (half_t)(x - (float)h[0]);
 }
 
 // A lane holds four rows of its column; four lanes side by side exchange them, and each ends up with four columns of a row of its own (its
@@ -168,7 +169,7 @@ __device__ __forceinline__ void small_put(const Tiles<Q> &v, float scale, int wr
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 half_t t[kP];
-                pieces<kP>(v.v[r][c][e] * scale, t);
+                pieces(v.v[r][c][e] * scale, t);
 #pragma unroll
                 for (int o = 0; o < kP; ++o) h[o][e] = t[o];
             }
@@ -273,17 +274,17 @@ template <typename T, int Q> __global__ void __launch_bounds__(1024) small_kerne
 }
 
 // ---------------------------------------------------------------------------------- large matrices
-// Sides padded with zeros to whole tiles.  Planes of a matrix, one after the other (P of each): X, its transpose twice (one is read while the
+// Sides padded with zeros to whole tiles.  Planes of a matrix, one after the other (kP of each): X, its transpose twice (one is read while the
 // other is written), A, B; then X and A in fp32.  A plane of R rows of K numbers lies as [K / 32][R][32]: what a product reads at a time,
 // 32 numbers of k of a tile's rows, is one stretch of whole lines from all channels of L2.
 struct Space {
     int64_t Mp, Np, x, t[2], A, B, xf, Af, bytes; // bytes of a matrix
-    Space(int64_t m, int64_t n, int tile, int P)
+    Space(int64_t m, int64_t n, int tile)
     {
         Mp = (m + tile - 1) / tile * tile, Np = (n + tile - 1) / tile * tile;
         int64_t at = 0;
         auto room = [&](int64_t b) { const int64_t o = at; at += b; return o; };
-        x = room(2 * P * Mp * Np), t[0] = room(2 * P * Mp * Np), t[1] = room(2 * P * Mp * Np), A = room(2 * P * Mp * Mp), B = room(2 * P * Mp * Mp);
+        x = room(2 * kP * Mp * Np), t[0] = room(2 * kP * Mp * Np), t[1] = room(2 * kP * Mp * Np), A = room(2 * kP * Mp * Mp), B = room(2 * kP * Mp * Mp);
         xf = room(4 * Mp * Np), Af = room(4 * Mp * Mp);
         bytes = at;
     }
@@ -341,20 +342,17 @@ struct ProductArgs {
 // and piece lie together; 16-byte chunks of a row are exchanged by bits 2 and 3 of its number, so that the 16 rows that a
 // quarter of a wavefront reads lie in different banks.
 // 32x32x16: lane l holds A[i = l % 32][k = 8 (l / 32) ..], B[k][j = l % 32] likewise; D[i = 8 (r / 4) + 4 (l / 32) + r % 4][j = l % 32].
-// Two pieces: a stage's products have a sum of their own, which is then added to the rest: the matrix instructions cut off what
+// A stage's products have a sum of their own, which is then added to the rest: the matrix instructions cut off what
 // does not reach a sum's last bit, always downwards, and over 1,000 numbers that was 1.5 times the error of fp32 products.
-template <int TI_, int TJ_, int WI_, int WJ_, int P_, int S_, int G_ = 1> struct Tiling {
-    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, P = P_, S = S_, G = G_; // G: teams of WI x WJ wavefronts, each with a stretch of k
-    static constexpr int threads = 64 * WI * WJ * G, FI = TI / 32 / WI, FJ = TJ / 32 / WJ, blocks = (TI + TJ) / 16 * P; // 16 rows, 1 KB
+template <int TI_, int TJ_, int WI_, int WJ_, int S_, int G_ = 1> struct Tiling {
+    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, S = S_, G = G_; // G: teams of WI x WJ wavefronts, each with a stretch of k
+    static constexpr int threads = 64 * WI * WJ * G, FI = TI / 32 / WI, FJ = TJ / 32 / WJ, blocks = (TI + TJ) / 16 * kP; // 16 rows, 1 KB
     static constexpr int loads = blocks / (WI * WJ), stage = blocks * 1024, lds = G * S * stage;
     static_assert(blocks % (WI * WJ) == 0 && lds <= 160 * 1024 && G <= 2, "whole loads, in LDS");
 };
-typedef Tiling<64, 64, 2, 2, 1, 4, 2> Small1;
-typedef Tiling<128, 128, 4, 2, 1, 4> Middle1;
-typedef Tiling<256, 256, 4, 2, 1, 4> Large1;
-typedef Tiling<64, 64, 2, 2, 2, 3, 2> Few2;
-typedef Tiling<64, 64, 2, 2, 2, 3> Small2;
-typedef Tiling<128, 128, 2, 4, 2, 4> Large2;
+typedef Tiling<64, 64, 2, 2, 3, 2> Few;
+typedef Tiling<64, 64, 2, 2, 3> Small;
+typedef Tiling<128, 128, 2, 4, 4> Large;
 
 template <int N> __device__ __forceinline__ void wait_loads() // until N of the wavefront's loads are on their way, for all wavefronts
 {
@@ -380,7 +378,6 @@ struct Operand {
 };
 template <typename C> __device__ __forceinline__ void product(const Operand &p, const Operand &q, int64_t Kp, char *lds, int lane, int wave, int team, Sums<C> &sum)
 {
-    constexpr int P = C::P;
     typedef __attribute__((address_space(3))) void *Lds;
     typedef __attribute__((address_space(1))) const void *Global;
     const half_t *from[C::loads];
@@ -389,9 +386,9 @@ template <typename C> __device__ __forceinline__ void product(const Operand &p, 
     for (int u = 0; u < C::loads; ++u) {
         const int block = wave + u * C::WI * C::WJ;
         constexpr int PI = C::TI / 16, PJ = C::TJ / 16;
-        const bool second = block >= P * PI;
+        const bool second = block >= kP * PI;
         const Operand &o = second ? q : p;
-        const int rest = second ? block - P * PI : block, per = second ? PJ : PI, plane = rest / per, row = (rest - plane * per) * 16 + (lane >> 2);
+        const int rest = second ? block - kP * PI : block, per = second ? PJ : PI, plane = rest / per, row = (rest - plane * per) * 16 + (lane >> 2);
         step[u] = o.R * 32;
         from[u] = o.at + plane * o.plane + row * 32 + (((lane & 3) ^ (lane >> 4)) << 3) + team * (Kp / 32 / C::G) * step[u];
     }
@@ -399,19 +396,19 @@ template <typename C> __device__ __forceinline__ void product(const Operand &p, 
         __builtin_amdgcn_global_load_lds((Global)(from[u] + s * step[u]), (Lds)(lds + s % C::S * C::stage + (wave + u * C::WI * C::WJ) * 1024), 16, 0, 0);
     };
     const int i = lane & 31, half = lane >> 5, wr = wave / C::WJ, wc = wave % C::WJ, turn = (i >> 2) & 3;
-    const int at0 = (wr * C::FI * 32 + i) * 64, at1 = (P * C::TI + wc * C::FJ * 32 + i) * 64;
+    const int at0 = (wr * C::FI * 32 + i) * 64, at1 = (kP * C::TI + wc * C::FJ * 32 + i) * 64;
     const int steps = (int)(Kp / 32 / C::G); // sides are whole tiles of 64 at least: an even number of stages
     lds += team * C::S * C::stage;
     sum.zero();
     // The operands of 16 numbers of k are read while the 16 before are multiplied.
     struct Half {
-        h8 x[C::FI][P], y[C::FJ][P];
+        h8 x[C::FI][kP], y[C::FJ][kP];
     };
     const auto read = [&](int s, int kk, Half &h) {
         const char *here = lds + s % C::S * C::stage;
         const int chunk = ((kk * 2 + half) ^ turn) * 16;
 #pragma unroll
-        for (int o = 0; o < P; ++o) {
+        for (int o = 0; o < kP; ++o) {
 #pragma unroll
             for (int f = 0; f < C::FI; ++f) h.x[f][o] = *reinterpret_cast<const h8 *>(here + at0 + (o * C::TI + f * 32) * 64 + chunk);
 #pragma unroll
@@ -423,10 +420,8 @@ template <typename C> __device__ __forceinline__ void product(const Operand &p, 
         for (int r = 0; r < C::FI; ++r) {
 #pragma unroll
             for (int c = 0; c < C::FJ; ++c) {
-                if (P == 2) {
-                    to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][1 % P], h.y[c][0], to.v[r][c], 0, 0, 0);
-                    to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][0], h.y[c][1 % P], to.v[r][c], 0, 0, 0);
-                }
+                to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][1], h.y[c][0], to.v[r][c], 0, 0, 0);
+                to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][0], h.y[c][1], to.v[r][c], 0, 0, 0);
                 to.v[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h.x[r][0], h.y[c][0], to.v[r][c], 0, 0, 0);
             }
             between(r);
@@ -434,12 +429,10 @@ template <typename C> __device__ __forceinline__ void product(const Operand &p, 
     };
     const auto nothing = [](int) {};
     const auto take_part = [&](Sums<C> &part) {
-        if (P == 2) {
 #pragma unroll
-            for (int r = 0; r < C::FI; ++r)
+        for (int r = 0; r < C::FI; ++r)
 #pragma unroll
-                for (int c = 0; c < C::FJ; ++c) sum.v[r][c] += part.v[r][c];
-        }
+            for (int c = 0; c < C::FJ; ++c) sum.v[r][c] += part.v[r][c];
     };
 #pragma unroll
     for (int s = 0; s < C::S - 1; ++s)
@@ -457,10 +450,10 @@ template <typename C> __device__ __forceinline__ void product(const Operand &p, 
     // joins are for everything.
     for (; s + C::S - 1 < steps; ++s) {
         Sums<C> part;
-        if (P == 2) part.zero();
+        part.zero();
         read(s, 1, h1);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(h0, P == 2 ? part : sum, [&](int r) {
+        multiply(h0, part, [&](int r) {
 #pragma unroll
             for (int u = r * C::loads / C::FI; u < (r + 1) * C::loads / C::FI; ++u) fetch(s + C::S - 1, u);
             __builtin_amdgcn_sched_barrier(0);
@@ -468,17 +461,17 @@ template <typename C> __device__ __forceinline__ void product(const Operand &p, 
         wait_loads<C::loads * (C::S - 2)>(); // all of stage s has been read by all wavefronts when they pass; stage s + 1 is there
         read(s + 1, 0, h0);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(h1, P == 2 ? part : sum, nothing);
+        multiply(h1, part, nothing);
         take_part(part);
     }
     for (; s < steps; ++s) { // the last stages: nothing is left to fetch
         Sums<C> part;
-        if (P == 2) part.zero();
+        part.zero();
         read(s, 1, h1);
-        multiply(h0, P == 2 ? part : sum, nothing);
+        multiply(h0, part, nothing);
         wait_loads<0>();
         if (s + 1 < steps) read(s + 1, 0, h0);
-        multiply(h1, P == 2 ? part : sum, nothing);
+        multiply(h1, part, nothing);
         take_part(part);
     }
     if (C::G == 2) { // the second team's sums
@@ -510,10 +503,9 @@ template <typename C> __device__ __forceinline__ int64_t own_place(int64_t tile,
     return ((((tile * C::WI * C::WJ + wave) * C::FI + r) * C::FJ + c) * 4 + e) * 64 + lane;
 }
 
-// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup.  4096 x 4096 in bf16: 51 us, 168 MB.
+// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup.  4096 x 4096 in bf16: 65 us, 235 MB.
 template <typename T, typename C> __global__ void __launch_bounds__(kT) pack_kernel(Items q, const double *sums, int blocks, char *ws, Space sp, float scale)
 {
-    constexpr int P = C::P;
     __shared__ float tile[32][33];
     const Item &it = q.item[blockIdx.z];
     char *base = ws + blockIdx.z * sp.bytes;
@@ -533,11 +525,11 @@ template <typename T, typename C> __global__ void __launch_bounds__(kT) pack_ker
     half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[0]);
     for (int k = ty; k < 32; k += 8) {
         const float v = it.flip ? tile[tx][k] : tile[k][tx], w = it.flip ? tile[k][tx] : tile[tx][k]; // X[i0 + k][j0 + tx], X[i0 + tx][j0 + k]
-        half_t hv[P], hw[P];
-        pieces<P>(v * scale, hv);
-        pieces<P>(w * scale, hw);
+        half_t hv[kP], hw[kP];
+        pieces(v * scale, hv);
+        pieces(w * scale, hw);
 #pragma unroll
-        for (int o = 0; o < P; ++o) {
+        for (int o = 0; o < kP; ++o) {
             x[o * sp.Mp * sp.Np + plane_at(sp.Mp, i0 + k, j0 + tx)] = hv[o];
             t[o * sp.Mp * sp.Np + plane_at(sp.Np, j0 + k, i0 + tx)] = hw[o];
         }
@@ -583,15 +575,13 @@ template <bool SYMMETRIC> __device__ __forceinline__ void place_of(int bid, int 
 }
 
 // A product and what follows it: pieces of the result as the next product reads them, by rows and by columns, fp32 where it is needed again.
-// 4096 x 4096 in bf16: A and B 103 us each (the half with i >= j: 136 tiles of 256, 0.7 PFLOP/s), X 157 us (0.88 PFLOP/s; a library product of
-// this size in fp16 alone 1.3).  A tile alone on the card takes 0.55 us a stage of 32, with all units at work 0.98, and that product of zeros
-// 437 us for 567 of random numbers: the card's power.  Some 19 us are what follows the products, 200 MB read and written for X.
+// 4096 x 4096: A and B 280 us each (the half with i >= j: 528 tiles of 128, 0.76 PFLOP/s of fp16 products), X 444 us (0.93 PFLOP/s; a library product of
+// this size in fp16 alone 1.05 to 1.3).
 // 4 of 1000 x 333 in fp32: A 11 us, B 8, X 14: a stage of two teams is 32 KB for a compute unit and takes 0.3 us, 45 bytes a cycle; the rest is the
 // launch, the first round trip and what follows. Deeper rings (4 and 5 stages) and tiles of 16 x 16 side by side, which wait less for one
 // another, changed nothing.
 template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C::threads) product_kernel(ProductArgs a, Items items)
 {
-    constexpr int P = C::P;
     extern __shared__ char memory[];
     const Space &sp = a.sp;
     char *base = a.ws + blockIdx.y * sp.bytes;
@@ -628,16 +618,16 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
                     } else {
                         v = st.b * Af + st.c * st.over_AA * v;
                     }
-                    h4 h[P];
+                    h4 h[kP];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        half_t t[P];
-                        pieces<P>(v[k] * (MODE == MAKE_A ? st.A : st.B), t);
+                        half_t t[kP];
+                        pieces(v[k] * (MODE == MAKE_A ? st.A : st.B), t);
 #pragma unroll
-                        for (int o = 0; o < P; ++o) h[o][k] = t[o];
+                        for (int o = 0; o < kP; ++o) h[o][k] = t[o];
                     }
 #pragma unroll
-                    for (int o = 0; o < P; ++o) {
+                    for (int o = 0; o < kP; ++o) {
                         *reinterpret_cast<h4 *>(out + o * sp.Mp * sp.Mp + plane_at(sp.Mp, jj, ii)) = h[o];
                         if (ti != tj) *reinterpret_cast<h4 *>(out + o * sp.Mp * sp.Mp + plane_at(sp.Mp, ii + (lane & 3), jj & ~3)) = quad_turn(h[o], lane);
                     }
@@ -653,17 +643,17 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
                         }
                     } else {
                         half_t *x = reinterpret_cast<half_t *>(base + sp.x), *t = reinterpret_cast<half_t *>(base + sp.t[1 - a.turn]);
-                        h4 h[P];
+                        h4 h[kP];
                         xf = v;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            half_t s[P];
-                            pieces<P>(v[k] * st.next, s);
+                            half_t s[kP];
+                            pieces(v[k] * st.next, s);
 #pragma unroll
-                            for (int o = 0; o < P; ++o) h[o][k] = s[o];
+                            for (int o = 0; o < kP; ++o) h[o][k] = s[o];
                         }
 #pragma unroll
-                        for (int o = 0; o < P; ++o) {
+                        for (int o = 0; o < kP; ++o) {
                             *reinterpret_cast<h4 *>(x + o * sp.Mp * sp.Np + plane_at(sp.Mp, ii + (lane & 3), jj & ~3)) = quad_turn(h[o], lane);
                             *reinterpret_cast<h4 *>(t + o * sp.Mp * sp.Np + plane_at(sp.Np, jj, ii)) = h[o];
                         }
@@ -722,35 +712,25 @@ bool plan_steps(const pcsr_ortho_t &how, Step *out)
 }
 
 bool is_small(const pcsr_matrix_t &m) { return m.rows <= kSmall && m.cols <= kSmall; }
-// One piece only where roundings of many directions average out: a single direction of a bf16 matrix was off by 1.1 times its result's own
-// rounding (129 x 5).
-constexpr int kOnePiece = 256;
-int pieces_of(int type, int64_t m) { return type == PCSR_BF16 && m >= kOnePiece ? 1 : 2; }
 
-// The tiling of a group of matrices: the largest tiles of which the symmetric products have half as many as there are compute units; tiles of 64
-// otherwise, with two teams to a tile where a product has fewer tiles than compute units (one piece: always).  Five steps, us:
-//   one piece    64 (a team / two)   128    256     two pieces   64 (a team / two)   128
-//   512 x 512        103 /   97      141    326                      153 /  135      241
-//   1024 x 1024      164 /  144      213    503                      251 /  207      387
-//   1024 x 4096      304 /  258      345    776                      554 /  562      700
-//   2048 x 2048      483 /  477      405    802                     1029 / 1087      894
-//   3000 x 3000     1190             1016   1169                    2464            2477
-//   4096 x 4096     2566 / 2562     2030   1889                     5593 / 6208     5073
-//   8 of 512         157 /  156      179    385                      238 /  277      293
-//   16 of 300        131 /  133      172    403                      179 /  200      264
-//   4 of 1000        285 /  299      271    540                      622 /  676      527
+// The tiling of a group of matrices: tiles of 128 where the symmetric products have half as many as there are compute units; tiles of 64
+// otherwise, with two teams to a tile where a product has fewer tiles than compute units.  Five steps, us:
+//                    64 (a team / two)   128
+//   512 x 512            153 /  135      241
+//   1024 x 1024          251 /  207      387
+//   1024 x 4096          554 /  562      700
+//   2048 x 2048         1029 / 1087      894
+//   3000 x 3000         2464            2477
+//   4096 x 4096         5593 / 6208     5073
+//   8 of 512             238 /  277      293
+//   16 of 300            179 /  200      264
+//   4 of 1000            622 /  676      527
 constexpr int64_t kUnits = 256; // compute units
-enum Which { SMALL1, MIDDLE1, LARGE1, SMALL2, LARGE2 };
-Which tiling_of(int64_t m, int64_t n, int64_t count, int pieces)
+bool large_tiles(int64_t m, int64_t count)
 {
-    const auto half_full = [&](int64_t t) {
-        const int64_t a = (m + t - 1) / t;
-        return a * (a + 1) / 2 * count >= kUnits / 2;
-    };
-    if (pieces == 1) return half_full(256) ? LARGE1 : half_full(128) ? MIDDLE1 : SMALL1;
-    return half_full(128) ? LARGE2 : SMALL2;
+    const int64_t a = (m + Large::TI - 1) / Large::TI;
+    return a * (a + 1) / 2 * count >= kUnits / 2;
 }
-int tile_of(Which w) { return w == LARGE1 ? 256 : w == MIDDLE1 || w == LARGE2 ? 128 : 64; }
 
 // the matrices from `first` on that go with it in one launch
 int64_t group_of(const pcsr_matrix_t *m, int64_t count, int64_t first, const char *done, int64_t *members)
@@ -764,11 +744,11 @@ int64_t group_of(const pcsr_matrix_t *m, int64_t count, int64_t first, const cha
     return n;
 }
 
-int64_t group_bytes(const pcsr_matrix_t &x, int64_t n, int type)
+int64_t group_bytes(const pcsr_matrix_t &x, int64_t n)
 {
     if (is_small(x)) return 0;
     const int64_t m = x.rows < x.cols ? x.rows : x.cols, w = x.rows < x.cols ? x.cols : x.rows;
-    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, tile_of(tiling_of(m, w, n, pieces_of(type, m))), pieces_of(type, m)).bytes;
+    return kItems * kNormBlocks * (int64_t)sizeof(double) + n * Space(m, w, large_tiles(m, n) ? Large::TI : Small::TI).bytes;
 }
 
 int ortho_check(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t *how)
@@ -804,7 +784,7 @@ template <typename T, typename C> int run_large(const Items &q, int n, const Ste
     static_assert(C::TI == C::TJ, "square tiles");
     const Item &it = q.item[0];
     const int64_t m = it.flip ? it.cols : it.rows, w = it.flip ? it.rows : it.cols;
-    const Space sp(m, w, C::TI, C::P);
+    const Space sp(m, w, C::TI);
     double *sums = reinterpret_cast<double *>(ws);
     ws += kItems * kNormBlocks * sizeof(double);
     const int64_t want = (m * w + kT * 4 - 1) / (kT * 4);
@@ -818,8 +798,8 @@ template <typename T, typename C> int run_large(const Items &q, int n, const Ste
         const auto run = [&](auto type, auto mode, unsigned tiles) {
             typedef decltype(type) U;
             constexpr int MODE = decltype(mode)::value;
-            if constexpr (std::is_same<C, Small2>::value) // the same tiles and places
-                if ((int64_t)tiles * n <= kUnits) return run_product<U, Few2, MODE>(a, q, tiles, n, s);
+            if constexpr (std::is_same<C, Small>::value) // the same tiles and places
+                if ((int64_t)tiles * n <= kUnits) return run_product<U, Few, MODE>(a, q, tiles, n, s);
             return run_product<U, C, MODE>(a, q, tiles, n, s);
         };
         ok = run(float{}, std::integral_constant<int, MAKE_A>{}, sym); // (the type matters to the last alone)
@@ -845,7 +825,7 @@ int64_t pcsr_ortho_workspace(const pcsr_matrix_t *m, int64_t count, const pcsr_o
         // a group that starts at any of them is no larger than all that are like it
         const int64_t n = group_of(m, count, k, nullptr, members);
         for (int64_t c = 1; c <= n; ++c) { // fewer matrices can mean smaller tiles, but never more memory than counted here
-            const int64_t b = group_bytes(m[k], c, how->type);
+            const int64_t b = group_bytes(m[k], c);
             most = b > most ? b : most;
         }
     }
@@ -884,23 +864,9 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
         const int r = for_type(how->type, [&](auto t) {
             typedef decltype(t) T;
             if (is_small(m[k])) return wide ? run_small<T, 2>(a, used, s) : run_small<T, 1>(a, used, s);
-            const int64_t lo = m[k].rows < m[k].cols ? m[k].rows : m[k].cols, hi = m[k].rows < m[k].cols ? m[k].cols : m[k].rows;
             char *at = static_cast<char *>(ws);
-            const auto run = [&](auto tiling) { return run_large<T, decltype(tiling)>(a.q, used, a.step, a.steps, at, s); };
-            switch (tiling_of(lo, hi, used, pieces_of(how->type, lo))) {
-            case SMALL1:
-                if constexpr (std::is_same<T, bfloat_t>::value) return run(Small1{});
-                break;
-            case MIDDLE1:
-                if constexpr (std::is_same<T, bfloat_t>::value) return run(Middle1{});
-                break;
-            case LARGE1:
-                if constexpr (std::is_same<T, bfloat_t>::value) return run(Large1{});
-                break;
-            case SMALL2: return run(Small2{});
-            case LARGE2: return run(Large2{});
-            }
-            return (int)PCSR_E_UNSUPPORTED; // (one piece is for bf16 alone)
+            const bool large = large_tiles(m[k].rows < m[k].cols ? m[k].rows : m[k].cols, used);
+            return large ? run_large<T, Large>(a.q, used, a.step, a.steps, at, s) : run_large<T, Small>(a.q, used, a.step, a.steps, at, s);
         });
         if (r != PCSR_OK) return r;
         any = true;

@@ -76,7 +76,7 @@ typedef struct {
 } pcsr_ortho_t;
 #define PCSR_ORTHO_STEPS 16
 // matrices: host, [count], which may overlap with no other's buf or out.  Products of fp16 numbers added up in fp32: operands are two fp16
-// numbers each (22 bits), of bf16 matrices with 256 rows and columns or more one (11 bits).
+// numbers each (22 bits).
 // ws: 16-byte aligned, pcsr_ortho_workspace bytes.  UNSUPPORTED where the coefficients let the numbers grow out of fp32's range.
 int64_t pcsr_ortho_workspace(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how);
 int pcsr_orthogonalize(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how, void *ws, void *stream);

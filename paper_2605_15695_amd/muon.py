@@ -70,7 +70,7 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS) ->
 
     G: (rows, columns) or (matrices, rows, columns) of float32, bfloat16 or float16 on a GPU; any strides.
     coefficients: (a, b, c), or one for each step.  The result has G's type; products are taken of 22 bits of their
-    operands (of 11 for bfloat16 matrices with 256 rows and columns or more) and summed in 32; X itself is held in 32."""
+    operands and summed in 32; X itself is held in 32."""
     fast = pc.train_module()
     if fast is not None and isinstance(steps, int):
         co = _coefficients(coefficients, steps)
