@@ -745,7 +745,7 @@ template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, con
                                    hipStream_t s)
 {
     const auto fillers = [](int64_t bytes, int threads) {
-        const int64_t want = (bytes / 16 + threads * 4 - 1) / (threads * 4), most = 2048 * kT / threads;
+        const int64_t want = ((bytes + 15) / 16 + threads * 4 - 1) / (threads * 4), most = 2048 * kT / threads; // one at least, unless there is nothing
         return (unsigned)(want < most ? want : most);
     };
     uint32_t *key = reinterpret_cast<uint32_t *>(ws + w.key), *pos = reinterpret_cast<uint32_t *>(ws + w.pos);

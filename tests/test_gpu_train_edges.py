@@ -46,3 +46,25 @@ def test_few_directions_of_large_bf16_matrices(path, shape, rank):
     out = orthogonalize(G)
     for x, o in zip(G if G.dim() == 3 else G[None], out if G.dim() == 3 else out[None]):
         _near(o, _polynomial(x), BOUND[torch.bfloat16])
+
+
+# tables of 1 to 17 bytes, more ids than one launch looks through: rows without an id are zeros
+@pytest.mark.parametrize("kind,rows,d", [("fp32", 3, 1), ("fp32", 1, 3), ("fp32", 1, 1), ("bf16", 7, 1), ("fp16", 2, 3), ("bf16", 8, 1), ("fp16", 9, 1)])
+@pytest.mark.parametrize("n", [4097, 5000, 16384, 20000, 70000])
+@pytest.mark.parametrize("wide", [False, True])
+def test_gradients_of_tables_of_a_few_bytes(kind, rows, d, n, wide):
+    from paper_2605_15695_amd import binding as pc
+
+    lib, number = pc._lib(), list(TYPES).index(kind)
+    dout = torch.ones(n, d, device="cuda", dtype=TYPES[kind])
+    ws = torch.empty(lib.pcsr_embed_workspace(n, rows, d), dtype=torch.uint8, device="cuda")
+    for which in (-1, rows, rows - 1):  # no row has an id; the last one has one
+        ids = torch.full((n,), -1, device="cuda", dtype=torch.int64 if wide else torch.int32)
+        ids[n // 2] = which
+        grad = torch.full((rows, d), float("nan"), device="cuda", dtype=TYPES[kind])
+        rc = lib.pcsr_embed_backward(n, rows, d, number, ids.data_ptr(), int(wide), dout.data_ptr(), d, 1.0, grad.data_ptr(), ws.data_ptr(),
+                                     torch.cuda.current_stream().cuda_stream)
+        want = torch.zeros(rows, d, device="cuda", dtype=TYPES[kind])
+        if 0 <= which < rows:
+            want[which] = 1.0
+        assert rc == pc.PCSR_OK and torch.equal(grad, want)
