@@ -23,7 +23,8 @@ constexpr int kMost = 512;     // threads of a workgroup at most
 constexpr int kKept = 8;       // 16-byte pieces a thread keeps of a short graph (of its rows and of their gradients, each)
 constexpr int kAhead = 4;      // pieces a thread has on their way
 constexpr int kSlots = 2;      // long graphs that meet a chunk
-constexpr int kGroupsOf = 8;   // groups that a workgroup adds up over the chunks
+constexpr int kGroupsOf = 8;   // groups that a workgroup adds up over the chunks at a time
+constexpr int kPartsMost = 8192; // workgroups to a chunk or graph for all its groups: with 1024 chunks and 2^22 channels fewer than 2^24 of 256 threads
 
 // how a kernel's threads lie over rows and channels
 struct Shape {
@@ -472,9 +473,10 @@ template <typename V, typename F> __device__ __forceinline__ void add_chunks(con
 }
 __global__ void __launch_bounds__(32 * kGroupsOf) norm_combine_kernel(NormArgs a)
 {
-    add_chunks<double>(a, blockIdx.x, (int64_t)blockIdx.y * kGroupsOf + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, double s, double q) {
-        mean_rstd(s, q, 1.0 / ((double)rows * a.cpg), a.eps, a.mean + graph * a.groups + g, a.rstd + graph * a.groups + g);
-    });
+    for (int64_t g0 = (int64_t)blockIdx.y * kGroupsOf; g0 < a.groups; g0 += (int64_t)gridDim.y * kGroupsOf)
+        add_chunks<double>(a, blockIdx.x, g0 + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, double s, double q) {
+            mean_rstd(s, q, 1.0 / ((double)rows * a.cpg), a.eps, a.mean + graph * a.groups + g, a.rstd + graph * a.groups + g);
+        });
 }
 
 template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_apply_kernel(NormArgs a)
@@ -666,15 +668,16 @@ template <typename T, bool ONE> __global__ void __launch_bounds__(kMost) norm_dx
 static_assert(2 * 128 == 32 * kGroupsOf, "one workgroup for both");
 // dweight and dbias: column sums of [workgroups][2][C], kSumCols columns to a workgroup; behind those the sums of long graphs' groups
 constexpr int kSumCols = 2, kSumRows = 128;
-__global__ void __launch_bounds__(kSumCols * kSumRows) norm_finish_kernel(NormArgs a, int columns)
+__global__ void __launch_bounds__(kSumCols * kSumRows) norm_finish_kernel(NormArgs a, int columns, int parts)
 {
     __shared__ float part[kSumRows][kSumCols + 1];
     if ((int)blockIdx.x >= columns) {
-        const int parts = (a.groups + kGroupsOf - 1) / kGroupsOf, k = blockIdx.x - columns;
-        add_chunks<float>(a, k / parts, (int64_t)(k % parts) * kGroupsOf + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, float s, float q) {
-            const float over = 1.0f / ((float)rows * (float)a.cpg);
-            a.means[(graph * a.groups + g) * 2] = s * over, a.means[(graph * a.groups + g) * 2 + 1] = q * over;
-        });
+        const int k = blockIdx.x - columns;
+        for (int64_t g0 = (int64_t)(k % parts) * kGroupsOf; g0 < a.groups; g0 += (int64_t)parts * kGroupsOf)
+            add_chunks<float>(a, k / parts, g0 + (threadIdx.x >> 5), [&](int64_t graph, int64_t rows, int64_t g, float s, float q) {
+                const float over = 1.0f / ((float)rows * (float)a.cpg);
+                a.means[(graph * a.groups + g) * 2] = s * over, a.means[(graph * a.groups + g) * 2 + 1] = q * over;
+            });
         return;
     }
     const int lane = threadIdx.x % kSumCols, r = threadIdx.x / kSumCols;
@@ -792,6 +795,12 @@ struct NormSpace { // of the workspace
     }
 };
 
+int parts_of(int groups)
+{
+    const int parts = (groups + kGroupsOf - 1) / kGroupsOf;
+    return parts < kPartsMost ? parts : kPartsMost;
+}
+
 unsigned slices(const NormPlan &q)
 {
     const int few = q.shorts ? q.few.slices : 0, many = q.chunks ? q.many.slices : 0;
@@ -848,7 +857,7 @@ int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream)
                 hipLaunchKernelGGL((norm_chunk_kernel<T, ONE>), grid, block, lds, s, p);
             }
             if (q.chunks) {
-                hipLaunchKernelGGL(norm_combine_kernel, dim3(p.offsets ? q.chunks : (unsigned)p.graphs, (p.groups + kGroupsOf - 1) / kGroupsOf),
+                hipLaunchKernelGGL(norm_combine_kernel, dim3(p.offsets ? q.chunks : (unsigned)p.graphs, parts_of(p.groups)),
                                    dim3(32 * kGroupsOf), 0, s, p);
                 hipLaunchKernelGGL((norm_apply_kernel<T, ONE>), dim3(q.chunks, q.many.slices), dim3(q.many.threads), 0, s, p);
             }
@@ -897,8 +906,8 @@ int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, 
                 if (!allow_lds(&norm_backward_chunk_kernel<T, ONE>, lds)) return (int)PCSR_E_HIP;
                 hipLaunchKernelGGL((norm_backward_chunk_kernel<T, ONE>), grid, block, lds, s, p);
             }
-            const int more = dx && q.chunks ? (p.offsets ? q.chunks : (int)p.graphs) * ((p.groups + kGroupsOf - 1) / kGroupsOf) : 0;
-            if (columns + more) hipLaunchKernelGGL(norm_finish_kernel, dim3(columns + more), dim3(kSumCols * kSumRows), 0, s, p, columns);
+            const int parts = parts_of(p.groups), more = dx && q.chunks ? (p.offsets ? q.chunks : (int)p.graphs) * parts : 0;
+            if (columns + more) hipLaunchKernelGGL(norm_finish_kernel, dim3(columns + more), dim3(kSumCols * kSumRows), 0, s, p, columns, parts);
             if (dx && q.chunks) hipLaunchKernelGGL((norm_dx_kernel<T, ONE>), dim3(q.chunks, q.many.slices), dim3(q.many.threads), 0, s, p);
             return launched();
         });

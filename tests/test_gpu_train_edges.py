@@ -68,3 +68,62 @@ def test_gradients_of_tables_of_a_few_bytes(kind, rows, d, n, wide):
         if 0 <= which < rows:
             want[which] = 1.0
         assert rc == pc.PCSR_OK and torch.equal(grad, want)
+
+
+# more groups than a launch has workgroups for in its second dimension (65,535 of 8), over long graphs
+@pytest.mark.parametrize("lengths", [[12], [13, 0, 1, 15]])
+def test_norms_of_half_a_million_groups(path, lengths):
+    from paper_2605_15695_amd.norm import group_norm
+
+    n, C = sum(lengths), 524_320
+    g = _gen(n)
+    X, dy = torch.randn(n, C, generator=g, device="cuda"), torch.randn(n, C, generator=g, device="cuda")
+    off = torch.tensor([0] + lengths, device="cuda").cumsum(0) if len(lengths) > 1 else None
+    x, w, b = X.clone().requires_grad_(), (torch.ones(C, device="cuda") * 1.5).requires_grad_(), torch.zeros(C, device="cuda").requires_grad_()
+    y = group_norm(x, C, w, b, off)
+    dx, dw, db = torch.autograd.grad(y, (x, w, b), dy)
+    dw64 = torch.zeros(C, dtype=torch.float64, device="cuda")
+    at = 0
+    for k in lengths:
+        if k == 0:
+            continue
+        v, gv = X[at:at + k].double(), dy[at:at + k].double()
+        rstd = (v.var(0, unbiased=False) + 1e-5).rsqrt()
+        xhat, d = (v - v.mean(0)) * rstd, gv * 1.5
+        # xhat is 4 at most, mean and products are rounded a dozen times; rstd is 316 at most (a graph of one row, whose numbers are 0)
+        want = rstd * (d - d.mean(0) - xhat * (d * xhat).mean(0))
+        assert float((y[at:at + k] - 1.5 * xhat).abs().max()) < 64 * U * (1 + float((v.abs().amax(0) * rstd).max()))
+        if k > 1:
+            err = (dx[at:at + k] - want).abs() / (rstd * (1 + v.abs().amax(0) * rstd) * 8)
+            assert float(err.max()) < 64 * U
+        dw64 += (gv * xhat).sum(0)
+        at += k
+    assert torch.allclose(db.double(), dy.double().sum(0), atol=64 * U * 8, rtol=0)
+    assert float(((dw.double() - dw64).abs()).max()) < 1e-2
+
+
+# as many workgroups to add up chunks of long graphs as a launch has threads for (2^24 of 256)
+def test_norms_of_many_groups_in_many_chunks(path):
+    from paper_2605_15695_amd.norm import group_norm
+
+    n, C, cut = 4096, 131_300, 3000
+    g = _gen(9)
+    X, dy = torch.randn(n, C, generator=g, device="cuda"), torch.randn(n, C, generator=g, device="cuda")
+    off = torch.tensor([0, cut, n], device="cuda")
+    x = X.requires_grad_()
+    w, b = torch.ones(C, device="cuda").requires_grad_(), torch.zeros(C, device="cuda").requires_grad_()
+    y = group_norm(x, C, w, b, off)
+    dx, dw, db = torch.autograd.grad(y, (x, w, b), dy)
+    for some in (slice(0, 40), slice(65_000, 65_040), slice(C - 40, C)):  # groups are single channels
+        dw64 = torch.zeros(40, dtype=torch.float64, device="cuda")
+        for rows in (slice(0, cut), slice(cut, n)):
+            v, d = X[rows, some].detach().double(), dy[rows, some].double()
+            rstd = (v.var(0, unbiased=False) + 1e-5).rsqrt()
+            xhat = (v - v.mean(0)) * rstd
+            want = rstd * (d - d.mean(0) - xhat * (d * xhat).mean(0))
+            # numbers of 5 at most, sums of thousands: roundings of 64 u of sizes of up to 25
+            assert float((y[rows, some] - xhat).abs().max()) < 64 * U * 25
+            assert float((dx[rows, some] - want).abs().max()) < 64 * U * 25
+            dw64 += (d * xhat).sum(0)
+        assert float((dw[some] - dw64).abs().max()) < 64 * U * n
+        assert float((db[some] - dy[:, some].double().sum(0)).abs().max()) < 64 * U * n
