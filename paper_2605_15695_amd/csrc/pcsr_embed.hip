@@ -817,7 +817,8 @@ int pcsr_embed(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids
     EmbedArgs p = {n, rows, d, stride, ids, table, out, scale};
     return for_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const int lanes = lanes_for((d + kPer16<T> - 1) / kPer16<T>, n);
+        int lanes = lanes_for((d + kPer16<T> - 1) / kPer16<T>, n);
+        while (lanes > 4 && (n + kAhead - 1) / kAhead * lanes >= (int64_t(1) << 32) - kT) lanes /= 2; // no launch has 2^32 threads
         if (wide)
             for_lanes<Lookup<T, int64_t>::template Of>(lanes, p, s);
         else

@@ -127,3 +127,24 @@ def test_norms_of_many_groups_in_many_chunks(path):
             dw64 += (d * xhat).sum(0)
         assert float((dw[some] - dw64).abs().max()) < 64 * U * n
         assert float((db[some] - dy[:, some].double().sum(0)).abs().max()) < 64 * U * n
+
+
+# 2^30 ids, 16 lanes to a row by its width: as many threads as no launch has
+def test_a_lookup_of_a_billion_ids():
+    from paper_2605_15695_amd.embedding import embedding
+
+    n, d = 1 << 30, 49
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < n * (4 * d + 8) + (4 << 30):
+        pytest.skip("not enough free memory for 210 GB of rows")
+    table = torch.randn(7, d, generator=_gen(1), device="cuda")
+    ids = torch.empty(n, dtype=torch.int32, device="cuda")
+    ids.view(-1, 1 << 20).copy_((torch.arange(1 << 20, device="cuda") % 8).to(torch.int32))  # 7: no row
+    out = embedding(ids, table, 2.0)
+    want = torch.cat([table * 2.0, torch.zeros(1, d, device="cuda")]).repeat(1 << 17, 1)  # of 2^20 ids
+    try:
+        for at in range(0, n, 1 << 20):
+            assert torch.equal(out[at:at + (1 << 20)], want), at
+    finally:
+        del out, ids, want
+        torch.cuda.empty_cache()
