@@ -578,8 +578,10 @@ template <typename T, typename I, int L> __global__ void __launch_bounds__(kT) o
         flush();
     };
     auto finish = [&](int row, float (&sum)[N]) {
+        if (met[row]) { // the others are zeros whatever the scale
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] *= p.scale;
+            for (int i = 0; i < N; ++i) sum[i] *= p.scale;
+        }
         if (in) store_upto<T, N>(grad + (int64_t)row * p.d, m, sum);
     };
     if (!p.whole) {

@@ -148,3 +148,19 @@ def test_a_lookup_of_a_billion_ids():
     finally:
         del out, ids, want
         torch.cuda.empty_cache()
+
+
+# rows without an id: +0, whatever the scale, by each way their zeros are written
+@pytest.mark.parametrize("n,rows,d", [(50, 20, 5), (50, 3000, 5), (1000, 600, 64), (5000, 9000, 5), (20000, 30000, 5)])
+@pytest.mark.parametrize("scale", [-2.0, float("inf"), float("nan")])
+def test_rows_without_ids_do_not_know_the_scale(path, n, rows, d, scale):
+    from paper_2605_15695_amd.embedding import embedding
+
+    ids = torch.randint(0, rows // 2, (n,), generator=_gen(n), device="cuda") * 2 + 1
+    table = torch.ones(rows, d, device="cuda").requires_grad_()
+    grad, = torch.autograd.grad(embedding(ids, table, scale), table, torch.ones(n, d, device="cuda"))
+    met = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    met[ids] = True
+    assert not bool(grad[~met].view(torch.int32).any())  # all bits 0
+    want = torch.bincount(ids, minlength=rows)[met].float()[:, None].expand(-1, d) * scale
+    assert torch.equal(grad[met].nan_to_num(nan=7.0), want.nan_to_num(nan=7.0))
