@@ -314,6 +314,13 @@ def train_module():
     return _train
 
 
+def has_tangent(*tensors) -> bool:
+    """Whether a forward-mode derivative goes with one of the tensors (None: not there)."""
+    from torch.autograd import forward_ad
+
+    return any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
 def _first_spmm(h, B, C, K, stream):
     load_call_module()
     return _spmm(h, B, C, K, stream)

@@ -47,10 +47,10 @@ int type_of(const at::Tensor &t)
     default: return -1;
     }
 }
-// on the current device, plain memory
+// on the current device, plain memory, without a forward-mode tangent
 bool here(const at::Tensor &t)
 {
-    return t.is_cuda() && t.layout() == at::kStrided && t.device().index() == c10::hip::current_device();
+    return t.is_cuda() && t.layout() == at::kStrided && t.device().index() == c10::hip::current_device() && !t._fw_grad(0).defined();
 }
 void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
 at::Tensor bytes(int64_t n, const at::Tensor &like) { return at::empty({n}, like.options().dtype(at::kByte)); }

@@ -70,7 +70,8 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS) ->
 
     G: (rows, columns) or (matrices, rows, columns) of float32, bfloat16 or float16 on a GPU; any strides.
     coefficients: (a, b, c), or one for each step.  The result has G's type; products are taken of 22 bits of their
-    operands and summed in 32; X itself is held in 32."""
+    operands and summed in 32; X itself is held in 32.  The result is a constant to autograd, and a G that carries a
+    forward-mode tangent is refused."""
     fast = pc.train_module()
     if fast is not None and isinstance(steps, int):
         co = _coefficients(coefficients, steps)
@@ -81,6 +82,8 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS) ->
             return out
     if not isinstance(G, torch.Tensor) or G.dim() not in (2, 3) or G.dtype not in _TYPES or not G.is_cuda:
         raise ValueError("G must be a float32, bfloat16 or float16 CUDA tensor of two or three dimensions")
+    if pc.has_tangent(G):
+        raise NotImplementedError("orthogonalize has no forward-mode derivative")
     co = _coefficients(coefficients, steps)
     out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
     if G.numel() == 0:

@@ -29,7 +29,7 @@ def group_norm(X: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     uploaded; on the GPU they are taken as they are (the call does not wait), and offsets that do not
     ascend give wrong numbers, never an access outside the arrays.
     weight, bias: (channels,) of one type, float32 or X's.  activation: none, relu, silu or gelu (the exact one).
-    Statistics are float32 at least, sums in an order that the sizes alone decide."""
+    Statistics are float32 at least, sums in an order that the sizes alone decide.  There is no forward-mode derivative."""
     fast = pc.train_module()
     if fast is not None and activation in ACTIVATIONS:
         out = fast.group_norm(X, groups, weight, bias, offsets, eps, ACTIVATIONS[activation])
@@ -52,7 +52,7 @@ def group_norm(X: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     if offsets is not None:
         offsets = _checked_offsets(offsets, X)
     args = (X, weight, bias)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in args):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in args) or pc.has_tangent(*args):  # the node refuses tangents
         return GroupNormFunction.apply(*args, groups, offsets, float(eps), ACTIVATIONS[activation])
     return _forward(*args, groups, offsets, float(eps), ACTIVATIONS[activation])[0]
 

@@ -164,3 +164,39 @@ def test_rows_without_ids_do_not_know_the_scale(path, n, rows, d, scale):
     assert not bool(grad[~met].view(torch.int32).any())  # all bits 0
     want = torch.bincount(ids, minlength=rows)[met].float()[:, None].expand(-1, d) * scale
     assert torch.equal(grad[met].nan_to_num(nan=7.0), want.nan_to_num(nan=7.0))
+
+
+# forward-mode derivatives: there are none, and a call says so
+def test_tangents_are_refused(path):
+    import torch.autograd.forward_ad as fw
+
+    from paper_2605_15695_amd.embedding import embedding
+    from paper_2605_15695_amd.muon import orthogonalize
+    from paper_2605_15695_amd.norm import group_norm
+
+    X, w, b = torch.randn(10, 8, device="cuda"), torch.ones(8, device="cuda"), torch.zeros(8, device="cuda")
+    ids, off = torch.tensor([0, 3, 3], device="cuda"), torch.tensor([0, 4, 10], device="cuda")
+    calls = [(lambda t: embedding(ids, t), X), (lambda t: group_norm(t, 2), X), (lambda t: group_norm(t, 2, w, b, off, activation="silu"), X),
+             (lambda t: group_norm(X, 2, t, b), w), (lambda t: group_norm(X, 2, None, t), b), (orthogonalize, X),
+             (lambda t: orthogonalize(t.view(2, 5, 8)), X)]
+    for call, at in calls:
+        for leaf in (at, at.clone().requires_grad_()):
+            want = call(leaf)
+            with fw.dual_level():
+                dual = fw.make_dual(leaf, torch.ones_like(leaf))
+                with pytest.raises(NotImplementedError):
+                    call(dual)
+                with torch.no_grad(), pytest.raises(NotImplementedError):
+                    call(dual)
+                assert torch.equal(call(leaf), want)  # without one
+    with fw.dual_level():  # a dual number whose primal lies elsewhere, and empty inputs
+        with pytest.raises(NotImplementedError):
+            group_norm(fw.make_dual(X[:0], X[:0]), 2)
+        with pytest.raises(NotImplementedError):
+            orthogonalize(fw.make_dual(X.t(), X.t()))
+
+
+def test_an_orthogonalised_matrix_is_a_constant(path):
+    from paper_2605_15695_amd.muon import orthogonalize
+
+    assert not orthogonalize(torch.randn(4, 5, device="cuda").requires_grad_()).requires_grad
