@@ -47,10 +47,10 @@ int type_of(const at::Tensor &t)
     default: return -1;
     }
 }
-// on the current device, plain memory, without a forward-mode tangent
+// on the current device, plain memory (numbers as they are stored), without a forward-mode tangent
 bool here(const at::Tensor &t)
 {
-    return t.is_cuda() && t.layout() == at::kStrided && t.device().index() == c10::hip::current_device() && !t._fw_grad(0).defined();
+    return t.is_cuda() && t.layout() == at::kStrided && t.device().index() == c10::hip::current_device() && !t.is_neg() && !t._fw_grad(0).defined();
 }
 void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
 at::Tensor bytes(int64_t n, const at::Tensor &like) { return at::empty({n}, like.options().dtype(at::kByte)); }
@@ -96,7 +96,7 @@ struct Embed : torch::autograd::Function<Embed> {
     {
         const at::Tensor ids = ctx->get_saved_variables()[0];
         const int64_t n = ids.numel(), d = grads[0].size(-1), rows = ctx->saved_data["rows"].toInt();
-        at::Tensor g = grads[0].detach().reshape({n, d});
+        at::Tensor g = grads[0].detach().resolve_neg().reshape({n, d});
         if (distance(g) < 0) g = g.contiguous();
         at::Tensor out = at::empty({rows, d}, g.options()), ws = bytes(lib.embed_workspace(n, rows, d), g);
         ok(lib.embed_backward(n, rows, d, type_of(g), ids.const_data_ptr(), ids.scalar_type() == at::kLong, g.const_data_ptr(), distance(g),
@@ -176,7 +176,7 @@ struct Norm : torch::autograd::Function<Norm> {
         auto plain = [](const at::Tensor &t) { return t.defined() ? t.detach() : t; };
         const NormCall c = norm_call(X, plain(saved[1]), plain(saved[2]), saved[3], saved[4], ctx->saved_data["groups"].toInt(),
                                      ctx->saved_data["eps"].toDouble(), ctx->saved_data["act"].toInt());
-        at::Tensor g = grads[0].detach().reshape({c.x.size(0), c.x.size(1)});
+        at::Tensor g = grads[0].detach().resolve_neg().reshape({c.x.size(0), c.x.size(1)});
         if (distance(g) < 0) g = g.contiguous();
         at::Tensor dx, dw, db, ws; // (tensors that are not there are not counted)
         if (ctx->needs_input_grad(0)) dx = at::empty(X.sizes(), X.options());

@@ -45,6 +45,7 @@ def _check(rc, where):
 
 def _rows_of(t):
     """The tensor, or a copy whose rows are whole, and the distance of its rows."""
+    t = t.resolve_neg()
     if t.stride(1) != 1 and t.shape[1] > 1 or t.stride(0) < t.shape[1] and t.shape[0] > 1:
         t = t.contiguous()
     return t, max(t.stride(0), t.shape[1])

@@ -88,7 +88,7 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS) ->
     out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
     if G.numel() == 0:
         return out
-    G = G.detach()
+    G = G.detach().resolve_neg()
     mats = [(G, out)] if G.dim() == 2 else list(zip(G, out))
     if _ld(mats[0][0]) is None:
         G = G.contiguous()
@@ -160,11 +160,11 @@ class Muon(torch.optim.Optimizer):
         for p in params:
             if not p.is_cuda or p.grad.layout != torch.strided or p.grad.dtype != p.dtype:
                 raise ValueError("Muon steps dense matrices on a GPU, with gradients of their type")
-            buf, grad, out = self._momentum(p), p.grad, p.detach()
+            buf, grad, out = self._momentum(p), p.grad.resolve_neg(), p.detach()
             if _ld(grad) is None:
                 grad = grad.contiguous()
-            if _ld(out) is None:
-                out = out.contiguous()
+            if _ld(out) is None or out.is_neg():
+                out = out.resolve_neg().contiguous()
                 back.append((p, out))
             rate = lr * math.sqrt(max(1.0, p.shape[0] / p.shape[1]))
             by_type.setdefault((p.dtype, p.device), []).append((grad, pc.pcsr_matrix_t(

@@ -81,7 +81,7 @@ def _check(rc, where):
 
 def _rows_of(t):
     """(rows, channels) of a tensor, or of a copy where its rows do not lie at one distance, and that distance."""
-    C = t.shape[-1]
+    C, t = t.shape[-1], t.resolve_neg()
     if t.dim() != 2:
         t = t.reshape(-1, C)
     if t.stride(1) != 1 and C > 1 or t.stride(0) < C and t.shape[0] > 1:
@@ -104,7 +104,7 @@ def _struct(X, weight, bias, groups, offsets, eps, act, graphs, x, stride, mean,
 def _forward(X, weight, bias, groups, offsets, eps, act):
     x, stride = _rows_of(X.detach())
     graphs = offsets.numel() - 1 if offsets is not None else 1 if X.dim() == 2 else X.shape[0]
-    weight, bias = (None if p is None else p.detach().contiguous() for p in (weight, bias))
+    weight, bias = (None if p is None else p.detach().resolve_neg().contiguous() for p in (weight, bias))
     stats = torch.empty((2, graphs, groups), dtype=torch.float32, device=X.device)
     y = torch.empty(X.shape, dtype=X.dtype, device=X.device)
     if x.shape[0]:
@@ -126,7 +126,7 @@ def _backward(X, weight, bias, offsets, stats, dy, groups, eps, act, graphs, nee
     db = torch.empty(bias.shape, dtype=bias.dtype, device=X.device) if needs[2] else None
     if not x.shape[0]:
         return dx, None if dw is None else dw.zero_(), None if db is None else db.zero_()
-    weight, bias = (None if p is None else p.detach().contiguous() for p in (weight, bias))
+    weight, bias = (None if p is None else p.detach().resolve_neg().contiguous() for p in (weight, bias))
     lib = pc._lib()
     a = _struct(X, weight, bias, groups, offsets, eps, act, graphs, x, stride, stats[0], stats[1])
     ws = torch.empty(lib.pcsr_norm_workspace(ctypes.byref(a), 1), dtype=torch.uint8, device=X.device)

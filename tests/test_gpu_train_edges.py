@@ -200,3 +200,34 @@ def test_an_orthogonalised_matrix_is_a_constant(path):
     from paper_2605_15695_amd.muon import orthogonalize
 
     assert not orthogonalize(torch.randn(4, 5, device="cuda").requires_grad_()).requires_grad
+
+
+# a view whose numbers are stored with the other sign
+def test_views_with_a_sign(path):
+    from paper_2605_15695_amd.embedding import embedding
+    from paper_2605_15695_amd.muon import Muon, orthogonalize
+    from paper_2605_15695_amd.norm import group_norm
+
+    z = torch.randn(30, 1, generator=_gen(2), device="cuda", dtype=torch.complex64)
+    wide = torch.randn(30, 8, generator=_gen(3), device="cuda")
+    ids = torch.tensor([3, -1, 29], device="cuda")
+    for t in (z.conj().imag, torch._neg_view(wide)):
+        assert t.is_neg()
+        plain = t.resolve_neg().clone()
+        assert not plain.is_neg()
+        assert torch.equal(embedding(ids, t), embedding(ids, plain))
+        assert torch.equal(group_norm(t, 1), group_norm(plain, 1))
+        assert torch.equal(orthogonalize(t), orthogonalize(plain))
+        w, signed = plain[0].contiguous(), torch._neg_view(-plain[0])
+        assert signed.is_neg()
+        assert torch.equal(group_norm(plain, 1, signed, signed), group_norm(plain, 1, w, w))
+        grads = []
+        for g in (t, plain):
+            x = plain.clone().requires_grad_()
+            p = torch.nn.Parameter(plain.clone())
+            p.grad = g
+            opt = Muon([p])
+            opt.step()
+            opt.step()
+            grads.append([*torch.autograd.grad(embedding(torch.arange(30, device="cuda"), x), x, g), *torch.autograd.grad(group_norm(x, 1), x, g), p.detach()])
+        assert all(torch.equal(a, b) for a, b in zip(*grads))
