@@ -62,7 +62,7 @@ int64_t distance(const at::Tensor &t)
     const int64_t n = t.size(0), d = t.size(1), s = t.stride(0);
     if (t.numel() == 0) return d;
     if ((t.stride(1) != 1 && d > 1) || (s < d && n > 1)) return -1;
-    return s > d ? s : d;
+    return s > d && n > 1 ? s : d; // (of one row it means nothing)
 }
 
 // Gradients of a backward pass that is recorded itself are marked as having none.

@@ -48,7 +48,7 @@ def _rows_of(t):
     t = t.resolve_neg()
     if t.stride(1) != 1 and t.shape[1] > 1 or t.stride(0) < t.shape[1] and t.shape[0] > 1:
         t = t.contiguous()
-    return t, max(t.stride(0), t.shape[1])
+    return t, max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
 
 
 def _lookup(ids, table, scale):

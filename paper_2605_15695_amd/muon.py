@@ -47,7 +47,7 @@ def _ld(t):
     """Distance of rows of a matrix whose numbers lie one behind the other, None if they do not."""
     if t.stride(1) != 1 and t.shape[1] > 1 or t.stride(0) < t.shape[1] and t.shape[0] > 1:
         return None
-    return max(t.stride(0), t.shape[1])
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
 
 
 def _run(matrices, dtype, device, steps, coefficients, update=False, nesterov=False, momentum=0.0, keep=0.0):

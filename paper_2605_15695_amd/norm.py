@@ -86,7 +86,7 @@ def _rows_of(t):
         t = t.reshape(-1, C)
     if t.stride(1) != 1 and C > 1 or t.stride(0) < C and t.shape[0] > 1:
         t = t.contiguous()
-    return t, max(t.stride(0), C)
+    return t, max(t.stride(0), C) if t.shape[0] > 1 else C
 
 
 def _p(t):

@@ -231,3 +231,26 @@ def test_views_with_a_sign(path):
             opt.step()
             grads.append([*torch.autograd.grad(embedding(torch.arange(30, device="cuda"), x), x, g), *torch.autograd.grad(group_norm(x, 1), x, g), p.detach()])
         assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
+# the distance of rows means nothing where there is one
+def test_one_row_at_any_distance(path):
+    from paper_2605_15695_amd.embedding import embedding
+    from paper_2605_15695_amd.muon import Muon, orthogonalize
+    from paper_2605_15695_amd.norm import group_norm
+
+    row = torch.randn(1, 40, generator=_gen(1), device="cuda")
+    far = row.as_strided((1, 40), ((1 << 31) + 8, 1))
+    ids = torch.tensor([0, 0, -1], device="cuda")
+    assert torch.equal(embedding(ids, far), embedding(ids, row))
+    assert torch.equal(group_norm(far, 4), group_norm(row, 4))
+    assert torch.equal(orthogonalize(far), orthogonalize(row))
+    out = []
+    for g in (row, far):
+        x, p = row.clone().requires_grad_(), torch.nn.Parameter(row.clone().as_strided(g.shape, g.stride()))
+        grads = torch.autograd.grad(embedding(ids[:1], x), x, g) + torch.autograd.grad(group_norm(x, 4), x, g)
+        p.grad, opt = g, Muon([p])
+        opt.step()
+        opt.step()
+        out.append([*grads, p.detach()])
+    assert all(torch.equal(a, b) for a, b in zip(*out))
