@@ -310,7 +310,9 @@ def train_module():
         lib = _lib()
         _train = _load_module("_pcsr_train", TRAIN_PATH, [getattr(lib, "pcsr_" + n) for n in (
             "embed", "embed_workspace", "embed_backward", "norm", "norm_workspace", "norm_backward", "orthogonalize",
-            "ortho_workspace", "strerror")], "calls of the training step")
+            "ortho_workspace")], "calls of the training step")
+        if _train is not None:
+            _train.raises(PcsrError)
     return _train
 
 

@@ -31,12 +31,22 @@ struct Library {
     decltype(&pcsr_norm_backward) norm_backward;
     decltype(&pcsr_orthogonalize) orthogonalize;
     decltype(&pcsr_ortho_workspace) ortho_workspace;
-    decltype(&pcsr_strerror) strerror;
 } lib;
 bool ready = false;
+PyObject *error_type = PyExc_RuntimeError; // what a call of the library that returned an error raises, given the code and the call's name
 
-// a call of the library that returned an error
-void ok(int rc, const char *where) { TORCH_CHECK(rc == PCSR_OK, where, ": ", lib.strerror(rc), " [", rc, "]"); }
+// Throws that, through autograd's threads too: as torch hands on what Python code raised.
+void ok(int rc, const char *where)
+{
+    if (rc == PCSR_OK) return;
+    pybind11::gil_scoped_acquire locked;
+    PyObject *e = PyObject_CallFunction(error_type, "is", rc, where);
+    if (e) PyErr_SetObject(error_type, e);
+    Py_XDECREF(e);
+    python_error raised;
+    raised.persist();
+    throw std::move(raised);
+}
 
 int type_of(const at::Tensor &t)
 {
@@ -336,12 +346,25 @@ PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// raises(exception type)
+PyObject *raises(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 1 || !PyExceptionClass_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "raises takes the type of an exception");
+        return nullptr;
+    }
+    Py_INCREF(args[0]);
+    error_type = args[0];
+    Py_RETURN_NONE;
+}
+
 template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)> PyMethodDef method(const char *name)
 {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(F)), METH_FASTCALL, nullptr};
 }
 PyMethodDef methods[] = {method<embed>("embed"),   method<group_norm>("group_norm"), method<orthogonalize>("orthogonalize"),
-                         method<update>("update"), method<init>("init"),             {nullptr, nullptr, 0, nullptr}};
+                         method<update>("update"), method<init>("init"),             method<raises>("raises"),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pcsr_train", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

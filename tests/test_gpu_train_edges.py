@@ -254,3 +254,33 @@ def test_one_row_at_any_distance(path):
         opt.step()
         out.append([*grads, p.detach()])
     assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+# sizes that the library refuses: the same exception with the same code by either path, with and without a gradient to come
+def test_refusals_of_the_library_are_one_exception(path):
+    import paper_2605_15695_amd as pc
+    from paper_2605_15695_amd.embedding import embedding
+    from paper_2605_15695_amd.norm import group_norm
+
+    ids = torch.zeros(1, dtype=torch.int64, device="cuda")
+    table = torch.zeros(1, (1 << 23) + 1, device="cuda")  # wider than a table may be
+    X = torch.zeros(1, (1 << 22) + 2048, device="cuda")   # more channels than there may be
+    for call, t in ((lambda t: embedding(ids, t), table), (lambda t: group_norm(t, 2049), X)):
+        for leaf in (t, t.clone().requires_grad_()):
+            with pytest.raises(pc.PcsrError) as e:
+                call(leaf)
+            assert e.value.code == pc.binding.PCSR_E_TOO_LARGE
+
+
+def test_refusals_in_a_backward_pass_are_the_same_exception(path):
+    import paper_2605_15695_amd as pc
+    from paper_2605_15695_amd.embedding import embedding
+
+    # a gradient whose rows lie further apart than the library takes: one long row of another array
+    ids = torch.zeros(2, dtype=torch.int64, device="cuda")
+    table = torch.zeros(3, 2, device="cuda", dtype=torch.bfloat16).requires_grad_()
+    far = torch.zeros((1 << 31) + 16, device="cuda", dtype=torch.bfloat16).as_strided((2, 2), ((1 << 31) + 8, 1))
+    out = embedding(ids, table)
+    with pytest.raises(pc.PcsrError) as e:
+        torch.autograd.grad(out, table, far)
+    assert e.value.code == pc.binding.PCSR_E_TOO_LARGE
