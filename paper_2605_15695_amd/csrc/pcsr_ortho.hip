@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <memory>
+#include <new>
 #include <type_traits>
 
 #include "pcsr_num.h"
@@ -844,14 +846,13 @@ int pcsr_orthogonalize(const pcsr_matrix_t *m, int64_t count, const pcsr_ortho_t
     hipStream_t s = static_cast<hipStream_t>(stream);
     int64_t members[kItems];
     bool any = false;
-    // matrices are taken in the order they come, each with those behind it that are like it; `from` marks what is done
-    constexpr int64_t kMost = 4096;
-    if (count > kMost) return PCSR_E_TOO_LARGE;
-    char done[kMost] = {};
+    // matrices are taken in the order they come, each with those behind it that are like it
+    const std::unique_ptr<char[]> done(new (std::nothrow) char[(size_t)count]());
+    if (!done) return PCSR_E_OOM;
     for (int64_t k = 0; k < count; ++k) {
         if (done[k]) continue;
         if (m[k].rows == 0 || m[k].cols == 0) continue;
-        const int64_t n = group_of(m, count, k, done, members);
+        const int64_t n = group_of(m, count, k, done.get(), members);
         int used = 0;
         bool wide = false;
         for (int64_t i = 0; i < n; ++i) {

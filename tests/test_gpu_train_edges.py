@@ -284,3 +284,34 @@ def test_refusals_in_a_backward_pass_are_the_same_exception(path):
     with pytest.raises(pc.PcsrError) as e:
         torch.autograd.grad(out, table, far)
     assert e.value.code == pc.binding.PCSR_E_TOO_LARGE
+
+
+# more matrices than fit any array of fixed size
+@pytest.mark.parametrize("shape", [(4097, 3, 5), (5000, 8, 8)])
+def test_thousands_of_matrices(path, shape):
+    from paper_2605_15695_amd.muon import orthogonalize
+
+    G = torch.randn(*shape, generator=_gen(4), device="cuda")
+    out = orthogonalize(G)
+    for at in (0, 23, 24, 4095, 4096, shape[0] - 1):
+        assert torch.equal(out[at], orthogonalize(G[at]))
+
+
+def test_a_step_of_thousands_of_matrices(path):
+    from paper_2605_15695_amd.muon import Muon
+
+    g = _gen(5)
+    shapes = [(2, 3), (4, 2), (130, 2), (1, 1)] * 1030  # 1030 of them too wide for the launch of small ones
+    params = [torch.nn.Parameter(torch.zeros(s, device="cuda")) for s in shapes]
+    for p in params:
+        p.grad = torch.randn(p.shape, generator=g, device="cuda")
+    opt = Muon(params, lr=0.1)
+    opt.step()
+    opt.step()  # not the first step
+    for at in (0, 1, 2, 3, 4094, 4097, 4098, len(shapes) - 1):
+        p = torch.nn.Parameter(torch.zeros(shapes[at], device="cuda"))
+        p.grad = params[at].grad
+        opt = Muon([p], lr=0.1)
+        opt.step()
+        opt.step()
+        assert torch.equal(p, params[at])
