@@ -119,12 +119,17 @@ template <typename T> __device__ __forceinline__ Raw<T> raw(const T *p, int m)
     return v;
 }
 
-// The share of the normal distribution below z, by formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions (error
-// 7.5e-8); bell: exp(-z^2 / 2), which the slope of gelu needs as well.
+// The share of the normal distribution below z; bell: exp(-z^2 / 2), which the slope of gelu needs as well.  Below zero the share over the
+// bell is t P(t) with t = 1 / (1 + 0.346 |z|), P of degree 8 by weighted least squares for the smallest relative error over z from -14 to 0 (3.5e-8;
+// in fp32 5 u (1 + z^2), u = 2^-24, of which z^2 is the exponential's), so that gelu keeps its digits far below zero, where it is small.
 __device__ __forceinline__ float below_normal(float z, float bell)
 {
-    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678f * fabsf(z));
-    const float q = 0.5f * bell * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.346f, fabsf(z), 1.0f));
+    constexpr float P[8] = {0.14520301f, -0.26838204f, 0.18176714f, -0.03471449f, 0.1105235f, 0.11777047f, 0.13838688f, 0.13801986f};
+    float h = -0.02857433f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) h = __builtin_fmaf(h, t, P[k]);
+    const float q = bell * t * h;
     return z < 0.0f ? q : 1.0f - q;
 }
 template <int N> __device__ __forceinline__ void activate(float (&z)[N], int act)

@@ -28,7 +28,8 @@ def group_norm(X: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     ascend from 0 to the number of rows, and a graph without rows is allowed.  In host memory they are checked and
     uploaded; on the GPU they are taken as they are (the call does not wait), and offsets that do not
     ascend give wrong numbers, never an access outside the arrays.
-    weight, bias: (channels,) of one type, float32 or X's.  activation: none, relu, silu or gelu (the exact one).
+    weight, bias: (channels,) of one type, float32 or X's.  activation: none, relu, silu or gelu (by erf,
+    not tanh; below zero good to (16 + 2 z^2) 2^-24 of itself).
     Statistics are float32 at least, sums in an order that the sizes alone decide.  There is no forward-mode derivative."""
     fast = pc.train_module()
     if fast is not None and activation in ACTIVATIONS:

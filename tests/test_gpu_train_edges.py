@@ -315,3 +315,23 @@ def test_a_step_of_thousands_of_matrices(path):
         opt.step()
         opt.step()
         assert torch.equal(p, params[at])
+
+
+# A weight of 0 leaves the bias: gelu and its slope at chosen places.  With u = 2^-24 the exponential of -z^2/2 is off by 1.2 z^2 u (its
+# argument is rounded twice) and 2 u, the share below z by the polynomial's 3e-8 and some ten roundings beside it, so 16 u; where z is
+# positive a difference from 1 makes these absolute.
+def test_gelu_keeps_its_digits_far_below_zero(path):
+    from paper_2605_15695_amd.norm import group_norm
+
+    z = torch.cat([torch.linspace(-12.5, 6.0, 40_000, device="cuda"), torch.zeros(1, device="cuda")])
+    C = z.numel()
+    x = torch.zeros(1, C, device="cuda").requires_grad_()
+    w, b = torch.zeros(C, device="cuda"), z.clone().requires_grad_()
+    y = group_norm(x, C, w, b, activation="gelu")
+    slope, = torch.autograd.grad(y, b, torch.ones_like(y))
+    z = z.double()
+    below, bell = 0.5 * torch.erfc(-z / 2.0 ** 0.5), torch.exp(-0.5 * z * z) / (2.0 * torch.pi) ** 0.5
+    size = torch.minimum(below, torch.erfc(z / 2.0 ** 0.5) * 0.5) * (16 + 2 * z * z) + below * (z > 0) * 2
+    tiny = 2.0 ** -126  # numbers without a leading bit may be zeros
+    assert bool(((y.detach().double()[0] - z * below).abs() <= U * (z.abs() * size + (z * below).abs()) + tiny).all())
+    assert bool(((slope.double() - below - z * bell).abs() <= U * (size + z.abs() * bell * (8 + 2 * z * z) + below + z.abs() * bell) + tiny).all())
