@@ -25,6 +25,8 @@ COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 def _coefficients(coefficients, steps):
     """ctypes array of (a, b, c) for each step"""
+    if not isinstance(steps, int):  # before the look-up, to which 5 and 5.0 are the same
+        raise ValueError("steps must be a whole number")
     try:
         return _coefficient_array(coefficients, steps)
     except TypeError:  # lists cannot be looked up
@@ -33,7 +35,7 @@ def _coefficients(coefficients, steps):
 
 @functools.lru_cache(maxsize=64)
 def _coefficient_array(coefficients, steps):
-    if not isinstance(steps, int) or not 1 <= steps <= MAX_STEPS:
+    if not 1 <= steps <= MAX_STEPS:
         raise ValueError(f"steps must be 1 to {MAX_STEPS}")
     rows = list(coefficients)
     if rows and not isinstance(rows[0], (tuple, list)):
