@@ -157,7 +157,7 @@ class GroupNorm(torch.nn.Module):
 
     def __init__(self, groups: int, channels: int, eps: float = 1e-5, activation: str = "none"):
         super().__init__()
-        if channels % groups:
+        if not isinstance(groups, int) or groups < 1 or channels % groups:
             raise ValueError(f"{channels} channels do not make {groups} groups")
         if activation not in ACTIVATIONS:
             raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")

@@ -16,3 +16,11 @@ def test_steps_are_whole_numbers_whatever_came_before():
     opt.param_groups[0]["steps"] = 5.0
     with pytest.raises(ValueError):
         opt.step()
+
+
+@pytest.mark.parametrize("groups", [0, -4, 2.0, None])
+def test_modules_of_no_groups_are_refused(groups):
+    from paper_2605_15695_amd.norm import GroupNorm
+
+    with pytest.raises(ValueError):
+        GroupNorm(groups, 8)
