@@ -115,7 +115,8 @@ __device__ __forceinline__ void fill(const Fill &f, int64_t block, int64_t block
 
 // The place of an id among n sorted ones is the number of smaller ones and of equal ones before it.  64 ids to a
 // workgroup, a sixteenth of the keys to each of its wavefronts, read from LDS four at a time.  Bound by the comparisons, 2.7e8 for 16,384 ids
-// in one launch, where the passes below would be six: 33 us with 100 MB of zeros beside it, which alone take 16.
+// in one launch, where the passes below would be six: 33 us with 100 MB of zeros beside it, which alone take 16.  Gradients of 100,000 rows of 64
+// in fp32, by ranks for by passes: 8192 ids 32 us for 42, 16,384 43 for 43 (60 for 67 of 50,000 rows of 1000 in bf16), 32,768 89 for 46.
 template <typename I>
 __global__ void __launch_bounds__(kRankT) rank_kernel(int64_t n_ids, int64_t rows, const void *ids, uint32_t *key, uint32_t *pos,
                                                       int sorters, Fill f)
@@ -403,7 +404,8 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) runs_kernel(G
 
 // The run that goes on behind a tile and did not begin before it: its pieces, in order.  Runs of more than kJoinAlone
 // tiles are left to the whole workgroup, whose groups take a stretch of them each.  11 us after the 42 above, 8 after the 14: a chain of
-// round trips (key, its run's end, pieces).
+// round trips (key, its run's end, pieces).  kJoinAlone of 8, 32 and 128: gradients of 300,000 ids in 100,000 rows of 32 in bf16, many ids frequent,
+// 67, 65 and 74 us; of 20,000 in 1000 rows of 64 27, 28 and 32; all the same where ten rows have all ids.
 constexpr int kJoinAlone = 32;
 template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(GradArgs p)
 {
@@ -484,6 +486,9 @@ template <typename T, int L> __global__ void __launch_bounds__(kT) join_kernel(G
 // by its round trips and the zeros.  The whole workgroup takes a row, a stretch of its ids to each group, where the table has few, and
 // where it has more than kOwnAlone ids; the parts of a sum are added in order.  777 ids of 75 numbers in a table of 1500: 6.2 us; 48 ids
 // in 92,826 rows of 204 in bf16: 11 us, 38 MB (21 in slices of 4 lanes, which left fewer of them idle).
+// Beside sorting, 100,000 rows of 64 in fp32: 512 ids 10 us for 14, 2048 14 for 19, 4096 20 for 23, 8192 36 for 28; where ids are skewed the two
+// meet at 2048 already (19 for 20, 4096: 31 for 24), and an id that has nearly all of 4096 takes 425 for 39, since each group walks the whole list.
+// kOwnAlone of 12, 48 and 192, 2000 rows of 64: 777 ids 10.8, 8.9 and 9.0 us, more skewed 28, 28 and 46.
 constexpr int kOwnMost = 4096, kOwnAlone = 48;
 struct OwnArgs {
     int64_t n, rows, d, stride;
@@ -734,6 +739,9 @@ template <typename T, typename I> struct Own {
         static void run(OwnArgs p, int64_t slices, hipStream_t s)
         {
             constexpr int G = kT / L;
+            // A workgroup to a row below 512 rows: 4000 ids of 64 in 200 rows 9.6 us (26 by groups), 400 9.0 (16.5), 1000 9.0 (10.7), 1500 12.8 (9.2).
+            // 1024 workgroups, a look through all ids each, where that leaves every group a row: 4000 ids in 30,000 rows of 64 11 us (21 with 256 of
+            // them, 14 with 4096), 50 ids in 90,000 rows of 204 in bf16 10.9 (12.6, 14.8).
             p.whole = p.rows < 512;
             const int64_t per = p.rows / 1024;
             p.own = p.whole ? 1 : (int)(per < G ? G : per > 256 ? 256 : per);
@@ -761,7 +769,8 @@ template <typename I> int sort_ids(int64_t n, int64_t rows, const void *ids, con
     p.n = n, p.chunk = q.chunk, p.rows = rows, p.bits = q.bits, p.tiles = q.tiles, p.ids = ids;
     p.counts = reinterpret_cast<int32_t *>(ws + w.counts), p.totals = reinterpret_cast<int32_t *>(ws + w.totals);
     uint32_t *key2 = reinterpret_cast<uint32_t *>(ws + w.key2), *pos2 = reinterpret_cast<uint32_t *>(ws + w.pos2);
-    // shares of the zeros, as long as the launches take without (300,000 ids: 6, 4 and 12 us)
+    // Shares of the zeros, as long as the launches take without (300,000 ids: 6, 4 and 12 us).  Gradients of 20,000 ids in 2^20 rows of 64 in fp32: 85 us
+    // (all with the last launch 91, all with the first 100); of 300,000: 125 (125, 137); smaller tables: within 3 %.
     constexpr int kShares[3] = {3, 2, 5};
     int64_t filled = 0;
     int parts = 0;

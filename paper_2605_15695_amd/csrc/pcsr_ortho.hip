@@ -505,7 +505,7 @@ template <typename C> __device__ __forceinline__ int64_t own_place(int64_t tile,
     return ((((tile * C::WI * C::WJ + wave) * C::FI + r) * C::FJ + c) * 4 + e) * 64 + lane;
 }
 
-// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup.  4096 x 4096 in bf16: 65 us, 235 MB.
+// X0 = U / ||U|| as planes, transposed planes and fp32; 32 x 32 numbers to a workgroup.  4096 x 4096 in bf16: 63 us, 268 MB.
 template <typename T, typename C> __global__ void __launch_bounds__(kT) pack_kernel(Items q, const double *sums, int blocks, char *ws, Space sp, float scale)
 {
     __shared__ float tile[32][33];

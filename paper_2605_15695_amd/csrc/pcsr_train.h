@@ -19,8 +19,9 @@ enum { PCSR_F32 = 0, PCSR_BF16 = 1, PCSR_F16 = 2 };
 // for no row and gives zeros.  Rows of the table are `stride` numbers apart, those of out d.
 int pcsr_embed(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids, int32_t wide, const void *table,
                int64_t stride, float scale, void *out, void *stream);
-// grad[rows x d] = scale * the sum of dout[i] over the i with ids[i] = row, in 32 bits in an order that n, rows and d
-// alone decide, rounded once; zeros for rows without an id.  Rows of dout are `stride` numbers apart.
+// grad[rows x d] = scale * the sum of dout[i] over the i with ids[i] = row, in 32 bits in an order that the ids, n, rows, d and the
+// type alone decide, rounded once; zeros for rows without an id.  Rows of dout are `stride` numbers apart.
+// TOO_LARGE: n of 2^31 - 1024 and more, rows of 2^31, d above 2^23, stride above 2^31.
 // ws: pcsr_embed_workspace bytes (0 for few ids), 16-byte aligned.
 int64_t pcsr_embed_workspace(int64_t n, int64_t rows, int64_t d);
 int pcsr_embed_backward(int64_t n, int64_t rows, int64_t d, int32_t type, const void *ids, int32_t wide,
@@ -49,7 +50,9 @@ typedef struct {
 
 // bytes of workspace (16-byte aligned) of the calls below
 int64_t pcsr_norm_workspace(const pcsr_norm_t *a, int32_t backward);
-// y: [rows x channels].  UNSUPPORTED for groups of more than 2048 (fp32) or 4096 channels.
+// y: [rows x channels].  UNSUPPORTED for groups of more than 2048 (fp32) or 4096 channels.  TOO_LARGE: channels above 2^22, strides above 2^31,
+// and more graphs than a launch has teams for: 2^26, but where a graph takes a workgroup (more than 8 KB a graph on the average, or groups of
+// more than 64 pieces of 16 bytes) 2^24, and of groups above 256 pieces 2^23.
 int pcsr_norm(const pcsr_norm_t *a, void *y, void *ws, void *stream);
 // From dy (rows dy_stride numbers apart): dx [rows x channels], dweight and dbias [channels]; each may be null.
 int pcsr_norm_backward(const pcsr_norm_t *a, const void *dy, int64_t dy_stride, void *dx, void *dweight, void *dbias, void *ws,
@@ -69,7 +72,7 @@ typedef struct {
     int32_t reserved;
 } pcsr_matrix_t;
 typedef struct {
-    int32_t type, steps; // steps 0 to PCSR_ORTHO_STEPS
+    int32_t type, steps; // steps 1 to PCSR_ORTHO_STEPS
     const double *coefficients; // host, [steps][3]
     int32_t update, nesterov;
     float momentum, keep;
@@ -77,7 +80,8 @@ typedef struct {
 #define PCSR_ORTHO_STEPS 16
 // matrices: host, [count], which may overlap with no other's buf or out.  Products of fp16 numbers added up in fp32: operands are two fp16
 // numbers each (22 bits).
-// ws: 16-byte aligned, pcsr_ortho_workspace bytes.  UNSUPPORTED where the coefficients let the numbers grow out of fp32's range.
+// ws: 16-byte aligned, pcsr_ortho_workspace bytes.  UNSUPPORTED where the coefficients let the numbers grow out of fp32's range; TOO_LARGE: sides
+// above 2^17, matrices of more than 2^32 numbers.
 int64_t pcsr_ortho_workspace(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how);
 int pcsr_orthogonalize(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how, void *ws, void *stream);
 }

@@ -21,7 +21,7 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0) -> tor
     ids: int32 or int64 tensor of any shape on the table's GPU.  An id outside ``[0, len(table))`` stands
     for no row (padding): zeros, and no gradient.  table: (rows, d); rows may lie apart, numbers of a
     row may not (such a table is copied).  The gradient is dense, of the table's type; its sums are
-    taken in 32 bits, in an order that the sizes alone decide: the same bits on every run.  There is no forward-mode derivative."""
+    taken in 32 bits, in an order that ids, sizes and type alone decide: the same bits on every run.  There is no forward-mode derivative."""
     fast = pc.train_module()
     if fast is not None:
         out = fast.embed(ids, table, scale)

@@ -5,7 +5,7 @@ them (Muon: momentum, orthogonalised, per matrix).
     rest = torch.optim.Adam([p for p in model.parameters() if p.dim() != 2])
 
 Momentum, products and the update of the weights are kernels of the library: matrices of up to 128 x 128 take one
-launch for up to 24 of them, larger ones three per Newton-Schulz step for all of one shape.
+launch for up to 24 of them, larger ones three per Newton-Schulz step for up to 24 of one shape.
 """
 from __future__ import annotations
 
@@ -19,7 +19,7 @@ from . import binding as pc
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MAX_STEPS = 16
-# a fixed quintic that takes singular values from 0.01 to 1 to about 0.7 to 1.2 in five steps
+# the quintic published with the Muon optimiser (Jordan and others, 2024), which takes singular values from 0.01 to 1 to about 0.7 to 1.2 in five steps
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 

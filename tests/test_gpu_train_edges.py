@@ -92,7 +92,7 @@ def test_norms_of_half_a_million_groups(path, lengths):
         xhat, d = (v - v.mean(0)) * rstd, gv * 1.5
         # xhat is 4 at most, mean and products are rounded a dozen times; rstd is 316 at most (a graph of one row, whose numbers are 0)
         want = rstd * (d - d.mean(0) - xhat * (d * xhat).mean(0))
-        assert float((y[at:at + k] - 1.5 * xhat).abs().max()) < 64 * U * (1 + float((v.abs().amax(0) * rstd).max()))
+        assert float((y.detach()[at:at + k] - 1.5 * xhat).abs().max()) < 64 * U * (1 + float((v.abs().amax(0) * rstd).max()))
         if k > 1:
             err = (dx[at:at + k] - want).abs() / (rstd * (1 + v.abs().amax(0) * rstd) * 8)
             assert float(err.max()) < 64 * U
@@ -122,7 +122,7 @@ def test_norms_of_many_groups_in_many_chunks(path):
             xhat = (v - v.mean(0)) * rstd
             want = rstd * (d - d.mean(0) - xhat * (d * xhat).mean(0))
             # numbers of 5 at most, sums of thousands: roundings of 64 u of sizes of up to 25
-            assert float((y[rows, some] - xhat).abs().max()) < 64 * U * 25
+            assert float((y.detach()[rows, some] - xhat).abs().max()) < 64 * U * 25
             assert float((dx[rows, some] - want).abs().max()) < 64 * U * 25
             dw64 += (d * xhat).sum(0)
         assert float((dw[some] - dw64).abs().max()) < 64 * U * n

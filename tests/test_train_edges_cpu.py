@@ -24,3 +24,26 @@ def test_modules_of_no_groups_are_refused(groups):
 
     with pytest.raises(ValueError):
         GroupNorm(groups, 8)
+
+
+# the sizes that the header names as the first ones refused (nothing is launched), and that those below need a workspace
+def test_stated_limits():
+    import ctypes
+
+    from paper_2605_15695_amd import binding as pc
+
+    lib, P = pc._lib(), 4096
+
+    def embed(n=3, rows=5, d=4, stride=None):
+        return lib.pcsr_embed(n, rows, d, 0, P, 0, P, d if stride is None else stride, 1.0, P, None)
+
+    for bad in (dict(n=(1 << 31) - 1024), dict(rows=1 << 31), dict(d=(1 << 23) + 1), dict(stride=(1 << 31) + 1)):
+        assert embed(**bad) == pc.PCSR_E_TOO_LARGE, bad
+
+    def norm(type, graphs, rows, channels, groups):
+        a = pc.pcsr_norm_t(rows, channels, groups, graphs, None, 0, type, 0, 0, P, channels, None, None, 1e-5, P, P)
+        return lib.pcsr_norm(ctypes.byref(a), P, P, None)
+
+    for bad in ((0, 1 << 26, 1 << 26, 8, 2), (1, 1 << 24, 1 << 24, 5000, 5000), (0, 1 << 24, 1 << 24, 260, 1), (0, 1 << 23, 1 << 23, 1032, 1),
+                (0, 1, 3, (1 << 22) + 8, 1 << 19 | 1)):
+        assert norm(*bad) == pc.PCSR_E_TOO_LARGE, bad
