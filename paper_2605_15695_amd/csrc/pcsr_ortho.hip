@@ -665,9 +665,10 @@ template <typename T, typename C, int MODE> __global__ void __launch_bounds__(C:
 }
 
 // ---------------------------------------------------------------------------------- host
-float power_below(double bound) // the power of two that takes numbers up to `bound` to 32768 at most, 2^14 at most
+// The power of two that takes numbers up to `bound` to 32768 at most; 2^60 at most, so that 1 over its square is an fp32 number.
+float power_below(double bound)
 {
-    int e = 14;
+    int e = 60;
     if (bound > 0.0) {
         const int up = 15 - (int)std::ceil(std::log2(bound));
         e = up < e ? up : e;

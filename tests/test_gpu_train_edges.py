@@ -335,3 +335,17 @@ def test_gelu_keeps_its_digits_far_below_zero(path):
     tiny = 2.0 ** -126  # numbers without a leading bit may be zeros
     assert bool(((y.detach().double()[0] - z * below).abs() <= U * (z.abs() * size + (z * below).abs()) + tiny).all())
     assert bool(((slope.double() - below - z * bell).abs() <= U * (size + z.abs() * bell * (8 + 2 * z * z) + below + z.abs() * bell) + tiny).all())
+
+
+# polynomials that first make singular values small: products of small numbers keep their bits too.  The second step takes s = 1e-6 to s (1 - 0.5 + 0.1)
+@pytest.mark.parametrize("shape", [(30, 50), (300, 170)])
+def test_polynomials_that_shrink_first(shape):
+    from paper_2605_15695_amd.muon import orthogonalize
+    from test_gpu_muon import BOUND, _near, _polynomial
+
+    # one strong direction: X has a singular value of nearly 1
+    G = torch.randn(shape[0], 1, generator=_gen(1), device="cuda") @ torch.randn(1, shape[1], generator=_gen(2), device="cuda")
+    G += 0.01 * torch.randn(*shape, generator=_gen(3), device="cuda")
+    for small in (1e-3, 1e-6, 1e-9):
+        steps = [(small, 0.0, 0.0), (1.0, -0.5 / small ** 2, 0.1 / small ** 4)]
+        _near(orthogonalize(G, 2, steps), _polynomial(G, 2, tuple(steps)), BOUND[torch.float32])
