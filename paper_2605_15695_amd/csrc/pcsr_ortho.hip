@@ -6,8 +6,8 @@
 // Products run on the fp16 matrix instructions, 16 times the rate of the fp32 ones, summed in fp32.  Operands are two fp16 numbers each,
 // h + l = x to 2^-23 of it, and a product is h h + h l + l h (the last, l l, is below 2^-22): three instructions, 5 times the fp32 rate.  So it is for
 // bf16 matrices as well: one fp16 number, 2^-12 of rounding, is an eighth of what their result is rounded by, but where a matrix has few directions the
-// roundings do not average out, and the polynomial's terms, which cancel, make them 20 times as large in a step (a matrix of equal numbers was off by
-// 0.010, the result's own rounding being 0.002).  X itself is held in fp32 from step to step (a X and the sum are fp32), so that what is rounded are the
+// roundings do not average out, and the polynomial's terms, which cancel, make them many times as large (520 x 700 of 1 and -1 in one direction was
+// off by 0.010, where the result's own rounding is 0.004 at most).  X itself is held in fp32 from step to step (a X and the sum are fp32), so that what is rounded are the
 // operands of the products alone: directions of small singular values, which a step makes 3.4 times as large, keep their bits.
 // fp16 ends at 65504 and loses bits below 2^-14: the planes hold numbers times a power of two that the host finds from how
 // large singular values can be in that step (X0 has norm 1, then the polynomial's maximum over the range).

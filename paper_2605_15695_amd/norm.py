@@ -30,8 +30,8 @@ def group_norm(X: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
     ascend give wrong numbers, never an access outside the arrays.
     weight, bias: (channels,) of one type, float32 or X's.  activation: none, relu, silu or gelu (by erf,
     not tanh; below zero good to (16 + 2 z^2) 2^-24 of itself).
-    A group has 2048 channels at most (4096 in 16 bits), and there are 2^22 channels and 2^26 graphs at most, 2^23 of groups above
-    1 KB or of more than 8 KB a graph on the average (PcsrError).
+    A group has 2048 channels at most (4096 in 16 bits).  There are 2^22 channels at most, and 2^26 graphs, 2^24 where a graph has
+    more than 8 KB on the average or a group more than 1 KB of a row (more than 4: 2^23); PcsrError otherwise.
     Statistics are float32 at least, sums in an order that sizes, offsets and type alone decide.  There is no forward-mode derivative."""
     fast = pc.train_module()
     if fast is not None and activation in ACTIVATIONS:
