@@ -65,6 +65,18 @@ class pcsr_ortho_t(ctypes.Structure):
                 ("keep", ctypes.c_float)]
 
 
+class pcsr_drop_t(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("state", ctypes.c_void_p),
+                ("used", ctypes.c_void_p)]
+
+
+class pcsr_linear_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "in", "out")]
+    _fields_ += [(n, ctypes.c_int32) for n in ("type", "bias_type", "act", "reserved")]
+    _fields_ += [(n, ctypes.c_void_p) for n in ("x", "w", "bias", "residual")]
+    _fields_ += [(n, ctypes.c_int64) for n in ("x_stride", "w_stride", "r_stride")] + [("drop", pcsr_drop_t)]
+
+
 class PcsrError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -139,6 +151,12 @@ def _lib():
         lib.pcsr_ortho_workspace.argtypes = [pm, i64, po]
         lib.pcsr_ortho_workspace.restype = i64
         lib.pcsr_orthogonalize.argtypes = [pm, i64, po, vp, vp]
+        lib.pcsr_dropout.argtypes = [i64, i64, i32, vp, i64, vp, i64, ctypes.POINTER(pcsr_drop_t), vp, vp]
+        pl = ctypes.POINTER(pcsr_linear_t)
+        lib.pcsr_linear_workspace.argtypes = [pl, i32]
+        lib.pcsr_linear_workspace.restype = i64
+        lib.pcsr_linear.argtypes = [pl, vp, vp, vp, vp]
+        lib.pcsr_linear_backward.argtypes = [pl, vp, vp, i64, vp, vp, vp, vp, vp]
         for name in ("pcsr_build", "pcsr_spmm", "pcsr_free", "pcsr_set_kernel_params",
                      "pcsr_query_launch", "pcsr_query_kernel", "pcsr_export", "pcsr_features", "pcsr_select",
                      "pcsr_window_stats", "pcsr_features_device", "pcsr_reorder", "pcsr_permute_csr",
@@ -146,7 +164,8 @@ def _lib():
                      "pcsr_export_schedule", "pcsr_reorder_by_degree", "pcsr_spmm_epilogue", "pcsr_gnn_linear",
                      "pcsr_gnn_mlp", "pcsr_gnn_mlp_backward", "pcsr_gnn_linear_backward", "pcsr_gnn_wgrad",
                      "pcsr_gnn_colsum", "pcsr_operator_build", "pcsr_release_cached", "pcsr_embed",
-                     "pcsr_embed_backward", "pcsr_norm", "pcsr_norm_backward", "pcsr_orthogonalize"):
+                     "pcsr_embed_backward", "pcsr_norm", "pcsr_norm_backward", "pcsr_orthogonalize", "pcsr_dropout",
+                     "pcsr_linear", "pcsr_linear_backward"):
             getattr(lib, name).restype = ctypes.c_int
         _LIB = lib
     return _LIB

@@ -1,0 +1,610 @@
+// Linear layers of any width with what follows them (see pcsr_train.h).
+//
+// y = r + f act(z), z = x w^T + b, f = 0 or 1 / (1 - p) (pcsr_drop.h).  Backward: dz = f act'(z) dy, dx = dz w, dw = dz^T x,
+// db = the sums of dz's columns (dr = dy).
+//
+// Products D[i][j] = sum over k of P(i, k) Q(j, k) run on the 16-bit matrix instructions, in tiles that go through LDS, summed in
+// fp32.  An operand lies with its k side by side (x and w forward, dz for dx) or with its rows side by side (w for dx, dz and x for dw);
+// the second kind is turned on its way to LDS, where k is always side by side.
+//
+// fp32 numbers are three bf16 numbers each, x = p0 + p1 + p2 exactly (8 bits each), and a product is the six p q of order 2^-16 and more,
+// six instructions of 16 times the fp32 rate (the method: Henry, Tang and Heinecke, "Leveraging the bfloat16 Artificial Intelligence Datatype For
+// Higher-Precision Computations", ARITH 2019).  Numbers are split 2^16 times as large, so that small ones keep all their pieces.  A tile that has
+// met numbers of 2^38 and more (products of which would leave the range; an infinity's pieces are none) is done again in fp32.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "pcsr_act.h"
+#include "pcsr_drop.h"
+#include "pcsr_num.h"
+
+namespace pcsr {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+constexpr int kT = 256;
+constexpr float kUp = 65536.0f, kDown = 1.0f / (65536.0f * 65536.0f), kHot = 0x1p54f; // 2^38 of a number as it is split
+
+// what an operand's numbers are in LDS
+template <typename T> struct Num {
+    typedef T E;
+    static constexpr int NP = 1, KS = 64; // pieces, numbers of k in a stage: 128 bytes a row
+};
+template <> struct Num<float> {
+    typedef bfloat_t E;
+    static constexpr int NP = 3, KS = 32;
+};
+
+typedef half_t h8 __attribute__((ext_vector_type(8)));
+typedef bfloat_t b8 __attribute__((ext_vector_type(8)));
+// 16x16x32: lane l holds A[i = l % 16][k = 8 (l / 16) ..] and B[k][j = l % 16] likewise; D[i = 4 (l / 16) + r][j = l % 16]
+__device__ __forceinline__ f4 mfma(half_t, u4 a, u4 b, f4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f4 mfma(bfloat_t, u4 a, u4 b, f4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+
+struct Side { // an operand: number (row, k) is at[row * ld + k], turned: at[k * ld + row]
+    const void *at;
+    int64_t ld, n; // rows
+};
+template <typename T, bool TURN> __device__ __forceinline__ float number(const Side &s, int64_t row, int64_t k)
+{
+    const T *p = static_cast<const T *>(s.at);
+    return (float)(TURN ? p[k * s.ld + row] : p[row * s.ld + k]);
+}
+
+// ---------------------------------------------------------------------------------- what follows a product
+struct Tail {
+    const void *bias, *residual;
+    void *y, *z;
+    int64_t r_stride, rows, cols; // of y, whose rows lie one behind the other
+    int act, bias_type, z_type;   // z: PCSR_F32 or PCSR_F16
+    Drop drop;
+};
+
+// a number of which the slope will be taken, in fp16: cut at the range's ends, where slopes no longer change, and never 0 if it is none
+__device__ __forceinline__ half_t slope_place(float z)
+{
+    half_t h = (half_t)(z > 65504.0f ? 65504.0f : z < -65504.0f ? -65504.0f : z);
+    if (h == (half_t)0.0f && z != 0.0f) h = (half_t)__builtin_copysignf(5.9604645e-8f, z); // the smallest there is
+    return h;
+}
+
+// 8 numbers of x w^T, m of them there, at a row and a column that is a multiple of 8
+template <typename T> __device__ __forceinline__ void put8(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8])
+{
+    if (a.bias) {
+        float b[8];
+        if (a.bias_type == PCSR_F32) load_upto<float, 8>(static_cast<const float *>(a.bias) + c, m, b);
+        else load_upto<T, 8>(static_cast<const T *>(a.bias) + c, m, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += b[i];
+    }
+    if (a.z) {
+        if (a.z_type == PCSR_F32) {
+            store_upto<float, 8>(static_cast<float *>(a.z) + row * a.cols + c, m, v);
+        } else {
+            half_t *to = static_cast<half_t *>(a.z) + row * a.cols + c;
+            typename Pack<half_t, 8>::type h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = slope_place(v[i]);
+            if (m >= 8) {
+                *reinterpret_cast<typename Pack<half_t, 8>::type *>(to) = h;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < m) to[i] = h[i];
+            }
+        }
+    }
+    activate(v, a.act);
+    if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, v);
+    if (a.residual) {
+        float r[8];
+        load_upto<T, 8>(static_cast<const T *>(a.residual) + row * a.r_stride + c, m, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    store_upto<T, 8>(static_cast<T *>(a.y) + row * a.cols + c, m, v);
+}
+
+// ---------------------------------------------------------------------------------- operands on their way to LDS
+// A row's 16-byte chunks of k are exchanged by bits of its number, so that rows read side by side lie in different banks, and so do chunks of one k
+// written for many rows.
+template <int KS> __device__ __forceinline__ int place(int row, int chunk)
+{
+    const int turn = KS == 64 ? (row ^ row >> 3) & 7 : row >> 2 & 3;
+    return (row * (KS / 8) + (chunk ^ turn)) * 16;
+}
+
+__device__ __forceinline__ uint32_t two(bfloat_t a, bfloat_t b)
+{
+    return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+}
+// two numbers side by side in k, in pieces
+__device__ __forceinline__ void pieces(float x, float y, float &hot, uint32_t (&p)[3])
+{
+    x *= kUp, y *= kUp;
+    hot = __builtin_fmaxf(hot, __builtin_fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)));
+#pragma unroll
+    for (int o = 0; o < 3; ++o) {
+        const bfloat_t a = (bfloat_t)x, b = (bfloat_t)y;
+        p[o] = two(a, b);
+        if (o < 2) x -= (float)a, y -= (float)b;
+    }
+}
+
+// R rows of KS numbers of k
+template <typename T, bool TURN, int R, int THREADS> struct Loader {
+    static constexpr int KS = Num<T>::KS, NP = Num<T>::NP, N = kPer16<T>;
+    // a unit: 8 numbers of a row, or turned 4 of k in N rows
+    static constexpr int across = TURN ? R / N : KS / 8, units = TURN ? R / N * (KS / 4) : R * (KS / 8), U = (units + THREADS - 1) / THREADS;
+    static constexpr int parts = TURN ? 4 : 8 / N;
+    static constexpr bool whole = units % THREADS == 0;
+    typedef typename Pack<T, N>::type Raw;
+    Raw raw[U][parts];
+
+    __device__ __forceinline__ void fetch(const Side &s, int64_t row0, int64_t k0, int64_t k1, int tid)
+    {
+        const T *base = static_cast<const T *>(s.at);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = tid + u * THREADS;
+            if (!whole && id >= units) break;
+            if (TURN) {
+                const int64_t row = row0 + id % across * N, k = k0 + id / across * 4;
+                const int m = s.n - row >= N ? N : s.n > row ? (int)(s.n - row) : 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const T *p = base + (k + q) * s.ld + row;
+                    if (k + q < k1 && m == N) raw[u][q] = *reinterpret_cast<const Raw *>(p);
+                    else
+#pragma unroll
+                        for (int i = 0; i < N; ++i) raw[u][q][i] = k + q < k1 && i < m ? p[i] : (T)0.0f;
+                }
+            } else {
+                int64_t row = row0 + id / across;
+                row = row < s.n ? row : s.n - 1; // what comes of it is not stored
+                const int64_t k = k0 + id % across * 8;
+                const T *p = base + row * s.ld + k;
+                if (k + 8 <= k1) {
+#pragma unroll
+                    for (int q = 0; q < parts; ++q) raw[u][q] = *reinterpret_cast<const Raw *>(p + q * N);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < parts; ++q)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) raw[u][q][i] = k + q * N + i < k1 ? p[q * N + i] : (T)0.0f;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char *lds, float &hot, int tid) const
+    {
+        constexpr int plane = R * KS * 2;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = tid + u * THREADS;
+            if (!whole && id >= units) break;
+            if constexpr (TURN) {
+                const int row = id % across * N, kg = id / across;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    char *to = lds + place<KS>(row + i, kg >> 1) + (kg & 1) * 8;
+                    if constexpr (NP == 3) {
+                        uint32_t a[3], b[3];
+                        pieces(raw[u][0][i], raw[u][1][i], hot, a);
+                        pieces(raw[u][2][i], raw[u][3][i], hot, b);
+#pragma unroll
+                        for (int o = 0; o < 3; ++o) *reinterpret_cast<u2 *>(to + o * plane) = u2{a[o], b[o]};
+                    } else {
+                        typedef T t4 __attribute__((ext_vector_type(4)));
+                        const t4 v = {raw[u][0][i], raw[u][1][i], raw[u][2][i], raw[u][3][i]};
+                        *reinterpret_cast<t4 *>(to) = v;
+                    }
+                }
+            } else {
+                char *to = lds + place<KS>(id / across, id % across);
+                if constexpr (NP == 3) {
+                    uint32_t a[4][3];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) pieces(raw[u][q >> 1][(q & 1) * 2], raw[u][q >> 1][(q & 1) * 2 + 1], hot, a[q]);
+#pragma unroll
+                    for (int o = 0; o < 3; ++o) *reinterpret_cast<u4 *>(to + o * plane) = u4{a[0][o], a[1][o], a[2][o], a[3][o]};
+                } else {
+                    *reinterpret_cast<u4 *>(to) = __builtin_bit_cast(u4, raw[u][0]);
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------- tiles
+struct TileArgs {
+    Side p, q;
+    int64_t K, stretch; // stretch: of k, for a workgroup
+    int tiles_i, tiles_j;
+    float *part; // [stretch][rows][cols] sums, null: whole sums, for `tail`
+    Tail tail;
+};
+
+template <int BI_, int BJ_, int WI_, int WJ_> struct Tiling {
+    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, threads = 64 * WI * WJ, FI = BI / 16 / WI, FJ = BJ / 16 / WJ;
+};
+typedef Tiling<128, 128, 2, 2> Wide;
+typedef Tiling<128, 64, 2, 2> Tall;
+typedef Tiling<64, 64, 2, 2> Small;
+
+template <typename T, typename C> constexpr int lds_bytes()
+{
+    constexpr int stage = (C::BI + C::BJ) * Num<T>::KS * 2 * Num<T>::NP, out = C::WI * C::WJ * 16 * (C::FJ * 16 + 4) * 4;
+    return stage > out ? stage : out;
+}
+
+template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads) tile_kernel(TileArgs a)
+{
+    typedef typename Num<T>::E E;
+    constexpr int KS = Num<T>::KS, NP = Num<T>::NP, FI = C::FI, FJ = C::FJ;
+    constexpr int planeP = C::BI * KS * 2, planeQ = C::BJ * KS * 2;
+    __shared__ __align__(16) char lds[lds_bytes<T, C>()];
+    __shared__ int met;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
+    const int tile = blockIdx.x, ti = tile / a.tiles_j, tj = tile - ti * a.tiles_j;
+    const int64_t i0 = (int64_t)ti * C::BI, j0 = (int64_t)tj * C::BJ;
+    const int64_t k0 = blockIdx.y * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
+    if (tid == 0) met = 0;
+    f4 sum[FI][FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    float hot = 0.0f;
+    Loader<T, TP, C::BI, C::threads> lp;
+    Loader<T, TQ, C::BJ, C::threads> lq;
+    char *ldsP = lds, *ldsQ = lds + NP * planeP;
+    lp.fetch(a.p, i0, k0, k1, tid);
+    lq.fetch(a.q, j0, k0, k1, tid);
+    const int at = lane & 15, chunk = lane >> 4;
+    for (int64_t k = k0; k < k1; k += KS) {
+        lp.put(ldsP, hot, tid);
+        lq.put(ldsQ, hot, tid);
+        __syncthreads();
+        if (k + KS < k1) {
+            lp.fetch(a.p, i0, k + KS, k1, tid);
+            lq.fetch(a.q, j0, k + KS, k1, tid);
+        }
+#pragma unroll
+        for (int kk = 0; kk < KS / 32; ++kk) {
+            u4 x[FI][NP], y[FJ][NP];
+#pragma unroll
+            for (int o = 0; o < NP; ++o) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+                    x[i][o] = *reinterpret_cast<const u4 *>(ldsP + o * planeP + place<KS>((wi * FI + i) * 16 + at, kk * 4 + chunk));
+#pragma unroll
+                for (int j = 0; j < FJ; ++j)
+                    y[j][o] = *reinterpret_cast<const u4 *>(ldsQ + o * planeQ + place<KS>((wj * FJ + j) * 16 + at, kk * 4 + chunk));
+            }
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) {
+                    if constexpr (NP == 3) {
+                        // a stage's products have a sum of their own, small ones first: the matrix instructions cut off what does not reach a
+                        // sum's last bit, always downwards
+                        f4 s = mfma(E(), x[i][2], y[j][0], f4{0.0f, 0.0f, 0.0f, 0.0f});
+                        s = mfma(E(), x[i][0], y[j][2], s);
+                        s = mfma(E(), x[i][1], y[j][1], s);
+                        s = mfma(E(), x[i][1], y[j][0], s);
+                        s = mfma(E(), x[i][0], y[j][1], s);
+                        s = mfma(E(), x[i][0], y[j][0], s);
+                        sum[i][j] += s;
+                    } else {
+                        sum[i][j] = mfma(E(), x[i][0], y[j][0], sum[i][j]);
+                    }
+                }
+        }
+        __syncthreads();
+    }
+    bool again = false;
+    if constexpr (NP == 3) {
+        if (hot >= kHot) met = 1; // (a NaN needs nothing: its pieces are NaN)
+        __syncthreads();
+        again = met;
+    }
+    // Sums go through LDS, 16 rows of the wavefront at a time, so that a lane has 8 columns side by side.
+    constexpr int LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
+    float *own = reinterpret_cast<float *>(lds) + wave * 16 * LD;
+    DropKey key = {};
+    if (!a.part && a.tail.drop.threshold) {
+        key = key_of(a.tail.drop);
+        if (tile == 0 && tid == 0) tell_key(a.tail.drop, key);
+    }
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+#pragma unroll
+        for (int j = 0; j < FJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) own[(chunk * 4 + e) * LD + j * 16 + at] = sum[i][j][e];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 16 * per / 64; ++h) {
+            const int r = (lane + h * 64) / per, c = (lane + h * 64) % per * 8;
+            const int64_t row = i0 + (wi * FI + i) * 16 + r, col = j0 + wj * FJ * 16 + c;
+            float v[8];
+            const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = NP == 3 ? lo[e] * kDown : lo[e];
+                v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
+            }
+            if (row >= a.tail.rows || col >= a.tail.cols) continue;
+            const int m = a.tail.cols - col < 8 ? (int)(a.tail.cols - col) : 8;
+            if (NP == 3 && again) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = 0.0f;
+                    if (e < m)
+                        for (int64_t k = k0; k < k1; ++k) v[e] = __builtin_fmaf(number<T, TP>(a.p, row, k), number<T, TQ>(a.q, col + e, k), v[e]);
+                }
+            }
+            if (a.part) store_upto<float, 8>(a.part + (blockIdx.y * a.tail.rows + row) * a.tail.cols + col, m, v);
+            else put8<T>(a.tail, key, row, col, m, v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// sums of the stretches of k, in their order, and what follows
+template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(const float *part, int stretches, Tail a, uint32_t groups)
+{
+    const int64_t t = (int64_t)blockIdx.x * kT + threadIdx.x, row = t / groups, c = (t - row * groups) * 8;
+    DropKey key = {};
+    if (a.drop.threshold) {
+        key = key_of(a.drop);
+        if (t == 0) tell_key(a.drop, key);
+    }
+    if (row >= a.rows) return;
+    const int m = a.cols - c < 8 ? (int)(a.cols - c) : 8;
+    float v[8] = {};
+    for (int s = 0; s < stretches; ++s) {
+        float x[8];
+        load_upto<float, 8>(part + (s * a.rows + row) * a.cols + c, m, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += x[i];
+    }
+    put8<T>(a, key, row, c, m, v);
+}
+
+// ---------------------------------------------------------------------------------- gradient at z
+struct SlopeArgs {
+    const void *dy, *z;
+    int64_t dy_stride, rows, cols, ld; // ld: of dz
+    void *dz;                          // null: sums alone
+    float *sums;                       // [workgroup][cols], null: none
+    int act, z_type, lanes;            // lanes: to a row
+    int64_t chunk;                     // rows of a workgroup
+    Drop drop;
+};
+
+// dz = f act'(z) dy, and sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows.
+template <typename T> __global__ void __launch_bounds__(kT) slope_kernel(SlopeArgs a)
+{
+    __shared__ float part[kT][8];
+    const int lane = threadIdx.x % a.lanes, r = threadIdx.x / a.lanes, per = kT / a.lanes;
+    const int64_t c = ((int64_t)blockIdx.y * a.lanes + lane) * 8, first = blockIdx.x * a.chunk, end = first + a.chunk < a.rows ? first + a.chunk : a.rows;
+    const int m = a.cols - c >= 8 ? 8 : a.cols > c ? (int)(a.cols - c) : 0;
+    const DropKey key = key_of(a.drop);
+    float sum[8] = {};
+    if (m > 0)
+        for (int64_t row = first + r; row < end; row += per) {
+            float d[8], z[8];
+            load_upto<T, 8>(static_cast<const T *>(a.dy) + row * a.dy_stride + c, m, d);
+            if (a.act != PCSR_ACT_NONE) {
+                if (a.z_type == PCSR_F32) load_upto<float, 8>(static_cast<const float *>(a.z) + row * a.cols + c, m, z);
+                else load_upto<half_t, 8>(static_cast<const half_t *>(a.z) + row * a.cols + c, m, z);
+                slopes(z, a.act);
+            }
+            if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (a.act != PCSR_ACT_NONE) d[i] *= z[i];
+                if (i >= m) d[i] = 0.0f;
+                sum[i] += d[i];
+            }
+            if (a.dz) store_upto<T, 8>(static_cast<T *>(a.dz) + row * a.ld + c, m, d);
+        }
+    if (!a.sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[threadIdx.x][i] = sum[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < a.lanes * 8; t += kT) {
+        float s = 0.0f;
+        for (int q = 0; q < per; ++q) s += part[q * a.lanes + t / 8][t % 8];
+        const int64_t col = (int64_t)blockIdx.y * a.lanes * 8 + t;
+        if (col < a.cols) a.sums[blockIdx.x * a.cols + col] = s;
+    }
+}
+// db: a wavefront to a column would read one number of a line, so a thread adds up a column of 64 side by side, four stretches of workgroups beside one another
+__global__ void __launch_bounds__(kT) sums_kernel(const float *sums, int64_t blocks, int64_t cols, int type, void *db)
+{
+    __shared__ double part[4][64];
+    const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    double s = 0.0;
+    if (c < cols)
+        for (int64_t b = q; b < blocks; b += 4) s += (double)sums[b * cols + c];
+    part[q][lane] = s;
+    __syncthreads();
+    if (q || c >= cols) return;
+    const float v = (float)(part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane]);
+    if (type == PCSR_F32) static_cast<float *>(db)[c] = v;
+    else if (type == PCSR_BF16) static_cast<bfloat_t *>(db)[c] = (bfloat_t)v;
+    else static_cast<half_t *>(db)[c] = (half_t)v;
+}
+
+// ---------------------------------------------------------------------------------- launches
+int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
+int64_t round16(int64_t n) { return up(n, 16) * 16; }
+constexpr int64_t kMostTiles = int64_t(1) << 23;
+
+// how a product of I x J numbers over K is cut
+struct Plan {
+    int which; // tiling
+    int64_t tiles_i, tiles_j, stretch;
+    int stretches;
+    int64_t bytes() const { return 0; }
+};
+template <typename T> Plan plan(int64_t I, int64_t J, int64_t K)
+{
+    Plan p;
+    const int BI[] = {Wide::BI, Tall::BI, Small::BI}, BJ[] = {Wide::BJ, Tall::BJ, Small::BJ};
+    p.which = J <= 64 ? 1 : 0;
+    if (up(I, 128) * up(J, 128) < 256) p.which = 2;
+    p.tiles_i = up(I, BI[p.which]), p.tiles_j = up(J, BJ[p.which]);
+    const int64_t tiles = p.tiles_i * p.tiles_j, stages = up(K, Num<T>::KS);
+    int64_t s = tiles >= 512 ? 1 : 512 / (tiles ? tiles : 1);
+    if (s > stages / 4) s = stages / 4;
+    if (s < 1) s = 1;
+    p.stretch = up(stages, s) * Num<T>::KS;
+    p.stretches = (int)(K ? up(K, p.stretch) : 1);
+    return p;
+}
+int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
+
+template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, const Tail &tail, void *ws, hipStream_t stream)
+{
+    const Plan c = plan<T>(p.n, q.n, K);
+    TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
+    const dim3 grid((unsigned)(c.tiles_i * c.tiles_j), (unsigned)c.stretches);
+    switch (c.which) {
+    case 0: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Wide>), grid, dim3(Wide::threads), 0, stream, a); break;
+    case 1: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Tall>), grid, dim3(Tall::threads), 0, stream, a); break;
+    default: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Small>), grid, dim3(Small::threads), 0, stream, a);
+    }
+    if (c.stretches > 1) {
+        const uint32_t groups = (uint32_t)up(tail.cols, 8);
+        hipLaunchKernelGGL(finish_kernel<T>, dim3((unsigned)up(tail.rows * groups, kT)), dim3(kT), 0, stream, a.part, c.stretches, tail, groups);
+    }
+    return launched();
+}
+
+// the parts of the workspace of a backward call
+struct Space {
+    int64_t ld, dz, sums, part, bytes;
+    int64_t blocks, chunk; // workgroups of slope_kernel along the rows, rows of each
+    int lanes;
+    template <typename T> static Space of(const pcsr_linear_t &a, bool own)
+    {
+        Space s;
+        s.ld = up(a.out, 8) * 8;
+        s.lanes = 1;
+        while (s.lanes < 64 && s.lanes * 8 < a.out) s.lanes *= 2;
+        const int64_t beside = up(a.out, s.lanes * 8), per = kT / s.lanes;
+        int64_t most = up(2048, beside);
+        if (most < 64) most = 64;
+        s.chunk = up(up(a.rows, most), per) * per;
+        s.blocks = up(a.rows, s.chunk);
+        s.dz = own ? round16(a.rows * s.ld * (int64_t)sizeof(T)) : 0;
+        s.sums = round16(4 * s.blocks * a.out);
+        const int64_t x = part_bytes(plan<T>(a.rows, a.in, a.out), a.rows, a.in), w = part_bytes(plan<T>(a.out, a.in, a.rows), a.out, a.in);
+        s.part = x > w ? x : w;
+        s.bytes = s.dz + s.sums + s.part;
+        return s;
+    }
+};
+bool has_slope(const pcsr_linear_t &a) { return a.act != PCSR_ACT_NONE || drop_of(&a.drop).threshold; }
+
+int check(const pcsr_linear_t *a)
+{
+    if (!a || a->rows < 0 || a->in < 0 || a->out < 1 || !(a->drop.p >= 0.0 && a->drop.p <= 1.0)) return PCSR_E_INVALID_ARG;
+    if (a->type < PCSR_F32 || a->type > PCSR_F16 || a->act < PCSR_ACT_NONE || a->act > PCSR_ACT_GELU) return PCSR_E_UNSUPPORTED;
+    if (a->bias_type != PCSR_F32 && a->bias_type != a->type) return PCSR_E_UNSUPPORTED;
+    const int64_t big = int64_t(1) << 31;
+    if (a->rows >= big * 2 || a->in >= big || a->out >= big) return PCSR_E_TOO_LARGE;
+    for (const int64_t t : {up(a->rows, 64) * up(a->out, 64), up(a->rows, 64) * up(a->in, 64), up(a->out, 64) * up(a->in, 64)})
+        if (t > kMostTiles) return PCSR_E_TOO_LARGE;
+    if (a->rows > 0 && a->in > 0 && (a->x_stride < a->in || a->w_stride < a->in)) return PCSR_E_INVALID_ARG;
+    return PCSR_OK;
+}
+
+} // namespace
+} // namespace pcsr
+
+using namespace pcsr;
+
+extern "C" {
+
+int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward)
+{
+    if (check(a) != PCSR_OK || a->rows == 0) return 0;
+    int64_t need = 0;
+    for_type(a->type, [&](auto z) {
+        typedef decltype(z) T;
+        need = backward ? Space::of<T>(*a, has_slope(*a)).bytes : part_bytes(plan<T>(a->rows, a->out, a->in), a->rows, a->out);
+        return 0;
+    });
+    return need;
+}
+
+int pcsr_linear(const pcsr_linear_t *a, void *y, void *z, void *ws, void *stream)
+{
+    if (const int rc = check(a)) return rc;
+    if (a->rows == 0) return PCSR_OK;
+    if (!y || (a->in > 0 && (!a->x || !a->w)) || (a->residual && a->r_stride < a->out)) return PCSR_E_INVALID_ARG;
+    if (!ws && pcsr_linear_workspace(a, 0)) return PCSR_E_INVALID_ARG;
+    const Tail tail = {a->bias, a->residual, y, z, a->r_stride, a->rows, a->out, a->act, a->bias_type, a->type == PCSR_F32 ? PCSR_F32 : PCSR_F16,
+                       drop_of(&a->drop)};
+    return for_type(a->type, [&](auto t) {
+        typedef decltype(t) T;
+        return product<T, false, false>({a->x, a->x_stride, a->rows}, {a->w, a->w_stride, a->out}, a->in, tail, ws, (hipStream_t)stream);
+    });
+}
+
+int pcsr_linear_backward(const pcsr_linear_t *a, const void *z, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws,
+                         void *stream_)
+{
+    if (const int rc = check(a)) return rc;
+    if (a->rows == 0 || (!dx && !dw && !db)) return PCSR_OK;
+    const hipStream_t stream = (hipStream_t)stream_;
+    if (!dy || dy_stride < a->out || (a->act != PCSR_ACT_NONE && !z) || (dx && !a->w) || (dw && !a->x) || !ws) return PCSR_E_INVALID_ARG;
+    return for_type(a->type, [&](auto t) -> int {
+        typedef decltype(t) T;
+        const bool own = has_slope(*a);
+        const Space sp = Space::of<T>(*a, own);
+        char *at = static_cast<char *>(ws);
+        float *sums = reinterpret_cast<float *>(at + sp.dz);
+        void *part = at + sp.dz + sp.sums;
+        Side dz = {dy, dy_stride, a->rows};
+        const Drop drop = drop_of(&a->drop);
+        if (own || db) {
+            SlopeArgs s = {dy, z, dy_stride, a->rows, a->out, sp.ld, own && (dx || dw) ? at : nullptr, db ? sums : nullptr, a->act,
+                           a->type == PCSR_F32 ? PCSR_F32 : PCSR_F16, sp.lanes, sp.chunk, drop};
+            hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)sp.blocks, (unsigned)up(a->out, sp.lanes * 8)), dim3(kT), 0, stream, s);
+            if (db)
+                hipLaunchKernelGGL(sums_kernel, dim3((unsigned)up(a->out, 64)), dim3(kT), 0, stream, sums, sp.blocks, a->out, a->bias_type, db);
+            if (own) dz = {at, sp.ld, a->rows};
+        }
+        int rc = launched();
+        if (dx && a->in > 0 && rc == PCSR_OK) {
+            const Tail tail = {nullptr, nullptr, dx, nullptr, 0, a->rows, a->in, PCSR_ACT_NONE, PCSR_F32, PCSR_F32, drop_of(nullptr)};
+            rc = product<T, false, true>(dz, {a->w, a->w_stride, a->in}, a->out, tail, part, stream);
+        }
+        if (dw && a->in > 0 && rc == PCSR_OK) {
+            const Tail tail = {nullptr, nullptr, dw, nullptr, 0, a->out, a->in, PCSR_ACT_NONE, PCSR_F32, PCSR_F32, drop_of(nullptr)};
+            rc = product<T, true, true>({dz.at, dz.ld, a->out}, {a->x, a->x_stride, a->in}, a->rows, tail, part, stream);
+        }
+        return rc;
+    });
+}
+}

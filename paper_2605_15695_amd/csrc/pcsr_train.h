@@ -1,6 +1,6 @@
-// What a training step needs around the graph layers (internal to the package: embedding.py, norm.py and muon.py call
-// these through ctypes): a table of node features and its gradient, group norm with an activation over rows of
-// channels, updates of weight matrices orthogonalised by Newton-Schulz products.
+// What a training step needs around the graph layers (internal to the package: embedding.py, norm.py, muon.py, dropout.py and
+// linear.py call these through ctypes): a table of node features and its gradient, group norm with an activation over rows of
+// channels, updates of weight matrices orthogonalised by Newton-Schulz products, dropout, linear layers of any width with what follows them.
 //
 // All arrays are device memory unless a host array is named; nothing is allocated here and the stream is not waited for.
 // Kernels go to the device that is current, which has to be that of the stream and the arrays.
@@ -84,4 +84,40 @@ typedef struct {
 // above 2^17, matrices of more than 2^32 numbers.
 int64_t pcsr_ortho_workspace(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how);
 int pcsr_orthogonalize(const pcsr_matrix_t *matrices, int64_t count, const pcsr_ortho_t *how, void *ws, void *stream);
+
+// ---------------------------------------------------------------------------------- dropout (pcsr_drop.hip)
+// What is dropped is a function of seed, offset, row and column (pcsr_drop.h).  p: in [0, 1], rounded to a multiple of 2^-16.
+typedef struct {
+    double p;
+    uint64_t seed, offset;
+    const int64_t *state; // device, null or {seed, offset}: read by the kernels when they run, in place of the two above
+    int64_t *used;        // device, null or [2]: seed and offset that were used (p > 0)
+} pcsr_drop_t;
+// out[rows x cols] = residual + x with numbers dropped and the others multiplied by 1 / (1 - p), in fp32, rounded once.  residual: null for
+// none.  Rows of x are x_stride, of residual r_stride numbers apart, those of out cols.  out may be x or residual where their rows lie as its own do.
+// TOO_LARGE: rows of 2^32 and more, columns of 2^31.
+int pcsr_dropout(int64_t rows, int64_t cols, int32_t type, const void *x, int64_t x_stride, const void *residual, int64_t r_stride,
+                 const pcsr_drop_t *how, void *out, void *stream);
+
+// ---------------------------------------------------------------------------------- linear layers (pcsr_linear.hip)
+// y = residual + dropout(act(x w^T + bias)): x [rows x in], w [out x in], y and residual [rows x out], one type; bias [out] of
+// that type or fp32, null for none; residual null for none.  Products of 16-bit numbers are exact and summed in fp32; those of
+// fp32 numbers are taken of three bf16 numbers each (24 bits).  Everything behind the product is fp32, rounded once.
+typedef struct {
+    int64_t rows, in, out;
+    int32_t type, bias_type, act, reserved;
+    const void *x, *w, *bias, *residual;
+    int64_t x_stride, w_stride, r_stride;
+    pcsr_drop_t drop;
+} pcsr_linear_t;
+// bytes of workspace (16-byte aligned) of the calls below; backward: those for all of its results
+int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward);
+// z: null, or [rows x out] for the backward call where act is not none: x w^T + bias, fp32 for fp32 and otherwise fp16 (cut at +-65504, and
+// numbers too small for it keep their sign), of which the slope is taken.
+// TOO_LARGE: rows of 2^32 and more, in or out of 2^31, and more than 2^23 tiles of 64 x 64 of y, of dx or of dw.
+int pcsr_linear(const pcsr_linear_t *a, void *y, void *z, void *ws, void *stream);
+// From dy (rows dy_stride numbers apart): dx [rows x in], dw [out x in], db [out] of bias_type; each may be null.  a->bias and a->residual are not read; a->x is for
+// dw alone, a->w for dx.
+int pcsr_linear_backward(const pcsr_linear_t *a, const void *z, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws,
+                         void *stream);
 }

@@ -1,0 +1,127 @@
+"""Dropout and linear layers without a GPU: the generator against its published values, what the C entry points and the Python calls refuse
+before they touch the device."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from drop_reference import kept, philox
+from paper_2605_15695_amd import binding as pc
+
+torch = pytest.importorskip("torch")
+
+OK, INVALID, UNSUPPORTED, TOO_LARGE = pc.PCSR_OK, pc.PCSR_E_INVALID_ARG, pc.PCSR_E_UNSUPPORTED, pc.PCSR_E_TOO_LARGE
+P = 4096  # an address: nothing is read there
+
+
+# the known answers that the generator was published with
+@pytest.mark.parametrize("counter,key,words", [
+    ([0] * 4, [0] * 2, "6627e8d5 e169c58d bc57ac4c 9b00dbd8"),
+    ([0xFFFFFFFF] * 4, [0xFFFFFFFF] * 2, "408f276d 41c83b0e a20bc7c6 6d5451fd"),
+    ([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0], "d16cfe09 94fdcceb 5001e420 24126ea1")])
+def test_reference_generator(counter, key, words):
+    assert " ".join("%08x" % int(w) for w in philox(counter, key)) == words
+
+
+def test_reference_places():
+    k, f = kept(3, 19, 0.25, 5, 1 << 33)
+    words = philox([2, 1, 0, 2], [5, 0])
+    bits = [h for w in words for h in (int(w) & 0xFFFF, int(w) >> 16)]
+    assert k[1, 16:].tolist() == [b >= 16384 for b in bits[:3]] and f == 65536 / 49152
+    assert np.array_equal(kept(1, 19, 0.25, 5, 1 << 33, first=2)[0], k[2:])
+    assert not kept(4, 4, 1.0, 1, 1)[0].any() and kept(4, 4, 0.0, 1, 1)[0].all()
+
+
+def test_dropout_entry_point():
+    lib = pc._lib()
+
+    def call(rows=3, cols=4, type=0, x=P, x_stride=4, residual=None, r_stride=0, p=0.5, out=P, how=True):
+        d = pc.pcsr_drop_t(p, 1, 2, None, None)
+        return lib.pcsr_dropout(rows, cols, type, x, x_stride, residual, r_stride, ctypes.byref(d) if how else None, out, None)
+
+    for bad in (dict(rows=-1), dict(cols=0), dict(x=None), dict(out=None), dict(x_stride=3), dict(residual=P, r_stride=3), dict(p=-0.1), dict(p=1.1),
+                dict(p=float("nan")), dict(how=False)):
+        assert call(**bad) == INVALID, bad
+    for bad in (dict(type=3), dict(type=-1)):
+        assert call(**bad) == UNSUPPORTED
+    for bad in (dict(rows=1 << 32), dict(cols=1 << 31, x_stride=1 << 31)):
+        assert call(**bad) == TOO_LARGE
+    assert call(rows=0, x=None, out=None) == OK
+
+
+def _linear(**kw):
+    a = pc.pcsr_linear_t(10, 12, 14, 0, 0, 0, 0, P, P, None, None, 12, 12, 14, pc.pcsr_drop_t(0.0, 0, 0, None, None))
+    for k, v in kw.items():
+        if k == "p":
+            a.drop.p = v
+        else:
+            setattr(a, k, v)
+    return a
+
+
+def test_linear_entry_points():
+    lib = pc._lib()
+
+    def fwd(y=P, z=None, ws=P, **kw):
+        return lib.pcsr_linear(ctypes.byref(_linear(**kw)), y, z, ws, None)
+
+    def bwd(z=P, dy=P, stride=14, dx=P, dw=P, db=P, ws=P, **kw):
+        return lib.pcsr_linear_backward(ctypes.byref(_linear(**kw)), z, dy, stride, dx, dw, db, ws, None)
+
+    for call in (fwd, bwd):
+        for bad in (dict(rows=-1), {"in": -1}, dict(out=0), dict(x_stride=11), dict(w_stride=11), dict(x=None), dict(w=None), dict(p=2.0),
+                    dict(p=float("nan"))):
+            assert call(**bad) == INVALID, bad
+        for bad in (dict(type=3), dict(type=-1), dict(act=4), dict(act=-1), dict(bias_type=1), dict(type=1, bias_type=2)):
+            assert call(**bad) == UNSUPPORTED, bad
+        # tiles of 64 x 64 past 2^23: 2^18 rows of 2^17 and more, and rows and columns past 32 bits
+        for bad in (dict(rows=(1 << 18) + 1, out=1 << 17), dict(rows=1 << 32), dict(out=1 << 31), {"in": 1 << 31, "x_stride": 1 << 31, "w_stride": 1 << 31},
+                    {"out": 1 << 20, "in": 1 << 20, "x_stride": 1 << 20, "w_stride": 1 << 20}):
+            assert call(**bad) == TOO_LARGE, bad
+    assert fwd(y=None) == INVALID and fwd(residual=P, r_stride=13) == INVALID and fwd(rows=0, y=None, x=None) == OK
+    assert bwd(dy=None) == INVALID and bwd(stride=13) == INVALID and bwd(ws=None) == INVALID and bwd(act=2, z=None) == INVALID
+    assert bwd(dx=None, dw=None, db=None) == OK and bwd(rows=0, dy=None) == OK
+    deep = _linear(**{"in": 100_000, "x_stride": 100_000, "w_stride": 100_000})
+    assert lib.pcsr_linear_workspace(ctypes.byref(deep), 0) > 0 and lib.pcsr_linear(ctypes.byref(deep), P, None, None, None) == INVALID
+    assert lib.pcsr_linear_workspace(None, 0) == 0 and lib.pcsr_linear(None, P, None, P, None) == INVALID
+
+
+def test_host_tensors_are_refused():
+    from paper_2605_15695_amd.dropout import Dropout, dropout
+    from paper_2605_15695_amd.linear import FeedForward, Linear, linear
+
+    X = torch.zeros(3, 4)
+    with pytest.raises(ValueError):
+        dropout(X, 0.5, 1)
+    with pytest.raises(ValueError):
+        Dropout(0.5)(X)
+    with pytest.raises(ValueError):
+        linear(X, torch.zeros(5, 4))
+    with pytest.raises(ValueError):
+        Linear(4, 5)(X)
+    with pytest.raises(ValueError):
+        FeedForward(4, 5)(X)
+    for p in (-0.5, 1.5, float("nan")):
+        with pytest.raises(ValueError):
+            Dropout(p)
+        with pytest.raises(ValueError):
+            Linear(4, 5, p=p)
+    for seed in (1 << 64, -(1 << 63) - 1, 0.5):
+        with pytest.raises(ValueError):
+            Dropout(0.5, seed=seed)
+    assert Dropout(0.5, seed=(1 << 64) - 1).counter.tolist() == [-1, 0]
+
+
+def test_modules_keep_what_they_are_given():
+    from paper_2605_15695_amd.dropout import Dropout
+    from paper_2605_15695_amd.linear import FeedForward, Linear
+
+    torch.manual_seed(1)
+    a, b = Dropout(0.5), Dropout(0.5)
+    torch.manual_seed(1)
+    c = Dropout(0.5)
+    assert a.counter.tolist() == c.counter.tolist() != b.counter.tolist()
+    assert a(X := torch.ones(2, 2)) is X if not a.train(False).training else False
+    assert set(Linear(3, 4).state_dict()) == {"weight", "bias"} and set(Linear(3, 4, False, p=0.1).state_dict()) == {"weight", "counter"}
+    block = FeedForward(3, 8, "silu", 0.1)
+    assert block.first.activation == "silu" and block.second.weight.shape == (3, 8)
