@@ -65,5 +65,35 @@ template <int N> __device__ __forceinline__ void slopes(float (&z)[N], int act)
     }
 }
 
+// both: z becomes the activation, s its slope
+template <int N> __device__ __forceinline__ void activate(float (&z)[N], float (&s)[N], int act)
+{
+    switch (act) {
+    case PCSR_ACT_RELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i] = z[i] > 0.0f ? 1.0f : z[i] <= 0.0f ? 0.0f : z[i];
+            z[i] = z[i] < 0.0f ? 0.0f : z[i];
+        }
+        break;
+    case PCSR_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-z[i]));
+            s[i] = p * (1.0f + z[i] * (1.0f - p));
+            z[i] *= p;
+        }
+        break;
+    case PCSR_ACT_GELU:
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float bell = __expf(-0.5f * z[i] * z[i]), p = below_normal(z[i], bell);
+            s[i] = p + z[i] * 0.39894228f * bell;
+            z[i] *= p;
+        }
+        break;
+    }
+}
+
 } // namespace
 } // namespace pcsr

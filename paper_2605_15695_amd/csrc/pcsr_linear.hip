@@ -64,19 +64,25 @@ template <typename T, bool TURN> __device__ __forceinline__ float number(const S
 // ---------------------------------------------------------------------------------- what follows a product
 struct Tail {
     const void *bias, *residual;
-    void *y, *z;
-    int64_t r_stride, rows, cols; // of y, whose rows lie one behind the other
-    int act, bias_type, z_type;   // z: PCSR_F32 or PCSR_F16
+    void *y, *slope;              // slope: null, or act'(z) as the backward pass reads it
+    int64_t r_stride, rows, cols; // of y and slope, whose rows lie one behind the other
+    int act, bias_type;
     Drop drop;
 };
 
-// a number of which the slope will be taken, in fp16: cut at the range's ends, where slopes no longer change, and never 0 if it is none
-__device__ __forceinline__ half_t slope_place(float z)
-{
-    half_t h = (half_t)(z > 65504.0f ? 65504.0f : z < -65504.0f ? -65504.0f : z);
-    if (h == (half_t)0.0f && z != 0.0f) h = (half_t)__builtin_copysignf(5.9604645e-8f, z); // the smallest there is
-    return h;
-}
+// Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 of them to 1 (0 and 1 are exact, others are 2^-16 off at
+// most, a 32nd of what fp16 rounds gradients of their size by; slopes are between -0.13 and 1.13).  Kept in place of z: a slope costs three
+// operations beside the activation and forty apart from it.
+template <typename T> struct Slope {
+    typedef uint16_t type;
+    static __device__ __forceinline__ uint16_t put(float s) { return s == s ? (uint16_t)__builtin_fmaf(s, 32768.0f, 8192.5f) : 65535; }
+    static __device__ __forceinline__ float take(uint16_t q) { return q == 65535 ? __builtin_nanf("") : (float)((int)q - 8192) * (1.0f / 32768.0f); }
+};
+template <> struct Slope<float> {
+    typedef float type;
+    static __device__ __forceinline__ float put(float s) { return s; }
+    static __device__ __forceinline__ float take(float s) { return s; }
+};
 
 // 8 numbers of x w^T, m of them there, at a row and a column that is a multiple of 8
 template <typename T> __device__ __forceinline__ void put8(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8])
@@ -88,24 +94,24 @@ template <typename T> __device__ __forceinline__ void put8(const Tail &a, const 
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += b[i];
     }
-    if (a.z) {
-        if (a.z_type == PCSR_F32) {
-            store_upto<float, 8>(static_cast<float *>(a.z) + row * a.cols + c, m, v);
+    if (a.slope) {
+        typedef typename Slope<T>::type S;
+        float f[8];
+        activate(v, f, a.act);
+        S *to = static_cast<S *>(a.slope) + row * a.cols + c;
+        typename Pack<S, 8>::type q;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = Slope<T>::put(f[i]);
+        if (m >= 8) {
+            *reinterpret_cast<typename Pack<S, 8>::type *>(to) = q;
         } else {
-            half_t *to = static_cast<half_t *>(a.z) + row * a.cols + c;
-            typename Pack<half_t, 8>::type h;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = slope_place(v[i]);
-            if (m >= 8) {
-                *reinterpret_cast<typename Pack<half_t, 8>::type *>(to) = h;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < m) to[i] = h[i];
-            }
+            for (int i = 0; i < 8; ++i)
+                if (i < m) to[i] = q[i];
         }
+    } else {
+        activate(v, a.act);
     }
-    activate(v, a.act);
     if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, v);
     if (a.residual) {
         float r[8];
@@ -231,7 +237,7 @@ template <typename T, bool TURN, int R, int THREADS> struct Loader {
 struct TileArgs {
     Side p, q;
     int64_t K, stretch; // stretch: of k, for a workgroup
-    int tiles_i, tiles_j;
+    int tiles_i, tiles_j, stretches;
     float *part; // [stretch][rows][cols] sums, null: whole sums, for `tail`
     Tail tail;
 };
@@ -241,7 +247,19 @@ template <int BI_, int BJ_, int WI_, int WJ_> struct Tiling {
 };
 typedef Tiling<128, 128, 2, 2> Wide;
 typedef Tiling<128, 64, 2, 2> Tall;
+typedef Tiling<64, 128, 2, 2> Flat;
 typedef Tiling<64, 64, 2, 2> Small;
+
+// A workgroup's tile and stretch of k.  Workgroups are dealt to the 8 dies one by one, each with an L2 of its own: a die takes the tiles of a
+// stretch one after the other, and of whole sums tiles that lie together.
+__device__ __forceinline__ void place_of(const TileArgs &a, int *ti, int *tj, int *stretch)
+{
+    const int tiles = a.tiles_i * a.tiles_j, all = tiles * a.stretches, per = all / 8, b = blockIdx.x;
+    const int t = b < per * 8 ? (b & 7) * per + (b >> 3) : b;
+    *stretch = t / tiles;
+    const int r = t - *stretch * tiles;
+    *ti = r / a.tiles_j, *tj = r - *ti * a.tiles_j;
+}
 
 template <typename T, typename C> constexpr int lds_bytes()
 {
@@ -257,9 +275,10 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     __shared__ __align__(16) char lds[lds_bytes<T, C>()];
     __shared__ int met;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
-    const int tile = blockIdx.x, ti = tile / a.tiles_j, tj = tile - ti * a.tiles_j;
+    int ti, tj, stretch;
+    place_of(a, &ti, &tj, &stretch);
     const int64_t i0 = (int64_t)ti * C::BI, j0 = (int64_t)tj * C::BJ;
-    const int64_t k0 = blockIdx.y * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
+    const int64_t k0 = (int64_t)stretch * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
     if (tid == 0) met = 0;
     f4 sum[FI][FJ];
 #pragma unroll
@@ -326,7 +345,7 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     DropKey key = {};
     if (!a.part && a.tail.drop.threshold) {
         key = key_of(a.tail.drop);
-        if (tile == 0 && tid == 0) tell_key(a.tail.drop, key);
+        if (blockIdx.x == 0 && tid == 0) tell_key(a.tail.drop, key);
     }
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
@@ -357,7 +376,7 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
                         for (int64_t k = k0; k < k1; ++k) v[e] = __builtin_fmaf(number<T, TP>(a.p, row, k), number<T, TQ>(a.q, col + e, k), v[e]);
                 }
             }
-            if (a.part) store_upto<float, 8>(a.part + (blockIdx.y * a.tail.rows + row) * a.tail.cols + col, m, v);
+            if (a.part) store_upto<float, 8>(a.part + (stretch * a.tail.rows + row) * a.tail.cols + col, m, v);
             else put8<T>(a.tail, key, row, col, m, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -365,89 +384,111 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     }
 }
 
-// sums of the stretches of k, in their order, and what follows
-template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(const float *part, int stretches, Tail a, uint32_t groups)
+// Sums of the stretches of k and what follows.  A workgroup takes `across` places of 8 columns; of its threads kT / across share a place and take
+// every so-manieth stretch each, and their sums are added up in order.
+template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(const float *part, int stretches, Tail a, uint32_t groups, int across)
 {
-    const int64_t t = (int64_t)blockIdx.x * kT + threadIdx.x, row = t / groups, c = (t - row * groups) * 8;
+    __shared__ float sums[kT][9];
+    const int lane = threadIdx.x % across, q = threadIdx.x / across, beside = kT / across;
+    const int64_t t = (int64_t)blockIdx.x * across + lane, row = t / groups, c = (t - row * groups) * 8;
     DropKey key = {};
     if (a.drop.threshold) {
         key = key_of(a.drop);
-        if (t == 0) tell_key(a.drop, key);
+        if (t == 0 && q == 0) tell_key(a.drop, key);
     }
-    if (row >= a.rows) return;
     const int m = a.cols - c < 8 ? (int)(a.cols - c) : 8;
     float v[8] = {};
-    for (int s = 0; s < stretches; ++s) {
-        float x[8];
-        load_upto<float, 8>(part + (s * a.rows + row) * a.cols + c, m, x);
+    if (row < a.rows)
+#pragma unroll 4
+        for (int s = q; s < stretches; s += beside) {
+            float x[8];
+            load_upto<float, 8>(part + (s * a.rows + row) * a.cols + c, m, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += x[i];
+            for (int i = 0; i < 8; ++i) v[i] += x[i];
+        }
+    if (beside > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = v[i];
+        __syncthreads();
+        if (q) return;
+        for (int p = 1; p < beside; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += sums[p * across + lane][i];
     }
-    put8<T>(a, key, row, c, m, v);
+    if (row < a.rows) put8<T>(a, key, row, c, m, v);
 }
 
 // ---------------------------------------------------------------------------------- gradient at z
 struct SlopeArgs {
-    const void *dy, *z;
+    const void *dy, *slope;
     int64_t dy_stride, rows, cols, ld; // ld: of dz
     void *dz;                          // null: sums alone
     float *sums;                       // [workgroup][cols], null: none
-    int act, z_type, lanes;            // lanes: to a row
+    int lanes;                         // to a row
     int64_t chunk;                     // rows of a workgroup
     Drop drop;
 };
+constexpr int kSlopeT = 1024, kSlopeBlocks = 512; // two workgroups a compute unit: as many sums as sums_kernel adds up in 6 us
 
 // dz = f act'(z) dy, and sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows.
-template <typename T> __global__ void __launch_bounds__(kT) slope_kernel(SlopeArgs a)
+template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(SlopeArgs a)
 {
-    __shared__ float part[kT][8];
-    const int lane = threadIdx.x % a.lanes, r = threadIdx.x / a.lanes, per = kT / a.lanes;
+    typedef typename Slope<T>::type S;
+    __shared__ float part[kSlopeT][9];
+    const int lane = threadIdx.x % a.lanes, r = threadIdx.x / a.lanes, per = kSlopeT / a.lanes;
     const int64_t c = ((int64_t)blockIdx.y * a.lanes + lane) * 8, first = blockIdx.x * a.chunk, end = first + a.chunk < a.rows ? first + a.chunk : a.rows;
     const int m = a.cols - c >= 8 ? 8 : a.cols > c ? (int)(a.cols - c) : 0;
-    const DropKey key = key_of(a.drop);
+    DropKey key = {};
+    if (a.drop.threshold) key = key_of(a.drop);
     float sum[8] = {};
     if (m > 0)
+#pragma unroll 2
         for (int64_t row = first + r; row < end; row += per) {
-            float d[8], z[8];
+            float d[8];
             load_upto<T, 8>(static_cast<const T *>(a.dy) + row * a.dy_stride + c, m, d);
-            if (a.act != PCSR_ACT_NONE) {
-                if (a.z_type == PCSR_F32) load_upto<float, 8>(static_cast<const float *>(a.z) + row * a.cols + c, m, z);
-                else load_upto<half_t, 8>(static_cast<const half_t *>(a.z) + row * a.cols + c, m, z);
-                slopes(z, a.act);
+            if (a.slope) {
+                const S *at = static_cast<const S *>(a.slope) + row * a.cols + c;
+                typename Pack<S, 8>::type q;
+                if (m >= 8) {
+                    q = *reinterpret_cast<const typename Pack<S, 8>::type *>(at);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[i] = i < m ? at[i] : (S)0;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= Slope<T>::take(q[i]);
             }
             if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (a.act != PCSR_ACT_NONE) d[i] *= z[i];
-                if (i >= m) d[i] = 0.0f;
-                sum[i] += d[i];
-            }
+            for (int i = 0; i < 8; ++i) sum[i] += d[i]; // (behind the end 0 times something)
             if (a.dz) store_upto<T, 8>(static_cast<T *>(a.dz) + row * a.ld + c, m, d);
         }
     if (!a.sums) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[threadIdx.x][i] = sum[i];
     __syncthreads();
-    for (int t = threadIdx.x; t < a.lanes * 8; t += kT) {
+    for (int t = threadIdx.x; t < a.lanes * 8; t += kSlopeT) {
         float s = 0.0f;
         for (int q = 0; q < per; ++q) s += part[q * a.lanes + t / 8][t % 8];
         const int64_t col = (int64_t)blockIdx.y * a.lanes * 8 + t;
         if (col < a.cols) a.sums[blockIdx.x * a.cols + col] = s;
     }
 }
-// db: a wavefront to a column would read one number of a line, so a thread adds up a column of 64 side by side, four stretches of workgroups beside one another
-__global__ void __launch_bounds__(kT) sums_kernel(const float *sums, int64_t blocks, int64_t cols, int type, void *db)
+// db: 16 columns to a workgroup, 64 threads to a column
+__global__ void __launch_bounds__(1024) sums_kernel(const float *sums, int64_t blocks, int64_t cols, int type, void *db)
 {
-    __shared__ double part[4][64];
-    const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ double part[64][17];
+    const int lane = threadIdx.x & 15, q = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + lane;
     double s = 0.0;
     if (c < cols)
-        for (int64_t b = q; b < blocks; b += 4) s += (double)sums[b * cols + c];
+#pragma unroll 8
+        for (int64_t b = q; b < blocks; b += 64) s += (double)sums[b * cols + c];
     part[q][lane] = s;
     __syncthreads();
     if (q || c >= cols) return;
-    const float v = (float)(part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane]);
+    for (int p = 1; p < 64; ++p) s += part[p][lane];
+    const float v = (float)s;
     if (type == PCSR_F32) static_cast<float *>(db)[c] = v;
     else if (type == PCSR_BF16) static_cast<bfloat_t *>(db)[c] = (bfloat_t)v;
     else static_cast<half_t *>(db)[c] = (half_t)v;
@@ -458,24 +499,25 @@ int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 int64_t round16(int64_t n) { return up(n, 16) * 16; }
 constexpr int64_t kMostTiles = int64_t(1) << 23;
 
-// how a product of I x J numbers over K is cut
+// How a product of I x J numbers over K is cut.  The widest tiles that the result fills; where they are too few for the chip k is cut into
+// stretches, whose sums go through memory, and where it is too short for that tiles are of 64 x 64.
 struct Plan {
     int which; // tiling
     int64_t tiles_i, tiles_j, stretch;
     int stretches;
-    int64_t bytes() const { return 0; }
 };
 template <typename T> Plan plan(int64_t I, int64_t J, int64_t K)
 {
+    constexpr int64_t kWanted = 512; // workgroups: two to a compute unit
+    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI}, BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ};
     Plan p;
-    const int BI[] = {Wide::BI, Tall::BI, Small::BI}, BJ[] = {Wide::BJ, Tall::BJ, Small::BJ};
-    p.which = J <= 64 ? 1 : 0;
-    if (up(I, 128) * up(J, 128) < 256) p.which = 2;
+    const int64_t stages = up(K, Num<T>::KS), most = stages / 4 < 1 ? 1 : stages / 4;
+    p.which = (I <= 64 ? 2 : 0) + (J <= 64 ? 1 : 0);
+    if (up(I, BI[p.which]) * up(J, BJ[p.which]) * most < 256) p.which = 3;
     p.tiles_i = up(I, BI[p.which]), p.tiles_j = up(J, BJ[p.which]);
-    const int64_t tiles = p.tiles_i * p.tiles_j, stages = up(K, Num<T>::KS);
-    int64_t s = tiles >= 512 ? 1 : 512 / (tiles ? tiles : 1);
-    if (s > stages / 4) s = stages / 4;
-    if (s < 1) s = 1;
+    const int64_t tiles = p.tiles_i * p.tiles_j;
+    int64_t s = tiles >= kWanted ? 1 : kWanted / (tiles ? tiles : 1);
+    if (s > most) s = most;
     p.stretch = up(stages, s) * Num<T>::KS;
     p.stretches = (int)(K ? up(K, p.stretch) : 1);
     return p;
@@ -485,16 +527,20 @@ int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1
 template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, const Tail &tail, void *ws, hipStream_t stream)
 {
     const Plan c = plan<T>(p.n, q.n, K);
-    TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
-    const dim3 grid((unsigned)(c.tiles_i * c.tiles_j), (unsigned)c.stretches);
+    TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
+    const dim3 grid((unsigned)(c.tiles_i * c.tiles_j * c.stretches));
     switch (c.which) {
     case 0: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Wide>), grid, dim3(Wide::threads), 0, stream, a); break;
     case 1: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Tall>), grid, dim3(Tall::threads), 0, stream, a); break;
+    case 2: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Flat>), grid, dim3(Flat::threads), 0, stream, a); break;
     default: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Small>), grid, dim3(Small::threads), 0, stream, a);
     }
     if (c.stretches > 1) {
         const uint32_t groups = (uint32_t)up(tail.cols, 8);
-        hipLaunchKernelGGL(finish_kernel<T>, dim3((unsigned)up(tail.rows * groups, kT)), dim3(kT), 0, stream, a.part, c.stretches, tail, groups);
+        const int64_t places = tail.rows * groups;
+        int across = kT;
+        while (across > 8 && places / across < 512 && kT / across * 4 < c.stretches) across /= 2;
+        hipLaunchKernelGGL(finish_kernel<T>, dim3((unsigned)up(places, across)), dim3(kT), 0, stream, a.part, c.stretches, tail, groups, across);
     }
     return launched();
 }
@@ -510,9 +556,8 @@ struct Space {
         s.ld = up(a.out, 8) * 8;
         s.lanes = 1;
         while (s.lanes < 64 && s.lanes * 8 < a.out) s.lanes *= 2;
-        const int64_t beside = up(a.out, s.lanes * 8), per = kT / s.lanes;
-        int64_t most = up(2048, beside);
-        if (most < 64) most = 64;
+        const int64_t beside = up(a.out, s.lanes * 8), per = kSlopeT / s.lanes;
+        const int64_t most = beside < kSlopeBlocks ? kSlopeBlocks / beside : 1;
         s.chunk = up(up(a.rows, most), per) * per;
         s.blocks = up(a.rows, s.chunk);
         s.dz = own ? round16(a.rows * s.ld * (int64_t)sizeof(T)) : 0;
@@ -557,27 +602,26 @@ int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward)
     return need;
 }
 
-int pcsr_linear(const pcsr_linear_t *a, void *y, void *z, void *ws, void *stream)
+int pcsr_linear(const pcsr_linear_t *a, void *y, void *slope, void *ws, void *stream)
 {
     if (const int rc = check(a)) return rc;
     if (a->rows == 0) return PCSR_OK;
     if (!y || (a->in > 0 && (!a->x || !a->w)) || (a->residual && a->r_stride < a->out)) return PCSR_E_INVALID_ARG;
     if (!ws && pcsr_linear_workspace(a, 0)) return PCSR_E_INVALID_ARG;
-    const Tail tail = {a->bias, a->residual, y, z, a->r_stride, a->rows, a->out, a->act, a->bias_type, a->type == PCSR_F32 ? PCSR_F32 : PCSR_F16,
-                       drop_of(&a->drop)};
+    const Tail tail = {a->bias, a->residual, y, a->act == PCSR_ACT_NONE ? nullptr : slope, a->r_stride, a->rows, a->out, a->act, a->bias_type, drop_of(&a->drop)};
     return for_type(a->type, [&](auto t) {
         typedef decltype(t) T;
         return product<T, false, false>({a->x, a->x_stride, a->rows}, {a->w, a->w_stride, a->out}, a->in, tail, ws, (hipStream_t)stream);
     });
 }
 
-int pcsr_linear_backward(const pcsr_linear_t *a, const void *z, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws,
+int pcsr_linear_backward(const pcsr_linear_t *a, const void *slope, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws,
                          void *stream_)
 {
     if (const int rc = check(a)) return rc;
     if (a->rows == 0 || (!dx && !dw && !db)) return PCSR_OK;
     const hipStream_t stream = (hipStream_t)stream_;
-    if (!dy || dy_stride < a->out || (a->act != PCSR_ACT_NONE && !z) || (dx && !a->w) || (dw && !a->x) || !ws) return PCSR_E_INVALID_ARG;
+    if (!dy || dy_stride < a->out || (a->act != PCSR_ACT_NONE && !slope) || (dx && !a->w) || (dw && !a->x) || !ws) return PCSR_E_INVALID_ARG;
     return for_type(a->type, [&](auto t) -> int {
         typedef decltype(t) T;
         const bool own = has_slope(*a);
@@ -588,20 +632,20 @@ int pcsr_linear_backward(const pcsr_linear_t *a, const void *z, const void *dy, 
         Side dz = {dy, dy_stride, a->rows};
         const Drop drop = drop_of(&a->drop);
         if (own || db) {
-            SlopeArgs s = {dy, z, dy_stride, a->rows, a->out, sp.ld, own && (dx || dw) ? at : nullptr, db ? sums : nullptr, a->act,
-                           a->type == PCSR_F32 ? PCSR_F32 : PCSR_F16, sp.lanes, sp.chunk, drop};
-            hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)sp.blocks, (unsigned)up(a->out, sp.lanes * 8)), dim3(kT), 0, stream, s);
+            SlopeArgs s = {dy, a->act == PCSR_ACT_NONE ? nullptr : slope, dy_stride, a->rows, a->out, sp.ld, own && (dx || dw) ? at : nullptr,
+                           db ? sums : nullptr, sp.lanes, sp.chunk, drop};
+            hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)sp.blocks, (unsigned)up(a->out, sp.lanes * 8)), dim3(kSlopeT), 0, stream, s);
             if (db)
-                hipLaunchKernelGGL(sums_kernel, dim3((unsigned)up(a->out, 64)), dim3(kT), 0, stream, sums, sp.blocks, a->out, a->bias_type, db);
+                hipLaunchKernelGGL(sums_kernel, dim3((unsigned)up(a->out, 16)), dim3(1024), 0, stream, sums, sp.blocks, a->out, a->bias_type, db);
             if (own) dz = {at, sp.ld, a->rows};
         }
         int rc = launched();
         if (dx && a->in > 0 && rc == PCSR_OK) {
-            const Tail tail = {nullptr, nullptr, dx, nullptr, 0, a->rows, a->in, PCSR_ACT_NONE, PCSR_F32, PCSR_F32, drop_of(nullptr)};
+            const Tail tail = {nullptr, nullptr, dx, nullptr, 0, a->rows, a->in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
             rc = product<T, false, true>(dz, {a->w, a->w_stride, a->in}, a->out, tail, part, stream);
         }
         if (dw && a->in > 0 && rc == PCSR_OK) {
-            const Tail tail = {nullptr, nullptr, dw, nullptr, 0, a->out, a->in, PCSR_ACT_NONE, PCSR_F32, PCSR_F32, drop_of(nullptr)};
+            const Tail tail = {nullptr, nullptr, dw, nullptr, 0, a->out, a->in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
             rc = product<T, true, true>({dz.at, dz.ld, a->out}, {a->x, a->x_stride, a->in}, a->rows, tail, part, stream);
         }
         return rc;

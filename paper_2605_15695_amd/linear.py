@@ -23,7 +23,8 @@ def linear(X: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     float32.  activation: none, relu, silu or gelu (by erf).  p, seed, offset: see dropout; p = 0 drops nothing.
     Products of 16-bit numbers are summed in float32; those of float32 numbers are taken of three bf16 numbers each, 24 bits, and summed in
     float32 (where numbers of 2^38 and more are met, in float32 throughout, which is slow).  What follows is computed in float32 and rounded once.
-    Backward, activations' slopes are taken of X @ weight.T + bias in float32, for 16-bit types in float16, and the gradient at it has X's type.
+    The activation's slopes are kept for the backward pass, in float32 or, for 16-bit types, as 16 bits that are 2^-16 off at most; the gradient at
+    X @ weight.T + bias has X's type.
     Sums are in an order that sizes and type alone decide: the same bits on every run.
     PcsrError: 2^32 rows or 2^31 columns and more, and where X, weight or the result are of more than 2^23 tiles of 64 x 64.
     There is no forward-mode derivative."""
@@ -66,14 +67,14 @@ def _operands(X, weight):
 
 
 def _forward(X, weight, bias, residual, act, p, seed, offset, used, keep):
-    """(Y, what the slopes are taken of or None)"""
+    """(Y, the activation's slopes or None)"""
     out = weight.shape[0]
     Y = torch.empty((*X.shape[:-1], out), dtype=X.dtype, device=X.device)
     x, x_stride, w, w_stride = _operands(X, weight)
     keep = keep and act != 0
-    z = torch.empty((x.shape[0], out), dtype=torch.float32 if X.dtype == torch.float32 else torch.float16, device=X.device) if keep else None
+    slope = torch.empty((x.shape[0], out), dtype=torch.float32 if X.dtype == torch.float32 else torch.int16, device=X.device) if keep else None
     if Y.numel() == 0:
-        return Y, z
+        return Y, slope
     r, r_stride = (None, 0) if residual is None else rows_of(residual.detach())
     bias = None if bias is None else bias.detach().resolve_neg().contiguous()
     if isinstance(seed, torch.Tensor):
@@ -84,11 +85,11 @@ def _forward(X, weight, bias, residual, act, p, seed, offset, used, keep):
     need = lib.pcsr_linear_workspace(ctypes.byref(a), 0)
     ws = torch.empty(need, dtype=torch.uint8, device=X.device) if need else None
     with torch.cuda.device(X.device):
-        _check(lib.pcsr_linear(ctypes.byref(a), Y.data_ptr(), _p(z), _p(ws), torch.cuda.current_stream().cuda_stream), "pcsr_linear")
-    return Y, z
+        _check(lib.pcsr_linear(ctypes.byref(a), Y.data_ptr(), _p(slope), _p(ws), torch.cuda.current_stream().cuda_stream), "pcsr_linear")
+    return Y, slope
 
 
-def _backward(X, weight, bias_dtype, z, dy, act, p, seed, offset, needs):
+def _backward(X, weight, bias_dtype, slope, dy, act, p, seed, offset, needs):
     """(dX, dweight, dbias), None for what is not needed"""
     out = weight.shape[0]
     dx = torch.empty(X.shape, dtype=X.dtype, device=X.device) if needs[0] else None
@@ -102,7 +103,7 @@ def _backward(X, weight, bias_dtype, z, dy, act, p, seed, offset, needs):
     a = _struct(x, x_stride, w, w_stride, None, None, 0, act, X.dtype, out, drop_struct(p, seed, offset), _TYPES[bias_dtype])
     ws = torch.empty(lib.pcsr_linear_workspace(ctypes.byref(a), 1), dtype=torch.uint8, device=X.device)
     with torch.cuda.device(X.device):
-        _check(lib.pcsr_linear_backward(ctypes.byref(a), _p(z), g.data_ptr(), g_stride, _p(dx), _p(dw), _p(db), ws.data_ptr(),
+        _check(lib.pcsr_linear_backward(ctypes.byref(a), _p(slope), g.data_ptr(), g_stride, _p(dx), _p(dw), _p(db), ws.data_ptr(),
                                         torch.cuda.current_stream().cuda_stream), "pcsr_linear_backward")
     return dx, dw, db
 
@@ -111,8 +112,8 @@ class LinearFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, weight, bias, residual, act, p, seed, offset):
         used = used_for(seed, p)
-        Y, z = _forward(X, weight, bias, residual, act, p, seed, offset, used, any(ctx.needs_input_grad[:3]))
-        ctx.save_for_backward(X, weight, z, used)
+        Y, slope = _forward(X, weight, bias, residual, act, p, seed, offset, used, any(ctx.needs_input_grad[:3]))
+        ctx.save_for_backward(X, weight, slope, used)
         ctx.how = act, p, 0 if isinstance(seed, torch.Tensor) else seed, offset
         ctx.bias_dtype = X.dtype if bias is None else bias.dtype
         return Y
@@ -120,11 +121,11 @@ class LinearFunction(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        X, weight, z, used = ctx.saved_tensors
+        X, weight, slope, used = ctx.saved_tensors
         act, p, seed, offset = ctx.how
         grads = None, None, None
         if any(ctx.needs_input_grad[:3]):
-            grads = _backward(X, weight, ctx.bias_dtype, z, dy, act, p, seed if used is None else used, offset, ctx.needs_input_grad[:3])
+            grads = _backward(X, weight, ctx.bias_dtype, slope, dy, act, p, seed if used is None else used, offset, ctx.needs_input_grad[:3])
         return *grads, dy if ctx.needs_input_grad[3] else None, None, None, None, None
 
 
