@@ -323,13 +323,13 @@ _train = False  # not asked for yet
 
 
 def train_module():
-    """The module that makes the calls of embedding.py, norm.py and muon.py without ctypes, or None."""
+    """The module that makes the calls of embedding.py, norm.py, muon.py, dropout.py and linear.py without ctypes, or None."""
     global _train
     if _train is False:
         lib = _lib()
         _train = _load_module("_pcsr_train", TRAIN_PATH, [getattr(lib, "pcsr_" + n) for n in (
             "embed", "embed_workspace", "embed_backward", "norm", "norm_workspace", "norm_backward", "orthogonalize",
-            "ortho_workspace")], "calls of the training step")
+            "ortho_workspace", "dropout", "linear", "linear_workspace", "linear_backward")], "calls of the training step")
         if _train is not None:
             _train.raises(PcsrError)
     return _train

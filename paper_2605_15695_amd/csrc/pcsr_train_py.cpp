@@ -1,4 +1,4 @@
-// What embedding.py, norm.py and muon.py do for a call - check tensors, make outputs and workspaces, take addresses
+// What embedding.py, norm.py, muon.py, dropout.py and linear.py do for a call - check tensors, make outputs and workspaces, take addresses
 // and the stream, call, and leave a node for autograd - on the tensors' C++ objects.  A call on few rows is bound by the
 // host: of 13 us for the features of one node, and of 130 us for a step of ten small matrices, the kernels were 4 and 20.
 // Tensors that a call does not take as they are (other types, devices or strides, wrong arguments) are left to the Python
@@ -31,6 +31,10 @@ struct Library {
     decltype(&pcsr_norm_backward) norm_backward;
     decltype(&pcsr_orthogonalize) orthogonalize;
     decltype(&pcsr_ortho_workspace) ortho_workspace;
+    decltype(&pcsr_dropout) dropout;
+    decltype(&pcsr_linear) linear;
+    decltype(&pcsr_linear_workspace) linear_workspace;
+    decltype(&pcsr_linear_backward) linear_backward;
 } lib;
 bool ready = false;
 PyObject *error_type = PyExc_RuntimeError; // what a call of the library that returned an error raises, given the code and the call's name
@@ -327,6 +331,219 @@ PyObject *orthogonalize(PyObject *, PyObject *const *args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------------------------ dropout and linear layers
+struct DropCall {
+    double p = 0.0;
+    int64_t seed = 0, offset = 0;
+    at::Tensor state; // in their place
+
+    // from a call's arguments; false: Python's to look at
+    bool take(PyObject *prob, PyObject *s, PyObject *o, const at::Tensor &X)
+    {
+        if (!PyFloat_Check(prob)) return false;
+        p = PyFloat_AS_DOUBLE(prob);
+        if (!(p >= 0.0 && p <= 1.0)) return false;
+        if (THPVariable_Check(s)) {
+            state = THPVariable_Unpack(s);
+            return here(state) && state.device() == X.device() && state.scalar_type() == at::kLong && state.dim() == 1 && state.numel() == 2 && state.is_contiguous();
+        }
+        return word(s, seed) && word(o, offset);
+    }
+    static bool word(PyObject *v, int64_t &to)
+    {
+        if (!PyLong_CheckExact(v)) return false;
+        int over = 0;
+        to = PyLong_AsLongLongAndOverflow(v, &over);
+        if (!over) return true;
+        if (over < 0) return false;
+        to = (int64_t)PyLong_AsUnsignedLongLong(v);
+        if (!PyErr_Occurred()) return true;
+        PyErr_Clear();
+        return false;
+    }
+    // where a call that reads its seed on the GPU writes what it read, for the backward pass
+    at::Tensor used() const { return state.defined() && p > 0.0 ? at::empty({2}, state.options().requires_grad(false)) : at::Tensor(); }
+    pcsr_drop_t to_library(const at::Tensor &used) const
+    {
+        return {p, (uint64_t)seed, (uint64_t)offset, state.defined() ? state.const_data_ptr<int64_t>() : nullptr,
+                used.defined() ? used.mutable_data_ptr<int64_t>() : nullptr};
+    }
+    std::vector<int64_t> numbers() const
+    {
+        int64_t bits;
+        memcpy(&bits, &p, 8);
+        return {bits, seed, offset};
+    }
+    static DropCall of(const std::vector<int64_t> &n, const at::Tensor &used)
+    {
+        DropCall d;
+        memcpy(&d.p, &n[0], 8);
+        d.seed = n[1], d.offset = n[2], d.state = used;
+        return d;
+    }
+};
+at::Tensor rows(const at::Tensor &t) { return t.dim() == 2 ? t : t.reshape({-1, t.size(-1)}); }
+// whether the library takes the rows as they lie
+bool whole(const at::Tensor &t) { return t.dim() == 2 ? distance(t) >= 0 : t.is_contiguous(); }
+std::optional<at::Tensor> maybe(const at::Tensor &t) { return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt; }
+at::Tensor of(const std::optional<at::Tensor> &t) { return t.has_value() ? *t : at::Tensor(); }
+at::Tensor gradient_rows(const at::Tensor &grad, int64_t n, int64_t d)
+{
+    const at::Tensor g = grad.detach().resolve_neg().reshape({n, d});
+    return distance(g) < 0 ? g.contiguous() : g;
+}
+const void *address(const at::Tensor &t) { return t.defined() ? t.const_data_ptr() : nullptr; }
+
+at::Tensor dropout_forward(const at::Tensor &X, const at::Tensor &R, const DropCall &d, const at::Tensor &used)
+{
+    at::Tensor out = at::empty(X.sizes(), X.options().requires_grad(false));
+    const at::Tensor x = rows(X), r = R.defined() ? rows(R) : R;
+    const pcsr_drop_t how = d.to_library(used);
+    ok(lib.dropout(x.size(0), x.size(1), type_of(X), x.const_data_ptr(), distance(x), address(r), r.defined() ? distance(r) : 0, &how, out.data_ptr(), stream()),
+       "pcsr_dropout");
+    return out;
+}
+
+struct Dropout : torch::autograd::Function<Dropout> {
+    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &X, const std::optional<at::Tensor> &R, const std::optional<at::Tensor> &state,
+                              const std::vector<int64_t> &numbers)
+    {
+        const DropCall d = DropCall::of(numbers, of(state));
+        const at::Tensor used = d.used();
+        ctx->save_for_backward({used});
+        ctx->saved_data["how"] = numbers;
+        ctx->saved_data["residual"] = R.has_value();
+        return dropout_forward(X, of(R), d, used);
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const DropCall d = DropCall::of(ctx->saved_data["how"].toIntVector(), ctx->get_saved_variables()[0]);
+        at::Tensor dx;
+        if (ctx->needs_input_grad(0)) {
+            const at::Tensor &dy = grads[0];
+            const int64_t C = dy.size(-1);
+            dx = dropout_forward(gradient_rows(dy, dy.numel() / C, C), at::Tensor(), d, at::Tensor()).view(dy.sizes());
+        }
+        const bool both = ctx->saved_data["residual"].toBool() && ctx->needs_input_grad(1);
+        return once({dx, both ? grads[0] : at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+};
+
+// dropout(X, p, seed or tensor, offset, residual or None)
+PyObject *dropout(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 5 || !ready || !THPVariable_Check(args[0]) || (args[4] != Py_None && !THPVariable_Check(args[4]))) Py_RETURN_NOTIMPLEMENTED;
+    const at::Tensor &X = THPVariable_Unpack(args[0]);
+    at::Tensor R;
+    if (args[4] != Py_None) R = THPVariable_Unpack(args[4]);
+    DropCall d;
+    if (!here(X) || X.dim() < 1 || type_of(X) < 0 || X.numel() == 0 || !whole(X) || !d.take(args[1], args[2], args[3], X)) Py_RETURN_NOTIMPLEMENTED;
+    if (R.defined() && (!here(R) || R.scalar_type() != X.scalar_type() || R.sizes() != X.sizes() || !whole(R))) Py_RETURN_NOTIMPLEMENTED;
+    at::Tensor out;
+    {
+        pybind11::gil_scoped_release unlocked;
+        out = at::GradMode::is_enabled() && (records(X) || records(R)) ? Dropout::apply(X, maybe(R), maybe(d.state), d.numbers())
+                                                                      : dropout_forward(X, R, d, at::Tensor());
+    }
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+pcsr_linear_t linear_call(const at::Tensor &x, const at::Tensor &W, const at::Tensor &b, const at::Tensor &r, int64_t bias_type, int64_t act, const pcsr_drop_t &how)
+{
+    return {x.size(0), x.size(1), W.size(0), type_of(x), (int32_t)bias_type, (int32_t)act, 0, x.const_data_ptr(), W.const_data_ptr(), address(b), address(r),
+            distance(x), distance(W), r.defined() ? distance(r) : 0, how};
+}
+at::Tensor linear_forward(const at::Tensor &X, const at::Tensor &W, const at::Tensor &b, const at::Tensor &R, int64_t act, const DropCall &d, const at::Tensor &used,
+                          at::Tensor *slope)
+{
+    auto shape = X.sizes().vec();
+    shape.back() = W.size(0);
+    const auto options = X.options().requires_grad(false);
+    at::Tensor out = at::empty(shape, options), ws;
+    const at::Tensor x = rows(X);
+    if (slope && act != PCSR_ACT_NONE)
+        *slope = at::empty({x.size(0), W.size(0)}, options.dtype(X.scalar_type() == at::kFloat ? at::kFloat : at::kShort));
+    const pcsr_linear_t a = linear_call(x, W, b, R.defined() ? rows(R) : R, type_of(b.defined() ? b : X), act, d.to_library(used));
+    const int64_t need = lib.linear_workspace(&a, 0);
+    if (need) ws = bytes(need, X);
+    ok(lib.linear(&a, out.data_ptr(), slope && slope->defined() ? slope->data_ptr() : nullptr, need ? ws.data_ptr() : nullptr, stream()), "pcsr_linear");
+    return out;
+}
+
+struct Linear : torch::autograd::Function<Linear> {
+    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &X, const at::Tensor &W, const std::optional<at::Tensor> &b, const std::optional<at::Tensor> &R,
+                              const std::optional<at::Tensor> &state, int64_t act, const std::vector<int64_t> &numbers)
+    {
+        const DropCall d = DropCall::of(numbers, of(state));
+        const at::Tensor used = d.used();
+        at::Tensor slope;
+        const bool keep = records(X) || records(W) || (b.has_value() && records(*b));
+        at::Tensor out = linear_forward(X, W, of(b), of(R), act, d, used, keep ? &slope : nullptr);
+        ctx->save_for_backward({X, W, slope, used});
+        std::vector<int64_t> how = numbers;
+        how.insert(how.end(), {act, b.has_value() ? type_of(*b) : -1, R.has_value()});
+        ctx->saved_data["how"] = std::move(how);
+        return out;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        const variable_list saved = ctx->get_saved_variables();
+        const std::vector<int64_t> how = ctx->saved_data["how"].toIntVector();
+        const DropCall d = DropCall::of(how, saved[3]);
+        const at::Tensor X = saved[0].detach(), W = saved[1].detach();
+        const int64_t act = how[3], bias = how[4];
+        size_t at = 2; // (tensors that are not there are not counted)
+        const bool need_b = bias >= 0 && ctx->needs_input_grad(at++), need_r = how[5] && ctx->needs_input_grad(at++);
+        at::Tensor dx, dw, db;
+        if (ctx->needs_input_grad(0)) dx = at::empty(X.sizes(), X.options());
+        if (ctx->needs_input_grad(1)) dw = at::empty(W.sizes(), X.options());
+        if (need_b) db = at::empty({W.size(0)}, X.options().dtype(bias == PCSR_F32 ? at::kFloat : X.scalar_type()));
+        if (dx.defined() || dw.defined() || db.defined()) {
+            const at::Tensor x = rows(X), g = gradient_rows(grads[0], x.size(0), W.size(0));
+            const pcsr_linear_t a = linear_call(x, W, at::Tensor(), at::Tensor(), bias < 0 ? type_of(X) : bias, act, d.to_library(at::Tensor()));
+            const at::Tensor ws = bytes(lib.linear_workspace(&a, 1), X);
+            auto ptr = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+            ok(lib.linear_backward(&a, address(saved[2]), g.const_data_ptr(), distance(g), ptr(dx), ptr(dw), ptr(db), ws.data_ptr(), stream()), "pcsr_linear_backward");
+        }
+        return once({dx, dw, db, need_r ? grads[0] : at::Tensor(), at::Tensor(), at::Tensor(), at::Tensor()});
+    }
+};
+
+// linear(X, weight, bias or None, activation's number, residual or None, p, seed or tensor, offset)
+PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8 || !ready || !THPVariable_Check(args[0]) || !THPVariable_Check(args[1]) || !PyLong_Check(args[3])) Py_RETURN_NOTIMPLEMENTED;
+    const at::Tensor &X = THPVariable_Unpack(args[0]), &W = THPVariable_Unpack(args[1]);
+    at::Tensor b, R;
+    for (const int k : {2, 4}) {
+        if (args[k] == Py_None) continue;
+        if (!THPVariable_Check(args[k])) Py_RETURN_NOTIMPLEMENTED;
+        (k == 2 ? b : R) = THPVariable_Unpack(args[k]);
+    }
+    const int64_t act = PyLong_AsLongLong(args[3]);
+    DropCall d;
+    if (!here(X) || X.dim() < 1 || type_of(X) < 0 || X.numel() == 0 || !whole(X) || !d.take(args[5], args[6], args[7], X)) Py_RETURN_NOTIMPLEMENTED;
+    if (!here(W) || W.dim() != 2 || W.scalar_type() != X.scalar_type() || W.size(0) < 1 || W.size(1) != X.size(-1) || distance(W) < 0) Py_RETURN_NOTIMPLEMENTED;
+    if (b.defined() && (!here(b) || b.dim() != 1 || b.numel() != W.size(0) || !b.is_contiguous() || (b.scalar_type() != at::kFloat && b.scalar_type() != X.scalar_type())))
+        Py_RETURN_NOTIMPLEMENTED;
+    if (R.defined() && (!here(R) || R.scalar_type() != X.scalar_type() || R.dim() != X.dim() || R.size(-1) != W.size(0) ||
+                        R.sizes().slice(0, (size_t)R.dim() - 1) != X.sizes().slice(0, (size_t)X.dim() - 1) || !whole(R)))
+        Py_RETURN_NOTIMPLEMENTED;
+    at::Tensor out;
+    {
+        pybind11::gil_scoped_release unlocked;
+        if (at::GradMode::is_enabled() && (records(X) || records(W) || records(b) || records(R)))
+            out = Linear::apply(X, W, maybe(b), maybe(R), maybe(d.state), act, d.numbers());
+        else
+            out = linear_forward(X, W, b, R, act, d, at::Tensor(), nullptr);
+    }
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
 // init(addresses of the library's functions, in the order of Library)
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -363,7 +580,8 @@ template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)> PyMethodDef
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(F)), METH_FASTCALL, nullptr};
 }
 PyMethodDef methods[] = {method<embed>("embed"),   method<group_norm>("group_norm"), method<orthogonalize>("orthogonalize"),
-                         method<update>("update"), method<init>("init"),             method<raises>("raises"),
+                         method<update>("update"), method<dropout>("dropout"),       method<linear>("linear"),
+                         method<init>("init"),     method<raises>("raises"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pcsr_train", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

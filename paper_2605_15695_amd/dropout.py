@@ -28,6 +28,11 @@ def dropout(X: torch.Tensor, p: float, seed, offset: int = 0, residual: torch.Te
     half first; a number is dropped where they are below T = round(65536 p), and the others are multiplied by 65536 / (65536 - T).
     Dropped numbers count as zeros whatever they are, and so do their gradients.  X: any shape and strides, of fewer than 2^32 rows and 2^31 columns (PcsrError);
     residual: X's shape and type.  There is no forward-mode derivative."""
+    fast = pc.train_module()
+    if fast is not None:
+        out = fast.dropout(X, p, seed, offset, residual)
+        if out is not NotImplemented:
+            return out
     _check_tensor(X, "X")
     if residual is not None and (not isinstance(residual, torch.Tensor) or residual.shape != X.shape or residual.dtype != X.dtype
                                  or residual.device != X.device):

@@ -28,6 +28,11 @@ def linear(X: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     Sums are in an order that sizes and type alone decide: the same bits on every run.
     PcsrError: 2^32 rows or 2^31 columns and more, and where X, weight or the result are of more than 2^23 tiles of 64 x 64.
     There is no forward-mode derivative."""
+    fast = pc.train_module()
+    if fast is not None and activation in ACTIVATIONS:
+        out = fast.linear(X, weight, bias, ACTIVATIONS[activation], residual, p, seed, offset)
+        if out is not NotImplemented:
+            return out
     if not isinstance(X, torch.Tensor) or X.dim() < 1 or X.dtype not in _TYPES or not X.is_cuda:
         raise ValueError("X must be a float32, bfloat16 or float16 CUDA tensor of one dimension or more")
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2 or weight.dtype != X.dtype or weight.device != X.device \
