@@ -242,31 +242,95 @@ struct TileArgs {
     Tail tail;
 };
 
-template <int BI_, int BJ_, int WI_, int WJ_> struct Tiling {
-    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, threads = 64 * WI * WJ, FI = BI / 16 / WI, FJ = BJ / 16 / WJ;
+template <int BI_, int BJ_, int WI_, int WJ_, int PER_ = 1> struct Tiling { // PER: wavefronts to a SIMD at least
+    static constexpr int per = PER_, BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, threads = 64 * WI * WJ, FI = BI / 16 / WI, FJ = BJ / 16 / WJ;
 };
 typedef Tiling<128, 128, 2, 2> Wide;
 typedef Tiling<128, 64, 2, 2> Tall;
 typedef Tiling<64, 128, 2, 2> Flat;
 typedef Tiling<64, 64, 2, 2> Small;
+typedef Tiling<256, 256, 2, 4, 2> Large;
+typedef Tiling<128, 128, 2, 2, 2> StraightWide;
+typedef Tiling<128, 64, 2, 2, 2> StraightTall;
+typedef Tiling<64, 128, 2, 2, 2> StraightFlat;
 
-// A workgroup's tile and stretch of k.  Workgroups are dealt to the 8 dies one by one, each with an L2 of its own: a die takes the tiles of a
-// stretch one after the other, and of whole sums tiles that lie together.
+// A workgroup's tile and stretch of k.  Workgroups are dealt to the 8 dies one by one, each with an L2 of its own: a die takes a run of tiles in
+// blocks of four rows (32 of them read 12 strips of operands, side by side in one row 33), and the tiles of a stretch one after the other.
 __device__ __forceinline__ void place_of(const TileArgs &a, int *ti, int *tj, int *stretch)
 {
     const int tiles = a.tiles_i * a.tiles_j, all = tiles * a.stretches, per = all / 8, b = blockIdx.x;
     const int t = b < per * 8 ? (b & 7) * per + (b >> 3) : b;
     *stretch = t / tiles;
-    const int r = t - *stretch * tiles;
-    *ti = r / a.tiles_j, *tj = r - *ti * a.tiles_j;
+    const int r = t - *stretch * tiles, block = r / (4 * a.tiles_j), in = r - block * 4 * a.tiles_j, n = a.tiles_i - block * 4 < 4 ? a.tiles_i - block * 4 : 4;
+    *tj = in / n, *ti = block * 4 + in - *tj * n;
+}
+
+
+template <typename C> using Sums = f4[C::FI][C::FJ];
+
+// What becomes of a tile's sums.  They go through LDS, G times 16 rows of a wavefront at a time, so that a lane has 8 columns side by side: whole lines
+// of y, and what one call of the generator is for.  again: the numbers are added up once more, in fp32.
+template <typename C, int G> constexpr int out_bytes() { return C::WI * C::WJ * G * 16 * (C::FJ * 16 + 4) * 4; }
+template <typename T, bool TP, bool TQ, typename C, int G>
+__device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &sum, char *lds, int64_t i0, int64_t j0, int64_t k0, int64_t k1, int stretch, bool again)
+{
+    constexpr int FI = C::FI, FJ = C::FJ, NP = Num<T>::NP, LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
+    static_assert(FI % G == 0, "whole passes");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / C::WJ, wj = wave % C::WJ, at = lane & 15, chunk = lane >> 4;
+    float *own = reinterpret_cast<float *>(lds) + wave * G * 16 * LD;
+    DropKey key = {};
+    if (!a.part && a.tail.drop.threshold) {
+        key = key_of(a.tail.drop);
+        if (blockIdx.x == 0 && threadIdx.x == 0) tell_key(a.tail.drop, key);
+    }
+    const int c = lane % per * 8;
+    const int64_t col = j0 + wj * FJ * 16 + c;
+    const int m = a.tail.cols - col >= 8 ? 8 : a.tail.cols > col ? (int)(a.tail.cols - col) : 0;
+#pragma unroll
+    for (int g = 0; g < FI / G; ++g) {
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[(i * 16 + chunk * 4 + e) * LD + j * 16 + at] = sum[g * G + i][j][e];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (m > 0)
+#pragma unroll 1 // (the code of what follows is long)
+            for (int r = lane / per; r < G * 16; r += 64 / per) {
+                const int64_t row = i0 + (wi * FI + g * G) * 16 + r;
+                if (row >= a.tail.rows) break;
+                float v[8];
+                const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = NP == 3 ? lo[e] * kDown : lo[e];
+                    v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
+                }
+                if (NP == 3 && again) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = 0.0f;
+                        if (e < m)
+                            for (int64_t k = k0; k < k1; ++k) v[e] = __builtin_fmaf(number<T, TP>(a.p, row, k), number<T, TQ>(a.q, col + e, k), v[e]);
+                    }
+                }
+                if (a.part) store_upto<float, 8>(a.part + (stretch * a.tail.rows + row) * a.tail.cols + col, m, v);
+                else put8<T>(a.tail, key, row, col, m, v);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 template <typename T, typename C> constexpr int lds_bytes()
 {
-    constexpr int stage = (C::BI + C::BJ) * Num<T>::KS * 2 * Num<T>::NP, out = C::WI * C::WJ * 16 * (C::FJ * 16 + 4) * 4;
+    constexpr int stage = (C::BI + C::BJ) * Num<T>::KS * 2 * Num<T>::NP, out = out_bytes<C, 2>();
     return stage > out ? stage : out;
 }
 
+// Any operands.  They go through registers to LDS.
 template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads) tile_kernel(TileArgs a)
 {
     typedef typename Num<T>::E E;
@@ -339,49 +403,156 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
         __syncthreads();
         again = met;
     }
-    // Sums go through LDS, 16 rows of the wavefront at a time, so that a lane has 8 columns side by side.
-    constexpr int LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
-    float *own = reinterpret_cast<float *>(lds) + wave * 16 * LD;
-    DropKey key = {};
-    if (!a.part && a.tail.drop.threshold) {
-        key = key_of(a.tail.drop);
-        if (blockIdx.x == 0 && tid == 0) tell_key(a.tail.drop, key);
+    finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, again);
+}
+
+// ---------------------------------------------------------------------------------- 16-bit numbers straight to LDS
+// Tiles of operands whose rows are whole 16-byte pieces.  Pieces go from memory straight to LDS, two stages of 64 numbers of k, one of them on its way while
+// the other is multiplied.  A load of a wavefront fills 1 KB.
+//
+// k side by side: 128 bytes a row, whose 8 pieces are exchanged by the row's number so that 8 rows read together lie in different banks.
+// Rows side by side: [k][rows], turned by the LDS reads that do so: 16 lanes give the addresses of 4 numbers each, 16 rows of 4 k, and each gets the 4 k of
+// one row.  A lane's k is 32 kk + 8 g + 4 h + r; kilobytes are numbered by r, g and kk, as far as that goes, and lie 1056 bytes apart: so
+// the four k of a read lie in different banks, and what an instruction reads is at a distance from the lane's first address that does not depend on the lane.
+template <typename T, bool TURN, int R, int THREADS> struct Straight {
+    static constexpr int KS = 64, blocks = R / 8, waves = THREADS / 64, loads = blocks / waves, apart = TURN ? 1056 : 1024, bytes = blocks * apart;
+    static_assert(blocks % waves == 0, "whole loads");
+    uint32_t off[loads]; // bytes from the tile's first number
+    const char *base;
+    int64_t step;
+
+    // k of a lane's piece in a block, and the row
+    static __device__ __forceinline__ int k_of(int block, int lane)
+    {
+        if (!TURN) return ((lane & 7) ^ (lane >> 3)) * 8;
+        const int in = lane / (R / 8), t = block + blocks * (in >> 1);
+        return (t >> 4) * 32 + (t >> 2 & 3) * 8 + (in & 1) * 4 + (t & 3);
     }
+    static __device__ __forceinline__ int row_of(int block, int lane) { return TURN ? lane % (R / 8) * 8 : block * 8 + (lane >> 3); }
+
+    __device__ __forceinline__ void begin(const Side &s, int64_t row0, int64_t k0, int lane, int wave)
+    {
+        base = static_cast<const char *>(s.at) + (TURN ? k0 * s.ld + row0 : row0 * s.ld + k0) * 2;
+        step = (TURN ? KS * s.ld : KS) * 2;
 #pragma unroll
-    for (int i = 0; i < FI; ++i) {
-#pragma unroll
-        for (int j = 0; j < FJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) own[(chunk * 4 + e) * LD + j * 16 + at] = sum[i][j][e];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int h = 0; h < 16 * per / 64; ++h) {
-            const int r = (lane + h * 64) / per, c = (lane + h * 64) % per * 8;
-            const int64_t row = i0 + (wi * FI + i) * 16 + r, col = j0 + wj * FJ * 16 + c;
-            float v[8];
-            const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = NP == 3 ? lo[e] * kDown : lo[e];
-                v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
-            }
-            if (row >= a.tail.rows || col >= a.tail.cols) continue;
-            const int m = a.tail.cols - col < 8 ? (int)(a.tail.cols - col) : 8;
-            if (NP == 3 && again) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = 0.0f;
-                    if (e < m)
-                        for (int64_t k = k0; k < k1; ++k) v[e] = __builtin_fmaf(number<T, TP>(a.p, row, k), number<T, TQ>(a.q, col + e, k), v[e]);
-                }
-            }
-            if (a.part) store_upto<float, 8>(a.part + (stretch * a.tail.rows + row) * a.tail.cols + col, m, v);
-            else put8<T>(a.tail, key, row, col, m, v);
+        for (int u = 0; u < loads; ++u) {
+            const int block = u * waves + wave, k = k_of(block, lane), r = row_of(block, lane);
+            const int64_t last = (TURN ? (s.n - 1) / 8 * 8 : s.n - 1) - row0, row = r < last ? r : last; // what comes of rows behind the last is not stored
+            off[u] = (uint32_t)((TURN ? k * s.ld + row : row * s.ld + k) * 2);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
+    // loads of the stage that `base` is at; left: numbers of k that there are
+    __device__ __forceinline__ void fetch(char *lds, int64_t left, int lane, int wave) const
+    {
+        typedef __attribute__((address_space(3))) void *Lds;
+        typedef __attribute__((address_space(1))) const void *Global;
+        if (left >= KS) {
+#pragma unroll
+            for (int u = 0; u < loads; ++u)
+                __builtin_amdgcn_global_load_lds((Global)(base + off[u]), (Lds)(lds + (u * waves + wave) * apart), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int u = 0; u < loads; ++u) {
+                char *to = lds + (u * waves + wave) * apart;
+                if (k_of(u * waves + wave, lane) < left) __builtin_amdgcn_global_load_lds((Global)(base + off[u]), (Lds)to, 16, 0, 0);
+                else *reinterpret_cast<u4 *>(to + lane * 16) = u4{0, 0, 0, 0};
+            }
+        }
+    }
+    __device__ __forceinline__ void next() { base += step; }
+    // numbers of k from 32 kk + 8 (lane / 16) on, of row 16 f + lane % 16
+    static __device__ __forceinline__ u4 read(const char *lds, int f, int kk, int lane)
+    {
+        if constexpr (TURN) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 *At;
+            const int t = (lane >> 4) * 4 + (lane >> 2 & 3); // r + 4 g
+            const char *p = lds + t % blocks * apart + t / blocks * (4 * R) + (lane & 3) * 8; // this lane's 4 of 16 rows
+            p += kk * (blocks > 16 ? 16 * apart : 16 / blocks * 4 * R) + f * 32;
+            const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)p));
+            const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p + 2 * R)));
+            return u4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            return *reinterpret_cast<const u4 *>(lds + (f * 16 + (lane & 15)) * 128 + ((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
+        }
+    }
+};
+
+template <bool TP, bool TQ, typename C> constexpr int straight_bytes()
+{
+    constexpr int stages = 2 * (Straight<half_t, TP, C::BI, C::threads>::bytes + Straight<half_t, TQ, C::BJ, C::threads>::bytes);
+    constexpr int out = out_bytes<C, C::FI < 4 ? C::FI : 4>();
+    return stages > out ? stages : out;
+}
+// The next numbers are read from LDS while those before are multiplied, and a stage's loads are given out when all wavefronts have read the one
+// before it, which is half a stage before they multiply its last numbers.
+template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) straight_kernel(TileArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    typedef Straight<T, TP, C::BI, C::threads> P;
+    typedef Straight<T, TQ, C::BJ, C::threads> Q;
+    constexpr int FI = C::FI, FJ = C::FJ, stage = P::bytes + Q::bytes;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
+    int ti, tj, stretch;
+    place_of(a, &ti, &tj, &stretch);
+    const int64_t i0 = (int64_t)ti * C::BI, j0 = (int64_t)tj * C::BJ;
+    const int64_t k0 = (int64_t)stretch * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
+    P p;
+    Q q;
+    p.begin(a.p, i0, k0, lane, wave);
+    q.begin(a.q, j0, k0, lane, wave);
+    const int steps = (int)((k1 - k0 + 63) / 64);
+    int64_t left = k1 - k0;
+    const auto fetch = [&](int s) {
+        char *to = lds + (s & 1) * stage;
+        p.fetch(to, left, lane, wave);
+        q.fetch(to + P::bytes, left, lane, wave);
+        p.next(), q.next(), left -= 64;
+    };
+    const auto all_here = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    Sums<C> sum;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    // A stage in units of GI x FJ products of 16 x 16 x 32; the numbers of a unit are read while the one before is multiplied.
+    constexpr int GI = FI < 4 ? FI : 4, per = FI / GI, units = 2 * per;
+    u4 x[2][GI], y[2][FJ];
+    const auto read = [&](int s, int u) {
+        const char *from = lds + (s & 1) * stage;
+        if (u % per == 0)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) y[u / per][j] = Q::read(from + P::bytes, wj * FJ + j, u / per, lane);
+#pragma unroll
+        for (int i = 0; i < GI; ++i) x[u & 1][i] = P::read(from, wi * FI + u % per * GI + i, u / per, lane);
+    };
+    const auto multiply = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < GI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[u % per * GI + i][j] = mfma(T(), x[u & 1][i], y[u / per][j], sum[u % per * GI + i][j]);
+    };
+    if (steps > 0) {
+        fetch(0);
+        all_here();
+        if (steps > 1) fetch(1);
+        read(0, 0);
+        for (int s = 0; s < steps; ++s) {
+#pragma unroll
+            for (int u = 0; u < units - 1; ++u) {
+                read(s, u + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(u);
+            }
+            all_here(); // stage s has been read, stage s + 1 is there
+            if (s + 2 < steps) fetch(s + 2);
+            if (s + 1 < steps) read(s + 1, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(units - 1);
+        }
+    }
+    __syncthreads(); // all of the last stage is read
+    finish_tile<T, TP, TQ, C, FI < 4 ? FI : 4>(a, sum, lds, i0, j0, k0, k1, stretch, false);
 }
 
 // Sums of the stretches of k and what follows.  A workgroup takes `across` places of 8 columns; of its threads kT / across share a place and take
@@ -499,6 +670,13 @@ int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 int64_t round16(int64_t n) { return up(n, 16) * 16; }
 constexpr int64_t kMostTiles = int64_t(1) << 23;
 
+// Whether an operand's pieces can go straight to LDS: 16-byte rows, or, with its rows side by side, runs of rows; of places that 32 bits reach.
+// padded: rows behind the last one can be read up to a whole piece.
+template <typename T> bool straight(const Side &s, bool turned, bool padded)
+{
+    return sizeof(T) == 2 && s.ld % 8 == 0 && (uintptr_t)s.at % 16 == 0 && s.ld < (1 << 22) && (!turned || s.n % 8 == 0 || padded);
+}
+
 // How a product of I x J numbers over K is cut.  The widest tiles that the result fills; where they are too few for the chip k is cut into
 // stretches, whose sums go through memory, and where it is too short for that tiles are of 64 x 64.
 struct Plan {
@@ -506,17 +684,20 @@ struct Plan {
     int64_t tiles_i, tiles_j, stretch;
     int stretches;
 };
-template <typename T> Plan plan(int64_t I, int64_t J, int64_t K)
+enum { WIDE, TALL, FLAT, SMALL, LARGE };
+template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct)
 {
     constexpr int64_t kWanted = 512; // workgroups: two to a compute unit
-    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI}, BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ};
+    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI, Large::BI}, BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ, Large::BJ};
     Plan p;
     const int64_t stages = up(K, Num<T>::KS), most = stages / 4 < 1 ? 1 : stages / 4;
-    p.which = (I <= 64 ? 2 : 0) + (J <= 64 ? 1 : 0);
-    if (up(I, BI[p.which]) * up(J, BJ[p.which]) * most < 256) p.which = 3;
+    int64_t wanted = kWanted;
+    p.which = (I <= 64 ? FLAT : WIDE) + (J <= 64 ? 1 : 0);
+    if (direct && I > 128 && J > 128 && up(I, 256) * up(J, 256) * most >= 192) p.which = LARGE, wanted = 256;
+    if (up(I, BI[p.which]) * up(J, BJ[p.which]) * most < 256 && p.which != LARGE) p.which = SMALL;
     p.tiles_i = up(I, BI[p.which]), p.tiles_j = up(J, BJ[p.which]);
     const int64_t tiles = p.tiles_i * p.tiles_j;
-    int64_t s = tiles >= kWanted ? 1 : kWanted / (tiles ? tiles : 1);
+    int64_t s = tiles >= wanted ? 1 : wanted / (tiles ? tiles : 1);
     if (s > most) s = most;
     p.stretch = up(stages, s) * Num<T>::KS;
     p.stretches = (int)(K ? up(K, p.stretch) : 1);
@@ -524,17 +705,39 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K)
 }
 int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
 
-template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, const Tail &tail, void *ws, hipStream_t stream)
+template <typename T, bool TP, bool TQ, typename C> int launch_straight(const TileArgs &a, unsigned grid, hipStream_t stream)
 {
-    const Plan c = plan<T>(p.n, q.n, K);
+    constexpr int bytes = straight_bytes<TP, TQ, C>();
+    if (!allow_lds(&straight_kernel<T, TP, TQ, C>, bytes)) return PCSR_E_HIP;
+    hipLaunchKernelGGL((straight_kernel<T, TP, TQ, C>), dim3(grid), dim3(C::threads), bytes, stream, a);
+    return PCSR_OK;
+}
+// direct: both operands' pieces can go straight to LDS
+template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, bool direct, const Tail &tail, void *ws, hipStream_t stream)
+{
+    const Plan c = plan<T>(p.n, q.n, K, direct);
     TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
-    const dim3 grid((unsigned)(c.tiles_i * c.tiles_j * c.stretches));
-    switch (c.which) {
-    case 0: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Wide>), grid, dim3(Wide::threads), 0, stream, a); break;
-    case 1: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Tall>), grid, dim3(Tall::threads), 0, stream, a); break;
-    case 2: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Flat>), grid, dim3(Flat::threads), 0, stream, a); break;
-    default: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Small>), grid, dim3(Small::threads), 0, stream, a);
+    const unsigned grid = (unsigned)(c.tiles_i * c.tiles_j * c.stretches);
+    int rc = PCSR_OK;
+    bool done = false;
+    if constexpr (sizeof(T) == 2) {
+        if (direct && c.which != SMALL) {
+            done = true;
+            switch (c.which) {
+            case WIDE: rc = launch_straight<T, TP, TQ, StraightWide>(a, grid, stream); break;
+            case TALL: rc = launch_straight<T, TP, TQ, StraightTall>(a, grid, stream); break;
+            case FLAT: rc = launch_straight<T, TP, TQ, StraightFlat>(a, grid, stream); break;
+            default: rc = launch_straight<T, TP, TQ, Large>(a, grid, stream);
+            }
+        }
     }
+    if (rc != PCSR_OK) return rc;
+    if (!done) switch (c.which) {
+        case WIDE: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Wide>), dim3(grid), dim3(Wide::threads), 0, stream, a); break;
+        case TALL: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Tall>), dim3(grid), dim3(Tall::threads), 0, stream, a); break;
+        case FLAT: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Flat>), dim3(grid), dim3(Flat::threads), 0, stream, a); break;
+        default: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Small>), dim3(grid), dim3(Small::threads), 0, stream, a);
+        }
     if (c.stretches > 1) {
         const uint32_t groups = (uint32_t)up(tail.cols, 8);
         const int64_t places = tail.rows * groups;
@@ -553,6 +756,10 @@ struct Space {
     template <typename T> static Space of(const pcsr_linear_t &a, bool own)
     {
         Space s;
+        const auto most_of = [](int64_t I, int64_t J, int64_t K) { // however the operands lie
+            const int64_t x = part_bytes(plan<T>(I, J, K, false), I, J), y = part_bytes(plan<T>(I, J, K, true), I, J);
+            return x > y ? x : y;
+        };
         s.ld = up(a.out, 8) * 8;
         s.lanes = 1;
         while (s.lanes < 64 && s.lanes * 8 < a.out) s.lanes *= 2;
@@ -562,12 +769,17 @@ struct Space {
         s.blocks = up(a.rows, s.chunk);
         s.dz = own ? round16(a.rows * s.ld * (int64_t)sizeof(T)) : 0;
         s.sums = round16(4 * s.blocks * a.out);
-        const int64_t x = part_bytes(plan<T>(a.rows, a.in, a.out), a.rows, a.in), w = part_bytes(plan<T>(a.out, a.in, a.rows), a.out, a.in);
+        const int64_t x = most_of(a.rows, a.in, a.out), w = most_of(a.out, a.in, a.rows);
         s.part = x > w ? x : w;
         s.bytes = s.dz + s.sums + s.part;
         return s;
     }
 };
+template <typename T> bool forward_direct(const pcsr_linear_t &a)
+{
+    return a.in % 8 == 0 && straight<T>({a.x, a.x_stride, a.rows}, false, false) && straight<T>({a.w, a.w_stride, a.out}, false, false);
+}
+template <typename T> Plan forward_plan(const pcsr_linear_t &a) { return plan<T>(a.rows, a.out, a.in, forward_direct<T>(a)); }
 bool has_slope(const pcsr_linear_t &a) { return a.act != PCSR_ACT_NONE || drop_of(&a.drop).threshold; }
 
 int check(const pcsr_linear_t *a)
@@ -596,7 +808,7 @@ int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward)
     int64_t need = 0;
     for_type(a->type, [&](auto z) {
         typedef decltype(z) T;
-        need = backward ? Space::of<T>(*a, has_slope(*a)).bytes : part_bytes(plan<T>(a->rows, a->out, a->in), a->rows, a->out);
+        need = backward ? Space::of<T>(*a, has_slope(*a)).bytes : part_bytes(forward_plan<T>(*a), a->rows, a->out);
         return 0;
     });
     return need;
@@ -611,7 +823,7 @@ int pcsr_linear(const pcsr_linear_t *a, void *y, void *slope, void *ws, void *st
     const Tail tail = {a->bias, a->residual, y, a->act == PCSR_ACT_NONE ? nullptr : slope, a->r_stride, a->rows, a->out, a->act, a->bias_type, drop_of(&a->drop)};
     return for_type(a->type, [&](auto t) {
         typedef decltype(t) T;
-        return product<T, false, false>({a->x, a->x_stride, a->rows}, {a->w, a->w_stride, a->out}, a->in, tail, ws, (hipStream_t)stream);
+        return product<T, false, false>({a->x, a->x_stride, a->rows}, {a->w, a->w_stride, a->out}, a->in, forward_direct<T>(*a), tail, ws, (hipStream_t)stream);
     });
 }
 
@@ -642,11 +854,13 @@ int pcsr_linear_backward(const pcsr_linear_t *a, const void *slope, const void *
         int rc = launched();
         if (dx && a->in > 0 && rc == PCSR_OK) {
             const Tail tail = {nullptr, nullptr, dx, nullptr, 0, a->rows, a->in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
-            rc = product<T, false, true>(dz, {a->w, a->w_stride, a->in}, a->out, tail, part, stream);
+            const Side w = {a->w, a->w_stride, a->in};
+            rc = product<T, false, true>(dz, w, a->out, a->out % 8 == 0 && straight<T>(dz, false, false) && straight<T>(w, true, false), tail, part, stream);
         }
         if (dw && a->in > 0 && rc == PCSR_OK) {
             const Tail tail = {nullptr, nullptr, dw, nullptr, 0, a->out, a->in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
-            rc = product<T, true, true>({dz.at, dz.ld, a->out}, {a->x, a->x_stride, a->in}, a->rows, tail, part, stream);
+            const Side g = {dz.at, dz.ld, a->out}, x = {a->x, a->x_stride, a->in};
+            rc = product<T, true, true>(g, x, a->rows, straight<T>(g, true, own) && straight<T>(x, true, false), tail, part, stream);
         }
         return rc;
     });

@@ -122,6 +122,17 @@ def test_sizes(kind, size, act, p, residual, bias):
     run(X, W, b, act, R, p, (7 << 40) + 5, 2, kind, _normal(5, M, N, kind=kind))
 
 
+# tiles of 256 x 256 with 16-bit numbers, whole ones and not, k that no stage divides, stretches of it
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("size", [(2100, 4104, 1544), (12_345, 200, 1032), (512, 2048, 512), (30_000, 512, 72), (260, 16_392, 264), (200, 520, 4000)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_wide_sizes(kind, size):
+    M, K, N = size
+    X, W, R = _normal(1, M, K, kind=kind), _normal(2, N, K, kind=kind, scale=K ** -0.5), _normal(4, M, N, kind=kind)
+    run(X, W, _normal(3, N, kind=kind), "gelu", R, 0.1, 9, 2, kind, _normal(5, M, N, kind=kind))
+    run(X, W, None, "none", None, 0.0, 0, 0, kind, _normal(5, M, N, kind=kind))
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 def test_both_calls(path, kind):
     for size in ((1, 64, 64), (200, 75, 50)):
