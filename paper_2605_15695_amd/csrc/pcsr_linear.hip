@@ -26,6 +26,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
+int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 constexpr int kT = 256;
 constexpr float kUp = 65536.0f, kDown = 1.0f / (65536.0f * 65536.0f), kHot = 0x1p54f; // 2^38 of a number as it is split
 
@@ -71,12 +72,12 @@ struct Tail {
 };
 
 // Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 of them to 1 (0 and 1 are exact, others are 2^-16 off at
-// most, a 32nd of what fp16 rounds gradients of their size by; slopes are between -0.13 and 1.13).  Kept in place of z: a slope costs three
-// operations beside the activation and forty apart from it.
+// most, a 32nd of what fp16 rounds gradients of their size by; slopes are between -0.13 and 1.13, and 0 stands for none).  Kept in place of z: a
+// slope costs three operations beside the activation and forty apart from it.
 template <typename T> struct Slope {
     typedef uint16_t type;
-    static __device__ __forceinline__ uint16_t put(float s) { return s == s ? (uint16_t)__builtin_fmaf(s, 32768.0f, 8192.5f) : 65535; }
-    static __device__ __forceinline__ float take(uint16_t q) { return q == 65535 ? __builtin_nanf("") : (float)((int)q - 8192) * (1.0f / 32768.0f); }
+    static __device__ __forceinline__ uint16_t put(float s) { return (uint16_t)(uint32_t)__builtin_fmaf(s, 32768.0f, 8192.5f); } // (of no number 0)
+    static __device__ __forceinline__ float take(uint16_t q) { return q ? __builtin_fmaf((float)q, 1.0f / 32768.0f, -0.25f) : __builtin_nanf(""); }
 };
 template <> struct Slope<float> {
     typedef float type;
@@ -84,25 +85,21 @@ template <> struct Slope<float> {
     static __device__ __forceinline__ float take(float s) { return s; }
 };
 
-// 8 numbers of x w^T, m of them there, at a row and a column that is a multiple of 8
-template <typename T> __device__ __forceinline__ void put8(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8])
+// 8 numbers of x w^T at a row and a column that is a multiple of 8, m of them there (WHOLE: all); bias: theirs; r: the residual's (RES)
+template <typename T, bool WHOLE, bool RES>
+__device__ __forceinline__ void put8(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8], const float (&bias)[8], const float (&r)[8])
 {
-    if (a.bias) {
-        float b[8];
-        if (a.bias_type == PCSR_F32) load_upto<float, 8>(static_cast<const float *>(a.bias) + c, m, b);
-        else load_upto<T, 8>(static_cast<const T *>(a.bias) + c, m, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += b[i];
-    }
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
     if (a.slope) {
         typedef typename Slope<T>::type S;
         float f[8];
-        activate(v, f, a.act);
+        activate_for<sizeof(T) == 2, true>(v, f, a.act);
         S *to = static_cast<S *>(a.slope) + row * a.cols + c;
         typename Pack<S, 8>::type q;
 #pragma unroll
         for (int i = 0; i < 8; ++i) q[i] = Slope<T>::put(f[i]);
-        if (m >= 8) {
+        if (WHOLE || m >= 8) {
             *reinterpret_cast<typename Pack<S, 8>::type *>(to) = q;
         } else {
 #pragma unroll
@@ -110,16 +107,35 @@ template <typename T> __device__ __forceinline__ void put8(const Tail &a, const 
                 if (i < m) to[i] = q[i];
         }
     } else {
-        activate(v, a.act);
+        float none[8];
+        activate_for<sizeof(T) == 2, false>(v, none, a.act);
     }
     if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, v);
-    if (a.residual) {
-        float r[8];
-        load_upto<T, 8>(static_cast<const T *>(a.residual) + row * a.r_stride + c, m, r);
+    if (RES)
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += r[i];
+    T *to = static_cast<T *>(a.y) + row * a.cols + c;
+    if (WHOLE) store<T, 8>(to, v);
+    else store_upto<T, 8>(to, m, v);
+}
+template <typename T, bool WHOLE> __device__ __forceinline__ void bias8(const Tail &a, int64_t c, int m, float (&b)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+    if (a.bias && m > 0) {
+        if (a.bias_type == PCSR_F32) load_upto<float, 8>(static_cast<const float *>(a.bias) + c, WHOLE ? 8 : m, b);
+        else load_upto<T, 8>(static_cast<const T *>(a.bias) + c, WHOLE ? 8 : m, b);
     }
-    store_upto<T, 8>(static_cast<T *>(a.y) + row * a.cols + c, m, v);
+}
+// any place, on its own
+template <typename T> __device__ __forceinline__ void put_one(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8])
+{
+    float b[8], r[8];
+    bias8<T, false>(a, c, m, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = 0.0f;
+    if (a.residual) load_upto<T, 8>(static_cast<const T *>(a.residual) + row * a.r_stride + c, m, r);
+    put8<T, false, true>(a, key, row, c, m, v, b, r);
 }
 
 // ---------------------------------------------------------------------------------- operands on their way to LDS
@@ -268,13 +284,90 @@ __device__ __forceinline__ void place_of(const TileArgs &a, int *ti, int *tj, in
 
 template <typename C> using Sums = f4[C::FI][C::FJ];
 
+// Products of 32 numbers of k in pieces, with tiles side by side so that an instruction does not wait for the one before it.  They have a sum of
+// their own, small ones first: the matrix instructions cut off what does not reach a sum's last bit, always downwards.
+template <int N> __device__ __forceinline__ void products32(const u4 (&x)[3], const u4 (&y)[N][3], f4 (&s)[N])
+{
+    constexpr int P[6] = {2, 0, 1, 1, 0, 0}, Q[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int o = 0; o < 6; ++o)
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = mfma(bfloat_t(), x[P[o]], y[j][Q[o]], s[j]);
+}
+// 8 columns of a row in fp32, where pieces would leave the range
+template <typename T, bool TP, bool TQ>
+__device__ __forceinline__ void once_more(const TileArgs &a, int64_t row, int64_t col, int m, int64_t k0, int64_t k1, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+#pragma unroll 1
+    for (int64_t k = k0; k < k1; ++k) {
+        const float x = number<T, TP>(a.p, row, k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < m) v[e] = __builtin_fmaf(x, number<T, TQ>(a.q, col + e, k), v[e]);
+    }
+}
+
 // What becomes of a tile's sums.  They go through LDS, G times 16 rows of a wavefront at a time, so that a lane has 8 columns side by side: whole lines
 // of y, and what one call of the generator is for.  again: the numbers are added up once more, in fp32.
 template <typename C, int G> constexpr int out_bytes() { return C::WI * C::WJ * G * 16 * (C::FJ * 16 + 4) * 4; }
+
+struct Where { // of a wavefront's sums
+    int64_t i0, col; // first row, a lane's column
+    int m;           // columns that are there from it on
+    int64_t k0, k1;
+    int stretch;
+    bool again;
+};
+// The rows that lie in LDS.  WHOLE: 8 columns are there or none.  RES: residuals come four rows ahead, since each is a round trip to memory.
+template <typename T, bool TP, bool TQ, int ROWS, int LD, int PER, bool WHOLE, bool RES>
+__device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &key, const Where &w, const float *own, const float (&bias)[8])
+{
+    constexpr int NP = Num<T>::NP, step = 64 / PER, passes = ROWS / step, A = RES ? (passes < 4 ? passes : 4) : 1;
+    const int lane = threadIdx.x & 63, r0 = lane / PER, c = lane % PER * 8;
+    if (w.m <= 0) return;
+#pragma unroll 1
+    for (int n = 0; n < passes; n += A) {
+        float res[A][8];
+        if (RES)
+#pragma unroll
+            for (int u = 0; u < A; ++u) {
+                const int64_t r = w.i0 + r0 + (n + u) * step, row = r < a.tail.rows ? r : a.tail.rows - 1;
+                const T *p = static_cast<const T *>(a.tail.residual) + row * a.tail.r_stride + w.col;
+                if (WHOLE) load<T, 8>(p, res[u]);
+                else load_upto<T, 8>(p, w.m, res[u]);
+            }
+#pragma unroll
+        for (int u = 0; u < A; ++u) {
+            const int r = r0 + (n + u) * step;
+            const int64_t row = w.i0 + r;
+            float v[8];
+            const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = NP == 3 ? lo[e] * kDown : lo[e];
+                v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
+            }
+            if (row < a.tail.rows) {
+                if (NP == 3 && w.again) once_more<T, TP, TQ>(a, row, w.col, w.m, w.k0, w.k1, v);
+                if (!a.part) {
+                    put8<T, WHOLE, RES>(a.tail, key, row, w.col, w.m, v, bias, res[u]);
+                } else {
+                    float *to = a.part + (w.stretch * a.tail.rows + row) * a.tail.cols + w.col;
+                    if (WHOLE) store<float, 8>(to, v);
+                    else store_upto<float, 8>(to, w.m, v);
+                }
+            }
+        }
+    }
+}
 template <typename T, bool TP, bool TQ, typename C, int G>
 __device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &sum, char *lds, int64_t i0, int64_t j0, int64_t k0, int64_t k1, int stretch, bool again)
 {
-    constexpr int FI = C::FI, FJ = C::FJ, NP = Num<T>::NP, LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
+    constexpr int FI = C::FI, FJ = C::FJ, LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
     static_assert(FI % G == 0, "whole passes");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / C::WJ, wj = wave % C::WJ, at = lane & 15, chunk = lane >> 4;
     float *own = reinterpret_cast<float *>(lds) + wave * G * 16 * LD;
@@ -283,11 +376,12 @@ __device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &su
         key = key_of(a.tail.drop);
         if (blockIdx.x == 0 && threadIdx.x == 0) tell_key(a.tail.drop, key);
     }
-    const int c = lane % per * 8;
-    const int64_t col = j0 + wj * FJ * 16 + c;
-    const int m = a.tail.cols - col >= 8 ? 8 : a.tail.cols > col ? (int)(a.tail.cols - col) : 0;
-#pragma unroll
-    for (int g = 0; g < FI / G; ++g) {
+    const bool whole = a.tail.cols % 8 == 0, res = a.tail.residual && !a.part;
+    Where w = {0, j0 + wj * FJ * 16 + lane % per * 8, 0, k0, k1, stretch, again};
+    w.m = a.tail.cols - w.col >= 8 ? 8 : a.tail.cols > w.col ? (int)(a.tail.cols - w.col) : 0;
+    float bias[8];
+    bias8<T, false>(a.tail, w.col, a.part ? 0 : w.m, bias);
+    const auto pass = [&](auto g) { // (written out, not unrolled: loops of this length are not)
 #pragma unroll
         for (int i = 0; i < G; ++i)
 #pragma unroll
@@ -296,32 +390,17 @@ __device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &su
                 for (int e = 0; e < 4; ++e) own[(i * 16 + chunk * 4 + e) * LD + j * 16 + at] = sum[g * G + i][j][e];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (m > 0)
-#pragma unroll 1 // (the code of what follows is long)
-            for (int r = lane / per; r < G * 16; r += 64 / per) {
-                const int64_t row = i0 + (wi * FI + g * G) * 16 + r;
-                if (row >= a.tail.rows) break;
-                float v[8];
-                const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = NP == 3 ? lo[e] * kDown : lo[e];
-                    v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
-                }
-                if (NP == 3 && again) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[e] = 0.0f;
-                        if (e < m)
-                            for (int64_t k = k0; k < k1; ++k) v[e] = __builtin_fmaf(number<T, TP>(a.p, row, k), number<T, TQ>(a.q, col + e, k), v[e]);
-                    }
-                }
-                if (a.part) store_upto<float, 8>(a.part + (stretch * a.tail.rows + row) * a.tail.cols + col, m, v);
-                else put8<T>(a.tail, key, row, col, m, v);
-            }
+        w.i0 = i0 + (wi * FI + g * G) * 16;
+        if (whole && res) finish_rows<T, TP, TQ, G * 16, LD, per, true, true>(a, key, w, own, bias);
+        else if (whole) finish_rows<T, TP, TQ, G * 16, LD, per, true, false>(a, key, w, own, bias);
+        else if (res) finish_rows<T, TP, TQ, G * 16, LD, per, false, true>(a, key, w, own, bias);
+        else finish_rows<T, TP, TQ, G * 16, LD, per, false, false>(a, key, w, own, bias);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-    }
+    };
+    static_assert(FI / G <= 2, "two passes at most");
+    pass(std::integral_constant<int, 0>());
+    if constexpr (FI / G == 2) pass(std::integral_constant<int, 1>());
 }
 
 template <typename T, typename C> constexpr int lds_bytes()
@@ -377,23 +456,17 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
                     y[j][o] = *reinterpret_cast<const u4 *>(ldsQ + o * planeQ + place<KS>((wj * FJ + j) * 16 + at, kk * 4 + chunk));
             }
 #pragma unroll
-            for (int i = 0; i < FI; ++i)
+            for (int i = 0; i < FI; ++i) {
+                if constexpr (NP == 3) {
+                    f4 part[FJ];
+                    products32<FJ>(x[i], y, part);
 #pragma unroll
-                for (int j = 0; j < FJ; ++j) {
-                    if constexpr (NP == 3) {
-                        // a stage's products have a sum of their own, small ones first: the matrix instructions cut off what does not reach a
-                        // sum's last bit, always downwards
-                        f4 s = mfma(E(), x[i][2], y[j][0], f4{0.0f, 0.0f, 0.0f, 0.0f});
-                        s = mfma(E(), x[i][0], y[j][2], s);
-                        s = mfma(E(), x[i][1], y[j][1], s);
-                        s = mfma(E(), x[i][1], y[j][0], s);
-                        s = mfma(E(), x[i][0], y[j][1], s);
-                        s = mfma(E(), x[i][0], y[j][0], s);
-                        sum[i][j] += s;
-                    } else {
-                        sum[i][j] = mfma(E(), x[i][0], y[j][0], sum[i][j]);
-                    }
+                    for (int j = 0; j < FJ; ++j) sum[i][j] += part[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) sum[i][j] = mfma(E(), x[i][0], y[j][0], sum[i][j]);
                 }
+            }
         }
         __syncthreads();
     }
@@ -555,6 +628,187 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     finish_tile<T, TP, TQ, C, FI < 4 ? FI : 4>(a, sum, lds, i0, j0, k0, k1, stretch, false);
 }
 
+// ---------------------------------------------------------------------------------- many rows and few weights
+// The weights lie in LDS for as long as the workgroup lives, in pieces, and wavefronts take 16 rows at a time, each for itself: a lane's numbers of the next rows
+// are on their way to its registers while these are multiplied, nothing waits for other wavefronts, and x is read once.
+// STEPS: of 32 numbers of k.  FJ tiles of 16 columns at a time.  WHOLE: all of k is there, and of columns 8 or none.  RES: a residual is there.
+// Loads come back in their order, and so do the waits: what a strip's end needs is asked for before the next strip's numbers, and the bias lies in LDS.
+template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64 + 16; } // bytes of a row: 16 rows lie in different banks
+template <typename T, int STEPS> int64_t weights_bytes(int64_t cols) { return Num<T>::NP * up(cols, 64) * 64 * weights_pitch<T, STEPS>(); }
+
+template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global__ void __launch_bounds__(512) rows_kernel(TileArgs a, int groups)
+{
+    typedef typename Num<T>::E E;
+    constexpr int NP = Num<T>::NP, N = kPer16<T>, parts = 8 / N, pitch = weights_pitch<T, STEPS>(), LD = FJ * 16 + 4, per = FJ * 2, passes = (16 * per + 63) / 64;
+    typedef typename Pack<T, N>::type Raw;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int met;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 15, chunk = lane >> 4;
+    const int cols = groups * FJ * 16, plane = cols * pitch;
+    float *biases = reinterpret_cast<float *>(lds + NP * plane), *own = biases + cols + wave * 16 * LD;
+    const int64_t rows = a.tail.rows, stride = (int64_t)gridDim.x * 8;
+    const int K = (int)a.K;
+    Raw raw[STEPS][parts];
+    const auto row_at = [&](int64_t strip) {
+        const int64_t r = strip * 16 + at, row = r < rows ? r : rows - 1; // what comes of rows behind the last is not stored
+        return static_cast<const T *>(a.p.at) + row * a.p.ld + chunk * 8;
+    };
+    const auto fetch = [&](const T *p, int t) {
+#pragma unroll
+        for (int q = 0; q < parts; ++q) {
+            const int k = t * 32 + chunk * 8 + q * N, o = t * 32 + q * N;
+            if (WHOLE || k + N <= K) raw[t][q] = *reinterpret_cast<const Raw *>(p + o);
+            else
+#pragma unroll
+                for (int i = 0; i < N; ++i) raw[t][q][i] = k + i < K ? p[o + i] : (T)0.0f;
+        }
+    };
+    int64_t strip = (int64_t)blockIdx.x * 8 + wave;
+    if (strip * 16 < rows) {
+        const T *p = row_at(strip);
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) fetch(p, t);
+    }
+    if (tid == 0) met = 0;
+    __syncthreads();
+    { // weights: a thread takes two numbers of k of a row
+        float hot = 0.0f;
+        for (int id = tid; id < cols * STEPS * 16; id += 512) {
+            const int j = TQ ? id % cols : id / (STEPS * 16), k = (TQ ? id / cols : id % (STEPS * 16)) * 2;
+            T w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                w[e] = j < a.q.n && k + e < K ? static_cast<const T *>(a.q.at)[TQ ? (k + e) * a.q.ld + j : j * a.q.ld + k + e] : (T)0.0f;
+            uint32_t *to = reinterpret_cast<uint32_t *>(lds + j * pitch + k * 2);
+            if constexpr (NP == 3) {
+                uint32_t h[3];
+                pieces(w[0], w[1], hot, h);
+#pragma unroll
+                for (int o = 0; o < 3; ++o) to[o * plane / 4] = h[o];
+            } else {
+                typedef T t2 __attribute__((ext_vector_type(2)));
+                *to = __builtin_bit_cast(uint32_t, t2{w[0], w[1]});
+            }
+        }
+        if (NP == 3 && hot >= kHot) met = 1;
+        for (int j = tid; j < cols; j += 512) {
+            float b = 0.0f;
+            if (a.tail.bias && j < a.tail.cols) b = a.tail.bias_type == PCSR_F32 ? static_cast<const float *>(a.tail.bias)[j] : (float)static_cast<const T *>(a.tail.bias)[j];
+            biases[j] = b;
+        }
+    }
+    __syncthreads();
+    const bool hot_weights = NP == 3 && met;
+    DropKey key = {};
+    if (a.tail.drop.threshold) {
+        key = key_of(a.tail.drop);
+        if (blockIdx.x == 0 && tid == 0) tell_key(a.tail.drop, key);
+    }
+    const char *mine = lds + at * pitch + chunk * 16;
+    const int c = lane % per * 8;
+    float hot = 0.0f;
+    for (; strip * 16 < rows; strip += stride) {
+        const T *next = row_at(strip + stride); // (behind the last rows the last row again)
+        const auto group = [&](int g, auto last) { // last: the next rows are fetched
+            const int64_t col = g * FJ * 16 + c;
+            const int m = a.tail.cols - col >= 8 ? 8 : a.tail.cols > col ? (int)(a.tail.cols - col) : 0;
+            float res[passes][8]; // on its way while the products are taken
+            if (RES)
+#pragma unroll
+                for (int h = 0; h < passes; ++h) {
+                    const int64_t r = strip * 16 + lane / per + h * (64 / per), row = r < rows ? r : rows - 1;
+                    const T *p = static_cast<const T *>(a.tail.residual) + row * a.tail.r_stride;
+                    if (WHOLE) load<T, 8>(p + (m > 0 ? col : 0), res[h]);
+                    else if (m > 0) load_upto<T, 8>(p + col, m, res[h]);
+                }
+            const char *w = mine + g * FJ * 16 * pitch;
+            f4 sum[FJ];
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                u4 x[NP];
+                if constexpr (NP == 3) {
+                    // the compiler is kept from making the pieces of all steps once for all groups: registers do not hold them
+#pragma unroll
+                    for (int q = 0; q < parts; ++q) {
+                        u4 same = __builtin_bit_cast(u4, raw[t][q]);
+                        asm volatile("" : "+v"(same));
+                        raw[t][q] = __builtin_bit_cast(Raw, same);
+                    }
+                    uint32_t h[4][3];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) pieces(raw[t][q >> 1][(q & 1) * 2], raw[t][q >> 1][(q & 1) * 2 + 1], hot, h[q]);
+#pragma unroll
+                    for (int o = 0; o < 3; ++o) x[o] = u4{h[0][o], h[1][o], h[2][o], h[3][o]};
+                } else {
+                    x[0] = __builtin_bit_cast(u4, raw[t][0]);
+                }
+                if (last) fetch(next, t);
+                constexpr int B = NP == 3 ? 2 : FJ; // tiles at a time
+#pragma unroll
+                for (int b = 0; b < FJ; b += B) {
+                    u4 y[B][NP];
+#pragma unroll
+                    for (int j = 0; j < B; ++j)
+#pragma unroll
+                        for (int o = 0; o < NP; ++o) y[j][o] = *reinterpret_cast<const u4 *>(w + o * plane + (b + j) * 16 * pitch + t * 64);
+                    if constexpr (NP == 3) {
+                        f4 part[B];
+                        products32<B>(x, y, part);
+#pragma unroll
+                        for (int j = 0; j < B; ++j) sum[b + j] += part[j];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < B; ++j) sum[b + j] = mfma(E(), x[0], y[j][0], sum[b + j]);
+                    }
+                }
+                if (NP == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[(chunk * 4 + e) * LD + j * 16 + at] = sum[j][e];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            float bias[8];
+            load<float, 8>(biases + col, bias);
+#pragma unroll
+            for (int h = 0; h < passes; ++h) {
+                const int r = lane / per + h * (64 / per);
+                const int64_t row = strip * 16 + r;
+                float v[8];
+                const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = NP == 3 ? lo[e] * kDown : lo[e];
+                    v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
+                }
+                if (m > 0 && row < rows) put8<T, WHOLE, RES>(a.tail, key, row, col, m, v, bias, res[h]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+#pragma unroll 1
+        for (int g = 0; g < groups - 1; ++g) group(g, std::false_type());
+        group(groups - 1, std::true_type());
+    }
+    if (NP == 3 && (hot_weights || __any(hot >= kHot))) // the wavefront's rows with such numbers once more (a loop of its own: the addresses that it needs are kept nowhere else)
+        for (strip = (int64_t)blockIdx.x * 8 + wave; strip * 16 < rows; strip += stride) {
+            float most = 0.0f;
+            for (int k = chunk; k < K; k += 4)
+                if (strip * 16 + at < rows) most = __builtin_fmaxf(most, __builtin_fabsf(number<T, false>(a.p, strip * 16 + at, k)) * kUp);
+            if (!hot_weights && !__any(most >= kHot)) continue;
+            for (int64_t col = c; col < a.tail.cols; col += FJ * 16)
+                for (int r = lane / per; r < 16 && strip * 16 + r < rows; r += 64 / per) {
+                    const int m = a.tail.cols - col >= 8 ? 8 : (int)(a.tail.cols - col);
+                    float v[8];
+                    once_more<T, false, TQ>(a, strip * 16 + r, col, m, 0, a.K, v);
+                    put_one<T>(a.tail, key, strip * 16 + r, col, m, v);
+                }
+        }
+}
+
 // Sums of the stretches of k and what follows.  A workgroup takes `across` places of 8 columns; of its threads kT / across share a place and take
 // every so-manieth stretch each, and their sums are added up in order.
 template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(const float *part, int stretches, Tail a, uint32_t groups, int across)
@@ -586,7 +840,7 @@ template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(const 
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += sums[p * across + lane][i];
     }
-    if (row < a.rows) put8<T>(a, key, row, c, m, v);
+    if (row < a.rows) put_one<T>(a, key, row, c, m, v);
 }
 
 // ---------------------------------------------------------------------------------- gradient at z
@@ -666,7 +920,6 @@ __global__ void __launch_bounds__(1024) sums_kernel(const float *sums, int64_t b
 }
 
 // ---------------------------------------------------------------------------------- launches
-int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 int64_t round16(int64_t n) { return up(n, 16) * 16; }
 constexpr int64_t kMostTiles = int64_t(1) << 23;
 
@@ -712,9 +965,54 @@ template <typename T, bool TP, bool TQ, typename C> int launch_straight(const Ti
     hipLaunchKernelGGL((straight_kernel<T, TP, TQ, C>), dim3(grid), dim3(C::threads), bytes, stream, a);
     return PCSR_OK;
 }
+// Many rows and few weights: what rows_kernel takes.  Weights of up to 104 KB, so that two workgroups or one of eight wavefronts fit with their own rows' room, and
+// rows enough to give every wavefront some.
+template <typename T> int64_t rows_lds(int64_t J, int64_t K)
+{
+    const int64_t w = K <= 32 ? weights_bytes<T, 1>(J) : K <= 64 ? weights_bytes<T, 2>(J) : K <= 128 ? weights_bytes<T, 4>(J) : weights_bytes<T, 8>(J);
+    return w + up(J, 64) * 64 * 4 + 8 * 16 * 68 * 4;
+}
+// (Registers do not hold eight steps of fp32 numbers and what ends of rows take.)
+template <typename T> constexpr bool ends_fit(int steps) { return sizeof(T) == 2 || steps < 8; }
+template <typename T> bool many_rows(int64_t I, int64_t J, int64_t K)
+{
+    return K <= 256 && I >= 32768 && rows_lds<T>(J, K) <= 140 * 1024 && (K <= 128 || (K == 256 && J % 8 == 0) || J <= 32 || ends_fit<T>(8));
+}
+
+template <typename T, bool TQ, int STEPS> int launch_rows(const TileArgs &a, hipStream_t stream)
+{
+    const int64_t J = a.tail.cols, lds = rows_lds<T>(J, a.K);
+    const unsigned blocks = lds <= 78 * 1024 ? 512 : 256;
+    const auto go = [&](auto *kernel, int width) {
+        if (!allow_lds(kernel, (size_t)lds)) return (int)PCSR_E_HIP;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(512), (size_t)lds, stream, a, (int)up(J, width));
+        return (int)PCSR_OK;
+    };
+    const bool whole = a.K == STEPS * 32 && J % 8 == 0;
+    if constexpr (TQ) { // gradients of x: nothing follows
+        if (J <= 32) return go(&rows_kernel<T, TQ, STEPS, 2, false, false>, 32);
+        if constexpr (ends_fit<T>(STEPS))
+            if (!whole) return go(&rows_kernel<T, TQ, STEPS, 4, false, false>, 64);
+        return go(&rows_kernel<T, TQ, STEPS, 4, true, false>, 64);
+    } else {
+        const bool res = a.tail.residual;
+        if (J <= 32) return res ? go(&rows_kernel<T, TQ, STEPS, 2, false, true>, 32) : go(&rows_kernel<T, TQ, STEPS, 2, false, false>, 32);
+        if constexpr (ends_fit<T>(STEPS))
+            if (!whole) return res ? go(&rows_kernel<T, TQ, STEPS, 4, false, true>, 64) : go(&rows_kernel<T, TQ, STEPS, 4, false, false>, 64);
+        return res ? go(&rows_kernel<T, TQ, STEPS, 4, true, true>, 64) : go(&rows_kernel<T, TQ, STEPS, 4, true, false>, 64);
+    }
+}
+
 // direct: both operands' pieces can go straight to LDS
 template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, bool direct, const Tail &tail, void *ws, hipStream_t stream)
 {
+    if constexpr (!TP) {
+        if (many_rows<T>(p.n, q.n, K)) {
+            const TileArgs a = {p, q, K, K, 1, 1, 1, nullptr, tail};
+            const int rc = K <= 32 ? launch_rows<T, TQ, 1>(a, stream) : K <= 64 ? launch_rows<T, TQ, 2>(a, stream) : K <= 128 ? launch_rows<T, TQ, 4>(a, stream) : launch_rows<T, TQ, 8>(a, stream);
+            return rc == PCSR_OK ? launched() : rc;
+        }
+    }
     const Plan c = plan<T>(p.n, q.n, K, direct);
     TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
     const unsigned grid = (unsigned)(c.tiles_i * c.tiles_j * c.stretches);

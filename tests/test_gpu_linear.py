@@ -3,7 +3,8 @@
 With u = 2^-24.  Sums over K numbers: a matrix instruction adds 32 products to a sum and cuts off what does not reach the last bit, of the sum
 and of each product beside the largest, so K / 32 of them and the sums between are off by at most (K / 8 + 48) u of the sum of magnitudes; of fp32
 numbers in three pieces, what is left out of a product is 2 u of it.  That is z_err.  Activations: slopes are at most 1.13 and second
-derivatives 0.8; own roundings u 8 (1 + |z|) |z|, of slopes u 16 (1 + |z|).  16-bit types keep slopes to 2^-16 (relu's, 0 and 1,
+derivatives 0.8; own roundings u 8 (1 + |z|) |z|, of slopes u 16 (1 + |z|); gelu of 16-bit types is good to
+2^-14 of itself, and its slope to 2^-14 of the normal distribution's share, which is at most 1.  16-bit types keep slopes to 2^-16 (relu's, 0 and 1,
 are exact) and the gradient at z in their type (half a step).  Results are rounded once more."""
 import numpy as np
 import pytest
@@ -66,13 +67,15 @@ def check(X, W, b, act, R, p, seed, offset, kind, dy=None, y=None, grads=None):
     want = f * a + (0.0 if R is None else R.detach().double().reshape(M, N))
     if y is not None:
         own = U * 8 * (1 + z.abs()) * z.abs() if act in ("silu", "gelu") else 0.0
+        if act == "gelu" and u > U:
+            own = own + 2.0 ** -14 * a.abs() / (1 - 0.5 * (z > 0).double())  # above zero of what is left to 1, at most the half
         _near(y, want, f * (1.13 * z_err + own + 2 * U * a.abs()) + (0.0 if R is None else U * (R.detach().double().reshape(M, N).abs() + want.abs())), u)
     if grads is None:
         return
     g = dy.detach().double().reshape(M, N) * f
     dz = g * slope
     half = u > U
-    kept_err = 2.0 ** -16 if half else 0.0
+    kept_err = (2.0 ** -16 + 2.0 ** -14 * (act == "gelu")) if half else 0.0
     if act == "none":
         err = U * g.abs()
     elif act == "relu":  # near 0 a right sum may have the other sign
@@ -131,6 +134,19 @@ def test_wide_sizes(kind, size):
     X, W, R = _normal(1, M, K, kind=kind), _normal(2, N, K, kind=kind, scale=K ** -0.5), _normal(4, M, N, kind=kind)
     run(X, W, _normal(3, N, kind=kind), "gelu", R, 0.1, 9, 2, kind, _normal(5, M, N, kind=kind))
     run(X, W, None, "none", None, 0.0, 0, 0, kind, _normal(5, M, N, kind=kind))
+
+
+# weights that stay in LDS while rows pass by, of each depth and width
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("size", [(32_768, 64, 256), (33_001, 70, 9), (32_800, 130, 40), (40_007, 250, 61), (33_000, 31, 20), (65_537, 1, 8), (33_333, 256, 64)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_many_rows(kind, size):
+    M, K, N = size
+    X, W, R = _normal(1, M, K, kind=kind), _normal(2, N, K, kind=kind, scale=K ** -0.5), _normal(4, M, N, kind=kind)
+    run(X, W, _normal(3, N, kind=kind), "gelu", R, 0.1, 9, 2, kind, _normal(5, M, N, kind=kind))
+    run(X, W, None, "none", None, 0.0, 0, 0, kind, _normal(5, M, N, kind=kind))
+    wide = _normal(6, M, K + N + 6, kind=kind)  # rows apart, at any address
+    run(wide[:, 3:3 + K], W, None, "silu", wide[:, 3 + K:3 + K + N], 0.0, 0, 0, kind, wide[:, 2:2 + N])
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
@@ -209,6 +225,16 @@ def test_range_of_32_bits(path):
         assert torch.equal(got[got.isinf()], ref[ref.isinf()])
         fine = ref.isfinite()
         _near(got[fine], (A.double() @ B.double().t())[fine], _sums(K) * (A.abs().double() @ B.abs().double().t())[fine], U)
+    A, B = _normal(17, 40_000, 40), _normal(18, 24, 40)
+    A[70], A[39_990, 3], A[500, 4], A[505, 5] = A[70] * 2.0 ** 100, inf, nan, -inf
+    for lot in (slice(0, 20_000), slice(0, None)):  # tiles, and rows that pass by
+        got, ref = linear(A[lot], B), A[lot] @ B.t()
+        assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf()) and torch.equal(got[got.isinf()], ref[ref.isinf()])
+        fine = ref.isfinite()
+        _near(got[fine], (A[lot].double() @ B.double().t())[fine], _sums(40) * (A[lot].abs().double() @ B.abs().double().t())[fine], U)
+    B[3, 7] = inf
+    got, ref = linear(A, B), A @ B.t()
+    assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf())
     A = torch.full((3, 8), 3e38, device="cuda")  # out of range from the second product on
     assert bool((linear(A, torch.ones(2, 8, device="cuda")) == inf).all())
     for kind in ("bf16", "fp16"):
