@@ -21,7 +21,8 @@ DEVICE = ["--offload-arch=gfx950", "-munsafe-fp-atomics",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 SOURCES = ["pcsr_kernels.hip", "pcsr_build_gpu.hip", "pcsr_gnn.hip", "pcsr_api.cpp", "pcsr_host.cpp", "pcsr_reorder.cpp",
            "pcsr_pool.cpp", "pcsr_window_gpu.hip", "pcsr_relabel_gpu.hip", "pcsr_cluster_gpu.hip",
-           "pcsr_transpose_gpu.hip", "pcsr_embed.hip", "pcsr_norm.hip", "pcsr_ortho.hip", "pcsr_drop.hip", "pcsr_linear.hip"]
+           "pcsr_transpose_gpu.hip", "pcsr_embed.hip", "pcsr_norm.hip", "pcsr_ortho.hip", "pcsr_drop.hip",
+           "pcsr_linear.hip", "pcsr_linear_f32.hip", "pcsr_linear_bf16.hip", "pcsr_linear_f16.hip"]
 
 
 def _compile(src: str) -> pathlib.Path:
@@ -77,7 +78,7 @@ def build(verbose: bool = False) -> pathlib.Path:
 
 
 def resources(sources=("pcsr_kernels.hip", "pcsr_gnn.hip", "pcsr_embed.hip", "pcsr_norm.hip", "pcsr_ortho.hip",
-                       "pcsr_drop.hip", "pcsr_linear.hip")) -> str:
+                       "pcsr_drop.hip", "pcsr_linear_f32.hip", "pcsr_linear_bf16.hip", "pcsr_linear_f16.hip")) -> str:
     """Registers, scratch, LDS and occupancy of every kernel in `sources` as the compiler
     reports them (-Rpass-analysis=kernel-resource-usage), as a markdown table."""
     import re

@@ -1,0 +1,1208 @@
+// Linear layers of any width with what follows them (see pcsr_train.h): the kernels and their launches for one type.  pcsr_linear_f32.hip,
+// pcsr_linear_bf16.hip and pcsr_linear_f16.hip make them, side by side; pcsr_linear.hip has the entry points.
+//
+// y = r + f act(z), z = x w^T + b, f = 0 or 1 / (1 - p) (pcsr_drop.h).  Backward: dz = f act'(z) dy, dx = dz w, dw = dz^T x,
+// db = the sums of dz's columns (dr = dy).
+//
+// Products D[i][j] = sum over k of P(i, k) Q(j, k) run on the 16-bit matrix instructions, in tiles that go through LDS, summed in
+// fp32.  An operand lies with its k side by side (x and w forward, dz for dx) or with its rows side by side (w for dx, dz and x for dw);
+// the second kind is turned on its way to LDS, where k is always side by side.
+//
+// fp32 numbers are three bf16 numbers each, x = p0 + p1 + p2 exactly (8 bits each), and a product is the six p q of order 2^-16 and more,
+// six instructions of 16 times the fp32 rate (the method: Henry, Tang and Heinecke, "Leveraging the bfloat16 Artificial Intelligence Datatype For
+// Higher-Precision Computations", ARITH 2019).  Numbers are split 2^16 times as large, so that small ones keep all their pieces.  A tile that has
+// met numbers of 2^38 and more (products of which would leave the range; an infinity's pieces are none) is done again in fp32.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "pcsr_act.h"
+#include "pcsr_drop.h"
+#include "pcsr_linear.h"
+#include "pcsr_num.h"
+
+namespace pcsr {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
+constexpr int kT = 256;
+constexpr float kUp = 65536.0f, kDown = 1.0f / (65536.0f * 65536.0f), kHot = 0x1p54f; // 2^38 of a number as it is split
+
+// what an operand's numbers are in LDS
+template <typename T> struct Num {
+    typedef T E;
+    static constexpr int NP = 1, KS = 64; // pieces, numbers of k in a stage: 128 bytes a row
+};
+template <> struct Num<float> {
+    typedef bfloat_t E;
+    static constexpr int NP = 3, KS = 32;
+};
+
+typedef half_t h8 __attribute__((ext_vector_type(8)));
+typedef bfloat_t b8 __attribute__((ext_vector_type(8)));
+// 16x16x32: lane l holds A[i = l % 16][k = 8 (l / 16) ..] and B[k][j = l % 16] likewise; D[i = 4 (l / 16) + r][j = l % 16]
+__device__ __forceinline__ f4 mfma(half_t, u4 a, u4 b, f4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f4 mfma(bfloat_t, u4 a, u4 b, f4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+
+struct Side { // an operand: number (row, k) is at[row * ld + k], turned: at[k * ld + row]
+    const void *at;
+    int64_t ld, n; // rows
+};
+template <typename T, bool TURN> __device__ __forceinline__ float number(const Side &s, int64_t row, int64_t k)
+{
+    const T *p = static_cast<const T *>(s.at);
+    return (float)(TURN ? p[k * s.ld + row] : p[row * s.ld + k]);
+}
+
+// ---------------------------------------------------------------------------------- what follows a product
+struct Tail {
+    const void *bias, *residual;
+    void *y, *slope;              // slope: null, or act'(z) as the backward pass reads it
+    int64_t r_stride, rows, cols; // of y and slope, whose rows lie one behind the other
+    int act, bias_type;
+    Drop drop;
+};
+
+// Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 of them to 1 (0 and 1 are exact, others are 2^-16 off at
+// most, a 32nd of what fp16 rounds gradients of their size by; slopes are between -0.13 and 1.13, and 0 stands for none).  Kept in place of z: a
+// slope costs three operations beside the activation and forty apart from it.
+template <typename T> struct Slope {
+    typedef uint16_t type;
+    static __device__ __forceinline__ uint16_t put(float s) { return (uint16_t)(uint32_t)__builtin_fmaf(s, 32768.0f, 8192.5f); } // (of no number 0)
+    static __device__ __forceinline__ float take(uint16_t q) { return q ? __builtin_fmaf((float)q, 1.0f / 32768.0f, -0.25f) : __builtin_nanf(""); }
+};
+template <> struct Slope<float> {
+    typedef float type;
+    static __device__ __forceinline__ float put(float s) { return s; }
+    static __device__ __forceinline__ float take(float s) { return s; }
+};
+
+// 8 numbers of x w^T at a row and a column that is a multiple of 8, m of them there (WHOLE: all); bias: theirs; r: the residual's (RES)
+template <typename T, bool WHOLE, bool RES>
+__device__ __forceinline__ void put8(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8], const float (&bias)[8], const float (&r)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
+    if (a.slope) {
+        typedef typename Slope<T>::type S;
+        float f[8];
+        activate_for<sizeof(T) == 2, true>(v, f, a.act);
+        S *to = static_cast<S *>(a.slope) + row * a.cols + c;
+        typename Pack<S, 8>::type q;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = Slope<T>::put(f[i]);
+        if (WHOLE || m >= 8) {
+            *reinterpret_cast<typename Pack<S, 8>::type *>(to) = q;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < m) to[i] = q[i];
+        }
+    } else {
+        float none[8];
+        activate_for<sizeof(T) == 2, false>(v, none, a.act);
+    }
+    if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, v);
+    if (RES)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    T *to = static_cast<T *>(a.y) + row * a.cols + c;
+    if (WHOLE) store<T, 8>(to, v);
+    else store_upto<T, 8>(to, m, v);
+}
+template <typename T, bool WHOLE> __device__ __forceinline__ void bias8(const Tail &a, int64_t c, int m, float (&b)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+    if (a.bias && m > 0) {
+        if (a.bias_type == PCSR_F32) load_upto<float, 8>(static_cast<const float *>(a.bias) + c, WHOLE ? 8 : m, b);
+        else load_upto<T, 8>(static_cast<const T *>(a.bias) + c, WHOLE ? 8 : m, b);
+    }
+}
+// any place, on its own
+template <typename T> __device__ __forceinline__ void put_one(const Tail &a, const DropKey &key, int64_t row, int64_t c, int m, float (&v)[8])
+{
+    float b[8], r[8];
+    bias8<T, false>(a, c, m, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = 0.0f;
+    if (a.residual) load_upto<T, 8>(static_cast<const T *>(a.residual) + row * a.r_stride + c, m, r);
+    put8<T, false, true>(a, key, row, c, m, v, b, r);
+}
+
+// ---------------------------------------------------------------------------------- operands on their way to LDS
+// A row's 16-byte chunks of k are exchanged by bits of its number, so that rows read side by side lie in different banks, and so do chunks of one k
+// written for many rows.
+template <int KS> __device__ __forceinline__ int place(int row, int chunk)
+{
+    const int turn = KS == 64 ? (row ^ row >> 3) & 7 : row >> 2 & 3;
+    return (row * (KS / 8) + (chunk ^ turn)) * 16;
+}
+
+__device__ __forceinline__ uint32_t two(bfloat_t a, bfloat_t b)
+{
+    return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+}
+// two numbers side by side in k, in pieces
+__device__ __forceinline__ void pieces(float x, float y, float &hot, uint32_t (&p)[3])
+{
+    x *= kUp, y *= kUp;
+    hot = __builtin_fmaxf(hot, __builtin_fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)));
+#pragma unroll
+    for (int o = 0; o < 3; ++o) {
+        const bfloat_t a = (bfloat_t)x, b = (bfloat_t)y;
+        p[o] = two(a, b);
+        if (o < 2) x -= (float)a, y -= (float)b;
+    }
+}
+
+// R rows of KS numbers of k
+template <typename T, bool TURN, int R, int THREADS> struct Loader {
+    static constexpr int KS = Num<T>::KS, NP = Num<T>::NP, N = kPer16<T>;
+    // a unit: 8 numbers of a row, or turned 4 of k in N rows
+    static constexpr int across = TURN ? R / N : KS / 8, units = TURN ? R / N * (KS / 4) : R * (KS / 8), U = (units + THREADS - 1) / THREADS;
+    static constexpr int parts = TURN ? 4 : 8 / N;
+    static constexpr bool whole = units % THREADS == 0;
+    typedef typename Pack<T, N>::type Raw;
+    Raw raw[U][parts];
+
+    __device__ __forceinline__ void fetch(const Side &s, int64_t row0, int64_t k0, int64_t k1, int tid)
+    {
+        const T *base = static_cast<const T *>(s.at);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = tid + u * THREADS;
+            if (!whole && id >= units) break;
+            if (TURN) {
+                const int64_t row = row0 + id % across * N, k = k0 + id / across * 4;
+                const int m = s.n - row >= N ? N : s.n > row ? (int)(s.n - row) : 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const T *p = base + (k + q) * s.ld + row;
+                    if (k + q < k1 && m == N) raw[u][q] = *reinterpret_cast<const Raw *>(p);
+                    else
+#pragma unroll
+                        for (int i = 0; i < N; ++i) raw[u][q][i] = k + q < k1 && i < m ? p[i] : (T)0.0f;
+                }
+            } else {
+                int64_t row = row0 + id / across;
+                row = row < s.n ? row : s.n - 1; // what comes of it is not stored
+                const int64_t k = k0 + id % across * 8;
+                const T *p = base + row * s.ld + k;
+                if (k + 8 <= k1) {
+#pragma unroll
+                    for (int q = 0; q < parts; ++q) raw[u][q] = *reinterpret_cast<const Raw *>(p + q * N);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < parts; ++q)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) raw[u][q][i] = k + q * N + i < k1 ? p[q * N + i] : (T)0.0f;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char *lds, float &hot, int tid) const
+    {
+        constexpr int plane = R * KS * 2;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = tid + u * THREADS;
+            if (!whole && id >= units) break;
+            if constexpr (TURN) {
+                const int row = id % across * N, kg = id / across;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    char *to = lds + place<KS>(row + i, kg >> 1) + (kg & 1) * 8;
+                    if constexpr (NP == 3) {
+                        uint32_t a[3], b[3];
+                        pieces(raw[u][0][i], raw[u][1][i], hot, a);
+                        pieces(raw[u][2][i], raw[u][3][i], hot, b);
+#pragma unroll
+                        for (int o = 0; o < 3; ++o) *reinterpret_cast<u2 *>(to + o * plane) = u2{a[o], b[o]};
+                    } else {
+                        typedef T t4 __attribute__((ext_vector_type(4)));
+                        const t4 v = {raw[u][0][i], raw[u][1][i], raw[u][2][i], raw[u][3][i]};
+                        *reinterpret_cast<t4 *>(to) = v;
+                    }
+                }
+            } else {
+                char *to = lds + place<KS>(id / across, id % across);
+                if constexpr (NP == 3) {
+                    uint32_t a[4][3];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) pieces(raw[u][q >> 1][(q & 1) * 2], raw[u][q >> 1][(q & 1) * 2 + 1], hot, a[q]);
+#pragma unroll
+                    for (int o = 0; o < 3; ++o) *reinterpret_cast<u4 *>(to + o * plane) = u4{a[0][o], a[1][o], a[2][o], a[3][o]};
+                } else {
+                    *reinterpret_cast<u4 *>(to) = __builtin_bit_cast(u4, raw[u][0]);
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------- tiles
+struct TileArgs {
+    Side p, q;
+    int64_t K, stretch; // stretch: of k, for a workgroup
+    int tiles_i, tiles_j, stretches;
+    float *part; // [stretch][rows][cols] sums, null: whole sums, for `tail`
+    Tail tail;
+};
+
+template <int BI_, int BJ_, int WI_, int WJ_, int PER_ = 1> struct Tiling { // PER: wavefronts to a SIMD at least
+    static constexpr int per = PER_, BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, threads = 64 * WI * WJ, FI = BI / 16 / WI, FJ = BJ / 16 / WJ;
+};
+typedef Tiling<128, 128, 2, 2> Wide;
+typedef Tiling<128, 64, 2, 2> Tall;
+typedef Tiling<64, 128, 2, 2> Flat;
+typedef Tiling<64, 64, 2, 2> Small;
+typedef Tiling<256, 256, 2, 4, 2> Large;
+typedef Tiling<128, 128, 2, 2, 2> StraightWide;
+typedef Tiling<128, 64, 2, 2, 2> StraightTall;
+typedef Tiling<64, 128, 2, 2, 2> StraightFlat;
+
+// A workgroup's tile and stretch of k.  Workgroups are dealt to the 8 dies one by one, each with an L2 of its own: a die takes a run of tiles in
+// blocks of four rows (32 of them read 12 strips of operands, side by side in one row 33), and the tiles of a stretch one after the other.
+__device__ __forceinline__ void place_of(const TileArgs &a, int *ti, int *tj, int *stretch)
+{
+    const int tiles = a.tiles_i * a.tiles_j, all = tiles * a.stretches, per = all / 8, b = blockIdx.x;
+    const int t = b < per * 8 ? (b & 7) * per + (b >> 3) : b;
+    *stretch = t / tiles;
+    const int r = t - *stretch * tiles, block = r / (4 * a.tiles_j), in = r - block * 4 * a.tiles_j, n = a.tiles_i - block * 4 < 4 ? a.tiles_i - block * 4 : 4;
+    *tj = in / n, *ti = block * 4 + in - *tj * n;
+}
+
+
+template <typename C> using Sums = f4[C::FI][C::FJ];
+
+// Products of 32 numbers of k in pieces, with tiles side by side so that an instruction does not wait for the one before it.  They have a sum of
+// their own, small ones first: the matrix instructions cut off what does not reach a sum's last bit, always downwards.
+template <int N> __device__ __forceinline__ void products32(const u4 (&x)[3], const u4 (&y)[N][3], f4 (&s)[N])
+{
+    constexpr int P[6] = {2, 0, 1, 1, 0, 0}, Q[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int o = 0; o < 6; ++o)
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = mfma(bfloat_t(), x[P[o]], y[j][Q[o]], s[j]);
+}
+// 8 columns of a row in fp32, where pieces would leave the range
+template <typename T, bool TP, bool TQ>
+__device__ __forceinline__ void once_more(const TileArgs &a, int64_t row, int64_t col, int m, int64_t k0, int64_t k1, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+#pragma unroll 1
+    for (int64_t k = k0; k < k1; ++k) {
+        const float x = number<T, TP>(a.p, row, k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < m) v[e] = __builtin_fmaf(x, number<T, TQ>(a.q, col + e, k), v[e]);
+    }
+}
+
+// What becomes of a tile's sums.  They go through LDS, G times 16 rows of a wavefront at a time, so that a lane has 8 columns side by side: whole lines
+// of y, and what one call of the generator is for.  again: the numbers are added up once more, in fp32.
+template <typename C, int G> constexpr int out_bytes() { return C::WI * C::WJ * G * 16 * (C::FJ * 16 + 4) * 4; }
+
+struct Where { // of a wavefront's sums
+    int64_t i0, col; // first row, a lane's column
+    int m;           // columns that are there from it on
+    int64_t k0, k1;
+    int stretch;
+    bool again;
+};
+// The rows that lie in LDS.  WHOLE: 8 columns are there or none.  RES: residuals come four rows ahead, since each is a round trip to memory.
+template <typename T, bool TP, bool TQ, int ROWS, int LD, int PER, bool WHOLE, bool RES>
+__device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &key, const Where &w, const float *own, const float (&bias)[8])
+{
+    constexpr int NP = Num<T>::NP, step = 64 / PER, passes = ROWS / step, A = RES ? (passes < 4 ? passes : 4) : 1;
+    const int lane = threadIdx.x & 63, r0 = lane / PER, c = lane % PER * 8;
+    if (w.m <= 0) return;
+#pragma unroll 1
+    for (int n = 0; n < passes; n += A) {
+        float res[A][8];
+        if (RES)
+#pragma unroll
+            for (int u = 0; u < A; ++u) {
+                const int64_t r = w.i0 + r0 + (n + u) * step, row = r < a.tail.rows ? r : a.tail.rows - 1;
+                const T *p = static_cast<const T *>(a.tail.residual) + row * a.tail.r_stride + w.col;
+                if (WHOLE) load<T, 8>(p, res[u]);
+                else load_upto<T, 8>(p, w.m, res[u]);
+            }
+#pragma unroll
+        for (int u = 0; u < A; ++u) {
+            const int r = r0 + (n + u) * step;
+            const int64_t row = w.i0 + r;
+            float v[8];
+            const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = NP == 3 ? lo[e] * kDown : lo[e];
+                v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
+            }
+            if (row < a.tail.rows) {
+                if (NP == 3 && w.again) once_more<T, TP, TQ>(a, row, w.col, w.m, w.k0, w.k1, v);
+                if (!a.part) {
+                    put8<T, WHOLE, RES>(a.tail, key, row, w.col, w.m, v, bias, res[u]);
+                } else {
+                    float *to = a.part + (w.stretch * a.tail.rows + row) * a.tail.cols + w.col;
+                    if (WHOLE) store<float, 8>(to, v);
+                    else store_upto<float, 8>(to, w.m, v);
+                }
+            }
+        }
+    }
+}
+template <typename T, bool TP, bool TQ, typename C, int G>
+__device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &sum, char *lds, int64_t i0, int64_t j0, int64_t k0, int64_t k1, int stretch, bool again)
+{
+    constexpr int FI = C::FI, FJ = C::FJ, LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
+    static_assert(FI % G == 0, "whole passes");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / C::WJ, wj = wave % C::WJ, at = lane & 15, chunk = lane >> 4;
+    float *own = reinterpret_cast<float *>(lds) + wave * G * 16 * LD;
+    DropKey key = {};
+    if (!a.part && a.tail.drop.threshold) {
+        key = key_of(a.tail.drop);
+        if (blockIdx.x == 0 && threadIdx.x == 0) tell_key(a.tail.drop, key);
+    }
+    const bool whole = a.tail.cols % 8 == 0, res = a.tail.residual && !a.part;
+    Where w = {0, j0 + wj * FJ * 16 + lane % per * 8, 0, k0, k1, stretch, again};
+    w.m = a.tail.cols - w.col >= 8 ? 8 : a.tail.cols > w.col ? (int)(a.tail.cols - w.col) : 0;
+    float bias[8];
+    bias8<T, false>(a.tail, w.col, a.part ? 0 : w.m, bias);
+    const auto pass = [&](auto g) { // (written out, not unrolled: loops of this length are not)
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[(i * 16 + chunk * 4 + e) * LD + j * 16 + at] = sum[g * G + i][j][e];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        w.i0 = i0 + (wi * FI + g * G) * 16;
+        if (whole && res) finish_rows<T, TP, TQ, G * 16, LD, per, true, true>(a, key, w, own, bias);
+        else if (whole) finish_rows<T, TP, TQ, G * 16, LD, per, true, false>(a, key, w, own, bias);
+        else if (res) finish_rows<T, TP, TQ, G * 16, LD, per, false, true>(a, key, w, own, bias);
+        else finish_rows<T, TP, TQ, G * 16, LD, per, false, false>(a, key, w, own, bias);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    static_assert(FI / G <= 2, "two passes at most");
+    pass(std::integral_constant<int, 0>());
+    if constexpr (FI / G == 2) pass(std::integral_constant<int, 1>());
+}
+
+template <typename T, typename C> constexpr int lds_bytes()
+{
+    constexpr int stage = (C::BI + C::BJ) * Num<T>::KS * 2 * Num<T>::NP, out = out_bytes<C, 2>();
+    return stage > out ? stage : out;
+}
+
+// Any operands.  They go through registers to LDS.
+template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads) tile_kernel(TileArgs a)
+{
+    typedef typename Num<T>::E E;
+    constexpr int KS = Num<T>::KS, NP = Num<T>::NP, FI = C::FI, FJ = C::FJ;
+    constexpr int planeP = C::BI * KS * 2, planeQ = C::BJ * KS * 2;
+    __shared__ __align__(16) char lds[lds_bytes<T, C>()];
+    __shared__ int met;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
+    int ti, tj, stretch;
+    place_of(a, &ti, &tj, &stretch);
+    const int64_t i0 = (int64_t)ti * C::BI, j0 = (int64_t)tj * C::BJ;
+    const int64_t k0 = (int64_t)stretch * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
+    if (tid == 0) met = 0;
+    f4 sum[FI][FJ];
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    float hot = 0.0f;
+    Loader<T, TP, C::BI, C::threads> lp;
+    Loader<T, TQ, C::BJ, C::threads> lq;
+    char *ldsP = lds, *ldsQ = lds + NP * planeP;
+    lp.fetch(a.p, i0, k0, k1, tid);
+    lq.fetch(a.q, j0, k0, k1, tid);
+    const int at = lane & 15, chunk = lane >> 4;
+    for (int64_t k = k0; k < k1; k += KS) {
+        lp.put(ldsP, hot, tid);
+        lq.put(ldsQ, hot, tid);
+        __syncthreads();
+        if (k + KS < k1) {
+            lp.fetch(a.p, i0, k + KS, k1, tid);
+            lq.fetch(a.q, j0, k + KS, k1, tid);
+        }
+#pragma unroll
+        for (int kk = 0; kk < KS / 32; ++kk) {
+            u4 x[FI][NP], y[FJ][NP];
+#pragma unroll
+            for (int o = 0; o < NP; ++o) {
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+                    x[i][o] = *reinterpret_cast<const u4 *>(ldsP + o * planeP + place<KS>((wi * FI + i) * 16 + at, kk * 4 + chunk));
+#pragma unroll
+                for (int j = 0; j < FJ; ++j)
+                    y[j][o] = *reinterpret_cast<const u4 *>(ldsQ + o * planeQ + place<KS>((wj * FJ + j) * 16 + at, kk * 4 + chunk));
+            }
+#pragma unroll
+            for (int i = 0; i < FI; ++i) {
+                if constexpr (NP == 3) {
+                    f4 part[FJ];
+                    products32<FJ>(x[i], y, part);
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) sum[i][j] += part[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < FJ; ++j) sum[i][j] = mfma(E(), x[i][0], y[j][0], sum[i][j]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    bool again = false;
+    if constexpr (NP == 3) {
+        if (hot >= kHot) met = 1; // (a NaN needs nothing: its pieces are NaN)
+        __syncthreads();
+        again = met;
+    }
+    finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, again);
+}
+
+// ---------------------------------------------------------------------------------- 16-bit numbers straight to LDS
+// Tiles of operands whose rows are whole 16-byte pieces.  Pieces go from memory straight to LDS, two stages of 64 numbers of k, one of them on its way while
+// the other is multiplied.  A load of a wavefront fills 1 KB.
+//
+// k side by side: 128 bytes a row, whose 8 pieces are exchanged by the row's number so that 8 rows read together lie in different banks.
+// Rows side by side: [k][rows], turned by the LDS reads that do so: 16 lanes give the addresses of 4 numbers each, 16 rows of 4 k, and each gets the 4 k of
+// one row.  A lane's k is 32 kk + 8 g + 4 h + r; kilobytes are numbered by r, g and kk, as far as that goes, and lie 1056 bytes apart: so
+// the four k of a read lie in different banks, and what an instruction reads is at a distance from the lane's first address that does not depend on the lane.
+template <typename T, bool TURN, int R, int THREADS> struct Straight {
+    static constexpr int KS = 64, blocks = R / 8, waves = THREADS / 64, loads = blocks / waves, apart = TURN ? 1056 : 1024, bytes = blocks * apart;
+    static_assert(blocks % waves == 0, "whole loads");
+    uint32_t off[loads]; // bytes from the tile's first number
+    const char *base;
+    int64_t step;
+
+    // k of a lane's piece in a block, and the row
+    static __device__ __forceinline__ int k_of(int block, int lane)
+    {
+        if (!TURN) return ((lane & 7) ^ (lane >> 3)) * 8;
+        const int in = lane / (R / 8), t = block + blocks * (in >> 1);
+        return (t >> 4) * 32 + (t >> 2 & 3) * 8 + (in & 1) * 4 + (t & 3);
+    }
+    static __device__ __forceinline__ int row_of(int block, int lane) { return TURN ? lane % (R / 8) * 8 : block * 8 + (lane >> 3); }
+
+    __device__ __forceinline__ void begin(const Side &s, int64_t row0, int64_t k0, int lane, int wave)
+    {
+        base = static_cast<const char *>(s.at) + (TURN ? k0 * s.ld + row0 : row0 * s.ld + k0) * 2;
+        step = (TURN ? KS * s.ld : KS) * 2;
+#pragma unroll
+        for (int u = 0; u < loads; ++u) {
+            const int block = u * waves + wave, k = k_of(block, lane), r = row_of(block, lane);
+            const int64_t last = (TURN ? (s.n - 1) / 8 * 8 : s.n - 1) - row0, row = r < last ? r : last; // what comes of rows behind the last is not stored
+            off[u] = (uint32_t)((TURN ? k * s.ld + row : row * s.ld + k) * 2);
+        }
+    }
+    // loads of the stage that `base` is at; left: numbers of k that there are
+    __device__ __forceinline__ void fetch(char *lds, int64_t left, int lane, int wave) const
+    {
+        typedef __attribute__((address_space(3))) void *Lds;
+        typedef __attribute__((address_space(1))) const void *Global;
+        if (left >= KS) {
+#pragma unroll
+            for (int u = 0; u < loads; ++u)
+                __builtin_amdgcn_global_load_lds((Global)(base + off[u]), (Lds)(lds + (u * waves + wave) * apart), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int u = 0; u < loads; ++u) {
+                char *to = lds + (u * waves + wave) * apart;
+                if (k_of(u * waves + wave, lane) < left) __builtin_amdgcn_global_load_lds((Global)(base + off[u]), (Lds)to, 16, 0, 0);
+                else *reinterpret_cast<u4 *>(to + lane * 16) = u4{0, 0, 0, 0};
+            }
+        }
+    }
+    __device__ __forceinline__ void next() { base += step; }
+    // numbers of k from 32 kk + 8 (lane / 16) on, of row 16 f + lane % 16
+    static __device__ __forceinline__ u4 read(const char *lds, int f, int kk, int lane)
+    {
+        if constexpr (TURN) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 *At;
+            const int t = (lane >> 4) * 4 + (lane >> 2 & 3); // r + 4 g
+            const char *p = lds + t % blocks * apart + t / blocks * (4 * R) + (lane & 3) * 8; // this lane's 4 of 16 rows
+            p += kk * (blocks > 16 ? 16 * apart : 16 / blocks * 4 * R) + f * 32;
+            const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)p));
+            const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p + 2 * R)));
+            return u4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            return *reinterpret_cast<const u4 *>(lds + (f * 16 + (lane & 15)) * 128 + ((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16);
+        }
+    }
+};
+
+template <bool TP, bool TQ, typename C> constexpr int straight_bytes()
+{
+    constexpr int stages = 2 * (Straight<half_t, TP, C::BI, C::threads>::bytes + Straight<half_t, TQ, C::BJ, C::threads>::bytes);
+    constexpr int out = out_bytes<C, C::FI < 4 ? C::FI : 4>();
+    return stages > out ? stages : out;
+}
+// The next numbers are read from LDS while those before are multiplied, and a stage's loads are given out when all wavefronts have read the one
+// before it, which is half a stage before they multiply its last numbers.
+template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) straight_kernel(TileArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    typedef Straight<T, TP, C::BI, C::threads> P;
+    typedef Straight<T, TQ, C::BJ, C::threads> Q;
+    constexpr int FI = C::FI, FJ = C::FJ, stage = P::bytes + Q::bytes;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
+    int ti, tj, stretch;
+    place_of(a, &ti, &tj, &stretch);
+    const int64_t i0 = (int64_t)ti * C::BI, j0 = (int64_t)tj * C::BJ;
+    const int64_t k0 = (int64_t)stretch * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
+    P p;
+    Q q;
+    p.begin(a.p, i0, k0, lane, wave);
+    q.begin(a.q, j0, k0, lane, wave);
+    const int steps = (int)((k1 - k0 + 63) / 64);
+    int64_t left = k1 - k0;
+    const auto fetch = [&](int s) {
+        char *to = lds + (s & 1) * stage;
+        p.fetch(to, left, lane, wave);
+        q.fetch(to + P::bytes, left, lane, wave);
+        p.next(), q.next(), left -= 64;
+    };
+    const auto all_here = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    Sums<C> sum;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    // A stage in units of GI x FJ products of 16 x 16 x 32; the numbers of a unit are read while the one before is multiplied.
+    constexpr int GI = FI < 4 ? FI : 4, per = FI / GI, units = 2 * per;
+    u4 x[2][GI], y[2][FJ];
+    const auto read = [&](int s, int u) {
+        const char *from = lds + (s & 1) * stage;
+        if (u % per == 0)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) y[u / per][j] = Q::read(from + P::bytes, wj * FJ + j, u / per, lane);
+#pragma unroll
+        for (int i = 0; i < GI; ++i) x[u & 1][i] = P::read(from, wi * FI + u % per * GI + i, u / per, lane);
+    };
+    const auto multiply = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < GI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[u % per * GI + i][j] = mfma(T(), x[u & 1][i], y[u / per][j], sum[u % per * GI + i][j]);
+    };
+    if (steps > 0) {
+        fetch(0);
+        all_here();
+        if (steps > 1) fetch(1);
+        read(0, 0);
+        for (int s = 0; s < steps; ++s) {
+#pragma unroll
+            for (int u = 0; u < units - 1; ++u) {
+                read(s, u + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(u);
+            }
+            all_here(); // stage s has been read, stage s + 1 is there
+            if (s + 2 < steps) fetch(s + 2);
+            if (s + 1 < steps) read(s + 1, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(units - 1);
+        }
+    }
+    __syncthreads(); // all of the last stage is read
+    finish_tile<T, TP, TQ, C, FI < 4 ? FI : 4>(a, sum, lds, i0, j0, k0, k1, stretch, false);
+}
+
+// ---------------------------------------------------------------------------------- many rows and few weights
+// The weights lie in LDS for as long as the workgroup lives, in pieces, and wavefronts take 16 rows at a time, each for itself: a lane's numbers of the next rows
+// are on their way to its registers while these are multiplied, nothing waits for other wavefronts, and x is read once.
+// STEPS: of 32 numbers of k.  FJ tiles of 16 columns at a time.  WHOLE: all of k is there, and of columns 8 or none.  RES: a residual is there.
+// Loads come back in their order, and so do the waits: what a strip's end needs is asked for before the next strip's numbers, and the bias lies in LDS.
+template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64 + 16; } // bytes of a row: 16 rows lie in different banks
+template <typename T, int STEPS> int64_t weights_bytes(int64_t cols) { return Num<T>::NP * up(cols, 64) * 64 * weights_pitch<T, STEPS>(); }
+
+template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global__ void __launch_bounds__(512) rows_kernel(TileArgs a, int groups)
+{
+    typedef typename Num<T>::E E;
+    constexpr int NP = Num<T>::NP, N = kPer16<T>, parts = 8 / N, pitch = weights_pitch<T, STEPS>(), LD = FJ * 16 + 4, per = FJ * 2, passes = (16 * per + 63) / 64;
+    typedef typename Pack<T, N>::type Raw;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int met;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 15, chunk = lane >> 4;
+    const int cols = groups * FJ * 16, plane = cols * pitch;
+    float *biases = reinterpret_cast<float *>(lds + NP * plane), *own = biases + cols + wave * 16 * LD;
+    const int64_t rows = a.tail.rows, stride = (int64_t)gridDim.x * 8;
+    const int K = (int)a.K;
+    Raw raw[STEPS][parts];
+    const auto row_at = [&](int64_t strip) {
+        const int64_t r = strip * 16 + at, row = r < rows ? r : rows - 1; // what comes of rows behind the last is not stored
+        return static_cast<const T *>(a.p.at) + row * a.p.ld + chunk * 8;
+    };
+    const auto fetch = [&](const T *p, int t) {
+#pragma unroll
+        for (int q = 0; q < parts; ++q) {
+            const int k = t * 32 + chunk * 8 + q * N, o = t * 32 + q * N;
+            if (WHOLE || k + N <= K) raw[t][q] = *reinterpret_cast<const Raw *>(p + o);
+            else
+#pragma unroll
+                for (int i = 0; i < N; ++i) raw[t][q][i] = k + i < K ? p[o + i] : (T)0.0f;
+        }
+    };
+    int64_t strip = (int64_t)blockIdx.x * 8 + wave;
+    if (strip * 16 < rows) {
+        const T *p = row_at(strip);
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) fetch(p, t);
+    }
+    if (tid == 0) met = 0;
+    __syncthreads();
+    { // weights: a thread takes two numbers of k of a row
+        float hot = 0.0f;
+        for (int id = tid; id < cols * STEPS * 16; id += 512) {
+            const int j = TQ ? id % cols : id / (STEPS * 16), k = (TQ ? id / cols : id % (STEPS * 16)) * 2;
+            T w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                w[e] = j < a.q.n && k + e < K ? static_cast<const T *>(a.q.at)[TQ ? (k + e) * a.q.ld + j : j * a.q.ld + k + e] : (T)0.0f;
+            uint32_t *to = reinterpret_cast<uint32_t *>(lds + j * pitch + k * 2);
+            if constexpr (NP == 3) {
+                uint32_t h[3];
+                pieces(w[0], w[1], hot, h);
+#pragma unroll
+                for (int o = 0; o < 3; ++o) to[o * plane / 4] = h[o];
+            } else {
+                typedef T t2 __attribute__((ext_vector_type(2)));
+                *to = __builtin_bit_cast(uint32_t, t2{w[0], w[1]});
+            }
+        }
+        if (NP == 3 && hot >= kHot) met = 1;
+        for (int j = tid; j < cols; j += 512) {
+            float b = 0.0f;
+            if (a.tail.bias && j < a.tail.cols) b = a.tail.bias_type == PCSR_F32 ? static_cast<const float *>(a.tail.bias)[j] : (float)static_cast<const T *>(a.tail.bias)[j];
+            biases[j] = b;
+        }
+    }
+    __syncthreads();
+    const bool hot_weights = NP == 3 && met;
+    DropKey key = {};
+    if (a.tail.drop.threshold) {
+        key = key_of(a.tail.drop);
+        if (blockIdx.x == 0 && tid == 0) tell_key(a.tail.drop, key);
+    }
+    const char *mine = lds + at * pitch + chunk * 16;
+    const int c = lane % per * 8;
+    float hot = 0.0f;
+    for (; strip * 16 < rows; strip += stride) {
+        const T *next = row_at(strip + stride); // (behind the last rows the last row again)
+        const auto group = [&](int g, auto last) { // last: the next rows are fetched
+            const int64_t col = g * FJ * 16 + c;
+            const int m = a.tail.cols - col >= 8 ? 8 : a.tail.cols > col ? (int)(a.tail.cols - col) : 0;
+            float res[passes][8]; // on its way while the products are taken
+            if (RES)
+#pragma unroll
+                for (int h = 0; h < passes; ++h) {
+                    const int64_t r = strip * 16 + lane / per + h * (64 / per), row = r < rows ? r : rows - 1;
+                    const T *p = static_cast<const T *>(a.tail.residual) + row * a.tail.r_stride;
+                    if (WHOLE) load<T, 8>(p + (m > 0 ? col : 0), res[h]);
+                    else if (m > 0) load_upto<T, 8>(p + col, m, res[h]);
+                }
+            const char *w = mine + g * FJ * 16 * pitch;
+            f4 sum[FJ];
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                u4 x[NP];
+                if constexpr (NP == 3) {
+                    // the compiler is kept from making the pieces of all steps once for all groups: registers do not hold them
+#pragma unroll
+                    for (int q = 0; q < parts; ++q) {
+                        u4 same = __builtin_bit_cast(u4, raw[t][q]);
+                        asm volatile("" : "+v"(same));
+                        raw[t][q] = __builtin_bit_cast(Raw, same);
+                    }
+                    uint32_t h[4][3];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) pieces(raw[t][q >> 1][(q & 1) * 2], raw[t][q >> 1][(q & 1) * 2 + 1], hot, h[q]);
+#pragma unroll
+                    for (int o = 0; o < 3; ++o) x[o] = u4{h[0][o], h[1][o], h[2][o], h[3][o]};
+                } else {
+                    x[0] = __builtin_bit_cast(u4, raw[t][0]);
+                }
+                if (last) fetch(next, t);
+                constexpr int B = NP == 3 ? 2 : FJ; // tiles at a time
+#pragma unroll
+                for (int b = 0; b < FJ; b += B) {
+                    u4 y[B][NP];
+#pragma unroll
+                    for (int j = 0; j < B; ++j)
+#pragma unroll
+                        for (int o = 0; o < NP; ++o) y[j][o] = *reinterpret_cast<const u4 *>(w + o * plane + (b + j) * 16 * pitch + t * 64);
+                    if constexpr (NP == 3) {
+                        f4 part[B];
+                        products32<B>(x, y, part);
+#pragma unroll
+                        for (int j = 0; j < B; ++j) sum[b + j] += part[j];
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < B; ++j) sum[b + j] = mfma(E(), x[0], y[j][0], sum[b + j]);
+                    }
+                }
+                if (NP == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int j = 0; j < FJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[(chunk * 4 + e) * LD + j * 16 + at] = sum[j][e];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            float bias[8];
+            load<float, 8>(biases + col, bias);
+#pragma unroll
+            for (int h = 0; h < passes; ++h) {
+                const int r = lane / per + h * (64 / per);
+                const int64_t row = strip * 16 + r;
+                float v[8];
+                const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = NP == 3 ? lo[e] * kDown : lo[e];
+                    v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
+                }
+                if (m > 0 && row < rows) put8<T, WHOLE, RES>(a.tail, key, row, col, m, v, bias, res[h]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+#pragma unroll 1
+        for (int g = 0; g < groups - 1; ++g) group(g, std::false_type());
+        group(groups - 1, std::true_type());
+    }
+    if (NP == 3 && (hot_weights || __any(hot >= kHot))) // the wavefront's rows with such numbers once more (a loop of its own: the addresses that it needs are kept nowhere else)
+        for (strip = (int64_t)blockIdx.x * 8 + wave; strip * 16 < rows; strip += stride) {
+            float most = 0.0f;
+            for (int k = chunk; k < K; k += 4)
+                if (strip * 16 + at < rows) most = __builtin_fmaxf(most, __builtin_fabsf(number<T, false>(a.p, strip * 16 + at, k)) * kUp);
+            if (!hot_weights && !__any(most >= kHot)) continue;
+            for (int64_t col = c; col < a.tail.cols; col += FJ * 16)
+                for (int r = lane / per; r < 16 && strip * 16 + r < rows; r += 64 / per) {
+                    const int m = a.tail.cols - col >= 8 ? 8 : (int)(a.tail.cols - col);
+                    float v[8];
+                    once_more<T, false, TQ>(a, strip * 16 + r, col, m, 0, a.K, v);
+                    put_one<T>(a.tail, key, strip * 16 + r, col, m, v);
+                }
+        }
+}
+
+// ---------------------------------------------------------------------------------- few rows
+// One to eight rows: bound by reading the weights.  `lanes` lanes take a row of them, 16 bytes each at a time, add up its products with all R rows of x in fp32,
+// and put their sums together; of the lanes that then have them, lane r ends row r.
+template <typename T, int R> __global__ void __launch_bounds__(kT) few_kernel(TileArgs a, int lanes)
+{
+    constexpr int N = kPer16<T>, A = R <= 2 ? 4 : 2; // loads on their way
+    const int lane = threadIdx.x % lanes, rows = (int)a.tail.rows;
+    const int64_t col = (int64_t)blockIdx.x * (kT / lanes) + threadIdx.x / lanes;
+    DropKey key = {};
+    if (a.tail.drop.threshold) {
+        key = key_of(a.tail.drop);
+        if (blockIdx.x == 0 && threadIdx.x == 0) tell_key(a.tail.drop, key);
+    }
+    const bool there = col < a.tail.cols;
+    const T *w = static_cast<const T *>(a.q.at) + (there ? col : 0) * a.q.ld, *x = static_cast<const T *>(a.p.at);
+    float sum[R] = {};
+    const int64_t step = (int64_t)lanes * N, whole = a.K / step * step;
+    const auto take = [&](const float (&y)[N], int64_t k, int m) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float v[N];
+            load_upto<T, N>(x + (r < rows ? r : 0) * a.p.ld + k, m, v);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (m >= N || i < m) sum[r] = __builtin_fmaf(y[i], v[i], sum[r]);
+        }
+    };
+    int64_t k = lane * N;
+    for (; k + (A - 1) * step < whole; k += A * step) {
+        float y[A][N];
+#pragma unroll
+        for (int u = 0; u < A; ++u) load<T, N>(w + k + u * step, y[u]);
+#pragma unroll
+        for (int u = 0; u < A; ++u) take(y[u], k + u * step, N);
+    }
+    for (; k < a.K; k += step) {
+        const int m = a.K - k < N ? (int)(a.K - k) : N;
+        float y[N];
+        load_upto<T, N>(w + k, m, y);
+        take(y, k, m);
+    }
+    for (int o = lanes / 2; o > 0; o /= 2)
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum[r] += __shfl_xor(sum[r], o);
+    if (lane >= rows || !there) return;
+    float v[1] = {sum[0]}, f[1];
+#pragma unroll
+    for (int r = 1; r < R; ++r) v[0] = lane == r ? sum[r] : v[0];
+    const Tail &t = a.tail;
+    const int64_t at = lane * t.cols + col;
+    if (t.bias) v[0] += t.bias_type == PCSR_F32 ? static_cast<const float *>(t.bias)[col] : (float)static_cast<const T *>(t.bias)[col];
+    activate_for<sizeof(T) == 2, true>(v, f, t.act);
+    if (t.slope) static_cast<typename Slope<T>::type *>(t.slope)[at] = Slope<T>::put(f[0]);
+    if (t.drop.threshold) {
+        uint32_t b[4];
+        philox(key, (uint32_t)(col >> 3), (uint32_t)lane, b);
+        const int e = col & 7;
+        const uint32_t word = e < 4 ? (e < 2 ? b[0] : b[1]) : (e < 6 ? b[2] : b[3]), bits = e & 1 ? word >> 16 : word & 0xffffu;
+        v[0] = bits >= t.drop.threshold ? v[0] * t.drop.keep : 0.0f;
+    }
+    if (t.residual) v[0] += (float)static_cast<const T *>(t.residual)[lane * t.r_stride + col];
+    static_cast<T *>(t.y)[at] = (T)v[0];
+}
+
+// Sums of the stretches of k and what follows.  A workgroup takes `across` places of 8 columns; of its threads kT / across share a place and take
+// every so-manieth stretch each, and their sums are added up in order.
+template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(const float *part, int stretches, Tail a, uint32_t groups, int across)
+{
+    __shared__ float sums[kT][9];
+    const int lane = threadIdx.x % across, q = threadIdx.x / across, beside = kT / across;
+    const int64_t t = (int64_t)blockIdx.x * across + lane, row = t / groups, c = (t - row * groups) * 8;
+    DropKey key = {};
+    if (a.drop.threshold) {
+        key = key_of(a.drop);
+        if (t == 0 && q == 0) tell_key(a.drop, key);
+    }
+    const int m = a.cols - c < 8 ? (int)(a.cols - c) : 8;
+    float v[8] = {};
+    if (row < a.rows)
+#pragma unroll 4
+        for (int s = q; s < stretches; s += beside) {
+            float x[8];
+            load_upto<float, 8>(part + (s * a.rows + row) * a.cols + c, m, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += x[i];
+        }
+    if (beside > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = v[i];
+        __syncthreads();
+        if (q) return;
+        for (int p = 1; p < beside; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += sums[p * across + lane][i];
+    }
+    if (row < a.rows) put_one<T>(a, key, row, c, m, v);
+}
+
+// ---------------------------------------------------------------------------------- gradient at z
+struct SlopeArgs {
+    const void *dy, *slope;
+    int64_t dy_stride, rows, cols, ld; // ld: of dz
+    void *dz;                          // null: sums alone
+    float *sums;                       // [workgroup][cols], null: none
+    int lanes;                         // to a row
+    Drop drop;
+};
+constexpr int kSlopeT = 1024, kSlopeBlocks = 512; // two workgroups a compute unit: as many sums as sums_kernel adds up in 6 us
+
+// dz = f act'(z) dy, and sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows.
+template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(SlopeArgs a)
+{
+    typedef typename Slope<T>::type S;
+    __shared__ float part[kSlopeT][9];
+    const int lane = threadIdx.x % a.lanes, r = threadIdx.x / a.lanes, per = kSlopeT / a.lanes;
+    const int64_t c = ((int64_t)blockIdx.y * a.lanes + lane) * 8;
+    const int m = a.cols - c >= 8 ? 8 : a.cols > c ? (int)(a.cols - c) : 0;
+    DropKey key = {};
+    if (a.drop.threshold) key = key_of(a.drop);
+    float sum[8] = {};
+    if (m > 0)
+#pragma unroll 2
+        for (int64_t row = (int64_t)blockIdx.x * per + r; row < a.rows; row += (int64_t)gridDim.x * per) { // workgroups side by side
+            float d[8];
+            load_upto<T, 8>(static_cast<const T *>(a.dy) + row * a.dy_stride + c, m, d);
+            if (a.slope) {
+                const S *at = static_cast<const S *>(a.slope) + row * a.cols + c;
+                typename Pack<S, 8>::type q;
+                if (m >= 8) {
+                    q = *reinterpret_cast<const typename Pack<S, 8>::type *>(at);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[i] = i < m ? at[i] : (S)0;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= Slope<T>::take(q[i]);
+            }
+            if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += d[i]; // (behind the end 0 times something)
+            if (a.dz) store_upto<T, 8>(static_cast<T *>(a.dz) + row * a.ld + c, m, d);
+        }
+    if (!a.sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[threadIdx.x][i] = sum[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < a.lanes * 8; t += kSlopeT) {
+        float s = 0.0f;
+        for (int q = 0; q < per; ++q) s += part[q * a.lanes + t / 8][t % 8];
+        const int64_t col = (int64_t)blockIdx.y * a.lanes * 8 + t;
+        if (col < a.cols) a.sums[blockIdx.x * a.cols + col] = s;
+    }
+}
+// db: 16 columns to a workgroup, 64 threads to a column
+__global__ void __launch_bounds__(1024) sums_kernel(const float *sums, int64_t blocks, int64_t cols, int type, void *db)
+{
+    __shared__ double part[64][17];
+    const int lane = threadIdx.x & 15, q = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + lane;
+    double s = 0.0;
+    if (c < cols)
+#pragma unroll 8
+        for (int64_t b = q; b < blocks; b += 64) s += (double)sums[b * cols + c];
+    part[q][lane] = s;
+    __syncthreads();
+    if (q || c >= cols) return;
+    for (int p = 1; p < 64; ++p) s += part[p][lane];
+    const float v = (float)s;
+    if (type == PCSR_F32) static_cast<float *>(db)[c] = v;
+    else if (type == PCSR_BF16) static_cast<bfloat_t *>(db)[c] = (bfloat_t)v;
+    else static_cast<half_t *>(db)[c] = (half_t)v;
+}
+
+// ---------------------------------------------------------------------------------- launches
+int64_t round16(int64_t n) { return up(n, 16) * 16; }
+
+// Whether an operand's pieces can go straight to LDS: 16-byte rows, or, with its rows side by side, runs of rows; of places that 32 bits reach.
+// padded: rows behind the last one can be read up to a whole piece.
+template <typename T> bool straight(const Side &s, bool turned, bool padded)
+{
+    return sizeof(T) == 2 && s.ld % 8 == 0 && (uintptr_t)s.at % 16 == 0 && s.ld < (1 << 22) && (!turned || s.n % 8 == 0 || padded);
+}
+
+// How a product of I x J numbers over K is cut.  The widest tiles that the result fills; where they are too few for the chip k is cut into
+// stretches, whose sums go through memory, and where it is too short for that tiles are of 64 x 64.
+struct Plan {
+    int which; // tiling
+    int64_t tiles_i, tiles_j, stretch;
+    int stretches;
+};
+enum { WIDE, TALL, FLAT, SMALL, LARGE };
+template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct)
+{
+    constexpr int64_t kWanted = 512; // workgroups: two to a compute unit
+    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI, Large::BI}, BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ, Large::BJ};
+    Plan p;
+    const int64_t stages = up(K, Num<T>::KS), most = stages / 4 < 1 ? 1 : stages / 4;
+    int64_t wanted = kWanted;
+    p.which = (I <= 64 ? FLAT : WIDE) + (J <= 64 ? 1 : 0);
+    if (direct && I > 128 && J > 128 && up(I, 256) * up(J, 256) * most >= 192) p.which = LARGE, wanted = 256;
+    if (up(I, BI[p.which]) * up(J, BJ[p.which]) * most < 256 && p.which != LARGE) p.which = SMALL;
+    p.tiles_i = up(I, BI[p.which]), p.tiles_j = up(J, BJ[p.which]);
+    const int64_t tiles = p.tiles_i * p.tiles_j;
+    int64_t s = tiles >= wanted ? 1 : wanted / (tiles ? tiles : 1);
+    if (s > most) s = most;
+    p.stretch = up(stages, s) * Num<T>::KS;
+    p.stretches = (int)(K ? up(K, p.stretch) : 1);
+    return p;
+}
+int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
+
+template <typename T, bool TP, bool TQ, typename C> int launch_straight(const TileArgs &a, unsigned grid, hipStream_t stream)
+{
+    constexpr int bytes = straight_bytes<TP, TQ, C>();
+    if (!allow_lds(&straight_kernel<T, TP, TQ, C>, bytes)) return PCSR_E_HIP;
+    hipLaunchKernelGGL((straight_kernel<T, TP, TQ, C>), dim3(grid), dim3(C::threads), bytes, stream, a);
+    return PCSR_OK;
+}
+// Many rows and few weights: what rows_kernel takes.  Weights of up to 104 KB, so that two workgroups or one of eight wavefronts fit with their own rows' room, and
+// rows enough to give every wavefront some.
+template <typename T> int64_t rows_lds(int64_t J, int64_t K)
+{
+    const int64_t w = K <= 32 ? weights_bytes<T, 1>(J) : K <= 64 ? weights_bytes<T, 2>(J) : K <= 128 ? weights_bytes<T, 4>(J) : weights_bytes<T, 8>(J);
+    return w + up(J, 64) * 64 * 4 + 8 * 16 * 68 * 4;
+}
+// (Registers do not hold eight steps of fp32 numbers and what ends of rows take.)
+template <typename T> constexpr bool ends_fit(int steps) { return sizeof(T) == 2 || steps < 8; }
+// direct: tiles whose pieces go straight to LDS are as fast for more than 128 numbers of k (480,000 x 256 -> 64 in bf16: 63 us for 72).
+template <typename T> bool many_rows(int64_t I, int64_t J, int64_t K, bool direct)
+{
+    return (K <= 128 || (K <= 256 && !direct)) && I >= 32768 && rows_lds<T>(J, K) <= 140 * 1024 && (K <= 128 || (K == 256 && J % 8 == 0) || J <= 32 || ends_fit<T>(8));
+}
+
+template <typename T, bool TQ, int STEPS> int launch_rows(const TileArgs &a, hipStream_t stream)
+{
+    const int64_t J = a.tail.cols, lds = rows_lds<T>(J, a.K);
+    const unsigned blocks = lds <= 78 * 1024 ? 512 : 256;
+    const auto go = [&](auto *kernel, int width) {
+        if (!allow_lds(kernel, (size_t)lds)) return (int)PCSR_E_HIP;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(512), (size_t)lds, stream, a, (int)up(J, width));
+        return (int)PCSR_OK;
+    };
+    const bool whole = a.K == STEPS * 32 && J % 8 == 0;
+    if constexpr (TQ) { // gradients of x: nothing follows
+        if (J <= 32) return go(&rows_kernel<T, TQ, STEPS, 2, false, false>, 32);
+        if constexpr (ends_fit<T>(STEPS))
+            if (!whole) return go(&rows_kernel<T, TQ, STEPS, 4, false, false>, 64);
+        return go(&rows_kernel<T, TQ, STEPS, 4, true, false>, 64);
+    } else {
+        const bool res = a.tail.residual;
+        if (J <= 32) return res ? go(&rows_kernel<T, TQ, STEPS, 2, false, true>, 32) : go(&rows_kernel<T, TQ, STEPS, 2, false, false>, 32);
+        if constexpr (ends_fit<T>(STEPS))
+            if (!whole) return res ? go(&rows_kernel<T, TQ, STEPS, 4, false, true>, 64) : go(&rows_kernel<T, TQ, STEPS, 4, false, false>, 64);
+        return res ? go(&rows_kernel<T, TQ, STEPS, 4, true, true>, 64) : go(&rows_kernel<T, TQ, STEPS, 4, true, false>, 64);
+    }
+}
+
+// direct: both operands' pieces can go straight to LDS
+template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, bool direct, const Tail &tail, void *ws, hipStream_t stream)
+{
+    if constexpr (!TP) {
+        if (many_rows<T>(p.n, q.n, K, direct)) {
+            const TileArgs a = {p, q, K, K, 1, 1, 1, nullptr, tail};
+            const int rc = K <= 32 ? launch_rows<T, TQ, 1>(a, stream) : K <= 64 ? launch_rows<T, TQ, 2>(a, stream) : K <= 128 ? launch_rows<T, TQ, 4>(a, stream) : launch_rows<T, TQ, 8>(a, stream);
+            return rc == PCSR_OK ? launched() : rc;
+        }
+    }
+    const Plan c = plan<T>(p.n, q.n, K, direct);
+    TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
+    const unsigned grid = (unsigned)(c.tiles_i * c.tiles_j * c.stretches);
+    int rc = PCSR_OK;
+    bool done = false;
+    if constexpr (sizeof(T) == 2) {
+        if (direct && c.which != SMALL) {
+            done = true;
+            switch (c.which) {
+            case WIDE: rc = launch_straight<T, TP, TQ, StraightWide>(a, grid, stream); break;
+            case TALL: rc = launch_straight<T, TP, TQ, StraightTall>(a, grid, stream); break;
+            case FLAT: rc = launch_straight<T, TP, TQ, StraightFlat>(a, grid, stream); break;
+            default: rc = launch_straight<T, TP, TQ, Large>(a, grid, stream);
+            }
+        }
+    }
+    if (rc != PCSR_OK) return rc;
+    if (!done) switch (c.which) {
+        case WIDE: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Wide>), dim3(grid), dim3(Wide::threads), 0, stream, a); break;
+        case TALL: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Tall>), dim3(grid), dim3(Tall::threads), 0, stream, a); break;
+        case FLAT: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Flat>), dim3(grid), dim3(Flat::threads), 0, stream, a); break;
+        default: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Small>), dim3(grid), dim3(Small::threads), 0, stream, a);
+        }
+    if (c.stretches > 1) {
+        const uint32_t groups = (uint32_t)up(tail.cols, 8);
+        const int64_t places = tail.rows * groups;
+        int across = kT;
+        while (across > 8 && places / across < 512 && kT / across * 4 < c.stretches) across /= 2;
+        hipLaunchKernelGGL(finish_kernel<T>, dim3((unsigned)up(places, across)), dim3(kT), 0, stream, a.part, c.stretches, tail, groups, across);
+    }
+    return launched();
+}
+
+// the parts of the workspace of a backward call
+struct Space {
+    int64_t ld, dz, sums, part, bytes;
+    int64_t blocks; // workgroups of slope_kernel along the rows
+    int lanes;
+    template <typename T> static Space of(const pcsr_linear_t &a, bool own)
+    {
+        Space s;
+        const auto most_of = [](int64_t I, int64_t J, int64_t K) { // however the operands lie
+            const int64_t x = part_bytes(plan<T>(I, J, K, false), I, J), y = part_bytes(plan<T>(I, J, K, true), I, J);
+            return x > y ? x : y;
+        };
+        s.ld = up(a.out, 8) * 8;
+        s.lanes = 1;
+        while (s.lanes < 64 && s.lanes * 8 < a.out) s.lanes *= 2;
+        const int64_t beside = up(a.out, s.lanes * 8), per = kSlopeT / s.lanes;
+        const int64_t most = beside < kSlopeBlocks ? kSlopeBlocks / beside : 1;
+        s.blocks = up(a.rows, per) < most ? up(a.rows, per) : most;
+        s.dz = own ? round16(a.rows * s.ld * (int64_t)sizeof(T)) : 0;
+        s.sums = round16(4 * s.blocks * a.out);
+        const int64_t x = most_of(a.rows, a.in, a.out), w = most_of(a.out, a.in, a.rows);
+        s.part = x > w ? x : w;
+        s.bytes = s.dz + s.sums + s.part;
+        return s;
+    }
+};
+template <typename T> bool forward_direct(const pcsr_linear_t &a)
+{
+    return a.in % 8 == 0 && straight<T>({a.x, a.x_stride, a.rows}, false, false) && straight<T>({a.w, a.w_stride, a.out}, false, false);
+}
+template <typename T> Plan forward_plan(const pcsr_linear_t &a) { return plan<T>(a.rows, a.out, a.in, forward_direct<T>(a)); }
+bool has_slope(const pcsr_linear_t &a) { return a.act != PCSR_ACT_NONE || drop_of(&a.drop).threshold; }
+
+// Rows that few_kernel takes: more of them are read again by every group of lanes.
+constexpr int64_t kFew = 8;
+template <typename T> int few_rows(const TileArgs &a, hipStream_t stream)
+{
+    int lanes = 8; // as many as rows at least
+    while (lanes < 64 && lanes * kPer16<T> < a.K) lanes *= 2;
+    const dim3 grid((unsigned)up(a.tail.cols, kT / lanes));
+    const int64_t rows = a.tail.rows;
+    if (rows == 1) hipLaunchKernelGGL((few_kernel<T, 1>), grid, dim3(kT), 0, stream, a, lanes);
+    else if (rows == 2) hipLaunchKernelGGL((few_kernel<T, 2>), grid, dim3(kT), 0, stream, a, lanes);
+    else if (rows <= 4) hipLaunchKernelGGL((few_kernel<T, 4>), grid, dim3(kT), 0, stream, a, lanes);
+    else hipLaunchKernelGGL((few_kernel<T, 8>), grid, dim3(kT), 0, stream, a, lanes);
+    return launched();
+}
+
+} // namespace
+
+template <typename T> int64_t LinearOf<T>::workspace(const pcsr_linear_t &a, bool backward)
+{
+    return backward ? Space::of<T>(a, has_slope(a)).bytes : a.rows <= kFew ? 0 : part_bytes(forward_plan<T>(a), a.rows, a.out);
+}
+
+template <typename T> int LinearOf<T>::forward(const pcsr_linear_t &a, void *y, void *slope, void *ws, hipStream_t stream)
+{
+    const Tail tail = {a.bias, a.residual, y, a.act == PCSR_ACT_NONE ? nullptr : slope, a.r_stride, a.rows, a.out, a.act, a.bias_type, drop_of(&a.drop)};
+    const Side x = {a.x, a.x_stride, a.rows}, w = {a.w, a.w_stride, a.out};
+    if (a.rows <= kFew) return few_rows<T>({x, w, a.in, a.in, 1, 1, 1, nullptr, tail}, stream);
+    return product<T, false, false>(x, w, a.in, forward_direct<T>(a), tail, ws, stream);
+}
+
+template <typename T>
+int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws, hipStream_t stream)
+{
+    const bool own = has_slope(a);
+    const Space sp = Space::of<T>(a, own);
+    char *at = static_cast<char *>(ws);
+    float *sums = reinterpret_cast<float *>(at + sp.dz);
+    void *part = at + sp.dz + sp.sums;
+    Side dz = {dy, dy_stride, a.rows};
+    if (own || db) {
+        SlopeArgs s = {dy, a.act == PCSR_ACT_NONE ? nullptr : slope, dy_stride, a.rows, a.out, sp.ld, own && (dx || dw) ? at : nullptr,
+                       db ? sums : nullptr, sp.lanes, drop_of(&a.drop)};
+        hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)sp.blocks, (unsigned)up(a.out, sp.lanes * 8)), dim3(kSlopeT), 0, stream, s);
+        if (db) hipLaunchKernelGGL(sums_kernel, dim3((unsigned)up(a.out, 16)), dim3(1024), 0, stream, sums, sp.blocks, a.out, a.bias_type, db);
+        if (own) dz = {at, sp.ld, a.rows};
+    }
+    int rc = launched();
+    if (dx && a.in > 0 && rc == PCSR_OK) {
+        const Tail tail = {nullptr, nullptr, dx, nullptr, 0, a.rows, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
+        const Side w = {a.w, a.w_stride, a.in};
+        rc = product<T, false, true>(dz, w, a.out, a.out % 8 == 0 && straight<T>(dz, false, false) && straight<T>(w, true, false), tail, part, stream);
+    }
+    if (dw && a.in > 0 && rc == PCSR_OK) {
+        const Tail tail = {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
+        const Side g = {dz.at, dz.ld, a.out}, x = {a.x, a.x_stride, a.in};
+        rc = product<T, true, true>(g, x, a.rows, straight<T>(g, true, own) && straight<T>(x, true, false), tail, part, stream);
+    }
+    return rc;
+}
+
+} // namespace pcsr

@@ -110,7 +110,8 @@ def run(X, W, b, act, R, p, seed, offset, kind, dy):
 
 
 SIZES = [(1, 1, 1), (1, 64, 64), (3, 1, 9), (5, 7, 3), (2, 1000, 33), (1, 4096, 40), (17, 8, 600), (64, 64, 64), (65, 32, 66), (129, 65, 130), (300, 8, 16),
-         (777, 75, 333), (130, 333, 1), (4000, 16, 64), (1000, 520, 260), (2500, 264, 1040), (40_000, 24, 100), (9, 2, 5000)]
+         (777, 75, 333), (130, 333, 1), (4000, 16, 64), (1000, 520, 260), (2500, 264, 1040), (40_000, 24, 100), (9, 2, 5000),
+         (2, 300, 100), (4, 75, 41), (8, 4096, 520), (7, 33, 12), (6, 8, 3000)]
 
 
 @pytest.mark.parametrize("kind", list(TYPES))

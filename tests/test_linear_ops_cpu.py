@@ -81,7 +81,7 @@ def test_linear_entry_points():
     assert fwd(y=None) == INVALID and fwd(residual=P, r_stride=13) == INVALID and fwd(rows=0, y=None, x=None) == OK
     assert bwd(dy=None) == INVALID and bwd(stride=13) == INVALID and bwd(ws=None) == INVALID and bwd(act=2, z=None) == INVALID
     assert bwd(dx=None, dw=None, db=None) == OK and bwd(rows=0, dy=None) == OK
-    deep = _linear(**{"in": 100_000, "x_stride": 100_000, "w_stride": 100_000})
+    deep = _linear(rows=100, **{"in": 100_000, "x_stride": 100_000, "w_stride": 100_000})
     assert lib.pcsr_linear_workspace(ctypes.byref(deep), 0) > 0 and lib.pcsr_linear(ctypes.byref(deep), P, None, None, None) == INVALID
     assert lib.pcsr_linear_workspace(None, 0) == 0 and lib.pcsr_linear(None, P, None, P, None) == INVALID
 
