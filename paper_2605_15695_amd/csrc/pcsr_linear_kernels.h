@@ -269,6 +269,8 @@ typedef Tiling<128, 64, 2, 2> Tall;
 typedef Tiling<64, 128, 2, 2> Flat;
 typedef Tiling<64, 64, 2, 2> Small;
 typedef Tiling<256, 256, 2, 4, 2> Large;
+typedef Tiling<128, 256, 2, 4, 2> PiecesFlat;
+typedef Tiling<256, 128, 4, 2, 2> PiecesTall;
 typedef Tiling<128, 128, 2, 2, 2> StraightWide;
 typedef Tiling<128, 64, 2, 2, 2> StraightTall;
 typedef Tiling<64, 128, 2, 2, 2> StraightFlat;
@@ -482,6 +484,16 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, again);
 }
 
+// Until at most N of the wavefront's loads are on their way and its LDS reads and writes are done, for all wavefronts.  Instructions that the compiler knows, so that its own
+// waits go by what is left (behind an asm it waits for everything at the head of a loop).
+template <int N> __device__ __forceinline__ void wait_for_all()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | (N >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // ---------------------------------------------------------------------------------- 16-bit numbers straight to LDS
 // Tiles of operands whose rows are whole 16-byte pieces.  Pieces go from memory straight to LDS, two stages of 64 numbers of k, one of them on its way while
 // the other is multiplied.  A load of a wavefront fills 1 KB.
@@ -517,12 +529,12 @@ template <typename T, bool TURN, int R, int THREADS> struct Straight {
             off[u] = (uint32_t)((TURN ? k * s.ld + row : row * s.ld + k) * 2);
         }
     }
-    // loads of the stage that `base` is at; left: numbers of k that there are
-    __device__ __forceinline__ void fetch(char *lds, int64_t left, int lane, int wave) const
+    // loads of the stage that `base` is at; left: numbers of k that there are (WHOLE: a stage's)
+    template <bool WHOLE> __device__ __forceinline__ void fetch(char *lds, int64_t left, int lane, int wave) const
     {
         typedef __attribute__((address_space(3))) void *Lds;
         typedef __attribute__((address_space(1))) const void *Global;
-        if (left >= KS) {
+        if (WHOLE || left >= KS) {
 #pragma unroll
             for (int u = 0; u < loads; ++u)
                 __builtin_amdgcn_global_load_lds((Global)(base + off[u]), (Lds)(lds + (u * waves + wave) * apart), 16, 0, 0);
@@ -579,13 +591,12 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     q.begin(a.q, j0, k0, lane, wave);
     const int steps = (int)((k1 - k0 + 63) / 64);
     int64_t left = k1 - k0;
-    const auto fetch = [&](int s) {
+    const auto fetch = [&](int s, auto whole) {
         char *to = lds + (s & 1) * stage;
-        p.fetch(to, left, lane, wave);
-        q.fetch(to + P::bytes, left, lane, wave);
+        p.template fetch<whole>(to, left, lane, wave);
+        q.template fetch<whole>(to + P::bytes, left, lane, wave);
         p.next(), q.next(), left -= 64;
     };
-    const auto all_here = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
     Sums<C> sum;
 #pragma unroll
     for (int i = 0; i < FI; ++i)
@@ -602,33 +613,194 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
 #pragma unroll
         for (int i = 0; i < GI; ++i) x[u & 1][i] = P::read(from, wi * FI + u % per * GI + i, u / per, lane);
     };
-    const auto multiply = [&](int u) {
+    const auto multiply = [&](int u, int first, int end) {
 #pragma unroll
-        for (int i = 0; i < GI; ++i)
+        for (int i = first; i < end; ++i)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) sum[u % per * GI + i][j] = mfma(T(), x[u & 1][i], y[u / per][j], sum[u % per * GI + i][j]);
     };
-    if (steps > 0) {
-        fetch(0);
-        all_here();
-        if (steps > 1) fetch(1);
-        read(0, 0);
-        for (int s = 0; s < steps; ++s) {
+    const auto begin_of = [&](int s) { // units of stage s but the last two, and the first products of the last but one
 #pragma unroll
-            for (int u = 0; u < units - 1; ++u) {
-                read(s, u + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(u);
-            }
-            all_here(); // stage s has been read, stage s + 1 is there
-            if (s + 2 < steps) fetch(s + 2);
-            if (s + 1 < steps) read(s + 1, 0);
+        for (int u = 0; u < units - 1; ++u) {
+            read(s, u + 1);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(units - 1);
+            multiply(u, 0, u < units - 2 ? GI : 1);
         }
+    };
+    // From there to the same place of the next stage.  Wavefronts wait for one another where they have products left to do behind that, beside which loads and reads begin.
+    // plain: the stage behind the next is there, a whole one.  That loop turns where everything is waited for anyway, and has no condition in it, or waits at
+    // its joins are for everything.
+    const auto go_on = [&](int s, auto plain) {
+        wait_for_all<0>(); // stage s has been read, stage s + 1 is there
+        multiply(units - 2, 1, GI);
+        if (plain || s + 2 < steps) fetch(s + 2, plain);
+        read(s + 1, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(units - 1, 0, GI);
+        begin_of(s + 1);
+    };
+    if (steps > 0) {
+        fetch(0, std::false_type());
+        wait_for_all<0>();
+        if (steps > 1) fetch(1, std::false_type());
+        read(0, 0);
+        begin_of(0);
+        int s = 0;
+        for (const int whole = (int)((k1 - k0) / 64); s + 2 < whole; ++s) go_on(s, std::true_type());
+        for (; s + 1 < steps; ++s) go_on(s, std::false_type());
+        multiply(units - 2, 1, GI);
+        multiply(units - 1, 0, GI);
     }
     __syncthreads(); // all of the last stage is read
     finish_tile<T, TP, TQ, C, FI < 4 ? FI : 4>(a, sum, lds, i0, j0, k0, k1, stretch, false);
+}
+
+// ---------------------------------------------------------------------------------- large products of fp32 numbers
+// Weights are split once, into planes [piece][k / 32][row][32] with zeros behind the ends, so that 16 rows of a stage are 1 KB for one load straight to LDS; the
+// other operand, and both of a gradient of weights, are split on their way through registers.  Two stages of 32 numbers of k lie in LDS: while one is
+// multiplied the next is split, and the numbers of the two after it are on their way.  96 instructions of 16 cycles to a wavefront's stage.
+constexpr int kSplitBlocks = 256;
+struct Planes {
+    const bfloat_t *at;
+    int64_t rows, plane; // padded rows, numbers of a plane
+    const int *hot;      // [kSplitBlocks]: whether numbers are too large for pieces
+};
+struct SplitArgs {
+    const float *w;
+    int64_t ld, n, K, rows, chunks; // padded rows, chunks of 8 numbers of k (padded)
+    bfloat_t *to;
+    int *hot;
+};
+// 4096 x 4096: 30 us.
+template <bool TURN> __global__ void __launch_bounds__(kT) split_kernel(SplitArgs a)
+{
+    float hot = 0.0f;
+    const int64_t all = a.rows * a.chunks, plane = all * 8;
+    for (int64_t id = (int64_t)blockIdx.x * kT + threadIdx.x; id < all; id += (int64_t)gridDim.x * kT) {
+        // the order in which the weights lie, but for the four chunks that lie together in a plane
+        const int64_t j = TURN ? id % a.rows : id / 4 % a.rows, c = TURN ? id / a.rows : id / 4 / a.rows * 4 + id % 4;
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t k = c * 8 + i;
+            x[i] = j < a.n && k < a.K ? a.w[TURN ? k * a.ld + j : j * a.ld + k] : 0.0f;
+        }
+        uint32_t p[4][3];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) pieces(x[2 * q], x[2 * q + 1], hot, p[q]);
+        bfloat_t *to = a.to + (c / 4 * a.rows + j) * 32 + c % 4 * 8;
+#pragma unroll
+        for (int o = 0; o < 3; ++o) *reinterpret_cast<u4 *>(to + o * plane) = u4{p[0][o], p[1][o], p[2][o], p[3][o]};
+    }
+    const int any = __syncthreads_or(hot >= kHot);
+    if (threadIdx.x == 0) a.hot[blockIdx.x] = any;
+}
+
+template <typename C> constexpr int pieces_bytes()
+{
+    constexpr int stages = 2 * (C::BI + C::BJ) * 64 * 3, out = out_bytes<C, 2>();
+    return stages > out ? stages : out;
+}
+// a.q: the weights as they are, or the other operand of a gradient of weights
+template <bool TP, bool TQ, bool PLANES, typename C> __global__ void __launch_bounds__(C::threads, C::per) pieces_kernel(TileArgs a, Planes w)
+{
+    typedef float T;
+    constexpr int KS = 32, FI = C::FI, FJ = C::FJ, planeP = C::BI * 64, planeQ = C::BJ * 64, stage = 3 * (planeP + planeQ), waves = C::threads / 64;
+    constexpr int loads = 3 * C::BJ / 16 / waves; // of planes, to a wavefront
+    static_assert(3 * C::BJ / 16 % waves == 0, "whole loads");
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int met;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
+    int ti, tj, stretch;
+    place_of(a, &ti, &tj, &stretch);
+    const int64_t i0 = (int64_t)ti * C::BI, j0 = (int64_t)tj * C::BJ;
+    const int64_t k0 = (int64_t)stretch * a.stretch, k1 = k0 + a.stretch < a.K ? k0 + a.stretch : a.K;
+    const int steps = (int)((k1 - k0 + KS - 1) / KS);
+    if (tid == 0) met = 0;
+    float hot = 0.0f;
+    typedef Loader<T, TP, C::BI, C::threads> P;
+    typedef Loader<T, TQ, C::BJ, C::threads> Q;
+    constexpr int ahead = PLANES ? 2 : 1; // stages on their way to registers (which do not hold two of both operands)
+    P lp[ahead];
+    Q lq[ahead];
+    const auto fetch = [&](int s, P &p, Q &q) {
+        if (s >= steps) return;
+        p.fetch(a.p, i0, k0 + s * KS, k1, tid);
+        if (!PLANES) q.fetch(a.q, j0, k0 + s * KS, k1, tid);
+    };
+    const auto put = [&](int s, const P &p, const Q &q) {
+        if (s >= steps) return;
+        char *to = lds + (s & 1) * stage;
+        p.put(to, hot, tid);
+        if (!PLANES) q.put(to + 3 * planeP, hot, tid);
+    };
+    const auto load_planes = [&](int s) {
+        if (!PLANES || s >= steps) return;
+        typedef __attribute__((address_space(3))) void *Lds;
+        typedef __attribute__((address_space(1))) const void *Global;
+#pragma unroll
+        for (int u = 0; u < loads; ++u) {
+            const int b = u * waves + wave, o = b / (C::BJ / 16), rows = b % (C::BJ / 16) * 16;
+            const bfloat_t *from = w.at + o * w.plane + ((k0 / KS + s) * w.rows + j0 + rows + (lane >> 2)) * 32 + ((lane & 3) ^ (lane >> 4)) * 8;
+            __builtin_amdgcn_global_load_lds((Global)from, (Lds)(lds + (s & 1) * stage + 3 * planeP + o * planeQ + rows * 64), 16, 0, 0);
+        }
+    };
+    Sums<C> sum;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int at = lane & 15, chunk = lane >> 4;
+    const auto step = [&](int s, P &p, Q &q) { // p, q: the numbers of stage s + 1, then of the one behind those on their way
+        const char *fromP = lds + (s & 1) * stage, *fromQ = fromP + 3 * planeP;
+        load_planes(s + 1);
+        u4 x[FI][3], y[FJ][3];
+        const auto read = [&](int i) {
+#pragma unroll
+            for (int o = 0; o < 3; ++o) x[i][o] = *reinterpret_cast<const u4 *>(fromP + o * planeP + place<32>((wi * FI + i) * 16 + at, chunk));
+        };
+#pragma unroll
+        for (int o = 0; o < 3; ++o)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) y[j][o] = *reinterpret_cast<const u4 *>(fromQ + o * planeQ + place<32>((wj * FJ + j) * 16 + at, chunk));
+#pragma unroll
+        for (int i = 0; i < (PLANES ? FI : FI / 2); ++i) read(i);
+        const auto multiply = [&](int i) {
+            f4 part[FJ];
+            products32<FJ>(x[i], y, part);
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[i][j] += part[j];
+        };
+#pragma unroll
+        for (int i = 0; i < FI / 2; ++i) multiply(i);
+        put(s + 1, p, q);
+        __builtin_amdgcn_sched_barrier(0); // the planes of stage s + 1 are older than what is fetched here, which need not be there
+        fetch(s + 1 + ahead, p, q);
+#pragma unroll
+        for (int i = FI / 2; i < FI; ++i) {
+            if (!PLANES) read(i);
+            multiply(i);
+        }
+        const bool whole = s + 1 + ahead < steps && k0 + (s + 2 + ahead) * KS <= k1 && P::whole && (!TP || i0 + C::BI <= a.p.n);
+        if (!PLANES) wait_for_all<63>();
+        else if (whole) wait_for_all<P::U * P::parts>();
+        else wait_for_all<0>();
+    };
+    if (steps > 0) {
+        fetch(0, lp[0], lq[0]);
+        load_planes(0);
+        if (ahead == 2) fetch(1, lp[ahead - 1], lq[ahead - 1]);
+        put(0, lp[0], lq[0]);
+        fetch(ahead, lp[0], lq[0]);
+        wait_for_all<0>();
+        for (int s = 0; s < steps; s += 2) {
+            step(s, lp[ahead - 1], lq[ahead - 1]);
+            if (s + 1 < steps) step(s + 1, lp[0], lq[0]);
+        }
+    }
+    if (hot >= kHot || (PLANES && tid < kSplitBlocks && w.hot[tid])) met = 1;
+    __syncthreads();
+    finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, met);
 }
 
 // ---------------------------------------------------------------------------------- many rows and few weights
@@ -1002,17 +1174,23 @@ struct Plan {
     int64_t tiles_i, tiles_j, stretch;
     int stretches;
 };
-enum { WIDE, TALL, FLAT, SMALL, LARGE };
+enum { WIDE, TALL, FLAT, SMALL, LARGE, PIECES_FLAT, PIECES_TALL };
 template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct)
 {
     constexpr int64_t kWanted = 512; // workgroups: two to a compute unit
-    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI, Large::BI}, BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ, Large::BJ};
+    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI, Large::BI, PiecesFlat::BI, PiecesTall::BI};
+    static const int BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ, Large::BJ, PiecesFlat::BJ, PiecesTall::BJ};
     Plan p;
     const int64_t stages = up(K, Num<T>::KS), most = stages / 4 < 1 ? 1 : stages / 4;
+    const auto tiles_of = [&](int which) { return up(I, BI[which]) * up(J, BJ[which]); };
     int64_t wanted = kWanted;
     p.which = (I <= 64 ? FLAT : WIDE) + (J <= 64 ? 1 : 0);
-    if (direct && I > 128 && J > 128 && up(I, 256) * up(J, 256) * most >= 192) p.which = LARGE, wanted = 256;
-    if (up(I, BI[p.which]) * up(J, BJ[p.which]) * most < 256 && p.which != LARGE) p.which = SMALL;
+    if (direct && I > 128 && J > 128 && tiles_of(LARGE) * most >= 192) p.which = LARGE, wanted = 256;
+    if (sizeof(T) == 4 && I > 64 && J > 64 && K >= 64) {
+        const int which = tiles_of(PIECES_TALL) < tiles_of(PIECES_FLAT) ? PIECES_TALL : PIECES_FLAT;
+        if (tiles_of(which) * most >= 192) p.which = which, wanted = 256;
+    }
+    if (tiles_of(p.which) * most < 256 && wanted == kWanted) p.which = SMALL;
     p.tiles_i = up(I, BI[p.which]), p.tiles_j = up(J, BJ[p.which]);
     const int64_t tiles = p.tiles_i * p.tiles_j;
     int64_t s = tiles >= wanted ? 1 : wanted / (tiles ? tiles : 1);
@@ -1022,6 +1200,11 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct)
     return p;
 }
 int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
+// planes of weights, and whether numbers in them are too large
+int64_t plane_rows(const Plan &p) { return p.tiles_j * (p.which == PIECES_FLAT ? PiecesFlat::BJ : PiecesTall::BJ); }
+int64_t plane_bytes(const Plan &p, int64_t K) { return p.which >= PIECES_FLAT ? 3 * 2 * plane_rows(p) * up(K, 32) * 32 + 4 * kSplitBlocks : 0; }
+// workspace of a product; weights: of rows with weights
+int64_t product_bytes(const Plan &p, int64_t I, int64_t J, int64_t K, bool weights) { return part_bytes(p, I, J) + (weights ? plane_bytes(p, K) : 0); }
 
 template <typename T, bool TP, bool TQ, typename C> int launch_straight(const TileArgs &a, unsigned grid, hipStream_t stream)
 {
@@ -1095,6 +1278,25 @@ template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q
             }
         }
     }
+    if constexpr (sizeof(T) == 4) {
+        if (c.which >= PIECES_FLAT) {
+            done = true;
+            char *at = static_cast<char *>(ws) + part_bytes(c, tail.rows, tail.cols);
+            const int64_t rows = plane_rows(c), chunks = up(K, 32) * 4;
+            Planes w = {reinterpret_cast<bfloat_t *>(at + 4 * kSplitBlocks), rows, rows * chunks * 8, reinterpret_cast<int *>(at)};
+            if (!TP) {
+                const SplitArgs s = {static_cast<const float *>(q.at), q.ld, q.n, K, rows, chunks, const_cast<bfloat_t *>(w.at), reinterpret_cast<int *>(at)};
+                hipLaunchKernelGGL(split_kernel<TQ>, dim3(kSplitBlocks), dim3(kT), 0, stream, s);
+            }
+            const auto go = [&](auto *kernel, int bytes, int threads) {
+                if (!allow_lds(kernel, (size_t)bytes)) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), (size_t)bytes, stream, a, w);
+                return (int)PCSR_OK;
+            };
+            rc = c.which == PIECES_FLAT ? go(&pieces_kernel<TP, TQ, !TP, PiecesFlat>, pieces_bytes<PiecesFlat>(), PiecesFlat::threads)
+                                        : go(&pieces_kernel<TP, TQ, !TP, PiecesTall>, pieces_bytes<PiecesTall>(), PiecesTall::threads);
+        }
+    }
     if (rc != PCSR_OK) return rc;
     if (!done) switch (c.which) {
         case WIDE: hipLaunchKernelGGL((tile_kernel<T, TP, TQ, Wide>), dim3(grid), dim3(Wide::threads), 0, stream, a); break;
@@ -1120,8 +1322,8 @@ struct Space {
     template <typename T> static Space of(const pcsr_linear_t &a, bool own)
     {
         Space s;
-        const auto most_of = [](int64_t I, int64_t J, int64_t K) { // however the operands lie
-            const int64_t x = part_bytes(plan<T>(I, J, K, false), I, J), y = part_bytes(plan<T>(I, J, K, true), I, J);
+        const auto most_of = [](int64_t I, int64_t J, int64_t K, bool weights) { // however the operands lie
+            const int64_t x = product_bytes(plan<T>(I, J, K, false), I, J, K, weights), y = product_bytes(plan<T>(I, J, K, true), I, J, K, weights);
             return x > y ? x : y;
         };
         s.ld = up(a.out, 8) * 8;
@@ -1132,7 +1334,7 @@ struct Space {
         s.blocks = up(a.rows, per) < most ? up(a.rows, per) : most;
         s.dz = own ? round16(a.rows * s.ld * (int64_t)sizeof(T)) : 0;
         s.sums = round16(4 * s.blocks * a.out);
-        const int64_t x = most_of(a.rows, a.in, a.out), w = most_of(a.out, a.in, a.rows);
+        const int64_t x = most_of(a.rows, a.in, a.out, true), w = most_of(a.out, a.in, a.rows, false);
         s.part = x > w ? x : w;
         s.bytes = s.dz + s.sums + s.part;
         return s;
@@ -1164,7 +1366,7 @@ template <typename T> int few_rows(const TileArgs &a, hipStream_t stream)
 
 template <typename T> int64_t LinearOf<T>::workspace(const pcsr_linear_t &a, bool backward)
 {
-    return backward ? Space::of<T>(a, has_slope(a)).bytes : a.rows <= kFew ? 0 : part_bytes(forward_plan<T>(a), a.rows, a.out);
+    return backward ? Space::of<T>(a, has_slope(a)).bytes : a.rows <= kFew ? 0 : product_bytes(forward_plan<T>(a), a.rows, a.out, a.in, true);
 }
 
 template <typename T> int LinearOf<T>::forward(const pcsr_linear_t &a, void *y, void *slope, void *ws, hipStream_t stream)
