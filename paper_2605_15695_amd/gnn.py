@@ -4,8 +4,8 @@ dB = A^T * dC, both through pcsr_spmm, plus minimal GCN / GIN layers built on it
 
 torch supplies tensors, streams, the loss and the optimiser; every sparse product runs in the
 library's kernels, and so do the dense products of layers up to MAX_WIDTH features wide with
-what surrounds them (bias, ReLU, its backward, the gradient sums): see FusedLayers.  embedding.py, norm.py
-and muon.py have what a training step needs around the layers.
+what surrounds them (bias, ReLU, its backward, the gradient sums): see FusedLayers.  embedding.py, norm.py,
+muon.py, dropout.py and linear.py have what a training step needs around and between the layers.
 """
 from __future__ import annotations
 
@@ -16,6 +16,8 @@ import torch
 from torch.nn.modules import module as _all_modules
 
 from . import binding as pc
+from .dropout import Dropout
+from .linear import FeedForward
 from .norm import GroupNorm
 
 
@@ -455,8 +457,8 @@ class GINLayer(torch.nn.Module):
 
 class LayerChain(torch.nn.Sequential):
     """Graph layers with ReLU between them, run as one chain where FusedLayers applies and module
-    by module otherwise (other operators, data types or devices, hooks, wide layers, norms between
-    the layers).  offsets: of the graphs in a batch, for the norms."""
+    by module otherwise (other operators, data types or devices, hooks, wide layers, norms, dropout or
+    feed-forward blocks between the layers).  offsets: of the graphs in a batch, for the norms."""
 
     def forward(self, X, offsets=None):
         mods = list(self)
@@ -480,10 +482,12 @@ class LayerChain(torch.nn.Sequential):
 
 
 def make_model(kind: str, op: PcsrOperator, d_in: int, hidden: int, d_out: int, n_layers: int = 5,
-               norm_groups: int = 0):
+               norm_groups: int = 0, dropout: float = 0.0, feed_forward: int = 0):
     """n_layers graph layers with ReLU between them (the paper trains 5-layer GCN / GIN
     models with hidden sizes 32, 64, 128 and 16 input / output features).  norm_groups: a group norm of
-    so many groups in front of each ReLU, over the nodes of a graph."""
+    so many groups in front of each ReLU, over the nodes of a graph.  feed_forward: behind each ReLU a
+    block of two linear layers, feed_forward times as wide between them, that is added to its input.  dropout: of
+    the features between the layers and within those blocks, in training."""
     dims = [d_in] + [hidden] * (n_layers - 1) + [d_out]
     layer = {"gcn": GCNLayer, "gin": GINLayer}[kind]
     mods = []
@@ -491,4 +495,8 @@ def make_model(kind: str, op: PcsrOperator, d_in: int, hidden: int, d_out: int, 
         mods.append(layer(op, dims[i], dims[i + 1]))
         if i + 1 < n_layers:
             mods.append(GroupNorm(norm_groups, hidden, activation="relu") if norm_groups else torch.nn.ReLU())
+            if feed_forward:
+                mods.append(FeedForward(hidden, feed_forward * hidden, p=dropout))
+            if dropout:
+                mods.append(Dropout(dropout))
     return LayerChain(*mods)

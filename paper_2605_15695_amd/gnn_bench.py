@@ -7,9 +7,12 @@ size 32 / 64 / 128.  Synthetic graphs and random features stand in for the OGB g
 
 --embed, --norm and --optimizer muon put the parts around the layers into the step: a learned table of node
 features looked up by id (every node once, in random order), a group norm in front of each ReLU, the
-orthogonalised update of the layers' weight matrices (Adam keeps the rest); without torch.sparse beside it.
+orthogonalised update of the layers' weight matrices (Adam keeps the rest); --dropout and --feed-forward those between
+them: dropout of the hidden features, a feed-forward block so many times as wide behind each ReLU.  Without torch.sparse
+beside them.
 
     python -m paper_2605_15695_amd.gnn_bench --workload road --model gin --embed --norm 8 --optimizer muon
+    python -m paper_2605_15695_amd.gnn_bench --workload road --model gcn --feed-forward 4 --dropout 0.1
 
 --dense times the layers' dense kernels on their own, the calls of a backward or a GIN layer both
 in one pass and one after the other, beside the torch operations they stand for.
@@ -101,6 +104,8 @@ def main(argv=None) -> int:
     ap.add_argument("--no-torch-sparse", action="store_true")
     ap.add_argument("--embed", action="store_true")
     ap.add_argument("--norm", type=int, default=0, metavar="GROUPS")
+    ap.add_argument("--dropout", type=float, default=0.0, metavar="P")
+    ap.add_argument("--feed-forward", type=int, default=0, metavar="TIMES")
     ap.add_argument("--optimizer", default="adam", choices=["adam", "muon"])
     ap.add_argument("--dense", type=int, default=0, metavar="ROWS")
     args = ap.parse_args(argv)
@@ -126,7 +131,7 @@ def main(argv=None) -> int:
 
     def run(op, label):
         torch.manual_seed(0)
-        model = make_model(args.model, op, 16, args.hidden, 16, args.layers, args.norm).cuda()
+        model = make_model(args.model, op, 16, args.hidden, 16, args.layers, args.norm, args.dropout, args.feed_forward).cuda()
         table = NodeEmbedding(g.n_cols, 16, scale=4.0, device="cuda") if args.embed else None
         ids = torch.randperm(g.n_cols, device="cuda") if args.embed else None
         matrices = [p for p in model.parameters() if p.dim() == 2] if args.optimizer == "muon" else []
@@ -158,7 +163,7 @@ def main(argv=None) -> int:
     op = PcsrOperator(g.n_rows, g.n_cols, g.rowptr, g.colidx, g.vals, symmetric=symmetric, K_hint=args.hidden)
     build_s = time.time() - t0
     res = [run(op, "pcsr")]
-    if not (args.no_torch_sparse or args.embed or args.norm or args.optimizer != "adam"):
+    if not (args.no_torch_sparse or args.embed or args.norm or args.dropout or args.feed_forward or args.optimizer != "adam"):
         A = torch.sparse_csr_tensor(torch.from_numpy(g.rowptr).cuda(), torch.from_numpy(g.colidx).cuda(),
                                     torch.from_numpy(g.vals).cuda(), size=(g.n_rows, g.n_cols))
 
@@ -172,7 +177,7 @@ def main(argv=None) -> int:
             res.append({"impl": "torch.sparse", "error": repr(e)[:200]})
     out = {"workload": f"{args.workload}-{args.size}", "n": g.n_rows, "nnz": g.nnz, "model": args.model,
            "layers": args.layers, "hidden": args.hidden, "embed": args.embed, "norm_groups": args.norm,
-           "optimizer": args.optimizer, "operator_build_s": build_s, "results": res}
+           "dropout": args.dropout, "feed_forward": args.feed_forward, "optimizer": args.optimizer, "operator_build_s": build_s, "results": res}
     if len(res) == 2 and "ms_per_step_median" in res[1]:
         out["speedup_vs_torch_sparse"] = res[1]["ms_per_step_median"] / res[0]["ms_per_step_median"]
     print(json.dumps(out))

@@ -125,3 +125,18 @@ def test_modules_keep_what_they_are_given():
     assert set(Linear(3, 4).state_dict()) == {"weight", "bias"} and set(Linear(3, 4, False, p=0.1).state_dict()) == {"weight", "counter"}
     block = FeedForward(3, 8, "silu", 0.1)
     assert block.first.activation == "silu" and block.second.weight.shape == (3, 8)
+
+
+def test_models_with_dropout_and_blocks_between_the_layers():
+    from paper_2605_15695_amd.gnn import make_model
+
+    def names(**kw):
+        return [type(m).__name__ for m in make_model("gcn", None, 4, 8, 4, 3, **kw)]
+
+    assert names() == ["GCNLayer", "ReLU"] * 2 + ["GCNLayer"]
+    assert names(dropout=0.5) == ["GCNLayer", "ReLU", "Dropout"] * 2 + ["GCNLayer"]
+    assert names(norm_groups=2, feed_forward=4) == ["GCNLayer", "GroupNorm", "FeedForward"] * 2 + ["GCNLayer"]
+    model = make_model("gin", None, 4, 8, 4, 3, dropout=0.5, feed_forward=4)
+    assert model[2].first.p == model[2].second.p == model[3].p == 0.5 and model[2].first.weight.shape == (32, 8)
+    with pytest.raises(ValueError):
+        make_model("gcn", None, 4, 8, 4, 3, dropout=1.5)
