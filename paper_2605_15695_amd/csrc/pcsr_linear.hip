@@ -4,7 +4,7 @@
 namespace pcsr {
 namespace {
 
-int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
+constexpr int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 constexpr int64_t kMostTiles = int64_t(1) << 23;
 
 int check(const pcsr_linear_t *a)
@@ -12,8 +12,8 @@ int check(const pcsr_linear_t *a)
     if (!a || a->rows < 0 || a->in < 0 || a->out < 1 || !(a->drop.p >= 0.0 && a->drop.p <= 1.0)) return PCSR_E_INVALID_ARG;
     if (a->type < PCSR_F32 || a->type > PCSR_F16 || a->act < PCSR_ACT_NONE || a->act > PCSR_ACT_GELU) return PCSR_E_UNSUPPORTED;
     if (a->bias_type != PCSR_F32 && a->bias_type != a->type) return PCSR_E_UNSUPPORTED;
-    const int64_t big = int64_t(1) << 31;
-    if (a->rows >= big * 2 || a->in >= big || a->out >= big) return PCSR_E_TOO_LARGE;
+    const int64_t wide = int64_t(1) << 24;
+    if (a->rows >= int64_t(1) << 32 || a->in >= wide || a->out >= wide) return PCSR_E_TOO_LARGE;
     for (const int64_t t : {up(a->rows, 64) * up(a->out, 64), up(a->rows, 64) * up(a->in, 64), up(a->out, 64) * up(a->in, 64)})
         if (t > kMostTiles) return PCSR_E_TOO_LARGE;
     if (a->rows > 0 && a->in > 0 && (a->x_stride < a->in || a->w_stride < a->in)) return PCSR_E_INVALID_ARG;

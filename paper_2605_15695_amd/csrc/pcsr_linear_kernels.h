@@ -29,7 +29,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
-int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
+constexpr int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 constexpr int kT = 256;
 constexpr float kUp = 65536.0f, kDown = 1.0f / (65536.0f * 65536.0f), kHot = 0x1p54f; // 2^38 of a number as it is split
 
@@ -1202,6 +1202,167 @@ template <typename T> __global__ void __launch_bounds__(kT) last_kernel(FinishAr
     else sums_of<kT>(b, block - blocks_x - blocks_w, reinterpret_cast<double (*)[17]>(memory));
 }
 
+// ---------------------------------------------------------------------------------- gradients of many rows and few weights
+// dz, dx, dw and db of 16-bit numbers from one read of dy, the slopes and x, where dw fits a workgroup's registers: up to 256 columns of dy and 64 of x.
+// A workgroup takes 64 or 128 rows at a time: dz and x go to LDS as they are, [row][column], the weights lie there turned, and dx = dz w reads dz by rows,
+// dw += dz^T x both by columns (turned by the LDS reads).  A thread keeps its 8 columns of dy, so that db is a sum of its own; when it has used a row's numbers
+// it asks for those that come next.  Bound by memory and, where something is dropped, by the generator: 480,000 x 64 -> 256 in bf16, gelu, p = 0.1.
+struct NarrowArgs {
+    const void *dy, *slope, *x, *w; // slope: null for none
+    int64_t dy_stride, x_stride, w_stride, rows;
+    int in, out;
+    void *dx;           // null: not needed, nor w
+    float *part, *sums; // [workgroup][out][in] (null: not needed, nor x), [workgroup][out]
+    Drop drop;
+};
+constexpr int kNarrowT = 1024, kNarrowBlocks = 256;
+constexpr int narrow_rows(int lanes) { return lanes == 32 ? 64 : 128; } // (of 32 lanes to a row registers hold two rows' numbers beside the rest)
+constexpr int64_t narrow_lds(int lanes, int64_t out, int64_t in) // dz, weights, x
+{
+    const int64_t pitch = up(out, 32) * 64 + 16, rows = narrow_rows(lanes);
+    return rows * pitch + up(in, 16) * 16 * pitch + rows * (up(in, 16) * 32 + 16);
+}
+
+// L: lanes to a row of dy
+template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_kernel(NarrowArgs a)
+{
+    typedef typename Slope<T>::type S;
+    typedef typename Pack<T, 8>::type Raw;
+    typedef typename Pack<S, 8>::type RawS;
+    constexpr int per = kNarrowT / L, ROWS = narrow_rows(L), passes = ROWS / per, J = ROWS / 64; // J: tiles of dx to a wavefront
+    extern __shared__ __align__(16) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 15, chunk = lane >> 4;
+    const int in = a.in, out = a.out, steps = (int)up(out, 32), tiles_k = (int)up(in, 16), pitch = steps * 64 + 16, pitch_x = tiles_k * 32 + 16;
+    char *const ldsW = lds + ROWS * pitch, *const ldsX = ldsW + tiles_k * 16 * pitch;
+    const int64_t all = (a.rows + ROWS - 1) / ROWS;
+    const int c = tid % L * 8, r0 = tid / L, xc = tid % 8 * 8, xr = tid / 8;
+    const bool mine = c < out, mine_x = a.x && xc < in && xr < ROWS;
+    Raw dy[passes], x;
+    RawS slope[passes];
+    const auto row_of = [&](int64_t tile, int r) { const int64_t row = tile * ROWS + r; return row < a.rows ? row : a.rows - 1; };
+    const auto fetch = [&](int64_t tile, int u) {
+        if (!mine) return;
+        const int64_t row = row_of(tile, r0 + u * per);
+        dy[u] = *reinterpret_cast<const Raw *>(static_cast<const T *>(a.dy) + row * a.dy_stride + c);
+        if (a.slope) slope[u] = *reinterpret_cast<const RawS *>(static_cast<const S *>(a.slope) + row * out + c);
+    };
+    const auto fetch_x = [&](int64_t tile) {
+        if (mine_x) x = *reinterpret_cast<const Raw *>(static_cast<const T *>(a.x) + row_of(tile, xr) * a.x_stride + xc);
+    };
+    int64_t tile = blockIdx.x;
+#pragma unroll
+    for (int u = 0; u < passes; ++u) fetch(tile, u);
+    fetch_x(tile);
+    // what is behind the ends stays 0
+    for (int id = tid; id < (int)(narrow_lds(L, out, in) / 16); id += kNarrowT) *reinterpret_cast<u4 *>(lds + id * 16) = u4{0, 0, 0, 0};
+    __syncthreads();
+    for (int id = a.w ? tid : out * in; id < out * in; id += kNarrowT) {
+        const int n = id / in, k = id - n * in;
+        *reinterpret_cast<T *>(ldsW + k * pitch + n * 2) = static_cast<const T *>(a.w)[n * a.w_stride + k];
+    }
+    DropKey key = {};
+    if (a.drop.threshold) key = key_of(a.drop);
+    float sum[8] = {};
+    f4 dw[4]; // 16 rows of dw, up to 64 columns
+#pragma unroll
+    for (int t = 0; t < 4; ++t) dw[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    // a number of 16 rows x 16 columns that lie at 4 k a lane, turned
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s4 *At;
+    const auto turned = [&](const char *from, int p) {
+        const char *q = from + (chunk * 8 + (lane >> 2 & 3)) * p + (lane & 3) * 8;
+        const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)q));
+        const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(q + 4 * p)));
+        return u4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    for (; tile < all; tile += gridDim.x) {
+        const int64_t next = tile + gridDim.x;
+        const auto pass = [&](auto u) {
+            const int r = r0 + u * per;
+            const int64_t row = tile * ROWS + r;
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = (float)dy[u][i];
+            if (a.slope)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= Slope<T>::take(slope[u][i]);
+            fetch(next, u);
+            if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
+            const bool there = row < a.rows;
+            Raw g;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[i] = there ? d[i] : 0.0f;
+                sum[i] += d[i];
+                g[i] = (T)d[i];
+            }
+            *reinterpret_cast<Raw *>(lds + r * pitch + c * 2) = g;
+            __builtin_amdgcn_sched_barrier(0); // one after the other: side by side registers do not hold them
+        };
+        if (mine) {
+            pass(std::integral_constant<int, 0>());
+            if constexpr (passes > 1) pass(std::integral_constant<int, 1>());
+            static_assert(passes <= 2, "two passes at most");
+        }
+        if (mine_x) {
+            Raw g = x;
+            if (tile * ROWS + xr >= a.rows)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] = (T)0.0f;
+            *reinterpret_cast<Raw *>(ldsX + xr * pitch_x + xc * 2) = g;
+        }
+        fetch_x(next);
+        __syncthreads();
+        if (a.dx) { // 16 rows and J tiles of 16 columns to a wavefront
+            const int rt = wave * J / 4, ct = wave * J % 4;
+            f4 s[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j) s[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (ct < tiles_k)
+                for (int t = 0; t < steps; ++t) {
+                    const u4 p = *reinterpret_cast<const u4 *>(lds + (rt * 16 + at) * pitch + t * 64 + chunk * 16);
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        if (ct + j < tiles_k) s[j] = mfma(T(), p, *reinterpret_cast<const u4 *>(ldsW + ((ct + j) * 16 + at) * pitch + t * 64 + chunk * 16), s[j]);
+                }
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int col = (ct + j) * 16 + at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t row = tile * ROWS + rt * 16 + chunk * 4 + e;
+                    if (ct + j < tiles_k && col < in && row < a.rows) static_cast<T *>(a.dx)[row * in + col] = (T)s[j][e];
+                }
+            }
+        }
+        if (a.part && wave * 16 < out) // dw: 16 of its rows to a wavefront
+#pragma unroll
+            for (int t = 0; t < ROWS / 32; ++t) {
+                const u4 p = turned(lds + t * 32 * pitch + wave * 32, pitch);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < tiles_k) dw[j] = mfma(T(), p, turned(ldsX + t * 32 * pitch_x + j * 32, pitch_x), dw[j]);
+            }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int n = wave * 16 + chunk * 4 + e, k = j * 16 + at;
+            if (a.part && n < out && k < in) a.part[((int64_t)blockIdx.x * out + n) * in + k] = dw[j][e];
+        }
+    float(*const sums)[9] = reinterpret_cast<float(*)[9]>(lds); // what lay there has been read
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[tid][i] = sum[i];
+    __syncthreads();
+    for (int t = tid; t < out; t += kNarrowT) {
+        float s = 0.0f;
+        for (int q = 0; q < per; ++q) s += sums[q * L + t / 8][t % 8];
+        a.sums[(int64_t)blockIdx.x * out + t] = s;
+    }
+}
+
 // ---------------------------------------------------------------------------------- launches
 int64_t round16(int64_t n) { return up(n, 16) * 16; }
 
@@ -1367,6 +1528,12 @@ template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q
     return launched();
 }
 
+// Whether narrow_kernel takes a backward pass: rows enough to give every workgroup a few times 128.
+template <typename T> bool narrow(const pcsr_linear_t &a)
+{
+    return sizeof(T) == 2 && a.rows >= 512 * kNarrowBlocks && a.out <= 256 && a.in <= 64 && a.out > 0 && a.in > 0 && a.out % 8 == 0 && a.in % 8 == 0;
+}
+
 // the parts of the workspace of a backward call
 struct Space {
     int64_t ld, dz, sums, part, part_w, bytes;
@@ -1389,6 +1556,10 @@ struct Space {
         s.sums = round16(4 * s.blocks * a.out);
         const int64_t x = most_of(a.rows, a.in, a.out, true), w = most_of(a.out, a.in, a.rows, false);
         s.part = round16(x) + round16(w); // (for both at once)
+        if (narrow<T>(a)) {
+            const int64_t sums = round16(4 * kNarrowBlocks * a.out), part = round16(4 * kNarrowBlocks * a.out * a.in);
+            s.sums = sums > s.sums ? sums : s.sums, s.part = part > s.part ? part : s.part;
+        }
         s.part_w = round16(x);
         s.bytes = s.dz + s.sums + s.part;
         return s;
@@ -1439,6 +1610,27 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
     char *at = static_cast<char *>(ws);
     float *sums = reinterpret_cast<float *>(at + sp.dz);
     void *part = at + sp.dz + sp.sums;
+    if (narrow<T>(a)) { // whatever is asked for, so that the bits do not depend on that
+        if constexpr (sizeof(T) == 2) {
+            const NarrowArgs n = {dy, a.act == PCSR_ACT_NONE ? nullptr : slope, dw ? a.x : nullptr, dx ? a.w : nullptr, dy_stride, a.x_stride, a.w_stride, a.rows, (int)a.in, (int)a.out, dx,
+                                  dw ? static_cast<float *>(part) : nullptr, sums, drop_of(&a.drop)};
+            const auto go = [&](auto *kernel, int lanes) {
+                const size_t lds = (size_t)narrow_lds(lanes, a.out, a.in), bytes = lds > kNarrowT * 36 ? lds : kNarrowT * 36;
+                if (!allow_lds(kernel, bytes)) return (int)PCSR_E_HIP;
+                hipLaunchKernelGGL(kernel, dim3(kNarrowBlocks), dim3(kNarrowT), bytes, stream, n);
+                return (int)PCSR_OK;
+            };
+            if (const int rc = a.out <= 64 ? go(&narrow_kernel<T, 8>, 8) : a.out <= 128 ? go(&narrow_kernel<T, 16>, 16) : go(&narrow_kernel<T, 32>, 32)) return rc;
+            Plan p = {};
+            p.stretches = kNarrowBlocks;
+            unsigned blocks = 0;
+            FinishArgs f = {};
+            if (dw) f = finish_args(p, n.part, {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)}, &blocks);
+            const SumsArgs b = {sums, kNarrowBlocks, a.out, a.bias_type, db};
+            if (dw || db) hipLaunchKernelGGL(last_kernel<T>, dim3(blocks + (db ? (unsigned)up(a.out, 16) : 0)), dim3(kT), 0, stream, FinishArgs{}, f, b, 0, (int)blocks);
+            return launched();
+        }
+    }
     Side dz = {dy, dy_stride, a.rows};
     if (own || db) {
         SlopeArgs s = {dy, a.act == PCSR_ACT_NONE ? nullptr : slope, dy_stride, a.rows, a.out, sp.ld, own && (dx || dw) ? at : nullptr,

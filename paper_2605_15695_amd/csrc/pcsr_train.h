@@ -114,7 +114,7 @@ typedef struct {
 int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward);
 // slope: null, or [rows x out] for the backward call where act is not none: the activation's slopes, fp32 for fp32 and otherwise
 // 16 bits, 2^15 (slope + 1/4) (0: not a number).
-// TOO_LARGE: rows of 2^32 and more, in or out of 2^31, and more than 2^23 tiles of 64 x 64 of y, of dx or of dw.
+// TOO_LARGE: rows of 2^32 and more, in or out of 2^24 and more, and more than 2^23 tiles of 64 x 64 of y, of dx or of dw.
 int pcsr_linear(const pcsr_linear_t *a, void *y, void *slope, void *ws, void *stream);
 // From dy (rows dy_stride numbers apart): dx [rows x in], dw [out x in], db [out] of bias_type; each may be null.  a->bias and a->residual are not read; a->x is for
 // dw alone, a->w for dx.

@@ -26,7 +26,7 @@ def linear(X: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     The activation's slopes are kept for the backward pass, in float32 or, for 16-bit types, as 16 bits that are 2^-16 off at most; the gradient at
     X @ weight.T + bias has X's type.
     Sums are in an order that sizes and type alone decide: the same bits on every run.
-    PcsrError: 2^32 rows or 2^31 columns and more, and where X, weight or the result are of more than 2^23 tiles of 64 x 64.
+    PcsrError: 2^32 rows or 2^24 columns and more, and where X, weight or the result are of more than 2^23 tiles of 64 x 64.
     There is no forward-mode derivative."""
     fast = pc.train_module()
     if fast is not None and activation in ACTIVATIONS:

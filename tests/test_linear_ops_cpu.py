@@ -74,8 +74,8 @@ def test_linear_entry_points():
             assert call(**bad) == INVALID, bad
         for bad in (dict(type=3), dict(type=-1), dict(act=4), dict(act=-1), dict(bias_type=1), dict(type=1, bias_type=2)):
             assert call(**bad) == UNSUPPORTED, bad
-        # tiles of 64 x 64 past 2^23: 2^18 rows of 2^17 and more, and rows and columns past 32 bits
-        for bad in (dict(rows=(1 << 18) + 1, out=1 << 17), dict(rows=1 << 32), dict(out=1 << 31), {"in": 1 << 31, "x_stride": 1 << 31, "w_stride": 1 << 31},
+        # tiles of 64 x 64 past 2^23: 2^18 rows of 2^17 and more, and too many rows and columns
+        for bad in (dict(rows=(1 << 18) + 1, out=1 << 17), dict(rows=1 << 32), dict(out=1 << 24), {"in": 1 << 24, "x_stride": 1 << 24, "w_stride": 1 << 24},
                     {"out": 1 << 20, "in": 1 << 20, "x_stride": 1 << 20, "w_stride": 1 << 20}):
             assert call(**bad) == TOO_LARGE, bad
     assert fwd(y=None) == INVALID and fwd(residual=P, r_stride=13) == INVALID and fwd(rows=0, y=None, x=None) == OK
