@@ -1391,7 +1391,12 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct)
     const auto tiles_of = [&](int which) { return up(I, BI[which]) * up(J, BJ[which]); };
     int64_t wanted = kWanted;
     p.which = (I <= 64 ? FLAT : WIDE) + (J <= 64 ? 1 : 0);
-    if (direct && I > 128 && J > 128 && tiles_of(LARGE) * most >= 192) p.which = LARGE, wanted = 256;
+    if (direct && I > 128 && J > 128 && tiles_of(LARGE) * most >= 192) {
+        // One to a compute unit, in 0.87 of the time that four of 128 x 128 take, of which two run side by side: rounds of the one against rounds of the other
+        // (32,768 x 1000 x 768, 384 tiles in two rounds: 81 us, 1536 in three 74; 32,768 x 768 x 1000, 512 and 2048 in two and four: 87 and 110).
+        const bool rounds = tiles_of(LARGE) >= 256 && 200 * up(tiles_of(WIDE), 512) < 348 * up(tiles_of(LARGE), 256);
+        if (!rounds) p.which = LARGE, wanted = 256;
+    }
     if (sizeof(T) == 4 && I > 64 && J > 64 && K >= 64) {
         const int which = tiles_of(PIECES_TALL) < tiles_of(PIECES_FLAT) ? PIECES_TALL : PIECES_FLAT;
         if (tiles_of(which) * most >= 192) p.which = which, wanted = 256;
