@@ -1373,42 +1373,62 @@ template <typename T> bool straight(const Side &s, bool turned, bool padded)
     return sizeof(T) == 2 && s.ld % 8 == 0 && (uintptr_t)s.at % 16 == 0 && s.ld < (1 << 22) && (!turned || s.n % 8 == 0 || padded);
 }
 
-// How a product of I x J numbers over K is cut.  The widest tiles that the result fills; where they are too few for the chip k is cut into
-// stretches, whose sums go through memory, and where it is too short for that tiles are of 64 x 64.
+// How a product of I x J numbers over K is cut: into tiles, and k into stretches, whose sums go through memory, where tiles are too few for the chip.  By what each
+// way would take, in us: a workgroup `fixed` and, for a stage, `stage` alone on a compute unit and `beside` more for each of up to `most` that run there side by
+// side; sums of stretches a launch and their bytes, twice.  The numbers are fitted to 64 products of 16 to 4096 columns over 64 to 250,000 numbers of k, in every
+// way they can be cut; what is picked takes 1.05 (16 bits, straight), 1.02 (16 bits) and 1.01 (fp32) of the best of them, at most 1.27, where
+// the widest tiles that fill the chip, in as many stretches as that takes, took up to 2.8 (1024^3 in bf16: 20.8 us, now 9.4; 2048^3 39.6 and 23).
 struct Plan {
     int which; // tiling
     int64_t tiles_i, tiles_j, stretch;
     int stretches;
+    float us;
 };
-enum { WIDE, TALL, FLAT, SMALL, LARGE, PIECES_FLAT, PIECES_TALL };
-template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct)
+enum { WIDE, TALL, FLAT, SMALL, LARGE, PIECES_FLAT, PIECES_TALL, TILINGS };
+constexpr int kTileI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI, Large::BI, PiecesFlat::BI, PiecesTall::BI};
+constexpr int kTileJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ, Large::BJ, PiecesFlat::BJ, PiecesTall::BJ};
+struct Cost {
+    float fixed, stage, beside;
+    int most; // 0: no such way
+};
+struct Costs {
+    float launch, bytes; // of sums of stretches; bytes in a us
+    Cost of[TILINGS];
+};
+constexpr Costs kStraight16 = {2.8f, 5.3e6f, {{2.4f, 0.55f, 0.28f, 2}, {2.0f, 0.48f, 0.13f, 3}, {2.2f, 0.47f, 0.14f, 3}, {1.8f, 0.50f, 0.085f, 4}, {5.4f, 1.07f, 0.4f, 1}, {}, {}}};
+constexpr Costs kAny16 = {3.1f, 7.7e6f, {{4.3f, 1.08f, 0.51f, 2}, {2.5f, 0.84f, 0.30f, 3}, {2.6f, 0.85f, 0.26f, 3}, {2.1f, 0.51f, 0.24f, 5}, {}, {}, {}}};
+constexpr Costs kAny32 = {3.9f, 6.9e6f, {{2.3f, 2.10f, 0.99f, 2}, {0.8f, 1.47f, 0.62f, 3}, {0.7f, 1.53f, 0.62f, 2}, {0.0f, 1.02f, 0.38f, 4}, {}, {7.4f, 2.34f, 0.4f, 1}, {7.1f, 2.56f, 0.4f, 1}}};
+
+// only: one tiling, or -1
+template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, int only = -1)
 {
-    constexpr int64_t kWanted = 512; // workgroups: two to a compute unit
-    static const int BI[] = {Wide::BI, Tall::BI, Flat::BI, Small::BI, Large::BI, PiecesFlat::BI, PiecesTall::BI};
-    static const int BJ[] = {Wide::BJ, Tall::BJ, Flat::BJ, Small::BJ, Large::BJ, PiecesFlat::BJ, PiecesTall::BJ};
-    Plan p;
-    const int64_t stages = up(K, Num<T>::KS), most = stages / 4 < 1 ? 1 : stages / 4;
-    const auto tiles_of = [&](int which) { return up(I, BI[which]) * up(J, BJ[which]); };
-    int64_t wanted = kWanted;
-    p.which = (I <= 64 ? FLAT : WIDE) + (J <= 64 ? 1 : 0);
-    if (direct && I > 128 && J > 128 && tiles_of(LARGE) * most >= 192) {
-        // One to a compute unit, in 0.87 of the time that four of 128 x 128 take, of which two run side by side: rounds of the one against rounds of the other
-        // (32,768 x 1000 x 768, 384 tiles in two rounds: 81 us, 1536 in three 74; 32,768 x 768 x 1000, 512 and 2048 in two and four: 87 and 110).
-        const bool rounds = tiles_of(LARGE) >= 256 && 200 * up(tiles_of(WIDE), 512) < 348 * up(tiles_of(LARGE), 256);
-        if (!rounds) p.which = LARGE, wanted = 256;
+    constexpr int64_t kUnits = 256;
+    const Costs &costs = sizeof(T) == 4 ? kAny32 : direct ? kStraight16 : kAny16;
+    const int64_t stages = up(K, Num<T>::KS), most = stages / 2 < 1 ? 1 : stages / 2;
+    Plan best = {};
+    best.us = -1.0f;
+    for (int which = 0; which < TILINGS; ++which) {
+        const Cost &c = costs.of[which];
+        if (c.most == 0 || (only >= 0 && which != only) || (which >= PIECES_FLAT && K < 64)) continue;
+        const int64_t ti = up(I, kTileI[which]), tj = up(J, kTileJ[which]), tiles = ti * tj;
+        const int64_t fill = tiles < kUnits ? kUnits / (tiles ? tiles : 1) : 1;
+        int64_t before = 0;
+        for (const int64_t want : {int64_t(1), fill, 2 * fill, c.most * fill}) {
+            int64_t s = want < most ? want : most;
+            if (tiles >= 2 * kUnits || 4 * I * J * s > int64_t(1) << 30) s = 1;
+            if (s <= before) continue;
+            before = s;
+            const int64_t each = up(stages, s);
+            s = stages ? up(stages, each) : 1;
+            const int64_t all = tiles * s, full = all / (kUnits * c.most), rest = all - full * kUnits * c.most;
+            float us = (float)full * (c.fixed + (float)each * (c.stage + c.beside * (float)(c.most - 1)));
+            if (rest) us += c.fixed + (float)each * (c.stage + c.beside * (float)(up(rest, kUnits) - 1));
+            if (s > 1) us += costs.launch + (float)(8 * I * J * s) / costs.bytes;
+            if (which >= PIECES_FLAT) us += (float)(10 * J * K) / 5e6f;
+            if (best.us < 0.0f || us < best.us) best = {which, ti, tj, each * Num<T>::KS, (int)s, us};
+        }
     }
-    if (sizeof(T) == 4 && I > 64 && J > 64 && K >= 64) {
-        const int which = tiles_of(PIECES_TALL) < tiles_of(PIECES_FLAT) ? PIECES_TALL : PIECES_FLAT;
-        if (tiles_of(which) * most >= 192) p.which = which, wanted = 256;
-    }
-    if (tiles_of(p.which) * most < 256 && wanted == kWanted) p.which = SMALL;
-    p.tiles_i = up(I, BI[p.which]), p.tiles_j = up(J, BJ[p.which]);
-    const int64_t tiles = p.tiles_i * p.tiles_j;
-    int64_t s = tiles >= wanted ? 1 : wanted / (tiles ? tiles : 1);
-    if (s > most) s = most;
-    p.stretch = up(stages, s) * Num<T>::KS;
-    p.stretches = (int)(K ? up(K, p.stretch) : 1);
-    return p;
+    return best;
 }
 int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
 // planes of weights, and whether numbers in them are too large
@@ -1474,7 +1494,7 @@ FinishArgs finish_args(const Plan &c, const float *part, const Tail &tail, unsig
 }
 
 // direct: both operands' pieces can go straight to LDS
-template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, bool direct, const Tail &tail, void *ws, hipStream_t stream)
+template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q, int64_t K, bool direct, const Plan &c, const Tail &tail, void *ws, hipStream_t stream)
 {
     if constexpr (!TP) {
         if (many_rows<T>(p.n, q.n, K, direct)) {
@@ -1483,7 +1503,6 @@ template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q
             return rc == PCSR_OK ? launched() : rc;
         }
     }
-    const Plan c = plan<T>(p.n, q.n, K, direct);
     TileArgs a = {p, q, K, c.stretch, (int)c.tiles_i, (int)c.tiles_j, c.stretches, c.stretches > 1 ? static_cast<float *>(ws) : nullptr, tail};
     const unsigned grid = (unsigned)(c.tiles_i * c.tiles_j * c.stretches);
     int rc = PCSR_OK;
@@ -1548,8 +1567,12 @@ struct Space {
     {
         Space s;
         const auto most_of = [](int64_t I, int64_t J, int64_t K, bool weights) { // however the operands lie
-            const int64_t x = product_bytes(plan<T>(I, J, K, false), I, J, K, weights), y = product_bytes(plan<T>(I, J, K, true), I, J, K, weights);
-            return x > y ? x : y;
+            int64_t most = product_bytes(plan<T>(I, J, K, false, SMALL), I, J, K, weights);
+            for (int direct = 0; direct < (sizeof(T) == 2 ? 2 : 1); ++direct) {
+                const int64_t need = product_bytes(plan<T>(I, J, K, direct), I, J, K, weights);
+                most = need > most ? need : most;
+            }
+            return most;
         };
         s.ld = up(a.out, 8) * 8;
         s.lanes = 1;
@@ -1604,7 +1627,8 @@ template <typename T> int LinearOf<T>::forward(const pcsr_linear_t &a, void *y, 
     const Tail tail = {a.bias, a.residual, y, a.act == PCSR_ACT_NONE ? nullptr : slope, a.r_stride, a.rows, a.out, a.act, a.bias_type, drop_of(&a.drop)};
     const Side x = {a.x, a.x_stride, a.rows}, w = {a.w, a.w_stride, a.out};
     if (a.rows <= kFew) return few_rows<T>({x, w, a.in, a.in, 1, 1, 1, nullptr, tail}, stream);
-    return product<T, false, false>(x, w, a.in, forward_direct<T>(a), tail, ws, stream);
+    const bool direct = forward_direct<T>(a);
+    return product<T, false, false>(x, w, a.in, direct, plan<T>(a.rows, a.out, a.in, direct), tail, ws, stream);
 }
 
 template <typename T>
@@ -1650,8 +1674,14 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
     const bool direct_x = a.out % 8 == 0 && straight<T>(dz, false, false) && straight<T>(w, true, false), direct_w = straight<T>(g, true, own) && straight<T>(x, true, false);
     int rc = launched();
     if (rc != PCSR_OK) return rc;
-    const Plan px = plan<T>(a.rows, a.in, a.out, direct_x), pw = plan<T>(a.out, a.in, a.rows, direct_w);
-    if (dx && dw && a.in > 0 && px.which == SMALL && pw.which == SMALL && !many_rows<T>(a.rows, a.in, a.out, direct_x)) {
+    Plan px = plan<T>(a.rows, a.in, a.out, direct_x), pw = plan<T>(a.out, a.in, a.rows, direct_w);
+    const bool rows = many_rows<T>(a.rows, a.in, a.out, direct_x);
+    { // tiles of 64 x 64 for both, where side by side they take less; whatever is asked for, so that the bits do not depend on that
+        const Plan sx = plan<T>(a.rows, a.in, a.out, direct_x, SMALL), sw = plan<T>(a.out, a.in, a.rows, direct_w, SMALL);
+        const bool fit = sx.tiles_i * sx.tiles_j * sx.stretches + sw.tiles_i * sw.tiles_j * sw.stretches <= 1024;
+        if (!rows && fit && 1.1f * (sx.us > sw.us ? sx.us : sw.us) < px.us + pw.us + 4.0f) px = sx, pw = sw;
+    }
+    if (dx && dw && a.in > 0 && px.which == SMALL && pw.which == SMALL && !rows) {
         float *part_x = px.stretches > 1 ? static_cast<float *>(part) : nullptr;
         float *part_w = pw.stretches > 1 ? reinterpret_cast<float *>(static_cast<char *>(part) + sp.part_w) : nullptr;
         const TileArgs ax = {dz, w, a.out, px.stretch, (int)px.tiles_i, (int)px.tiles_j, px.stretches, part_x, tail_x};
@@ -1670,8 +1700,8 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
         hipLaunchKernelGGL(sums_kernel, dim3((unsigned)up(a.out, 16)), dim3(1024), 0, stream, b);
         rc = launched();
     }
-    if (dx && a.in > 0 && rc == PCSR_OK) rc = product<T, false, true>(dz, w, a.out, direct_x, tail_x, part, stream);
-    if (dw && a.in > 0 && rc == PCSR_OK) rc = product<T, true, true>(g, x, a.rows, direct_w, tail_w, part, stream);
+    if (dx && a.in > 0 && rc == PCSR_OK) rc = product<T, false, true>(dz, w, a.out, direct_x, px, tail_x, part, stream);
+    if (dw && a.in > 0 && rc == PCSR_OK) rc = product<T, true, true>(g, x, a.rows, direct_w, pw, tail_w, part, stream);
     return rc;
 }
 
