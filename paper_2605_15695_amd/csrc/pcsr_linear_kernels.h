@@ -1395,12 +1395,12 @@ struct Costs {
     float launch, bytes; // of sums of stretches; bytes in a us
     Cost of[TILINGS];
 };
-constexpr Costs kStraight16 = {2.8f, 5.3e6f, {{2.4f, 0.55f, 0.28f, 2}, {2.0f, 0.48f, 0.13f, 3}, {2.2f, 0.47f, 0.14f, 3}, {1.8f, 0.50f, 0.085f, 4}, {5.4f, 1.07f, 0.4f, 1}, {}, {}}};
+constexpr Costs kStraight16 = {2.8f, 5.3e6f, {{2.4f, 0.55f, 0.28f, 2}, {2.0f, 0.48f, 0.13f, 3}, {2.2f, 0.47f, 0.14f, 3}, {1.8f, 0.50f, 0.085f, 4}, {8.0f, 1.07f, 0.4f, 1}, {}, {}}};
 constexpr Costs kAny16 = {3.1f, 7.7e6f, {{4.3f, 1.08f, 0.51f, 2}, {2.5f, 0.84f, 0.30f, 3}, {2.6f, 0.85f, 0.26f, 3}, {2.1f, 0.51f, 0.24f, 5}, {}, {}, {}}};
 constexpr Costs kAny32 = {3.9f, 6.9e6f, {{2.3f, 2.10f, 0.99f, 2}, {0.8f, 1.47f, 0.62f, 3}, {0.7f, 1.53f, 0.62f, 2}, {0.0f, 1.02f, 0.38f, 4}, {}, {7.4f, 2.34f, 0.4f, 1}, {7.1f, 2.56f, 0.4f, 1}}};
 
-// only: one tiling, or -1
-template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, int only = -1)
+// weights: q is W, whose planes PIECES_* write first; only: one tiling, or -1
+template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, bool weights, int only = -1)
 {
     constexpr int64_t kUnits = 256;
     const Costs &costs = sizeof(T) == 4 ? kAny32 : direct ? kStraight16 : kAny16;
@@ -1424,7 +1424,7 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, in
             float us = (float)full * (c.fixed + (float)each * (c.stage + c.beside * (float)(c.most - 1)));
             if (rest) us += c.fixed + (float)each * (c.stage + c.beside * (float)(up(rest, kUnits) - 1));
             if (s > 1) us += costs.launch + (float)(8 * I * J * s) / costs.bytes;
-            if (which >= PIECES_FLAT) us += (float)(10 * J * K) / 5e6f;
+            if (which >= PIECES_FLAT && weights) us += (float)(10 * J * K) / 5e6f;
             if (best.us < 0.0f || us < best.us) best = {which, ti, tj, each * Num<T>::KS, (int)s, us};
         }
     }
@@ -1567,9 +1567,9 @@ struct Space {
     {
         Space s;
         const auto most_of = [](int64_t I, int64_t J, int64_t K, bool weights) { // however the operands lie
-            int64_t most = product_bytes(plan<T>(I, J, K, false, SMALL), I, J, K, weights);
+            int64_t most = product_bytes(plan<T>(I, J, K, false, weights, SMALL), I, J, K, weights);
             for (int direct = 0; direct < (sizeof(T) == 2 ? 2 : 1); ++direct) {
-                const int64_t need = product_bytes(plan<T>(I, J, K, direct), I, J, K, weights);
+                const int64_t need = product_bytes(plan<T>(I, J, K, direct, weights), I, J, K, weights);
                 most = need > most ? need : most;
             }
             return most;
@@ -1597,7 +1597,7 @@ template <typename T> bool forward_direct(const pcsr_linear_t &a)
 {
     return a.in % 8 == 0 && straight<T>({a.x, a.x_stride, a.rows}, false, false) && straight<T>({a.w, a.w_stride, a.out}, false, false);
 }
-template <typename T> Plan forward_plan(const pcsr_linear_t &a) { return plan<T>(a.rows, a.out, a.in, forward_direct<T>(a)); }
+template <typename T> Plan forward_plan(const pcsr_linear_t &a) { return plan<T>(a.rows, a.out, a.in, forward_direct<T>(a), true); }
 bool has_slope(const pcsr_linear_t &a) { return a.act != PCSR_ACT_NONE || drop_of(&a.drop).threshold; }
 
 // Rows that few_kernel takes: more of them are read again by every group of lanes.
@@ -1628,7 +1628,7 @@ template <typename T> int LinearOf<T>::forward(const pcsr_linear_t &a, void *y, 
     const Side x = {a.x, a.x_stride, a.rows}, w = {a.w, a.w_stride, a.out};
     if (a.rows <= kFew) return few_rows<T>({x, w, a.in, a.in, 1, 1, 1, nullptr, tail}, stream);
     const bool direct = forward_direct<T>(a);
-    return product<T, false, false>(x, w, a.in, direct, plan<T>(a.rows, a.out, a.in, direct), tail, ws, stream);
+    return product<T, false, false>(x, w, a.in, direct, plan<T>(a.rows, a.out, a.in, direct, true), tail, ws, stream);
 }
 
 template <typename T>
@@ -1674,10 +1674,10 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
     const bool direct_x = a.out % 8 == 0 && straight<T>(dz, false, false) && straight<T>(w, true, false), direct_w = straight<T>(g, true, own) && straight<T>(x, true, false);
     int rc = launched();
     if (rc != PCSR_OK) return rc;
-    Plan px = plan<T>(a.rows, a.in, a.out, direct_x), pw = plan<T>(a.out, a.in, a.rows, direct_w);
+    Plan px = plan<T>(a.rows, a.in, a.out, direct_x, true), pw = plan<T>(a.out, a.in, a.rows, direct_w, false);
     const bool rows = many_rows<T>(a.rows, a.in, a.out, direct_x);
     { // tiles of 64 x 64 for both, where side by side they take less; whatever is asked for, so that the bits do not depend on that
-        const Plan sx = plan<T>(a.rows, a.in, a.out, direct_x, SMALL), sw = plan<T>(a.out, a.in, a.rows, direct_w, SMALL);
+        const Plan sx = plan<T>(a.rows, a.in, a.out, direct_x, true, SMALL), sw = plan<T>(a.out, a.in, a.rows, direct_w, false, SMALL);
         const bool fit = sx.tiles_i * sx.tiles_j * sx.stretches + sw.tiles_i * sw.tiles_j * sw.stretches <= 1024;
         if (!rows && fit && 1.1f * (sx.us > sw.us ? sx.us : sw.us) < px.us + pw.us + 4.0f) px = sx, pw = sw;
     }
