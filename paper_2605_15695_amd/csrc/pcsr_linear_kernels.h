@@ -11,7 +11,7 @@
 // fp32 numbers are three bf16 numbers each, x = p0 + p1 + p2 exactly (8 bits each), and a product is the six p q of order 2^-16 and more,
 // six instructions of 16 times the fp32 rate (the method: Henry, Tang and Heinecke, "Leveraging the bfloat16 Artificial Intelligence Datatype For
 // Higher-Precision Computations", ARITH 2019).  Numbers are split 2^16 times as large, so that small ones keep all their pieces.  A tile that has
-// met numbers of 2^38 and more (products of which would leave the range; an infinity's pieces are none) is done again in fp32.
+// met numbers of 2^31 and more is done again in fp32: of smaller ones 2^32 products, 2^94 each as they are split, stay in the range (an infinity's pieces are none).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -31,7 +31,7 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
 constexpr int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by; }
 constexpr int kT = 256;
-constexpr float kUp = 65536.0f, kDown = 1.0f / (65536.0f * 65536.0f), kHot = 0x1p54f; // 2^38 of a number as it is split
+constexpr float kUp = 65536.0f, kDown = 1.0f / (65536.0f * 65536.0f), kHot = 0x1p47f; // 2^31 of a number as it is split
 
 // what an operand's numbers are in LDS
 template <typename T> struct Num {
@@ -1420,6 +1420,7 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, bo
             before = s;
             const int64_t each = up(stages, s);
             s = stages ? up(stages, each) : 1;
+            if (which >= PIECES_FLAT && each * Num<T>::KS >= int64_t(1) << 31) continue; // (which count k of a stretch in 32 bits)
             const int64_t all = tiles * s, full = all / (kUnits * c.most), rest = all - full * kUnits * c.most;
             float us = (float)full * (c.fixed + (float)each * (c.stage + c.beside * (float)(c.most - 1)));
             if (rest) us += c.fixed + (float)each * (c.stage + c.beside * (float)(up(rest, kUnits) - 1));

@@ -110,13 +110,13 @@ typedef struct {
     int64_t x_stride, w_stride, r_stride;
     pcsr_drop_t drop;
 } pcsr_linear_t;
-// bytes of workspace (16-byte aligned) of the calls below; backward: those for all of its results
+// bytes of workspace (16-byte aligned) of the calls below with the same a; backward: those for all of its results
 int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward);
 // slope: null, or [rows x out] for the backward call where act is not none: the activation's slopes, fp32 for fp32 and otherwise
 // 16 bits, 2^15 (slope + 1/4) (0: not a number).
 // TOO_LARGE: rows of 2^32 and more, in or out of 2^24 and more, and more than 2^23 tiles of 64 x 64 of y, of dx or of dw.
 int pcsr_linear(const pcsr_linear_t *a, void *y, void *slope, void *ws, void *stream);
-// From dy (rows dy_stride numbers apart): dx [rows x in], dw [out x in], db [out] of bias_type; each may be null.  a->bias and a->residual are not read; a->x is for
+// From dy (rows dy_stride numbers apart): dx [rows x in], dw [out x in], db [out] of bias_type; each may be null (rows of 0: nothing is written).  a->bias and a->residual are not read; a->x is for
 // dw alone, a->w for dx.
 int pcsr_linear_backward(const pcsr_linear_t *a, const void *slope, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws,
                          void *stream);

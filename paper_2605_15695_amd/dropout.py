@@ -126,7 +126,8 @@ class Dropout(torch.nn.Module):
     """dropout with a seed of its own and an offset that every call in training counts up, both in ``counter``, a
     buffer: on the GPU, so that a captured graph drops others on every replay, and in the state_dict, so that a resumed training goes on with
     what comes next.  seed: an integer, or none: drawn from torch's default generator.  Copies of a module drop the same; ranks of
-    a job that are seeded alike do too, unless they are given seeds of their own."""
+    a job that are seeded alike, or that are sent one rank's buffers, do too, unless they are given seeds of their own.  A forward pass that is run
+    again for its activations counts on: there, call dropout with the step's own seed and offset."""
 
     def __init__(self, p: float = 0.5, seed: int | None = None):
         super().__init__()
