@@ -150,20 +150,17 @@ template <int KS> __device__ __forceinline__ int place(int row, int chunk)
     return (row * (KS / 8) + (chunk ^ turn)) * 16;
 }
 
-__device__ __forceinline__ uint32_t two(bfloat_t a, bfloat_t b)
-{
-    return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
-}
 // two numbers side by side in k, in pieces
 __device__ __forceinline__ void pieces(float x, float y, float &hot, uint32_t (&p)[3])
 {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef bfloat_t b2 __attribute__((ext_vector_type(2)));
     x *= kUp, y *= kUp;
     hot = __builtin_fmaxf(hot, __builtin_fmaxf(__builtin_fabsf(x), __builtin_fabsf(y)));
 #pragma unroll
     for (int o = 0; o < 3; ++o) {
-        const bfloat_t a = (bfloat_t)x, b = (bfloat_t)y;
-        p[o] = two(a, b);
-        if (o < 2) x -= (float)a, y -= (float)b;
+        p[o] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{x, y}), b2)); // both in one instruction
+        if (o < 2) x -= __builtin_bit_cast(float, p[o] << 16), y -= __builtin_bit_cast(float, p[o] & 0xffff0000u);
     }
 }
 
@@ -320,6 +317,12 @@ __device__ __forceinline__ void once_more(const TileArgs &a, int64_t row, int64_
 // of y, and what one call of the generator is for.  again: the numbers are added up once more, in fp32.
 template <typename C, int G> constexpr int out_bytes() { return C::WI * C::WJ * G * 16 * (C::FJ * 16 + 4) * 4; }
 
+// Numbers that are used under a condition are waited for in front of it: where one path waits and another does not, a wait for everything follows behind them.
+__device__ __forceinline__ void arrived(float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(x[i]));
+}
 struct Where { // of a wavefront's sums
     int64_t i0, col; // first row, a lane's column
     int m;           // columns that are there from it on
@@ -329,10 +332,10 @@ struct Where { // of a wavefront's sums
 };
 // The rows that lie in LDS.  WHOLE: 8 columns are there or none.  RES: residuals come four rows ahead, since each is a round trip to memory.
 template <typename T, bool TP, bool TQ, int ROWS, int LD, int PER, bool WHOLE, bool RES>
-__device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &key, const Where &w, const float *own, const float (&bias)[8])
+__device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &key, const Where &w, const float *own, const float (&bias)[8], int lane)
 {
     constexpr int NP = Num<T>::NP, step = 64 / PER, passes = ROWS / step, A = RES ? (passes < 4 ? passes : 4) : 1;
-    const int lane = threadIdx.x & 63, r0 = lane / PER, c = lane % PER * 8;
+    const int r0 = lane / PER, c = lane % PER * 8;
     if (w.m <= 0) return;
 #pragma unroll 1
     for (int n = 0; n < passes; n += A) {
@@ -351,6 +354,7 @@ __device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &ke
             const int64_t row = w.i0 + r;
             float v[8];
             const f4 lo = *reinterpret_cast<const f4 *>(own + r * LD + c), hi = *reinterpret_cast<const f4 *>(own + r * LD + c + 4);
+            if (RES) arrived(res[u]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 v[e] = NP == 3 ? lo[e] * kDown : lo[e];
@@ -370,22 +374,23 @@ __device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &ke
     }
 }
 template <typename T, bool TP, bool TQ, typename C, int G>
-__device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &sum, char *lds, int64_t i0, int64_t j0, int64_t k0, int64_t k1, int stretch, bool again)
+__device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &sum, char *lds, int64_t i0, int64_t j0, int64_t k0, int64_t k1, int stretch, bool again, int tid)
 {
     constexpr int FI = C::FI, FJ = C::FJ, LD = FJ * 16 + 4, per = FJ * 2; // lanes to a row
     static_assert(FI % G == 0, "whole passes");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / C::WJ, wj = wave % C::WJ, at = lane & 15, chunk = lane >> 4;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ, at = lane & 15, chunk = lane >> 4;
     float *own = reinterpret_cast<float *>(lds) + wave * G * 16 * LD;
     DropKey key = {};
     if (!a.part && a.tail.drop.threshold) {
         key = key_of(a.tail.drop);
-        if (blockIdx.x == 0 && threadIdx.x == 0) tell_key(a.tail.drop, key);
+        if (blockIdx.x == 0 && tid == 0) tell_key(a.tail.drop, key);
     }
     const bool whole = a.tail.cols % 8 == 0, res = a.tail.residual && !a.part;
     Where w = {0, j0 + wj * FJ * 16 + lane % per * 8, 0, k0, k1, stretch, again};
     w.m = a.tail.cols - w.col >= 8 ? 8 : a.tail.cols > w.col ? (int)(a.tail.cols - w.col) : 0;
     float bias[8];
     bias8<T, false>(a.tail, w.col, a.part ? 0 : w.m, bias);
+    arrived(bias);
     const auto pass = [&](auto g) { // (written out, not unrolled: loops of this length are not)
 #pragma unroll
         for (int i = 0; i < G; ++i)
@@ -396,10 +401,10 @@ __device__ __forceinline__ void finish_tile(const TileArgs &a, const Sums<C> &su
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         w.i0 = i0 + (wi * FI + g * G) * 16;
-        if (whole && res) finish_rows<T, TP, TQ, G * 16, LD, per, true, true>(a, key, w, own, bias);
-        else if (whole) finish_rows<T, TP, TQ, G * 16, LD, per, true, false>(a, key, w, own, bias);
-        else if (res) finish_rows<T, TP, TQ, G * 16, LD, per, false, true>(a, key, w, own, bias);
-        else finish_rows<T, TP, TQ, G * 16, LD, per, false, false>(a, key, w, own, bias);
+        if (whole && res) finish_rows<T, TP, TQ, G * 16, LD, per, true, true>(a, key, w, own, bias, lane);
+        else if (whole) finish_rows<T, TP, TQ, G * 16, LD, per, true, false>(a, key, w, own, bias, lane);
+        else if (res) finish_rows<T, TP, TQ, G * 16, LD, per, false, true>(a, key, w, own, bias, lane);
+        else finish_rows<T, TP, TQ, G * 16, LD, per, false, false>(a, key, w, own, bias, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
@@ -479,7 +484,7 @@ template <typename T, bool TP, bool TQ, typename C> __device__ __forceinline__ v
         __syncthreads();
         again = met;
     }
-    finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, again);
+    finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, again, tid);
 }
 template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads) tile_kernel(TileArgs a)
 {
@@ -664,14 +669,14 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
         multiply(units - 1, 0, GI);
     }
     __syncthreads(); // all of the last stage is read
-    finish_tile<T, TP, TQ, C, FI < 4 ? FI : 4>(a, sum, lds, i0, j0, k0, k1, stretch, false);
+    finish_tile<T, TP, TQ, C, FI < 4 ? FI : 4>(a, sum, lds, i0, j0, k0, k1, stretch, false, tid);
 }
 
 // ---------------------------------------------------------------------------------- large products of fp32 numbers
 // Weights are split once, into planes [piece][k / 32][row][32] with zeros behind the ends, so that 16 rows of a stage are 1 KB for one load straight to LDS; the
 // other operand, and both of a gradient of weights, are split on their way through registers.  Two stages of 32 numbers of k lie in LDS: while one is
 // multiplied the next is split, and the numbers of the two after it are on their way.  96 instructions of 16 cycles to a wavefront's stage.
-constexpr int kSplitBlocks = 256;
+constexpr int kSplitBlocks = 256, kUnits = 256;
 struct Planes {
     const bfloat_t *at;
     int64_t rows, plane; // padded rows, numbers of a plane
@@ -713,13 +718,189 @@ template <typename C> constexpr int pieces_bytes()
     constexpr int stages = 2 * (C::BI + C::BJ) * 64 * 3, out = out_bytes<C, 2>();
     return stages > out ? stages : out;
 }
-// a.q: the weights as they are, or the other operand of a gradient of weights
-template <bool TP, bool TQ, bool PLANES, typename C> __global__ void __launch_bounds__(C::threads, C::per) pieces_kernel(TileArgs a, Planes w)
+struct Spot { // a tile and its stretch of k, which is taken in pairs of stages, two at least
+    int64_t i0, j0;
+    int k0, k1, end, stretch;
+};
+template <typename C> __device__ __forceinline__ Spot spot_of(const TileArgs &a, int tile)
+{
+    Spot s;
+    int ti, tj;
+    place_of(a, tile, &ti, &tj, &s.stretch);
+    s.i0 = (int64_t)ti * C::BI, s.j0 = (int64_t)tj * C::BJ;
+    s.k0 = (int)(s.stretch * a.stretch), s.k1 = (int)(s.k0 + a.stretch < a.K ? s.k0 + a.stretch : a.K);
+    s.end = s.k0 + (s.k1 - s.k0 <= 128 ? 128 : (s.k1 - s.k0 + 63) / 64 * 64);
+    return s;
+}
+// The thread's number, from which the compiler is to work out addresses where they are used: kept in registers for a whole loop they leave sums no room.
+__device__ __forceinline__ int again_of(int tid)
+{
+    asm volatile("" : "+v"(tid));
+    return tid;
+}
+// Products with weights.  A compute unit's workgroup takes its tiles one behind the other, and the first numbers of a tile are on their way, and in LDS, while
+// what follows the one before it is done.  No load stands behind a condition, or waits behind it would be for all of them: places behind a row's end are read in front
+// of it, and what lies there is put right on its way to LDS.
+template <bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) planes_kernel(TileArgs a, Planes w)
 {
     typedef float T;
-    constexpr int KS = 32, FI = C::FI, FJ = C::FJ, planeP = C::BI * 64, planeQ = C::BJ * 64, stage = 3 * (planeP + planeQ), waves = C::threads / 64;
+    typedef typename Pack<float, 4>::type Raw;
+    constexpr int FI = C::FI, FJ = C::FJ, planeP = C::BI * 64, planeQ = C::BJ * 64, stage = 3 * (planeP + planeQ), waves = C::threads / 64, U = C::BI * 4 / C::threads;
     constexpr int loads = 3 * C::BJ / 16 / waves; // of planes, to a wavefront
-    static_assert(3 * C::BJ / 16 % waves == 0, "whole loads");
+    static_assert(3 * C::BJ / 16 % waves == 0 && C::BI * 4 % C::threads == 0 && out_bytes<C, 2>() <= stage, "whole loads, a tile's end in a stage");
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int met[2]; // large numbers of weights, of a tile's rows
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
+    const int all = a.tiles_i * a.tiles_j * a.stretches, beside = all < kUnits ? all : kUnits, K = (int)a.K;
+    if (tid < 2) met[tid] = 0;
+    __syncthreads();
+    if (tid < kSplitBlocks && w.hot[tid]) met[0] = 1;
+    float hot = 0.0f;
+    const char *first; // a tile's first row
+    uint32_t rows[U];  // numbers from there to a thread's rows
+    const auto rows_of = [&](int64_t i0) {
+        first = static_cast<const char *>(a.p.at) + i0 * a.p.ld * 4;
+        const int last = a.p.n - 1 - i0 < C::BI ? (int)(a.p.n - 1 - i0) : C::BI; // what comes of rows behind the last is not stored
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = (tid + u * C::threads) / 4;
+            rows[u] = (uint32_t)(row < last ? row : last) * (uint32_t)a.p.ld;
+        }
+    };
+    struct Numbers {
+        Raw raw[U][2];
+    } even, odd; // of stages
+    const auto fetch = [&](Numbers &n, int k) {
+        const int c = k + again_of(tid) % 4 * 8;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) n.raw[u][q] = *reinterpret_cast<const Raw *>(first + (rows[u] + (c + q * 4 < K - 4 ? c + q * 4 : K - 4)) * 4u);
+    };
+    const auto load_planes = [&](char *to, int64_t j0, int k) {
+        typedef __attribute__((address_space(3))) void *Lds;
+        typedef __attribute__((address_space(1))) const void *Global;
+        const int l = again_of(tid) & 63;
+        const uint32_t off = (l >> 2) * 64 + ((l & 3) ^ (l >> 4)) * 16;
+#pragma unroll
+        for (int u = 0; u < loads; ++u) {
+            const int b = u * waves + wave, o = b / (C::BJ / 16), row = b % (C::BJ / 16) * 16;
+            const char *from = reinterpret_cast<const char *>(w.at + o * w.plane + (k / 32 * w.rows + j0 + row) * 32);
+            __builtin_amdgcn_global_load_lds((Global)(from + off), (Lds)(to + 3 * planeP + o * planeQ + row * 64), 16, 0, 0);
+        }
+    };
+    const auto put = [&](char *to, Numbers &n, int k, int k1) { // numbers of k from k on; those behind k1 are 0
+        const int t = again_of(tid);
+        if (k + 32 > k1) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int c = k + t % 4 * 8 + q * 4, by = c < K - 4 ? 0 : c - (K - 4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { // (upwards: those behind it are as they were)
+                        float v = 0.0f;
+#pragma unroll
+                        for (int e = i; e < 4; ++e) v = by == e - i ? n.raw[u][q][e] : v;
+                        n.raw[u][q][i] = c + i < k1 ? v : 0.0f;
+                    }
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int id = t + u * C::threads;
+            uint32_t h[4][3];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) pieces(n.raw[u][q >> 1][(q & 1) * 2], n.raw[u][q >> 1][(q & 1) * 2 + 1], hot, h[q]);
+#pragma unroll
+            for (int o = 0; o < 3; ++o) *reinterpret_cast<u4 *>(to + o * planeP + place<32>(id / 4, id % 4)) = u4{h[0][o], h[1][o], h[2][o], h[3][o]};
+        }
+    };
+    Sums<C> sum;
+    // from: the stage that is multiplied, to: where the next one goes, planes of j0 and numbers of k from k to k1; n: those, then the ones two stages behind them, from `ahead` on
+    const auto step = [&](char *from, char *to, Numbers &n, int64_t j0, int k, int k1, int ahead) {
+        const int t = again_of(tid), at = t & 15, chunk = t >> 4 & 3;
+        u4 x[FI][3], y[FJ][3];
+#pragma unroll
+        for (int o = 0; o < 3; ++o)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) y[j][o] = *reinterpret_cast<const u4 *>(from + 3 * planeP + o * planeQ + place<32>((wj * FJ + j) * 16 + at, chunk));
+        const auto read = [&](int i) {
+#pragma unroll
+            for (int o = 0; o < 3; ++o) x[i][o] = *reinterpret_cast<const u4 *>(from + o * planeP + place<32>((wi * FI + i) * 16 + at, chunk));
+        };
+#pragma unroll
+        for (int i = 0; i < FI / 2; ++i) read(i);
+        __builtin_amdgcn_sched_barrier(0); // (reads and writes of LDS behind loads to it wait for them)
+        load_planes(to, j0, k);
+        const auto multiply = [&](int i) {
+            f4 part[FJ];
+            products32<FJ>(x[i], y, part);
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[i][j] += part[j];
+        };
+#pragma unroll
+        for (int i = 0; i < FI / 2; ++i) multiply(i);
+        __builtin_amdgcn_sched_barrier(0);
+        put(to, n, k, k1);
+#pragma unroll
+        for (int i = FI / 2; i < FI; ++i) read(i);
+        __builtin_amdgcn_sched_barrier(0); // the planes of the next stage are older than what is fetched here, which need not be there
+        fetch(n, ahead);
+#pragma unroll
+        for (int i = FI / 2; i < FI; ++i) multiply(i);
+        wait_for_all<U * 2>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Spot here = spot_of<C>(a, blockIdx.x);
+    rows_of(here.i0);
+    fetch(even, here.k0);
+    load_planes(lds, here.j0, here.k0);
+    fetch(odd, here.k0 + 32);
+    put(lds, even, here.k0, here.k1);
+    fetch(even, here.k0 + 64);
+    wait_for_all<0>();
+    const bool large = met[0];
+    for (int tile = blockIdx.x;; tile += beside) {
+        const bool last = tile + beside >= all;
+        const Spot next = last ? here : spot_of<C>(a, tile + beside); // (behind the last the last again)
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = here.k0; k < here.end; k += 64) {
+            const int left = here.end - k; // of k; what is behind is the next tile's
+            step(lds, lds + stage, odd, here.j0, k + 32, here.k1, left > 64 ? k + 96 : next.k0 + 32);
+            if (left == 128) rows_of(next.i0);
+            step(lds + stage, lds, even, left > 64 ? here.j0 : next.j0, left > 64 ? k + 64 : next.k0, left > 64 ? here.k1 : next.k1,
+                 left > 128 ? k + 128 : next.k0 + 128 - left);
+        }
+        if (hot >= kHot) met[1] = 1;
+        wait_for_all<63>();
+        const bool again = met[1];
+        finish_tile<T, false, TQ, C, 2>(a, sum, lds + stage, here.i0, here.j0, here.k0, here.k1, here.stretch, again || large, again_of(tid));
+        if (last) break;
+        here = next;
+        wait_for_all<63>();
+        if (again) { // of the numbers met so far those of the next tile, in LDS, count on: a thread's own
+            if (tid == 0) met[1] = 0;
+            hot = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int id = tid + u * C::threads;
+                const b8 v = *reinterpret_cast<const b8 *>(lds + place<32>(id / 4, id % 4));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) hot = __builtin_fmaxf(hot, __builtin_fabsf((float)v[i]));
+            }
+            wait_for_all<63>();
+        }
+    }
+}
+// Gradients of weights: both operands are split on their way.
+template <typename C> __global__ void __launch_bounds__(C::threads, C::per) pieces_kernel(TileArgs a)
+{
+    typedef float T;
+    constexpr int KS = 32, FI = C::FI, FJ = C::FJ, planeP = C::BI * 64, planeQ = C::BJ * 64, stage = 3 * (planeP + planeQ);
     extern __shared__ __align__(16) char lds[];
     __shared__ int met;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / C::WJ, wj = wave % C::WJ;
@@ -730,32 +911,18 @@ template <bool TP, bool TQ, bool PLANES, typename C> __global__ void __launch_bo
     const int steps = (int)((k1 - k0 + KS - 1) / KS);
     if (tid == 0) met = 0;
     float hot = 0.0f;
-    typedef Loader<T, TP, C::BI, C::threads> P;
-    typedef Loader<T, TQ, C::BJ, C::threads> Q;
-    constexpr int ahead = PLANES ? 2 : 1; // stages on their way to registers (which do not hold two of both operands)
-    P lp[ahead];
-    Q lq[ahead];
-    const auto fetch = [&](int s, P &p, Q &q) {
+    Loader<T, true, C::BI, C::threads> p;
+    Loader<T, true, C::BJ, C::threads> q;
+    const auto fetch = [&](int s) {
         if (s >= steps) return;
         p.fetch(a.p, i0, k0 + s * KS, k1, tid);
-        if (!PLANES) q.fetch(a.q, j0, k0 + s * KS, k1, tid);
+        q.fetch(a.q, j0, k0 + s * KS, k1, tid);
     };
-    const auto put = [&](int s, const P &p, const Q &q) {
+    const auto put = [&](int s) {
         if (s >= steps) return;
         char *to = lds + (s & 1) * stage;
         p.put(to, hot, tid);
-        if (!PLANES) q.put(to + 3 * planeP, hot, tid);
-    };
-    const auto load_planes = [&](int s) {
-        if (!PLANES || s >= steps) return;
-        typedef __attribute__((address_space(3))) void *Lds;
-        typedef __attribute__((address_space(1))) const void *Global;
-#pragma unroll
-        for (int u = 0; u < loads; ++u) {
-            const int b = u * waves + wave, o = b / (C::BJ / 16), rows = b % (C::BJ / 16) * 16;
-            const bfloat_t *from = w.at + o * w.plane + ((k0 / KS + s) * w.rows + j0 + rows + (lane >> 2)) * 32 + ((lane & 3) ^ (lane >> 4)) * 8;
-            __builtin_amdgcn_global_load_lds((Global)from, (Lds)(lds + (s & 1) * stage + 3 * planeP + o * planeQ + rows * 64), 16, 0, 0);
-        }
+        q.put(to + 3 * planeP, hot, tid);
     };
     Sums<C> sum;
 #pragma unroll
@@ -763,9 +930,12 @@ template <bool TP, bool TQ, bool PLANES, typename C> __global__ void __launch_bo
 #pragma unroll
         for (int j = 0; j < FJ; ++j) sum[i][j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     const int at = lane & 15, chunk = lane >> 4;
-    const auto step = [&](int s, P &p, Q &q) { // p, q: the numbers of stage s + 1, then of the one behind those on their way
+    fetch(0);
+    put(0);
+    fetch(1);
+    wait_for_all<63>();
+    for (int s = 0; s < steps; ++s) {
         const char *fromP = lds + (s & 1) * stage, *fromQ = fromP + 3 * planeP;
-        load_planes(s + 1);
         u4 x[FI][3], y[FJ][3];
         const auto read = [&](int i) {
 #pragma unroll
@@ -776,7 +946,7 @@ template <bool TP, bool TQ, bool PLANES, typename C> __global__ void __launch_bo
 #pragma unroll
             for (int j = 0; j < FJ; ++j) y[j][o] = *reinterpret_cast<const u4 *>(fromQ + o * planeQ + place<32>((wj * FJ + j) * 16 + at, chunk));
 #pragma unroll
-        for (int i = 0; i < (PLANES ? FI : FI / 2); ++i) read(i);
+        for (int i = 0; i < FI / 2; ++i) read(i);
         const auto multiply = [&](int i) {
             f4 part[FJ];
             products32<FJ>(x[i], y, part);
@@ -785,34 +955,19 @@ template <bool TP, bool TQ, bool PLANES, typename C> __global__ void __launch_bo
         };
 #pragma unroll
         for (int i = 0; i < FI / 2; ++i) multiply(i);
-        put(s + 1, p, q);
-        __builtin_amdgcn_sched_barrier(0); // the planes of stage s + 1 are older than what is fetched here, which need not be there
-        fetch(s + 1 + ahead, p, q);
+        put(s + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(s + 2);
 #pragma unroll
         for (int i = FI / 2; i < FI; ++i) {
-            if (!PLANES) read(i);
+            read(i);
             multiply(i);
         }
-        const bool whole = s + 1 + ahead < steps && k0 + (s + 2 + ahead) * KS <= k1 && P::whole && (!TP || i0 + C::BI <= a.p.n);
-        if (!PLANES) wait_for_all<63>();
-        else if (whole) wait_for_all<P::U * P::parts>();
-        else wait_for_all<0>();
-    };
-    if (steps > 0) {
-        fetch(0, lp[0], lq[0]);
-        load_planes(0);
-        if (ahead == 2) fetch(1, lp[ahead - 1], lq[ahead - 1]);
-        put(0, lp[0], lq[0]);
-        fetch(ahead, lp[0], lq[0]);
-        wait_for_all<0>();
-        for (int s = 0; s < steps; s += 2) {
-            step(s, lp[ahead - 1], lq[ahead - 1]);
-            if (s + 1 < steps) step(s + 1, lp[0], lq[0]);
-        }
+        wait_for_all<63>();
     }
-    if (hot >= kHot || (PLANES && tid < kSplitBlocks && w.hot[tid])) met = 1;
+    if (hot >= kHot) met = 1;
     __syncthreads();
-    finish_tile<T, TP, TQ, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, met);
+    finish_tile<T, true, true, C, 2>(a, sum, lds, i0, j0, k0, k1, stretch, met, tid);
 }
 
 // ---------------------------------------------------------------------------------- many rows and few weights
@@ -1372,6 +1527,12 @@ template <typename T> bool straight(const Side &s, bool turned, bool padded)
 {
     return sizeof(T) == 2 && s.ld % 8 == 0 && (uintptr_t)s.at % 16 == 0 && s.ld < (1 << 22) && (!turned || s.n % 8 == 0 || padded);
 }
+// Whether a product with weights w can go straight to LDS, or, of fp32 numbers, to planes_kernel.
+template <typename T> bool straight_with(const Side &x, const Side &w, bool turned, int64_t K)
+{
+    if (sizeof(T) == 4) return x.ld < (1 << 21); // places of a tile that 32 bits reach
+    return K % 8 == 0 && straight<T>(x, false, false) && straight<T>(w, turned, false);
+}
 
 // How a product of I x J numbers over K is cut: into tiles, and k into stretches, whose sums go through memory, where tiles are too few for the chip.  By what each
 // way would take, in us: a workgroup `fixed` and, for a stage, `stage` alone on a compute unit and `beside` more for each of up to `most` that run there side by
@@ -1402,14 +1563,13 @@ constexpr Costs kAny32 = {3.9f, 6.9e6f, {{2.3f, 2.10f, 0.99f, 2}, {0.8f, 1.47f, 
 // weights: q is W, whose planes PIECES_* write first; only: one tiling, or -1
 template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, bool weights, int only = -1)
 {
-    constexpr int64_t kUnits = 256;
     const Costs &costs = sizeof(T) == 4 ? kAny32 : direct ? kStraight16 : kAny16;
     const int64_t stages = up(K, Num<T>::KS), most = stages / 2 < 1 ? 1 : stages / 2;
     Plan best = {};
     best.us = -1.0f;
     for (int which = 0; which < TILINGS; ++which) {
         const Cost &c = costs.of[which];
-        if (c.most == 0 || (only >= 0 && which != only) || (which >= PIECES_FLAT && K < 64)) continue;
+        if (c.most == 0 || (only >= 0 && which != only) || (which >= PIECES_FLAT && K < 64) || (weights && (which == PIECES_TALL || (which == PIECES_FLAT && !direct)))) continue;
         const int64_t ti = up(I, kTileI[which]), tj = up(J, kTileJ[which]), tiles = ti * tj;
         const int64_t fill = tiles < kUnits ? kUnits / (tiles ? tiles : 1) : 1;
         int64_t before = 0;
@@ -1433,8 +1593,8 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, bo
 }
 int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
 // planes of weights, and whether numbers in them are too large
-int64_t plane_rows(const Plan &p) { return p.tiles_j * (p.which == PIECES_FLAT ? PiecesFlat::BJ : PiecesTall::BJ); }
-int64_t plane_bytes(const Plan &p, int64_t K) { return p.which >= PIECES_FLAT ? 3 * 2 * plane_rows(p) * up(K, 32) * 32 + 4 * kSplitBlocks : 0; }
+int64_t plane_rows(const Plan &p) { return p.tiles_j * PiecesFlat::BJ; }
+int64_t plane_bytes(const Plan &p, int64_t K) { return p.which >= PIECES_FLAT ? 3 * 2 * plane_rows(p) * (up(K, 64) + 1) * 64 + 4 * kSplitBlocks : 0; }
 // workspace of a product; weights: of rows with weights
 int64_t product_bytes(const Plan &p, int64_t I, int64_t J, int64_t K, bool weights) { return part_bytes(p, I, J) + (weights ? plane_bytes(p, K) : 0); }
 
@@ -1457,7 +1617,7 @@ template <typename T> constexpr bool ends_fit(int steps) { return sizeof(T) == 2
 // direct: tiles whose pieces go straight to LDS are as fast for more than 128 numbers of k (480,000 x 256 -> 64 in bf16: 63 us for 72).
 template <typename T> bool many_rows(int64_t I, int64_t J, int64_t K, bool direct)
 {
-    return (K <= 128 || (K <= 256 && !direct)) && I >= 32768 && rows_lds<T>(J, K) <= 140 * 1024 && (K <= 128 || (K == 256 && J % 8 == 0) || J <= 32 || ends_fit<T>(8));
+    return (K <= 128 || (K <= 256 && !(direct && sizeof(T) == 2))) && I >= 32768 && rows_lds<T>(J, K) <= 140 * 1024 && (K <= 128 || (K == 256 && J % 8 == 0) || J <= 32 || ends_fit<T>(8));
 }
 
 template <typename T, bool TQ, int STEPS> int launch_rows(const TileArgs &a, hipStream_t stream)
@@ -1522,20 +1682,23 @@ template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q
     if constexpr (sizeof(T) == 4) {
         if (c.which >= PIECES_FLAT) {
             done = true;
-            char *at = static_cast<char *>(ws) + part_bytes(c, tail.rows, tail.cols);
-            const int64_t rows = plane_rows(c), chunks = up(K, 32) * 4;
-            Planes w = {reinterpret_cast<bfloat_t *>(at + 4 * kSplitBlocks), rows, rows * chunks * 8, reinterpret_cast<int *>(at)};
-            if (!TP) {
-                const SplitArgs s = {static_cast<const float *>(q.at), q.ld, q.n, K, rows, chunks, const_cast<bfloat_t *>(w.at), reinterpret_cast<int *>(at)};
-                hipLaunchKernelGGL(split_kernel<TQ>, dim3(kSplitBlocks), dim3(kT), 0, stream, s);
-            }
-            const auto go = [&](auto *kernel, int bytes, int threads) {
+            const auto go = [&](auto *kernel, unsigned blocks, int bytes, int threads, auto... more) {
                 if (!allow_lds(kernel, (size_t)bytes)) return (int)PCSR_E_HIP;
-                hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), (size_t)bytes, stream, a, w);
+                hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), (size_t)bytes, stream, a, more...);
                 return (int)PCSR_OK;
             };
-            rc = c.which == PIECES_FLAT ? go(&pieces_kernel<TP, TQ, !TP, PiecesFlat>, pieces_bytes<PiecesFlat>(), PiecesFlat::threads)
-                                        : go(&pieces_kernel<TP, TQ, !TP, PiecesTall>, pieces_bytes<PiecesTall>(), PiecesTall::threads);
+            if constexpr (TP) {
+                rc = c.which == PIECES_FLAT ? go(&pieces_kernel<PiecesFlat>, grid, pieces_bytes<PiecesFlat>(), PiecesFlat::threads)
+                                            : go(&pieces_kernel<PiecesTall>, grid, pieces_bytes<PiecesTall>(), PiecesTall::threads);
+            } else {
+                char *at = static_cast<char *>(ws) + part_bytes(c, tail.rows, tail.cols);
+                const int64_t rows = plane_rows(c), chunks = (up(K, 64) + 1) * 8;
+                const Planes w = {reinterpret_cast<bfloat_t *>(at + 4 * kSplitBlocks), rows, rows * chunks * 8, reinterpret_cast<int *>(at)};
+                const SplitArgs s = {static_cast<const float *>(q.at), q.ld, q.n, K, rows, chunks, const_cast<bfloat_t *>(w.at), reinterpret_cast<int *>(at)};
+                hipLaunchKernelGGL(split_kernel<TQ>, dim3(kSplitBlocks), dim3(kT), 0, stream, s);
+                const unsigned blocks = grid < kUnits ? grid : kUnits;
+                rc = go(&planes_kernel<TQ, PiecesFlat>, blocks, pieces_bytes<PiecesFlat>(), PiecesFlat::threads, w);
+            }
         }
     }
     if (rc != PCSR_OK) return rc;
@@ -1569,7 +1732,7 @@ struct Space {
         Space s;
         const auto most_of = [](int64_t I, int64_t J, int64_t K, bool weights) { // however the operands lie
             int64_t most = product_bytes(plan<T>(I, J, K, false, weights, SMALL), I, J, K, weights);
-            for (int direct = 0; direct < (sizeof(T) == 2 ? 2 : 1); ++direct) {
+            for (int direct = 0; direct < 2; ++direct) {
                 const int64_t need = product_bytes(plan<T>(I, J, K, direct, weights), I, J, K, weights);
                 most = need > most ? need : most;
             }
@@ -1596,7 +1759,7 @@ struct Space {
 };
 template <typename T> bool forward_direct(const pcsr_linear_t &a)
 {
-    return a.in % 8 == 0 && straight<T>({a.x, a.x_stride, a.rows}, false, false) && straight<T>({a.w, a.w_stride, a.out}, false, false);
+    return straight_with<T>({a.x, a.x_stride, a.rows}, {a.w, a.w_stride, a.out}, false, a.in);
 }
 template <typename T> Plan forward_plan(const pcsr_linear_t &a) { return plan<T>(a.rows, a.out, a.in, forward_direct<T>(a), true); }
 bool has_slope(const pcsr_linear_t &a) { return a.act != PCSR_ACT_NONE || drop_of(&a.drop).threshold; }
@@ -1672,7 +1835,7 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
     const Tail tail_x = {nullptr, nullptr, dx, nullptr, 0, a.rows, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
     const Tail tail_w = {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
     const Side w = {a.w, a.w_stride, a.in}, g = {dz.at, dz.ld, a.out}, x = {a.x, a.x_stride, a.in};
-    const bool direct_x = a.out % 8 == 0 && straight<T>(dz, false, false) && straight<T>(w, true, false), direct_w = straight<T>(g, true, own) && straight<T>(x, true, false);
+    const bool direct_x = straight_with<T>(dz, w, true, a.out), direct_w = straight<T>(g, true, own) && straight<T>(x, true, false);
     int rc = launched();
     if (rc != PCSR_OK) return rc;
     Plan px = plan<T>(a.rows, a.in, a.out, direct_x, true), pw = plan<T>(a.out, a.in, a.rows, direct_w, false);
