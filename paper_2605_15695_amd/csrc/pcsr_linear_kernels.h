@@ -1285,28 +1285,40 @@ template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(Sl
     DropKey key = {};
     if (a.drop.threshold) key = key_of(a.drop);
     float sum[8] = {};
-    if (m > 0)
-#pragma unroll 2
-        for (int64_t row = (int64_t)blockIdx.x * per + r; row < a.rows; row += (int64_t)gridDim.x * per) { // workgroups side by side
-            float d[8];
-            load_upto<T, 8>(static_cast<const T *>(a.dy) + row * a.dy_stride + c, m, d);
+    if (m > 0) {
+        const int64_t step = (int64_t)gridDim.x * per; // workgroups side by side
+        float next[8];
+        typename Pack<S, 8>::type q, q_next;
+        const auto fetch = [&](int64_t row) { // behind the last row the last again
+            row = row < a.rows ? row : a.rows - 1;
+            load_upto<T, 8>(static_cast<const T *>(a.dy) + row * a.dy_stride + c, m, next);
             if (a.slope) {
                 const S *at = static_cast<const S *>(a.slope) + row * a.cols + c;
-                typename Pack<S, 8>::type q;
                 if (m >= 8) {
-                    q = *reinterpret_cast<const typename Pack<S, 8>::type *>(at);
+                    q_next = *reinterpret_cast<const typename Pack<S, 8>::type *>(at);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) q[i] = i < m ? at[i] : (S)0;
+                    for (int i = 0; i < 8; ++i) q_next[i] = i < m ? at[i] : (S)0;
                 }
+            }
+        };
+        int64_t row = (int64_t)blockIdx.x * per + r;
+        fetch(row);
+        for (; row < a.rows; row += step) {
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = next[i];
+            q = q_next;
+            fetch(row + step);
+            if (a.slope)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] *= Slope<T>::take(q[i]);
-            }
             if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += d[i]; // (behind the end 0 times something)
             if (a.dz) store_upto<T, 8>(static_cast<T *>(a.dz) + row * a.ld + c, m, d);
         }
+    }
     if (!a.sums) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[threadIdx.x][i] = sum[i];
