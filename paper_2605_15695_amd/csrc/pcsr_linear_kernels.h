@@ -1384,10 +1384,10 @@ struct NarrowArgs {
 };
 constexpr int kNarrowT = 1024, kNarrowBlocks = 256;
 constexpr int narrow_rows(int lanes) { return lanes == 32 ? 64 : 128; } // (of 32 lanes to a row registers hold two rows' numbers beside the rest)
-constexpr int64_t narrow_lds(int lanes, int64_t out, int64_t in) // dz, weights, x
+constexpr int64_t narrow_lds(int lanes, int64_t out, int64_t in) // dz and x, of two tiles, weights
 {
     const int64_t pitch = up(out, 32) * 64 + 16, rows = narrow_rows(lanes);
-    return rows * pitch + up(in, 16) * 16 * pitch + rows * (up(in, 16) * 32 + 16);
+    return 2 * rows * (pitch + up(in, 16) * 32 + 16) + up(in, 16) * 16 * pitch;
 }
 
 // L: lanes to a row of dy
@@ -1400,7 +1400,8 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
     extern __shared__ __align__(16) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), at = lane & 15, chunk = lane >> 4;
     const int in = a.in, out = a.out, steps = (int)up(out, 32), tiles_k = (int)up(in, 16), pitch = steps * 64 + 16, pitch_x = tiles_k * 32 + 16;
-    char *const ldsW = lds + ROWS * pitch, *const ldsX = ldsW + tiles_k * 16 * pitch;
+    const int buffer = ROWS * (pitch + pitch_x);
+    char *const ldsW = lds + 2 * buffer;
     const int64_t all = (a.rows + ROWS - 1) / ROWS;
     const int c = tid % L * 8, r0 = tid / L, xc = tid % 8 * 8, xr = tid / 8;
     const bool mine = c < out, mine_x = a.x && xc < in && xr < ROWS;
@@ -1442,7 +1443,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
         const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(q + 4 * p)));
         return u4{lo[0], lo[1], hi[0], hi[1]};
     };
-    for (; tile < all; tile += gridDim.x) {
+    const auto fill = [&](int64_t tile, char *ldsZ, char *ldsX) { // with what is there of this tile; the one behind it is asked for
         const int64_t next = tile + gridDim.x;
         const auto pass = [&](auto u) {
             const int r = r0 + u * per;
@@ -1463,7 +1464,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
                 sum[i] += d[i];
                 g[i] = (T)d[i];
             }
-            *reinterpret_cast<Raw *>(lds + r * pitch + c * 2) = g;
+            *reinterpret_cast<Raw *>(ldsZ + r * pitch + c * 2) = g;
             __builtin_amdgcn_sched_barrier(0); // one after the other: side by side registers do not hold them
         };
         if (mine) {
@@ -1479,7 +1480,8 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
             *reinterpret_cast<Raw *>(ldsX + xr * pitch_x + xc * 2) = g;
         }
         fetch_x(next);
-        __syncthreads();
+    };
+    const auto multiply = [&](int64_t tile, const char *ldsZ, const char *ldsX) {
         if (a.dx) { // 16 rows and J tiles of 16 columns to a wavefront
             const int rt = wave * J / 4, ct = wave * J % 4;
             f4 s[J];
@@ -1487,7 +1489,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
             for (int j = 0; j < J; ++j) s[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
             if (ct < tiles_k)
                 for (int t = 0; t < steps; ++t) {
-                    const u4 p = *reinterpret_cast<const u4 *>(lds + (rt * 16 + at) * pitch + t * 64 + chunk * 16);
+                    const u4 p = *reinterpret_cast<const u4 *>(ldsZ + (rt * 16 + at) * pitch + t * 64 + chunk * 16);
 #pragma unroll
                     for (int j = 0; j < J; ++j)
                         if (ct + j < tiles_k) s[j] = mfma(T(), p, *reinterpret_cast<const u4 *>(ldsW + ((ct + j) * 16 + at) * pitch + t * 64 + chunk * 16), s[j]);
@@ -1505,13 +1507,26 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
         if (a.part && wave * 16 < out) // dw: 16 of its rows to a wavefront
 #pragma unroll
             for (int t = 0; t < ROWS / 32; ++t) {
-                const u4 p = turned(lds + t * 32 * pitch + wave * 32, pitch);
+                const u4 p = turned(ldsZ + t * 32 * pitch + wave * 32, pitch);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (j < tiles_k) dw[j] = mfma(T(), p, turned(ldsX + t * 32 * pitch_x + j * 32, pitch_x), dw[j]);
             }
-        __syncthreads();
+    };
+    // Half of the wavefronts of a SIMD multiply a tile before they fill the other buffer with the next one, half afterwards, so that the one's reads from LDS
+    // and the other's arithmetic share the time.
+    fill(tile, lds, lds + ROWS * pitch);
+    for (int cur = 0;; cur ^= buffer) {
+        char *const z = lds + cur, *const z_next = lds + (cur ^ buffer);
+        const bool more = tile + gridDim.x < all, first = wave >> 2 & 1;
+        __syncthreads(); // the tile is whole, and all have multiplied the one before
+        if (first) multiply(tile, z, z + ROWS * pitch);
+        if (more) fill(tile + gridDim.x, z_next, z_next + ROWS * pitch);
+        if (!first) multiply(tile, z, z + ROWS * pitch);
+        if (!more) break;
+        tile += gridDim.x;
     }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
