@@ -1,4 +1,4 @@
-// Activations and their slopes in 32 bits: what kernels that end in one share (pcsr_norm.hip, pcsr_linear.hip).
+// Activations and their slopes in 32 bits: what kernels that end in one share (pcsr_norm.hip, pcsr_linear_kernels.h).
 #pragma once
 #include <hip/hip_runtime.h>
 

@@ -1,4 +1,4 @@
-// What is dropped, as a function of a seed, an offset and a number's place: nothing is stored (pcsr_drop.hip, pcsr_linear.hip).
+// What is dropped, as a function of a seed, an offset and a number's place: nothing is stored (pcsr_drop.hip, pcsr_linear_kernels.h).
 //
 // Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel Random Numbers: As Easy as 1, 2, 3", SC 2011) with the seed as key and the
 // counter (column / 8, row, offset) gives 128 bits: 16 for each of 8 columns side by side, word by word, low half first.  A number is

@@ -419,7 +419,9 @@ template <typename T, typename C> constexpr int lds_bytes()
     return stage > out ? stage : out;
 }
 
-// Any operands.  They go through registers to LDS.
+// Any operands.  They go through registers to LDS, one stage ahead; two to five workgroups on a compute unit fill one another's waits.  Bound by what an operand takes
+// on its way (loads of single numbers at ends, turned writes, splits).  777 x 75 -> 333 in fp32 9.3 us in 78 tiles of 64 x 64 (with dropout, slopes, a residual);
+// 4096 x 1001 -> 1001 in bf16 23 us, 0.35 PFLOP/s.
 template <typename T, bool TP, bool TQ, typename C> __device__ __forceinline__ void tile_of(const TileArgs &a, int block, char *lds, int &met)
 {
     typedef typename Num<T>::E E;
@@ -492,7 +494,8 @@ template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bou
     __shared__ int met;
     tile_of<T, TP, TQ, C>(a, blockIdx.x, lds, met);
 }
-// Both products of a backward pass side by side: where each leaves most of the chip idle.  777 x 75 -> 333 in fp32: 15 us for 13 and 15.
+// Both products of a backward pass side by side: where each leaves most of the chip idle.  777 x 75 -> 333 in fp32: 15 us for 13 and
+// 15 (12 now that two numbers are split at once).
 template <typename T> __global__ void __launch_bounds__(Small::threads) pair_kernel(TileArgs x, TileArgs w, int first)
 {
     __shared__ __align__(16) char lds[lds_bytes<T, Small>()];
@@ -589,6 +592,9 @@ template <bool TP, bool TQ, typename C> constexpr int straight_bytes()
     constexpr int out = out_bytes<C, C::FI < 4 ? C::FI : 4>();
     return stages > out ? stages : out;
 }
+// Bound by the matrix units, which alone reach 2.4 PFLOP/s on zeros and 1.8 on random numbers here.  4096^3 in bf16: 115 us (1.2 PFLOP/s) where operands stay in caches, 126 to 135 where not,
+// matrix units 51 to 54 % busy, 256 x 256 tiles (one to a compute unit: 512 numbers of operands from LDS for 65,536 products; 128 x 128 take 131 us).  32,768 x 768 -> 1000 in
+// fp16 88 us, of which some 20 are what ends the tiles (gelu, dropout, slopes) with nothing beside it; its gradient of x 75 us in tiles of 128 x 128.
 // The next numbers are read from LDS while those before are multiplied, and a stage's loads are given out when all wavefronts have read the one
 // before it, which is half a stage before they multiply its last numbers.
 template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) straight_kernel(TileArgs a)
@@ -688,7 +694,7 @@ struct SplitArgs {
     bfloat_t *to;
     int *hot;
 };
-// 4096 x 4096: 30 us.
+// Weights of 256 x 256: 5 to 7 us; 4096 x 4096: 30 us, of memory.
 template <bool TURN> __global__ void __launch_bounds__(kT) split_kernel(SplitArgs a)
 {
     float hot = 0.0f;
@@ -741,6 +747,10 @@ __device__ __forceinline__ int again_of(int tid)
 // Products with weights.  A compute unit's workgroup takes its tiles one behind the other, and the first numbers of a tile are on their way, and in LDS, while
 // what follows the one before it is done.  No load stands behind a condition, or waits behind it would be for all of them: places behind a row's end are read in front
 // of it, and what lies there is put right on its way to LDS.
+// 250,000 x 256 -> 256: 317 us (silu, dropout, a residual, slopes; 1.04 GB), gradient of x 222 (0.54 GB); a tile to a workgroup took 331 and 251.  Six products of 33 GFLOP would be 110 us
+// at the rate of random numbers above; matrix units are 29 and 43 % busy, the rest is the ends of tiles and, in a stage, reads from LDS and the wait for numbers that were asked for one and a half
+// stages before (loads return in order, so that the wait for a stage's planes is one for them too).  Halves of the wavefronts a stage apart, one moving while the other
+// multiplies, took 1.04 of this for gradients.
 template <bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) planes_kernel(TileArgs a, Planes w)
 {
     typedef float T;
@@ -896,7 +906,8 @@ template <bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::
         }
     }
 }
-// Gradients of weights: both operands are split on their way.
+// Gradients of weights: both operands are split on their way, and few tiles mean many stretches of k.  250,000 x 256 -> 256: 229 us in 254 workgroups (0.55 GB), matrix units 41 %
+// busy; bound as planes_kernel is.
 template <typename C> __global__ void __launch_bounds__(C::threads, C::per) pieces_kernel(TileArgs a)
 {
     typedef float T;
@@ -974,6 +985,8 @@ template <typename C> __global__ void __launch_bounds__(C::threads, C::per) piec
 // The weights lie in LDS for as long as the workgroup lives, in pieces, and wavefronts take 16 rows at a time, each for itself: a lane's numbers of the next rows
 // are on their way to its registers while these are multiplied, nothing waits for other wavefronts, and x is read once.
 // STEPS: of 32 numbers of k.  FJ tiles of 16 columns at a time.  WHOLE: all of k is there, and of columns 8 or none.  RES: a residual is there.
+// 2,000,000 x 256 -> 64 in fp32 with a residual 614 to 658 us: 3.07 GB, 4.7 to 5.0 TB/s; matrix units are 32 % busy, vector units 37 beside them.  480,000 x 64 -> 256 in bf16 with gelu,
+// dropout and slopes 141 to 152 us: vector units are 91 % busy with what follows the product (memory would take 89).
 // Loads come back in their order, and so do the waits: what a strip's end needs is asked for before the next strip's numbers, and the bias lies in LDS.
 template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64 + 16; } // bytes of a row: 16 rows lie in different banks
 template <typename T, int STEPS> int64_t weights_bytes(int64_t cols) { return Num<T>::NP * up(cols, 64) * 64 * weights_pitch<T, STEPS>(); }
@@ -1154,6 +1167,7 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
 // ---------------------------------------------------------------------------------- few rows
 // One to eight rows: bound by reading the weights.  `lanes` lanes take a row of them, 16 bytes each at a time, add up its products with all R rows of x in fp32,
 // and put their sums together; of the lanes that then have them, lane r ends row r.
+// One row, 4096 x 4096 in bf16: 9.7 us (33.6 MB; 64 x 64 take 2.8, so 4.9 TB/s of the rest).
 template <typename T, int R> __global__ void __launch_bounds__(kT) few_kernel(TileArgs a, int lanes)
 {
     constexpr int N = kPer16<T>, A = R == 1 ? 8 : R == 2 ? 4 : 2; // loads on their way
@@ -1216,7 +1230,7 @@ template <typename T, int R> __global__ void __launch_bounds__(kT) few_kernel(Ti
 }
 
 // Sums of the stretches of k and what follows.  A workgroup takes `across` places of 8 columns; of its threads kT / across share a place and take
-// every so-manieth stretch each, and their sums are added up in order.
+// every so-manieth stretch each, and their sums are added up in order.  127 stretches of 256 x 256: 9.6 us; three of 1000 x 768: 7.5.
 struct FinishArgs {
     const float *part;
     int stretches, across;
@@ -1274,7 +1288,8 @@ struct SlopeArgs {
 };
 constexpr int kSlopeT = 1024, kSlopeBlocks = 512; // two workgroups a compute unit: as many sums as sums_kernel adds up in 6 us
 
-// dz = f act'(z) dy, and sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows.
+// dz = f act'(z) dy, and sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows, the next row's numbers on their way.
+// Bound by memory: 250,000 x 256 in fp32 144 us (768 MB, 5.3 TB/s; 152 without the row ahead), 32,768 x 1000 in fp16 42, 4096 x 4096 in bf16 25 (100 MB).
 template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(SlopeArgs a)
 {
     typedef typename Slope<T>::type S;
@@ -1373,7 +1388,8 @@ template <typename T> __global__ void __launch_bounds__(kT) last_kernel(FinishAr
 // dz, dx, dw and db of 16-bit numbers from one read of dy, the slopes and x, where dw fits a workgroup's registers: up to 256 columns of dy and 64 of x.
 // A workgroup takes 64 or 128 rows at a time: dz and x go to LDS as they are, [row][column], the weights lie there turned, and dx = dz w reads dz by rows,
 // dw += dz^T x both by columns (turned by the LDS reads).  A thread keeps its 8 columns of dy, so that db is a sum of its own; when it has used a row's numbers
-// it asks for those that come next.  Bound by memory and, where something is dropped, by the generator: 480,000 x 64 -> 256 in bf16, gelu, p = 0.1.
+// it asks for those that come next.  480,000 x 64 -> 256 in bf16, dropout: 164 us (630 MB: memory would take 102), vector units 56 % busy with the
+// generator and the slopes, LDS 31 %; all wavefronts at the same of both took 174, with one buffer too; slope_kernel and both products 285.
 struct NarrowArgs {
     const void *dy, *slope, *x, *w; // slope: null for none
     int64_t dy_stride, x_stride, w_stride, rows;

@@ -1,5 +1,5 @@
 // Numbers of 32 and 16 bits in memory, 32 bits in registers: what the kernels of the training step share
-// (pcsr_embed.hip, pcsr_norm.hip, pcsr_ortho.hip).
+// (pcsr_embed.hip, pcsr_norm.hip, pcsr_ortho.hip, pcsr_drop.hip, pcsr_linear_kernels.h).
 #pragma once
 #include <hip/hip_runtime.h>
 
