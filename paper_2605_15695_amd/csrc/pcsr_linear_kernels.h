@@ -142,12 +142,15 @@ template <typename T> __device__ __forceinline__ void put_one(const Tail &a, con
 }
 
 // ---------------------------------------------------------------------------------- operands on their way to LDS
-// A row's 16-byte chunks of k are exchanged by bits of its number, so that rows read side by side lie in different banks, and so do chunks of one k
-// written for many rows.
-template <int KS> __device__ __forceinline__ int place(int row, int chunk)
+// Where a row's 16-byte chunk of k lies, so that what an instruction reads or writes lies in different banks.  128 bytes a row: chunks are exchanged by bits of the row's number.
+// 64 bytes, four rows to all banks: likewise, by a permutation of four that suits both 16 lanes side by side and the 16 that a read of 64 x 16 bytes takes at once (four of each
+// four rows, two chunks).  TURNED: 4 k of every fourth row are written at once, so 4 x 4 rows are exchanged as well (with the other's places 65 % of LDS cycles were lost to conflicts).
+__device__ __forceinline__ int turn_of(int q) { return (q << 1 & 2) ^ (q & 2) ^ q >> 1; } // 0, 2, 3, 1
+template <int KS, bool TURNED = false> __device__ __forceinline__ int place(int row, int chunk)
 {
-    const int turn = KS == 64 ? (row ^ row >> 3) & 7 : row >> 2 & 3;
-    return (row * (KS / 8) + (chunk ^ turn)) * 16;
+    if (KS == 64) return (row * 8 + (chunk ^ ((row ^ row >> 3) & 7))) * 16;
+    if (TURNED) return (((row & ~15) | (row & 3) << 2 | (row >> 2 & 3)) * 4 + (chunk ^ ((row ^ row >> 4) & 3))) * 16;
+    return (row * 4 + (chunk ^ turn_of(row >> 2 & 3))) * 16;
 }
 
 // two numbers side by side in k, in pieces
@@ -220,7 +223,7 @@ template <typename T, bool TURN, int R, int THREADS> struct Loader {
                 const int row = id % across * N, kg = id / across;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    char *to = lds + place<KS>(row + i, kg >> 1) + (kg & 1) * 8;
+                    char *to = lds + place<KS, true>(row + i, kg >> 1) + (kg & 1) * 8;
                     if constexpr (NP == 3) {
                         uint32_t a[3], b[3];
                         pieces(raw[u][0][i], raw[u][1][i], hot, a);
@@ -460,10 +463,10 @@ template <typename T, bool TP, bool TQ, typename C> __device__ __forceinline__ v
             for (int o = 0; o < NP; ++o) {
 #pragma unroll
                 for (int i = 0; i < FI; ++i)
-                    x[i][o] = *reinterpret_cast<const u4 *>(ldsP + o * planeP + place<KS>((wi * FI + i) * 16 + at, kk * 4 + chunk));
+                    x[i][o] = *reinterpret_cast<const u4 *>(ldsP + o * planeP + place<KS, TP>((wi * FI + i) * 16 + at, kk * 4 + chunk));
 #pragma unroll
                 for (int j = 0; j < FJ; ++j)
-                    y[j][o] = *reinterpret_cast<const u4 *>(ldsQ + o * planeQ + place<KS>((wj * FJ + j) * 16 + at, kk * 4 + chunk));
+                    y[j][o] = *reinterpret_cast<const u4 *>(ldsQ + o * planeQ + place<KS, TQ>((wj * FJ + j) * 16 + at, kk * 4 + chunk));
             }
 #pragma unroll
             for (int i = 0; i < FI; ++i) {
@@ -791,7 +794,7 @@ template <bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::
         typedef __attribute__((address_space(3))) void *Lds;
         typedef __attribute__((address_space(1))) const void *Global;
         const int l = again_of(tid) & 63;
-        const uint32_t off = (l >> 2) * 64 + ((l & 3) ^ (l >> 4)) * 16;
+        const uint32_t off = (l >> 2) * 64 + ((l & 3) ^ turn_of(l >> 4)) * 16;
 #pragma unroll
         for (int u = 0; u < loads; ++u) {
             const int b = u * waves + wave, o = b / (C::BJ / 16), row = b % (C::BJ / 16) * 16;
@@ -950,12 +953,12 @@ template <typename C> __global__ void __launch_bounds__(C::threads, C::per) piec
         u4 x[FI][3], y[FJ][3];
         const auto read = [&](int i) {
 #pragma unroll
-            for (int o = 0; o < 3; ++o) x[i][o] = *reinterpret_cast<const u4 *>(fromP + o * planeP + place<32>((wi * FI + i) * 16 + at, chunk));
+            for (int o = 0; o < 3; ++o) x[i][o] = *reinterpret_cast<const u4 *>(fromP + o * planeP + place<32, true>((wi * FI + i) * 16 + at, chunk));
         };
 #pragma unroll
         for (int o = 0; o < 3; ++o)
 #pragma unroll
-            for (int j = 0; j < FJ; ++j) y[j][o] = *reinterpret_cast<const u4 *>(fromQ + o * planeQ + place<32>((wj * FJ + j) * 16 + at, chunk));
+            for (int j = 0; j < FJ; ++j) y[j][o] = *reinterpret_cast<const u4 *>(fromQ + o * planeQ + place<32, true>((wj * FJ + j) * 16 + at, chunk));
 #pragma unroll
         for (int i = 0; i < FI / 2; ++i) read(i);
         const auto multiply = [&](int i) {
