@@ -157,6 +157,53 @@ def test_many_rows(kind, size):
     run(wide[:, 3:3 + K], W, None, "silu", wide[:, 3 + K:3 + K + N], 0.0, 0, 0, kind, wide[:, 2:2 + N])
 
 
+# more tiles of fp32 numbers than compute units: a workgroup takes several, k that neither stages nor loads divide
+@pytest.mark.parametrize("size", [(50_001, 301, 300), (66_000, 131, 520), (36_000, 67, 700), (9000, 1030, 1290)], ids=lambda s: "x".join(map(str, s)))
+def test_many_tiles(size):
+    M, K, N = size
+    X, W, R = _normal(1, M, K), _normal(2, N, K, scale=K ** -0.5), _normal(4, M, N)
+    run(X, W, _normal(3, N), "silu", R, 0.1, 9, 2, "fp32", _normal(5, M, N))
+    run(X, W, None, "none", None, 0.0, 0, 0, "fp32", _normal(5, M, N))
+
+
+# numbers out of the pieces' range in some of a workgroup's tiles of up to 128 rows, the last row and column among them: there the product is one of fp32 numbers,
+# K roundings one after the other, elsewhere as it was
+def test_range_among_many_tiles():
+    from paper_2605_15695_amd.linear import linear
+
+    M, K, N = 50_000, 300, 300
+    X, W = _normal(6, M, K), _normal(7, N, K)
+    plain = linear(X, W)
+    A = X.clone()
+    inf, nan = float("inf"), float("nan")
+    rows = [5, 127, 128, 20_000, 33_000, 49_999]
+    A[5, 0], A[127, 299], A[128, 31], A[20_000, 32], A[33_000, 160], A[49_999, 299] = inf, -inf, nan, 2.0 ** 100, 2.0 ** 31, -2.0 ** 90
+    got, ref = linear(A, W), A @ W.t()
+    assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf()) and torch.equal(got[got.isinf()], ref[ref.isinf()])
+    fine = ref.isfinite()
+    _near(got[fine], (A.double() @ W.double().t())[fine], (K + 2) * U * (A.double().abs() @ W.double().abs().t())[fine], U)
+    assert torch.equal(got.nan_to_num(7.0), linear(A, W).nan_to_num(7.0))
+    tiles = {r // 128 for r in rows}
+    far = torch.tensor([r for r in range(M) if r // 128 not in tiles], device="cuda")
+    assert torch.equal(got[far], plain[far])
+    V = W.clone()
+    V[299, 299] = 2.0 ** 60  # weights: all tiles
+    _near(linear(X, V), X.double() @ V.double().t(), (K + 2) * U * (X.double().abs() @ V.double().abs().t()), U)
+
+
+# rows so far apart that places within a tile pass 2^31 bytes
+def test_rows_far_apart():
+    from paper_2605_15695_amd.linear import linear
+
+    apart, M, K, N = (1 << 22) + 8, 150, 128, 700
+    room = torch.empty(M * apart, device="cuda")
+    X, dy = room.as_strided((M, K), (apart, 1)), room.as_strided((M, N), (apart, 1), K)
+    X.copy_(_normal(1, M, K)), dy.copy_(_normal(2, M, N))
+    W = _normal(3, N, K)
+    run(X, W, None, "none", None, 0.0, 0, 0, "fp32", dy)
+    assert torch.equal(linear(X[:, :64], W[:, :64]), linear(X[:, :64], W[:, :64].contiguous()))
+
+
 # gradients of 16-bit numbers in one read, where dw fits a workgroup
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 @pytest.mark.parametrize("size", [(131_072, 64, 256), (140_001, 8, 8), (131_200, 40, 200), (150_000, 48, 72), (262_145, 16, 64), (131_073, 56, 104)],
