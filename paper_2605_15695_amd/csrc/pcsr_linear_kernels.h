@@ -991,7 +991,9 @@ template <typename C> __global__ void __launch_bounds__(C::threads, C::per) piec
 // 2,000,000 x 256 -> 64 in fp32 with a residual 614 to 658 us: 3.07 GB, 4.7 to 5.0 TB/s; matrix units are 32 % busy, vector units 37 beside them.  480,000 x 64 -> 256 in bf16 with gelu,
 // dropout and slopes 141 to 152 us: vector units are 91 % busy with what follows the product (memory would take 89).
 // Loads come back in their order, and so do the waits: what a strip's end needs is asked for before the next strip's numbers, and the bias lies in LDS.
-template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64 + 16; } // bytes of a row: 16 rows lie in different banks
+template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64; } // bytes of a row
+// Chunks of 16 bytes are exchanged by these bits of a row's number, so that the 16 that are read at once (place) lie in different banks.
+template <int STEPS> __device__ __forceinline__ int exchange(int row) { return STEPS >= 4 ? row & 15 : STEPS == 2 ? row >> 1 & 7 : turn_of(row >> 2 & 3); }
 template <typename T, int STEPS> int64_t weights_bytes(int64_t cols) { return Num<T>::NP * up(cols, 64) * 64 * weights_pitch<T, STEPS>(); }
 
 template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global__ void __launch_bounds__(512) rows_kernel(TileArgs a, int groups)
@@ -1037,7 +1039,7 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
 #pragma unroll
             for (int e = 0; e < 2; ++e)
                 w[e] = j < a.q.n && k + e < K ? static_cast<const T *>(a.q.at)[TQ ? (k + e) * a.q.ld + j : j * a.q.ld + k + e] : (T)0.0f;
-            uint32_t *to = reinterpret_cast<uint32_t *>(lds + j * pitch + k * 2);
+            uint32_t *to = reinterpret_cast<uint32_t *>(lds + j * pitch + (k / 8 ^ exchange<STEPS>(j)) * 16 + k % 8 * 2);
             if constexpr (NP == 3) {
                 uint32_t h[3];
                 pieces(w[0], w[1], hot, h);
@@ -1062,7 +1064,7 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
         key = key_of(a.tail.drop);
         if (blockIdx.x == 0 && tid == 0) tell_key(a.tail.drop, key);
     }
-    const char *mine = lds + at * pitch + chunk * 16;
+    const int mine = at * pitch + (chunk ^ exchange<STEPS>(at)) * 16;
     const int c = lane % per * 8;
     float hot = 0.0f;
     for (; strip * 16 < rows; strip += stride) {
@@ -1079,13 +1081,14 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
                     if (WHOLE) load<T, 8>(p + (m > 0 ? col : 0), res[h]);
                     else if (m > 0) load_upto<T, 8>(p + col, m, res[h]);
                 }
-            const char *w = mine + g * FJ * 16 * pitch;
+            const char *w = lds + g * FJ * 16 * pitch;
             f4 sum[FJ];
 #pragma unroll
             for (int j = 0; j < FJ; ++j) sum[j] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 u4 x[NP];
+                const int here = NP == 3 ? again_of(mine) : mine;
                 if constexpr (NP == 3) {
                     // the compiler is kept from making the pieces of all steps once for all groups: registers do not hold them
 #pragma unroll
@@ -1110,7 +1113,7 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
 #pragma unroll
                     for (int j = 0; j < B; ++j)
 #pragma unroll
-                        for (int o = 0; o < NP; ++o) y[j][o] = *reinterpret_cast<const u4 *>(w + o * plane + (b + j) * 16 * pitch + t * 64);
+                        for (int o = 0; o < NP; ++o) y[j][o] = *reinterpret_cast<const u4 *>(w + o * plane + (b + j) * 16 * pitch + (t & ~3) * 64 + (here ^ (t & 3) * 64));
                     if constexpr (NP == 3) {
                         f4 part[B];
                         products32<B>(x, y, part);
