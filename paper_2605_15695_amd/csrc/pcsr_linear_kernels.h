@@ -750,7 +750,7 @@ __device__ __forceinline__ int again_of(int tid)
 // Products with weights.  A compute unit's workgroup takes its tiles one behind the other, and the first numbers of a tile are on their way, and in LDS, while
 // what follows the one before it is done.  No load stands behind a condition, or waits behind it would be for all of them: places behind a row's end are read in front
 // of it, and what lies there is put right on its way to LDS.
-// 250,000 x 256 -> 256: 317 us (silu, dropout, a residual, slopes; 1.04 GB), gradient of x 222 (0.54 GB); a tile to a workgroup took 331 and 251.  Six products of 33 GFLOP would be 110 us
+// 250,000 x 256 -> 256: 311 us (silu, dropout, a residual, slopes; 1.04 GB), gradient of x 220 (0.55 GB); a tile to a workgroup took 331 and 251.  Six products of 33 GFLOP would be 110 us
 // at the rate of random numbers above; matrix units are 29 and 43 % busy, the rest is the ends of tiles and, in a stage, reads from LDS and the wait for numbers that were asked for one and a half
 // stages before (loads return in order, so that the wait for a stage's planes is one for them too).  Halves of the wavefronts a stage apart, one moving while the other
 // multiplies, took 1.04 of this for gradients.
@@ -909,8 +909,8 @@ template <bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::
         }
     }
 }
-// Gradients of weights: both operands are split on their way, and few tiles mean many stretches of k.  250,000 x 256 -> 256: 229 us in 254 workgroups (0.55 GB), matrix units 41 %
-// busy; bound as planes_kernel is.
+// Gradients of weights: both operands are split on their way, and few tiles mean many stretches of k.  250,000 x 256 -> 256: 211 us in 254 workgroups (0.56 GB), matrix units 45 %
+// busy (226 where writes that turn met in a bank); bound as planes_kernel is.
 template <typename C> __global__ void __launch_bounds__(C::threads, C::per) pieces_kernel(TileArgs a)
 {
     typedef float T;
@@ -988,8 +988,8 @@ template <typename C> __global__ void __launch_bounds__(C::threads, C::per) piec
 // The weights lie in LDS for as long as the workgroup lives, in pieces, and wavefronts take 16 rows at a time, each for itself: a lane's numbers of the next rows
 // are on their way to its registers while these are multiplied, nothing waits for other wavefronts, and x is read once.
 // STEPS: of 32 numbers of k.  FJ tiles of 16 columns at a time.  WHOLE: all of k is there, and of columns 8 or none.  RES: a residual is there.
-// 2,000,000 x 256 -> 64 in fp32 with a residual 614 to 658 us: 3.07 GB, 4.7 to 5.0 TB/s; matrix units are 32 % busy, vector units 37 beside them.  480,000 x 64 -> 256 in bf16 with gelu,
-// dropout and slopes 141 to 152 us: vector units are 91 % busy with what follows the product (memory would take 89).
+// 2,000,000 x 256 -> 64 in fp32 with a residual 614 to 624 us: 3.07 GB, 4.9 to 5.0 TB/s; matrix units are 35 % busy, vector units 43.  480,000 x 64 -> 256 in bf16 with gelu,
+// dropout and slopes 141 to 158 us: vector units are 92 % busy with what follows the product (memory would take 89).
 // Loads come back in their order, and so do the waits: what a strip's end needs is asked for before the next strip's numbers, and the bias lies in LDS.
 template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64; } // bytes of a row
 // Chunks of 16 bytes are exchanged by these bits of a row's number, so that the 16 that are read at once (place) lie in different banks.
@@ -1394,8 +1394,8 @@ template <typename T> __global__ void __launch_bounds__(kT) last_kernel(FinishAr
 // dz, dx, dw and db of 16-bit numbers from one read of dy, the slopes and x, where dw fits a workgroup's registers: up to 256 columns of dy and 64 of x.
 // A workgroup takes 64 or 128 rows at a time: dz and x go to LDS as they are, [row][column], the weights lie there turned, and dx = dz w reads dz by rows,
 // dw += dz^T x both by columns (turned by the LDS reads).  A thread keeps its 8 columns of dy, so that db is a sum of its own; when it has used a row's numbers
-// it asks for those that come next.  480,000 x 64 -> 256 in bf16, dropout: 164 us (630 MB: memory would take 102), vector units 56 % busy with the
-// generator and the slopes, LDS 31 %; all wavefronts at the same of both took 174, with one buffer too; slope_kernel and both products 285.
+// it asks for those that come next.  480,000 x 64 -> 256 in bf16, dropout: 164 us (630 MB: memory would take 102), vector units 58 % busy with the
+// generator and the slopes, LDS 32 %; all wavefronts at the same of both took 174, with one buffer too; slope_kernel and both products 285.
 struct NarrowArgs {
     const void *dy, *slope, *x, *w; // slope: null for none
     int64_t dy_stride, x_stride, w_stride, rows;
