@@ -1643,7 +1643,8 @@ template <typename T> Plan plan(int64_t I, int64_t J, int64_t K, bool direct, bo
 int64_t part_bytes(const Plan &p, int64_t I, int64_t J) { return p.stretches > 1 ? round16(4 * I * J * p.stretches) : 0; }
 // planes of weights, and whether numbers in them are too large
 int64_t plane_rows(const Plan &p) { return p.tiles_j * PiecesFlat::BJ; }
-int64_t plane_bytes(const Plan &p, int64_t K) { return p.which >= PIECES_FLAT ? 3 * 2 * plane_rows(p) * (up(K, 64) + 1) * 64 + 4 * kSplitBlocks : 0; }
+int64_t plane_depth(int64_t K) { return up(K, 64) * 64 + 128; } // a stretch begins below K and is read to four stages of 32 from there, or to the end of its last pair
+int64_t plane_bytes(const Plan &p, int64_t K) { return p.which >= PIECES_FLAT ? 3 * 2 * plane_rows(p) * plane_depth(K) + 4 * kSplitBlocks : 0; }
 // workspace of a product; weights: of rows with weights
 int64_t product_bytes(const Plan &p, int64_t I, int64_t J, int64_t K, bool weights) { return part_bytes(p, I, J) + (weights ? plane_bytes(p, K) : 0); }
 
@@ -1741,7 +1742,7 @@ template <typename T, bool TP, bool TQ> int product(const Side &p, const Side &q
                                             : go(&pieces_kernel<PiecesTall>, grid, pieces_bytes<PiecesTall>(), PiecesTall::threads);
             } else {
                 char *at = static_cast<char *>(ws) + part_bytes(c, tail.rows, tail.cols);
-                const int64_t rows = plane_rows(c), chunks = (up(K, 64) + 1) * 8;
+                const int64_t rows = plane_rows(c), chunks = plane_depth(K) / 8;
                 const Planes w = {reinterpret_cast<bfloat_t *>(at + 4 * kSplitBlocks), rows, rows * chunks * 8, reinterpret_cast<int *>(at)};
                 const SplitArgs s = {static_cast<const float *>(q.at), q.ld, q.n, K, rows, chunks, const_cast<bfloat_t *>(w.at), reinterpret_cast<int *>(at)};
                 hipLaunchKernelGGL(split_kernel<TQ>, dim3(kSplitBlocks), dim3(kT), 0, stream, s);

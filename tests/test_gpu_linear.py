@@ -166,6 +166,18 @@ def test_many_tiles(size):
     run(X, W, None, "none", None, 0.0, 0, 0, "fp32", _normal(5, M, N))
 
 
+# stretches of an odd number of stages, the last of which is shorter than the four that are read at least: planes of weights reach behind it, with zeros
+@pytest.mark.parametrize("size", [(8192, K, N) for K, N in ((289, 256), (300, 250), (320, 256), (97, 256), (161, 250))] + [(4096, 545, 512), (2048, 353, 1000)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_ends_of_stretches(size):
+    M, K, N = size
+    room = torch.full((1 << 26,), float("nan"), device="cuda")  # what a workspace is cut from
+    del room
+    X, W, dy = _normal(1, M, K), _normal(2, N, K, scale=K ** -0.5), _normal(5, M, N)
+    run(X, W, None, "none", None, 0.0, 0, 0, "fp32", dy)
+    run(dy, W.t().contiguous(), None, "silu", None, 0.0, 0, 0, "fp32", X)
+
+
 # numbers out of the pieces' range in some of a workgroup's tiles of up to 128 rows, the last row and column among them: there the product is one of fp32 numbers,
 # K roundings one after the other, elsewhere as it was
 def test_range_among_many_tiles():
