@@ -389,6 +389,7 @@ std::optional<at::Tensor> maybe(const at::Tensor &t) { return t.defined() ? std:
 at::Tensor of(const std::optional<at::Tensor> &t) { return t.has_value() ? *t : at::Tensor(); }
 at::Tensor gradient_rows(const at::Tensor &grad, int64_t n, int64_t d)
 {
+    if (grad.dim() == 2 && !grad.is_neg() && distance(grad) >= 0) return grad;
     const at::Tensor g = grad.detach().resolve_neg().reshape({n, d});
     return distance(g) < 0 ? g.contiguous() : g;
 }
@@ -492,7 +493,7 @@ struct Linear : torch::autograd::Function<Linear> {
         const variable_list saved = ctx->get_saved_variables();
         const std::vector<int64_t> how = ctx->saved_data["how"].toIntVector();
         const DropCall d = DropCall::of(how, saved[3]);
-        const at::Tensor X = saved[0].detach(), W = saved[1].detach();
+        const at::Tensor X = saved[0].dim() == 2 ? saved[0] : saved[0].detach(), &W = saved[1];
         const int64_t act = how[3], bias = how[4];
         size_t at = 2; // (tensors that are not there are not counted)
         const bool need_b = bias >= 0 && ctx->needs_input_grad(at++), need_r = how[5] && ctx->needs_input_grad(at++);
