@@ -597,7 +597,7 @@ template <bool TP, bool TQ, typename C> constexpr int straight_bytes()
 }
 // Bound by the matrix units, which alone reach 2.4 PFLOP/s on zeros and 1.8 on random numbers here.  4096^3 in bf16: 115 us (1.2 PFLOP/s) where operands stay in caches, 126 to 135 where not,
 // matrix units 51 to 54 % busy, 256 x 256 tiles (one to a compute unit: 512 numbers of operands from LDS for 65,536 products; 128 x 128 take 131 us).  32,768 x 768 -> 1000 in
-// fp16 88 us, of which some 20 are what ends the tiles (gelu, dropout, slopes) with nothing beside it; its gradient of x 75 us in tiles of 128 x 128.
+// fp16 87 us, 36 of them what ends the tiles (gelu, dropout, slopes) with nothing beside it, and 113 in tiles of 128 x 128; its gradient of x 75 us in tiles of 128 x 128.
 // The next numbers are read from LDS while those before are multiplied, and a stage's loads are given out when all wavefronts have read the one
 // before it, which is half a stage before they multiply its last numbers.
 template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) straight_kernel(TileArgs a)
