@@ -157,6 +157,7 @@ def _lib():
         lib.pcsr_linear_workspace.restype = i64
         lib.pcsr_linear.argtypes = [pl, vp, vp, vp, vp]
         lib.pcsr_linear_backward.argtypes = [pl, vp, vp, i64, vp, vp, vp, vp, vp]
+        lib.pcsr_linear_uses.argtypes = [pl, vp, i64, vp]
         for name in ("pcsr_build", "pcsr_spmm", "pcsr_free", "pcsr_set_kernel_params",
                      "pcsr_query_launch", "pcsr_query_kernel", "pcsr_export", "pcsr_features", "pcsr_select",
                      "pcsr_window_stats", "pcsr_features_device", "pcsr_reorder", "pcsr_permute_csr",
@@ -165,7 +166,7 @@ def _lib():
                      "pcsr_gnn_mlp", "pcsr_gnn_mlp_backward", "pcsr_gnn_linear_backward", "pcsr_gnn_wgrad",
                      "pcsr_gnn_colsum", "pcsr_operator_build", "pcsr_release_cached", "pcsr_embed",
                      "pcsr_embed_backward", "pcsr_norm", "pcsr_norm_backward", "pcsr_orthogonalize", "pcsr_dropout",
-                     "pcsr_linear", "pcsr_linear_backward"):
+                     "pcsr_linear", "pcsr_linear_backward", "pcsr_linear_uses"):
             getattr(lib, name).restype = ctypes.c_int
         _LIB = lib
     return _LIB

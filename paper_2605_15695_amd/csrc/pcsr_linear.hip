@@ -55,4 +55,14 @@ int pcsr_linear_backward(const pcsr_linear_t *a, const void *slope, const void *
     if (!dy || dy_stride < a->out || (a->act != PCSR_ACT_NONE && !slope) || (dx && !a->w) || (dw && !a->x) || !ws) return PCSR_E_INVALID_ARG;
     return for_type(a->type, [&](auto t) { return LinearOf<decltype(t)>::backward(*a, slope, dy, dy_stride, dx, dw, db, ws, (hipStream_t)stream); });
 }
+
+int pcsr_linear_uses(const pcsr_linear_t *a, const void *dy, int64_t dy_stride, int64_t *ends)
+{
+    if (const int rc = check(a)) return rc;
+    if (a->rows == 0 || dy_stride < a->out || !ends) return PCSR_E_INVALID_ARG;
+    return for_type(a->type, [&](auto t) {
+        LinearOf<decltype(t)>::uses(*a, dy, dy_stride, *reinterpret_cast<int64_t (*)[4][2]>(ends));
+        return (int)PCSR_OK;
+    });
+}
 }

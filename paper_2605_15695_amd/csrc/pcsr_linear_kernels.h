@@ -1772,22 +1772,45 @@ template <typename T> bool narrow(const pcsr_linear_t &a)
     return sizeof(T) == 2 && a.rows >= 512 * kNarrowBlocks && a.out <= 256 && a.in <= 64 && a.out > 0 && a.in > 0 && a.out % 8 == 0 && a.in % 8 == 0;
 }
 
+// The products of a backward pass, dx = dz w and dw = dz^T x: one choice, for what runs and for what is asked for to hold its sums.
+struct Ways {
+    Plan best, small; // the cheapest, and in tiles of 64 x 64
+};
+template <typename T> Ways ways(int64_t I, int64_t J, int64_t K, bool direct, bool weights)
+{
+    return {plan<T>(I, J, K, direct, weights), plan<T>(I, J, K, direct, weights, SMALL)};
+}
+template <typename T> Ways ways_x(const pcsr_linear_t &a, bool direct) { return ways<T>(a.rows, a.in, a.out, direct, true); }
+template <typename T> Ways ways_w(const pcsr_linear_t &a, bool direct) { return ways<T>(a.out, a.in, a.rows, direct, false); }
+struct Products {
+    Plan x, w;
+    bool rows, pair;          // rows_kernel takes dx; both side by side in tiles of 64 x 64
+    int64_t bytes_x, bytes_w; // of workspace that they write
+    template <typename T> static Products of(const pcsr_linear_t &a, const Ways &x, const Ways &w, bool direct_x)
+    {
+        Products p = {x.best, w.best, many_rows<T>(a.rows, a.in, a.out, direct_x), false, 0, 0};
+        // tiles of 64 x 64 for both, where side by side they take less; whatever is asked for, so that the bits do not depend on that
+        const Plan &sx = x.small, &sw = w.small;
+        const bool fit = sx.tiles_i * sx.tiles_j * sx.stretches + sw.tiles_i * sw.tiles_j * sw.stretches <= 1024;
+        if (!p.rows && fit && 1.1f * (sx.us > sw.us ? sx.us : sw.us) < p.x.us + p.w.us + 4.0f) p.x = sx, p.w = sw;
+        p.pair = !p.rows && a.in > 0 && p.x.which == SMALL && p.w.which == SMALL;
+        p.bytes_x = p.rows ? 0 : round16(product_bytes(p.x, a.rows, a.in, a.out, true));
+        p.bytes_w = round16(product_bytes(p.w, a.out, a.in, a.rows, false));
+        return p;
+    }
+};
+
 // the parts of the workspace of a backward call
 struct Space {
-    int64_t ld, dz, sums, part, part_w, bytes;
+    int64_t ld, dz, sums, x, w, bytes; // bytes of dz (rows ld numbers apart), of sums of its columns, of what the products write
     int64_t blocks; // workgroups of slope_kernel along the rows
     int lanes;
+    int64_t at_sums() const { return dz; }
+    int64_t at_x() const { return dz + sums; }
+    int64_t at_w() const { return dz + sums + x; }
     template <typename T> static Space of(const pcsr_linear_t &a, bool own)
     {
-        Space s;
-        const auto most_of = [](int64_t I, int64_t J, int64_t K, bool weights) { // however the operands lie
-            int64_t most = product_bytes(plan<T>(I, J, K, false, weights, SMALL), I, J, K, weights);
-            for (int direct = 0; direct < 2; ++direct) {
-                const int64_t need = product_bytes(plan<T>(I, J, K, direct, weights), I, J, K, weights);
-                most = need > most ? need : most;
-            }
-            return most;
-        };
+        Space s = {};
         s.ld = up(a.out, 8) * 8;
         s.lanes = 1;
         while (s.lanes < 64 && s.lanes * 8 < a.out) s.lanes *= 2;
@@ -1796,14 +1819,17 @@ struct Space {
         s.blocks = up(a.rows, per) < most ? up(a.rows, per) : most;
         s.dz = own ? round16(a.rows * s.ld * (int64_t)sizeof(T)) : 0;
         s.sums = round16(4 * s.blocks * a.out);
-        const int64_t x = most_of(a.rows, a.in, a.out, true), w = most_of(a.out, a.in, a.rows, false);
-        s.part = round16(x) + round16(w); // (for both at once)
+        // however the operands lie, dy's place is not known here
+        const Ways x[2] = {ways_x<T>(a, false), ways_x<T>(a, true)}, w[2] = {ways_w<T>(a, false), ways_w<T>(a, true)};
+        for (int d = 0; d < 4; ++d) {
+            const Products p = Products::of<T>(a, x[d & 1], w[d >> 1], d & 1);
+            s.x = p.bytes_x > s.x ? p.bytes_x : s.x, s.w = p.bytes_w > s.w ? p.bytes_w : s.w;
+        }
         if (narrow<T>(a)) {
             const int64_t sums = round16(4 * kNarrowBlocks * a.out), part = round16(4 * kNarrowBlocks * a.out * a.in);
-            s.sums = sums > s.sums ? sums : s.sums, s.part = part > s.part ? part : s.part;
+            s.sums = sums > s.sums ? sums : s.sums, s.w = part > s.w ? part : s.w;
         }
-        s.part_w = round16(x);
-        s.bytes = s.dz + s.sums + s.part;
+        s.bytes = s.dz + s.sums + s.x + s.w;
         return s;
     }
 };
@@ -1829,6 +1855,26 @@ template <typename T> int few_rows(const TileArgs &a, hipStream_t stream)
     return launched();
 }
 
+// A backward call as it runs, from arguments that are checked.  at: its workspace.
+struct Pass {
+    bool own; // dz is written; it is dy otherwise
+    Space space;
+    Side dz;
+    bool direct_x, direct_w;
+    Products products;
+    template <typename T> static Pass of(const pcsr_linear_t &a, const void *dy, int64_t dy_stride, const void *at)
+    {
+        Pass p = {};
+        p.own = has_slope(a);
+        p.space = Space::of<T>(a, p.own);
+        p.dz = p.own ? Side{at, p.space.ld, a.rows} : Side{dy, dy_stride, a.rows};
+        p.direct_x = straight_with<T>(p.dz, {a.w, a.w_stride, a.in}, true, a.out);
+        p.direct_w = straight<T>({p.dz.at, p.dz.ld, a.out}, true, p.own) && straight<T>({a.x, a.x_stride, a.in}, true, false);
+        p.products = Products::of<T>(a, ways_x<T>(a, p.direct_x), ways_w<T>(a, p.direct_w), p.direct_x);
+        return p;
+    }
+};
+
 } // namespace
 
 template <typename T> int64_t LinearOf<T>::workspace(const pcsr_linear_t &a, bool backward)
@@ -1848,15 +1894,15 @@ template <typename T> int LinearOf<T>::forward(const pcsr_linear_t &a, void *y, 
 template <typename T>
 int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws, hipStream_t stream)
 {
-    const bool own = has_slope(a);
-    const Space sp = Space::of<T>(a, own);
     char *at = static_cast<char *>(ws);
-    float *sums = reinterpret_cast<float *>(at + sp.dz);
-    void *part = at + sp.dz + sp.sums;
+    const Pass pass = Pass::of<T>(a, dy, dy_stride, at);
+    const Space &sp = pass.space;
+    const bool own = pass.own;
+    float *sums = reinterpret_cast<float *>(at + sp.at_sums()), *part_w = reinterpret_cast<float *>(at + sp.at_w());
     if (narrow<T>(a)) { // whatever is asked for, so that the bits do not depend on that
         if constexpr (sizeof(T) == 2) {
             const NarrowArgs n = {dy, a.act == PCSR_ACT_NONE ? nullptr : slope, dw ? a.x : nullptr, dx ? a.w : nullptr, dy_stride, a.x_stride, a.w_stride, a.rows, (int)a.in, (int)a.out, dx,
-                                  dw ? static_cast<float *>(part) : nullptr, sums, drop_of(&a.drop)};
+                                  dw ? part_w : nullptr, sums, drop_of(&a.drop)};
             const auto go = [&](auto *kernel, int lanes) {
                 const size_t lds = (size_t)narrow_lds(lanes, a.out, a.in), bytes = lds > kNarrowT * 36 ? lds : kNarrowT * 36;
                 if (!allow_lds(kernel, bytes)) return (int)PCSR_E_HIP;
@@ -1874,30 +1920,21 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
             return launched();
         }
     }
-    Side dz = {dy, dy_stride, a.rows};
     if (own || db) {
         SlopeArgs s = {dy, a.act == PCSR_ACT_NONE ? nullptr : slope, dy_stride, a.rows, a.out, sp.ld, own && (dx || dw) ? at : nullptr,
                        db ? sums : nullptr, sp.lanes, drop_of(&a.drop)};
         hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)sp.blocks, (unsigned)up(a.out, sp.lanes * 8)), dim3(kSlopeT), 0, stream, s);
-        if (own) dz = {at, sp.ld, a.rows};
     }
     const SumsArgs b = {sums, sp.blocks, a.out, a.bias_type, db};
     const Tail tail_x = {nullptr, nullptr, dx, nullptr, 0, a.rows, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
     const Tail tail_w = {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
-    const Side w = {a.w, a.w_stride, a.in}, g = {dz.at, dz.ld, a.out}, x = {a.x, a.x_stride, a.in};
-    const bool direct_x = straight_with<T>(dz, w, true, a.out), direct_w = straight<T>(g, true, own) && straight<T>(x, true, false);
+    const Side &dz = pass.dz, w = {a.w, a.w_stride, a.in}, g = {dz.at, dz.ld, a.out}, x = {a.x, a.x_stride, a.in};
     int rc = launched();
     if (rc != PCSR_OK) return rc;
-    Plan px = plan<T>(a.rows, a.in, a.out, direct_x, true), pw = plan<T>(a.out, a.in, a.rows, direct_w, false);
-    const bool rows = many_rows<T>(a.rows, a.in, a.out, direct_x);
-    { // tiles of 64 x 64 for both, where side by side they take less; whatever is asked for, so that the bits do not depend on that
-        const Plan sx = plan<T>(a.rows, a.in, a.out, direct_x, true, SMALL), sw = plan<T>(a.out, a.in, a.rows, direct_w, false, SMALL);
-        const bool fit = sx.tiles_i * sx.tiles_j * sx.stretches + sw.tiles_i * sw.tiles_j * sw.stretches <= 1024;
-        if (!rows && fit && 1.1f * (sx.us > sw.us ? sx.us : sw.us) < px.us + pw.us + 4.0f) px = sx, pw = sw;
-    }
-    if (dx && dw && a.in > 0 && px.which == SMALL && pw.which == SMALL && !rows) {
-        float *part_x = px.stretches > 1 ? static_cast<float *>(part) : nullptr;
-        float *part_w = pw.stretches > 1 ? reinterpret_cast<float *>(static_cast<char *>(part) + sp.part_w) : nullptr;
+    const Plan &px = pass.products.x, &pw = pass.products.w;
+    if (dx && dw && pass.products.pair) {
+        float *part_x = px.stretches > 1 ? reinterpret_cast<float *>(at + sp.at_x()) : nullptr;
+        if (pw.stretches == 1) part_w = nullptr;
         const TileArgs ax = {dz, w, a.out, px.stretch, (int)px.tiles_i, (int)px.tiles_j, px.stretches, part_x, tail_x};
         const TileArgs aw = {g, x, a.rows, pw.stretch, (int)pw.tiles_i, (int)pw.tiles_j, pw.stretches, part_w, tail_w};
         const unsigned first = (unsigned)(px.tiles_i * px.tiles_j * px.stretches), second = (unsigned)(pw.tiles_i * pw.tiles_j * pw.stretches);
@@ -1914,9 +1951,21 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
         hipLaunchKernelGGL(sums_kernel, dim3((unsigned)up(a.out, 16)), dim3(1024), 0, stream, b);
         rc = launched();
     }
-    if (dx && a.in > 0 && rc == PCSR_OK) rc = product<T, false, true>(dz, w, a.out, direct_x, px, tail_x, part, stream);
-    if (dw && a.in > 0 && rc == PCSR_OK) rc = product<T, true, true>(g, x, a.rows, direct_w, pw, tail_w, part, stream);
+    if (dx && a.in > 0 && rc == PCSR_OK) rc = product<T, false, true>(dz, w, a.out, pass.direct_x, px, tail_x, at + sp.at_x(), stream);
+    if (dw && a.in > 0 && rc == PCSR_OK) rc = product<T, true, true>(g, x, a.rows, pass.direct_w, pw, tail_w, part_w, stream);
     return rc;
+}
+
+template <typename T> void LinearOf<T>::uses(const pcsr_linear_t &a, const void *dy, int64_t dy_stride, int64_t (&ends)[4][2])
+{
+    const Pass pass = Pass::of<T>(a, dy, dy_stride, nullptr);
+    const Space &sp = pass.space;
+    const bool one = narrow<T>(a);
+    const int64_t in[4][2] = {{0, pass.own && !one ? a.rows * sp.ld * (int64_t)sizeof(T) : 0},
+                              {sp.at_sums(), 4 * (one ? kNarrowBlocks : sp.blocks) * a.out},
+                              {sp.at_x(), one ? 0 : pass.products.bytes_x},
+                              {sp.at_w(), one ? 4 * kNarrowBlocks * a.out * a.in : pass.products.bytes_w}};
+    for (int k = 0; k < 4; ++k) ends[k][0] = in[k][0], ends[k][1] = in[k][0] + in[k][1];
 }
 
 } // namespace pcsr

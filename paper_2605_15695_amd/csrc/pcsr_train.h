@@ -120,4 +120,7 @@ int pcsr_linear(const pcsr_linear_t *a, void *y, void *slope, void *ws, void *st
 // dw alone, a->w for dx.
 int pcsr_linear_backward(const pcsr_linear_t *a, const void *slope, const void *dy, int64_t dy_stride, void *dx, void *dw, void *db, void *ws,
                          void *stream);
+// Where a backward call that is asked for all of its results writes its workspace, the host's arithmetic alone: first and last byte (exclusive) of dz, of sums of its columns, of
+// what the products of dx and of dw write: ends[4][2].  dy: its address, which is not read.
+int pcsr_linear_uses(const pcsr_linear_t *a, const void *dy, int64_t dy_stride, int64_t *ends);
 }

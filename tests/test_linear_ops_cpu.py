@@ -86,6 +86,62 @@ def test_linear_entry_points():
     assert lib.pcsr_linear_workspace(None, 0) == 0 and lib.pcsr_linear(None, P, None, P, None) == INVALID
 
 
+# what a backward pass writes of its workspace lies within what is asked for, however its operands lie: each part behind the one before
+def _parts(rows, cols_in, out, kind, act=0, odd=(0, 0, 0), p=0.0):
+    """bytes asked for, and (first, last) of the four parts that are written; odd: of x, w and dy, whether they lie at odd addresses"""
+    size = 2 if kind else 4
+    a = _linear(rows=rows, out=out, type=kind, act=act, x_stride=cols_in, w_stride=cols_in, x=P + size * odd[0], w=P + size * odd[1], p=p, **{"in": cols_in})
+    ends = (ctypes.c_int64 * 8)()
+    assert pc._lib().pcsr_linear_uses(ctypes.byref(a), P + size * odd[2], out, ends) == OK
+    return pc._lib().pcsr_linear_workspace(ctypes.byref(a), 1), [(ends[2 * k], ends[2 * k + 1]) for k in range(4)]
+
+
+def _fits(*case, **kw):
+    asked, parts = _parts(*case, **kw)
+    at = 0
+    for first, last in parts:
+        assert at <= first <= last and first % 16 == 0, (case, kw, asked, parts)
+        at = last
+    assert at <= asked, (case, kw, asked, parts)
+    return asked, parts
+
+
+LYING = [(x, w, dy) for x in (0, 1) for w in (0, 1) for dy in (0, 1)]
+
+
+@pytest.mark.parametrize("size", [(12_288, 192, 192), (18_432, 128, 192), (8286, 152, 176), (22_528, 64, 320), (2048, 512, 320), (8192, 160, 160),
+                                  (16_384, 32, 768), (512, 320, 2048), (480_000, 64, 256), (777, 75, 333), (1, 1, 1), (131_072, 8, 8), (40, 0, 9)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_workspace_of_a_backward_pass(size):
+    for kind in (0, 1, 2):
+        for odd in LYING:
+            for kw in (dict(), dict(act=2), dict(p=0.5)):
+                _fits(*size, kind, odd=odd, **kw)
+
+
+def test_workspace_of_many_sizes():
+    rng = np.random.default_rng(11)
+    for n in range(30_000):
+        M, K, N = (int(np.exp(v)) for v in rng.uniform(0, (13.5, 8.5, 8.5)))
+        if n % 4:  # whole pieces of 16 bytes, as a model's widths are: operands that can lie either way
+            K, N = -(-K // 8) * 8, -(-N // 8) * 8
+        if -(-K // 64) * -(-N // 64) > 1 << 23:
+            continue
+        for kind in (n % 2 + 1, 0) if n % 3 == 0 else (n % 2 + 1,):
+            for odd in LYING[:4:2] + LYING[4:6]:
+                _fits(M, K, N, kind, odd=odd, act=2 * (n % 5 == 0))
+
+
+def test_uses_refuses():
+    ends = (ctypes.c_int64 * 8)()
+
+    def call(dy_stride=14, out=ends, **kw):
+        return pc._lib().pcsr_linear_uses(ctypes.byref(_linear(**kw)), P, dy_stride, out)
+
+    assert call() == OK and call(dy_stride=13) == INVALID and call(out=None) == INVALID and call(rows=0) == INVALID and call(type=3) == UNSUPPORTED
+    assert pc._lib().pcsr_linear_uses(None, P, 14, ends) == INVALID
+
+
 def test_host_tensors_are_refused():
     from paper_2605_15695_amd.dropout import Dropout, dropout
     from paper_2605_15695_amd.linear import FeedForward, Linear, linear
