@@ -67,15 +67,15 @@ __device__ __forceinline__ void philox(const DropKey &key, uint32_t group, uint3
     w[0] = c0, w[1] = c1, w[2] = c2, w[3] = c3;
 }
 
-// 8 columns from 8 group on, of a row: multiplied or dropped.  What is dropped is 0 whatever it was.
-__device__ __forceinline__ void drop8(const Drop &d, const DropKey &key, uint32_t group, uint32_t row, float (&x)[8])
+// 8 columns from 8 group on, of a row: multiplied (TIMES) or dropped.  What is dropped is 0 whatever it was.
+template <bool TIMES = true> __device__ __forceinline__ void drop8(const Drop &d, const DropKey &key, uint32_t group, uint32_t row, float (&x)[8])
 {
     uint32_t w[4];
     philox(key, group, row, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t bits = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
-        x[i] = bits >= d.threshold ? x[i] * d.keep : 0.0f;
+        x[i] = bits >= d.threshold ? TIMES ? x[i] * d.keep : x[i] : 0.0f;
     }
 }
 

@@ -1,8 +1,9 @@
 // Linear layers of any width with what follows them (see pcsr_train.h): the kernels and their launches for one type.  pcsr_linear_f32.hip,
 // pcsr_linear_bf16.hip and pcsr_linear_f16.hip make them, side by side; pcsr_linear.hip has the entry points.
 //
-// y = r + f act(z), z = x w^T + b, f = 0 or 1 / (1 - p) (pcsr_drop.h).  Backward: dz = f act'(z) dy, dx = dz w, dw = dz^T x,
-// db = the sums of dz's columns (dr = dy).
+// y = r + f act(z), z = x w^T + b, f = 0 or c = 1 / (1 - p) (pcsr_drop.h).  Backward: dz = f / c act'(z) dy, dx = c dz w, dw = c dz^T x,
+// db = c times the sums of dz's columns (dr = dy).  c multiplies sums in fp32 and not dz, which is rounded to x's type: fp16 ends at 65,504, and without an
+// activation, or with relu, dz is dy's numbers or none.
 //
 // Products D[i][j] = sum over k of P(i, k) Q(j, k) run on the 16-bit matrix instructions, in tiles that go through LDS, summed in
 // fp32.  An operand lies with its k side by side (x and w forward, dz for dx) or with its rows side by side (w for dx, dz and x for dw);
@@ -72,6 +73,7 @@ struct Tail {
     int64_t r_stride, rows, cols; // of y and slope, whose rows lie one behind the other
     int act, bias_type;
     Drop drop;
+    float times; // of the sums of a backward pass's product
 };
 
 // Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 of them to 1 (0 and 1 are exact, others are 2^-16 off at
@@ -366,6 +368,9 @@ __device__ __forceinline__ void finish_rows(const TileArgs &a, const DropKey &ke
             if (row < a.tail.rows) {
                 if (NP == 3 && w.again) once_more<T, TP, TQ>(a, row, w.col, w.m, w.k0, w.k1, v);
                 if (!a.part) {
+                    if (TQ) // (of backward passes alone)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] *= a.tail.times;
                     put8<T, WHOLE, RES>(a.tail, key, row, w.col, w.m, v, bias, res[u]);
                 } else {
                     float *to = a.part + (w.stretch * a.tail.rows + row) * a.tail.cols + w.col;
@@ -1145,6 +1150,9 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
                     v[e] = NP == 3 ? lo[e] * kDown : lo[e];
                     v[e + 4] = NP == 3 ? hi[e] * kDown : hi[e];
                 }
+                if (TQ)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= a.tail.times;
                 if (m > 0 && row < rows) put8<T, WHOLE, RES>(a.tail, key, row, col, m, v, bias, res[h]);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -1165,6 +1173,9 @@ template <typename T, bool TQ, int STEPS, int FJ, bool WHOLE, bool RES> __global
                     const int m = a.tail.cols - col >= 8 ? 8 : (int)(a.tail.cols - col);
                     float v[8];
                     once_more<T, false, TQ>(a, strip * 16 + r, col, m, 0, a.K, v);
+                    if (TQ)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] *= a.tail.times;
                     put_one<T>(a.tail, key, strip * 16 + r, col, m, v);
                 }
         }
@@ -1275,6 +1286,8 @@ template <typename T> __device__ __forceinline__ void finish_of(const FinishArgs
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += sums[p * across + lane][i];
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= a.times;
     if (row < a.rows) put_one<T>(a, key, row, c, m, v);
 }
 template <typename T> __global__ void __launch_bounds__(kT) finish_kernel(FinishArgs f)
@@ -1294,7 +1307,7 @@ struct SlopeArgs {
 };
 constexpr int kSlopeT = 1024, kSlopeBlocks = 512; // two workgroups a compute unit: as many sums as sums_kernel adds up in 6 us
 
-// dz = f act'(z) dy, and sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows, the next row's numbers on their way.
+// dz = act'(z) dy or 0 where it was dropped, and c times the sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows, the next row's numbers on their way.
 // Bound by memory: 250,000 x 256 in fp32 144 us (768 MB, 5.3 TB/s; 152 without the row ahead), 32,768 x 1000 in fp16 42, 4096 x 4096 in bf16 25 (100 MB).
 template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(SlopeArgs a)
 {
@@ -1334,7 +1347,7 @@ template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(Sl
             if (a.slope)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] *= Slope<T>::take(q[i]);
-            if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
+            if (a.drop.threshold) drop8<false>(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += d[i]; // (behind the end 0 times something)
             if (a.dz) store_upto<T, 8>(static_cast<T *>(a.dz) + row * a.ld + c, m, d);
@@ -1348,7 +1361,7 @@ template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(Sl
         float s = 0.0f;
         for (int q = 0; q < per; ++q) s += part[q * a.lanes + t / 8][t % 8];
         const int64_t col = (int64_t)blockIdx.y * a.lanes * 8 + t;
-        if (col < a.cols) a.sums[blockIdx.x * a.cols + col] = s;
+        if (col < a.cols) a.sums[blockIdx.x * a.cols + col] = s * a.drop.keep;
     }
 }
 // db: 16 columns to a workgroup of W threads
@@ -1477,7 +1490,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] *= Slope<T>::take(slope[u][i]);
             fetch(next, u);
-            if (a.drop.threshold) drop8(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
+            if (a.drop.threshold) drop8<false>(a.drop, key, (uint32_t)(c >> 3), (uint32_t)row, d);
             const bool there = row < a.rows;
             Raw g;
 #pragma unroll
@@ -1522,7 +1535,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int64_t row = tile * ROWS + rt * 16 + chunk * 4 + e;
-                    if (ct + j < tiles_k && col < in && row < a.rows) static_cast<T *>(a.dx)[row * in + col] = (T)s[j][e];
+                    if (ct + j < tiles_k && col < in && row < a.rows) static_cast<T *>(a.dx)[row * in + col] = (T)(s[j][e] * a.drop.keep);
                 }
             }
         }
@@ -1554,7 +1567,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int n = wave * 16 + chunk * 4 + e, k = j * 16 + at;
-            if (a.part && n < out && k < in) a.part[((int64_t)blockIdx.x * out + n) * in + k] = dw[j][e];
+            if (a.part && n < out && k < in) a.part[((int64_t)blockIdx.x * out + n) * in + k] = dw[j][e] * a.drop.keep;
         }
     float(*const sums)[9] = reinterpret_cast<float(*)[9]>(lds); // what lay there has been read
 #pragma unroll
@@ -1563,7 +1576,7 @@ template <typename T, int L> __global__ void __launch_bounds__(kNarrowT) narrow_
     for (int t = tid; t < out; t += kNarrowT) {
         float s = 0.0f;
         for (int q = 0; q < per; ++q) s += sums[q * L + t / 8][t % 8];
-        a.sums[(int64_t)blockIdx.x * out + t] = s;
+        a.sums[(int64_t)blockIdx.x * out + t] = s * a.drop.keep;
     }
 }
 
@@ -1884,7 +1897,7 @@ template <typename T> int64_t LinearOf<T>::workspace(const pcsr_linear_t &a, boo
 
 template <typename T> int LinearOf<T>::forward(const pcsr_linear_t &a, void *y, void *slope, void *ws, hipStream_t stream)
 {
-    const Tail tail = {a.bias, a.residual, y, a.act == PCSR_ACT_NONE ? nullptr : slope, a.r_stride, a.rows, a.out, a.act, a.bias_type, drop_of(&a.drop)};
+    const Tail tail = {a.bias, a.residual, y, a.act == PCSR_ACT_NONE ? nullptr : slope, a.r_stride, a.rows, a.out, a.act, a.bias_type, drop_of(&a.drop), 1.0f};
     const Side x = {a.x, a.x_stride, a.rows}, w = {a.w, a.w_stride, a.out};
     if (a.rows <= kFew) return few_rows<T>({x, w, a.in, a.in, 1, 1, 1, nullptr, tail}, stream);
     const bool direct = forward_direct<T>(a);
@@ -1914,7 +1927,7 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
             p.stretches = kNarrowBlocks;
             unsigned blocks = 0;
             FinishArgs f = {};
-            if (dw) f = finish_args(p, n.part, {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)}, &blocks);
+            if (dw) f = finish_args(p, n.part, {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr), 1.0f}, &blocks);
             const SumsArgs b = {sums, kNarrowBlocks, a.out, a.bias_type, db};
             if (dw || db) hipLaunchKernelGGL(last_kernel<T>, dim3(blocks + (db ? (unsigned)up(a.out, 16) : 0)), dim3(kT), 0, stream, FinishArgs{}, f, b, 0, (int)blocks);
             return launched();
@@ -1926,8 +1939,9 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
         hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)sp.blocks, (unsigned)up(a.out, sp.lanes * 8)), dim3(kSlopeT), 0, stream, s);
     }
     const SumsArgs b = {sums, sp.blocks, a.out, a.bias_type, db};
-    const Tail tail_x = {nullptr, nullptr, dx, nullptr, 0, a.rows, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
-    const Tail tail_w = {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr)};
+    const float times = drop_of(&a.drop).keep;
+    const Tail tail_x = {nullptr, nullptr, dx, nullptr, 0, a.rows, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr), times};
+    const Tail tail_w = {nullptr, nullptr, dw, nullptr, 0, a.out, a.in, PCSR_ACT_NONE, PCSR_F32, drop_of(nullptr), times};
     const Side &dz = pass.dz, w = {a.w, a.w_stride, a.in}, g = {dz.at, dz.ld, a.out}, x = {a.x, a.x_stride, a.in};
     int rc = launched();
     if (rc != PCSR_OK) return rc;
