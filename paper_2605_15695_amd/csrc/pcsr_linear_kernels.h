@@ -76,13 +76,23 @@ struct Tail {
     float times; // of the sums of a backward pass's product
 };
 
-// Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 of them to 1 (0 and 1 are exact, others are 2^-16 off at
-// most, a 32nd of what fp16 rounds gradients of their size by; slopes are between -0.13 and 1.13, and 0 stands for none).  Kept in place of z: a
-// slope costs three operations beside the activation and forty apart from it.
+// Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 (s + 1/4) (0 and 1 are exact, others are 2^-16 off at
+// most; slopes are between -0.13 and 1.13, so that codes end at 45,187; 0 stands for none).  Those below zero become small far out, where a row or a column may have no others:
+// from -2^-6 to -2^-45 (silu at -34) the codes from 45,312 on are their fp32 exponent and 9 bits behind it, 2^-10 off at most.  Kept in place of z: a
+// slope costs ten operations beside the activation and forty apart from it.
 template <typename T> struct Slope {
     typedef uint16_t type;
-    static __device__ __forceinline__ uint16_t put(float s) { return (uint16_t)(uint32_t)__builtin_fmaf(s, 32768.0f, 8192.5f); } // (of no number 0)
-    static __device__ __forceinline__ float take(uint16_t q) { return q ? __builtin_fmaf((float)q, 1.0f / 32768.0f, -0.25f) : __builtin_nanf(""); }
+    static constexpr uint32_t first = 0xA9000000u, binades = 39, code = 45312; // -2^-45 as fp32
+    static __device__ __forceinline__ uint16_t put(float s)
+    {
+        const uint32_t bits = __builtin_bit_cast(uint32_t, s), plain = (uint32_t)__builtin_fmaf(s, 32768.0f, 8192.5f); // (of no number 0)
+        return (uint16_t)(bits - first < binades << 23 ? bits + ((code << 14) + (1u << 13) - first) >> 14 : plain);
+    }
+    static __device__ __forceinline__ float take(uint16_t q)
+    {
+        const float small = __builtin_bit_cast(float, ((uint32_t)q << 14) + (first - (code << 14))), plain = __builtin_fmaf((float)q, 1.0f / 32768.0f, -0.25f);
+        return q >= code ? small : q ? plain : __builtin_nanf("");
+    }
 };
 template <> struct Slope<float> {
     typedef float type;

@@ -113,7 +113,7 @@ typedef struct {
 // bytes of workspace (16-byte aligned) of the calls below with the same a; backward: those for all of its results
 int64_t pcsr_linear_workspace(const pcsr_linear_t *a, int32_t backward);
 // slope: null, or [rows x out] for the backward call where act is not none: the activation's slopes, fp32 for fp32 and otherwise
-// 16 bits, 2^15 (slope + 1/4) (0: not a number).
+// 16 bits, 2^15 (slope + 1/4) (0: not a number), or, from 45312 on, of slopes between -2^-6 and -2^-45 (their bits as fp32 - 0xA9000000) / 2^14 + 45312, each rounded.
 // TOO_LARGE: rows of 2^32 and more, in or out of 2^24 and more, and more than 2^23 tiles of 64 x 64 of y, of dx or of dw.
 int pcsr_linear(const pcsr_linear_t *a, void *y, void *slope, void *ws, void *stream);
 // From dy (rows dy_stride numbers apart): dx [rows x in], dw [out x in], db [out] of bias_type; each may be null (rows of 0: nothing is written).  a->bias and a->residual are not read; a->x is for

@@ -67,3 +67,71 @@ def test_large_gradients_behind_dropout(kind, size, act, p):
                                   (grads[1], g.t() @ X.detach().double(), g.abs().t() @ X.detach().double().abs(), M)):
         err = ((n / 8 + 51) * U * size_of) * (1 + u) + u * want.abs() + 2.0 ** -24
         assert bool(((got.double() - want).abs() <= err).all())
+
+
+# Slopes as they are kept for 16-bit types: within 2^-16, and those below zero, which become small far out, within 2^-10 of themselves down to 2^-45.  Beside that an
+# activation's own arithmetic: with s = p + z q, p the share below z and z q the other term, of which roundings take up to 16 U (1 + z^2) or 16 U (1 + |z|)
+# of both; gelu's share of 16-bit types is good to 2^-14 of what it is below zero, and above zero of what is left to 1.
+def _slopes(z, act):
+    """slope and what it may be off by beside the way it is kept"""
+    U = 2.0 ** -24
+    if act == "silu":
+        p, left = torch.sigmoid(z), torch.sigmoid(-z)
+        return p * (1 + z * left), 16 * U * (1 + z.abs()) * p * (1 + z.abs() * left)
+    p, left = 0.5 * torch.erfc(-z / 2.0 ** 0.5), 0.5 * torch.erfc(z / 2.0 ** 0.5)
+    q = torch.exp(-0.5 * z * z) / (2 * torch.pi) ** 0.5
+    return p + z * q, 16 * U * (1 + z * z) * (p + z.abs() * q) + 2.0 ** -14 * torch.minimum(p, left)
+
+
+def _taken(code):
+    """16 bits as pcsr_train.h describes them"""
+    code = code.long() & 0xFFFF
+    small = (((code - 45312) << 14) + 0xA9000000) & 0xFFFFFFFF
+    small = torch.where(small >= 1 << 31, small - (1 << 32), small).int().view(torch.float32).double()
+    return torch.where(code >= 45312, small, torch.where(code == 0, torch.nan, code.double() / 32768 - 0.25))
+
+
+def _kept_within(s, own):
+    half = 2.0 ** -16 + 2.0 ** -23
+    return torch.where(s < 0, torch.minimum(torch.full_like(s, half), s.abs() * 2.0 ** -10), torch.full_like(s, half)) * (1 + 2.0 ** -12) + own * (1 + 2.0 ** -9) + 2.0 ** -45
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows", [1, 8, 20, 600, 33_000])  # few of them, tiles, weights in LDS
+def test_kept_slopes(kind, act, rows):
+    from paper_2605_15695_amd import binding as pc
+
+    N, K = 512, 32
+    lib = pc._lib()
+    X, W = torch.zeros(rows, K, device="cuda", dtype=TYPES[kind][0]), torch.zeros(N, K, device="cuda", dtype=TYPES[kind][0])
+    y = torch.empty(rows, N, device="cuda", dtype=TYPES[kind][0])
+    for lo, hi in ((-36.0, -12.0), (-12.0, -4.0), (-4.0, 0.0), (-1.3, -1.25), (-0.8, -0.7), (0.0, 8.0), (8.0, 60.0)):
+        b = torch.linspace(lo, hi, N, device="cuda")
+        code = torch.zeros(rows, N, dtype=torch.int16, device="cuda")
+        a = pc.pcsr_linear_t(rows, K, N, NUMBERS[kind], 0, {"silu": 2, "gelu": 3}[act], 0, X.data_ptr(), W.data_ptr(), b.data_ptr(), None, K, K, 0,
+                             pc.pcsr_drop_t(0.0, 0, 0, None, None))
+        ws = torch.empty(lib.pcsr_linear_workspace(ctypes.byref(a), 0) + 16, dtype=torch.uint8, device="cuda")
+        assert lib.pcsr_linear(ctypes.byref(a), y.data_ptr(), code.data_ptr(), ws.data_ptr(), torch.cuda.current_stream().cuda_stream) == pc.PCSR_OK
+        s, own = _slopes(b.double(), act)
+        far = (_taken(code) - s).abs() - _kept_within(s, own)
+        assert bool((far <= 0).all()), (lo, hi, float(far.max()))
+
+
+# units whose sums are all far below zero: their gradients are small, not none.  dz = s dy is rounded to the type (fp16: 2^-25 where it is small).
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows", [5, 300, 5000, 131_072])
+def test_gradients_of_small_slopes(kind, act, rows):
+    from paper_2605_15695_amd.linear import linear
+
+    N = 64
+    u, dtype = TYPES[kind][1], TYPES[kind][0]
+    X, W = torch.zeros(rows, N, device="cuda", dtype=dtype, requires_grad=True), torch.eye(N, device="cuda", dtype=dtype)
+    b = torch.linspace(-20.0 if act == "silu" else -6.0, -2.0, N, device="cuda").requires_grad_()
+    dy = torch.full((rows, N), 2.0 ** 15, device="cuda", dtype=dtype)
+    dx, db = torch.autograd.grad(linear(X, W, b, act), (X, b), dy)
+    s, own = _slopes(b.detach().double(), act)
+    off = _kept_within(s, own)
+    assert bool(((dx.double() - 2.0 ** 15 * s).abs() <= 2.0 ** 15 * (off * (1 + u) + 2 * u * s.abs()) + 2.0 ** -23).all())
+    assert bool(((db.double() - rows * 2.0 ** 15 * s).abs() <= rows * 2.0 ** 15 * (off + 140 * 2.0 ** -24 * s.abs())).all())
