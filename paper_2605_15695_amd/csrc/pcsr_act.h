@@ -66,7 +66,7 @@ template <int N> __device__ __forceinline__ void slopes(float (&z)[N], int act)
 }
 
 // The same share for results of 16 bits: P of degree 4, good to 2^-14 of itself, where fp16 rounds by up to 2^-11 (five operations and a
-// constant less, of nineteen).
+// constant less, of nineteen).  The slope of gelu, whose share this is, is 1.15 2^-16 off at most, at 0.
 __device__ __forceinline__ float below_normal16(float z, float bell)
 {
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.38f, fabsf(z), 1.0f));

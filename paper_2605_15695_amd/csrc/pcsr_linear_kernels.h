@@ -77,7 +77,7 @@ struct Tail {
 };
 
 // Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 (s + 1/4) (0 and 1 are exact, others are 2^-16 off at
-// most; slopes are between -0.13 and 1.13, so that codes end at 45,187; 0 stands for none).  Those below zero become small far out, where a row or a column may have no others:
+// most, gelu's up to 1.15 2^-16 more, by below_normal16; slopes are between -0.13 and 1.13, so that codes end at 45,187; 0 stands for none).  Those below zero become small far out, where a row or a column may have no others:
 // from -2^-6 to -2^-45 (silu at -34) the codes from 45,312 on are their fp32 exponent and 9 bits behind it, 2^-10 off at most.  Kept in place of z: a
 // slope costs ten operations beside the activation and forty apart from it.
 template <typename T> struct Slope {

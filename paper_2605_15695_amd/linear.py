@@ -23,7 +23,7 @@ def linear(X: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     float32.  activation: none, relu, silu or gelu (by erf).  p, seed, offset: see dropout; p = 0 drops nothing.
     Products of 16-bit numbers are summed in float32; those of float32 numbers are taken of three bf16 numbers each, 24 bits, and summed in
     float32 (where numbers of 2^31 and more are met, in float32 throughout, which is slow).  What follows is computed in float32 and rounded once.
-    The activation's slopes are kept for the backward pass, in float32 or, for 16-bit types, as 16 bits that are 2^-16 off at most and, of slopes below zero, 2^-10 of themselves; the gradient at
+    The activation's slopes are kept for the backward pass, in float32 or, for 16-bit types, as 16 bits, which are 2^-16 off at most (gelu's 2.2 2^-16, with its own arithmetic) and, of slopes below zero, 2^-10 of themselves; the gradient at
     X @ weight.T + bias, but for dropout's 1 / (1 - p), which multiplies what is summed, is rounded to X's type (in float16 infinite past 65504, which is a
     gradient of 58,000 and more where a slope is above 1; exact without an activation and with relu).
     Sums are in an order that sizes and type alone decide: the same bits on every run.

@@ -118,6 +118,22 @@ def test_kept_slopes(kind, act, rows):
         assert bool((far <= 0).all()), (lo, hi, float(far.max()))
 
 
+# In all: gelu's arithmetic for 16-bit types adds up to 1.15 2^-16 (the degree 4 share at 0, by its polynomial in 64 bits), fp32 roundings 64 U at most where slopes are not small.
+@pytest.mark.parametrize("act,most", [("relu", 0.0), ("silu", 2.0 ** -16), ("gelu", 2.15 * 2.0 ** -16)])
+def test_kept_slopes_in_all(act, most):
+    from paper_2605_15695_amd import binding as pc
+
+    N, K = 4096, 8
+    X, W = torch.zeros(1, K, device="cuda", dtype=torch.float16), torch.zeros(N, K, device="cuda", dtype=torch.float16)
+    y, code, b = torch.empty(1, N, device="cuda", dtype=torch.float16), torch.zeros(1, N, dtype=torch.int16, device="cuda"), torch.linspace(-8.0, 8.0, N, device="cuda")
+    b[N // 2] = 0.0
+    a = pc.pcsr_linear_t(1, K, N, 2, 0, {"relu": 1, "silu": 2, "gelu": 3}[act], 0, X.data_ptr(), W.data_ptr(), b.data_ptr(), None, K, K, 0, pc.pcsr_drop_t(0.0, 0, 0, None, None))
+    assert pc._lib().pcsr_linear(ctypes.byref(a), y.data_ptr(), code.data_ptr(), None, torch.cuda.current_stream().cuda_stream) == pc.PCSR_OK
+    s = (b > 0).double() if act == "relu" else _slopes(b.double(), act)[0]
+    far = (_taken(code)[0] - s).abs().max()
+    assert float(far) <= most + (64 * 2.0 ** -24 if act != "relu" else 0.0)
+
+
 # units whose sums are all far below zero: their gradients are small, not none.  dz = s dy is rounded to the type (fp16: 2^-25 where it is small).
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
