@@ -1834,6 +1834,11 @@ struct Space {
     template <typename T> static Space of(const pcsr_linear_t &a, bool own)
     {
         Space s = {};
+        if (narrow<T>(a)) { // sums alone: it keeps dz to itself
+            s.sums = round16(4 * kNarrowBlocks * a.out), s.w = round16(4 * kNarrowBlocks * a.out * a.in);
+            s.bytes = s.sums + s.w;
+            return s;
+        }
         s.ld = up(a.out, 8) * 8;
         s.lanes = 1;
         while (s.lanes < 64 && s.lanes * 8 < a.out) s.lanes *= 2;
@@ -1847,10 +1852,6 @@ struct Space {
         for (int d = 0; d < 4; ++d) {
             const Products p = Products::of<T>(a, x[d & 1], w[d >> 1], d & 1);
             s.x = p.bytes_x > s.x ? p.bytes_x : s.x, s.w = p.bytes_w > s.w ? p.bytes_w : s.w;
-        }
-        if (narrow<T>(a)) {
-            const int64_t sums = round16(4 * kNarrowBlocks * a.out), part = round16(4 * kNarrowBlocks * a.out * a.in);
-            s.sums = sums > s.sums ? sums : s.sums, s.w = part > s.w ? part : s.w;
         }
         s.bytes = s.dz + s.sums + s.x + s.w;
         return s;
@@ -1880,6 +1881,7 @@ template <typename T> int few_rows(const TileArgs &a, hipStream_t stream)
 
 // A backward call as it runs, from arguments that are checked.  at: its workspace.
 struct Pass {
+    bool one; // narrow_kernel takes it: what is below space is not used
     bool own; // dz is written; it is dy otherwise
     Space space;
     Side dz;
@@ -1890,6 +1892,7 @@ struct Pass {
         Pass p = {};
         p.own = has_slope(a);
         p.space = Space::of<T>(a, p.own);
+        if ((p.one = narrow<T>(a))) return p;
         p.dz = p.own ? Side{at, p.space.ld, a.rows} : Side{dy, dy_stride, a.rows};
         p.direct_x = straight_with<T>(p.dz, {a.w, a.w_stride, a.in}, true, a.out);
         p.direct_w = straight<T>({p.dz.at, p.dz.ld, a.out}, true, p.own) && straight<T>({a.x, a.x_stride, a.in}, true, false);
@@ -1922,7 +1925,7 @@ int LinearOf<T>::backward(const pcsr_linear_t &a, const void *slope, const void 
     const Space &sp = pass.space;
     const bool own = pass.own;
     float *sums = reinterpret_cast<float *>(at + sp.at_sums()), *part_w = reinterpret_cast<float *>(at + sp.at_w());
-    if (narrow<T>(a)) { // whatever is asked for, so that the bits do not depend on that
+    if (pass.one) { // whatever is asked for, so that the bits do not depend on that
         if constexpr (sizeof(T) == 2) {
             const NarrowArgs n = {dy, a.act == PCSR_ACT_NONE ? nullptr : slope, dw ? a.x : nullptr, dx ? a.w : nullptr, dy_stride, a.x_stride, a.w_stride, a.rows, (int)a.in, (int)a.out, dx,
                                   dw ? part_w : nullptr, sums, drop_of(&a.drop)};
@@ -1984,7 +1987,7 @@ template <typename T> void LinearOf<T>::uses(const pcsr_linear_t &a, const void 
 {
     const Pass pass = Pass::of<T>(a, dy, dy_stride, nullptr);
     const Space &sp = pass.space;
-    const bool one = narrow<T>(a);
+    const bool one = pass.one;
     const int64_t in[4][2] = {{0, pass.own && !one ? a.rows * sp.ld * (int64_t)sizeof(T) : 0},
                               {sp.at_sums(), 4 * (one ? kNarrowBlocks : sp.blocks) * a.out},
                               {sp.at_x(), one ? 0 : pass.products.bytes_x},

@@ -15,7 +15,7 @@ BAND = 16 << 20
 # What lies behind a workspace of the size that is asked for is as it was: sums of stretches are as long as the way that runs makes them, however operands lie.
 @pytest.mark.parametrize("kind", ["bf16", "fp16"])
 @pytest.mark.parametrize("size", [(12_288, 192, 192), (18_432, 128, 192), (8286, 152, 176), (22_528, 64, 320), (2048, 512, 320), (8192, 160, 160),
-                                  (16_384, 32, 768), (512, 320, 2048)], ids=lambda s: "x".join(map(str, s)))
+                                  (16_384, 32, 768), (512, 320, 2048), (131_072, 64, 256), (140_001, 8, 40)], ids=lambda s: "x".join(map(str, s)))
 def test_nothing_behind_the_workspace(kind, size):
     from paper_2605_15695_amd import binding as pc
 

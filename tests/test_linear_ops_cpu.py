@@ -132,6 +132,16 @@ def test_workspace_of_many_sizes():
                 _fits(M, K, N, kind, odd=odd, act=2 * (n % 5 == 0))
 
 
+# one read for all gradients: sums of its 256 workgroups and nothing else
+@pytest.mark.parametrize("size", [(480_000, 64, 256), (131_072, 8, 8), (2_000_000, 64, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_workspace_of_one_read(size):
+    M, K, N = size
+    for kind in (1, 2):
+        for kw in (dict(), dict(act=3), dict(p=0.5), dict(odd=(1, 1, 1))):
+            asked, parts = _fits(*size, kind, **kw)
+            assert asked == 4 * 256 * N * (K + 1) == sum(last - first for first, last in parts), (asked, parts)
+
+
 def test_uses_refuses():
     ends = (ctypes.c_int64 * 8)()
 
