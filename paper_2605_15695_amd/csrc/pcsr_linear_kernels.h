@@ -79,7 +79,7 @@ struct Tail {
 // Slopes as they are kept for the backward pass: fp32, or of 16-bit types 16 bits as well, 2^15 (s + 1/4) (0 and 1 are exact, others are 2^-16 off at
 // most, gelu's up to 1.15 2^-16 more, by below_normal16; slopes are between -0.13 and 1.13, so that codes end at 45,187; 0 stands for none).  Those below zero become small far out, where a row or a column may have no others:
 // from -2^-6 to -2^-45 (silu at -34) the codes from 45,312 on are their fp32 exponent and 9 bits behind it, 2^-10 off at most.  Kept in place of z: a
-// slope costs ten operations beside the activation and forty apart from it.
+// slope costs eight operations beside the activation, and six to take, and forty apart from it.
 template <typename T> struct Slope {
     typedef uint16_t type;
     static constexpr uint32_t first = 0xA9000000u, binades = 39, code = 45312; // -2^-45 as fp32
@@ -612,7 +612,7 @@ template <bool TP, bool TQ, typename C> constexpr int straight_bytes()
 }
 // Bound by the matrix units, which alone reach 2.4 PFLOP/s on zeros and 1.8 on random numbers here.  4096^3 in bf16: 115 us (1.2 PFLOP/s) where operands stay in caches, 126 to 135 where not,
 // matrix units 51 to 54 % busy, 256 x 256 tiles (one to a compute unit: 512 numbers of operands from LDS for 65,536 products; 128 x 128 take 131 us).  32,768 x 768 -> 1000 in
-// fp16 87 us, 36 of them what ends the tiles (gelu, dropout, slopes) with nothing beside it, and 113 in tiles of 128 x 128; its gradient of x 75 us in tiles of 128 x 128.
+// fp16 92 us, 40 of them what ends the tiles (gelu, dropout, slopes) with nothing beside it, and 113 in tiles of 128 x 128; its gradient of x 75 us in tiles of 128 x 128.
 // The next numbers are read from LDS while those before are multiplied, and a stage's loads are given out when all wavefronts have read the one
 // before it, which is half a stage before they multiply its last numbers.
 template <typename T, bool TP, bool TQ, typename C> __global__ void __launch_bounds__(C::threads, C::per) straight_kernel(TileArgs a)
@@ -1004,7 +1004,7 @@ template <typename C> __global__ void __launch_bounds__(C::threads, C::per) piec
 // are on their way to its registers while these are multiplied, nothing waits for other wavefronts, and x is read once.
 // STEPS: of 32 numbers of k.  FJ tiles of 16 columns at a time.  WHOLE: all of k is there, and of columns 8 or none.  RES: a residual is there.
 // 2,000,000 x 256 -> 64 in fp32 with a residual 614 to 624 us: 3.07 GB, 4.9 to 5.0 TB/s; matrix units are 35 % busy, vector units 43.  480,000 x 64 -> 256 in bf16 with gelu,
-// dropout and slopes 141 to 158 us: vector units are 92 % busy with what follows the product (memory would take 89).
+// dropout and slopes 157 us (141 where slopes were kept to 2^-16 alone): vector units are 98 % busy with what follows the product (memory would take 89).
 // Loads come back in their order, and so do the waits: what a strip's end needs is asked for before the next strip's numbers, and the bias lies in LDS.
 template <typename T, int STEPS> constexpr int weights_pitch() { return STEPS * 64; } // bytes of a row
 // Chunks of 16 bytes are exchanged by these bits of a row's number, so that the 16 that are read at once (place) lie in different banks.
@@ -1318,7 +1318,10 @@ struct SlopeArgs {
 constexpr int kSlopeT = 1024, kSlopeBlocks = 512; // two workgroups a compute unit: as many sums as sums_kernel adds up in 6 us
 
 // dz = act'(z) dy or 0 where it was dropped, and c times the sums of its columns over a workgroup's rows.  A thread keeps its 8 columns and walks down the rows, the next row's numbers on their way.
-// Bound by memory: 250,000 x 256 in fp32 144 us (768 MB, 5.3 TB/s; 152 without the row ahead), 32,768 x 1000 in fp16 42, 4096 x 4096 in bf16 25 (100 MB).
+// dz is rounded to T, as matrix instructions take it, which for 16-bit types makes gradients of X and W behind silu or gelu 1.41 times as inexact as their own rounding.  In two
+// pieces it would not, with products over twice as many numbers: 32,768 x 768 -> 1000 in fp16 75.7 and 81.3 us for dx and dw, twice as many numbers 135 and 127; 4096^3 in bf16
+// 123 and 127, 224 and 217.  That is 1.4 to 1.5 of a training pass, for gradients that are rounded once more anyway.
+// Bound by memory: 250,000 x 256 in fp32 144 us (768 MB, 5.3 TB/s; 152 without the row ahead), 32,768 x 1000 in fp16 43, 4096 x 4096 in bf16 26 (100 MB).
 template <typename T> __global__ void __launch_bounds__(kSlopeT) slope_kernel(SlopeArgs a)
 {
     typedef typename Slope<T>::type S;
@@ -1417,8 +1420,8 @@ template <typename T> __global__ void __launch_bounds__(kT) last_kernel(FinishAr
 // dz, dx, dw and db of 16-bit numbers from one read of dy, the slopes and x, where dw fits a workgroup's registers: up to 256 columns of dy and 64 of x.
 // A workgroup takes 64 or 128 rows at a time: dz and x go to LDS as they are, [row][column], the weights lie there turned, and dx = dz w reads dz by rows,
 // dw += dz^T x both by columns (turned by the LDS reads).  A thread keeps its 8 columns of dy, so that db is a sum of its own; when it has used a row's numbers
-// it asks for those that come next.  480,000 x 64 -> 256 in bf16, dropout: 164 us (630 MB: memory would take 102), vector units 58 % busy with the
-// generator and the slopes, LDS 32 %; all wavefronts at the same of both took 174, with one buffer too; slope_kernel and both products 285.
+// it asks for those that come next.  480,000 x 64 -> 256 in bf16, dropout: 162 to 169 us (630 MB: memory would take 102), vector units 68 % busy with the
+// generator and the slopes, LDS 34 %; all wavefronts at the same of both took 1.06 of it, with one buffer too; slope_kernel and both products 285.
 struct NarrowArgs {
     const void *dy, *slope, *x, *w; // slope: null for none
     int64_t dy_stride, x_stride, w_stride, rows;
@@ -1607,9 +1610,10 @@ template <typename T> bool straight_with(const Side &x, const Side &w, bool turn
 }
 
 // How a product of I x J numbers over K is cut: into tiles, and k into stretches, whose sums go through memory, where tiles are too few for the chip.  By what each
-// way would take, in us: a workgroup `fixed` and, for a stage, `stage` alone on a compute unit and `beside` more for each of up to `most` that run there side by
-// side; sums of stretches a launch and their bytes, twice.  The numbers are fitted to 64 products of 16 to 4096 columns over 64 to 250,000 numbers of k, in every
-// way they can be cut; what is picked takes 1.05 (16 bits, straight), 1.02 (16 bits) and 1.01 (fp32) of the best of them, at most 1.27, where
+// way's loops would take beside the other ways' (`us`): a workgroup `fixed` and, for a stage, `stage` alone on a compute unit and `beside` more for each of up to `most` that run there side by
+// side; sums of stretches a launch and their bytes, twice.  Operands that come from memory and what ends a tile are left out, so that these are no times of
+// large products: 47 and 60 for the gradients of 32,768 x 768 -> 1000 in fp16, which take 75 and 77 us.  The numbers are fitted to 64 products of 16 to 4096 columns over 64 to 250,000 numbers of k, in every
+// way they can be cut, each table to products of its own (so that tiles of 64 x 64, one kernel for 16 bits, have two prices); what is picked takes 1.05 (16 bits, straight), 1.02 (16 bits) and 1.01 (fp32) of the best of them, at most 1.27, where
 // the widest tiles that fill the chip, in as many stretches as that takes, took up to 2.8 (1024^3 in bf16: 20.8 us, now 9.4; 2048^3 39.6 and 23).
 struct Plan {
     int which; // tiling

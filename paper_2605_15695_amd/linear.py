@@ -26,7 +26,8 @@ def linear(X: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     The activation's slopes are kept for the backward pass, in float32 or, for 16-bit types, as 16 bits, which are 2^-16 off at most (gelu's 2.2 2^-16, with its own arithmetic) and, of slopes below zero, 2^-10 of themselves; the gradient at
     X @ weight.T + bias, but for dropout's 1 / (1 - p), which multiplies what is summed, is rounded to X's type (in float16 infinite past 65504, which is a
     gradient of 58,000 and more where a slope is above 1; exact without an activation and with relu).
-    Sums are in an order that sizes and type alone decide: the same bits on every run.
+    Sums are in an order that sizes, type and how the operands lie (strides, addresses of whole 16 bytes) decide: the same bits on every run, though a
+    copy that lies otherwise may give others.
     PcsrError: 2^32 rows or 2^24 columns and more, and where X, weight or the result are of more than 2^23 tiles of 64 x 64.
     There is no forward-mode derivative."""
     fast = pc.train_module()
