@@ -151,3 +151,23 @@ def test_gradients_of_small_slopes(kind, act, rows):
     off = _kept_within(s, own)
     assert bool(((dx.double() - 2.0 ** 15 * s).abs() <= 2.0 ** 15 * (off * (1 + u) + 2 * u * s.abs()) + 2.0 ** -23).all())
     assert bool(((db.double() - rows * 2.0 ** 15 * s).abs() <= rows * 2.0 ** 15 * (off + 140 * 2.0 ** -24 * s.abs())).all())
+
+
+# fp32 numbers out of the pieces' range in a backward pass: the tiles that meet them are done again as products of fp32 numbers, K roundings one after the other, and multiplied by
+# 1 / (1 - p) like the others (small tiles side by side, rows past weights in LDS, weights in planes, both operands in pieces)
+@pytest.mark.parametrize("size", [(200, 96, 70), (40_000, 24, 40), (50_000, 300, 300), (20, 3000, 40)], ids=lambda s: "x".join(map(str, s)))
+def test_range_behind_dropout(size):
+    from drop_reference import kept
+    from paper_2605_15695_amd.linear import linear
+
+    M, K, N = size
+    U, p = 2.0 ** -24, 0.25
+    X, W, dy = _normal(21, M, K), _normal(22, N, K), _normal(23, M, N)
+    W[N - 1, K - 1], X[M - 1, 0], dy[M // 2, N // 2] = 2.0 ** 60, 2.0 ** 50, -2.0 ** 40
+    k, f = kept(M, N, p, 4, 3)
+    g = torch.from_numpy(k).cuda().double() * f * dy.double()
+    X.requires_grad_(), W.requires_grad_()
+    dx, dw = torch.autograd.grad(linear(X, W, p=p, seed=4, offset=3), (X, W), dy)
+    for got, a, b, n in ((dx, g, W.detach().double(), N), (dw, g.t(), X.detach().double(), M)):
+        err = (n + 4) * U * (a.abs() @ b.abs())
+        assert bool(((got.double() - a @ b).abs() <= err + 2.0 ** -120).all())
